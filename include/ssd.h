@@ -45,7 +45,7 @@ enum ssd_status {
     SSD_EUNSUPPORTED = -5   /* dtype / feature not built                                             */
 };
 
-enum ssd_dtype { SSD_F32 = 0, SSD_BF16 = 1 };
+enum ssd_dtype { SSD_F32 = 0, SSD_BF16 = 1, SSD_F16 = 2 };   /* SSD_F16: rows of an ssd_kv_view only */
 /* Matrix-core operand type of an SSD_BF16 model (the paper's stack runs in bfloat16, Sec. 3.2).
  *   SSD_OP_F16  (default) activations are rounded to IEEE half (11 significant bits) where they enter a
  *               contraction; the bf16 weights are converted once to half times a per-tensor power of two
@@ -354,6 +354,96 @@ int accept_prefix(ssd_ctx *ctx, const void *h_verify, const int32_t *draft_ids /
                   const int32_t *cu_draft /*host*/, int Bv, float tau_slm,
                   float *draft_logp /*dev [cu_draft[Bv]]*/, int32_t *accept_len /*dev [Bv]*/,
                   uint8_t *all_accepted /*dev [Bv]*/, int32_t *greedy_tok /*dev [cu_draft[Bv]] or NULL*/);
+
+/* ---- Several continuations at once: a tree of drafted tokens over the cached rows of an utterance.
+ *
+ * Utterance b has ctx_len[b] rows in a K/V cache from slot kv_start[b] on and cu_nodes[b + 1] - cu_nodes[b] nodes, at most
+ * SSD_MAX_TREE_NODES, whose K/V rows are the slots behind them in the order of the nodes.  parent[cu_nodes[b] + i] (host) is the node that
+ * node i continues, a number of the same utterance below i, or -1 for a node that continues the context itself (several may).
+ * A node sees every cached row, its ancestors and itself.
+ *
+ * The rows of a cache, the library's own (ssd_kv_cache_view) or any other: row `slot` of K/V head h of layer l begins at element
+ * l * layer_stride + slot * slot_stride + h * head_stride of k and of v, and its head_dim elements are consecutive.  Rows must not share
+ * memory, every row begins at a multiple of 16 bytes, 64 slots are less than 2 GiB apart.  slots <= 2^31 - 1.
+ * dtype SSD_F16 or SSD_BF16: head_dim 64 or 128; SSD_F32: a multiple of 4 up to 128 (SSD_ESHAPE otherwise). */
+#define SSD_MAX_TREE_NODES 1024
+typedef struct {
+    void   *k, *v;            /* dev */
+    int64_t slots;
+    int64_t slot_stride, head_stride, layer_stride;    /* elements; layer_stride is not read for one layer */
+    int32_t n_layers, n_kv_heads, head_dim, dtype;     /* enum ssd_dtype */
+} ssd_kv_view;
+
+/* The view of a K/V cache of this context's model: of the attached one (dev_ptr NULL), or of a buffer of ssd_kv_cache_bytes(ctx, slots)
+ * bytes.  Errors: SSD_EINVAL (no model, nothing attached, slots <= 0 with a buffer). */
+int ssd_kv_cache_view(ssd_ctx *ctx, void *dev_ptr, int64_t slots, ssd_kv_view *view /*host, out*/);
+
+/* Bytes of workspace for tree_attention and tree_path calls of at most max_nodes nodes (all utterances), max_utts utterances and contexts of
+ * any length.  n_q_heads, n_kv_heads and head_dim are not read for tree_path alone (0).  A size serves all smaller calls. */
+size_t ssd_tree_workspace_bytes(const ssd_ctx *ctx, int n_q_heads, int n_kv_heads, int head_dim, int64_t max_nodes, int64_t max_utts);
+
+/* Attention of all nodes (Eq. 4 for the nodes of a tree).  Per node i and query head h (its K/V head is h / (n_q_heads / n_kv_heads)), over
+ * the rows j that the node sees:  s_j = scale q . k_j;  lse = log sum_j exp s_j;  out = sum_j exp(s_j - lse) v_j.
+ *   q      dev, row cu_nodes[b] + i begins at element (cu_nodes[b] + i) * q_stride: n_q_heads * head_dim elements of the cache's type
+ *          (q and q_stride multiples of 16 bytes)
+ *   kv     one layer (n_layers 1)
+ *   out    dev [cu_nodes[B], n_q_heads * head_dim], the cache's type, 16-byte aligned
+ *   lse    dev [cu_nodes[B], n_q_heads] fp32, or NULL
+ *   mass   dev [n_kv_heads, slots] fp32, or NULL: the weight a row collects, sum over the nodes that see it and the query heads of its K/V
+ *          head of exp(s_j - lse), is added to the entries of cached rows and stored to those of node rows (they are new); no other
+ *          entry is touched.  The slots of different utterances must then be distinct.
+ * Scores, sums and statistics are fp32; with 16-bit caches the weights that enter the second product are rounded to the cache's type.
+ * A row that a node does not see has no influence on it, whatever it holds.  An utterance without nodes is skipped, ctx_len may be 0.
+ * Calls under stream capture may be replayed.  Errors: SSD_EINVAL, SSD_ESHAPE, SSD_EUNSUPPORTED (dtype), SSD_EWORKSPACE. */
+int tree_attention(ssd_ctx *ctx, const void *q /*dev*/, int64_t q_stride, int n_q_heads, const ssd_kv_view *kv /*host*/, int B,
+                   const int32_t *kv_start /*host [B]*/, const int32_t *ctx_len /*host [B]*/, const int32_t *cu_nodes /*host [B+1]*/,
+                   const int32_t *parent /*host [cu_nodes[B]]*/, float scale, void *out, float *lse, float *mass);
+
+/* Eq. 5 and the definition of j (Sec. 2.3) for the nodes of a tree: a node passes iff node_logp > ln(tau) (fp32, as in accept_prefix; tau <= 0
+ * accepts everything), and stands iff it and all its ancestors pass.  accept_node[b] is the deepest node that stands, the lowest number
+ * among equally deep ones (callers list the better continuation first), -1 if none does; accept_len[b] the number of nodes on its path;
+ * path[cu_nodes[b] + d], d < accept_len[b], that path from the top, -1 behind it.  A NaN likelihood does not pass.
+ * Errors: SSD_EINVAL, SSD_ESHAPE, SSD_EWORKSPACE (size: ssd_tree_workspace_bytes). */
+int tree_path(ssd_ctx *ctx, const float *node_logp /*dev [cu_nodes[B]]*/, int B, const int32_t *cu_nodes /*host*/,
+              const int32_t *parent /*host*/, float tau, int32_t *accept_len /*dev [B]*/, int32_t *accept_node /*dev [B]*/,
+              int32_t *path /*dev [cu_nodes[B]]*/);
+
+/* Eviction of cached rows by the weight they have collected (mass of tree_attention).  Of the ctx_len[b] rows of utterance b every layer and
+ * K/V head keeps min(keep[b], ctx_len[b]): all if that many, else the first n_first, the last n_recent and, of the rows between, those of
+ * the largest mass (equal ones: the lowest row; NaN counts below everything).  K/V rows are copied as they are to slots out_start[b] ..
+ * of another cache in the order they had: rotated keys keep their positions, so verify_tree continues with pos0 = the length before.
+ *   mass      dev [n_layers, n_kv_heads, from->slots] fp32
+ *   mass_out  dev [n_layers, n_kv_heads, to->slots] or NULL: the kept rows' entries, moved with them
+ *   rows_out  dev int32 [n_layers, n_kv_heads, sum of kept rows] or NULL: numbers of the kept rows inside their utterance, utterances one
+ *             behind the other
+ * from and to must agree but for slots and strides and must not overlap in memory; the slots written for different utterances must be
+ * distinct.  Entries and rows behind an utterance's kept ones are left as they were.
+ * Errors: SSD_EINVAL (keep[b] < n_first + n_recent where rows go, ...), SSD_ESHAPE, SSD_EUNSUPPORTED, SSD_EWORKSPACE. */
+size_t ssd_evict_workspace_bytes(const ssd_ctx *ctx, int n_layers, int n_kv_heads, int64_t max_kept_rows, int64_t max_utts);
+int kv_evict(ssd_ctx *ctx, const ssd_kv_view *from /*host*/, const float *mass, int B, const int32_t *kv_start /*host [B]*/,
+             const int32_t *ctx_len /*host [B]*/, const int32_t *keep /*host [B]*/, int n_first, int n_recent, const ssd_kv_view *to /*host*/,
+             const int32_t *out_start /*host [B]*/, float *mass_out, int32_t *rows_out);
+
+/* The decoder pass over the nodes of B trees with the attached K/V cache (ssd_set_kv_cache; filled by verify_forward_kv, earlier trees or
+ * kv_evict): node i of utterance b is token node_ids[cu_nodes[b] + i] (dev; clamped into [0, vocab)) at position pos0[b] + its depth (0 for
+ * parent -1), its rotated key and its value go to slot kv_start[b] + ctx_len[b] + i of every layer.  pos0 (host) may be NULL: ctx_len, right
+ * unless rows have been evicted.  kv_mass: dev [n_layers, n_kv_heads, slots] or NULL, updated as by tree_attention in every layer.
+ * h_tree: dev [cu_nodes[B], d_model], the final-RMSNormed hidden row of every node in the type of verify_forward's h_verify.
+ * ctx_len[b] may be 0; the slot ranges of different utterances must be distinct.
+ * Workspace of both calls: ssd_verify_tree_workspace_bytes.  Errors as for verify_forward_kv. */
+size_t ssd_verify_tree_workspace_bytes(const ssd_ctx *ctx, int64_t max_nodes, int64_t max_utts);
+int verify_tree(ssd_ctx *ctx, const int32_t *node_ids /*dev*/, int B, const int32_t *cu_nodes /*host*/, const int32_t *parent /*host*/,
+                const int32_t *kv_start /*host*/, const int32_t *ctx_len /*host*/, const int32_t *pos0 /*host or NULL*/, float *kv_mass, void *h_tree);
+
+/* Acceptance over the trees of verify_tree.  Nodes with parent -1 are given (decided before, e.g. by greedy_tok of an earlier call) and pass;
+ * for the others node_logp[i] = log softmax(lm_head . h_tree[parent]) at node_ids[i]; node_logp of given nodes is 0.  greedy_tok[i]: the
+ * lowest-index argmax of the distribution behind node i (the given node of the next tree is greedy_tok at accept_node).  accept_len,
+ * accept_node, path as in tree_path.  With kv_start not NULL the K/V rows of the accepted path, and their entries of kv_mass if that is not NULL, are moved to
+ * the slots behind the context, kv_start[b] + ctx_len[b] + d, in every layer: the context is then accept_len[b] rows longer. */
+int accept_tree(ssd_ctx *ctx, const void *h_tree, const int32_t *node_ids /*dev*/, int B, const int32_t *cu_nodes /*host*/,
+                const int32_t *parent /*host*/, float tau_slm, const int32_t *kv_start /*host or NULL*/, const int32_t *ctx_len /*host*/,
+                float *kv_mass, float *node_logp /*dev [cu_nodes[B]]*/, int32_t *greedy_tok /*dev [cu_nodes[B]]*/,
+                int32_t *accept_len /*dev [B]*/, int32_t *accept_node /*dev [B]*/, int32_t *path /*dev [cu_nodes[B]]*/);
 
 #ifdef __cplusplus
 }

@@ -12,8 +12,9 @@ import torch
 
 _LIB_PATH = os.path.join(os.path.dirname(os.path.abspath(__file__)), "libssd.so")
 
-SSD_F32, SSD_BF16 = 0, 1
+SSD_F32, SSD_BF16, SSD_F16 = 0, 1, 2
 _DTYPE_CODE = {torch.float32: SSD_F32, torch.bfloat16: SSD_BF16}
+_KV_CODE = {torch.float32: SSD_F32, torch.bfloat16: SSD_BF16, torch.float16: SSD_F16}
 _STATUS = {0: "SSD_OK", -1: "SSD_EINVAL", -2: "SSD_ESHAPE", -3: "SSD_EWORKSPACE", -4: "SSD_EHIP",
            -5: "SSD_EUNSUPPORTED"}
 
@@ -21,7 +22,9 @@ EXPORTS = ["ssd_create", "ssd_destroy", "ssd_workspace_bytes", "ssd_set_workspac
            "ssd_profile_select", "ssd_profile_read", "ssd_measure_mfma_ceiling", "ssd_measure_hbm_read", "ctc_gate", "verify_forward", "accept_prefix",
            "verify_forward_kv", "ssd_kv_cache_bytes", "ssd_set_kv_cache", "ssd_ar_workspace_bytes", "ar_fallback",
            "ssd_gate_grid", "ssd_accept_grid", "ssd_plan_batches", "ssd_set_ctc_head", "ctc_head_gate", "ssd_device_flags",
-           "ctc_gate_noalloc", "ssd_inexact_weights", "ssd_select_unconfident", "ssd_gather_i32", "ssd_set_qformer", "qformer_pool"]
+           "ctc_gate_noalloc", "ssd_inexact_weights", "ssd_select_unconfident", "ssd_gather_i32", "ssd_set_qformer", "qformer_pool",
+           "ssd_kv_cache_view", "ssd_tree_workspace_bytes", "tree_attention", "tree_path", "ssd_evict_workspace_bytes", "kv_evict",
+           "ssd_verify_tree_workspace_bytes", "verify_tree", "accept_tree"]
 
 PROF_OFF, PROF_ALL = -2, -1
 PROF_CLASSES = ["gate", "gemm_qkv", "attention", "gemm_o", "gemm_gate_up", "gemm_down", "lmhead_accept", "other",
@@ -46,6 +49,11 @@ class WeightsC(C.Structure):
                [(n, C.POINTER(C.c_void_p)) for n in ("wq", "wk", "wv", "wo", "w_gate", "w_up", "w_down",
                                                       "norm_attn", "norm_mlp")] + \
                [("norm_final", C.c_void_p), ("lm_head", C.c_void_p)]
+
+
+class KvViewC(C.Structure):
+    _fields_ = [("k", C.c_void_p), ("v", C.c_void_p), ("slots", C.c_int64), ("slot_stride", C.c_int64), ("head_stride", C.c_int64),
+                ("layer_stride", C.c_int64), ("n_layers", C.c_int32), ("n_kv_heads", C.c_int32), ("head_dim", C.c_int32), ("dtype", C.c_int32)]
 
 
 def load_library() -> C.CDLL:
@@ -110,6 +118,24 @@ def load_library() -> C.CDLL:
     lib.qformer_pool.restype = i32
     lib.ssd_gather_i32.argtypes = [vp, vp, vp, i32, vp]
     lib.ssd_gather_i32.restype = i32
+    lib.ssd_kv_cache_view.argtypes = [vp, vp, i64, vp]
+    lib.ssd_kv_cache_view.restype = i32
+    lib.ssd_tree_workspace_bytes.argtypes = [vp, i32, i32, i32, i64, i64]
+    lib.ssd_tree_workspace_bytes.restype = C.c_size_t
+    lib.tree_attention.argtypes = [vp, vp, i64, i32, vp, i32, vp, vp, vp, vp, f32, vp, vp, vp]
+    lib.tree_attention.restype = i32
+    lib.tree_path.argtypes = [vp, vp, i32, vp, vp, f32, vp, vp, vp]
+    lib.tree_path.restype = i32
+    lib.ssd_evict_workspace_bytes.argtypes = [vp, i32, i32, i64, i64]
+    lib.ssd_evict_workspace_bytes.restype = C.c_size_t
+    lib.kv_evict.argtypes = [vp, vp, vp, i32, vp, vp, vp, i32, i32, vp, vp, vp, vp]
+    lib.kv_evict.restype = i32
+    lib.ssd_verify_tree_workspace_bytes.argtypes = [vp, i64, i64]
+    lib.ssd_verify_tree_workspace_bytes.restype = C.c_size_t
+    lib.verify_tree.argtypes = [vp, vp, i32, vp, vp, vp, vp, vp, vp, vp]
+    lib.verify_tree.restype = i32
+    lib.accept_tree.argtypes = [vp, vp, vp, i32, vp, vp, f32, vp, vp, vp, vp, vp, vp, vp, vp]
+    lib.accept_tree.restype = i32
     lib.ssd_inexact_weights.argtypes = [vp]
     lib.ssd_inexact_weights.restype = i64
     return lib
@@ -136,6 +162,33 @@ def _ptr(t: Optional[torch.Tensor]):
 
 def _host_i32(a: Sequence[int]) -> np.ndarray:
     return np.ascontiguousarray(np.asarray(a, dtype=np.int32))
+
+
+def _at(t: torch.Tensor, device) -> bool:
+    return t.device == device or (device.index is None and t.device.type == device.type)
+
+
+def _on(device, dtype, **tensors):
+    """Tensors that a call reads or writes as contiguous memory of its device: ValueError names the one that is not."""
+    for name, t in tensors.items():
+        if t is not None and (not _at(t, device) or t.dtype != dtype or not t.is_contiguous()):
+            raise ValueError(f"{name} must be a contiguous {dtype} tensor on {device}")
+
+
+def _kv_view(device, k: torch.Tensor, v: torch.Tensor) -> KvViewC:
+    """ssd_kv_view of k and v [slots, K/V heads, head_dim], or with a dimension of layers before; any strides but the last."""
+    if k.shape != v.shape or k.dim() not in (3, 4) or k.dtype != v.dtype or k.dtype not in _KV_CODE or not _at(k, device) or not _at(v, device):
+        raise ValueError(f"k and v must be alike: [layers,] slots, K/V heads, head_dim, float16, bfloat16 or float32, on {device}")
+    L, (n, H, hd) = (int(k.shape[0]) if k.dim() == 4 else 1), k.shape[-3:]
+
+    def strides(t):                                          # of dimensions of one entry: as if the rows lay close together
+        ss, hs = int(t.stride(-3)), int(t.stride(-2)) if H > 1 else int(hd)
+        if n <= 1:
+            ss = max(int(hd), hs * (int(H) - 1) + int(hd))
+        return ss, hs, int(t.stride(0)) if L > 1 else 0
+    if strides(k) != strides(v) or k.stride(-1) != 1 and hd > 1 or v.stride(-1) != 1 and hd > 1:
+        raise ValueError("k and v must have the same strides, and consecutive elements in a row")
+    return KvViewC(k.data_ptr(), v.data_ptr(), int(n), *strides(k), L, int(H), int(hd), _KV_CODE[k.dtype])
 
 
 class Context:
@@ -202,11 +255,19 @@ class Context:
     def workspace_bytes(self, max_frames=0, max_tokens=0, max_verify_rows=0, max_utts=0) -> int:
         return int(self._lib.ssd_workspace_bytes(self._h, max_frames, max_tokens, max_verify_rows, max_utts))
 
-    def reserve(self, max_frames=0, max_tokens=0, max_verify_rows=0, max_utts=0, ar_utts=0, ar_steps=0):
-        """Allocates (through torch) and hands over a workspace big enough for the given maxima."""
+    def reserve(self, max_frames=0, max_tokens=0, max_verify_rows=0, max_utts=0, ar_utts=0, ar_steps=0, tree_nodes=0, tree_utts=0,
+                tree_heads=None, evict_rows=0, evict_utts=0, evict_heads=None):
+        """Allocates (through torch) and hands over a workspace big enough for the given maxima.  tree_nodes, tree_utts: tree_path, with
+        tree_heads (query heads, K/V heads, head_dim) tree_attention, and for a context with a model verify_tree and accept_tree;
+        evict_rows (kept by all utterances), evict_utts and evict_heads (layers, K/V heads): kv_evict."""
         n = self.workspace_bytes(max_frames, max_tokens, max_verify_rows, max_utts)
         if ar_utts and ar_steps:
             n = max(n, int(self._lib.ssd_ar_workspace_bytes(self._h, ar_utts, ar_steps)))
+        if tree_utts:
+            n = max(n, int(self._lib.ssd_tree_workspace_bytes(self._h, *(tree_heads or (0, 0, 0)), tree_nodes, tree_utts)),
+                    int(self._lib.ssd_verify_tree_workspace_bytes(self._h, tree_nodes, tree_utts)))
+        if evict_utts:
+            n = max(n, int(self._lib.ssd_evict_workspace_bytes(self._h, *evict_heads, evict_rows, evict_utts)))
         if self._ws is None or self._ws.numel() < n:
             self._ws = torch.empty(n, dtype=torch.uint8, device=self.device)
             self._check(self._lib.ssd_set_workspace(self._h, _ptr(self._ws), n))
@@ -409,6 +470,128 @@ class Context:
         if out is None:
             out = torch.empty((n_steps, Br), dtype=torch.int32, device=self.device)
         self._check(self._lib.ar_fallback(self._h, Br, ks.tobytes(), cl.tobytes(), _ptr(first_tok), n_steps, _ptr(out)))
+        return out
+
+    # ---- trees of drafted tokens over cached rows ----------------------------------------------
+
+    def tree_attention(self, q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, kv_start, ctx_len, cu_nodes, parent, scale: Optional[float] = None,
+                       out: Optional[torch.Tensor] = None, mass: Optional[torch.Tensor] = None, lse: Optional[torch.Tensor] = None) -> torch.Tensor:
+        """Attention of the nodes of trees (tree_attention): q [nodes, query heads, head_dim] (any stride between nodes) over k, v [slots, K/V heads,
+        head_dim] (any strides but the last).  Returns out [nodes, query heads, head_dim]; mass [K/V heads, slots] collects the rows' weights, lse
+        [nodes, query heads] takes the log-sum-exps (both fp32, optional).  scale: 1 / sqrt(head_dim) unless given."""
+        ks, cl, cn, pa = _host_i32(kv_start), _host_i32(ctx_len), _host_i32(cu_nodes), _host_i32(parent)
+        B, view = len(cn) - 1, _kv_view(self.device, k, v)
+        N, Hq, hd = (int(x) for x in q.shape)
+        if k.dim() != 3 or q.dtype != k.dtype or not _at(q, self.device) or hd != view.head_dim or q.stride(2) != 1 or (Hq > 1 and q.stride(1) != hd):
+            raise ValueError("q must be [nodes, query heads, head_dim] in the type of k and v, the heads of a node consecutive, k and v of one layer")
+        if len(ks) != B or len(cl) != B or len(pa) != N or (B >= 0 and int(cn[-1]) != N):
+            raise ValueError("kv_start, ctx_len, cu_nodes, parent and q do not fit together")
+        if out is None:
+            out = torch.empty((N, Hq, hd), dtype=q.dtype, device=self.device)
+        _on(self.device, q.dtype, out=out)
+        _on(self.device, torch.float32, mass=mass, lse=lse)
+        if out.numel() != N * Hq * hd or (lse is not None and lse.numel() != N * Hq) or (mass is not None and mass.numel() != view.n_kv_heads * view.slots):
+            raise ValueError("out, lse or mass has the wrong size")
+        self._check(self._lib.tree_attention(self._h, q.data_ptr(), int(q.stride(0)) if N > 1 else Hq * hd, Hq, C.byref(view), B, ks.tobytes(), cl.tobytes(),
+                                             cn.tobytes(), pa.tobytes(), hd ** -0.5 if scale is None else scale, _ptr(out), _ptr(lse), _ptr(mass)))
+        return out
+
+    def tree_path(self, node_logp: torch.Tensor, cu_nodes, parent, tau: float, out: Optional[dict] = None) -> dict:
+        """Accepted path of every tree (tree_path)."""
+        cn, pa = _host_i32(cu_nodes), _host_i32(parent)
+        B, N = len(cn) - 1, len(pa)
+        _on(self.device, torch.float32, node_logp=node_logp)
+        if node_logp.numel() != N or int(cn[-1]) != N:
+            raise ValueError("cu_nodes, parent and node_logp do not fit together")
+        if out is None:
+            out = {"accept_len": torch.empty(max(B, 0), dtype=torch.int32, device=self.device),
+                   "accept_node": torch.empty(max(B, 0), dtype=torch.int32, device=self.device),
+                   "path": torch.empty(N, dtype=torch.int32, device=self.device)}
+        self._check(self._lib.tree_path(self._h, _ptr(node_logp), B, cn.tobytes(), pa.tobytes(), tau, _ptr(out["accept_len"]),
+                                        _ptr(out["accept_node"]), _ptr(out["path"])))
+        return out
+
+    def kv_evict(self, k: torch.Tensor, v: torch.Tensor, mass: torch.Tensor, kv_start, ctx_len, keep, n_first: int, n_recent: int,
+                 k_out: torch.Tensor, v_out: torch.Tensor, out_start, mass_out: Optional[torch.Tensor] = None,
+                 want_rows: bool = False) -> Optional[torch.Tensor]:
+        """Copies the rows of largest weight to another cache (kv_evict): k, v [layers, slots, K/V heads, head_dim], mass [layers, K/V heads, slots].
+        Returns the numbers of the kept rows [layers, K/V heads, kept rows] if they are wanted."""
+        ks, cl, kp, os_ = _host_i32(kv_start), _host_i32(ctx_len), _host_i32(keep), _host_i32(out_start)
+        view, to = _kv_view(self.device, k, v), _kv_view(self.device, k_out, v_out)
+        lh = view.n_layers * view.n_kv_heads
+        if not len(ks) == len(cl) == len(kp) == len(os_):
+            raise ValueError("kv_start, ctx_len, keep and out_start must be of one length")
+        _on(self.device, torch.float32, mass=mass, mass_out=mass_out)
+        if mass.numel() != lh * view.slots or (mass_out is not None and mass_out.numel() != lh * to.slots):
+            raise ValueError("mass or mass_out has the wrong size")
+        rows = None
+        if want_rows:
+            rows = torch.empty((view.n_layers, view.n_kv_heads, int(np.minimum(kp, cl).clip(0).sum())), dtype=torch.int32, device=self.device)
+        self._check(self._lib.kv_evict(self._h, C.byref(view), _ptr(mass), len(ks), ks.tobytes(), cl.tobytes(), kp.tobytes(), n_first, n_recent,
+                                       C.byref(to), os_.tobytes(), _ptr(mass_out), _ptr(rows)))
+        return rows
+
+    def kv_tensors(self, buf: Optional[torch.Tensor] = None, slots: int = 0):
+        """(k, v) [layers, slots, K/V heads, head_dim] of the attached K/V cache, or of a uint8 tensor laid out for `slots` slots (ssd_kv_cache_view)."""
+        view = KvViewC()
+        self._check(self._lib.ssd_kv_cache_view(self._h, _ptr(buf), slots, C.byref(view)))
+        flat = (self._kv if buf is None else buf).view(self.act_dtype)
+        shape = (view.n_layers, view.slots, view.n_kv_heads, view.head_dim)
+        stride = (view.layer_stride, view.slot_stride, view.head_stride, 1)
+        return tuple(flat.as_strided(shape, stride, flat.storage_offset() + (p - flat.data_ptr()) // flat.element_size()) for p in (view.k, view.v))
+
+    def kv_cache_bytes(self, slots: int) -> int:
+        return int(self._lib.ssd_kv_cache_bytes(self._h, slots))
+
+    def attach_kv_cache(self, buf: torch.Tensor, slots: int):
+        """Attaches a uint8 tensor of kv_cache_bytes(slots) bytes as K/V cache."""
+        self._check(self._lib.ssd_set_kv_cache(self._h, _ptr(buf), buf.numel(), slots))
+        self._kv = buf
+
+    def verify_tree(self, node_ids: torch.Tensor, cu_nodes, parent, kv_start, ctx_len, pos0=None, kv_mass: Optional[torch.Tensor] = None,
+                    out: Optional[torch.Tensor] = None) -> torch.Tensor:
+        """The decoder pass over the nodes of trees with the attached K/V cache (verify_tree); returns h_tree."""
+        cn, pa, ks, cl = _host_i32(cu_nodes), _host_i32(parent), _host_i32(kv_start), _host_i32(ctx_len)
+        p0 = None if pos0 is None else _host_i32(pos0)
+        B, N = len(cn) - 1, len(pa)
+        _on(self.device, torch.int32, node_ids=node_ids)
+        _on(self.device, torch.float32, kv_mass=kv_mass)
+        if int(cn[-1]) != N or node_ids.numel() != N or len(ks) != B or len(cl) != B or (p0 is not None and len(p0) != B):
+            raise ValueError("cu_nodes, parent, node_ids, kv_start, ctx_len and pos0 do not fit together")
+        self._check_kv_mass(kv_mass)
+        if out is None:
+            out = torch.empty((N, self.cfg.d_model), dtype=self.act_dtype, device=self.device)
+        self._check(self._lib.verify_tree(self._h, _ptr(node_ids), B, cn.tobytes(), pa.tobytes(), ks.tobytes(), cl.tobytes(),
+                                          None if p0 is None else p0.tobytes(), _ptr(kv_mass), _ptr(out)))
+        return out
+
+    def _check_kv_mass(self, kv_mass):
+        if kv_mass is None:
+            return
+        view = KvViewC()
+        self._check(self._lib.ssd_kv_cache_view(self._h, None, 0, C.byref(view)))
+        if kv_mass.numel() != view.n_layers * view.n_kv_heads * view.slots:
+            raise ValueError("kv_mass must be [layers, K/V heads, slots of the attached cache]")
+
+    def accept_tree(self, h_tree: torch.Tensor, node_ids: torch.Tensor, cu_nodes, parent, tau_slm: float, kv_start=None, ctx_len=None,
+                    kv_mass: Optional[torch.Tensor] = None) -> dict:
+        """Acceptance over the trees of verify_tree (accept_tree); with kv_start the accepted rows move behind the context."""
+        cn, pa = _host_i32(cu_nodes), _host_i32(parent)
+        ks, cl = (None, None) if kv_start is None else (_host_i32(kv_start), _host_i32(ctx_len))
+        B, N, dev = len(cn) - 1, len(pa), self.device
+        _on(dev, torch.int32, node_ids=node_ids)
+        _on(dev, self.act_dtype, h_tree=h_tree)
+        _on(dev, torch.float32, kv_mass=kv_mass)
+        if int(cn[-1]) != N or node_ids.numel() != N or h_tree.numel() != N * self.cfg.d_model or (ks is not None and not len(ks) == len(cl) == B):
+            raise ValueError("cu_nodes, parent, node_ids, h_tree, kv_start and ctx_len do not fit together")
+        if ks is not None:
+            self._check_kv_mass(kv_mass)
+        out = {"node_logp": torch.empty(N, dtype=torch.float32, device=dev), "greedy_tok": torch.empty(N, dtype=torch.int32, device=dev),
+               "accept_len": torch.empty(max(B, 0), dtype=torch.int32, device=dev), "accept_node": torch.empty(max(B, 0), dtype=torch.int32, device=dev),
+               "path": torch.empty(N, dtype=torch.int32, device=dev)}
+        self._check(self._lib.accept_tree(self._h, _ptr(h_tree), _ptr(node_ids), B, cn.tobytes(), pa.tobytes(), tau_slm, None if ks is None else ks.tobytes(),
+                                          None if cl is None else cl.tobytes(), _ptr(kv_mass) if ks is not None else None, _ptr(out["node_logp"]),
+                                          _ptr(out["greedy_tok"]), _ptr(out["accept_len"]), _ptr(out["accept_node"]), _ptr(out["path"])))
         return out
 
     def accept_prefix(self, h_verify: torch.Tensor, draft_ids: torch.Tensor, cu_draft, tau_slm: float,

@@ -7,6 +7,7 @@
 #include <algorithm>
 
 #include "ssd_internal.h"
+#include "tree.h"
 
 using namespace ssd;
 
@@ -78,6 +79,7 @@ struct Profiler {
 
 struct ssd_ctx {
     hipStream_t stream = nullptr;
+    int device = -1;                         // current when the context was made
     bool has_model = false;
     bool bf16_ops = false;                   // matrix-core operand type of a 16-bit model: bfloat16 instead of IEEE half
     ssd_model_cfg cfg{};
@@ -336,6 +338,7 @@ int ssd_create(ssd_ctx** out, const ssd_model_cfg* cfg, const ssd_weights* w, vo
     if ((cfg == nullptr) != (w == nullptr)) return SSD_EINVAL;
     ssd_ctx* c = new ssd_ctx();
     c->stream = static_cast<hipStream_t>(hip_stream);
+    if (hipGetDevice(&c->device) != hipSuccess) { c->device = -1; (void)hipGetLastError(); }
     if (!cfg) {
         alloc_gate_counters(c);
         *out = c;
@@ -1314,6 +1317,608 @@ int accept_prefix(ssd_ctx* ctx, const void* h_verify, const int32_t* draft_ids, 
     const float ln_tau = tau_slm > 0.f ? (float)log((double)tau_slm) : -INFINITY;
     if (as_args) launch_accept_scan_host(draft_logp, cu_draft, Bv, ln_tau, accept_len, all_accepted, st);
     else launch_accept_scan(draft_logp, cu_dev, Bv, ln_tau, accept_len, all_accepted, st);
+    HIP_TRY(ctx, hipGetLastError());
+    return SSD_OK;
+}
+
+}  // extern "C"
+
+// ---- trees of drafted tokens -----------------------------------------------------------------------------------------------------
+
+namespace {
+
+// The context's device is the current one while a call lasts.
+struct OnDevice {
+    int before = -1;
+    explicit OnDevice(const ssd_ctx* c) {
+        int d;
+        if (c->device >= 0 && hipGetDevice(&d) == hipSuccess && d != c->device && hipSetDevice(c->device) == hipSuccess) before = d;
+    }
+    ~OnDevice() { if (before >= 0) (void)hipSetDevice(before); }
+};
+
+size_t kv_elem(int dtype) { return dtype == SSD_F32 ? 4 : 2; }
+
+// Rows of the caller's arrays as the kernels need them; `what` names the call in messages.
+int check_view(ssd_ctx* c, const char* what, const ssd_kv_view* v) {
+    if (!v || !v->k || !v->v) return fail(c, SSD_EINVAL, "%s: NULL cache", what);
+    if (v->dtype != SSD_F32 && v->dtype != SSD_BF16 && v->dtype != SSD_F16) return fail(c, SSD_EUNSUPPORTED, "%s: dtype %d", what, v->dtype);
+    if (v->slots <= 0 || v->slots > 0x7fffffff || v->n_layers <= 0 || v->n_kv_heads <= 0 || v->head_dim <= 0)
+        return fail(c, SSD_EINVAL, "%s: non-positive size of a cache, or more than 2^31 - 1 slots", what);
+    if (v->n_kv_heads > 65535 || (int64_t)v->n_layers * v->n_kv_heads > 65535) return fail(c, SSD_ESHAPE, "%s: more than 65535 layers times K/V heads", what);
+    const bool f32 = v->dtype == SSD_F32;
+    if (f32 ? v->head_dim % 4 || v->head_dim > 128 : v->head_dim != 64 && v->head_dim != 128)
+        return fail(c, SSD_ESHAPE, "%s: head_dim %d (64 or 128 for 16-bit rows, a multiple of 4 up to 128 for fp32)", what, v->head_dim);
+    const int64_t hd = v->head_dim, H = v->n_kv_heads, L = v->n_layers, unit = 16 / (int64_t)kv_elem(v->dtype);
+    const int64_t ss = v->slot_stride, hs = v->head_stride, ls = L > 1 ? v->layer_stride : 0;
+    if (((uintptr_t)v->k | (uintptr_t)v->v) & 15 || ss % unit || hs % unit || ls % unit)
+        return fail(c, SSD_EINVAL, "%s: rows of a cache must begin at multiples of 16 bytes", what);
+    // slots inside a head or heads inside a slot; then layers
+    const int64_t top = (int64_t)1 << 46;
+    if (ss < hd || ss > top || hs > top || ls > top || (H > 1 && hs < hd)) return fail(c, SSD_EINVAL, "%s: strides of a cache", what);
+    const bool heads_inside = H == 1 || hs * (H - 1) + hd <= ss;
+    if (!heads_inside && hs / ss < v->slots - 1) return fail(c, SSD_EINVAL, "%s: rows of a cache share memory", what);
+    if (!heads_inside && hs < (v->slots - 1) * ss + hd) return fail(c, SSD_EINVAL, "%s: rows of a cache share memory", what);
+    if (ss * (int64_t)kv_elem(v->dtype) >= (int64_t)1 << 25) return fail(c, SSD_ESHAPE, "%s: 64 slots of a cache are 2 GiB apart or more", what);
+    const int64_t layer = (H - 1) * hs + (v->slots - 1) * ss + hd;
+    if (L > 1 && ls < layer) return fail(c, SSD_EINVAL, "%s: layers of a cache share memory", what);
+    return SSD_OK;
+}
+
+bool ranges_distinct(int B, const int32_t* start, const std::vector<int64_t>& len) {
+    std::vector<int> order(B);
+    for (int b = 0; b < B; ++b) order[b] = b;
+    std::sort(order.begin(), order.end(), [&](int a, int b) { return start[a] < start[b]; });
+    int64_t end = 0;
+    for (int b : order) {
+        if (!len[b]) continue;
+        if (start[b] < end) return false;
+        end = start[b] + len[b];
+    }
+    return true;
+}
+
+// cu_nodes and parent; most: nodes of the largest utterance
+int check_trees(ssd_ctx* c, const char* what, int B, const int32_t* cu_nodes, const int32_t* parent, int& most) {
+    if (!cu_nodes) return fail(c, SSD_EINVAL, "%s: NULL cu_nodes", what);
+    if (B <= 0) return fail(c, SSD_EINVAL, "%s: B must be positive (got %d)", what, B);
+    if (!check_cu(cu_nodes, B, false)) return fail(c, SSD_EINVAL, "%s: cu_nodes must start at 0 and be non-decreasing", what);
+    if (cu_nodes[B] && !parent) return fail(c, SSD_EINVAL, "%s: NULL parent", what);
+    most = 0;
+    for (int b = 0; b < B; ++b) {
+        const int32_t* p = parent + cu_nodes[b];
+        const int n = cu_nodes[b + 1] - cu_nodes[b];
+        most = std::max(most, n);
+        if (n > MAX_TREE_NODES) return fail(c, SSD_ESHAPE, "%s: utterance %d has %d nodes, at most %d", what, b, n, MAX_TREE_NODES);
+        int bad = 0;
+        for (int i = 0; i < n; ++i) bad |= (p[i] < -1) | (p[i] >= i);
+        if (bad) return fail(c, SSD_EINVAL, "%s: a parent of utterance %d is not a node before its child, nor -1", what, b);
+    }
+    return SSD_OK;
+}
+
+int check_places(ssd_ctx* c, const char* what, int B, const int32_t* kv_start, const int32_t* ctx_len, const int32_t* cu_nodes, int64_t slots, bool distinct) {
+    if (!kv_start || !ctx_len) return fail(c, SSD_EINVAL, "%s: NULL kv_start or ctx_len", what);
+    std::vector<int64_t> len(B);
+    for (int b = 0; b < B; ++b) {
+        const int n = cu_nodes ? cu_nodes[b + 1] - cu_nodes[b] : 0;
+        if (ctx_len[b] < 0 || kv_start[b] < 0 || (int64_t)kv_start[b] + ctx_len[b] + n > slots)
+            return fail(c, SSD_EINVAL, "%s: utterance %d does not fit the K/V cache (start %d, %d rows and %d nodes, %lld slots)", what, b, kv_start[b],
+                        ctx_len[b], n, (long long)slots);
+        len[b] = (int64_t)ctx_len[b] + n;
+    }
+    if (distinct && !ranges_distinct(B, kv_start, len)) return fail(c, SSD_EINVAL, "%s: utterances share slots of the K/V cache", what);
+    return SSD_OK;
+}
+
+// Host metadata of a call to its place in the workspace: as arguments of a launch where they are few, and in pieces of that size under
+// capture (the staging buffers of an upload would be read again by every replay); else one upload.
+int place_meta(ssd_ctx* c, const std::vector<uint32_t>& meta, void* dev) {
+    if (meta.size() > MetaWords::WORDS && !capturing(c->stream)) return upload(c, meta.data(), dev, meta.size() * 4);
+    for (size_t at = 0; at < meta.size(); at += MetaWords::WORDS) {
+        MetaWords w;
+        w.n = (int)std::min<size_t>(MetaWords::WORDS, meta.size() - at);
+        memcpy(w.word, meta.data() + at, (size_t)w.n * 4);
+        launch_write_words(w, static_cast<uint32_t*>(dev) + at, c->stream);
+    }
+    return SSD_OK;
+}
+
+struct TreeWork {
+    int tile_rows;
+    std::vector<TreeItem> items, mass_items;
+};
+// Nodes in depth-first order: a node's place, the end of its subtree.
+void tree_spans(int n, const int32_t* parent, uint32_t* span) {
+    int size[MAX_TREE_NODES], next[MAX_TREE_NODES], roots = 0;
+    for (int i = 0; i < n; ++i) size[i] = 1;
+    for (int i = n - 1; i >= 0; --i)
+        if (parent[i] >= 0) size[parent[i]] += size[i];
+    for (int i = 0; i < n; ++i) {
+        int& from = parent[i] < 0 ? roots : next[parent[i]];
+        const int at = from;
+        from += size[i];
+        next[i] = at + 1;
+        span[i] = (uint32_t)at | (uint32_t)(at + size[i]) << 16;
+    }
+}
+void tree_work(int B, const int32_t* kv_start, const int32_t* ctx_len, const int32_t* cu_nodes, int G, bool mass, TreeWork& w) {
+    w.tile_rows = TREE_ROWS;
+    int64_t total = 0;
+    for (int b = 0; b < B; ++b) total += cu_nodes[b + 1] > cu_nodes[b] ? ctx_len[b] + cu_nodes[b + 1] - cu_nodes[b] : 0;
+    const int step = (int)align_up((size_t)std::max<int64_t>(1, (total + TREE_MAX_PARTS - 1) / TREE_MAX_PARTS), TREE_MASS_KEYS);
+    for (int b = 0; b < B; ++b) {
+        const int n = cu_nodes[b + 1] - cu_nodes[b], keys = ctx_len[b] + n;
+        for (int r = 0; r < n * G; r += w.tile_rows) w.items.push_back(TreeItem{kv_start[b], ctx_len[b], n, cu_nodes[b], r, 0, keys, -1});
+        for (int64_t k = 0; mass && n && k < keys; k += step)
+            w.mass_items.push_back(TreeItem{kv_start[b], ctx_len[b], n, cu_nodes[b], 0, (int)k, (int)std::min<int64_t>(keys, k + step), -1});
+    }
+}
+struct TreePlan { size_t spans, items, mass_items, meta_bytes, lse, total; };
+TreePlan plan_tree(int64_t nodes, int64_t n_items, int64_t n_mass_items, int64_t lse_values) {
+    TreePlan p;
+    size_t o = 0;
+    p.spans = o; o = align_up(o + (size_t)nodes * 4);
+    p.items = o; o = align_up(o + (size_t)n_items * sizeof(TreeItem));
+    p.mass_items = o; o = align_up(o + (size_t)n_mass_items * sizeof(TreeItem));
+    p.meta_bytes = o;
+    p.lse = o; o = align_up(o + (size_t)lse_values * 4);
+    p.total = o;
+    return p;
+}
+
+// The same bytes for all trees of at most max_nodes nodes: an item holds at least one row, and what is split is bounded.
+size_t max_tree_bytes(int n_q_heads, int n_kv_heads, int head_dim, int64_t max_nodes, int64_t max_utts) {
+    (void)head_dim;
+    const int64_t G = n_kv_heads > 0 ? (n_q_heads + n_kv_heads - 1) / n_kv_heads : 1;
+    return plan_tree(max_nodes, max_nodes * G, max_utts + TREE_MAX_PARTS, max_nodes * n_q_heads).total;
+}
+void tree_meta(const TreePlan& p, const TreeWork& w, int B, const int32_t* cu_nodes, const int32_t* parent, uint32_t* meta) {
+    for (int b = 0; b < B; ++b) tree_spans(cu_nodes[b + 1] - cu_nodes[b], parent + cu_nodes[b], meta + p.spans / 4 + cu_nodes[b]);
+    memcpy(meta + p.items / 4, w.items.data(), w.items.size() * sizeof(TreeItem));
+    memcpy(meta + p.mass_items / 4, w.mass_items.data(), w.mass_items.size() * sizeof(TreeItem));
+}
+TreeAttnArgs tree_args(const TreePlan& p, const TreeWork& w, char* ws, const ssd_kv_view& kv, const void* q, int64_t q_stride, int n_q_heads, float scale,
+                       void* out, float* lse, float* mass) {
+    TreeAttnArgs a;
+    a.q = q; a.q_stride = q_stride;
+    a.k = kv.k; a.v = kv.v; a.slot_stride = kv.slot_stride; a.head_stride = kv.n_kv_heads > 1 ? kv.head_stride : 0;
+    a.n_q_heads = n_q_heads; a.n_kv_heads = kv.n_kv_heads; a.head_dim = kv.head_dim; a.dtype = kv.dtype;
+    a.scale = scale;
+    a.out = out;
+    a.lse = lse ? lse : mass ? reinterpret_cast<float*>(ws + p.lse) : nullptr;
+    a.mass = mass; a.mass_stride = kv.slots;
+    a.items = reinterpret_cast<const TreeItem*>(ws + p.items); a.n_items = (int)w.items.size();
+    a.mass_items = reinterpret_cast<const TreeItem*>(ws + p.mass_items); a.n_mass_items = (int)w.mass_items.size();
+    a.spans = reinterpret_cast<const uint32_t*>(ws + p.spans);
+    return a;
+}
+
+struct PathPlan { size_t parent, meta_bytes; };
+PathPlan plan_path(int64_t nodes, int64_t utts) {
+    PathPlan p;
+    p.parent = align_up((size_t)(utts + 1) * 4);
+    p.meta_bytes = p.parent + align_up((size_t)nodes * 2);
+    return p;
+}
+void path_meta(const PathPlan& p, int B, const int32_t* cu_nodes, const int32_t* parent, uint32_t* meta) {
+    memcpy(meta, cu_nodes, (size_t)(B + 1) * 4);
+    int16_t* up = reinterpret_cast<int16_t*>(reinterpret_cast<char*>(meta) + p.parent);
+    for (int i = 0; i < cu_nodes[B]; ++i) up[i] = (int16_t)parent[i];
+}
+float ln_of(float tau) { return tau > 0.f ? (float)log((double)tau) : -INFINITY; }
+
+// memory that the K rows or the V rows of a view lie in
+struct Extent { uintptr_t a, z; };
+Extent extent_of(const ssd_kv_view& v, const void* p) {
+    const int64_t n = (v.n_layers > 1 ? (v.n_layers - 1) * v.layer_stride : 0) + (v.n_kv_heads - 1) * v.head_stride + (v.slots - 1) * v.slot_stride + v.head_dim;
+    return Extent{(uintptr_t)p, (uintptr_t)p + (uintptr_t)n * kv_elem(v.dtype)};
+}
+bool overlap(const Extent& a, const Extent& b) { return a.a < b.z && b.a < a.z; }
+
+struct EvictPlan { size_t utts, rows, total; };
+EvictPlan plan_evict(int64_t layers_heads, int64_t kept, int64_t utts) {
+    EvictPlan p;
+    size_t o = 0;
+    p.utts = o; o = align_up(o + (size_t)utts * sizeof(EvictUtt));
+    p.rows = o; o = align_up(o + (size_t)(layers_heads * kept) * 4);
+    p.total = o;
+    return p;
+}
+
+ssd_kv_view model_view(const ssd_model_cfg& m, bool bf16_ops, void* dev, int64_t slots) {
+    const int64_t row = (int64_t)m.n_kv_heads * m.head_dim;
+    ssd_kv_view v;
+    v.k = dev;
+    v.v = static_cast<char*>(dev) + kv_layer_bytes(m, slots);
+    v.slots = slots;
+    v.slot_stride = row; v.head_stride = m.head_dim; v.layer_stride = 2 * slots * row;
+    v.n_layers = m.n_layers; v.n_kv_heads = m.n_kv_heads; v.head_dim = m.head_dim;
+    v.dtype = m.dtype == SSD_F32 ? SSD_F32 : bf16_ops ? SSD_BF16 : SSD_F16;
+    return v;
+}
+
+struct VerifyTreePlan {
+    size_t row_src, pos, row_slot, tree, meta_bytes;
+    size_t lse, x, a, qkv, attn, h, partials, rope_rows, total;
+};
+VerifyTreePlan plan_verify_tree(const ssd_model_cfg& c, int64_t N, const TreePlan& t) {
+    VerifyTreePlan p;
+    const size_t es = elem_size(c.dtype);
+    const int64_t d = c.d_model, dq = (int64_t)c.n_q_heads * c.head_dim, dkv = (int64_t)c.n_kv_heads * c.head_dim;
+    size_t o = 0;
+    p.row_src = o; o = align_up(o + (size_t)N * 4);
+    p.pos = o; o = align_up(o + (size_t)N * 4);
+    p.row_slot = o; o = align_up(o + (size_t)N * 4);
+    p.tree = o;
+    p.meta_bytes = o + t.meta_bytes;
+    o += t.total;
+    p.x = o; o = align_up(o + (size_t)(N * d) * 4);
+    p.a = o; o = align_up(o + (size_t)(N * d) * es);
+    p.qkv = o; o = align_up(o + (size_t)(N * (dq + 2 * dkv)) * es);
+    p.attn = o; o = align_up(o + (size_t)(N * dq) * es);
+    p.h = o; o = align_up(o + (size_t)(N * c.d_ff) * es);
+    p.partials = o; if (c.dtype == SSD_BF16) o = align_up(o + (size_t)residual_partial_floats(N, d) * 4);
+    p.rope_rows = o; if (c.dtype == SSD_BF16) o = align_up(o + (size_t)N * 64 * sizeof(float2));
+    p.total = o;
+    return p;
+}
+
+struct AcceptTreePlan {
+    size_t row, target, row_of, path, meta_bytes;
+    size_t h, tgt_ids, logp, greedy, part_ms, tgt, part_arg, total;
+};
+AcceptTreePlan plan_accept_tree(const ssd_model_cfg& c, int64_t N, int64_t rows, int64_t utts) {
+    AcceptTreePlan p;
+    const int64_t g = head_groups(c);
+    size_t o = 0;
+    p.row = o; o = align_up(o + (size_t)rows * 4);
+    p.target = o; o = align_up(o + (size_t)rows * 4);
+    p.row_of = o; o = align_up(o + (size_t)N * 4);
+    p.path = o; o += plan_path(N, utts).meta_bytes;
+    o = align_up(o + (size_t)utts * 8);                      // kv_start, ctx_len
+    p.meta_bytes = o;
+    p.h = o; o = align_up(o + (size_t)(rows * c.d_model) * elem_size(c.dtype));
+    p.tgt_ids = o; o = align_up(o + (size_t)rows * 4);
+    p.logp = o; o = align_up(o + (size_t)rows * 4);
+    p.greedy = o; o = align_up(o + (size_t)rows * 4);
+    p.part_ms = o; o = align_up(o + (size_t)(g * rows) * sizeof(float2));
+    p.tgt = o; o = align_up(o + (size_t)rows * 4);
+    p.part_arg = o; o = align_up(o + (size_t)(g * rows) * sizeof(int2));
+    p.total = o;
+    return p;
+}
+
+}  // namespace
+
+extern "C" {
+
+int ssd_kv_cache_view(ssd_ctx* ctx, void* dev_ptr, int64_t slots, ssd_kv_view* view) {
+    if (!ctx || !view) return SSD_EINVAL;
+    if (!ctx->has_model) return fail(ctx, SSD_EINVAL, "ssd_kv_cache_view: context was created without a model");
+    if (dev_ptr ? slots <= 0 : !ctx->kv) return fail(ctx, SSD_EINVAL, "ssd_kv_cache_view: no slots, or no K/V cache set");
+    *view = model_view(ctx->cfg, ctx->bf16_ops, dev_ptr ? dev_ptr : ctx->kv, dev_ptr ? slots : ctx->kv_slots);
+    return SSD_OK;
+}
+
+size_t ssd_tree_workspace_bytes(const ssd_ctx* ctx, int n_q_heads, int n_kv_heads, int head_dim, int64_t max_nodes, int64_t max_utts) {
+    if (!ctx || n_q_heads < 0 || n_kv_heads < 0 || head_dim < 0 || max_nodes < 0 || max_utts < 0) return 0;
+    size_t need = plan_path(max_nodes, max_utts).meta_bytes;
+    if (n_kv_heads > 0) need = std::max(need, max_tree_bytes(n_q_heads, n_kv_heads, head_dim, max_nodes, max_utts));
+    return need + 256;
+}
+
+int tree_attention(ssd_ctx* ctx, const void* q, int64_t q_stride, int n_q_heads, const ssd_kv_view* kv, int B, const int32_t* kv_start,
+                   const int32_t* ctx_len, const int32_t* cu_nodes, const int32_t* parent, float scale, void* out, float* lse, float* mass) {
+    if (!ctx) return SSD_EINVAL;
+    const OnDevice on(ctx);
+    int most, rc = check_view(ctx, "tree_attention", kv);
+    if (rc == SSD_OK) rc = check_trees(ctx, "tree_attention", B, cu_nodes, parent, most);
+    if (rc == SSD_OK) rc = check_places(ctx, "tree_attention", B, kv_start, ctx_len, cu_nodes, kv->slots, mass != nullptr);
+    if (rc != SSD_OK) return rc;
+    const int64_t N = cu_nodes[B], dq = (int64_t)n_q_heads * kv->head_dim, es = (int64_t)kv_elem(kv->dtype);
+    if (kv->n_layers != 1) return fail(ctx, SSD_EINVAL, "tree_attention: a cache of one layer is needed (got %d)", kv->n_layers);
+    if (n_q_heads <= 0 || n_q_heads % kv->n_kv_heads) return fail(ctx, SSD_ESHAPE, "tree_attention: n_q_heads must be a multiple of n_kv_heads");
+    if (n_q_heads > 65535) return fail(ctx, SSD_ESHAPE, "tree_attention: more than 65535 query heads");
+    if (!std::isfinite(scale)) return fail(ctx, SSD_EINVAL, "tree_attention: scale is not finite");
+    if (N == 0) return SSD_OK;
+    if (!q || !out) return fail(ctx, SSD_EINVAL, "tree_attention: NULL data pointer");
+    if (q_stride < dq || q_stride > (int64_t)1 << 40 || q_stride * es % 16 || ((uintptr_t)q | (uintptr_t)out) & 15)
+        return fail(ctx, SSD_EINVAL, "tree_attention: rows of q and out must begin at multiples of 16 bytes, q_stride be at least n_q_heads * head_dim");
+    TreeWork w;
+    tree_work(B, kv_start, ctx_len, cu_nodes, n_q_heads / kv->n_kv_heads, mass != nullptr, w);
+    const TreePlan p = plan_tree(N, w.items.size(), w.mass_items.size(), mass && !lse ? N * n_q_heads : 0);
+    if (!ctx->ws || ctx->ws_bytes < p.total)
+        return fail(ctx, SSD_EWORKSPACE, "tree_attention: workspace of %zu bytes needed, %zu set", p.total, ctx->ws_bytes);
+    std::vector<uint32_t> meta(p.meta_bytes / 4);
+    tree_meta(p, w, B, cu_nodes, parent, meta.data());
+    rc = place_meta(ctx, meta, ctx->ws);
+    if (rc != SSD_OK) return rc;
+    {
+        ProfScope ps(ctx, SSD_PROF_ATTN);
+        launch_tree_attention(tree_args(p, w, static_cast<char*>(ctx->ws), *kv, q, q_stride, n_q_heads, scale, out, lse, mass), ctx->stream);
+    }
+    HIP_TRY(ctx, hipGetLastError());
+    return SSD_OK;
+}
+
+int tree_path(ssd_ctx* ctx, const float* node_logp, int B, const int32_t* cu_nodes, const int32_t* parent, float tau, int32_t* accept_len,
+              int32_t* accept_node, int32_t* path) {
+    if (!ctx) return SSD_EINVAL;
+    const OnDevice on(ctx);
+    int most, rc = check_trees(ctx, "tree_path", B, cu_nodes, parent, most);
+    if (rc != SSD_OK) return rc;
+    if (!accept_len || !accept_node || (cu_nodes[B] && (!node_logp || !path))) return fail(ctx, SSD_EINVAL, "tree_path: NULL data pointer");
+    if (tau != tau) return fail(ctx, SSD_EINVAL, "tree_path: tau is NaN");
+    const PathPlan p = plan_path(cu_nodes[B], B);
+    if (!ctx->ws || ctx->ws_bytes < p.meta_bytes)
+        return fail(ctx, SSD_EWORKSPACE, "tree_path: workspace of %zu bytes needed, %zu set", p.meta_bytes, ctx->ws_bytes);
+    std::vector<uint32_t> meta(p.meta_bytes / 4);
+    path_meta(p, B, cu_nodes, parent, meta.data());
+    rc = place_meta(ctx, meta, ctx->ws);
+    if (rc != SSD_OK) return rc;
+    const char* ws = static_cast<const char*>(ctx->ws);
+    {
+        ProfScope ps(ctx, SSD_PROF_OTHER);
+        launch_tree_path(node_logp, reinterpret_cast<const int32_t*>(ws), reinterpret_cast<const int16_t*>(ws + p.parent), B, most, ln_of(tau), false,
+                         accept_len, accept_node, path, ctx->stream);
+    }
+    HIP_TRY(ctx, hipGetLastError());
+    return SSD_OK;
+}
+
+size_t ssd_evict_workspace_bytes(const ssd_ctx* ctx, int n_layers, int n_kv_heads, int64_t max_kept_rows, int64_t max_utts) {
+    if (!ctx || n_layers <= 0 || n_kv_heads <= 0 || max_kept_rows < 0 || max_utts < 0) return 0;
+    return plan_evict((int64_t)n_layers * n_kv_heads, max_kept_rows, max_utts).total + 256;
+}
+
+int kv_evict(ssd_ctx* ctx, const ssd_kv_view* from, const float* mass, int B, const int32_t* kv_start, const int32_t* ctx_len, const int32_t* keep,
+             int n_first, int n_recent, const ssd_kv_view* to, const int32_t* out_start, float* mass_out, int32_t* rows_out) {
+    if (!ctx) return SSD_EINVAL;
+    const OnDevice on(ctx);
+    int rc = check_view(ctx, "kv_evict", from);
+    if (rc == SSD_OK) rc = check_view(ctx, "kv_evict", to);
+    if (rc != SSD_OK) return rc;
+    if (from->n_layers != to->n_layers || from->n_kv_heads != to->n_kv_heads || from->head_dim != to->head_dim || from->dtype != to->dtype)
+        return fail(ctx, SSD_EINVAL, "kv_evict: the caches differ in layers, heads, head_dim or dtype");
+    if (!mass || !keep || !out_start) return fail(ctx, SSD_EINVAL, "kv_evict: NULL argument");
+    if (B <= 0 || n_first < 0 || n_recent < 0) return fail(ctx, SSD_EINVAL, "kv_evict: B must be positive, n_first and n_recent not negative");
+    rc = check_places(ctx, "kv_evict", B, kv_start, ctx_len, nullptr, from->slots, false);
+    if (rc != SSD_OK) return rc;
+    const Extent a[2] = {extent_of(*from, from->k), extent_of(*from, from->v)}, z[2] = {extent_of(*to, to->k), extent_of(*to, to->v)};
+    if (overlap(a[0], z[0]) || overlap(a[0], z[1]) || overlap(a[1], z[0]) || overlap(a[1], z[1]))
+        return fail(ctx, SSD_EINVAL, "kv_evict: the caches overlap in memory");
+    const int64_t lh = (int64_t)from->n_layers * from->n_kv_heads;
+    if (mass_out && overlap(Extent{(uintptr_t)mass, (uintptr_t)mass + (uintptr_t)(lh * from->slots * 4)},
+                            Extent{(uintptr_t)mass_out, (uintptr_t)mass_out + (uintptr_t)(lh * to->slots * 4)}))
+        return fail(ctx, SSD_EINVAL, "kv_evict: mass and mass_out overlap in memory");
+    std::vector<EvictUtt> utts(B);
+    std::vector<int64_t> len(B);
+    int64_t kept = 0;
+    for (int b = 0; b < B; ++b) {
+        if (keep[b] < 0) return fail(ctx, SSD_EINVAL, "kv_evict: keep[%d] is negative", b);
+        if (keep[b] < ctx_len[b] && (int64_t)n_first + n_recent > keep[b])
+            return fail(ctx, SSD_EINVAL, "kv_evict: utterance %d keeps %d rows, fewer than n_first + n_recent", b, keep[b]);
+        const int k = std::min(keep[b], ctx_len[b]);
+        if (out_start[b] < 0 || (int64_t)out_start[b] + k > to->slots) return fail(ctx, SSD_EINVAL, "kv_evict: utterance %d does not fit the other cache", b);
+        utts[b] = EvictUtt{kv_start[b], ctx_len[b], k, out_start[b], (int32_t)kept};
+        len[b] = k;
+        kept += k;
+    }
+    if (kept > 0x7fffffff) return fail(ctx, SSD_ESHAPE, "kv_evict: more than 2^31 - 1 rows are kept; split the batch");
+    if (!ranges_distinct(B, out_start, len)) return fail(ctx, SSD_EINVAL, "kv_evict: utterances share slots of the other cache");
+    if (!kept) return SSD_OK;
+    const EvictPlan p = plan_evict(lh, rows_out ? 0 : kept, B);
+    if (!ctx->ws || ctx->ws_bytes < p.total) return fail(ctx, SSD_EWORKSPACE, "kv_evict: workspace of %zu bytes needed, %zu set", p.total, ctx->ws_bytes);
+    std::vector<uint32_t> meta((size_t)B * sizeof(EvictUtt) / 4);
+    memcpy(meta.data(), utts.data(), meta.size() * 4);
+    rc = place_meta(ctx, meta, ctx->ws);
+    if (rc != SSD_OK) return rc;
+    char* ws = static_cast<char*>(ctx->ws);
+    const int64_t unit = 16 / (int64_t)kv_elem(from->dtype);
+    EvictArgs e;
+    e.k = from->k; e.v = from->v;
+    e.slot_stride = from->slot_stride / unit; e.head_stride = from->head_stride / unit; e.layer_stride = from->n_layers > 1 ? from->layer_stride / unit : 0;
+    e.k_out = to->k; e.v_out = to->v;
+    e.out_slot_stride = to->slot_stride / unit; e.out_head_stride = to->head_stride / unit; e.out_layer_stride = to->n_layers > 1 ? to->layer_stride / unit : 0;
+    e.n_layers = from->n_layers; e.n_kv_heads = from->n_kv_heads; e.row_chunks = from->head_dim / (int)unit;
+    e.mass = mass; e.mass_slots = from->slots;
+    e.mass_out = mass_out; e.mass_out_slots = to->slots;
+    e.utts = reinterpret_cast<const EvictUtt*>(ws + p.utts); e.B = B;
+    e.n_first = n_first; e.n_recent = n_recent; e.n_kept = (int)kept;
+    e.rows = rows_out ? rows_out : reinterpret_cast<int32_t*>(ws + p.rows);
+    {
+        ProfScope ps(ctx, SSD_PROF_OTHER);
+        launch_kv_evict(e, ctx->stream);
+    }
+    HIP_TRY(ctx, hipGetLastError());
+    return SSD_OK;
+}
+
+size_t ssd_verify_tree_workspace_bytes(const ssd_ctx* ctx, int64_t max_nodes, int64_t max_utts) {
+    if (!ctx || !ctx->has_model || max_nodes < 0 || max_utts < 0) return 0;
+    const ssd_model_cfg& m = ctx->cfg;
+    TreePlan t;
+    t.meta_bytes = t.total = max_tree_bytes(m.n_q_heads, m.n_kv_heads, m.head_dim, max_nodes, max_utts);
+    return std::max(plan_verify_tree(m, max_nodes, t).total, plan_accept_tree(m, max_nodes, 2 * max_nodes, max_utts).total) + 256;
+}
+
+int verify_tree(ssd_ctx* ctx, const int32_t* node_ids, int B, const int32_t* cu_nodes, const int32_t* parent, const int32_t* kv_start,
+                const int32_t* ctx_len, const int32_t* pos0, float* kv_mass, void* h_tree) {
+    if (!ctx) return SSD_EINVAL;
+    const OnDevice on(ctx);
+    if (!ctx->has_model) return fail(ctx, SSD_EINVAL, "verify_tree: context was created without a model");
+    if (!ctx->kv) return fail(ctx, SSD_EINVAL, "verify_tree: no K/V cache set");
+    const ssd_model_cfg& m = ctx->cfg;
+    ssd_kv_view view = model_view(m, ctx->bf16_ops, ctx->kv, ctx->kv_slots);
+    int most, rc = check_view(ctx, "verify_tree", &view);
+    if (rc == SSD_OK) rc = check_trees(ctx, "verify_tree", B, cu_nodes, parent, most);
+    if (rc == SSD_OK) rc = check_places(ctx, "verify_tree", B, kv_start, ctx_len, cu_nodes, ctx->kv_slots, true);
+    if (rc != SSD_OK) return rc;
+    const int64_t N = cu_nodes[B];
+    if (N == 0) return SSD_OK;
+    if (!node_ids || !h_tree) return fail(ctx, SSD_EINVAL, "verify_tree: NULL data pointer");
+    {
+        const int64_t widest = std::max<int64_t>({(int64_t)m.d_ff, (int64_t)(m.n_q_heads + 2 * m.n_kv_heads) * m.head_dim, (int64_t)m.d_model});
+        if (N * widest * (int64_t)elem_size(m.dtype) >= ((int64_t)1 << 32))
+            return fail(ctx, SSD_ESHAPE, "verify_tree: %lld nodes of %lld columns exceed the 4 GiB an activation matrix may have; split the batch",
+                        (long long)N, (long long)widest);
+    }
+    TreeWork w;
+    tree_work(B, kv_start, ctx_len, cu_nodes, m.n_q_heads / m.n_kv_heads, kv_mass != nullptr, w);
+    const TreePlan t = plan_tree(N, w.items.size(), w.mass_items.size(), kv_mass ? N * m.n_q_heads : 0);
+    const VerifyTreePlan p = plan_verify_tree(m, N, t);
+    if (!ctx->ws || ctx->ws_bytes < p.total)
+        return fail(ctx, SSD_EWORKSPACE, "verify_tree: workspace of %zu bytes needed, %zu set", p.total, ctx->ws_bytes);
+    std::vector<uint32_t> meta(p.meta_bytes / 4);
+    int32_t* row_src = reinterpret_cast<int32_t*>(meta.data() + p.row_src / 4);
+    int32_t* pos = reinterpret_cast<int32_t*>(meta.data() + p.pos / 4);
+    int32_t* row_slot = reinterpret_cast<int32_t*>(meta.data() + p.row_slot / 4);
+    for (int b = 0; b < B; ++b) {
+        const int64_t first = pos0 ? pos0[b] : ctx_len[b];
+        if (first < 0) return fail(ctx, SSD_EINVAL, "verify_tree: pos0[%d] is negative", b);
+        for (int i = cu_nodes[b]; i < cu_nodes[b + 1]; ++i) {
+            const int64_t at = parent[i] < 0 ? first : pos[cu_nodes[b] + parent[i]] + (int64_t)1;
+            if (at >= m.max_positions) return fail(ctx, SSD_ESHAPE, "verify_tree: utterance %d would reach position %lld, max_positions is %d", b, (long long)at, m.max_positions);
+            row_src[i] = SRC_DRAFT | i;
+            pos[i] = (int32_t)at;
+            row_slot[i] = kv_start[b] + ctx_len[b] + (i - cu_nodes[b]);
+        }
+    }
+    tree_meta(t, w, B, cu_nodes, parent, meta.data() + p.tree / 4);
+    rc = place_meta(ctx, meta, ctx->ws);
+    if (rc != SSD_OK) return rc;
+    char* ws = static_cast<char*>(ctx->ws);
+    const int32_t* d_pos = reinterpret_cast<const int32_t*>(ws + p.pos);
+    const int32_t* d_slot = reinterpret_cast<const int32_t*>(ws + p.row_slot);
+    float* x = reinterpret_cast<float*>(ws + p.x);
+    void* a = ws + p.a; void* qkv = ws + p.qkv; void* att = ws + p.attn; void* h = ws + p.h;
+    float* partials = reinterpret_cast<float*>(ws + p.partials);
+    hipStream_t st = ctx->stream;
+    const int Ni = (int)N, d = m.d_model, dq = m.n_q_heads * m.head_dim, dkv = m.n_kv_heads * m.head_dim;
+    const int64_t stride = N * d;
+    const float scale = 1.0f / sqrtf((float)m.head_dim);
+    {
+        ProfScope ps(ctx, SSD_PROF_OTHER);
+        launch_embed_rows(m.dtype, nullptr, ctx->embed, nullptr, node_ids, reinterpret_cast<const int32_t*>(ws + p.row_src), Ni, d, m.vocab, x, ctx->dev_flags, st);
+    }
+    float* rope_rows = nullptr;
+    if (m.dtype == SSD_BF16 && N > SKINNY_MAX_ROWS) {
+        ProfScope ps(ctx, SSD_PROF_OTHER);
+        rope_rows = reinterpret_cast<float*>(ws + p.rope_rows);
+        launch_gather_rows(ctx->rope_tab, d_pos, Ni, 64 * sizeof(float2), rope_rows, st);
+    }
+    view.n_layers = 1;
+    int pending = 1;
+    for (int l = 0; l < m.n_layers; ++l) {
+        view.k = kv_k(ctx, l);
+        view.v = kv_v(ctx, l);
+        const TreeAttnArgs ta = tree_args(t, w, ws + p.tree, view, qkv, dq + 2 * dkv, m.n_q_heads, scale, att, nullptr,
+                                          kv_mass ? kv_mass + (int64_t)l * m.n_kv_heads * ctx->kv_slots : nullptr);
+        if (m.dtype == SSD_BF16) {
+            { ProfScope ps(ctx, SSD_PROF_OTHER); launch_rmsnorm(m.dtype, x, ctx->norm_attn[l], nullptr, Ni, d, m.rms_eps, a, partials, pending, stride, ctx->dev_flags, ctx->bf16_ops, st); }
+            { ProfScope ps(ctx, SSD_PROF_GEMM_QKV); launch_gemm_qkv_rope((const uint16_t*)a, (const uint16_t*)ctx->wqkv[l], ctx->s_qkv[l], (uint16_t*)qkv, d_pos, ctx->rope_tab, Ni, d, dq, dkv, ctx->ds_qkv[l],
+                                                                         d_slot, (uint16_t*)view.k, (uint16_t*)view.v, rope_rows, ctx->dev_flags, ctx->bf16_ops, st); }
+            { ProfScope ps(ctx, SSD_PROF_ATTN); launch_tree_attention(ta, st); }
+            { ProfScope ps(ctx, SSD_PROF_GEMM_O); pending = launch_gemm_residual((const uint16_t*)att, (const uint16_t*)ctx->wo[l], ctx->s_o[l], x, partials, Ni, d, dq, ctx->ds_o[l], ctx->bf16_ops, st); }
+            { ProfScope ps(ctx, SSD_PROF_OTHER); launch_rmsnorm(m.dtype, x, ctx->norm_mlp[l], nullptr, Ni, d, m.rms_eps, a, partials, pending, stride, ctx->dev_flags, ctx->bf16_ops, st); }
+            { ProfScope ps(ctx, SSD_PROF_GEMM_GATE_UP); launch_gemm_swiglu((const uint16_t*)a, (const uint16_t*)ctx->wgu[l], ctx->s_gu[l], (uint16_t*)h, Ni, m.d_ff, d, ctx->ds_gu[l], ctx->dev_flags, ctx->bf16_ops, st); }
+            { ProfScope ps(ctx, SSD_PROF_GEMM_DOWN); pending = launch_gemm_residual((const uint16_t*)h, (const uint16_t*)ctx->w_down[l], ctx->s_down[l], x, partials, Ni, d, m.d_ff, ctx->ds_down[l], ctx->bf16_ops, st); }
+        } else {
+            launch_gemm_f32_qkv(x, (const float*)ctx->norm_attn[l], m.rms_eps, (const float*)ctx->wqkv[l], (float*)qkv, d_pos, ctx->rope_tab, Ni, d, dq, dkv, m.head_dim,
+                                d_slot, (float*)view.k, (float*)view.v, st);
+            launch_tree_attention(ta, st);
+            launch_gemm_f32_residual((const float*)att, (const float*)ctx->wo[l], x, Ni, d, dq, nullptr, nullptr, st);
+            launch_gemm_f32_swiglu(x, (const float*)ctx->norm_mlp[l], m.rms_eps, (const float*)ctx->wgu[l], (float*)h, Ni, m.d_ff, d, nullptr, st);
+            launch_gemm_f32_residual((const float*)h, (const float*)ctx->w_down[l], x, Ni, d, m.d_ff, nullptr, nullptr, st);
+        }
+    }
+    { ProfScope ps(ctx, SSD_PROF_OTHER); launch_rmsnorm(m.dtype, x, ctx->norm_final, nullptr, Ni, d, m.rms_eps, h_tree, partials, pending, stride, ctx->dev_flags, ctx->bf16_ops, st); }
+    HIP_TRY(ctx, hipGetLastError());
+    return SSD_OK;
+}
+
+int accept_tree(ssd_ctx* ctx, const void* h_tree, const int32_t* node_ids, int B, const int32_t* cu_nodes, const int32_t* parent, float tau_slm,
+                const int32_t* kv_start, const int32_t* ctx_len, float* kv_mass, float* node_logp, int32_t* greedy_tok, int32_t* accept_len,
+                int32_t* accept_node, int32_t* path) {
+    if (!ctx) return SSD_EINVAL;
+    const OnDevice on(ctx);
+    if (!ctx->has_model) return fail(ctx, SSD_EINVAL, "accept_tree: context was created without a model");
+    int most, rc = check_trees(ctx, "accept_tree", B, cu_nodes, parent, most);
+    if (rc == SSD_OK && kv_start) {
+        if (!ctx->kv) return fail(ctx, SSD_EINVAL, "accept_tree: no K/V cache set");
+        rc = check_places(ctx, "accept_tree", B, kv_start, ctx_len, cu_nodes, ctx->kv_slots, true);
+    }
+    if (rc != SSD_OK) return rc;
+    const int64_t N = cu_nodes[B];
+    if (!accept_len || !accept_node || (N && (!h_tree || !node_ids || !node_logp || !greedy_tok || !path)))
+        return fail(ctx, SSD_EINVAL, "accept_tree: NULL data pointer");
+    if (tau_slm != tau_slm) return fail(ctx, SSD_EINVAL, "accept_tree: tau_slm is NaN");
+    const ssd_model_cfg& m = ctx->cfg;
+    // LM-head rows: entry i < N the row that scores node i (its parent's; a given node's own), then the rows of the leaves
+    std::vector<int32_t> row(N), target(N), row_of(N, -1);
+    for (int b = 0; b < B; ++b)
+        for (int i = cu_nodes[b]; i < cu_nodes[b + 1]; ++i) {
+            row[i] = parent[i] < 0 ? i : cu_nodes[b] + parent[i];
+            target[i] = i;
+            row_of[row[i]] = i;
+        }
+    for (int i = 0; i < (int)N; ++i)
+        if (row_of[i] < 0) {
+            row_of[i] = (int32_t)row.size();
+            row.push_back(i);
+            target.push_back(i);
+        }
+    const int64_t R = (int64_t)row.size();
+    if (R * (int64_t)m.d_model * (int64_t)elem_size(m.dtype) >= ((int64_t)1 << 32))
+        return fail(ctx, SSD_ESHAPE, "accept_tree: %lld rows exceed the 4 GiB the hidden rows may have; split the batch", (long long)R);
+    const AcceptTreePlan p = plan_accept_tree(m, N, R, B);
+    if (!ctx->ws || ctx->ws_bytes < p.total)
+        return fail(ctx, SSD_EWORKSPACE, "accept_tree: workspace of %zu bytes needed, %zu set", p.total, ctx->ws_bytes);
+    const PathPlan pp = plan_path(N, B);
+    std::vector<uint32_t> meta(p.meta_bytes / 4);
+    memcpy(meta.data() + p.row / 4, row.data(), (size_t)R * 4);
+    memcpy(meta.data() + p.target / 4, target.data(), (size_t)R * 4);
+    memcpy(meta.data() + p.row_of / 4, row_of.data(), (size_t)N * 4);
+    path_meta(pp, B, cu_nodes, parent, meta.data() + p.path / 4);
+    const size_t places = p.path + pp.meta_bytes;
+    if (kv_start) {
+        memcpy(meta.data() + places / 4, kv_start, (size_t)B * 4);
+        memcpy(meta.data() + places / 4 + B, ctx_len, (size_t)B * 4);
+    }
+    rc = place_meta(ctx, meta, ctx->ws);
+    if (rc != SSD_OK) return rc;
+    char* ws = static_cast<char*>(ctx->ws);
+    const int32_t* d_row = reinterpret_cast<const int32_t*>(ws + p.row);
+    int32_t* tgt_ids = reinterpret_cast<int32_t*>(ws + p.tgt_ids);
+    float* logp = reinterpret_cast<float*>(ws + p.logp);
+    int32_t* greedy = reinterpret_cast<int32_t*>(ws + p.greedy);
+    float2* part_ms = reinterpret_cast<float2*>(ws + p.part_ms);
+    float* tgt = reinterpret_cast<float*>(ws + p.tgt);
+    int2* part_arg = reinterpret_cast<int2*>(ws + p.part_arg);
+    const int32_t* d_cu = reinterpret_cast<const int32_t*>(ws + p.path);
+    const int16_t* d_parent = reinterpret_cast<const int16_t*>(ws + p.path + pp.parent);
+    const int32_t* d_places = reinterpret_cast<const int32_t*>(ws + places);
+    hipStream_t st = ctx->stream;
+    ProfScope ps_all(ctx, SSD_PROF_LMHEAD);
+    if (N) {
+        launch_gather_rows(h_tree, d_row, (int)R, (int64_t)m.d_model * elem_size(m.dtype), ws + p.h, st);
+        launch_gather_ids(node_ids, reinterpret_cast<const int32_t*>(ws + p.target), (int)R, nullptr, 0, tgt_ids, st);
+        if (m.dtype == SSD_BF16)
+            launch_lmhead_mfma((const uint16_t*)(ws + p.h), (const uint16_t*)ctx->lm_head, tgt_ids, (int)R, m.d_model, m.vocab, part_ms, tgt, part_arg, true,
+                               ctx->ds_lm, ctx->bf16_ops, st);
+        else
+            launch_lmhead_f32((const float*)(ws + p.h), (const float*)ctx->lm_head, tgt_ids, (int)R, m.d_model, m.vocab, part_ms, tgt, part_arg, st);
+        launch_lmhead_finalize(part_ms, tgt, part_arg, head_groups(m), (int)R, logp, greedy, head_flags(ctx), st);
+        launch_tree_scatter(logp, greedy, reinterpret_cast<const int32_t*>(ws + p.row_of), d_parent, (int)N, node_logp, greedy_tok, st);
+    }
+    launch_tree_path(node_logp, d_cu, d_parent, B, most, ln_of(tau_slm), true, accept_len, accept_node, path, st);
+    if (kv_start && N) {
+        const ssd_kv_view v = model_view(m, ctx->bf16_ops, ctx->kv, ctx->kv_slots);
+        const int64_t unit = 16 / (int64_t)kv_elem(v.dtype);
+        launch_tree_commit(v.k, v.v, v.slot_stride / unit, v.layer_stride / unit, m.n_layers, m.n_kv_heads, m.head_dim / (int)unit, kv_mass, ctx->kv_slots, d_places,
+                           d_places + B, d_cu, accept_len, path, B, st);
+    }
     HIP_TRY(ctx, hipGetLastError());
     return SSD_OK;
 }

@@ -1,0 +1,70 @@
+// Trees of drafted tokens over cached rows: what the host layer hands to the kernels of tree_attn.hip, tree_path.hip and kv_evict.hip.
+#pragma once
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+
+#include "../../include/ssd.h"
+
+namespace ssd {
+
+constexpr int MAX_TREE_NODES = SSD_MAX_TREE_NODES;
+
+// Query rows of one K/V head are numbered node * G + head of the group.  Keys k0 .. k1 - 1 (rows of the utterance: n_ctx cached ones, then
+// the nodes) for rows row0 .. of the utterance.
+struct TreeItem {
+    int32_t slot0, n_ctx, n_nodes, node0;    // first cache slot, cached rows, nodes, first node of the utterance in the call
+    int32_t row0, k0, k1, part;
+};
+
+// Words that travel as arguments of a launch (4 KB with the rest) to memory of the device.
+struct MetaWords {
+    static constexpr int WORDS = 960;
+    int n;
+    uint32_t word[WORDS];
+};
+void launch_write_words(const MetaWords& w, uint32_t* dst, hipStream_t st);
+
+struct TreeAttnArgs {
+    const void* q; int64_t q_stride;
+    const void* k; const void* v; int64_t slot_stride, head_stride;
+    int n_q_heads, n_kv_heads, head_dim, dtype;
+    float scale;
+    void* out;
+    float* lse;                              // [nodes, n_q_heads]; NULL: not wanted
+    float* mass; int64_t mass_stride;        // [n_kv_heads, mass_stride]; NULL: not wanted
+    const TreeItem* items; int n_items;
+    const TreeItem* mass_items; int n_mass_items;
+    const uint32_t* spans;                   // per node: place in depth-first order, end of its subtree << 16
+};
+void launch_tree_attention(const TreeAttnArgs& a, hipStream_t st);
+constexpr int TREE_ROWS = 16;                // query rows of an item
+constexpr int TREE_MASS_KEYS = 256;          // keys of an item of the weights: a multiple of these
+constexpr int TREE_MAX_PARTS = 1024;         // long contexts are cut into about as many pieces in all
+
+// nodes of an utterance: cu[b] .. cu[b + 1] - 1 (at most MAX_TREE_NODES); parent: index inside the utterance or -1
+void launch_tree_path(const float* logp, const int32_t* cu, const int16_t* parent, int B, int most_nodes, float ln_tau, bool roots_given, int32_t* accept_len,
+                      int32_t* accept_node, int32_t* path, hipStream_t st);
+
+// node_logp[i] = logp[i], 0 where parent[i] < 0; greedy_tok[i] = greedy[row_of[i]]
+void launch_tree_scatter(const float* logp, const int32_t* greedy, const int32_t* row_of, const int16_t* parent, int n, float* node_logp,
+                         int32_t* greedy_tok, hipStream_t st);
+// K/V rows of the accepted path (and their entries of mass [n_layers, n_kv_heads, slots], unless NULL) to the slots behind the context; strides in
+// 16-byte units, a slot's heads one behind the other, row_chunks units each
+void launch_tree_commit(void* k, void* v, int64_t slot_stride, int64_t layer_stride, int n_layers, int n_kv_heads, int row_chunks, float* mass, int64_t slots,
+                        const int32_t* kv_start, const int32_t* ctx_len, const int32_t* cu, const int32_t* accept_len, const int32_t* path, int B,
+                        hipStream_t st);
+
+struct EvictUtt { int32_t slot0, n_ctx, keep, out0, kept0; };     // kept0: kept rows of the utterances before
+struct EvictArgs {
+    const void* k; const void* v; int64_t slot_stride, head_stride, layer_stride;         // in 16-byte units
+    void* k_out; void* v_out; int64_t out_slot_stride, out_head_stride, out_layer_stride;
+    int n_layers, n_kv_heads, row_chunks;    // 16-byte units of a row
+    const float* mass; int64_t mass_slots;
+    float* mass_out; int64_t mass_out_slots; // mass_out NULL: not wanted
+    const EvictUtt* utts; int B;
+    int n_first, n_recent, n_kept;           // n_kept: rows that all utterances keep
+    int32_t* rows;                           // [n_layers, n_kv_heads, n_kept]
+};
+void launch_kv_evict(const EvictArgs& a, hipStream_t st);
+
+}  // namespace ssd

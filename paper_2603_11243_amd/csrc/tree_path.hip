@@ -1,0 +1,107 @@
+// Accepted path of a tree of drafted tokens (Eq. 5 and the definition of j, Sec. 2.3, for more than one continuation): a node stands if
+// its own likelihood and those of all its ancestors pass; the deepest node that stands wins, the lowest index among equally deep ones.
+#include "device_utils.h"
+#include "tree.h"
+
+namespace ssd {
+
+// One workgroup a tree, one thread a node (NT of them).  Pointer jumping: after round r a node knows whether the 2^r nodes on the way up
+// from it pass, how many there are, and who comes next.
+template <int NT>
+__global__ void __launch_bounds__(NT) tree_path_kernel(const float* __restrict__ logp, const int32_t* __restrict__ cu, const int16_t* __restrict__ parent,
+                                                       float ln_tau, bool roots_given, int32_t* __restrict__ accept_len,
+                                                       int32_t* __restrict__ accept_node, int32_t* __restrict__ path) {
+    __shared__ int up_s[NT], way_s[NT], best_s;              // way: nodes on the way, negative if one of them fails
+    const int i = threadIdx.x, node0 = cu[blockIdx.x], n = cu[blockIdx.x + 1] - node0;
+    int up = -1, way = -1;
+    if (i < n) {
+        up = parent[node0 + i];
+        way = (up < 0 && roots_given) || logp[node0 + i] > ln_tau ? 1 : -0x10000;
+        path[node0 + i] = -1;
+    }
+    const int first_up = up;
+    if (i == 0) best_s = -1;
+    for (int r = 1; r < NT; r *= 2) {
+        up_s[i] = up;
+        way_s[i] = way;
+        __syncthreads();
+        if (up >= 0) {
+            way += way_s[up];
+            if (way < 0) way = -0x10000;
+            up = up_s[up];
+        }
+        __syncthreads();
+    }
+    if (i < n && way > 0) atomicMax(&best_s, way * NT + (NT - 1 - i));
+    up_s[i] = first_up;
+    __syncthreads();
+    if (i == 0) {
+        const int best = best_s < 0 ? -1 : NT - 1 - best_s % NT, len = best_s < 0 ? 0 : best_s / NT;
+        accept_len[blockIdx.x] = len;
+        accept_node[blockIdx.x] = best;
+        int at = best;
+        for (int d = len - 1; d >= 0; --d) {
+            path[node0 + d] = at;
+            at = up_s[at];
+        }
+    }
+}
+
+__global__ void __launch_bounds__(256) write_words_kernel(MetaWords w, uint32_t* __restrict__ dst) {
+    for (int i = threadIdx.x; i < w.n; i += 256) dst[i] = w.word[i];
+}
+void launch_write_words(const MetaWords& w, uint32_t* dst, hipStream_t st) {
+    hipLaunchKernelGGL(write_words_kernel, dim3(1), dim3(256), 0, st, w, dst);
+}
+
+__global__ void __launch_bounds__(256) tree_scatter_kernel(const float* __restrict__ logp, const int32_t* __restrict__ greedy, const int32_t* __restrict__ row_of,
+                                                          const int16_t* __restrict__ parent, int n, float* __restrict__ node_logp,
+                                                          int32_t* __restrict__ greedy_tok) {
+    const int i = blockIdx.x * 256 + threadIdx.x;
+    if (i >= n) return;
+    node_logp[i] = parent[i] < 0 ? 0.f : logp[i];
+    greedy_tok[i] = greedy[row_of[i]];
+}
+void launch_tree_scatter(const float* logp, const int32_t* greedy, const int32_t* row_of, const int16_t* parent, int n, float* node_logp,
+                         int32_t* greedy_tok, hipStream_t st) {
+    hipLaunchKernelGGL(tree_scatter_kernel, dim3((n + 255) / 256), dim3(256), 0, st, logp, greedy, row_of, parent, n, node_logp, greedy_tok);
+}
+
+// One thread a 16-byte column of an utterance's rows in a layer.  Step d moves row path[d] >= d, so that in the order of d no row is
+// written that this thread still reads, and no other thread touches the column.
+__global__ void __launch_bounds__(256) tree_commit_kernel(uint4* __restrict__ k, uint4* __restrict__ v, int64_t slot_stride, int64_t layer_stride, int n_kv_heads,
+                                                         int cols, float* __restrict__ mass, int64_t slots, const int32_t* __restrict__ kv_start,
+                                                         const int32_t* __restrict__ ctx_len, const int32_t* __restrict__ cu,
+                                                         const int32_t* __restrict__ accept_len, const int32_t* __restrict__ path) {
+    const int b = blockIdx.x, layer = blockIdx.y, n = accept_len[b];
+    const int32_t* from = path + cu[b];
+    const int64_t slot0 = (int64_t)kv_start[b] + ctx_len[b], base = layer * layer_stride + slot0 * slot_stride;
+    for (int c = threadIdx.x; c < 2 * cols; c += 256) {
+        uint4* col = (c < cols ? k : v) + base + c % cols;
+        for (int d = 0; d < n; ++d)
+            if (from[d] != d) col[d * slot_stride] = col[from[d] * slot_stride];
+    }
+    if (mass)
+        for (int h = threadIdx.x; h < n_kv_heads; h += 256) {
+            float* col = mass + ((int64_t)layer * n_kv_heads + h) * slots + slot0;
+            for (int d = 0; d < n; ++d)
+                if (from[d] != d) col[d] = col[from[d]];
+        }
+}
+void launch_tree_commit(void* k, void* v, int64_t slot_stride, int64_t layer_stride, int n_layers, int n_kv_heads, int row_chunks, float* mass, int64_t slots,
+                        const int32_t* kv_start, const int32_t* ctx_len, const int32_t* cu, const int32_t* accept_len, const int32_t* path, int B,
+                        hipStream_t st) {
+    hipLaunchKernelGGL(tree_commit_kernel, dim3(B, n_layers), dim3(256), 0, st, (uint4*)k, (uint4*)v, slot_stride, layer_stride, n_kv_heads, n_kv_heads * row_chunks,
+                       mass, slots, kv_start, ctx_len, cu, accept_len, path);
+}
+
+void launch_tree_path(const float* logp, const int32_t* cu, const int16_t* parent, int B, int most_nodes, float ln_tau, bool roots_given, int32_t* accept_len,
+                      int32_t* accept_node, int32_t* path, hipStream_t st) {
+#define SSD_PATH(NT_) hipLaunchKernelGGL(tree_path_kernel<NT_>, dim3(B), dim3(NT_), 0, st, logp, cu, parent, ln_tau, roots_given, accept_len, accept_node, path)
+    if (most_nodes <= 64) SSD_PATH(64);
+    else if (most_nodes <= 256) SSD_PATH(256);
+    else SSD_PATH(MAX_TREE_NODES);
+#undef SSD_PATH
+}
+
+}  // namespace ssd

@@ -1425,8 +1425,9 @@ int place_meta(ssd_ctx* c, const std::vector<uint32_t>& meta, void* dev) {
 }
 
 struct TreeWork {
-    int tile_rows;
+    int tile_rows, n_parts = 0;
     std::vector<TreeItem> items, mass_items;
+    std::vector<TreeJoin> joins;
 };
 // Nodes in depth-first order: a node's place, the end of its subtree.
 void tree_spans(int n, const int32_t* parent, uint32_t* span) {
@@ -1442,41 +1443,71 @@ void tree_spans(int n, const int32_t* parent, uint32_t* span) {
         span[i] = (uint32_t)at | (uint32_t)(at + size[i]) << 16;
     }
 }
-void tree_work(int B, const int32_t* kv_start, const int32_t* ctx_len, const int32_t* cu_nodes, int G, bool mass, TreeWork& w) {
-    w.tile_rows = TREE_ROWS;
-    int64_t total = 0;
-    for (int b = 0; b < B; ++b) total += cu_nodes[b + 1] > cu_nodes[b] ? ctx_len[b] + cu_nodes[b + 1] - cu_nodes[b] : 0;
-    const int step = (int)align_up((size_t)std::max<int64_t>(1, (total + TREE_MAX_PARTS - 1) / TREE_MAX_PARTS), TREE_MASS_KEYS);
+// Query rows of an item: as many as the largest tree has, at most 64.  Ranges of keys: a range per item, unless that leaves most of the chip
+// without work; then about TREE_WORKGROUPS ranges in all.
+int tree_tile_rows(int dtype, int rows) { return dtype == SSD_F32 || rows <= 16 ? 16 : rows <= 32 ? 32 : 64; }
+void tree_work(int B, const int32_t* kv_start, const int32_t* ctx_len, const int32_t* cu_nodes, int most, int n_q_heads, int n_kv_heads, int dtype, bool mass, TreeWork& w) {
+    const int G = n_q_heads / n_kv_heads;
+    w.tile_rows = tree_tile_rows(dtype, most * G);
+    int64_t total = 0, per_row = 0;                          // keys of all items, of all utterances
     for (int b = 0; b < B; ++b) {
-        const int n = cu_nodes[b + 1] - cu_nodes[b], keys = ctx_len[b] + n;
-        for (int r = 0; r < n * G; r += w.tile_rows) w.items.push_back(TreeItem{kv_start[b], ctx_len[b], n, cu_nodes[b], r, 0, keys, -1});
-        for (int64_t k = 0; mass && n && k < keys; k += step)
-            w.mass_items.push_back(TreeItem{kv_start[b], ctx_len[b], n, cu_nodes[b], 0, (int)k, (int)std::min<int64_t>(keys, k + step), -1});
+        const int n = cu_nodes[b + 1] - cu_nodes[b];
+        const int64_t keys = (int64_t)ctx_len[b] + n;
+        per_row += n ? keys : 0;
+        total += keys * ((n * G + w.tile_rows - 1) / w.tile_rows);
+    }
+    auto step_of = [](int64_t keys, int64_t pieces, int64_t unit) { return std::max<int64_t>(1, (keys + pieces * unit - 1) / (pieces * unit)) * unit; };
+    const int64_t pieces = std::max(1, TREE_WORKGROUPS / n_kv_heads);
+    const int64_t step = dtype == SSD_F32 ? (int64_t)1 << 40 : std::max<int64_t>(TREE_SPLIT_KEYS, step_of(total, pieces, 128));
+    const int64_t mass_step = step_of(per_row, pieces, TREE_MASS_KEYS);
+    for (int b = 0; b < B; ++b) {
+        const int n = cu_nodes[b + 1] - cu_nodes[b], R = n * G, keys = ctx_len[b] + n;
+        if (!n) continue;
+        const int tiles = (R + w.tile_rows - 1) / w.tile_rows, parts = (int)((keys + step - 1) / step), part0 = w.n_parts;
+        for (int p = 0; p < parts; ++p)                      // tiles of the same keys one behind the other: they meet in an L2
+            for (int t = 0; t < tiles; ++t) {
+                const int row0 = t * w.tile_rows, node = (std::min(R, row0 + w.tile_rows) - 1) / G;       // no row of the tile sees a later node
+                const int k0 = (int)(p * step), k1 = (int)std::min<int64_t>(ctx_len[b] + node + 1, (p + 1) * step);
+                w.items.push_back(TreeItem{kv_start[b], ctx_len[b], n, cu_nodes[b], row0, k0, std::max(k0, k1), parts > 1 ? w.n_parts++ : -1});
+            }
+        for (int t = 0; parts > 1 && t < tiles; ++t) w.joins.push_back(TreeJoin{n, cu_nodes[b], t * w.tile_rows, part0 + t, tiles, parts});
+        for (int64_t k = 0; mass && k < keys; k += mass_step)
+            w.mass_items.push_back(TreeItem{kv_start[b], ctx_len[b], n, cu_nodes[b], 0, (int)k, (int)std::min<int64_t>(keys, k + mass_step), -1});
     }
 }
-struct TreePlan { size_t spans, items, mass_items, meta_bytes, lse, total; };
-TreePlan plan_tree(int64_t nodes, int64_t n_items, int64_t n_mass_items, int64_t lse_values) {
+struct TreePlan { size_t spans, items, mass_items, joins, meta_bytes, lse, part_o, part_ml, total; };
+TreePlan plan_tree(int64_t nodes, int64_t n_items, int64_t n_mass_items, int64_t n_joins, int64_t lse_values, int64_t part_rows, int head_dim) {
     TreePlan p;
     size_t o = 0;
     p.spans = o; o = align_up(o + (size_t)nodes * 4);
     p.items = o; o = align_up(o + (size_t)n_items * sizeof(TreeItem));
     p.mass_items = o; o = align_up(o + (size_t)n_mass_items * sizeof(TreeItem));
+    p.joins = o; o = align_up(o + (size_t)n_joins * sizeof(TreeJoin));
     p.meta_bytes = o;
     p.lse = o; o = align_up(o + (size_t)lse_values * 4);
+    p.part_o = o; o = align_up(o + (size_t)(part_rows * head_dim) * 4);
+    p.part_ml = o; o = align_up(o + (size_t)part_rows * sizeof(float2));
     p.total = o;
     return p;
 }
-
-// The same bytes for all trees of at most max_nodes nodes: an item holds at least one row, and what is split is bounded.
+TreePlan plan_tree(const TreeWork& w, int64_t nodes, int n_q_heads, const ssd_kv_view& kv, bool own_lse) {
+    return plan_tree(nodes, w.items.size(), w.mass_items.size(), w.joins.size(), own_lse ? nodes * n_q_heads : 0,
+                     (int64_t)w.n_parts * kv.n_kv_heads * w.tile_rows, (kv.head_dim + 63) / 64 * 64);
+}
+// The same for all trees of at most max_nodes nodes in all.  An item has at least one row, or is one of the pieces of a cut context: a context is
+// cut only where its keys, times its tiles, are more than one of TREE_WORKGROUPS / n_kv_heads shares, so that there are at most twice as many pieces.
 size_t max_tree_bytes(int n_q_heads, int n_kv_heads, int head_dim, int64_t max_nodes, int64_t max_utts) {
-    (void)head_dim;
-    const int64_t G = n_kv_heads > 0 ? (n_q_heads + n_kv_heads - 1) / n_kv_heads : 1;
-    return plan_tree(max_nodes, max_nodes * G, max_utts + TREE_MAX_PARTS, max_nodes * n_q_heads).total;
+    const int64_t G = (n_q_heads + n_kv_heads - 1) / n_kv_heads, pieces = std::max(1, TREE_WORKGROUPS / n_kv_heads);
+    const int64_t cut = 2 * pieces, rows = max_nodes * G;
+    // pieces that are not cut have a row each; a tile of 64 rows is used only for trees of more than 32
+    return plan_tree(max_nodes, rows + cut, max_utts + pieces, rows, max_nodes * n_q_heads, cut * n_kv_heads * std::min<int64_t>(64, 2 * std::max<int64_t>(rows, 16)),
+                     (head_dim + 63) / 64 * 64).total;
 }
 void tree_meta(const TreePlan& p, const TreeWork& w, int B, const int32_t* cu_nodes, const int32_t* parent, uint32_t* meta) {
     for (int b = 0; b < B; ++b) tree_spans(cu_nodes[b + 1] - cu_nodes[b], parent + cu_nodes[b], meta + p.spans / 4 + cu_nodes[b]);
     memcpy(meta + p.items / 4, w.items.data(), w.items.size() * sizeof(TreeItem));
     memcpy(meta + p.mass_items / 4, w.mass_items.data(), w.mass_items.size() * sizeof(TreeItem));
+    memcpy(meta + p.joins / 4, w.joins.data(), w.joins.size() * sizeof(TreeJoin));
 }
 TreeAttnArgs tree_args(const TreePlan& p, const TreeWork& w, char* ws, const ssd_kv_view& kv, const void* q, int64_t q_stride, int n_q_heads, float scale,
                        void* out, float* lse, float* mass) {
@@ -1488,8 +1519,11 @@ TreeAttnArgs tree_args(const TreePlan& p, const TreeWork& w, char* ws, const ssd
     a.out = out;
     a.lse = lse ? lse : mass ? reinterpret_cast<float*>(ws + p.lse) : nullptr;
     a.mass = mass; a.mass_stride = kv.slots;
+    a.tile_rows = w.tile_rows;
     a.items = reinterpret_cast<const TreeItem*>(ws + p.items); a.n_items = (int)w.items.size();
     a.mass_items = reinterpret_cast<const TreeItem*>(ws + p.mass_items); a.n_mass_items = (int)w.mass_items.size();
+    a.joins = reinterpret_cast<const TreeJoin*>(ws + p.joins); a.n_joins = (int)w.joins.size();
+    a.part_o = reinterpret_cast<float*>(ws + p.part_o); a.part_ml = reinterpret_cast<float2*>(ws + p.part_ml);
     a.spans = reinterpret_cast<const uint32_t*>(ws + p.spans);
     return a;
 }
@@ -1626,8 +1660,8 @@ int tree_attention(ssd_ctx* ctx, const void* q, int64_t q_stride, int n_q_heads,
     if (q_stride < dq || q_stride > (int64_t)1 << 40 || q_stride * es % 16 || ((uintptr_t)q | (uintptr_t)out) & 15)
         return fail(ctx, SSD_EINVAL, "tree_attention: rows of q and out must begin at multiples of 16 bytes, q_stride be at least n_q_heads * head_dim");
     TreeWork w;
-    tree_work(B, kv_start, ctx_len, cu_nodes, n_q_heads / kv->n_kv_heads, mass != nullptr, w);
-    const TreePlan p = plan_tree(N, w.items.size(), w.mass_items.size(), mass && !lse ? N * n_q_heads : 0);
+    tree_work(B, kv_start, ctx_len, cu_nodes, most, n_q_heads, kv->n_kv_heads, kv->dtype, mass != nullptr, w);
+    const TreePlan p = plan_tree(w, N, n_q_heads, *kv, mass && !lse);
     if (!ctx->ws || ctx->ws_bytes < p.total)
         return fail(ctx, SSD_EWORKSPACE, "tree_attention: workspace of %zu bytes needed, %zu set", p.total, ctx->ws_bytes);
     std::vector<uint32_t> meta(p.meta_bytes / 4);
@@ -1765,8 +1799,8 @@ int verify_tree(ssd_ctx* ctx, const int32_t* node_ids, int B, const int32_t* cu_
                         (long long)N, (long long)widest);
     }
     TreeWork w;
-    tree_work(B, kv_start, ctx_len, cu_nodes, m.n_q_heads / m.n_kv_heads, kv_mass != nullptr, w);
-    const TreePlan t = plan_tree(N, w.items.size(), w.mass_items.size(), kv_mass ? N * m.n_q_heads : 0);
+    tree_work(B, kv_start, ctx_len, cu_nodes, most, m.n_q_heads, m.n_kv_heads, view.dtype, kv_mass != nullptr, w);
+    const TreePlan t = plan_tree(w, N, m.n_q_heads, view, kv_mass != nullptr);
     const VerifyTreePlan p = plan_verify_tree(m, N, t);
     if (!ctx->ws || ctx->ws_bytes < p.total)
         return fail(ctx, SSD_EWORKSPACE, "verify_tree: workspace of %zu bytes needed, %zu set", p.total, ctx->ws_bytes);

@@ -16,6 +16,9 @@ struct TreeItem {
     int32_t row0, k0, k1, part;
 };
 
+// Pieces of rows row0 .. of an utterance, to be joined: numbers part0, part0 + stride, ..
+struct TreeJoin { int32_t n_nodes, node0, row0, part0, stride, n_parts; };
+
 // Words that travel as arguments of a launch (4 KB with the rest) to memory of the device.
 struct MetaWords {
     static constexpr int WORDS = 960;
@@ -32,14 +35,17 @@ struct TreeAttnArgs {
     void* out;
     float* lse;                              // [nodes, n_q_heads]; NULL: not wanted
     float* mass; int64_t mass_stride;        // [n_kv_heads, mass_stride]; NULL: not wanted
+    int tile_rows;                           // query rows of an item
     const TreeItem* items; int n_items;
+    const TreeJoin* joins; int n_joins;
+    float* part_o; float2* part_ml;          // [piece][K/V head][tile_rows] output and (maximum, sum)
     const TreeItem* mass_items; int n_mass_items;
     const uint32_t* spans;                   // per node: place in depth-first order, end of its subtree << 16
 };
 void launch_tree_attention(const TreeAttnArgs& a, hipStream_t st);
-constexpr int TREE_ROWS = 16;                // query rows of an item
 constexpr int TREE_MASS_KEYS = 256;          // keys of an item of the weights: a multiple of these
-constexpr int TREE_MAX_PARTS = 1024;         // long contexts are cut into about as many pieces in all
+constexpr int TREE_WORKGROUPS = 1024;        // long contexts are cut into about as many pieces in all, times K/V heads
+constexpr int TREE_SPLIT_KEYS = 256;         // a piece has at least as many keys
 
 // nodes of an utterance: cu[b] .. cu[b + 1] - 1 (at most MAX_TREE_NODES); parent: index inside the utterance or -1
 void launch_tree_path(const float* logp, const int32_t* cu, const int16_t* parent, int B, int most_nodes, float ln_tau, bool roots_given, int32_t* accept_len,

@@ -17,8 +17,11 @@ in host memory between the two.  `TwoPhaseDecoder.run` is that schedule:
 
 Everything numeric happens inside the library; this module only decides what goes into which call.  Copies between
 device and pinned host memory are plain memcpys issued through torch on the context's stream.
+
+`TreeFallback` is another phase 2: where a draft was rejected at one token, the tokens behind it are mostly still right, so
+the fallback verifies them, at their place and shifted by one, as a tree behind the model's own token, several tokens a pass.
 """
-from typing import Optional
+from typing import List, Optional
 
 import numpy as np
 import torch
@@ -26,11 +29,110 @@ import torch
 from .binding import Context, plan_batches
 
 
+class TreeFallback:
+    """Continuation of rejected utterances by trees over their cached rows.  A round: the model's own next token with the rest of the draft behind
+    it, once as if that token had replaced the draft's (substitution), once as if it had come before it (insertion) and once as if one more had been
+    left out (deletion), common beginnings shared, goes through verify_tree; accept_tree keeps the longest branch whose tokens pass tau and moves its rows
+    behind the context; the model's choice behind it begins the next round.  From tau 0.5 on a token that passes is the model's own choice, and the
+    result that of ar_fallback.
+
+    most_rows: contexts longer than that are cut between rounds by kv_evict to keep_rows rows (three quarters of it unless given): the first n_first and last
+    n_recent ones stay, of the others those of the largest attention weight here.  They go to two caches of the fallback's own in turn; the rows
+    of the attached one are only read, and it is attached again at the end."""
+
+    def __init__(self, ctx: Context, max_utts: int, tau: float = 0.5, depth: int = 6, most_rows: Optional[int] = None, keep_rows: Optional[int] = None,
+                 n_first: int = 4, n_recent: int = 32):
+        self.ctx, self.tau, self.depth, self.most_rows, self.n_first, self.n_recent = ctx, tau, depth, most_rows, n_first, n_recent
+        self.keep_rows = keep_rows if keep_rows is not None or most_rows is None else 3 * most_rows // 4
+        assert depth >= 1 and (most_rows is None or n_first + n_recent <= self.keep_rows <= most_rows and self.keep_rows > 0)
+        self.max_utts = max_utts
+        self.room = 1 + 3 * depth                            # nodes of a tree at most
+        self.own = [None, None]
+        more = {}
+        if most_rows is not None:
+            self.slots = max_utts * (most_rows + 2 * self.room)
+            more = {"evict_rows": self.slots, "evict_utts": max_utts, "evict_heads": (ctx.cfg.n_layers, ctx.cfg.n_kv_heads)}
+        ctx.reserve(tree_nodes=max_utts * self.room, tree_utts=max_utts, **more)
+
+    def _tree(self, token: int, draft, at: int, room: int):
+        """(tokens, parents, draft positions behind each node) of the tree behind `token`, which stands where draft[at] was."""
+        tokens, parent, follow, child = [token], [-1], [at + 1], {}
+        for first in (at + 1, at, at + 2):
+            node = 0
+            for i in range(first, min(first + self.depth, len(draft))):
+                key = (node, int(draft[i]))
+                if key not in child:
+                    if len(tokens) == room:
+                        break
+                    child[key] = len(tokens)
+                    tokens.append(int(draft[i]))
+                    parent.append(node)
+                    follow.append(i + 1)
+                node = child[key]
+        return tokens, parent, follow
+
+    def run(self, kv_start, ctx_len, first_tok, drafts: List[np.ndarray], n_steps: int) -> List[np.ndarray]:
+        """kv_start, ctx_len: cached rows as for ar_fallback, with room for n_steps tokens and a tree behind them; first_tok (host): the model's own tokens at
+        position ctx_len; drafts: the draft from the rejected token on.  Returns n_steps + 1 tokens an utterance, first_tok the first."""
+        with torch.cuda.stream(self.ctx.stream):
+            return self._run(kv_start, ctx_len, first_tok, drafts, n_steps)
+
+    def _run(self, kv_start, ctx_len, first_tok, drafts, n_steps):
+        ctx, dev = self.ctx, self.ctx.device
+        start, length = np.array(kv_start, dtype=np.int32), np.array(ctx_len, dtype=np.int32)
+        pos, done = length.copy(), [[] for _ in start]
+        token, at = [int(t) for t in first_tok], [0] * len(start)
+        k, _ = ctx.kv_tensors()
+        mass = None if self.most_rows is None else torch.zeros((k.shape[0], k.shape[2], k.shape[1]), device=dev)
+        before, cuts = (ctx._kv, int(k.shape[1])), 0
+        assert len(start) <= self.max_utts
+        while True:
+            live = [b for b in range(len(start)) if len(done[b]) < n_steps]
+            if not live:
+                break
+            if mass is not None and any(done) and max(length[live]) > self.most_rows:
+                mass = self._evict(live, start, length, mass, cuts % 2)
+                cuts += 1
+            trees = [self._tree(token[b], drafts[b], at[b], min(self.room, n_steps - len(done[b]))) for b in live]
+            ids = torch.tensor([t for x in trees for t in x[0]], dtype=torch.int32, device=dev)
+            cu, parent = np.cumsum([0] + [len(x[0]) for x in trees]), np.array([p for x in trees for p in x[1]])
+            h = ctx.verify_tree(ids, cu, parent, start[live], length[live], pos0=pos[live], kv_mass=mass)
+            acc = ctx.accept_tree(h, ids, cu, parent, self.tau, kv_start=start[live], ctx_len=length[live], kv_mass=mass)
+            n, path, greedy = acc["accept_len"].tolist(), acc["path"].tolist(), acc["greedy_tok"].tolist()
+            for i, b in enumerate(live):
+                nodes = path[cu[i]:cu[i] + n[i]]
+                done[b] += [trees[i][0][j] for j in nodes]
+                length[b] += n[i]
+                pos[b] += n[i]
+                token[b], at[b] = greedy[cu[i] + nodes[-1]], trees[i][2][nodes[-1]]
+        if cuts:
+            ctx.attach_kv_cache(*before)
+        return [np.array(d + [t], dtype=np.int32) for d, t in zip(done, token)]
+
+    def _evict(self, live, start, length, mass, turn):
+        """Cuts the live utterances into a cache of the fallback's own and attaches it; returns the weights of the rows there."""
+        ctx = self.ctx
+        k, v = ctx.kv_tensors()
+        if self.own[turn] is None:
+            self.own[turn] = torch.empty(ctx.kv_cache_bytes(self.slots), dtype=torch.uint8, device=ctx.device)
+        k_out, v_out = ctx.kv_tensors(self.own[turn], self.slots)
+        mass_out = torch.zeros((k.shape[0], k.shape[2], self.slots), device=ctx.device)
+        keep = np.where(length[live] > self.most_rows, self.keep_rows, length[live])
+        to = (np.arange(len(live)) * (self.most_rows + 2 * self.room)).astype(np.int32)
+        ctx.kv_evict(k, v, mass, start[live], length[live], keep, self.n_first, self.n_recent, k_out, v_out, to, mass_out=mass_out)
+        start[live], length[live] = to, keep
+        ctx.attach_kv_cache(self.own[turn], self.slots)
+        return mass_out
+
+
 class TwoPhaseDecoder:
     def __init__(self, ctx: Context, wl, logits: torch.Tensor, cu_frames, ctc_to_llm: torch.Tensor,
                  speech_all: torch.Tensor, cu_speech_all, prompt_all: torch.Tensor, cu_prompt_all,
-                 budget: int = 50000, mode: str = "resident", n_steps: int = 8):
+                 budget: int = 50000, mode: str = "resident", n_steps: int = 8, trees: Optional[dict] = None):
+        """trees: arguments of a TreeFallback (tau, depth, most_rows, ...) that continues the rejected utterances in place of ar_fallback."""
         assert mode in ("offload", "resident")
+        self.trees = None if trees is None else TreeFallback(ctx, len(cu_frames) - 1, **trees)
+        self.room = n_steps + 2 + (0 if trees is None else self.trees.room)        # slots an utterance needs behind its rows
         self.ctx, self.wl, self.mode, self.budget, self.n_steps = ctx, wl, mode, int(budget), int(n_steps)
         self.logits, self.table = logits, ctc_to_llm
         self.cu_frames = np.ascontiguousarray(cu_frames, dtype=np.int32)
@@ -55,7 +157,7 @@ class TwoPhaseDecoder:
         self.greedy_all = torch.empty(n_frames, dtype=torch.int32, device=dev)
         self.gate_out = None
         # K/V slots: every verified utterance keeps its rows (resident), or one fallback bin at a time (offload)
-        slots = (nS + nP + n_frames + self.B * (self.n_steps + 2)) if mode == "resident" else cap + self.B * (self.n_steps + 2)
+        slots = (nS + nP + n_frames + self.B * self.room) if mode == "resident" else cap + self.B * self.room
         ctx.set_kv_cache(int(slots))
         self.kv_slots = int(slots)
         self.host_g: Optional[torch.Tensor] = None       # pinned staging for the acoustic embeddings (offload mode)
@@ -93,7 +195,7 @@ class TwoPhaseDecoder:
             Mv = int(sel["cu_draft"][-1])
             ks = None
             if self.mode == "resident":
-                cap = (self.S + self.P + draft_len)[utts] + n_steps + 2
+                cap = (self.S + self.P + draft_len)[utts] + self.room
                 ks = (kv_next + np.concatenate([[0], np.cumsum(cap)[:-1]])).astype(np.int32)
                 kv_start[utts] = ks
                 kv_next += int(cap.sum())
@@ -146,7 +248,7 @@ class TwoPhaseDecoder:
                                              out={"speech": self.sel_buf["speech"][:0], "prompt": self.sel_buf["prompt"],
                                                   "draft_ids": self.sel_buf["draft_ids"]}, d_model=int(self.speech_all.shape[1]),
                                              dtype=self.speech_all.dtype)
-                cap = (self.S + self.P + A)[utts] + n_steps + 2
+                cap = (self.S + self.P + A)[utts] + self.room
                 ks = np.concatenate([[0], np.cumsum(cap)[:-1]]).astype(np.int32)
                 cl = ctx_len_all[utts]
                 Mv = int(sel["cu_draft"][-1])
@@ -154,6 +256,12 @@ class TwoPhaseDecoder:
                                         sel["cu_draft"], out=self.hv_buf[:Mv], kv_start=ks)
                 acc = ctx.accept_prefix(hv, sel["draft_ids"], sel["cu_draft"], tau_slm, want_greedy=True)
                 first = ctx.gather_i32(acc["greedy_tok"], sel["cu_draft"][1:] - 1)
+            if self.trees is not None:
+                f, ids = first.cpu().numpy(), g["draft_ctc"].cpu()
+                rest = [self.table.cpu()[ids[self.cu_frames[b] + A[b]:self.cu_frames[b] + draft_len[b]].long()].numpy() for b in utts]
+                for b, t in zip(utts, self.trees.run(ks, cl, f, rest, n_steps)):
+                    res["tokens"][int(b)] = t
+                continue
             toks = ctx.ar_fallback(ks, cl, first, n_steps)
             outs.append((utts, first, toks))
         for utts, first, toks in outs:

@@ -1443,9 +1443,9 @@ void tree_spans(int n, const int32_t* parent, uint32_t* span) {
         span[i] = (uint32_t)at | (uint32_t)(at + size[i]) << 16;
     }
 }
-// Query rows of an item: as many as the largest tree has, at most 64.  Ranges of keys: a range per item, unless that leaves most of the chip
+// Query rows of an item: as many as the largest tree has, at most 64 (fp32: 32, what its registers hold).  Ranges of keys: a range per item, unless that leaves most of the chip
 // without work; then about TREE_WORKGROUPS ranges in all.
-int tree_tile_rows(int dtype, int rows) { return dtype == SSD_F32 || rows <= 16 ? 16 : rows <= 32 ? 32 : 64; }
+int tree_tile_rows(int dtype, int rows) { return rows <= 16 ? 16 : rows <= 32 || dtype == SSD_F32 ? 32 : 64; }
 void tree_work(int B, const int32_t* kv_start, const int32_t* ctx_len, const int32_t* cu_nodes, int most, int n_q_heads, int n_kv_heads, int dtype, bool mass, TreeWork& w) {
     const int G = n_q_heads / n_kv_heads;
     w.tile_rows = tree_tile_rows(dtype, most * G);
@@ -1458,7 +1458,7 @@ void tree_work(int B, const int32_t* kv_start, const int32_t* ctx_len, const int
     }
     auto step_of = [](int64_t keys, int64_t pieces, int64_t unit) { return std::max<int64_t>(1, (keys + pieces * unit - 1) / (pieces * unit)) * unit; };
     const int64_t pieces = std::max(1, TREE_WORKGROUPS / n_kv_heads);
-    const int64_t step = dtype == SSD_F32 ? (int64_t)1 << 40 : std::max<int64_t>(TREE_SPLIT_KEYS, step_of(total, pieces, 128));
+    const int64_t step = std::max<int64_t>(TREE_SPLIT_KEYS, step_of(total, pieces, 128));
     const int64_t mass_step = step_of(per_row, pieces, TREE_MASS_KEYS);
     for (int b = 0; b < B; ++b) {
         const int n = cu_nodes[b + 1] - cu_nodes[b], R = n * G, keys = ctx_len[b] + n;

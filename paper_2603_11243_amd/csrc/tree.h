@@ -43,7 +43,7 @@ struct TreeAttnArgs {
     const uint32_t* spans;                   // per node: place in depth-first order, end of its subtree << 16
 };
 void launch_tree_attention(const TreeAttnArgs& a, hipStream_t st);
-constexpr int TREE_MASS_KEYS = 256;          // keys of an item of the weights: a multiple of these
+constexpr int TREE_MASS_KEYS = 128;          // keys of an item of the weights: a multiple of these
 constexpr int TREE_WORKGROUPS = 1024;        // long contexts are cut into about as many pieces in all, times K/V heads
 constexpr int TREE_SPLIT_KEYS = 256;         // a piece has at least as many keys
 

@@ -1,0 +1,266 @@
+// The same for fp32 caches, head_dim a multiple of 4 up to 128, on v_mfma_f32_16x16x4_f32 (fp32 products and sums): the layout of tree_attn.hip with
+// 16-key blocks.  A lane's four dims 16 c + 4 g .. of a key row are its elements of four products, in the same order for the queries; a
+// lane's scores of keys 4 g .. 4 g + 3 are its elements of the second product, key r of every group in product r.
+#include "tree_attn.h"
+
+namespace ssd {
+
+constexpr int TREE32_KEYS = 16;
+
+__device__ __forceinline__ f32x4_t mfma_16x16x4(float a, float b, const f32x4_t& c) { return __builtin_amdgcn_mfma_f32_16x16x4f32(a, b, c, 0, 0, 0); }
+
+// Rows of a block in operand registers: row lane % 16, dims 16 c + 4 (lane / 16) ..; dims from head_dim on are zero.
+template <int HD>
+__device__ __forceinline__ void load_rows32(f32x4_t (&x)[HD / 16], const float* row, int head_dim, int kg) {
+#pragma unroll
+    for (int c = 0; c < HD / 16; ++c) {
+        const int d = 16 * c + 4 * kg;
+        const f32x4_t v = *reinterpret_cast<const f32x4_t*>(row + (d < head_dim ? d : 0));
+        x[c] = d < head_dim ? v : (f32x4_t){0.f, 0.f, 0.f, 0.f};
+    }
+}
+
+template <int HD, int NT>
+__global__ void __launch_bounds__(64 * TREE_WAVES, 2) tree_attn32_kernel(TreeAttnArgs a) {
+    constexpr int ROW = HD * 4, BLOCK = TREE32_KEYS * ROW, STEP = TREE32_KEYS * TREE_WAVES, DT = HD / 16, TR = 16 * NT;
+    constexpr int ROW_CHUNKS = ROW / 16, V_ROWS = 64 / ROW_CHUNKS, V_LOADS = TREE32_KEYS / V_ROWS;
+    __shared__ __align__(1024) unsigned char v_s[TREE_WAVES][BLOCK];
+    __shared__ float2 ml_s[TREE_WAVES * TR];
+    __shared__ uint32_t span_s[MAX_TREE_NODES];
+    const int lane = threadIdx.x % 64, kg = lane / 16, dc = lane % 16;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
+    const int work = xcd_contiguous_index(blockIdx.x, gridDim.x);
+    const TreeItem t = a.items[work / a.n_kv_heads];
+    const int kvh = work % a.n_kv_heads, hd = a.head_dim;
+    const int G = a.n_q_heads / a.n_kv_heads, R = t.n_nodes * G;
+    const int last = max(t.k0, t.k1 - 1);                    // (a range without keys: any row)
+    const int n_spans = t.k1 > t.n_ctx ? t.n_nodes : 0;
+    for (int i = threadIdx.x; i < n_spans; i += 64 * TREE_WAVES) span_s[i] = a.spans[t.node0 + i];
+    const int64_t first = (int64_t)t.slot0 * a.slot_stride + kvh * a.head_stride;
+    const float* kbase = (const float*)a.k + first;
+    const float* vbase = (const float*)a.v + first;
+    f32x4_t kr[DT];
+    auto load_keys = [&](int k0) { load_rows32<HD>(kr, kbase + (int64_t)min(k0 + dc, last) * a.slot_stride, hd, kg); };
+    // values: the 16-byte chunks of row r permuted by r / 4, so that the four rows of a read lie in different banks; dims from head_dim on
+    // hold copies of the first ones (their outputs are not stored)
+    auto load_values = [&](int k0) {
+        const int r0 = min(k0, last), beyond = last - r0;
+        const __amdgpu_buffer_rsrc_t rsrc = make_rsrc(vbase + (int64_t)r0 * a.slot_stride);
+#pragma unroll
+        for (int i = 0; i < V_LOADS; ++i) {
+            const int row = V_ROWS * i + lane / ROW_CHUNKS, chunk = (lane % ROW_CHUNKS) ^ (row / 4 % 4 * 4);
+            const int off = min(row, beyond) * (int)a.slot_stride * 4 + (chunk * 4 < hd ? chunk * 16 : 0);
+            __builtin_amdgcn_raw_ptr_buffer_load_lds(rsrc, (lds_void_t*)(v_s[wave] + i * 1024), 16, off, 0, 0, 0);
+        }
+    };
+    int k0 = t.k0 + wave * TREE32_KEYS;
+    load_keys(k0);
+    f32x4_t qf[NT][DT];
+    const float sign = a.scale < 0.f ? -1.f : 1.f;
+#pragma unroll
+    for (int n = 0; n < NT; ++n) {
+        const int row = min(t.row0 + 16 * n + dc, R - 1);
+        load_rows32<HD>(qf[n], (const float*)a.q + (int64_t)(t.node0 + row / G) * a.q_stride + (kvh * G + row % G) * hd, hd, kg);
+#pragma unroll
+        for (int c = 0; c < DT; ++c) qf[n][c] *= sign;
+    }
+    const float sc = fabsf(a.scale) * LOG2E;
+    float m[NT], l[NT];
+    f32x4_t o[NT][DT];
+#pragma unroll
+    for (int n = 0; n < NT; ++n) {
+        m[n] = -F32_MOST;
+        l[n] = 0.f;
+#pragma unroll
+        for (int i = 0; i < DT; ++i) o[n][i] = (f32x4_t){0.f, 0.f, 0.f, 0.f};
+    }
+    __syncthreads();
+    load_values(k0);
+    const float* vr = reinterpret_cast<const float*>(v_s[wave]);
+    for (; k0 < t.k1; k0 += STEP) {
+        f32x4_t s[NT];
+#pragma unroll
+        for (int n = 0; n < NT; ++n) {
+            s[n] = (f32x4_t){0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+            for (int c = 0; c < DT; ++c)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) s[n] = mfma_16x16x4(kr[c][e], qf[n][c][e], s[n]);
+        }
+        const bool masked = k0 + TREE32_KEYS > min(t.n_ctx, t.k1);
+        if (masked) {
+            uint32_t key[4];
+#pragma unroll
+            for (int r = 0; r < 4; ++r) {
+                const int at = k0 + 4 * kg + r;
+                key[r] = at < t.n_ctx ? 0xffff0000u : at < t.k1 ? span_s[at - t.n_ctx] : 0u;
+            }
+#pragma unroll
+            for (int n = 0; n < NT; ++n) {
+                const uint32_t mine = span_s[min(t.row0 + 16 * n + dc, R - 1) / G];
+#pragma unroll
+                for (int r = 0; r < 4; ++r) s[n][r] = sees(mine, key[r]) ? s[n][r] : -INFINITY;
+            }
+        }
+        bool above = false;
+        float mx[NT];
+#pragma unroll
+        for (int n = 0; n < NT; ++n) {
+            mx[n] = fmaxf(fmaxf(s[n][0], s[n][1]), fmaxf(s[n][2], s[n][3]));
+            above |= mx[n] > m[n];
+        }
+        if (__any(above)) {
+#pragma unroll
+            for (int n = 0; n < NT; ++n) {
+                float top = fmaxf(mx[n], __shfl_xor(mx[n], 16));
+                top = fmaxf(m[n], fmaxf(top, __shfl_xor(top, 32)));
+                const float alpha = __builtin_amdgcn_exp2f((m[n] - top) * sc);
+                m[n] = top;
+                l[n] *= alpha;
+#pragma unroll
+                for (int i = 0; i < DT; ++i) o[n][i] *= alpha;
+            }
+        }
+#pragma unroll
+        for (int n = 0; n < NT; ++n) {
+            const float base = fminf(-m[n] * sc, F32_MOST);
+#pragma unroll
+            for (int r = 0; r < 4; ++r) {
+                s[n][r] = s[n][r] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(fmaf(s[n][r], sc, base));
+                l[n] += s[n][r];
+            }
+        }
+        __builtin_amdgcn_sched_barrier(0);
+        __builtin_amdgcn_s_waitcnt(0x0F70);
+        __builtin_amdgcn_sched_barrier(0);
+        load_keys(k0 + STEP);
+        // A value that is not finite would reach the rows that do not see it as 0 times infinity: as in tree_attn.hip, the products run on the
+        // others, and two more count the infinities of either sign (a NaN as both) that rows with a probability meet.
+#pragma unroll
+        for (int i = 0; i < DT; ++i) {
+            float v[4];
+            bool odd = false;
+#pragma unroll
+            for (int r = 0; r < 4; ++r) {
+                v[r] = vr[(4 * kg + r) * HD + ((16 * i + dc) ^ (kg * 16))];
+                odd |= !(fabsf(v[r]) <= F32_MOST);
+            }
+            if (masked && __any(odd)) {
+#pragma unroll
+                for (int n = 0; n < NT; ++n) {
+                    f32x4_t up = {0.f, 0.f, 0.f, 0.f}, down = up;
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) {
+                        const float there = s[n][r] > 0.f || s[n][r] != s[n][r] ? 1.f : 0.f;
+                        up = mfma_16x16x4(!(v[r] <= F32_MOST) ? 1.f : 0.f, there, up);
+                        down = mfma_16x16x4(!(v[r] >= -F32_MOST) ? 1.f : 0.f, there, down);
+                    }
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) o[n][i][r] += (up[r] > 0.f ? INFINITY : 0.f) - (down[r] > 0.f ? INFINITY : 0.f);
+                }
+#pragma unroll
+                for (int r = 0; r < 4; ++r) v[r] = fabsf(v[r]) <= F32_MOST ? v[r] : 0.f;
+            }
+#pragma unroll
+            for (int n = 0; n < NT; ++n)
+#pragma unroll
+                for (int r = 0; r < 4; ++r) o[n][i] = mfma_16x16x4(v[r], s[n][r], o[n][i]);
+        }
+        __builtin_amdgcn_s_waitcnt(0xC07F);                  // the reads of this block are done
+        __builtin_amdgcn_sched_barrier(0);
+        load_values(k0 + STEP);
+    }
+    __builtin_amdgcn_sched_barrier(0);
+    __builtin_amdgcn_s_waitcnt(0x0F70);                      // the values behind the last block: they land where the output goes
+    __builtin_amdgcn_sched_barrier(0);
+    merge_wavefronts<SSD_F32, HD, NT>(a, t, kvh, m, l, o, sc, 0.f, reinterpret_cast<float*>(v_s), ml_s);
+}
+
+constexpr int MASS32_ROWS = 64;
+
+template <int HD>
+__global__ void __launch_bounds__(64 * TREE_WAVES, 2) tree_mass32_kernel(TreeAttnArgs a) {
+    constexpr int STEP = TREE32_KEYS * TREE_WAVES, DT = HD / 16, CHUNKS = HD / 4;
+    __shared__ __align__(1024) float q_s[MASS32_ROWS * HD];
+    __shared__ float lse_s[MASS32_ROWS];
+    __shared__ uint32_t row_span[MASS32_ROWS], span_s[MAX_TREE_NODES];
+    const int lane = threadIdx.x % 64, kg = lane / 16, dc = lane % 16;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
+    const int work = xcd_contiguous_index(blockIdx.x, gridDim.x);
+    const TreeItem t = a.mass_items[work / a.n_kv_heads];
+    const int kvh = work % a.n_kv_heads, hd = a.head_dim;
+    const int G = a.n_q_heads / a.n_kv_heads, R = t.n_nodes * G, last = t.k1 - 1;
+    const float* kbase = (const float*)a.k + (int64_t)t.slot0 * a.slot_stride + kvh * a.head_stride;
+    f32x4_t kr[DT];
+    auto load_keys = [&](int k0) { load_rows32<HD>(kr, kbase + (int64_t)min(k0 + dc, last) * a.slot_stride, hd, kg); };
+    const int first = t.k0 + wave * TREE32_KEYS;
+    load_keys(first);
+    if (t.k1 > t.n_ctx)
+        for (int i = threadIdx.x; i < t.n_nodes; i += 64 * TREE_WAVES) span_s[i] = a.spans[t.node0 + i];
+    const float sc = fabsf(a.scale) * LOG2E, sign = a.scale < 0.f ? -1.f : 1.f;
+    for (int r0 = 0; r0 < R; r0 += MASS32_ROWS) {
+        const int rows = min(MASS32_ROWS, R - r0), tiles = (rows + 15) / 16;
+        if (r0) __syncthreads();
+        for (int i = threadIdx.x; i < tiles * 16 * CHUNKS; i += 64 * TREE_WAVES) {
+            const int r = i / CHUNKS, c = i % CHUNKS, row = min(r0 + r, R - 1);
+            f32x4_t w = {0.f, 0.f, 0.f, 0.f};
+            if (c * 4 < hd) w = *reinterpret_cast<const f32x4_t*>((const float*)a.q + (int64_t)(t.node0 + row / G) * a.q_stride + (kvh * G + row % G) * hd + c * 4);
+            *reinterpret_cast<f32x4_t*>(q_s + r * HD + (c ^ (r & 15)) * 4) = w * sign;
+        }
+        for (int r = threadIdx.x; r < tiles * 16; r += 64 * TREE_WAVES) {
+            const int row = min(r0 + r, R - 1);
+            lse_s[r] = r < rows ? a.lse[(int64_t)(t.node0 + row / G) * a.n_q_heads + kvh * G + row % G] * -LOG2E : -INFINITY;   // (rows behind the last: no weight)
+            row_span[r] = r < rows ? a.spans[t.node0 + row / G] : 0xffffu;
+        }
+        __syncthreads();
+        if (r0) load_keys(first);
+        for (int k0 = first; k0 < t.k1; k0 += STEP) {
+            f32x4_t acc[1] = {(f32x4_t){0.f, 0.f, 0.f, 0.f}};
+            const bool masked = k0 + TREE32_KEYS > t.n_ctx;
+            uint32_t key[4];
+            if (masked)
+#pragma unroll
+                for (int r = 0; r < 4; ++r) {
+                    const int at = k0 + 4 * kg + r;
+                    key[r] = at < t.n_ctx ? 0xffff0000u : at < t.k1 ? span_s[at - t.n_ctx] : 0u;
+                }
+            for (int n = 0; n < tiles; ++n) {
+                const int r = 16 * n + dc;
+                f32x4_t s = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+                for (int c = 0; c < DT; ++c) {
+                    const f32x4_t q = *reinterpret_cast<const f32x4_t*>(q_s + r * HD + ((4 * c + kg) ^ (r & 15)) * 4);
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) s = mfma_16x16x4(kr[c][e], q[e], s);
+                }
+                const float base = lse_s[r];
+                const uint32_t mine = row_span[r];
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    const float p = __builtin_amdgcn_exp2f(fmaf(s[e], sc, base));
+                    acc[0][e] += masked && !sees(mine, key[e]) ? 0.f : p;
+                }
+            }
+            load_keys(k0 + STEP);
+            add_mass(a, t, kvh, k0, r0 == 0, acc);
+        }
+    }
+}
+
+template <int HD>
+static void launch32(const TreeAttnArgs& a, hipStream_t st) {
+    const dim3 grid(a.n_items * a.n_kv_heads);
+    if (a.tile_rows == 16) hipLaunchKernelGGL((tree_attn32_kernel<HD, 1>), grid, dim3(64 * TREE_WAVES), 0, st, a);
+    else hipLaunchKernelGGL((tree_attn32_kernel<HD, 2>), grid, dim3(64 * TREE_WAVES), 0, st, a);
+    constexpr int ROWS = 256 / (HD / 4);
+    if (a.n_joins)
+        hipLaunchKernelGGL((tree_join_kernel<SSD_F32, HD>), dim3(a.n_joins, a.n_kv_heads, (a.tile_rows + ROWS - 1) / ROWS), dim3(256), 0, st, a, a.tile_rows, 0.f);
+    if (a.mass) hipLaunchKernelGGL((tree_mass32_kernel<HD>), dim3(a.n_mass_items * a.n_kv_heads), dim3(64 * TREE_WAVES), 0, st, a);
+}
+
+void launch_tree_attention32(const TreeAttnArgs& a, hipStream_t st) {
+    if (a.head_dim <= 64) launch32<64>(a, st);
+    else launch32<128>(a, st);
+}
+
+}  // namespace ssd

@@ -1382,6 +1382,7 @@ bool ranges_distinct(int B, const int32_t* start, const std::vector<int64_t>& le
 int check_trees(ssd_ctx* c, const char* what, int B, const int32_t* cu_nodes, const int32_t* parent, int& most) {
     if (!cu_nodes) return fail(c, SSD_EINVAL, "%s: NULL cu_nodes", what);
     if (B <= 0) return fail(c, SSD_EINVAL, "%s: B must be positive (got %d)", what, B);
+    if (B > 65535) return fail(c, SSD_ESHAPE, "%s: more than 65535 utterances; split the batch", what);
     if (!check_cu(cu_nodes, B, false)) return fail(c, SSD_EINVAL, "%s: cu_nodes must start at 0 and be non-decreasing", what);
     if (cu_nodes[B] && !parent) return fail(c, SSD_EINVAL, "%s: NULL parent", what);
     most = 0;
@@ -1424,10 +1425,10 @@ int place_meta(ssd_ctx* c, const std::vector<uint32_t>& meta, void* dev) {
     return SSD_OK;
 }
 
+// What a tree_attention call does: the arguments of its launches but for pointers, and the words they read.
 struct TreeWork {
-    int tile_rows, n_parts = 0;
-    std::vector<TreeItem> items, mass_items;
-    std::vector<TreeJoin> joins;
+    TreeAttnArgs a;
+    std::vector<uint32_t> words;
 };
 // Nodes in depth-first order: a node's place, the end of its subtree.
 void tree_spans(int n, const int32_t* parent, uint32_t* span) {
@@ -1443,89 +1444,95 @@ void tree_spans(int n, const int32_t* parent, uint32_t* span) {
         span[i] = (uint32_t)at | (uint32_t)(at + size[i]) << 16;
     }
 }
-// Query rows of an item: as many as the largest tree has, at most 64 (fp32: 32, what its registers hold).  Ranges of keys: a range per item, unless that leaves most of the chip
-// without work; then about TREE_WORKGROUPS ranges in all.
-int tree_tile_rows(int dtype, int rows) { return rows <= 16 ? 16 : rows <= 32 || dtype == SSD_F32 ? 32 : 64; }
-void tree_work(int B, const int32_t* kv_start, const int32_t* ctx_len, const int32_t* cu_nodes, int most, int n_q_heads, int n_kv_heads, int dtype, bool mass, TreeWork& w) {
-    const int G = n_q_heads / n_kv_heads;
-    w.tile_rows = tree_tile_rows(dtype, most * G);
+// Query rows of an item of work: as many as the largest tree has, in one of the shapes of the kernels.  Up to TREE_KEY_ROWS rows the wavefronts of a workgroup
+// split the keys; fp32 has no other kernel.
+int tree_tile_rows(int dtype, int rows) { return rows <= 16 ? 16 : rows <= TREE_KEY_ROWS || dtype == SSD_F32 ? TREE_KEY_ROWS : rows <= 64 ? 64 : 128; }
+// Ranges of keys: one per item, unless that leaves most of the chip without work or an utterance is longer than its share; then pieces of such a share.
+void tree_work(int B, const int32_t* kv_start, const int32_t* ctx_len, const int32_t* cu_nodes, const int32_t* parent, int most, int n_q_heads, const ssd_kv_view& kv,
+               bool mass, TreeWork& w) {
+    const int n_kv_heads = kv.n_kv_heads, G = n_q_heads / n_kv_heads, rows = tree_tile_rows(kv.dtype, most * G);
     int64_t total = 0, per_row = 0;                          // keys of all items, of all utterances
     for (int b = 0; b < B; ++b) {
         const int n = cu_nodes[b + 1] - cu_nodes[b];
-        const int64_t keys = (int64_t)ctx_len[b] + n;
-        per_row += n ? keys : 0;
-        total += keys * ((n * G + w.tile_rows - 1) / w.tile_rows);
+        const int64_t keys = n ? (int64_t)ctx_len[b] + n : 0;
+        per_row += keys;
+        total += keys * ((n * G + rows - 1) / rows);
     }
     auto step_of = [](int64_t keys, int64_t pieces, int64_t unit) { return std::max<int64_t>(1, (keys + pieces * unit - 1) / (pieces * unit)) * unit; };
     const int64_t pieces = std::max(1, TREE_WORKGROUPS / n_kv_heads);
-    const int64_t step = std::max<int64_t>(TREE_SPLIT_KEYS, step_of(total, pieces, 128));
-    const int64_t mass_step = step_of(per_row, pieces, TREE_MASS_KEYS);
-    for (int b = 0; b < B; ++b) {
-        const int n = cu_nodes[b + 1] - cu_nodes[b], R = n * G, keys = ctx_len[b] + n;
-        if (!n) continue;
-        const int tiles = (R + w.tile_rows - 1) / w.tile_rows, parts = (int)((keys + step - 1) / step), part0 = w.n_parts;
-        for (int p = 0; p < parts; ++p)                      // tiles of the same keys one behind the other: they meet in an L2
-            for (int t = 0; t < tiles; ++t) {
-                const int row0 = t * w.tile_rows, node = (std::min(R, row0 + w.tile_rows) - 1) / G;       // no row of the tile sees a later node
-                const int k0 = (int)(p * step), k1 = (int)std::min<int64_t>(ctx_len[b] + node + 1, (p + 1) * step);
-                w.items.push_back(TreeItem{kv_start[b], ctx_len[b], n, cu_nodes[b], row0, k0, std::max(k0, k1), parts > 1 ? w.n_parts++ : -1});
-            }
-        for (int t = 0; parts > 1 && t < tiles; ++t) w.joins.push_back(TreeJoin{n, cu_nodes[b], t * w.tile_rows, part0 + t, tiles, parts});
-        for (int64_t k = 0; mass && k < keys; k += mass_step)
-            w.mass_items.push_back(TreeItem{kv_start[b], ctx_len[b], n, cu_nodes[b], 0, (int)k, (int)std::min<int64_t>(keys, k + mass_step), -1});
+    const int64_t step = std::min<int64_t>(std::max<int64_t>(TREE_SPLIT_KEYS, step_of(total, pieces, 256)), 0x7fffff00);
+    const int64_t mass_step = std::min<int64_t>(step_of(per_row, pieces, TREE_MASS_KEYS), 0x7fffff00);
+    std::vector<uint32_t>& v = w.words;
+    TreeAttnArgs& a = w.a;
+    v.reserve((size_t)B * 8 + cu_nodes[B] + 256);
+    for (int b = 0; b < B; ++b) { v.push_back(kv_start[b]); v.push_back(ctx_len[b]); }
+    a.cu = (int)v.size();
+    v.insert(v.end(), cu_nodes, cu_nodes + B + 1);
+    a.items = (int)v.size();
+    a.n_items = a.n_parts = a.n_joins = a.n_mass = 0;
+    auto tiles_of = [&](int b) { return ((cu_nodes[b + 1] - cu_nodes[b]) * G + rows - 1) / rows; };
+    auto parts_of = [&](int b) { return ((int64_t)ctx_len[b] + cu_nodes[b + 1] - cu_nodes[b] + step - 1) / step; };
+    for (int cut = 1; cut >= 0; --cut)
+        for (int b = 0; b < B; ++b) {
+            const int tiles = tiles_of(b), parts = (int)parts_of(b);
+            if (!tiles || (parts > 1) != (cut == 1)) continue;
+            for (int p = 0; p < parts; ++p)                  // tiles of the same keys one behind the other: they meet in an L2
+                for (int t = 0; t < tiles; ++t) { v.push_back((uint32_t)b | (uint32_t)t << 16); v.push_back(p); }
+            a.n_items += parts * tiles;
+            if (cut) a.n_parts = a.n_items;
+        }
+    a.joins = (int)v.size();
+    for (int b = 0, first = 0; b < B; ++b) {
+        const int tiles = tiles_of(b), parts = (int)parts_of(b);
+        if (!tiles || parts <= 1) continue;
+        for (int t = 0; t < tiles; ++t) { v.push_back((uint32_t)b | (uint32_t)t << 16); v.push_back(first + t); v.push_back(parts); }
+        a.n_joins += tiles;
+        first += parts * tiles;
     }
+    a.mass_items = (int)v.size();
+    for (int b = 0; mass && b < B; ++b) {
+        const int64_t n = cu_nodes[b + 1] - cu_nodes[b], keys = ctx_len[b] + n;
+        for (int64_t p = 0; n && p * mass_step < keys; ++p, ++a.n_mass) v.push_back((uint32_t)b | (uint32_t)p << 16);
+    }
+    a.spans = (int)v.size();
+    v.resize(v.size() + cu_nodes[B]);
+    for (int b = 0; b < B; ++b) tree_spans(cu_nodes[b + 1] - cu_nodes[b], parent + cu_nodes[b], v.data() + a.spans + cu_nodes[b]);
+    a.n_q_heads = n_q_heads; a.n_kv_heads = n_kv_heads; a.head_dim = kv.head_dim; a.dtype = kv.dtype;
+    a.slot_stride = kv.slot_stride; a.head_stride = n_kv_heads > 1 ? kv.head_stride : 0;
+    a.tile_rows = rows; a.step = (int)step; a.mass_step = (int)mass_step;
 }
-struct TreePlan { size_t spans, items, mass_items, joins, meta_bytes, lse, part_o, part_ml, total; };
-TreePlan plan_tree(int64_t nodes, int64_t n_items, int64_t n_mass_items, int64_t n_joins, int64_t lse_values, int64_t part_rows, int head_dim) {
+struct TreePlan { size_t words, lse, part_o, part_ml, total; };
+TreePlan plan_tree(int64_t n_words, int64_t lse_values, int64_t part_rows, int head_dim) {
     TreePlan p;
     size_t o = 0;
-    p.spans = o; o = align_up(o + (size_t)nodes * 4);
-    p.items = o; o = align_up(o + (size_t)n_items * sizeof(TreeItem));
-    p.mass_items = o; o = align_up(o + (size_t)n_mass_items * sizeof(TreeItem));
-    p.joins = o; o = align_up(o + (size_t)n_joins * sizeof(TreeJoin));
-    p.meta_bytes = o;
+    p.words = o; o = align_up(o + (size_t)n_words * 4);
     p.lse = o; o = align_up(o + (size_t)lse_values * 4);
-    p.part_o = o; o = align_up(o + (size_t)(part_rows * head_dim) * 4);
+    p.part_o = o; o = align_up(o + (size_t)(part_rows * (head_dim <= 64 ? 64 : 128)) * 4);
     p.part_ml = o; o = align_up(o + (size_t)part_rows * sizeof(float2));
     p.total = o;
     return p;
 }
-TreePlan plan_tree(const TreeWork& w, int64_t nodes, int n_q_heads, const ssd_kv_view& kv, bool own_lse) {
-    return plan_tree(nodes, w.items.size(), w.mass_items.size(), w.joins.size(), own_lse ? nodes * n_q_heads : 0,
-                     (int64_t)w.n_parts * kv.n_kv_heads * w.tile_rows, (kv.head_dim + 63) / 64 * 64);
+TreePlan plan_tree(const TreeWork& w, int64_t nodes, bool own_lse) {
+    return plan_tree(w.words.size(), own_lse ? nodes * w.a.n_q_heads : 0, (int64_t)w.a.n_parts * w.a.n_kv_heads * w.a.tile_rows, w.a.head_dim);
 }
 // The same for all trees of at most max_nodes nodes in all.  An item has at least one row, or is one of the pieces of a cut context: a context is
 // cut only where its keys, times its tiles, are more than one of TREE_WORKGROUPS / n_kv_heads shares, so that there are at most twice as many pieces.
 size_t max_tree_bytes(int n_q_heads, int n_kv_heads, int head_dim, int64_t max_nodes, int64_t max_utts) {
-    const int64_t G = (n_q_heads + n_kv_heads - 1) / n_kv_heads, pieces = std::max(1, TREE_WORKGROUPS / n_kv_heads);
-    const int64_t cut = 2 * pieces, rows = max_nodes * G;
-    // pieces that are not cut have a row each; a tile of 64 rows is used only for trees of more than 32
-    return plan_tree(max_nodes, rows + cut, max_utts + pieces, rows, max_nodes * n_q_heads, cut * n_kv_heads * std::min<int64_t>(64, 2 * std::max<int64_t>(rows, 16)),
-                     (head_dim + 63) / 64 * 64).total;
+    const int64_t G = (n_q_heads + n_kv_heads - 1) / n_kv_heads, cut = 2 * std::max(1, TREE_WORKGROUPS / n_kv_heads), rows = max_nodes * G;
+    const int64_t tile = rows <= 16 ? 16 : rows <= TREE_KEY_ROWS ? TREE_KEY_ROWS : rows <= 64 ? 64 : 128;
+    return plan_tree(3 * max_utts + 1 + 2 * (rows + cut) + 3 * rows + max_utts + cut + max_nodes, max_nodes * n_q_heads, cut * n_kv_heads * tile, head_dim).total;
 }
-void tree_meta(const TreePlan& p, const TreeWork& w, int B, const int32_t* cu_nodes, const int32_t* parent, uint32_t* meta) {
-    for (int b = 0; b < B; ++b) tree_spans(cu_nodes[b + 1] - cu_nodes[b], parent + cu_nodes[b], meta + p.spans / 4 + cu_nodes[b]);
-    memcpy(meta + p.items / 4, w.items.data(), w.items.size() * sizeof(TreeItem));
-    memcpy(meta + p.mass_items / 4, w.mass_items.data(), w.mass_items.size() * sizeof(TreeItem));
-    memcpy(meta + p.joins / 4, w.joins.data(), w.joins.size() * sizeof(TreeJoin));
-}
-TreeAttnArgs tree_args(const TreePlan& p, const TreeWork& w, char* ws, const ssd_kv_view& kv, const void* q, int64_t q_stride, int n_q_heads, float scale,
-                       void* out, float* lse, float* mass) {
-    TreeAttnArgs a;
+void run_tree_attention(ssd_ctx* c, TreeWork& w, const TreePlan& p, char* ws, bool in_args, const void* k, const void* v, int64_t slots, const void* q, int64_t q_stride,
+                        float scale, void* out, float* lse, float* mass) {
+    TreeAttnArgs& a = w.a;
     a.q = q; a.q_stride = q_stride;
-    a.k = kv.k; a.v = kv.v; a.slot_stride = kv.slot_stride; a.head_stride = kv.n_kv_heads > 1 ? kv.head_stride : 0;
-    a.n_q_heads = n_q_heads; a.n_kv_heads = kv.n_kv_heads; a.head_dim = kv.head_dim; a.dtype = kv.dtype;
+    a.k = k; a.v = v;
     a.scale = scale;
     a.out = out;
     a.lse = lse ? lse : mass ? reinterpret_cast<float*>(ws + p.lse) : nullptr;
-    a.mass = mass; a.mass_stride = kv.slots;
-    a.tile_rows = w.tile_rows;
-    a.items = reinterpret_cast<const TreeItem*>(ws + p.items); a.n_items = (int)w.items.size();
-    a.mass_items = reinterpret_cast<const TreeItem*>(ws + p.mass_items); a.n_mass_items = (int)w.mass_items.size();
-    a.joins = reinterpret_cast<const TreeJoin*>(ws + p.joins); a.n_joins = (int)w.joins.size();
+    a.mass = mass; a.mass_stride = slots;
     a.part_o = reinterpret_cast<float*>(ws + p.part_o); a.part_ml = reinterpret_cast<float2*>(ws + p.part_ml);
-    a.spans = reinterpret_cast<const uint32_t*>(ws + p.spans);
-    return a;
+    launch_tree_attention(a, in_args ? w.words.data() : nullptr, (int)w.words.size(), reinterpret_cast<const uint32_t*>(ws + p.words), c->stream);
 }
 
 struct PathPlan { size_t parent, meta_bytes; };
@@ -1585,7 +1592,7 @@ VerifyTreePlan plan_verify_tree(const ssd_model_cfg& c, int64_t N, const TreePla
     p.pos = o; o = align_up(o + (size_t)N * 4);
     p.row_slot = o; o = align_up(o + (size_t)N * 4);
     p.tree = o;
-    p.meta_bytes = o + t.meta_bytes;
+    p.meta_bytes = o + t.lse;                                // the words come first
     o += t.total;
     p.x = o; o = align_up(o + (size_t)(N * d) * 4);
     p.a = o; o = align_up(o + (size_t)(N * d) * es);
@@ -1653,24 +1660,26 @@ int tree_attention(ssd_ctx* ctx, const void* q, int64_t q_stride, int n_q_heads,
     const int64_t N = cu_nodes[B], dq = (int64_t)n_q_heads * kv->head_dim, es = (int64_t)kv_elem(kv->dtype);
     if (kv->n_layers != 1) return fail(ctx, SSD_EINVAL, "tree_attention: a cache of one layer is needed (got %d)", kv->n_layers);
     if (n_q_heads <= 0 || n_q_heads % kv->n_kv_heads) return fail(ctx, SSD_ESHAPE, "tree_attention: n_q_heads must be a multiple of n_kv_heads");
-    if (n_q_heads > 65535) return fail(ctx, SSD_ESHAPE, "tree_attention: more than 65535 query heads");
+    if (n_q_heads > 65535 || n_q_heads / kv->n_kv_heads > 512) return fail(ctx, SSD_ESHAPE, "tree_attention: more than 65535 query heads, or 512 per K/V head");
     if (!std::isfinite(scale)) return fail(ctx, SSD_EINVAL, "tree_attention: scale is not finite");
     if (N == 0) return SSD_OK;
     if (!q || !out) return fail(ctx, SSD_EINVAL, "tree_attention: NULL data pointer");
     if (q_stride < dq || q_stride > (int64_t)1 << 40 || q_stride * es % 16 || ((uintptr_t)q | (uintptr_t)out) & 15)
         return fail(ctx, SSD_EINVAL, "tree_attention: rows of q and out must begin at multiples of 16 bytes, q_stride be at least n_q_heads * head_dim");
     TreeWork w;
-    tree_work(B, kv_start, ctx_len, cu_nodes, most, n_q_heads, kv->n_kv_heads, kv->dtype, mass != nullptr, w);
-    const TreePlan p = plan_tree(w, N, n_q_heads, *kv, mass && !lse);
+    tree_work(B, kv_start, ctx_len, cu_nodes, parent, most, n_q_heads, *kv, mass != nullptr, w);
+    const TreePlan p = plan_tree(w, N, mass && !lse);
     if (!ctx->ws || ctx->ws_bytes < p.total)
         return fail(ctx, SSD_EWORKSPACE, "tree_attention: workspace of %zu bytes needed, %zu set", p.total, ctx->ws_bytes);
-    std::vector<uint32_t> meta(p.meta_bytes / 4);
-    tree_meta(p, w, B, cu_nodes, parent, meta.data());
-    rc = place_meta(ctx, meta, ctx->ws);
-    if (rc != SSD_OK) return rc;
+    char* ws = static_cast<char*>(ctx->ws);
+    const bool in_args = w.words.size() <= MetaWords::WORDS;
+    if (!in_args) {
+        rc = place_meta(ctx, w.words, ws + p.words);
+        if (rc != SSD_OK) return rc;
+    }
     {
         ProfScope ps(ctx, SSD_PROF_ATTN);
-        launch_tree_attention(tree_args(p, w, static_cast<char*>(ctx->ws), *kv, q, q_stride, n_q_heads, scale, out, lse, mass), ctx->stream);
+        run_tree_attention(ctx, w, p, ws, in_args, kv->k, kv->v, kv->slots, q, q_stride, scale, out, lse, mass);
     }
     HIP_TRY(ctx, hipGetLastError());
     return SSD_OK;
@@ -1773,7 +1782,7 @@ size_t ssd_verify_tree_workspace_bytes(const ssd_ctx* ctx, int64_t max_nodes, in
     if (!ctx || !ctx->has_model || max_nodes < 0 || max_utts < 0) return 0;
     const ssd_model_cfg& m = ctx->cfg;
     TreePlan t;
-    t.meta_bytes = t.total = max_tree_bytes(m.n_q_heads, m.n_kv_heads, m.head_dim, max_nodes, max_utts);
+    t.lse = t.total = max_tree_bytes(m.n_q_heads, m.n_kv_heads, m.head_dim, max_nodes, max_utts);
     return std::max(plan_verify_tree(m, max_nodes, t).total, plan_accept_tree(m, max_nodes, 2 * max_nodes, max_utts).total) + 256;
 }
 
@@ -1799,8 +1808,8 @@ int verify_tree(ssd_ctx* ctx, const int32_t* node_ids, int B, const int32_t* cu_
                         (long long)N, (long long)widest);
     }
     TreeWork w;
-    tree_work(B, kv_start, ctx_len, cu_nodes, most, m.n_q_heads, m.n_kv_heads, view.dtype, kv_mass != nullptr, w);
-    const TreePlan t = plan_tree(w, N, m.n_q_heads, view, kv_mass != nullptr);
+    tree_work(B, kv_start, ctx_len, cu_nodes, parent, most, m.n_q_heads, view, kv_mass != nullptr, w);
+    const TreePlan t = plan_tree(w, N, kv_mass != nullptr);
     const VerifyTreePlan p = plan_verify_tree(m, N, t);
     if (!ctx->ws || ctx->ws_bytes < p.total)
         return fail(ctx, SSD_EWORKSPACE, "verify_tree: workspace of %zu bytes needed, %zu set", p.total, ctx->ws_bytes);
@@ -1819,7 +1828,7 @@ int verify_tree(ssd_ctx* ctx, const int32_t* node_ids, int B, const int32_t* cu_
             row_slot[i] = kv_start[b] + ctx_len[b] + (i - cu_nodes[b]);
         }
     }
-    tree_meta(t, w, B, cu_nodes, parent, meta.data() + p.tree / 4);
+    memcpy(meta.data() + p.tree / 4, w.words.data(), w.words.size() * 4);
     rc = place_meta(ctx, meta, ctx->ws);
     if (rc != SSD_OK) return rc;
     char* ws = static_cast<char*>(ctx->ws);
@@ -1847,13 +1856,13 @@ int verify_tree(ssd_ctx* ctx, const int32_t* node_ids, int B, const int32_t* cu_
     for (int l = 0; l < m.n_layers; ++l) {
         view.k = kv_k(ctx, l);
         view.v = kv_v(ctx, l);
-        const TreeAttnArgs ta = tree_args(t, w, ws + p.tree, view, qkv, dq + 2 * dkv, m.n_q_heads, scale, att, nullptr,
-                                          kv_mass ? kv_mass + (int64_t)l * m.n_kv_heads * ctx->kv_slots : nullptr);
+        float* mass = kv_mass ? kv_mass + (int64_t)l * m.n_kv_heads * ctx->kv_slots : nullptr;
+        auto attention = [&] { run_tree_attention(ctx, w, t, ws + p.tree, false, view.k, view.v, ctx->kv_slots, qkv, dq + 2 * dkv, scale, att, nullptr, mass); };
         if (m.dtype == SSD_BF16) {
             { ProfScope ps(ctx, SSD_PROF_OTHER); launch_rmsnorm(m.dtype, x, ctx->norm_attn[l], nullptr, Ni, d, m.rms_eps, a, partials, pending, stride, ctx->dev_flags, ctx->bf16_ops, st); }
             { ProfScope ps(ctx, SSD_PROF_GEMM_QKV); launch_gemm_qkv_rope((const uint16_t*)a, (const uint16_t*)ctx->wqkv[l], ctx->s_qkv[l], (uint16_t*)qkv, d_pos, ctx->rope_tab, Ni, d, dq, dkv, ctx->ds_qkv[l],
                                                                          d_slot, (uint16_t*)view.k, (uint16_t*)view.v, rope_rows, ctx->dev_flags, ctx->bf16_ops, st); }
-            { ProfScope ps(ctx, SSD_PROF_ATTN); launch_tree_attention(ta, st); }
+            { ProfScope ps(ctx, SSD_PROF_ATTN); attention(); }
             { ProfScope ps(ctx, SSD_PROF_GEMM_O); pending = launch_gemm_residual((const uint16_t*)att, (const uint16_t*)ctx->wo[l], ctx->s_o[l], x, partials, Ni, d, dq, ctx->ds_o[l], ctx->bf16_ops, st); }
             { ProfScope ps(ctx, SSD_PROF_OTHER); launch_rmsnorm(m.dtype, x, ctx->norm_mlp[l], nullptr, Ni, d, m.rms_eps, a, partials, pending, stride, ctx->dev_flags, ctx->bf16_ops, st); }
             { ProfScope ps(ctx, SSD_PROF_GEMM_GATE_UP); launch_gemm_swiglu((const uint16_t*)a, (const uint16_t*)ctx->wgu[l], ctx->s_gu[l], (uint16_t*)h, Ni, m.d_ff, d, ctx->ds_gu[l], ctx->dev_flags, ctx->bf16_ops, st); }
@@ -1861,7 +1870,7 @@ int verify_tree(ssd_ctx* ctx, const int32_t* node_ids, int B, const int32_t* cu_
         } else {
             launch_gemm_f32_qkv(x, (const float*)ctx->norm_attn[l], m.rms_eps, (const float*)ctx->wqkv[l], (float*)qkv, d_pos, ctx->rope_tab, Ni, d, dq, dkv, m.head_dim,
                                 d_slot, (float*)view.k, (float*)view.v, st);
-            launch_tree_attention(ta, st);
+            attention();
             launch_gemm_f32_residual((const float*)att, (const float*)ctx->wo[l], x, Ni, d, dq, nullptr, nullptr, st);
             launch_gemm_f32_swiglu(x, (const float*)ctx->norm_mlp[l], m.rms_eps, (const float*)ctx->wgu[l], (float*)h, Ni, m.d_ff, d, nullptr, st);
             launch_gemm_f32_residual((const float*)h, (const float*)ctx->w_down[l], x, Ni, d, m.d_ff, nullptr, nullptr, st);

@@ -9,43 +9,42 @@ namespace ssd {
 
 constexpr int MAX_TREE_NODES = SSD_MAX_TREE_NODES;
 
-// Query rows of one K/V head are numbered node * G + head of the group.  Keys k0 .. k1 - 1 (rows of the utterance: n_ctx cached ones, then
-// the nodes) for rows row0 .. of the utterance.
-struct TreeItem {
-    int32_t slot0, n_ctx, n_nodes, node0;    // first cache slot, cached rows, nodes, first node of the utterance in the call
-    int32_t row0, k0, k1, part;
-};
-
-// Pieces of rows row0 .. of an utterance, to be joined: numbers part0, part0 + stride, ..
-struct TreeJoin { int32_t n_nodes, node0, row0, part0, stride, n_parts; };
-
-// Words that travel as arguments of a launch (4 KB with the rest) to memory of the device.
+// Host metadata of a call as 32-bit words: arguments of the launch where they are few (4 KB with the rest), else in the workspace.
 struct MetaWords {
-    static constexpr int WORDS = 960;
+    static constexpr int WORDS = 940;
     int n;
     uint32_t word[WORDS];
+    __device__ __forceinline__ uint32_t operator()(int i) const { return word[i]; }
+};
+struct MetaArray {
+    const uint32_t* word;
+    __device__ __forceinline__ uint32_t operator()(int i) const { return word[i]; }
 };
 void launch_write_words(const MetaWords& w, uint32_t* dst, hipStream_t st);
 
+// Attention of nodes.  Query rows of one K/V head are numbered node * G + head of the group; keys are the rows of the utterance, n_ctx cached ones, then
+// the nodes.  The words: per utterance (first slot, n_ctx); from `cu` on the B + 1 prefix sums of the nodes; from `items` on per item of work two: utterance |
+// tile of tile_rows query rows << 16, piece of `step` keys (the first n_parts items leave partial results); from `joins` on per tile of a cut
+// utterance three: utterance | tile << 16, item of its first piece, pieces; from `mass` on per item of the weights one: utterance |
+// piece of mass_step keys << 16; from `spans` on per node its place in depth-first order | end of its subtree << 16.
 struct TreeAttnArgs {
     const void* q; int64_t q_stride;
     const void* k; const void* v; int64_t slot_stride, head_stride;
-    int n_q_heads, n_kv_heads, head_dim, dtype;
-    float scale;
     void* out;
     float* lse;                              // [nodes, n_q_heads]; NULL: not wanted
     float* mass; int64_t mass_stride;        // [n_kv_heads, mass_stride]; NULL: not wanted
-    int tile_rows;                           // query rows of an item
-    const TreeItem* items; int n_items;
-    const TreeJoin* joins; int n_joins;
-    float* part_o; float2* part_ml;          // [piece][K/V head][tile_rows] output and (maximum, sum)
-    const TreeItem* mass_items; int n_mass_items;
-    const uint32_t* spans;                   // per node: place in depth-first order, end of its subtree << 16
+    float* part_o; float2* part_ml;          // [item][K/V head][tile_rows] outputs and (maximum, sum) of pieces
+    int n_q_heads, n_kv_heads, head_dim, dtype;
+    float scale;
+    int tile_rows, step, mass_step, n_items, n_parts, n_joins, n_mass;
+    int cu, items, joins, mass_items, spans;
 };
-void launch_tree_attention(const TreeAttnArgs& a, hipStream_t st);
-constexpr int TREE_MASS_KEYS = 128;          // keys of an item of the weights: a multiple of these
-constexpr int TREE_WORKGROUPS = 1024;        // long contexts are cut into about as many pieces in all, times K/V heads
-constexpr int TREE_SPLIT_KEYS = 256;         // a piece has at least as many keys
+// words: host memory, n of them, to travel as arguments; or NULL, then they are in dev_words
+void launch_tree_attention(const TreeAttnArgs& a, const uint32_t* words, int n, const uint32_t* dev_words, hipStream_t st);
+constexpr int TREE_KEY_ROWS = 32;            // up to as many query rows in the largest tree: the wavefronts of a workgroup split the keys
+constexpr int TREE_WORKGROUPS = 512;         // long contexts are cut into about as many pieces in all, times K/V heads
+constexpr int TREE_SPLIT_KEYS = 512;         // a piece has at least as many keys
+constexpr int TREE_MASS_KEYS = 128;          // and one of the weights a multiple of these
 
 // nodes of an utterance: cu[b] .. cu[b + 1] - 1 (at most MAX_TREE_NODES); parent: index inside the utterance or -1
 void launch_tree_path(const float* logp, const int32_t* cu, const int16_t* parent, int B, int most_nodes, float ln_tau, bool roots_given, int32_t* accept_len,

@@ -30,16 +30,54 @@ __device__ __forceinline__ bool sees(uint32_t node, uint32_t key) {
 constexpr float LOG2E = 1.4426950408889634f, LN2 = 0.6931471805599453f;
 constexpr float F32_MOST = 3.4028234663852886e38f;
 
-constexpr int TREE_WAVES = 4;
+// An item of work: what its words say.
+struct Work { int slot0, n_ctx, n_nodes, node0, row0, k0, k1, index; };
+template <class M>
+__device__ __forceinline__ void utterance_of(const TreeAttnArgs& a, const M& w, int b, Work& t) {
+    t.slot0 = (int)w(2 * b);
+    t.n_ctx = (int)w(2 * b + 1);
+    t.node0 = (int)w(a.cu + b);
+    t.n_nodes = (int)w(a.cu + b + 1) - t.node0;
+}
+template <class M>
+__device__ __forceinline__ Work item_of(const TreeAttnArgs& a, const M& w, int index, int tile_rows) {
+    Work t;
+    const uint32_t x = w(a.items + 2 * index);
+    utterance_of(a, w, x & 0xffffu, t);
+    const int G = a.n_q_heads / a.n_kv_heads;
+    t.index = index;
+    t.row0 = (int)(x >> 16) * tile_rows;
+    const int64_t k0 = (int64_t)w(a.items + 2 * index + 1) * a.step;
+    const int node = (min(t.n_nodes * G, t.row0 + tile_rows) - 1) / G;              // no row of the tile sees a later one
+    t.k0 = (int)k0;
+    t.k1 = (int)min((int64_t)t.n_ctx + node + 1, k0 + a.step);
+    return t;
+}
+
+template <class M>
+__device__ __forceinline__ Work mass_item_of(const TreeAttnArgs& a, const M& w, int index) {
+    Work t;
+    const uint32_t x = w(a.mass_items + index);
+    utterance_of(a, w, x & 0xffffu, t);
+    const int64_t k0 = (int64_t)(x >> 16) * a.mass_step;
+    t.index = index;
+    t.row0 = 0;
+    t.k0 = (int)k0;
+    t.k1 = (int)min((int64_t)t.n_ctx + t.n_nodes, k0 + a.mass_step);
+    return t;
+}
+
+constexpr int MASS_WAVES = 4;                // wavefronts of a workgroup of the weights
+constexpr int KEY_WAVES = 8;                 // wavefronts of a workgroup that split the keys
 
 // The end of an attention workgroup: its wavefronts hold, for 16 NT rows, maxima m (raw scores), sums l (a lane's share) and outputs o[n][i] (row
 // 16 n + lane % 16, dims 16 i + 4 (lane / 16) ..) relative to 2^(m sc - bias).  DPASS dims of all rows at a time go through LDS (buf: 16 HD floats a wavefront,
 // the 16-byte chunks of a row permuted by its number); every thread adds VPT values of a row and stores them, or the sums of a piece.
-template <int DT, int HD, int NT>
-__device__ __forceinline__ void merge_wavefronts(const TreeAttnArgs& a, const TreeItem& t, int kvh, const float (&m)[NT], float (&l)[NT], const f32x4_t (&o)[NT][HD / 16],
+template <int DT, int HD, int NT, int WAVES>
+__device__ __forceinline__ void merge_wavefronts(const TreeAttnArgs& a, const Work& t, int kvh, const float (&m)[NT], float (&l)[NT], const f32x4_t (&o)[NT][HD / 16],
                                                  float sc, float bias, float* buf, float2* ml_s) {
     typedef Elem<DT> E;
-    constexpr int TR = 16 * NT, DPASS = 16 * HD / TR, VPT = HD / 16;
+    constexpr int TR = 16 * NT, DPASS = 16 * HD / TR, VPT = TR * DPASS / (64 * WAVES), TPR = 64 * WAVES / TR;      // values of a thread, threads of a row
     const int lane = threadIdx.x % 64, kg = lane / 16, dc = lane % 16, wave = threadIdx.x / 64;
     const int G = a.n_q_heads / a.n_kv_heads, R = t.n_nodes * G;
 #pragma unroll
@@ -48,10 +86,11 @@ __device__ __forceinline__ void merge_wavefronts(const TreeAttnArgs& a, const Tr
         l[n] += __shfl_xor(l[n], 32);
         if (kg == 0) ml_s[wave * TR + 16 * n + dc] = make_float2(m[n], l[n]);
     }
+    static_assert(VPT == 2 || VPT == 4, "values of a thread");
     constexpr int CH = DPASS / 4;                            // chunks of a row
-    const int orow = threadIdx.x / (256 / TR), ocol = threadIdx.x % (256 / TR) * VPT;
+    const int orow = threadIdx.x / TPR, ocol = threadIdx.x % TPR * VPT;
     const int row = t.row0 + orow;
-    float w[TREE_WAVES], mt = -F32_MOST, lt = 0.f;
+    float w[WAVES], mt = -F32_MOST, lt = 0.f;
 #pragma unroll
     for (int pass = 0; pass < HD / DPASS; ++pass) {
         if (pass) __syncthreads();
@@ -65,9 +104,9 @@ __device__ __forceinline__ void merge_wavefronts(const TreeAttnArgs& a, const Tr
         __syncthreads();
         if (pass == 0) {
 #pragma unroll
-            for (int u = 0; u < TREE_WAVES; ++u) mt = fmaxf(mt, ml_s[u * TR + orow].x);
+            for (int u = 0; u < WAVES; ++u) mt = fmaxf(mt, ml_s[u * TR + orow].x);
 #pragma unroll
-            for (int u = 0; u < TREE_WAVES; ++u) {
+            for (int u = 0; u < WAVES; ++u) {
                 const float2 x = ml_s[u * TR + orow];
                 w[u] = x.y == 0.f ? 0.f : __builtin_amdgcn_exp2f((x.x - mt) * sc);
                 lt = fmaf(x.y, w[u], lt);
@@ -77,76 +116,104 @@ __device__ __forceinline__ void merge_wavefronts(const TreeAttnArgs& a, const Tr
 #pragma unroll
         for (int e = 0; e < VPT; ++e) v[e] = 0.f;
 #pragma unroll
-        for (int u = 0; u < TREE_WAVES; ++u)
+        for (int u = 0; u < WAVES; ++u)
 #pragma unroll
-            for (int e = 0; e < VPT; e += 4) {
-                const f32x4_t x = *reinterpret_cast<const f32x4_t*>(buf + (u * TR + orow) * DPASS + ((ocol + e) / 4 ^ (orow & (CH - 1))) * 4);
-#pragma unroll
-                for (int f = 0; f < 4; ++f) v[e + f] = fmaf(x[f], w[u], v[e + f]);
-            }
+            for (int e = 0; e < VPT; ++e) v[e] = fmaf(buf[(u * TR + orow) * DPASS + (ocol / 4 ^ (orow & (CH - 1))) * 4 + ocol % 4 + e], w[u], v[e]);
         if (row >= R) continue;
         const int dim = pass * DPASS + ocol;
-        if (t.part >= 0) {
-            float* dst = a.part_o + ((int64_t)(t.part * a.n_kv_heads + kvh) * TR + orow) * HD + dim;
+        if (t.index < a.n_parts) {
+            float* dst = a.part_o + ((int64_t)(t.index * a.n_kv_heads + kvh) * TR + orow) * HD + dim;
 #pragma unroll
-            for (int e = 0; e < VPT; e += 4) *reinterpret_cast<f32x4_t*>(dst + e) = (f32x4_t){v[e], v[e + 1], v[e + 2], v[e + 3]};
+            for (int e = 0; e < VPT; ++e) dst[e] = v[e];
         } else {
             const float inv = 1.f / lt;
             typename E::type* dst = (typename E::type*)a.out + ((int64_t)(t.node0 + row / G) * a.n_q_heads + kvh * G + row % G) * a.head_dim + dim;
             if constexpr (DT == SSD_F32) {
 #pragma unroll
-                for (int e = 0; e < VPT; e += 4)
-                    if (dim + e < a.head_dim) *reinterpret_cast<f32x4_t*>(dst + e) = (f32x4_t){v[e] * inv, v[e + 1] * inv, v[e + 2] * inv, v[e + 3] * inv};
+                for (int e = 0; e < VPT; ++e)
+                    if (dim < a.head_dim) dst[e] = v[e] * inv;
             } else {
                 uint32_t x[VPT / 2];
 #pragma unroll
                 for (int e = 0; e < VPT; e += 2) x[e / 2] = op_pack2<DT == SSD_BF16>(v[e] * inv, v[e + 1] * inv);
-                if constexpr (VPT == 8) *reinterpret_cast<uint4*>(dst) = make_uint4(x[0], x[1], x[2], x[3]);
-                else *reinterpret_cast<uint2*>(dst) = make_uint2(x[0], x[1]);
+                if constexpr (VPT == 4) *reinterpret_cast<uint2*>(dst) = make_uint2(x[0], x[1]);
+                else *reinterpret_cast<uint32_t*>(dst) = x[0];
             }
         }
     }
     if (ocol == 0 && row < R) {
-        if (t.part >= 0) a.part_ml[(int64_t)(t.part * a.n_kv_heads + kvh) * TR + orow] = make_float2(mt, lt);
+        if (t.index < a.n_parts) a.part_ml[(int64_t)(t.index * a.n_kv_heads + kvh) * TR + orow] = make_float2(mt, lt);
         else if (a.lse) a.lse[(int64_t)(t.node0 + row / G) * a.n_q_heads + kvh * G + row % G] = (mt * sc - bias + __builtin_amdgcn_logf(lt)) * LN2;
     }
 }
 
-// The pieces of a long context joined: one group of HD / 4 lanes a query row.
-template <int DT, int HD>
-__global__ void __launch_bounds__(256) tree_join_kernel(TreeAttnArgs a, int tile_rows, float bias) {
+// The pieces of a long context joined.  A workgroup has a query row: groups of HD / 4 lanes take its pieces in turn, each with a running maximum, and
+// are joined through LDS.
+template <int DT, int HD, class M>
+__global__ void __launch_bounds__(256) tree_join_kernel(TreeAttnArgs a, M w, float bias) {
     typedef Elem<DT> E;
-    constexpr int LANES = HD / 4, ROWS = 256 / LANES;
-    const TreeJoin t = a.joins[blockIdx.x];
-    const int kvh = blockIdx.y, G = a.n_q_heads / a.n_kv_heads;
-    const int r = blockIdx.z * ROWS + threadIdx.x / LANES, row = t.row0 + r, dim = threadIdx.x % LANES * 4;
-    if (r >= tile_rows || row >= t.n_nodes * G) return;
+    constexpr int LANES = HD / 4, GROUPS = 256 / LANES;
+    __shared__ f32x4_t o_s[GROUPS][LANES];
+    __shared__ float2 ml_s[GROUPS];
+    const int j = blockIdx.x / a.tile_rows, r = blockIdx.x % a.tile_rows, kvh = blockIdx.y, G = a.n_q_heads / a.n_kv_heads;
+    const uint32_t x = w(a.joins + 3 * j);
+    const int item0 = (int)w(a.joins + 3 * j + 1), n_parts = (int)w(a.joins + 3 * j + 2);
+    Work t;
+    utterance_of(a, w, x & 0xffffu, t);
+    const int R = t.n_nodes * G, tiles = (R + a.tile_rows - 1) / a.tile_rows, row = (int)(x >> 16) * a.tile_rows + r;
+    if (row >= R) return;
     const float sc = fabsf(a.scale) * LOG2E;
-    float mt = -F32_MOST, lt = 0.f;
-    for (int p = 0; p < t.n_parts; ++p) mt = fmaxf(mt, a.part_ml[(int64_t)((t.part0 + p * t.stride) * a.n_kv_heads + kvh) * tile_rows + r].x);
+    const int group = threadIdx.x / LANES, dim = threadIdx.x % LANES * 4;
+    float m = -F32_MOST, l = 0.f;
     f32x4_t v = {0.f, 0.f, 0.f, 0.f};
-    for (int p = 0; p < t.n_parts; ++p) {
-        const int64_t at = (int64_t)((t.part0 + p * t.stride) * a.n_kv_heads + kvh) * tile_rows + r;
-        const float2 x = a.part_ml[at];
-        const float w = x.y == 0.f ? 0.f : __builtin_amdgcn_exp2f((x.x - mt) * sc);
-        lt = fmaf(x.y, w, lt);
-        const f32x4_t y = *reinterpret_cast<const f32x4_t*>(a.part_o + at * HD + dim);
+    constexpr int U = 4;                                     // pieces requested at once
+    for (int p0 = group; p0 < n_parts; p0 += U * GROUPS) {
+        float2 y[U];
+        f32x4_t z[U];
 #pragma unroll
-        for (int e = 0; e < 4; ++e) v[e] = fmaf(y[e], w, v[e]);
+        for (int u = 0; u < U; ++u) {
+            const int p = min(p0 + u * GROUPS, n_parts - 1);
+            const int64_t at = ((int64_t)(item0 + p * tiles) * a.n_kv_heads + kvh) * a.tile_rows + r;
+            y[u] = a.part_ml[at];
+            z[u] = *reinterpret_cast<const f32x4_t*>(a.part_o + at * HD + dim);
+        }
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            if (p0 + u * GROUPS >= n_parts || y[u].y == 0.f) continue;                     // (a piece whose keys no row of the tile sees)
+            const float top = fmaxf(m, y[u].x), old = __builtin_amdgcn_exp2f((m - top) * sc), now = __builtin_amdgcn_exp2f((y[u].x - top) * sc);
+            m = top;
+            l = l * old + y[u].y * now;
+            v = v * old + z[u] * now;
+        }
+    }
+    o_s[group][dim / 4] = v;
+    if (dim == 0) ml_s[group] = make_float2(m, l);
+    __syncthreads();
+    if (group) return;
+    float mt = -F32_MOST, lt = 0.f;
+#pragma unroll
+    for (int g = 0; g < GROUPS; ++g) mt = fmaxf(mt, ml_s[g].x);
+    f32x4_t s = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int g = 0; g < GROUPS; ++g) {
+        const float2 y = ml_s[g];
+        const float f = y.y == 0.f ? 0.f : __builtin_amdgcn_exp2f((y.x - mt) * sc);
+        lt += y.y * f;
+        s += o_s[g][dim / 4] * f;
     }
     const int64_t at = (int64_t)(t.node0 + row / G) * a.n_q_heads + kvh * G + row % G;
     typename E::type* dst = (typename E::type*)a.out + at * a.head_dim + dim;
     const float inv = 1.f / lt;
+    if (dim < a.head_dim)
 #pragma unroll
-    for (int e = 0; e < 4; ++e)
-        if (dim + e < a.head_dim) dst[e] = E::put(v[e] * inv);
+        for (int e = 0; e < 4; ++e) dst[e] = E::put(s[e] * inv);
     if (a.lse && dim == 0) a.lse[at] = (mt * sc - bias + __builtin_amdgcn_logf(lt)) * LN2;
 }
 
 // Adds the weights of a 32- or 16-key block: acc[c][r] belongs to key k0 + 16 c + 4 (lane / 16) + r and is a lane's share of it.  fresh: the first rows
 // of the tree are in it, so that the entry of a node row is stored; every key has one workgroup and one lane.
 template <int C>
-__device__ __forceinline__ void add_mass(const TreeAttnArgs& a, const TreeItem& t, int kvh, int k0, bool fresh, f32x4_t (&acc)[C]) {
+__device__ __forceinline__ void add_mass(const TreeAttnArgs& a, const Work& t, int kvh, int k0, bool fresh, f32x4_t (&acc)[C]) {
     const int lane = threadIdx.x % 64, kg = lane / 16, dc = lane % 16;
     float mine = 0.f;
 #pragma unroll
@@ -158,10 +225,10 @@ __device__ __forceinline__ void add_mass(const TreeAttnArgs& a, const TreeItem& 
         }
     const int key = k0 + 16 * (dc / 4) + 4 * kg + dc % 4;
     if (dc >= 4 * C || key >= t.k1) return;
-    float* dst = a.mass + kvh * a.mass_stride + t.slot0 + key;
+    float* dst = a.mass + (int64_t)kvh * a.mass_stride + t.slot0 + key;
     *dst = fresh && key >= t.n_ctx ? mine : *dst + mine;
 }
 
-void launch_tree_attention32(const TreeAttnArgs& a, hipStream_t st);
+template <class M> void launch_tree_attention32(const TreeAttnArgs& a, const M& w, hipStream_t st);
 
 }  // namespace ssd

@@ -3,22 +3,20 @@
 // subtree, so that two integers a node are the mask of a tree of any shape.
 //   s_ij = scale q_i . k_j,  lse_i = log sum_j exp s_ij,  o_i = sum_j exp(s_ij - lse_i) v_j
 // and the weight that row j collects: sum over the nodes and the heads of the K/V head's group of exp(s_ij - lse_i).
+#include <string.h>
+
 #include "tree_attn.h"
 
 namespace ssd {
 
 // ---- 16-bit caches ----------------------------------------------------------------------------------------------------------------
-// A workgroup is four wavefronts and serves 16 NT query rows (node, head of the group) of one K/V head over a range of keys.  The
-// wavefronts take the 32-key blocks of the range in turn, so that every cached row is read once for all of these rows, and merge their
-// (max, sum, output) through LDS.  Both products are v_mfma_f32_16x16x32: S^T = K Q^T with the key rows straight from memory in operand
-// registers, O^T += V^T P^T with the values in LDS (global -> LDS loads, read back through the transposing ds_read_b64_tr_b16); keys
-// 4g .. 4g + 3 and 16 + 4g .. of a block are a lane's scores and its operand of the second product alike.
+// Both products are v_mfma_f32_16x16x32: S^T = K Q^T, then O^T += V^T P^T with the values in LDS (global -> LDS loads, read back through the
+// transposing ds_read_b64_tr_b16): keys 4g .. 4g + 3 and 16 + 4g .. of 32 are the scores of lane group g and its operand of the second product alike.
 // The maximum that the exponents refer to may lag behind the true one by 2^LAG: it is raised (and the output rescaled) only by a score
 // beyond that, which spares nearly every block the exchange between lanes and the rescaling.  Probabilities enter the second product in
 // the type of the cache, their sum does not: half a step of the type each, as the output's own rounding.  IEEE half holds them times
 // 2^BIAS, so that those down to 2^-31 of the largest count (2^(BIAS + LAG) is in its range); bfloat16 has the range of fp32, and there they
 // stay below 1 so that values near its end do not overflow the sums.
-constexpr int TREE_KEYS = 32;
 constexpr float LAG = 8.f;
 template <bool BF> constexpr float BIAS = BF ? -LAG : 6.f;
 
@@ -36,31 +34,187 @@ template <bool BF> __device__ __forceinline__ uint32_t infinite_of(uint32_t w, u
 }
 template <bool BF> __device__ __forceinline__ uint32_t finite_of(uint32_t w) { return w & ~(((beyond_of<BF>(w) & SIGNS) >> 15) * 0xffffu); }
 
-template <bool BF, int HD, int NT>
-__global__ void __launch_bounds__(64 * TREE_WAVES, NT == 4 ? 1 : 2) tree_attn16_kernel(TreeAttnArgs a) {
-    constexpr int ROW = HD * 2, BLOCK = TREE_KEYS * ROW, STEP = TREE_KEYS * TREE_WAVES;
+// Spans of a lane's keys k0 + 16 c + 4 (lane / 16) + r: every node's place lies in that of a cached row, nobody's in that of a key behind the range.
+template <int C>
+__device__ __forceinline__ void key_spans(uint32_t (&key)[C][4], const Work& t, int k0, const uint32_t* span_s) {
+    const int kg = threadIdx.x % 64 / 16;
+#pragma unroll
+    for (int c = 0; c < C; ++c)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+            const int at = k0 + 16 * c + 4 * kg + r;
+            key[c][r] = at < t.n_ctx ? 0xffff0000u : at < t.k1 ? span_s[at - t.n_ctx] : 0u;
+        }
+}
+
+// Scores of 16 C keys to weights in the operand type; maxima, sums and outputs follow.
+template <bool BF, int NT, int C, int DT, bool MASKED>
+__device__ __forceinline__ void weights_of(f32x4_t (&s)[NT][C], float (&m)[NT], float (&l)[NT], f32x4_t (&o)[NT][DT], float sc, f16x8_t (&pf)[NT][C / 2]) {
+    float mx[NT];
+    bool above = false;
+#pragma unroll
+    for (int n = 0; n < NT; ++n) {
+        mx[n] = -INFINITY;
+#pragma unroll
+        for (int c = 0; c < C; ++c) mx[n] = fmaxf(mx[n], fmaxf(fmaxf(s[n][c][0], s[n][c][1]), fmaxf(s[n][c][2], s[n][c][3])));
+        above |= (mx[n] - m[n]) * sc > LAG;
+    }
+    if (__any(above)) {
+#pragma unroll
+        for (int n = 0; n < NT; ++n) {
+            float top = fmaxf(mx[n], __shfl_xor(mx[n], 16));
+            top = fmaxf(m[n], fmaxf(top, __shfl_xor(top, 32)));
+            const float alpha = __builtin_amdgcn_exp2f((m[n] - top) * sc);
+            m[n] = top;
+            l[n] *= alpha;
+#pragma unroll
+            for (int i = 0; i < DT; ++i) o[n][i] *= alpha;
+        }
+    }
+#pragma unroll
+    for (int n = 0; n < NT; ++n) {
+        const float base = fminf(BIAS<BF> - m[n] * sc, F32_MOST);    // (finite: a score may be -infinity)
+#pragma unroll
+        for (int h = 0; h < C / 2; ++h) {
+            uint32_t pw[4];
+#pragma unroll
+            for (int c = 0; c < 2; ++c) {
+                f32x4_t& x = s[n][2 * h + c];
+#pragma unroll
+                for (int r = 0; r < 4; ++r) {
+                    const float p = __builtin_amdgcn_exp2f(fmaf(x[r], sc, base));
+                    x[r] = MASKED && x[r] == -INFINITY ? 0.f : p;
+                    l[n] += x[r];
+                }
+                pw[2 * c] = op_pack2<BF>(x[0], x[1]);
+                pw[2 * c + 1] = op_pack2<BF>(x[2], x[3]);
+            }
+            pf[n][h] = as_f16x8(make_uint4(pw[0], pw[1], pw[2], pw[3]));
+        }
+    }
+}
+
+// Place of the 16-byte chunks of value row `row` in LDS: the 32-byte pieces that half a wavefront reads lie in all banks.
+template <int HD> __device__ __forceinline__ int v_swizzle(int row) { return HD == 128 ? 4 * (row & 3) + 2 * (row >> 2 & 1) : 2 * (row >> 1 & 3); }
+
+// The same for key and query rows, of which an operand read takes the same chunk of 16.
+template <int HD> __device__ __forceinline__ int k_swizzle(int row) { return HD == 128 ? row & 15 : row >> 1 & 7; }
+
+// O^T += V^T P^T over the 32 value rows at v, DG 16-dim tiles at a time.  Transposing read: lane i of 16 passes row i / 4 and dims 4 (i % 4) .. + 3 of a
+// 16-dim tile, lane j receives dim j of four rows.
+template <bool BF, int HD, int NT, int DG, bool MASKED>
+__device__ __forceinline__ void add_values(const unsigned char* v, const f16x8_t (&pf)[NT], f32x4_t (&o)[NT][HD / 16]) {
+    constexpr int ROW = HD * 2;
+    const int lane = threadIdx.x % 64, kg = lane / 16, dc = lane % 16;
+    const int v_row = 4 * kg + dc / 4, v_low = (dc % 4) / 2, v_sub = (dc % 2) * 8;
+#pragma unroll
+    for (int g = 0; g < HD / 16; g += DG) {
+        tr_v4i16 vf[DG][2];
+#pragma unroll
+        for (int i = 0; i < DG; ++i) {
+            const unsigned char* p = v + v_row * ROW + (((2 * (g + i)) | v_low) ^ v_swizzle<HD>(v_row)) * 16 + v_sub;
+            vf[i][0] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_tr_v4i16*)p);
+            vf[i][1] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_tr_v4i16*)(p + 16 * ROW));
+        }
+        __builtin_amdgcn_sched_barrier(0);
+        // A value that is not finite would reach the rows that do not see it as 0 times infinity.  In a block that holds one the products run
+        // on the others, and two more count the infinities of either sign (a NaN as both) that rows with a probability meet.
+        uint32_t odd = 0;
+        if constexpr (MASKED) {
+#pragma unroll
+            for (int i = 0; i < DG; ++i)
+#pragma unroll
+                for (int e = 0; e < 2; ++e) {
+                    const uint2 x = __builtin_bit_cast(uint2, vf[i][e]);
+                    odd |= beyond_of<BF>(x.x) | beyond_of<BF>(x.y);
+                }
+        }
+        if (MASKED && __any(odd & SIGNS)) {
+            f16x8_t there[NT];
+#pragma unroll
+            for (int n = 0; n < NT; ++n) {
+                const uint4 x = __builtin_bit_cast(uint4, pf[n]);
+                there[n] = as_f16x8(make_uint4(one_where<BF>(not_zero(x.x)), one_where<BF>(not_zero(x.y)), one_where<BF>(not_zero(x.z)), one_where<BF>(not_zero(x.w))));
+            }
+#pragma unroll
+            for (int i = 0; i < DG; ++i) {
+                __builtin_amdgcn_sched_barrier(0);           // (one after the other: registers, not speed)
+                const uint2 x = __builtin_bit_cast(uint2, vf[i][0]), y = __builtin_bit_cast(uint2, vf[i][1]);
+                const f16x8_t up = as_f16x8(make_uint4(infinite_of<BF>(x.x, 0), infinite_of<BF>(x.y, 0), infinite_of<BF>(y.x, 0), infinite_of<BF>(y.y, 0)));
+                const f16x8_t down = as_f16x8(make_uint4(infinite_of<BF>(x.x, ~0u), infinite_of<BF>(x.y, ~0u), infinite_of<BF>(y.x, ~0u), infinite_of<BF>(y.y, ~0u)));
+#pragma unroll
+                for (int n = 0; n < NT; ++n) {
+                    const f32x4_t zero = {0.f, 0.f, 0.f, 0.f}, u = mfma_16x16x32<BF>(up, there[n], zero), d = mfma_16x16x32<BF>(down, there[n], zero);
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) o[n][g + i][r] += (u[r] > 0.f ? INFINITY : 0.f) - (d[r] > 0.f ? INFINITY : 0.f);
+                }
+                vf[i][0] = __builtin_bit_cast(tr_v4i16, make_uint2(finite_of<BF>(x.x), finite_of<BF>(x.y)));
+                vf[i][1] = __builtin_bit_cast(tr_v4i16, make_uint2(finite_of<BF>(y.x), finite_of<BF>(y.y)));
+            }
+        }
+#pragma unroll
+        for (int i = 0; i < DG; ++i) {
+            const f16x8_t x = __builtin_bit_cast(f16x8_t, __builtin_shufflevector(vf[i][0], vf[i][1], 0, 1, 2, 3, 4, 5, 6, 7));
+#pragma unroll
+            for (int n = 0; n < NT; ++n) o[n][g + i] = mfma_16x16x32<BF>(x, pf[n], o[n][g + i]);
+        }
+    }
+}
+
+// Queries as operands: column lane % 16 of tile n is query row row0 + 16 n + lane % 16 (a copy of the last one behind it); a negative scale is theirs.
+template <int HD, int NT>
+__device__ __forceinline__ void load_queries(f16x8_t (&qf)[NT][HD / 32], const TreeAttnArgs& a, const Work& t, int kvh, int row0) {
+    const int lane = threadIdx.x % 64, G = a.n_q_heads / a.n_kv_heads;
+    const uint32_t flip = a.scale < 0.f ? 0x80008000u : 0u;
+#pragma unroll
+    for (int n = 0; n < NT; ++n) {
+        const int row = min(row0 + 16 * n + lane % 16, t.n_nodes * G - 1);
+        const uint16_t* q = (const uint16_t*)a.q + (int64_t)(t.node0 + row / G) * a.q_stride + (kvh * G + row % G) * HD + lane / 16 * 8;
+#pragma unroll
+        for (int s = 0; s < HD / 32; ++s) {
+            uint4 x = *reinterpret_cast<const uint4*>(q + 32 * s);
+            x.x ^= flip; x.y ^= flip; x.z ^= flip; x.w ^= flip;
+            qf[n][s] = as_f16x8(x);
+        }
+    }
+}
+
+// What all wavefronts have stored to LDS, and with it what they loaded straight into it and have waited for; a barrier with a fence would wait for
+// every load in flight.
+__device__ __forceinline__ void lds_barrier() {
+    asm volatile("" ::: "memory");
+    __builtin_amdgcn_s_waitcnt(0xC07F);
+    __builtin_amdgcn_s_barrier();
+    asm volatile("" ::: "memory");
+}
+
+// ---- few query rows: 16 NT of a K/V head a workgroup, whose wavefronts take the 32-key blocks of the range in turn, so that every cached row is read once,
+// and merge their (maximum, sum, output) through LDS.  Key rows come straight from memory in operand registers; a wavefront's values are its own
+// and need no barrier.
+template <bool BF, int HD, int NT, class M>
+__global__ void __launch_bounds__(64 * KEY_WAVES, 2) tree_keys16_kernel(TreeAttnArgs a, M w) {
+    constexpr int KEYS = 32, ROW = HD * 2, BLOCK = KEYS * ROW, STEP = KEYS * KEY_WAVES;
     constexpr int KS = HD / 32, DT = HD / 16, TR = 16 * NT;
-    constexpr int ROW_CHUNKS = ROW / 16, V_ROWS = 64 / ROW_CHUNKS, V_LOADS = TREE_KEYS / V_ROWS, K_LOADS = 2 * KS;
-    __shared__ __align__(1024) unsigned char v_s[TREE_WAVES][BLOCK];
-    __shared__ float2 ml_s[TREE_WAVES * TR];
+    constexpr int ROW_CHUNKS = ROW / 16, V_ROWS = 64 / ROW_CHUNKS, V_LOADS = KEYS / V_ROWS, K_LOADS = 2 * KS;
+    __shared__ __align__(1024) unsigned char v_s[KEY_WAVES][BLOCK];
+    __shared__ float2 ml_s[KEY_WAVES * TR];
     __shared__ uint32_t span_s[MAX_TREE_NODES];
     const int lane = threadIdx.x % 64, kg = lane / 16, dc = lane % 16;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
     const int work = xcd_contiguous_index(blockIdx.x, gridDim.x);
-    const TreeItem t = a.items[work / a.n_kv_heads];
+    const Work t = item_of(a, w, work / a.n_kv_heads, TR);
     const int kvh = work % a.n_kv_heads;
     const int G = a.n_q_heads / a.n_kv_heads, R = t.n_nodes * G;
     const int last = max(t.k0, t.k1 - 1);                    // (a range without keys: any row)
     const int n_spans = t.k1 > t.n_ctx ? t.n_nodes : 0;
-    const uint32_t span = (int)threadIdx.x < n_spans ? a.spans[t.node0 + threadIdx.x] : 0u;
+    const uint32_t span = (int)threadIdx.x < n_spans ? w(a.spans + t.node0 + (int)threadIdx.x) : 0u;
     const int stride2 = (int)a.slot_stride * 2;
     const int64_t first = (int64_t)t.slot0 * a.slot_stride + kvh * a.head_stride;
     const uint16_t* kbase = (const uint16_t*)a.k + first;
     const uint16_t* vbase = (const uint16_t*)a.v + first;
 
-    // Keys k0 .. k0 + 31: lane (row dc of a half of 16, dims 8 kg + 32 s) in registers.  Values: rows of an instruction one behind the
-    // other, the 16-byte chunks of a row permuted by its number so that the 32-byte pieces that half a wavefront reads lie in all LDS
-    // banks.  Rows behind the range are copies of its last one: masked, or of a block behind the wavefront's last, which is requested all the same.
+    // Keys k0 .. k0 + 31: lane (row dc of a half of 16, dims 8 kg + 32 s) in registers.  Values: rows of an instruction one behind the other.  Rows behind
+    // the range are copies of its last one: masked, or of a block behind the wavefront's last, which is requested all the same.
     u32x4_t kr[2][KS];
     auto load_keys = [&](int k0) {
         const int r0 = min(k0, last), beyond = last - r0;
@@ -72,35 +226,21 @@ __global__ void __launch_bounds__(64 * TREE_WAVES, NT == 4 ? 1 : 2) tree_attn16_
             for (int s = 0; s < KS; ++s) kr[c][s] = __builtin_amdgcn_raw_buffer_load_b128(rsrc, off + 64 * s, 0, 0);
         }
     };
-    auto swizzle = [](int row) { return HD == 128 ? 4 * (row & 3) + 2 * (row >> 2 & 1) : 2 * (row >> 1 & 3); };
     auto load_values = [&](int k0) {
         const int r0 = min(k0, last), beyond = last - r0;
         const __amdgpu_buffer_rsrc_t rsrc = make_rsrc(vbase + (int64_t)r0 * a.slot_stride);
 #pragma unroll
         for (int i = 0; i < V_LOADS; ++i) {
             const int row = V_ROWS * i + lane / ROW_CHUNKS;
-            const int off = min(row, beyond) * stride2 + ((lane % ROW_CHUNKS) ^ swizzle(row)) * 16;
+            const int off = min(row, beyond) * stride2 + ((lane % ROW_CHUNKS) ^ v_swizzle<HD>(row)) * 16;
             __builtin_amdgcn_raw_ptr_buffer_load_lds(rsrc, (lds_void_t*)(v_s[wave] + i * 1024), 16, off, 0, 0, 0);
         }
     };
-    int k0 = t.k0 + wave * TREE_KEYS;
+    int k0 = t.k0 + wave * KEYS;
     load_keys(k0);
     load_values(k0);
-
-    // queries: column dc of tile n is row row0 + 16 n + dc (a copy of the last one behind it); a negative scale is theirs
     f16x8_t qf[NT][KS];
-    const uint32_t flip = a.scale < 0.f ? 0x80008000u : 0u;
-#pragma unroll
-    for (int n = 0; n < NT; ++n) {
-        const int row = min(t.row0 + 16 * n + dc, R - 1);
-        const uint16_t* q = (const uint16_t*)a.q + (int64_t)(t.node0 + row / G) * a.q_stride + (kvh * G + row % G) * HD + kg * 8;
-#pragma unroll
-        for (int s = 0; s < KS; ++s) {
-            uint4 w = *reinterpret_cast<const uint4*>(q + 32 * s);
-            w.x ^= flip; w.y ^= flip; w.z ^= flip; w.w ^= flip;
-            qf[n][s] = as_f16x8(w);
-        }
-    }
+    load_queries<HD, NT>(qf, a, t, kvh, t.row0);
     const float sc = fabsf(a.scale) * LOG2E;
     float m[NT], l[NT];
     f32x4_t o[NT][DT];
@@ -112,15 +252,8 @@ __global__ void __launch_bounds__(64 * TREE_WAVES, NT == 4 ? 1 : 2) tree_attn16_
         for (int i = 0; i < DT; ++i) o[n][i] = (f32x4_t){0.f, 0.f, 0.f, 0.f};
     }
     if ((int)threadIdx.x < n_spans) span_s[threadIdx.x] = span;
-    for (int i = threadIdx.x + 64 * TREE_WAVES; i < n_spans; i += 64 * TREE_WAVES) span_s[i] = a.spans[t.node0 + i];
-    // the spans have been written; a barrier with a fence would wait for the rows as well
-    asm volatile("" ::: "memory");
-    __builtin_amdgcn_s_waitcnt(0xC07F);
-    __builtin_amdgcn_s_barrier();
-    asm volatile("" ::: "memory");
-
-    // transposing read: lane i of 16 passes row i / 4 and dims 4 (i % 4) .. + 3 of a 16-dim block, lane j receives dim j of four rows
-    const int v_row = 4 * kg + dc / 4, v_low = (dc % 4) / 2, v_sub = (dc % 2) * 8;
+    for (int i = threadIdx.x + 64 * KEY_WAVES; i < n_spans; i += 64 * KEY_WAVES) span_s[i] = w(a.spans + t.node0 + i);
+    lds_barrier();
     auto block = [&](auto masked_c, int k0) {
         constexpr bool MASKED = decltype(masked_c)::value;
         f32x4_t s[NT][2];
@@ -136,14 +269,8 @@ __global__ void __launch_bounds__(64 * TREE_WAVES, NT == 4 ? 1 : 2) tree_attn16_
         load_keys(k0 + STEP);
         __builtin_amdgcn_sched_barrier(0);
         if constexpr (MASKED) {
-            uint32_t key[2][4];                              // the keys' spans: all of the context, nothing behind the range
-#pragma unroll
-            for (int c = 0; c < 2; ++c)
-#pragma unroll
-                for (int r = 0; r < 4; ++r) {
-                    const int at = k0 + 16 * c + 4 * kg + r;
-                    key[c][r] = at < t.n_ctx ? 0xffff0000u : at < t.k1 ? span_s[at - t.n_ctx] : 0u;
-                }
+            uint32_t key[2][4];
+            key_spans<2>(key, t, k0, span_s);
 #pragma unroll
             for (int n = 0; n < NT; ++n) {
                 const uint32_t mine = span_s[min(t.row0 + 16 * n + dc, R - 1) / G];
@@ -153,106 +280,153 @@ __global__ void __launch_bounds__(64 * TREE_WAVES, NT == 4 ? 1 : 2) tree_attn16_
                     for (int r = 0; r < 4; ++r) s[n][c][r] = sees(mine, key[c][r]) ? s[n][c][r] : -INFINITY;
             }
         }
-        float mx[NT];
-        bool above = false;
+        f16x8_t pf[NT][1];
+        weights_of<BF, NT, 2, DT, MASKED>(s, m, l, o, sc, pf);
+        f16x8_t p[NT];
 #pragma unroll
-        for (int n = 0; n < NT; ++n) {
-            mx[n] = fmaxf(fmaxf(fmaxf(s[n][0][0], s[n][0][1]), fmaxf(s[n][0][2], s[n][0][3])), fmaxf(fmaxf(s[n][1][0], s[n][1][1]), fmaxf(s[n][1][2], s[n][1][3])));
-            above |= (mx[n] - m[n]) * sc > LAG;
-        }
-        if (__any(above)) {
-#pragma unroll
-            for (int n = 0; n < NT; ++n) {
-                float top = fmaxf(mx[n], __shfl_xor(mx[n], 16));
-                top = fmaxf(m[n], fmaxf(top, __shfl_xor(top, 32)));
-                const float alpha = __builtin_amdgcn_exp2f((m[n] - top) * sc);
-                m[n] = top;
-                l[n] *= alpha;
-#pragma unroll
-                for (int i = 0; i < DT; ++i) o[n][i] *= alpha;
-            }
-        }
-        f16x8_t pf[NT];
-#pragma unroll
-        for (int n = 0; n < NT; ++n) {
-            const float base = fminf(BIAS<BF> - m[n] * sc, F32_MOST);    // (finite: a score may be -infinity)
-            uint32_t pw[4];
-#pragma unroll
-            for (int c = 0; c < 2; ++c) {
-#pragma unroll
-                for (int r = 0; r < 4; ++r) {
-                    const float p = __builtin_amdgcn_exp2f(fmaf(s[n][c][r], sc, base));
-                    s[n][c][r] = MASKED && s[n][c][r] == -INFINITY ? 0.f : p;
-                    l[n] += s[n][c][r];
-                }
-                pw[2 * c] = op_pack2<BF>(s[n][c][0], s[n][c][1]);
-                pw[2 * c + 1] = op_pack2<BF>(s[n][c][2], s[n][c][3]);
-            }
-            pf[n] = as_f16x8(make_uint4(pw[0], pw[1], pw[2], pw[3]));
-        }
+        for (int n = 0; n < NT; ++n) p[n] = pf[n][0];
         __builtin_amdgcn_sched_barrier(0);
         __builtin_amdgcn_s_waitcnt(0x0F70 | K_LOADS);        // the values of this block have landed (a wavefront reads its own only)
         __builtin_amdgcn_sched_barrier(0);
-        tr_v4i16 vf[DT][2];
-#pragma unroll
-        for (int i = 0; i < DT; ++i) {
-            const unsigned char* p = v_s[wave] + v_row * ROW + (((2 * i) | v_low) ^ swizzle(v_row)) * 16 + v_sub;
-            vf[i][0] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_tr_v4i16*)p);
-            vf[i][1] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_tr_v4i16*)(p + 16 * ROW));
-        }
-        __builtin_amdgcn_sched_barrier(0);
-        // A value that is not finite would reach the rows that do not see it as 0 times infinity.  In a block that holds one the products run
-        // on the others, and two more count the infinities of either sign (a NaN as both) that rows with a probability meet.
-        uint32_t odd = 0;
-        if constexpr (MASKED) {
-#pragma unroll
-            for (int i = 0; i < DT; ++i)
-#pragma unroll
-                for (int e = 0; e < 2; ++e) {
-                    const uint2 w = __builtin_bit_cast(uint2, vf[i][e]);
-                    odd |= beyond_of<BF>(w.x) | beyond_of<BF>(w.y);
-                }
-        }
-        if (MASKED && __any(odd & SIGNS)) {
-            f16x8_t there[NT];
-#pragma unroll
-            for (int n = 0; n < NT; ++n) {
-                const uint4 w = __builtin_bit_cast(uint4, pf[n]);
-                there[n] = as_f16x8(make_uint4(one_where<BF>(not_zero(w.x)), one_where<BF>(not_zero(w.y)), one_where<BF>(not_zero(w.z)), one_where<BF>(not_zero(w.w))));
-            }
-#pragma unroll
-            for (int i = 0; i < DT; ++i) {
-                __builtin_amdgcn_sched_barrier(0);           // (one after the other: registers, not speed)
-                const uint2 x = __builtin_bit_cast(uint2, vf[i][0]), y = __builtin_bit_cast(uint2, vf[i][1]);
-                const f16x8_t up = as_f16x8(make_uint4(infinite_of<BF>(x.x, 0), infinite_of<BF>(x.y, 0), infinite_of<BF>(y.x, 0), infinite_of<BF>(y.y, 0)));
-                const f16x8_t down = as_f16x8(make_uint4(infinite_of<BF>(x.x, ~0u), infinite_of<BF>(x.y, ~0u), infinite_of<BF>(y.x, ~0u), infinite_of<BF>(y.y, ~0u)));
-#pragma unroll
-                for (int n = 0; n < NT; ++n) {
-                    const f32x4_t zero = {0.f, 0.f, 0.f, 0.f}, u = mfma_16x16x32<BF>(up, there[n], zero), d = mfma_16x16x32<BF>(down, there[n], zero);
-#pragma unroll
-                    for (int r = 0; r < 4; ++r) o[n][i][r] += (u[r] > 0.f ? INFINITY : 0.f) - (d[r] > 0.f ? INFINITY : 0.f);
-                }
-                vf[i][0] = __builtin_bit_cast(tr_v4i16, make_uint2(finite_of<BF>(x.x), finite_of<BF>(x.y)));
-                vf[i][1] = __builtin_bit_cast(tr_v4i16, make_uint2(finite_of<BF>(y.x), finite_of<BF>(y.y)));
-            }
-        }
-#pragma unroll
-        for (int i = 0; i < DT; ++i) {
-            const f16x8_t v = __builtin_bit_cast(f16x8_t, __builtin_shufflevector(vf[i][0], vf[i][1], 0, 1, 2, 3, 4, 5, 6, 7));
-#pragma unroll
-            for (int n = 0; n < NT; ++n) o[n][i] = mfma_16x16x32<BF>(v, pf[n], o[n][i]);
-        }
+        add_values<BF, HD, NT, (NT > 1 ? 4 : DT), MASKED>(v_s[wave], p, o);
         __builtin_amdgcn_s_waitcnt(0xC07F);                  // the reads of this block are done
         __builtin_amdgcn_sched_barrier(0);
         load_values(k0 + STEP);
     };
-    for (; k0 + TREE_KEYS <= min(t.n_ctx, t.k1); k0 += STEP) block(std::false_type(), k0);
+    for (; k0 + KEYS <= min(t.n_ctx, t.k1); k0 += STEP) block(std::false_type(), k0);
     for (; k0 < t.k1; k0 += STEP) block(std::true_type(), k0);
     __builtin_amdgcn_sched_barrier(0);
     __builtin_amdgcn_s_waitcnt(0x0F70);                      // the values behind the last block: they land where the output goes
     __builtin_amdgcn_sched_barrier(0);
+    merge_wavefronts<BF ? SSD_BF16 : SSD_F16, HD, NT, KEY_WAVES>(a, t, kvh, m, l, o, sc, BIAS<BF>, reinterpret_cast<float*>(v_s), ml_s);
+}
 
-    merge_wavefronts<BF ? SSD_BF16 : SSD_F16, HD, NT>(a, t, kvh, m, l, o, sc, BIAS<BF>, reinterpret_cast<float*>(v_s), ml_s);
+// ---- many query rows: a wavefront has 16 NT of a K/V head for itself, the ROW_WAVES of a workgroup share 64-key blocks of keys and values in LDS, two of them
+// in turn: the next one loads while this one is used.
+constexpr int ROW_WAVES = 4;
+
+template <bool BF, int HD, int NT, class M>
+__global__ void __launch_bounds__(64 * ROW_WAVES, 2) tree_rows16_kernel(TreeAttnArgs a, M w) {
+    constexpr int KEYS = 64, ROW = HD * 2, BLOCK = KEYS * ROW, KS = HD / 32, DT = HD / 16, TR = 16 * NT * ROW_WAVES;
+    constexpr int CHUNKS = ROW / 16, L_ROWS = 64 / CHUNKS, LOADS = KEYS / L_ROWS / ROW_WAVES;
+    __shared__ __align__(1024) unsigned char kv_s[2][2][BLOCK];
+    __shared__ uint32_t span_s[MAX_TREE_NODES];
+    const int lane = threadIdx.x % 64, kg = lane / 16, dc = lane % 16;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
+    const int work = xcd_contiguous_index(blockIdx.x, gridDim.x);
+    const Work t = item_of(a, w, work / a.n_kv_heads, TR);
+    const int kvh = work % a.n_kv_heads;
+    const int G = a.n_q_heads / a.n_kv_heads, R = t.n_nodes * G;
+    const int last = max(t.k0, t.k1 - 1), row0 = t.row0 + wave * 16 * NT;
+    const int n_spans = t.k1 > t.n_ctx ? t.n_nodes : 0;
+    for (int i = threadIdx.x; i < n_spans; i += 64 * ROW_WAVES) span_s[i] = w(a.spans + t.node0 + i);
+    const int stride2 = (int)a.slot_stride * 2;
+    const int64_t first = (int64_t)t.slot0 * a.slot_stride + kvh * a.head_stride;
+    const uint16_t* kbase = (const uint16_t*)a.k + first;
+    const uint16_t* vbase = (const uint16_t*)a.v + first;
+    // Instruction i of a wavefront fills L_ROWS rows of the block.  Rows behind the range are copies of its last one.
+    auto load = [&](int k0, int stage) {
+        const int r0 = min(k0, last), beyond = last - r0;
+        const __amdgpu_buffer_rsrc_t k_rsrc = make_rsrc(kbase + (int64_t)r0 * a.slot_stride), v_rsrc = make_rsrc(vbase + (int64_t)r0 * a.slot_stride);
+#pragma unroll
+        for (int i = 0; i < LOADS; ++i) {
+            const int row = (i * ROW_WAVES + wave) * L_ROWS + lane / CHUNKS, off = min(row, beyond) * stride2, c = lane % CHUNKS;
+            const int k_off = off + (c ^ k_swizzle<HD>(row)) * 16, v_off = off + (c ^ v_swizzle<HD>(row)) * 16, at = (i * ROW_WAVES + wave) * 1024;
+            __builtin_amdgcn_raw_ptr_buffer_load_lds(k_rsrc, (lds_void_t*)(kv_s[stage][0] + at), 16, k_off, 0, 0, 0);
+            __builtin_amdgcn_raw_ptr_buffer_load_lds(v_rsrc, (lds_void_t*)(kv_s[stage][1] + at), 16, v_off, 0, 0, 0);
+        }
+    };
+    f16x8_t qf[NT][KS];
+    load_queries<HD, NT>(qf, a, t, kvh, row0);
+    load(t.k0, 0);
+    load(t.k0 + KEYS, 1);
+    const float sc = fabsf(a.scale) * LOG2E;
+    float m[NT], l[NT];
+    f32x4_t o[NT][DT];
+#pragma unroll
+    for (int n = 0; n < NT; ++n) {
+        m[n] = -F32_MOST;
+        l[n] = 0.f;
+#pragma unroll
+        for (int i = 0; i < DT; ++i) o[n][i] = (f32x4_t){0.f, 0.f, 0.f, 0.f};
+    }
+    const bool live = row0 < R;
+    auto block = [&](auto masked_c, int k0, int stage) {
+        constexpr bool MASKED = decltype(masked_c)::value;
+        f32x4_t s[NT][4];
+#pragma unroll
+        for (int c = 0; c < 4; ++c) {
+            f16x8_t kf[KS];
+#pragma unroll
+            for (int e = 0; e < KS; ++e) {
+                const int r = 16 * c + dc;
+                kf[e] = as_f16x8(*reinterpret_cast<const uint4*>(kv_s[stage][0] + r * ROW + ((kg + 4 * e) ^ k_swizzle<HD>(r)) * 16));
+            }
+#pragma unroll
+            for (int n = 0; n < NT; ++n) {
+                s[n][c] = (f32x4_t){0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+                for (int e = 0; e < KS; ++e) s[n][c] = mfma_16x16x32<BF>(kf[e], qf[n][e], s[n][c]);
+            }
+        }
+        if constexpr (MASKED) {
+            uint32_t key[4][4];
+            key_spans<4>(key, t, k0, span_s);
+#pragma unroll
+            for (int n = 0; n < NT; ++n) {
+                const uint32_t mine = span_s[min(row0 + 16 * n + dc, R - 1) / G];
+#pragma unroll
+                for (int c = 0; c < 4; ++c)
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) s[n][c][r] = sees(mine, key[c][r]) ? s[n][c][r] : -INFINITY;
+            }
+        }
+        f16x8_t pf[NT][2];
+        weights_of<BF, NT, 4, DT, MASKED>(s, m, l, o, sc, pf);
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            f16x8_t p[NT];
+#pragma unroll
+            for (int n = 0; n < NT; ++n) p[n] = pf[n][h];
+            add_values<BF, HD, NT, 4, MASKED>(kv_s[stage][1] + h * 32 * ROW, p, o);
+        }
+    };
+    int stage = 0;
+    for (int k0 = t.k0; k0 < t.k1; k0 += KEYS, stage ^= 1) {
+        __builtin_amdgcn_sched_barrier(0);
+        __builtin_amdgcn_s_waitcnt(0x0F70 | 2 * LOADS);      // this block; the next one may be in flight
+        lds_barrier();
+        if (live) {
+            if (k0 + KEYS <= min(t.n_ctx, t.k1)) block(std::false_type(), k0, stage);
+            else block(std::true_type(), k0, stage);
+        }
+        lds_barrier();                                       // all wavefronts are done with the block
+        load(k0 + 2 * KEYS, stage);
+    }
+    __builtin_amdgcn_sched_barrier(0);
+    __builtin_amdgcn_s_waitcnt(0x0F70);                      // nothing lands in LDS after the end
+    __builtin_amdgcn_sched_barrier(0);
+    if (!live) return;
+#pragma unroll
+    for (int n = 0; n < NT; ++n) {
+        l[n] += __shfl_xor(l[n], 16);
+        l[n] += __shfl_xor(l[n], 32);
+        const int r = 16 * n + dc, row = row0 + r;
+        if (row >= R) continue;
+        const int64_t at = (int64_t)(t.node0 + row / G) * a.n_q_heads + kvh * G + row % G;
+        if (t.index < a.n_parts) {
+            const int64_t part = ((int64_t)t.index * a.n_kv_heads + kvh) * TR + wave * 16 * NT + r;
+#pragma unroll
+            for (int i = 0; i < DT; ++i) *reinterpret_cast<f32x4_t*>(a.part_o + part * HD + 16 * i + 4 * kg) = o[n][i];
+            if (kg == 0) a.part_ml[part] = make_float2(m[n], l[n]);
+        } else {
+            const float inv = 1.f / l[n];
+#pragma unroll
+            for (int i = 0; i < DT; ++i)
+                *reinterpret_cast<uint2*>((uint16_t*)a.out + at * HD + 16 * i + 4 * kg) = make_uint2(op_pack2<BF>(o[n][i][0] * inv, o[n][i][1] * inv), op_pack2<BF>(o[n][i][2] * inv, o[n][i][3] * inv));
+            if (a.lse && kg == 0) a.lse[at] = (m[n] * sc - BIAS<BF> + __builtin_amdgcn_logf(l[n])) * LN2;
+        }
+    }
 }
 
 // The weight of every row: the scores once more, now that the log-sum-exps are known.  A workgroup owns a range of keys of a K/V head, a wavefront
@@ -260,16 +434,16 @@ __global__ void __launch_bounds__(64 * TREE_WAVES, NT == 4 ? 1 : 2) tree_attn16_
 // read spread over all banks.
 constexpr int MASS_ROWS = 128;
 
-template <bool BF, int HD>
-__global__ void __launch_bounds__(64 * TREE_WAVES, 2) tree_mass16_kernel(TreeAttnArgs a) {
-    constexpr int ROW = HD * 2, STEP = TREE_KEYS * TREE_WAVES, KS = HD / 32, CHUNKS = ROW / 16;
+template <bool BF, int HD, class M>
+__global__ void __launch_bounds__(64 * MASS_WAVES, 2) tree_mass16_kernel(TreeAttnArgs a, M w) {
+    constexpr int MASS_KEYS = 32, ROW = HD * 2, STEP = MASS_KEYS * MASS_WAVES, KS = HD / 32, CHUNKS = ROW / 16;
     __shared__ __align__(1024) unsigned char q_s[MASS_ROWS * ROW];
     __shared__ float lse_s[MASS_ROWS];
     __shared__ uint32_t row_span[MASS_ROWS], span_s[MAX_TREE_NODES];
     const int lane = threadIdx.x % 64, kg = lane / 16, dc = lane % 16;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
     const int work = xcd_contiguous_index(blockIdx.x, gridDim.x);
-    const TreeItem t = a.mass_items[work / a.n_kv_heads];
+    const Work t = mass_item_of(a, w, work / a.n_kv_heads);
     const int kvh = work % a.n_kv_heads;
     const int G = a.n_q_heads / a.n_kv_heads, R = t.n_nodes * G, last = t.k1 - 1;
     const int stride2 = (int)a.slot_stride * 2;
@@ -285,26 +459,25 @@ __global__ void __launch_bounds__(64 * TREE_WAVES, 2) tree_mass16_kernel(TreeAtt
             for (int s = 0; s < KS; ++s) kr[c][s] = __builtin_amdgcn_raw_buffer_load_b128(rsrc, off + 64 * s, 0, 0);
         }
     };
-    const int first = t.k0 + wave * TREE_KEYS;
+    const int first = t.k0 + wave * MASS_KEYS;
     load_keys(first);
     if (t.k1 > t.n_ctx)
-        for (int i = threadIdx.x; i < t.n_nodes; i += 64 * TREE_WAVES) span_s[i] = a.spans[t.node0 + i];
-    auto swizzle = [](int row) { return HD == 128 ? row & 15 : row >> 1 & 7; };
+        for (int i = threadIdx.x; i < t.n_nodes; i += 64 * MASS_WAVES) span_s[i] = w(a.spans + t.node0 + i);
     const float sc = fabsf(a.scale) * LOG2E;
     const uint32_t flip = a.scale < 0.f ? 0x80008000u : 0u;
     for (int r0 = 0; r0 < R; r0 += MASS_ROWS) {
         const int rows = min(MASS_ROWS, R - r0), tiles = (rows + 15) / 16;
         if (r0) __syncthreads();
-        for (int i = threadIdx.x; i < tiles * 16 * CHUNKS; i += 64 * TREE_WAVES) {
+        for (int i = threadIdx.x; i < tiles * 16 * CHUNKS; i += 64 * MASS_WAVES) {
             const int r = i / CHUNKS, c = i % CHUNKS, row = min(r0 + r, R - 1);
-            uint4 w = *reinterpret_cast<const uint4*>((const uint16_t*)a.q + (int64_t)(t.node0 + row / G) * a.q_stride + (kvh * G + row % G) * HD + c * 8);
-            w.x ^= flip; w.y ^= flip; w.z ^= flip; w.w ^= flip;
-            *reinterpret_cast<uint4*>(q_s + r * ROW + (c ^ swizzle(r)) * 16) = w;
+            uint4 x = *reinterpret_cast<const uint4*>((const uint16_t*)a.q + (int64_t)(t.node0 + row / G) * a.q_stride + (kvh * G + row % G) * HD + c * 8);
+            x.x ^= flip; x.y ^= flip; x.z ^= flip; x.w ^= flip;
+            *reinterpret_cast<uint4*>(q_s + r * ROW + (c ^ k_swizzle<HD>(r)) * 16) = x;
         }
-        for (int r = threadIdx.x; r < tiles * 16; r += 64 * TREE_WAVES) {
+        for (int r = threadIdx.x; r < tiles * 16; r += 64 * MASS_WAVES) {
             const int row = min(r0 + r, R - 1);
             lse_s[r] = r < rows ? a.lse[(int64_t)(t.node0 + row / G) * a.n_q_heads + kvh * G + row % G] * -LOG2E : -INFINITY;   // (rows behind the last: no weight)
-            row_span[r] = r < rows ? a.spans[t.node0 + row / G] : 0xffffu;
+            row_span[r] = r < rows ? w(a.spans + t.node0 + row / G) : 0xffffu;
         }
         __syncthreads();
         if (r0) load_keys(first);
@@ -312,16 +485,9 @@ __global__ void __launch_bounds__(64 * TREE_WAVES, 2) tree_mass16_kernel(TreeAtt
             f32x4_t acc[2];
 #pragma unroll
             for (int c = 0; c < 2; ++c) acc[c] = (f32x4_t){0.f, 0.f, 0.f, 0.f};
-            const bool masked = k0 + TREE_KEYS > t.n_ctx;
+            const bool masked = k0 + MASS_KEYS > t.n_ctx;
             uint32_t key[2][4];
-            if (masked)
-#pragma unroll
-                for (int c = 0; c < 2; ++c)
-#pragma unroll
-                    for (int r = 0; r < 4; ++r) {
-                        const int at = k0 + 16 * c + 4 * kg + r;
-                        key[c][r] = at < t.n_ctx ? 0xffff0000u : at < t.k1 ? span_s[at - t.n_ctx] : 0u;
-                    }
+            if (masked) key_spans<2>(key, t, k0, span_s);
             for (int n = 0; n < tiles; ++n) {
                 const int r = 16 * n + dc;
                 f32x4_t s[2];
@@ -329,7 +495,7 @@ __global__ void __launch_bounds__(64 * TREE_WAVES, 2) tree_mass16_kernel(TreeAtt
                 for (int c = 0; c < 2; ++c) s[c] = (f32x4_t){0.f, 0.f, 0.f, 0.f};
 #pragma unroll
                 for (int e = 0; e < KS; ++e) {
-                    const f16x8_t q = as_f16x8(*reinterpret_cast<const uint4*>(q_s + r * ROW + ((kg + 4 * e) ^ swizzle(r)) * 16));
+                    const f16x8_t q = as_f16x8(*reinterpret_cast<const uint4*>(q_s + r * ROW + ((kg + 4 * e) ^ k_swizzle<HD>(r)) * 16));
 #pragma unroll
                     for (int c = 0; c < 2; ++c) s[c] = mfma_16x16x32<BF>(__builtin_bit_cast(f16x8_t, kr[c][e]), q, s[c]);
                 }
@@ -349,22 +515,32 @@ __global__ void __launch_bounds__(64 * TREE_WAVES, 2) tree_mass16_kernel(TreeAtt
     }
 }
 
-template <bool BF, int HD>
-static void launch16(const TreeAttnArgs& a, hipStream_t st) {
+template <bool BF, int HD, class M>
+static void launch16(const TreeAttnArgs& a, const M& w, hipStream_t st) {
     const dim3 grid(a.n_items * a.n_kv_heads);
-    if (a.tile_rows == 16) hipLaunchKernelGGL((tree_attn16_kernel<BF, HD, 1>), grid, dim3(64 * TREE_WAVES), 0, st, a);
-    else if (a.tile_rows == 32) hipLaunchKernelGGL((tree_attn16_kernel<BF, HD, 2>), grid, dim3(64 * TREE_WAVES), 0, st, a);
-    else hipLaunchKernelGGL((tree_attn16_kernel<BF, HD, 4>), grid, dim3(64 * TREE_WAVES), 0, st, a);
-    constexpr int DT = BF ? SSD_BF16 : SSD_F16, ROWS = 256 / (HD / 4);
+    if (a.tile_rows == 16) hipLaunchKernelGGL((tree_keys16_kernel<BF, HD, 1, M>), grid, dim3(64 * KEY_WAVES), 0, st, a, w);
+    else if (a.tile_rows == 32) hipLaunchKernelGGL((tree_keys16_kernel<BF, HD, 2, M>), grid, dim3(64 * KEY_WAVES), 0, st, a, w);
+    else if (a.tile_rows == 64) hipLaunchKernelGGL((tree_rows16_kernel<BF, HD, 1, M>), grid, dim3(64 * ROW_WAVES), 0, st, a, w);
+    else hipLaunchKernelGGL((tree_rows16_kernel<BF, HD, 2, M>), grid, dim3(64 * ROW_WAVES), 0, st, a, w);
     if (a.n_joins)
-        hipLaunchKernelGGL((tree_join_kernel<DT, HD>), dim3(a.n_joins, a.n_kv_heads, (a.tile_rows + ROWS - 1) / ROWS), dim3(256), 0, st, a, a.tile_rows, BIAS<BF>);
-    if (a.mass) hipLaunchKernelGGL((tree_mass16_kernel<BF, HD>), dim3(a.n_mass_items * a.n_kv_heads), dim3(64 * TREE_WAVES), 0, st, a);
+        hipLaunchKernelGGL((tree_join_kernel<BF ? SSD_BF16 : SSD_F16, HD, M>), dim3(a.n_joins * a.tile_rows, a.n_kv_heads), dim3(256), 0, st, a, w, BIAS<BF>);
+    if (a.mass) hipLaunchKernelGGL((tree_mass16_kernel<BF, HD, M>), dim3(a.n_mass * a.n_kv_heads), dim3(64 * MASS_WAVES), 0, st, a, w);
 }
 
-void launch_tree_attention(const TreeAttnArgs& a, hipStream_t st) {
-    if (a.dtype == SSD_F32) launch_tree_attention32(a, st);
-    else if (a.head_dim == 64) a.dtype == SSD_BF16 ? launch16<true, 64>(a, st) : launch16<false, 64>(a, st);
-    else a.dtype == SSD_BF16 ? launch16<true, 128>(a, st) : launch16<false, 128>(a, st);
+template <class M>
+static void launch_any(const TreeAttnArgs& a, const M& w, hipStream_t st) {
+    if (a.dtype == SSD_F32) launch_tree_attention32(a, w, st);
+    else if (a.head_dim == 64) a.dtype == SSD_BF16 ? launch16<true, 64>(a, w, st) : launch16<false, 64>(a, w, st);
+    else a.dtype == SSD_BF16 ? launch16<true, 128>(a, w, st) : launch16<false, 128>(a, w, st);
+}
+
+void launch_tree_attention(const TreeAttnArgs& a, const uint32_t* words, int n, const uint32_t* dev_words, hipStream_t st) {
+    static_assert(sizeof(TreeAttnArgs) + sizeof(MetaWords) + 16 <= 4096, "arguments of a launch");
+    if (!words) { launch_any(a, MetaArray{dev_words}, st); return; }
+    MetaWords w;
+    w.n = n;
+    memcpy(w.word, words, (size_t)n * 4);
+    launch_any(a, w, st);
 }
 
 }  // namespace ssd

@@ -20,22 +20,22 @@ __device__ __forceinline__ void load_rows32(f32x4_t (&x)[HD / 16], const float* 
     }
 }
 
-template <int HD, int NT>
-__global__ void __launch_bounds__(64 * TREE_WAVES, 2) tree_attn32_kernel(TreeAttnArgs a) {
-    constexpr int ROW = HD * 4, BLOCK = TREE32_KEYS * ROW, STEP = TREE32_KEYS * TREE_WAVES, DT = HD / 16, TR = 16 * NT;
+template <int HD, int NT, class M>
+__global__ void __launch_bounds__(64 * KEY_WAVES, 2) tree_attn32_kernel(TreeAttnArgs a, M w) {
+    constexpr int ROW = HD * 4, BLOCK = TREE32_KEYS * ROW, STEP = TREE32_KEYS * KEY_WAVES, DT = HD / 16, TR = 16 * NT;
     constexpr int ROW_CHUNKS = ROW / 16, V_ROWS = 64 / ROW_CHUNKS, V_LOADS = TREE32_KEYS / V_ROWS;
-    __shared__ __align__(1024) unsigned char v_s[TREE_WAVES][BLOCK];
-    __shared__ float2 ml_s[TREE_WAVES * TR];
+    __shared__ __align__(1024) unsigned char v_s[KEY_WAVES][BLOCK];
+    __shared__ float2 ml_s[KEY_WAVES * TR];
     __shared__ uint32_t span_s[MAX_TREE_NODES];
     const int lane = threadIdx.x % 64, kg = lane / 16, dc = lane % 16;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
     const int work = xcd_contiguous_index(blockIdx.x, gridDim.x);
-    const TreeItem t = a.items[work / a.n_kv_heads];
+    const Work t = item_of(a, w, work / a.n_kv_heads, TR);
     const int kvh = work % a.n_kv_heads, hd = a.head_dim;
     const int G = a.n_q_heads / a.n_kv_heads, R = t.n_nodes * G;
     const int last = max(t.k0, t.k1 - 1);                    // (a range without keys: any row)
     const int n_spans = t.k1 > t.n_ctx ? t.n_nodes : 0;
-    for (int i = threadIdx.x; i < n_spans; i += 64 * TREE_WAVES) span_s[i] = a.spans[t.node0 + i];
+    for (int i = threadIdx.x; i < n_spans; i += 64 * KEY_WAVES) span_s[i] = w(a.spans + t.node0 + i);
     const int64_t first = (int64_t)t.slot0 * a.slot_stride + kvh * a.head_stride;
     const float* kbase = (const float*)a.k + first;
     const float* vbase = (const float*)a.v + first;
@@ -173,21 +173,21 @@ __global__ void __launch_bounds__(64 * TREE_WAVES, 2) tree_attn32_kernel(TreeAtt
     __builtin_amdgcn_sched_barrier(0);
     __builtin_amdgcn_s_waitcnt(0x0F70);                      // the values behind the last block: they land where the output goes
     __builtin_amdgcn_sched_barrier(0);
-    merge_wavefronts<SSD_F32, HD, NT>(a, t, kvh, m, l, o, sc, 0.f, reinterpret_cast<float*>(v_s), ml_s);
+    merge_wavefronts<SSD_F32, HD, NT, KEY_WAVES>(a, t, kvh, m, l, o, sc, 0.f, reinterpret_cast<float*>(v_s), ml_s);
 }
 
 constexpr int MASS32_ROWS = 64;
 
-template <int HD>
-__global__ void __launch_bounds__(64 * TREE_WAVES, 2) tree_mass32_kernel(TreeAttnArgs a) {
-    constexpr int STEP = TREE32_KEYS * TREE_WAVES, DT = HD / 16, CHUNKS = HD / 4;
+template <int HD, class M>
+__global__ void __launch_bounds__(64 * MASS_WAVES, 2) tree_mass32_kernel(TreeAttnArgs a, M w) {
+    constexpr int STEP = TREE32_KEYS * MASS_WAVES, DT = HD / 16, CHUNKS = HD / 4;
     __shared__ __align__(1024) float q_s[MASS32_ROWS * HD];
     __shared__ float lse_s[MASS32_ROWS];
     __shared__ uint32_t row_span[MASS32_ROWS], span_s[MAX_TREE_NODES];
     const int lane = threadIdx.x % 64, kg = lane / 16, dc = lane % 16;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
     const int work = xcd_contiguous_index(blockIdx.x, gridDim.x);
-    const TreeItem t = a.mass_items[work / a.n_kv_heads];
+    const Work t = mass_item_of(a, w, work / a.n_kv_heads);
     const int kvh = work % a.n_kv_heads, hd = a.head_dim;
     const int G = a.n_q_heads / a.n_kv_heads, R = t.n_nodes * G, last = t.k1 - 1;
     const float* kbase = (const float*)a.k + (int64_t)t.slot0 * a.slot_stride + kvh * a.head_stride;
@@ -196,21 +196,21 @@ __global__ void __launch_bounds__(64 * TREE_WAVES, 2) tree_mass32_kernel(TreeAtt
     const int first = t.k0 + wave * TREE32_KEYS;
     load_keys(first);
     if (t.k1 > t.n_ctx)
-        for (int i = threadIdx.x; i < t.n_nodes; i += 64 * TREE_WAVES) span_s[i] = a.spans[t.node0 + i];
+        for (int i = threadIdx.x; i < t.n_nodes; i += 64 * MASS_WAVES) span_s[i] = w(a.spans + t.node0 + i);
     const float sc = fabsf(a.scale) * LOG2E, sign = a.scale < 0.f ? -1.f : 1.f;
     for (int r0 = 0; r0 < R; r0 += MASS32_ROWS) {
         const int rows = min(MASS32_ROWS, R - r0), tiles = (rows + 15) / 16;
         if (r0) __syncthreads();
-        for (int i = threadIdx.x; i < tiles * 16 * CHUNKS; i += 64 * TREE_WAVES) {
+        for (int i = threadIdx.x; i < tiles * 16 * CHUNKS; i += 64 * MASS_WAVES) {
             const int r = i / CHUNKS, c = i % CHUNKS, row = min(r0 + r, R - 1);
-            f32x4_t w = {0.f, 0.f, 0.f, 0.f};
-            if (c * 4 < hd) w = *reinterpret_cast<const f32x4_t*>((const float*)a.q + (int64_t)(t.node0 + row / G) * a.q_stride + (kvh * G + row % G) * hd + c * 4);
-            *reinterpret_cast<f32x4_t*>(q_s + r * HD + (c ^ (r & 15)) * 4) = w * sign;
+            f32x4_t x = {0.f, 0.f, 0.f, 0.f};
+            if (c * 4 < hd) x = *reinterpret_cast<const f32x4_t*>((const float*)a.q + (int64_t)(t.node0 + row / G) * a.q_stride + (kvh * G + row % G) * hd + c * 4);
+            *reinterpret_cast<f32x4_t*>(q_s + r * HD + (c ^ (r & 15)) * 4) = x * sign;
         }
-        for (int r = threadIdx.x; r < tiles * 16; r += 64 * TREE_WAVES) {
+        for (int r = threadIdx.x; r < tiles * 16; r += 64 * MASS_WAVES) {
             const int row = min(r0 + r, R - 1);
             lse_s[r] = r < rows ? a.lse[(int64_t)(t.node0 + row / G) * a.n_q_heads + kvh * G + row % G] * -LOG2E : -INFINITY;   // (rows behind the last: no weight)
-            row_span[r] = r < rows ? a.spans[t.node0 + row / G] : 0xffffu;
+            row_span[r] = r < rows ? w(a.spans + t.node0 + row / G) : 0xffffu;
         }
         __syncthreads();
         if (r0) load_keys(first);
@@ -247,20 +247,21 @@ __global__ void __launch_bounds__(64 * TREE_WAVES, 2) tree_mass32_kernel(TreeAtt
     }
 }
 
-template <int HD>
-static void launch32(const TreeAttnArgs& a, hipStream_t st) {
+template <int HD, class M>
+static void launch32(const TreeAttnArgs& a, const M& w, hipStream_t st) {
     const dim3 grid(a.n_items * a.n_kv_heads);
-    if (a.tile_rows == 16) hipLaunchKernelGGL((tree_attn32_kernel<HD, 1>), grid, dim3(64 * TREE_WAVES), 0, st, a);
-    else hipLaunchKernelGGL((tree_attn32_kernel<HD, 2>), grid, dim3(64 * TREE_WAVES), 0, st, a);
-    constexpr int ROWS = 256 / (HD / 4);
-    if (a.n_joins)
-        hipLaunchKernelGGL((tree_join_kernel<SSD_F32, HD>), dim3(a.n_joins, a.n_kv_heads, (a.tile_rows + ROWS - 1) / ROWS), dim3(256), 0, st, a, a.tile_rows, 0.f);
-    if (a.mass) hipLaunchKernelGGL((tree_mass32_kernel<HD>), dim3(a.n_mass_items * a.n_kv_heads), dim3(64 * TREE_WAVES), 0, st, a);
+    if (a.tile_rows == 16) hipLaunchKernelGGL((tree_attn32_kernel<HD, 1, M>), grid, dim3(64 * KEY_WAVES), 0, st, a, w);
+    else hipLaunchKernelGGL((tree_attn32_kernel<HD, 2, M>), grid, dim3(64 * KEY_WAVES), 0, st, a, w);
+    if (a.n_joins) hipLaunchKernelGGL((tree_join_kernel<SSD_F32, HD, M>), dim3(a.n_joins * a.tile_rows, a.n_kv_heads), dim3(256), 0, st, a, w, 0.f);
+    if (a.mass) hipLaunchKernelGGL((tree_mass32_kernel<HD, M>), dim3(a.n_mass * a.n_kv_heads), dim3(64 * MASS_WAVES), 0, st, a, w);
 }
 
-void launch_tree_attention32(const TreeAttnArgs& a, hipStream_t st) {
-    if (a.head_dim <= 64) launch32<64>(a, st);
-    else launch32<128>(a, st);
+template <class M>
+void launch_tree_attention32(const TreeAttnArgs& a, const M& w, hipStream_t st) {
+    if (a.head_dim <= 64) launch32<64>(a, w, st);
+    else launch32<128>(a, w, st);
 }
+template void launch_tree_attention32(const TreeAttnArgs&, const MetaWords&, hipStream_t);
+template void launch_tree_attention32(const TreeAttnArgs&, const MetaArray&, hipStream_t);
 
 }  // namespace ssd

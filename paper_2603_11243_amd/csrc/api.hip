@@ -1446,7 +1446,7 @@ void tree_spans(int n, const int32_t* parent, uint32_t* span) {
 }
 // Query rows of an item of work: as many as the largest tree has, in one of the shapes of the kernels.  Up to TREE_KEY_ROWS rows the wavefronts of a workgroup
 // split the keys; fp32 has no other kernel.
-int tree_tile_rows(int dtype, int rows) { return rows <= 16 ? 16 : rows <= TREE_KEY_ROWS || dtype == SSD_F32 ? TREE_KEY_ROWS : rows <= 64 ? 64 : 128; }
+int tree_tile_rows(int dtype, int rows) { return rows <= 16 ? 16 : dtype == SSD_F32 || rows <= TREE_KEY_ROWS ? 32 : rows <= 64 ? 64 : 128; }
 // Ranges of keys: one per item, unless that leaves most of the chip without work or an utterance is longer than its share; then pieces of such a share.
 void tree_work(int B, const int32_t* kv_start, const int32_t* ctx_len, const int32_t* cu_nodes, const int32_t* parent, int most, int n_q_heads, const ssd_kv_view& kv,
                bool mass, TreeWork& w) {
@@ -1464,11 +1464,7 @@ void tree_work(int B, const int32_t* kv_start, const int32_t* ctx_len, const int
     const int64_t mass_step = std::min<int64_t>(step_of(per_row, pieces, TREE_MASS_KEYS), 0x7fffff00);
     std::vector<uint32_t>& v = w.words;
     TreeAttnArgs& a = w.a;
-    v.reserve((size_t)B * 8 + cu_nodes[B] + 256);
-    for (int b = 0; b < B; ++b) { v.push_back(kv_start[b]); v.push_back(ctx_len[b]); }
-    a.cu = (int)v.size();
-    v.insert(v.end(), cu_nodes, cu_nodes + B + 1);
-    a.items = (int)v.size();
+    v.reserve((size_t)B * 12 + cu_nodes[B] + 512);
     a.n_items = a.n_parts = a.n_joins = a.n_mass = 0;
     auto tiles_of = [&](int b) { return ((cu_nodes[b + 1] - cu_nodes[b]) * G + rows - 1) / rows; };
     auto parts_of = [&](int b) { return ((int64_t)ctx_len[b] + cu_nodes[b + 1] - cu_nodes[b] + step - 1) / step; };
@@ -1477,10 +1473,17 @@ void tree_work(int B, const int32_t* kv_start, const int32_t* ctx_len, const int
             const int tiles = tiles_of(b), parts = (int)parts_of(b);
             if (!tiles || (parts > 1) != (cut == 1)) continue;
             for (int p = 0; p < parts; ++p)                  // tiles of the same keys one behind the other: they meet in an L2
-                for (int t = 0; t < tiles; ++t) { v.push_back((uint32_t)b | (uint32_t)t << 16); v.push_back(p); }
+                for (int t = 0; t < tiles; ++t)
+                    for (uint32_t x : {(uint32_t)kv_start[b], (uint32_t)ctx_len[b], (uint32_t)cu_nodes[b], (uint32_t)(cu_nodes[b + 1] - cu_nodes[b]) | (uint32_t)t << 11,
+                                       (uint32_t)p})
+                        v.push_back(x);
             a.n_items += parts * tiles;
             if (cut) a.n_parts = a.n_items;
         }
+    a.utts = (int)v.size();
+    for (int b = 0; b < B; ++b) { v.push_back(kv_start[b]); v.push_back(ctx_len[b]); }
+    a.cu = (int)v.size();
+    v.insert(v.end(), cu_nodes, cu_nodes + B + 1);
     a.joins = (int)v.size();
     for (int b = 0, first = 0; b < B; ++b) {
         const int tiles = tiles_of(b), parts = (int)parts_of(b);
@@ -1519,8 +1522,8 @@ TreePlan plan_tree(const TreeWork& w, int64_t nodes, bool own_lse) {
 // cut only where its keys, times its tiles, are more than one of TREE_WORKGROUPS / n_kv_heads shares, so that there are at most twice as many pieces.
 size_t max_tree_bytes(int n_q_heads, int n_kv_heads, int head_dim, int64_t max_nodes, int64_t max_utts) {
     const int64_t G = (n_q_heads + n_kv_heads - 1) / n_kv_heads, cut = 2 * std::max(1, TREE_WORKGROUPS / n_kv_heads), rows = max_nodes * G;
-    const int64_t tile = rows <= 16 ? 16 : rows <= TREE_KEY_ROWS ? TREE_KEY_ROWS : rows <= 64 ? 64 : 128;
-    return plan_tree(3 * max_utts + 1 + 2 * (rows + cut) + 3 * rows + max_utts + cut + max_nodes, max_nodes * n_q_heads, cut * n_kv_heads * tile, head_dim).total;
+    const int64_t tile = rows <= 16 ? 16 : rows <= 32 ? (TREE_KEY_ROWS < 32 ? 64 : 32) : rows <= 64 ? 64 : 128;
+    return plan_tree(3 * max_utts + 1 + 5 * (rows + cut) + 3 * rows + max_utts + cut + max_nodes, max_nodes * n_q_heads, cut * n_kv_heads * tile, head_dim).total;
 }
 void run_tree_attention(ssd_ctx* c, TreeWork& w, const TreePlan& p, char* ws, bool in_args, const void* k, const void* v, int64_t slots, const void* q, int64_t q_stride,
                         float scale, void* out, float* lse, float* mass) {

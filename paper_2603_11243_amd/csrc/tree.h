@@ -23,10 +23,11 @@ struct MetaArray {
 void launch_write_words(const MetaWords& w, uint32_t* dst, hipStream_t st);
 
 // Attention of nodes.  Query rows of one K/V head are numbered node * G + head of the group; keys are the rows of the utterance, n_ctx cached ones, then
-// the nodes.  The words: per utterance (first slot, n_ctx); from `cu` on the B + 1 prefix sums of the nodes; from `items` on per item of work two: utterance |
-// tile of tile_rows query rows << 16, piece of `step` keys (the first n_parts items leave partial results); from `joins` on per tile of a cut
-// utterance three: utterance | tile << 16, item of its first piece, pieces; from `mass` on per item of the weights one: utterance |
-// piece of mass_step keys << 16; from `spans` on per node its place in depth-first order | end of its subtree << 16.
+// the nodes.  The words: per item of work five, at a place known without another: first slot, n_ctx, first node, nodes | tile of tile_rows query rows << 11,
+// piece of `step` keys (the first n_parts items leave partial results); from `utts` on per utterance first slot and n_ctx, from `cu` on the
+// B + 1 prefix sums of the nodes; from `joins` on per tile of a cut utterance three: utterance | tile << 16, item of its first piece,
+// pieces; from `mass_items` on per item of the weights one: utterance | piece of mass_step keys << 16; from `spans` on per node its place in
+// depth-first order | end of its subtree << 16.
 struct TreeAttnArgs {
     const void* q; int64_t q_stride;
     const void* k; const void* v; int64_t slot_stride, head_stride;
@@ -37,11 +38,11 @@ struct TreeAttnArgs {
     int n_q_heads, n_kv_heads, head_dim, dtype;
     float scale;
     int tile_rows, step, mass_step, n_items, n_parts, n_joins, n_mass;
-    int cu, items, joins, mass_items, spans;
+    int utts, cu, joins, mass_items, spans;
 };
 // words: host memory, n of them, to travel as arguments; or NULL, then they are in dev_words
 void launch_tree_attention(const TreeAttnArgs& a, const uint32_t* words, int n, const uint32_t* dev_words, hipStream_t st);
-constexpr int TREE_KEY_ROWS = 32;            // up to as many query rows in the largest tree: the wavefronts of a workgroup split the keys
+constexpr int TREE_KEY_ROWS = 16;            // up to as many query rows in the largest tree: the wavefronts of a workgroup split the keys
 constexpr int TREE_WORKGROUPS = 512;         // long contexts are cut into about as many pieces in all, times K/V heads
 constexpr int TREE_SPLIT_KEYS = 512;         // a piece has at least as many keys
 constexpr int TREE_MASS_KEYS = 128;          // and one of the weights a multiple of these

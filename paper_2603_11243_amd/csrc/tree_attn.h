@@ -34,26 +34,27 @@ constexpr float F32_MOST = 3.4028234663852886e38f;
 struct Work { int slot0, n_ctx, n_nodes, node0, row0, k0, k1, index; };
 template <class M>
 __device__ __forceinline__ void utterance_of(const TreeAttnArgs& a, const M& w, int b, Work& t) {
-    t.slot0 = (int)w(2 * b);
-    t.n_ctx = (int)w(2 * b + 1);
+    t.slot0 = (int)w(a.utts + 2 * b);
+    t.n_ctx = (int)w(a.utts + 2 * b + 1);
     t.node0 = (int)w(a.cu + b);
     t.n_nodes = (int)w(a.cu + b + 1) - t.node0;
 }
 template <class M>
 __device__ __forceinline__ Work item_of(const TreeAttnArgs& a, const M& w, int index, int tile_rows) {
     Work t;
-    const uint32_t x = w(a.items + 2 * index);
-    utterance_of(a, w, x & 0xffffu, t);
-    const int G = a.n_q_heads / a.n_kv_heads;
+    const uint32_t x = w(5 * index + 3);
     t.index = index;
-    t.row0 = (int)(x >> 16) * tile_rows;
-    const int64_t k0 = (int64_t)w(a.items + 2 * index + 1) * a.step;
-    const int node = (min(t.n_nodes * G, t.row0 + tile_rows) - 1) / G;              // no row of the tile sees a later one
+    t.slot0 = (int)w(5 * index);
+    t.n_ctx = (int)w(5 * index + 1);
+    t.node0 = (int)w(5 * index + 2);
+    t.n_nodes = (int)(x & 0x7ffu);
+    t.row0 = (int)(x >> 11) * tile_rows;
+    const int64_t k0 = (int64_t)w(5 * index + 4) * a.step;
+    const int G = a.n_q_heads / a.n_kv_heads, node = (min(t.n_nodes * G, t.row0 + tile_rows) - 1) / G;       // no row of the tile sees a later one
     t.k0 = (int)k0;
     t.k1 = (int)min((int64_t)t.n_ctx + node + 1, k0 + a.step);
     return t;
 }
-
 template <class M>
 __device__ __forceinline__ Work mass_item_of(const TreeAttnArgs& a, const M& w, int index) {
     Work t;

@@ -47,16 +47,16 @@ __device__ __forceinline__ void key_spans(uint32_t (&key)[C][4], const Work& t, 
         }
 }
 
-// Scores of 16 C keys to weights in the operand type; maxima, sums and outputs follow.
-template <bool BF, int NT, int C, int DT, bool MASKED>
-__device__ __forceinline__ void weights_of(f32x4_t (&s)[NT][C], float (&m)[NT], float (&l)[NT], f32x4_t (&o)[NT][DT], float sc, f16x8_t (&pf)[NT][C / 2]) {
+// Scores of 32 keys to weights in the operand type; maxima, sums and outputs follow.
+template <bool BF, int NT, int DT, bool MASKED>
+__device__ __forceinline__ void weights_of(f32x4_t (&s)[NT][2], float (&m)[NT], float (&l)[NT], f32x4_t (&o)[NT][DT], float sc, f16x8_t (&pf)[NT]) {
     float mx[NT];
     bool above = false;
 #pragma unroll
     for (int n = 0; n < NT; ++n) {
         mx[n] = -INFINITY;
 #pragma unroll
-        for (int c = 0; c < C; ++c) mx[n] = fmaxf(mx[n], fmaxf(fmaxf(s[n][c][0], s[n][c][1]), fmaxf(s[n][c][2], s[n][c][3])));
+        for (int c = 0; c < 2; ++c) mx[n] = fmaxf(mx[n], fmaxf(fmaxf(s[n][c][0], s[n][c][1]), fmaxf(s[n][c][2], s[n][c][3])));
         above |= (mx[n] - m[n]) * sc > LAG;
     }
     if (__any(above)) {
@@ -74,23 +74,20 @@ __device__ __forceinline__ void weights_of(f32x4_t (&s)[NT][C], float (&m)[NT], 
 #pragma unroll
     for (int n = 0; n < NT; ++n) {
         const float base = fminf(BIAS<BF> - m[n] * sc, F32_MOST);    // (finite: a score may be -infinity)
+        uint32_t pw[4];
 #pragma unroll
-        for (int h = 0; h < C / 2; ++h) {
-            uint32_t pw[4];
+        for (int c = 0; c < 2; ++c) {
+            f32x4_t& x = s[n][c];
 #pragma unroll
-            for (int c = 0; c < 2; ++c) {
-                f32x4_t& x = s[n][2 * h + c];
-#pragma unroll
-                for (int r = 0; r < 4; ++r) {
-                    const float p = __builtin_amdgcn_exp2f(fmaf(x[r], sc, base));
-                    x[r] = MASKED && x[r] == -INFINITY ? 0.f : p;
-                    l[n] += x[r];
-                }
-                pw[2 * c] = op_pack2<BF>(x[0], x[1]);
-                pw[2 * c + 1] = op_pack2<BF>(x[2], x[3]);
+            for (int r = 0; r < 4; ++r) {
+                const float p = __builtin_amdgcn_exp2f(fmaf(x[r], sc, base));
+                x[r] = MASKED && x[r] == -INFINITY ? 0.f : p;
+                l[n] += x[r];
             }
-            pf[n][h] = as_f16x8(make_uint4(pw[0], pw[1], pw[2], pw[3]));
+            pw[2 * c] = op_pack2<BF>(x[0], x[1]);
+            pw[2 * c + 1] = op_pack2<BF>(x[2], x[3]);
         }
+        pf[n] = as_f16x8(make_uint4(pw[0], pw[1], pw[2], pw[3]));
     }
 }
 
@@ -280,11 +277,8 @@ __global__ void __launch_bounds__(64 * KEY_WAVES, 2) tree_keys16_kernel(TreeAttn
                     for (int r = 0; r < 4; ++r) s[n][c][r] = sees(mine, key[c][r]) ? s[n][c][r] : -INFINITY;
             }
         }
-        f16x8_t pf[NT][1];
-        weights_of<BF, NT, 2, DT, MASKED>(s, m, l, o, sc, pf);
         f16x8_t p[NT];
-#pragma unroll
-        for (int n = 0; n < NT; ++n) p[n] = pf[n][0];
+        weights_of<BF, NT, DT, MASKED>(s, m, l, o, sc, p);
         __builtin_amdgcn_sched_barrier(0);
         __builtin_amdgcn_s_waitcnt(0x0F70 | K_LOADS);        // the values of this block have landed (a wavefront reads its own only)
         __builtin_amdgcn_sched_barrier(0);
@@ -319,7 +313,7 @@ __global__ void __launch_bounds__(64 * ROW_WAVES, 2) tree_rows16_kernel(TreeAttn
     const int G = a.n_q_heads / a.n_kv_heads, R = t.n_nodes * G;
     const int last = max(t.k0, t.k1 - 1), row0 = t.row0 + wave * 16 * NT;
     const int n_spans = t.k1 > t.n_ctx ? t.n_nodes : 0;
-    for (int i = threadIdx.x; i < n_spans; i += 64 * ROW_WAVES) span_s[i] = w(a.spans + t.node0 + i);
+    const uint32_t span = (int)threadIdx.x < n_spans ? w(a.spans + t.node0 + (int)threadIdx.x) : 0u;
     const int stride2 = (int)a.slot_stride * 2;
     const int64_t first = (int64_t)t.slot0 * a.slot_stride + kvh * a.head_stride;
     const uint16_t* kbase = (const uint16_t*)a.k + first;
@@ -340,6 +334,8 @@ __global__ void __launch_bounds__(64 * ROW_WAVES, 2) tree_rows16_kernel(TreeAttn
     load_queries<HD, NT>(qf, a, t, kvh, row0);
     load(t.k0, 0);
     load(t.k0 + KEYS, 1);
+    if ((int)threadIdx.x < n_spans) span_s[threadIdx.x] = span;
+    for (int i = threadIdx.x + 64 * ROW_WAVES; i < n_spans; i += 64 * ROW_WAVES) span_s[i] = w(a.spans + t.node0 + i);
     const float sc = fabsf(a.scale) * LOG2E;
     float m[NT], l[NT];
     f32x4_t o[NT][DT];
@@ -351,16 +347,16 @@ __global__ void __launch_bounds__(64 * ROW_WAVES, 2) tree_rows16_kernel(TreeAttn
         for (int i = 0; i < DT; ++i) o[n][i] = (f32x4_t){0.f, 0.f, 0.f, 0.f};
     }
     const bool live = row0 < R;
-    auto block = [&](auto masked_c, int k0, int stage) {
+    auto half = [&](auto masked_c, int k0, const unsigned char* k, const unsigned char* v) {      // 32 keys
         constexpr bool MASKED = decltype(masked_c)::value;
-        f32x4_t s[NT][4];
+        f32x4_t s[NT][2];
 #pragma unroll
-        for (int c = 0; c < 4; ++c) {
+        for (int c = 0; c < 2; ++c) {
             f16x8_t kf[KS];
 #pragma unroll
             for (int e = 0; e < KS; ++e) {
                 const int r = 16 * c + dc;
-                kf[e] = as_f16x8(*reinterpret_cast<const uint4*>(kv_s[stage][0] + r * ROW + ((kg + 4 * e) ^ k_swizzle<HD>(r)) * 16));
+                kf[e] = as_f16x8(*reinterpret_cast<const uint4*>(k + r * ROW + ((kg + 4 * e) ^ k_swizzle<HD>(r)) * 16));
             }
 #pragma unroll
             for (int n = 0; n < NT; ++n) {
@@ -370,26 +366,20 @@ __global__ void __launch_bounds__(64 * ROW_WAVES, 2) tree_rows16_kernel(TreeAttn
             }
         }
         if constexpr (MASKED) {
-            uint32_t key[4][4];
-            key_spans<4>(key, t, k0, span_s);
+            uint32_t key[2][4];
+            key_spans<2>(key, t, k0, span_s);
 #pragma unroll
             for (int n = 0; n < NT; ++n) {
                 const uint32_t mine = span_s[min(row0 + 16 * n + dc, R - 1) / G];
 #pragma unroll
-                for (int c = 0; c < 4; ++c)
+                for (int c = 0; c < 2; ++c)
 #pragma unroll
                     for (int r = 0; r < 4; ++r) s[n][c][r] = sees(mine, key[c][r]) ? s[n][c][r] : -INFINITY;
             }
         }
-        f16x8_t pf[NT][2];
-        weights_of<BF, NT, 4, DT, MASKED>(s, m, l, o, sc, pf);
-#pragma unroll
-        for (int h = 0; h < 2; ++h) {
-            f16x8_t p[NT];
-#pragma unroll
-            for (int n = 0; n < NT; ++n) p[n] = pf[n][h];
-            add_values<BF, HD, NT, 4, MASKED>(kv_s[stage][1] + h * 32 * ROW, p, o);
-        }
+        f16x8_t p[NT];
+        weights_of<BF, NT, DT, MASKED>(s, m, l, o, sc, p);
+        add_values<BF, HD, NT, 4, MASKED>(v, p, o);
     };
     int stage = 0;
     for (int k0 = t.k0; k0 < t.k1; k0 += KEYS, stage ^= 1) {
@@ -397,8 +387,12 @@ __global__ void __launch_bounds__(64 * ROW_WAVES, 2) tree_rows16_kernel(TreeAttn
         __builtin_amdgcn_s_waitcnt(0x0F70 | 2 * LOADS);      // this block; the next one may be in flight
         lds_barrier();
         if (live) {
-            if (k0 + KEYS <= min(t.n_ctx, t.k1)) block(std::false_type(), k0, stage);
-            else block(std::true_type(), k0, stage);
+#pragma unroll 1
+            for (int h = 0; h < 2; ++h) {
+                const unsigned char *k = kv_s[stage][0] + h * 32 * ROW, *v = kv_s[stage][1] + h * 32 * ROW;
+                if (k0 + 32 * h + 32 <= min(t.n_ctx, t.k1)) half(std::false_type(), k0 + 32 * h, k, v);
+                else if (k0 + 32 * h < t.k1) half(std::true_type(), k0 + 32 * h, k, v);
+            }
         }
         lds_barrier();                                       // all wavefronts are done with the block
         load(k0 + 2 * KEYS, stage);

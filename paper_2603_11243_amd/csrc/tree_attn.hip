@@ -34,6 +34,17 @@ template <bool BF> __device__ __forceinline__ uint32_t infinite_of(uint32_t w, u
 }
 template <bool BF> __device__ __forceinline__ uint32_t finite_of(uint32_t w) { return w & ~(((beyond_of<BF>(w) & SIGNS) >> 15) * 0xffffu); }
 
+// Two values to the operand type, round to nearest even, by the conversion instruction of a pair.
+typedef float f32x2_t __attribute__((ext_vector_type(2)));
+typedef _Float16 f16x2_t __attribute__((ext_vector_type(2)));
+typedef __bf16 bf16x2_t __attribute__((ext_vector_type(2)));
+typedef uint32_t u32x2_t __attribute__((ext_vector_type(2)));
+template <bool BF> __device__ __forceinline__ uint32_t pack16(float lo, float hi) {
+    const f32x2_t v = {lo, hi};
+    if constexpr (BF) return __builtin_bit_cast(uint32_t, __builtin_convertvector(v, bf16x2_t));
+    else return __builtin_bit_cast(uint32_t, __builtin_convertvector(v, f16x2_t));
+}
+
 // Spans of a lane's keys k0 + 16 c + 4 (lane / 16) + r: every node's place lies in that of a cached row, nobody's in that of a key behind the range.
 template <int C>
 __device__ __forceinline__ void key_spans(uint32_t (&key)[C][4], const Work& t, int k0, const uint32_t* span_s) {
@@ -84,8 +95,8 @@ __device__ __forceinline__ void weights_of(f32x4_t (&s)[NT][2], float (&m)[NT], 
                 x[r] = MASKED && x[r] == -INFINITY ? 0.f : p;
                 l[n] += x[r];
             }
-            pw[2 * c] = op_pack2<BF>(x[0], x[1]);
-            pw[2 * c + 1] = op_pack2<BF>(x[2], x[3]);
+            pw[2 * c] = pack16<BF>(x[0], x[1]);
+            pw[2 * c + 1] = pack16<BF>(x[2], x[3]);
         }
         pf[n] = as_f16x8(make_uint4(pw[0], pw[1], pw[2], pw[3]));
     }
@@ -97,32 +108,67 @@ template <int HD> __device__ __forceinline__ int v_swizzle(int row) { return HD 
 // The same for key and query rows, of which an operand read takes the same chunk of 16.
 template <int HD> __device__ __forceinline__ int k_swizzle(int row) { return HD == 128 ? row & 15 : row >> 1 & 7; }
 
-// O^T += V^T P^T over the 32 value rows at v, DG 16-dim tiles at a time.  Transposing read: lane i of 16 passes row i / 4 and dims 4 (i % 4) .. + 3 of a
+// The operands of 32 key rows at k: rows 16 c + lane % 16, dims 8 (lane / 16) + 32 e.  Written out because the compiler waits for all loads into LDS
+// before a plain read of it, those of the next block among them, which go elsewhere.
+template <int HD>
+__device__ __forceinline__ void read_keys(const unsigned char* k, f16x8_t (&kf)[2][HD / 32]) {
+    const int kg = threadIdx.x % 64 / 16, dc = threadIdx.x % 16;
+    const uint32_t base = (uint32_t)(uintptr_t)(lds_void_t*)k + dc * HD * 2;
+    const uint32_t a0 = base + (kg ^ k_swizzle<HD>(dc)) * 16, a1 = base + ((kg + 4) ^ k_swizzle<HD>(dc)) * 16;
+    u32x4_t x[2][HD / 32];
+    if constexpr (HD == 128) {
+        const uint32_t a2 = base + ((kg + 8) ^ k_swizzle<HD>(dc)) * 16, a3 = base + ((kg + 12) ^ k_swizzle<HD>(dc)) * 16;
+        asm volatile("ds_read_b128 %0, %8\n\tds_read_b128 %1, %9\n\tds_read_b128 %2, %10\n\tds_read_b128 %3, %11\n\t"
+                     "ds_read_b128 %4, %8 offset:4096\n\tds_read_b128 %5, %9 offset:4096\n\tds_read_b128 %6, %10 offset:4096\n\tds_read_b128 %7, %11 offset:4096\n\t"
+                     "s_waitcnt lgkmcnt(0)"
+                     : "=&v"(x[0][0]), "=&v"(x[0][1]), "=&v"(x[0][2]), "=&v"(x[0][3]), "=&v"(x[1][0]), "=&v"(x[1][1]), "=&v"(x[1][2]), "=&v"(x[1][3])
+                     : "v"(a0), "v"(a1), "v"(a2), "v"(a3) : "memory");
+    } else {
+        asm volatile("ds_read_b128 %0, %4\n\tds_read_b128 %1, %5\n\tds_read_b128 %2, %4 offset:2048\n\tds_read_b128 %3, %5 offset:2048\n\t"
+                     "s_waitcnt lgkmcnt(0)"
+                     : "=&v"(x[0][0]), "=&v"(x[0][1]), "=&v"(x[1][0]), "=&v"(x[1][1]) : "v"(a0), "v"(a1) : "memory");
+    }
+#pragma unroll
+    for (int c = 0; c < 2; ++c)
+#pragma unroll
+        for (int e = 0; e < HD / 32; ++e) kf[c][e] = __builtin_bit_cast(f16x8_t, x[c][e]);
+}
+
+// O^T += V^T P^T over the 32 value rows at v, four 16-dim tiles at a time (read as in read_keys, for the same reason).  Transposing read: lane i of 16 passes row i / 4 and dims 4 (i % 4) .. + 3 of a
 // 16-dim tile, lane j receives dim j of four rows.
-template <bool BF, int HD, int NT, int DG, bool MASKED>
+template <bool BF, int HD, int NT, bool MASKED>
 __device__ __forceinline__ void add_values(const unsigned char* v, const f16x8_t (&pf)[NT], f32x4_t (&o)[NT][HD / 16]) {
     constexpr int ROW = HD * 2;
     const int lane = threadIdx.x % 64, kg = lane / 16, dc = lane % 16;
-    const int v_row = 4 * kg + dc / 4, v_low = (dc % 4) / 2, v_sub = (dc % 2) * 8;
+    const int v_row = 4 * kg + dc / 4, v_low = (dc % 4) / 2;
+    const uint32_t base = (uint32_t)(uintptr_t)(lds_void_t*)v + v_row * ROW + (dc % 2) * 8;
 #pragma unroll
-    for (int g = 0; g < HD / 16; g += DG) {
-        tr_v4i16 vf[DG][2];
+    for (int g = 0; g < HD / 16; g += 4) {
+        u32x2_t vf[4][2];
+        uint32_t at[4];
 #pragma unroll
-        for (int i = 0; i < DG; ++i) {
-            const unsigned char* p = v + v_row * ROW + (((2 * (g + i)) | v_low) ^ v_swizzle<HD>(v_row)) * 16 + v_sub;
-            vf[i][0] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_tr_v4i16*)p);
-            vf[i][1] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_tr_v4i16*)(p + 16 * ROW));
-        }
-        __builtin_amdgcn_sched_barrier(0);
+        for (int i = 0; i < 4; ++i) at[i] = base + (((2 * (g + i)) | v_low) ^ v_swizzle<HD>(v_row)) * 16;
+        if constexpr (HD == 128)
+            asm volatile("ds_read_b64_tr_b16 %0, %8\n\tds_read_b64_tr_b16 %1, %8 offset:4096\n\tds_read_b64_tr_b16 %2, %9\n\tds_read_b64_tr_b16 %3, %9 offset:4096\n\t"
+                         "ds_read_b64_tr_b16 %4, %10\n\tds_read_b64_tr_b16 %5, %10 offset:4096\n\tds_read_b64_tr_b16 %6, %11\n\tds_read_b64_tr_b16 %7, %11 offset:4096\n\t"
+                         "s_waitcnt lgkmcnt(0)"
+                         : "=&v"(vf[0][0]), "=&v"(vf[0][1]), "=&v"(vf[1][0]), "=&v"(vf[1][1]), "=&v"(vf[2][0]), "=&v"(vf[2][1]), "=&v"(vf[3][0]), "=&v"(vf[3][1])
+                         : "v"(at[0]), "v"(at[1]), "v"(at[2]), "v"(at[3]) : "memory");
+        else
+            asm volatile("ds_read_b64_tr_b16 %0, %8\n\tds_read_b64_tr_b16 %1, %8 offset:2048\n\tds_read_b64_tr_b16 %2, %9\n\tds_read_b64_tr_b16 %3, %9 offset:2048\n\t"
+                         "ds_read_b64_tr_b16 %4, %10\n\tds_read_b64_tr_b16 %5, %10 offset:2048\n\tds_read_b64_tr_b16 %6, %11\n\tds_read_b64_tr_b16 %7, %11 offset:2048\n\t"
+                         "s_waitcnt lgkmcnt(0)"
+                         : "=&v"(vf[0][0]), "=&v"(vf[0][1]), "=&v"(vf[1][0]), "=&v"(vf[1][1]), "=&v"(vf[2][0]), "=&v"(vf[2][1]), "=&v"(vf[3][0]), "=&v"(vf[3][1])
+                         : "v"(at[0]), "v"(at[1]), "v"(at[2]), "v"(at[3]) : "memory");
         // A value that is not finite would reach the rows that do not see it as 0 times infinity.  In a block that holds one the products run
         // on the others, and two more count the infinities of either sign (a NaN as both) that rows with a probability meet.
         uint32_t odd = 0;
         if constexpr (MASKED) {
 #pragma unroll
-            for (int i = 0; i < DG; ++i)
+            for (int i = 0; i < 4; ++i)
 #pragma unroll
                 for (int e = 0; e < 2; ++e) {
-                    const uint2 x = __builtin_bit_cast(uint2, vf[i][e]);
+                    const u32x2_t x = vf[i][e];
                     odd |= beyond_of<BF>(x.x) | beyond_of<BF>(x.y);
                 }
         }
@@ -134,9 +180,9 @@ __device__ __forceinline__ void add_values(const unsigned char* v, const f16x8_t
                 there[n] = as_f16x8(make_uint4(one_where<BF>(not_zero(x.x)), one_where<BF>(not_zero(x.y)), one_where<BF>(not_zero(x.z)), one_where<BF>(not_zero(x.w))));
             }
 #pragma unroll
-            for (int i = 0; i < DG; ++i) {
+            for (int i = 0; i < 4; ++i) {
                 __builtin_amdgcn_sched_barrier(0);           // (one after the other: registers, not speed)
-                const uint2 x = __builtin_bit_cast(uint2, vf[i][0]), y = __builtin_bit_cast(uint2, vf[i][1]);
+                const u32x2_t x = vf[i][0], y = vf[i][1];
                 const f16x8_t up = as_f16x8(make_uint4(infinite_of<BF>(x.x, 0), infinite_of<BF>(x.y, 0), infinite_of<BF>(y.x, 0), infinite_of<BF>(y.y, 0)));
                 const f16x8_t down = as_f16x8(make_uint4(infinite_of<BF>(x.x, ~0u), infinite_of<BF>(x.y, ~0u), infinite_of<BF>(y.x, ~0u), infinite_of<BF>(y.y, ~0u)));
 #pragma unroll
@@ -145,13 +191,13 @@ __device__ __forceinline__ void add_values(const unsigned char* v, const f16x8_t
 #pragma unroll
                     for (int r = 0; r < 4; ++r) o[n][g + i][r] += (u[r] > 0.f ? INFINITY : 0.f) - (d[r] > 0.f ? INFINITY : 0.f);
                 }
-                vf[i][0] = __builtin_bit_cast(tr_v4i16, make_uint2(finite_of<BF>(x.x), finite_of<BF>(x.y)));
-                vf[i][1] = __builtin_bit_cast(tr_v4i16, make_uint2(finite_of<BF>(y.x), finite_of<BF>(y.y)));
+                vf[i][0] = (u32x2_t){finite_of<BF>(x.x), finite_of<BF>(x.y)};
+                vf[i][1] = (u32x2_t){finite_of<BF>(y.x), finite_of<BF>(y.y)};
             }
         }
 #pragma unroll
-        for (int i = 0; i < DG; ++i) {
-            const f16x8_t x = __builtin_bit_cast(f16x8_t, __builtin_shufflevector(vf[i][0], vf[i][1], 0, 1, 2, 3, 4, 5, 6, 7));
+        for (int i = 0; i < 4; ++i) {
+            const f16x8_t x = __builtin_bit_cast(f16x8_t, __builtin_shufflevector(vf[i][0], vf[i][1], 0, 1, 2, 3));
 #pragma unroll
             for (int n = 0; n < NT; ++n) o[n][g + i] = mfma_16x16x32<BF>(x, pf[n], o[n][g + i]);
         }
@@ -235,9 +281,9 @@ __global__ void __launch_bounds__(64 * KEY_WAVES, 2) tree_keys16_kernel(TreeAttn
     };
     int k0 = t.k0 + wave * KEYS;
     load_keys(k0);
-    load_values(k0);
     f16x8_t qf[NT][KS];
     load_queries<HD, NT>(qf, a, t, kvh, t.row0);
+    load_values(k0);
     const float sc = fabsf(a.scale) * LOG2E;
     float m[NT], l[NT];
     f32x4_t o[NT][DT];
@@ -251,7 +297,7 @@ __global__ void __launch_bounds__(64 * KEY_WAVES, 2) tree_keys16_kernel(TreeAttn
     if ((int)threadIdx.x < n_spans) span_s[threadIdx.x] = span;
     for (int i = threadIdx.x + 64 * KEY_WAVES; i < n_spans; i += 64 * KEY_WAVES) span_s[i] = w(a.spans + t.node0 + i);
     lds_barrier();
-    auto block = [&](auto masked_c, int k0) {
+    auto block = [&](auto masked_c, int k0) __attribute__((always_inline)) {
         constexpr bool MASKED = decltype(masked_c)::value;
         f32x4_t s[NT][2];
 #pragma unroll
@@ -282,7 +328,7 @@ __global__ void __launch_bounds__(64 * KEY_WAVES, 2) tree_keys16_kernel(TreeAttn
         __builtin_amdgcn_sched_barrier(0);
         __builtin_amdgcn_s_waitcnt(0x0F70 | K_LOADS);        // the values of this block have landed (a wavefront reads its own only)
         __builtin_amdgcn_sched_barrier(0);
-        add_values<BF, HD, NT, (NT > 1 ? 4 : DT), MASKED>(v_s[wave], p, o);
+        add_values<BF, HD, NT, MASKED>(v_s[wave], p, o);
         __builtin_amdgcn_s_waitcnt(0xC07F);                  // the reads of this block are done
         __builtin_amdgcn_sched_barrier(0);
         load_values(k0 + STEP);
@@ -319,7 +365,7 @@ __global__ void __launch_bounds__(64 * ROW_WAVES, 2) tree_rows16_kernel(TreeAttn
     const uint16_t* kbase = (const uint16_t*)a.k + first;
     const uint16_t* vbase = (const uint16_t*)a.v + first;
     // Instruction i of a wavefront fills L_ROWS rows of the block.  Rows behind the range are copies of its last one.
-    auto load = [&](int k0, int stage) {
+    auto load = [&](int k0, int stage) __attribute__((always_inline)) {
         const int r0 = min(k0, last), beyond = last - r0;
         const __amdgpu_buffer_rsrc_t k_rsrc = make_rsrc(kbase + (int64_t)r0 * a.slot_stride), v_rsrc = make_rsrc(vbase + (int64_t)r0 * a.slot_stride);
 #pragma unroll
@@ -347,24 +393,19 @@ __global__ void __launch_bounds__(64 * ROW_WAVES, 2) tree_rows16_kernel(TreeAttn
         for (int i = 0; i < DT; ++i) o[n][i] = (f32x4_t){0.f, 0.f, 0.f, 0.f};
     }
     const bool live = row0 < R;
-    auto half = [&](auto masked_c, int k0, const unsigned char* k, const unsigned char* v) {      // 32 keys
+    auto half = [&](auto masked_c, int k0, const unsigned char* k, const unsigned char* v) __attribute__((always_inline)) {      // 32 keys
         constexpr bool MASKED = decltype(masked_c)::value;
         f32x4_t s[NT][2];
+        f16x8_t kf[2][KS];
+        read_keys<HD>(k, kf);
 #pragma unroll
-        for (int c = 0; c < 2; ++c) {
-            f16x8_t kf[KS];
-#pragma unroll
-            for (int e = 0; e < KS; ++e) {
-                const int r = 16 * c + dc;
-                kf[e] = as_f16x8(*reinterpret_cast<const uint4*>(k + r * ROW + ((kg + 4 * e) ^ k_swizzle<HD>(r)) * 16));
-            }
+        for (int c = 0; c < 2; ++c)
 #pragma unroll
             for (int n = 0; n < NT; ++n) {
                 s[n][c] = (f32x4_t){0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-                for (int e = 0; e < KS; ++e) s[n][c] = mfma_16x16x32<BF>(kf[e], qf[n][e], s[n][c]);
+                for (int e = 0; e < KS; ++e) s[n][c] = mfma_16x16x32<BF>(kf[c][e], qf[n][e], s[n][c]);
             }
-        }
         if constexpr (MASKED) {
             uint32_t key[2][4];
             key_spans<2>(key, t, k0, span_s);
@@ -379,24 +420,23 @@ __global__ void __launch_bounds__(64 * ROW_WAVES, 2) tree_rows16_kernel(TreeAttn
         }
         f16x8_t p[NT];
         weights_of<BF, NT, DT, MASKED>(s, m, l, o, sc, p);
-        add_values<BF, HD, NT, 4, MASKED>(v, p, o);
+        add_values<BF, HD, NT, MASKED>(v, p, o);
     };
-    int stage = 0;
-    for (int k0 = t.k0; k0 < t.k1; k0 += KEYS, stage ^= 1) {
+    auto block = [&](auto masked_c, int k0, int stage) __attribute__((always_inline)) {
+        constexpr bool MASKED = decltype(masked_c)::value;
         __builtin_amdgcn_sched_barrier(0);
         __builtin_amdgcn_s_waitcnt(0x0F70 | 2 * LOADS);      // this block; the next one may be in flight
         lds_barrier();
         if (live) {
-#pragma unroll 1
-            for (int h = 0; h < 2; ++h) {
-                const unsigned char *k = kv_s[stage][0] + h * 32 * ROW, *v = kv_s[stage][1] + h * 32 * ROW;
-                if (k0 + 32 * h + 32 <= min(t.n_ctx, t.k1)) half(std::false_type(), k0 + 32 * h, k, v);
-                else if (k0 + 32 * h < t.k1) half(std::true_type(), k0 + 32 * h, k, v);
-            }
+            half(masked_c, k0, kv_s[stage][0], kv_s[stage][1]);
+            if (!MASKED || k0 + 32 < t.k1) half(masked_c, k0 + 32, kv_s[stage][0] + 32 * ROW, kv_s[stage][1] + 32 * ROW);
         }
         lds_barrier();                                       // all wavefronts are done with the block
         load(k0 + 2 * KEYS, stage);
-    }
+    };
+    int stage = 0, k0 = t.k0;
+    for (; k0 + KEYS <= min(t.n_ctx, t.k1); k0 += KEYS, stage ^= 1) block(std::false_type(), k0, stage);
+    for (; k0 < t.k1; k0 += KEYS, stage ^= 1) block(std::true_type(), k0, stage);
     __builtin_amdgcn_sched_barrier(0);
     __builtin_amdgcn_s_waitcnt(0x0F70);                      // nothing lands in LDS after the end
     __builtin_amdgcn_sched_barrier(0);

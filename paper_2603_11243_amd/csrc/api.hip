@@ -1502,6 +1502,7 @@ void tree_work(int B, const int32_t* kv_start, const int32_t* ctx_len, const int
     for (int b = 0; b < B; ++b) tree_spans(cu_nodes[b + 1] - cu_nodes[b], parent + cu_nodes[b], v.data() + a.spans + cu_nodes[b]);
     a.n_q_heads = n_q_heads; a.n_kv_heads = n_kv_heads; a.head_dim = kv.head_dim; a.dtype = kv.dtype;
     a.slot_stride = kv.slot_stride; a.head_stride = n_kv_heads > 1 ? kv.head_stride : 0;
+    a.group = G; a.group_magic = G > 1 ? (uint32_t)(((uint64_t)1 << 32) / G + 1) : 0;
     a.tile_rows = rows; a.step = (int)step; a.mass_step = (int)mass_step;
 }
 struct TreePlan { size_t words, lse, part_o, part_ml, total; };
@@ -1671,6 +1672,7 @@ int tree_attention(ssd_ctx* ctx, const void* q, int64_t q_stride, int n_q_heads,
         return fail(ctx, SSD_EINVAL, "tree_attention: rows of q and out must begin at multiples of 16 bytes, q_stride be at least n_q_heads * head_dim");
     TreeWork w;
     tree_work(B, kv_start, ctx_len, cu_nodes, parent, most, n_q_heads, *kv, mass != nullptr, w);
+    if (w.a.n_items > 65535 || w.a.n_mass > 65535) return fail(ctx, SSD_ESHAPE, "tree_attention: more than 65535 tiles of query rows; split the batch");
     const TreePlan p = plan_tree(w, N, mass && !lse);
     if (!ctx->ws || ctx->ws_bytes < p.total)
         return fail(ctx, SSD_EWORKSPACE, "tree_attention: workspace of %zu bytes needed, %zu set", p.total, ctx->ws_bytes);
@@ -1812,6 +1814,7 @@ int verify_tree(ssd_ctx* ctx, const int32_t* node_ids, int B, const int32_t* cu_
     }
     TreeWork w;
     tree_work(B, kv_start, ctx_len, cu_nodes, parent, most, m.n_q_heads, view, kv_mass != nullptr, w);
+    if (w.a.n_items > 65535 || w.a.n_mass > 65535) return fail(ctx, SSD_ESHAPE, "verify_tree: more than 65535 tiles of query rows; split the batch");
     const TreePlan t = plan_tree(w, N, kv_mass != nullptr);
     const VerifyTreePlan p = plan_verify_tree(m, N, t);
     if (!ctx->ws || ctx->ws_bytes < p.total)

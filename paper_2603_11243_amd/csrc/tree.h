@@ -36,6 +36,7 @@ struct TreeAttnArgs {
     float* mass; int64_t mass_stride;        // [n_kv_heads, mass_stride]; NULL: not wanted
     float* part_o; float2* part_ml;          // [item][K/V head][tile_rows] outputs and (maximum, sum) of pieces
     int n_q_heads, n_kv_heads, head_dim, dtype;
+    int group; uint32_t group_magic;         // n_q_heads / n_kv_heads; 2^32 / group rounded up, 0 for 1
     float scale;
     int tile_rows, step, mass_step, n_items, n_parts, n_joins, n_mass;
     int utts, cu, joins, mass_items, spans;

@@ -30,8 +30,20 @@ __device__ __forceinline__ bool sees(uint32_t node, uint32_t key) {
 constexpr float LOG2E = 1.4426950408889634f, LN2 = 0.6931471805599453f;
 constexpr float F32_MOST = 3.4028234663852886e38f;
 
+// Node of a query row (rows are fewer than 2^19, groups at most 512: the product is exact).
+__device__ __forceinline__ int node_of(const TreeAttnArgs& a, int row) { return a.group_magic ? (int)__umulhi((uint32_t)row, a.group_magic) : row; }
+
 // An item of work: what its words say.
 struct Work { int slot0, n_ctx, n_nodes, node0, row0, k0, k1, index; };
+// Query row's number among those of all heads, [node][query head].
+__device__ __forceinline__ int64_t row_at(const TreeAttnArgs& a, const Work& t, int kvh, int row) {
+    const int node = node_of(a, row);
+    return (int64_t)(t.node0 + node) * a.n_q_heads + kvh * a.group + row - node * a.group;
+}
+__device__ __forceinline__ int64_t query_at(const TreeAttnArgs& a, const Work& t, int kvh, int row, int head_dim) {
+    const int node = node_of(a, row);
+    return (int64_t)(t.node0 + node) * a.q_stride + (int64_t)(kvh * a.group + row - node * a.group) * head_dim;
+}
 template <class M>
 __device__ __forceinline__ void utterance_of(const TreeAttnArgs& a, const M& w, int b, Work& t) {
     t.slot0 = (int)w(a.utts + 2 * b);
@@ -50,7 +62,7 @@ __device__ __forceinline__ Work item_of(const TreeAttnArgs& a, const M& w, int i
     t.n_nodes = (int)(x & 0x7ffu);
     t.row0 = (int)(x >> 11) * tile_rows;
     const int64_t k0 = (int64_t)w(5 * index + 4) * a.step;
-    const int G = a.n_q_heads / a.n_kv_heads, node = (min(t.n_nodes * G, t.row0 + tile_rows) - 1) / G;       // no row of the tile sees a later one
+    const int node = node_of(a, min(t.n_nodes * a.group, t.row0 + tile_rows) - 1);       // no row of the tile sees a later one
     t.k0 = (int)k0;
     t.k1 = (int)min((int64_t)t.n_ctx + node + 1, k0 + a.step);
     return t;
@@ -71,6 +83,20 @@ __device__ __forceinline__ Work mass_item_of(const TreeAttnArgs& a, const M& w, 
 constexpr int MASS_WAVES = 4;                // wavefronts of a workgroup of the weights
 constexpr int KEY_WAVES = 8;                 // wavefronts of a workgroup that split the keys
 
+// Spans of a lane's keys k0 + 16 c + 4 (lane / 16) + r: every node's place lies in that of a cached row, nobody's in that of a key behind the range.
+template <int C>
+__device__ __forceinline__ void key_spans(uint32_t (&key)[C][4], const Work& t, int k0, const uint32_t* span_s) {
+    const int kg = threadIdx.x % 64 / 16;
+#pragma unroll
+    for (int c = 0; c < C; ++c)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+            const int at = k0 + 16 * c + 4 * kg + r - t.n_ctx;
+            const uint32_t span = span_s[min(max(at, 0), t.n_nodes - 1)];
+            key[c][r] = at < 0 ? 0xffff0000u : at < t.k1 - t.n_ctx ? span : 0u;
+        }
+}
+
 // The end of an attention workgroup: its wavefronts hold, for 16 NT rows, maxima m (raw scores), sums l (a lane's share) and outputs o[n][i] (row
 // 16 n + lane % 16, dims 16 i + 4 (lane / 16) ..) relative to 2^(m sc - bias).  DPASS dims of all rows at a time go through LDS (buf: 16 HD floats a wavefront,
 // the 16-byte chunks of a row permuted by its number); every thread adds VPT values of a row and stores them, or the sums of a piece.
@@ -80,7 +106,7 @@ __device__ __forceinline__ void merge_wavefronts(const TreeAttnArgs& a, const Wo
     typedef Elem<DT> E;
     constexpr int TR = 16 * NT, DPASS = 16 * HD / TR, VPT = TR * DPASS / (64 * WAVES), TPR = 64 * WAVES / TR;      // values of a thread, threads of a row
     const int lane = threadIdx.x % 64, kg = lane / 16, dc = lane % 16, wave = threadIdx.x / 64;
-    const int G = a.n_q_heads / a.n_kv_heads, R = t.n_nodes * G;
+    const int G = a.group, R = t.n_nodes * G;
 #pragma unroll
     for (int n = 0; n < NT; ++n) {
         l[n] += __shfl_xor(l[n], 16);
@@ -128,7 +154,7 @@ __device__ __forceinline__ void merge_wavefronts(const TreeAttnArgs& a, const Wo
             for (int e = 0; e < VPT; ++e) dst[e] = v[e];
         } else {
             const float inv = 1.f / lt;
-            typename E::type* dst = (typename E::type*)a.out + ((int64_t)(t.node0 + row / G) * a.n_q_heads + kvh * G + row % G) * a.head_dim + dim;
+            typename E::type* dst = (typename E::type*)a.out + (row_at(a, t, kvh, row)) * a.head_dim + dim;
             if constexpr (DT == SSD_F32) {
 #pragma unroll
                 for (int e = 0; e < VPT; ++e)
@@ -144,7 +170,7 @@ __device__ __forceinline__ void merge_wavefronts(const TreeAttnArgs& a, const Wo
     }
     if (ocol == 0 && row < R) {
         if (t.index < a.n_parts) a.part_ml[(int64_t)(t.index * a.n_kv_heads + kvh) * TR + orow] = make_float2(mt, lt);
-        else if (a.lse) a.lse[(int64_t)(t.node0 + row / G) * a.n_q_heads + kvh * G + row % G] = (mt * sc - bias + __builtin_amdgcn_logf(lt)) * LN2;
+        else if (a.lse) a.lse[row_at(a, t, kvh, row)] = (mt * sc - bias + __builtin_amdgcn_logf(lt)) * LN2;
     }
 }
 
@@ -156,7 +182,7 @@ __global__ void __launch_bounds__(256) tree_join_kernel(TreeAttnArgs a, M w, flo
     constexpr int LANES = HD / 4, GROUPS = 256 / LANES;
     __shared__ f32x4_t o_s[GROUPS][LANES];
     __shared__ float2 ml_s[GROUPS];
-    const int j = blockIdx.x / a.tile_rows, r = blockIdx.x % a.tile_rows, kvh = blockIdx.y, G = a.n_q_heads / a.n_kv_heads;
+    const int j = blockIdx.x / a.tile_rows, r = blockIdx.x % a.tile_rows, kvh = blockIdx.y, G = a.group;
     const uint32_t x = w(a.joins + 3 * j);
     const int item0 = (int)w(a.joins + 3 * j + 1), n_parts = (int)w(a.joins + 3 * j + 2);
     Work t;
@@ -202,7 +228,7 @@ __global__ void __launch_bounds__(256) tree_join_kernel(TreeAttnArgs a, M w, flo
         lt += y.y * f;
         s += o_s[g][dim / 4] * f;
     }
-    const int64_t at = (int64_t)(t.node0 + row / G) * a.n_q_heads + kvh * G + row % G;
+    const int64_t at = row_at(a, t, kvh, row);
     typename E::type* dst = (typename E::type*)a.out + at * a.head_dim + dim;
     const float inv = 1.f / lt;
     if (dim < a.head_dim)

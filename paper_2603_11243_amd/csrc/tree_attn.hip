@@ -45,19 +45,6 @@ template <bool BF> __device__ __forceinline__ uint32_t pack16(float lo, float hi
     else return __builtin_bit_cast(uint32_t, __builtin_convertvector(v, f16x2_t));
 }
 
-// Spans of a lane's keys k0 + 16 c + 4 (lane / 16) + r: every node's place lies in that of a cached row, nobody's in that of a key behind the range.
-template <int C>
-__device__ __forceinline__ void key_spans(uint32_t (&key)[C][4], const Work& t, int k0, const uint32_t* span_s) {
-    const int kg = threadIdx.x % 64 / 16;
-#pragma unroll
-    for (int c = 0; c < C; ++c)
-#pragma unroll
-        for (int r = 0; r < 4; ++r) {
-            const int at = k0 + 16 * c + 4 * kg + r;
-            key[c][r] = at < t.n_ctx ? 0xffff0000u : at < t.k1 ? span_s[at - t.n_ctx] : 0u;
-        }
-}
-
 // Scores of 32 keys to weights in the operand type; maxima, sums and outputs follow.
 template <bool BF, int NT, int DT, bool MASKED>
 __device__ __forceinline__ void weights_of(f32x4_t (&s)[NT][2], float (&m)[NT], float (&l)[NT], f32x4_t (&o)[NT][DT], float sc, f16x8_t (&pf)[NT]) {
@@ -134,10 +121,35 @@ __device__ __forceinline__ void read_keys(const unsigned char* k, f16x8_t (&kf)[
         for (int e = 0; e < HD / 32; ++e) kf[c][e] = __builtin_bit_cast(f16x8_t, x[c][e]);
 }
 
+template <int NT, int DT>
+__device__ __forceinline__ void start(float (&m)[NT], float (&l)[NT], f32x4_t (&o)[NT][DT]) {
+#pragma unroll
+    for (int n = 0; n < NT; ++n) {
+        m[n] = -F32_MOST;
+        l[n] = 0.f;
+#pragma unroll
+        for (int i = 0; i < DT; ++i) o[n][i] = (f32x4_t){0.f, 0.f, 0.f, 0.f};
+    }
+}
+
+// Whether a wavefront's output holds a NaN.
+template <int NT, int DT>
+__device__ __forceinline__ bool any_nan(const f32x4_t (&o)[NT][DT]) {
+    bool bad = false;
+#pragma unroll
+    for (int n = 0; n < NT; ++n)
+#pragma unroll
+        for (int i = 0; i < DT; ++i) {
+            const float sum = (o[n][i][0] + o[n][i][1]) + (o[n][i][2] + o[n][i][3]);      // (of infinities of both signs: one more pass for nothing)
+            bad |= sum != sum;
+        }
+    return __any(bad);
+}
+
 // O^T += V^T P^T over the 32 value rows at v, four 16-dim tiles at a time (read as in read_keys, for the same reason).  Transposing read: lane i of 16 passes row i / 4 and dims 4 (i % 4) .. + 3 of a
 // 16-dim tile, lane j receives dim j of four rows.
 template <bool BF, int HD, int NT, bool MASKED>
-__device__ __forceinline__ void add_values(const unsigned char* v, const f16x8_t (&pf)[NT], f32x4_t (&o)[NT][HD / 16]) {
+__device__ __forceinline__ void add_values(const unsigned char* v, const f16x8_t (&pf)[NT], f32x4_t (&o)[NT][HD / 16], bool careful) {
     constexpr int ROW = HD * 2;
     const int lane = threadIdx.x % 64, kg = lane / 16, dc = lane % 16;
     const int v_row = 4 * kg + dc / 4, v_low = (dc % 4) / 2;
@@ -160,19 +172,17 @@ __device__ __forceinline__ void add_values(const unsigned char* v, const f16x8_t
                          "s_waitcnt lgkmcnt(0)"
                          : "=&v"(vf[0][0]), "=&v"(vf[0][1]), "=&v"(vf[1][0]), "=&v"(vf[1][1]), "=&v"(vf[2][0]), "=&v"(vf[2][1]), "=&v"(vf[3][0]), "=&v"(vf[3][1])
                          : "v"(at[0]), "v"(at[1]), "v"(at[2]), "v"(at[3]) : "memory");
-        // A value that is not finite would reach the rows that do not see it as 0 times infinity.  In a block that holds one the products run
-        // on the others, and two more count the infinities of either sign (a NaN as both) that rows with a probability meet.
+        // A value that is not finite reaches the rows that do not see it as 0 times infinity, a NaN that stays.  A pass that ends with one is repeated with care:
+        // where a block holds such values the products run on the others, and two more count the infinities of either sign (a NaN as both) that rows
+        // with a probability meet.
         uint32_t odd = 0;
-        if constexpr (MASKED) {
+        if (MASKED && careful) {
 #pragma unroll
             for (int i = 0; i < 4; ++i)
 #pragma unroll
-                for (int e = 0; e < 2; ++e) {
-                    const u32x2_t x = vf[i][e];
-                    odd |= beyond_of<BF>(x.x) | beyond_of<BF>(x.y);
-                }
+                for (int e = 0; e < 2; ++e) odd |= beyond_of<BF>(vf[i][e].x) | beyond_of<BF>(vf[i][e].y);
         }
-        if (MASKED && __any(odd & SIGNS)) {
+        if (MASKED && careful && __any(odd & SIGNS)) {
             f16x8_t there[NT];
 #pragma unroll
             for (int n = 0; n < NT; ++n) {
@@ -207,12 +217,12 @@ __device__ __forceinline__ void add_values(const unsigned char* v, const f16x8_t
 // Queries as operands: column lane % 16 of tile n is query row row0 + 16 n + lane % 16 (a copy of the last one behind it); a negative scale is theirs.
 template <int HD, int NT>
 __device__ __forceinline__ void load_queries(f16x8_t (&qf)[NT][HD / 32], const TreeAttnArgs& a, const Work& t, int kvh, int row0) {
-    const int lane = threadIdx.x % 64, G = a.n_q_heads / a.n_kv_heads;
+    const int lane = threadIdx.x % 64;
     const uint32_t flip = a.scale < 0.f ? 0x80008000u : 0u;
 #pragma unroll
     for (int n = 0; n < NT; ++n) {
-        const int row = min(row0 + 16 * n + lane % 16, t.n_nodes * G - 1);
-        const uint16_t* q = (const uint16_t*)a.q + (int64_t)(t.node0 + row / G) * a.q_stride + (kvh * G + row % G) * HD + lane / 16 * 8;
+        const int row = min(row0 + 16 * n + lane % 16, t.n_nodes * a.group - 1);
+        const uint16_t* q = (const uint16_t*)a.q + query_at(a, t, kvh, row, HD) + lane / 16 * 8;
 #pragma unroll
         for (int s = 0; s < HD / 32; ++s) {
             uint4 x = *reinterpret_cast<const uint4*>(q + 32 * s);
@@ -244,10 +254,9 @@ __global__ void __launch_bounds__(64 * KEY_WAVES, 2) tree_keys16_kernel(TreeAttn
     __shared__ uint32_t span_s[MAX_TREE_NODES];
     const int lane = threadIdx.x % 64, kg = lane / 16, dc = lane % 16;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
-    const int work = xcd_contiguous_index(blockIdx.x, gridDim.x);
-    const Work t = item_of(a, w, work / a.n_kv_heads, TR);
-    const int kvh = work % a.n_kv_heads;
-    const int G = a.n_q_heads / a.n_kv_heads, R = t.n_nodes * G;
+    const Work t = item_of(a, w, blockIdx.y, TR);
+    const int kvh = blockIdx.x;
+    const int R = t.n_nodes * a.group;
     const int last = max(t.k0, t.k1 - 1);                    // (a range without keys: any row)
     const int n_spans = t.k1 > t.n_ctx ? t.n_nodes : 0;
     const uint32_t span = (int)threadIdx.x < n_spans ? w(a.spans + t.node0 + (int)threadIdx.x) : 0u;
@@ -279,24 +288,21 @@ __global__ void __launch_bounds__(64 * KEY_WAVES, 2) tree_keys16_kernel(TreeAttn
             __builtin_amdgcn_raw_ptr_buffer_load_lds(rsrc, (lds_void_t*)(v_s[wave] + i * 1024), 16, off, 0, 0, 0);
         }
     };
-    int k0 = t.k0 + wave * KEYS;
-    load_keys(k0);
+    const int k_first = t.k0 + wave * KEYS;
+    load_keys(k_first);
     f16x8_t qf[NT][KS];
     load_queries<HD, NT>(qf, a, t, kvh, t.row0);
-    load_values(k0);
+    load_values(k_first);
     const float sc = fabsf(a.scale) * LOG2E;
     float m[NT], l[NT];
     f32x4_t o[NT][DT];
-#pragma unroll
-    for (int n = 0; n < NT; ++n) {
-        m[n] = -F32_MOST;
-        l[n] = 0.f;
-#pragma unroll
-        for (int i = 0; i < DT; ++i) o[n][i] = (f32x4_t){0.f, 0.f, 0.f, 0.f};
-    }
     if ((int)threadIdx.x < n_spans) span_s[threadIdx.x] = span;
     for (int i = threadIdx.x + 64 * KEY_WAVES; i < n_spans; i += 64 * KEY_WAVES) span_s[i] = w(a.spans + t.node0 + i);
     lds_barrier();
+    uint32_t mine[NT];
+#pragma unroll
+    for (int n = 0; n < NT; ++n) mine[n] = span_s[node_of(a, min(t.row0 + 16 * n + dc, R - 1))];           // (not read without node keys)
+    bool careful = false;
     auto block = [&](auto masked_c, int k0) __attribute__((always_inline)) {
         constexpr bool MASKED = decltype(masked_c)::value;
         f32x4_t s[NT][2];
@@ -316,11 +322,10 @@ __global__ void __launch_bounds__(64 * KEY_WAVES, 2) tree_keys16_kernel(TreeAttn
             key_spans<2>(key, t, k0, span_s);
 #pragma unroll
             for (int n = 0; n < NT; ++n) {
-                const uint32_t mine = span_s[min(t.row0 + 16 * n + dc, R - 1) / G];
 #pragma unroll
                 for (int c = 0; c < 2; ++c)
 #pragma unroll
-                    for (int r = 0; r < 4; ++r) s[n][c][r] = sees(mine, key[c][r]) ? s[n][c][r] : -INFINITY;
+                    for (int r = 0; r < 4; ++r) s[n][c][r] = sees(mine[n], key[c][r]) ? s[n][c][r] : -INFINITY;
             }
         }
         f16x8_t p[NT];
@@ -328,16 +333,24 @@ __global__ void __launch_bounds__(64 * KEY_WAVES, 2) tree_keys16_kernel(TreeAttn
         __builtin_amdgcn_sched_barrier(0);
         __builtin_amdgcn_s_waitcnt(0x0F70 | K_LOADS);        // the values of this block have landed (a wavefront reads its own only)
         __builtin_amdgcn_sched_barrier(0);
-        add_values<BF, HD, NT, MASKED>(v_s[wave], p, o);
+        add_values<BF, HD, NT, MASKED>(v_s[wave], p, o, careful);
         __builtin_amdgcn_s_waitcnt(0xC07F);                  // the reads of this block are done
         __builtin_amdgcn_sched_barrier(0);
         load_values(k0 + STEP);
     };
-    for (; k0 + KEYS <= min(t.n_ctx, t.k1); k0 += STEP) block(std::false_type(), k0);
-    for (; k0 < t.k1; k0 += STEP) block(std::true_type(), k0);
-    __builtin_amdgcn_sched_barrier(0);
-    __builtin_amdgcn_s_waitcnt(0x0F70);                      // the values behind the last block: they land where the output goes
-    __builtin_amdgcn_sched_barrier(0);
+    for (;;) {
+        start<NT, DT>(m, l, o);
+        int k0 = k_first;
+        for (; k0 + KEYS <= min(t.n_ctx, t.k1); k0 += STEP) block(std::false_type(), k0);
+        for (; k0 < t.k1; k0 += STEP) block(std::true_type(), k0);
+        __builtin_amdgcn_sched_barrier(0);
+        __builtin_amdgcn_s_waitcnt(0x0F70);                  // the values behind the last block: they land where the output goes
+        __builtin_amdgcn_sched_barrier(0);
+        if (careful || t.k1 <= t.n_ctx || !any_nan<NT, DT>(o)) break;
+        careful = true;
+        load_keys(k_first);
+        load_values(k_first);
+    }
     merge_wavefronts<BF ? SSD_BF16 : SSD_F16, HD, NT, KEY_WAVES>(a, t, kvh, m, l, o, sc, BIAS<BF>, reinterpret_cast<float*>(v_s), ml_s);
 }
 
@@ -353,10 +366,9 @@ __global__ void __launch_bounds__(64 * ROW_WAVES, 2) tree_rows16_kernel(TreeAttn
     __shared__ uint32_t span_s[MAX_TREE_NODES];
     const int lane = threadIdx.x % 64, kg = lane / 16, dc = lane % 16;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
-    const int work = xcd_contiguous_index(blockIdx.x, gridDim.x);
-    const Work t = item_of(a, w, work / a.n_kv_heads, TR);
-    const int kvh = work % a.n_kv_heads;
-    const int G = a.n_q_heads / a.n_kv_heads, R = t.n_nodes * G;
+    const Work t = item_of(a, w, blockIdx.y, TR);
+    const int kvh = blockIdx.x;
+    const int R = t.n_nodes * a.group;
     const int last = max(t.k0, t.k1 - 1), row0 = t.row0 + wave * 16 * NT;
     const int n_spans = t.k1 > t.n_ctx ? t.n_nodes : 0;
     const uint32_t span = (int)threadIdx.x < n_spans ? w(a.spans + t.node0 + (int)threadIdx.x) : 0u;
@@ -382,16 +394,14 @@ __global__ void __launch_bounds__(64 * ROW_WAVES, 2) tree_rows16_kernel(TreeAttn
     load(t.k0 + KEYS, 1);
     if ((int)threadIdx.x < n_spans) span_s[threadIdx.x] = span;
     for (int i = threadIdx.x + 64 * ROW_WAVES; i < n_spans; i += 64 * ROW_WAVES) span_s[i] = w(a.spans + t.node0 + i);
+    lds_barrier();
+    uint32_t mine[NT];
+#pragma unroll
+    for (int n = 0; n < NT; ++n) mine[n] = span_s[node_of(a, min(row0 + 16 * n + dc, R - 1))];             // (not read without node keys)
     const float sc = fabsf(a.scale) * LOG2E;
     float m[NT], l[NT];
     f32x4_t o[NT][DT];
-#pragma unroll
-    for (int n = 0; n < NT; ++n) {
-        m[n] = -F32_MOST;
-        l[n] = 0.f;
-#pragma unroll
-        for (int i = 0; i < DT; ++i) o[n][i] = (f32x4_t){0.f, 0.f, 0.f, 0.f};
-    }
+    bool careful = false;
     const bool live = row0 < R;
     auto half = [&](auto masked_c, int k0, const unsigned char* k, const unsigned char* v) __attribute__((always_inline)) {      // 32 keys
         constexpr bool MASKED = decltype(masked_c)::value;
@@ -411,16 +421,15 @@ __global__ void __launch_bounds__(64 * ROW_WAVES, 2) tree_rows16_kernel(TreeAttn
             key_spans<2>(key, t, k0, span_s);
 #pragma unroll
             for (int n = 0; n < NT; ++n) {
-                const uint32_t mine = span_s[min(row0 + 16 * n + dc, R - 1) / G];
 #pragma unroll
                 for (int c = 0; c < 2; ++c)
 #pragma unroll
-                    for (int r = 0; r < 4; ++r) s[n][c][r] = sees(mine, key[c][r]) ? s[n][c][r] : -INFINITY;
+                    for (int r = 0; r < 4; ++r) s[n][c][r] = sees(mine[n], key[c][r]) ? s[n][c][r] : -INFINITY;
             }
         }
         f16x8_t p[NT];
         weights_of<BF, NT, DT, MASKED>(s, m, l, o, sc, p);
-        add_values<BF, HD, NT, MASKED>(v, p, o);
+        add_values<BF, HD, NT, MASKED>(v, p, o, careful);
     };
     auto block = [&](auto masked_c, int k0, int stage) __attribute__((always_inline)) {
         constexpr bool MASKED = decltype(masked_c)::value;
@@ -434,12 +443,20 @@ __global__ void __launch_bounds__(64 * ROW_WAVES, 2) tree_rows16_kernel(TreeAttn
         lds_barrier();                                       // all wavefronts are done with the block
         load(k0 + 2 * KEYS, stage);
     };
-    int stage = 0, k0 = t.k0;
-    for (; k0 + KEYS <= min(t.n_ctx, t.k1); k0 += KEYS, stage ^= 1) block(std::false_type(), k0, stage);
-    for (; k0 < t.k1; k0 += KEYS, stage ^= 1) block(std::true_type(), k0, stage);
-    __builtin_amdgcn_sched_barrier(0);
-    __builtin_amdgcn_s_waitcnt(0x0F70);                      // nothing lands in LDS after the end
-    __builtin_amdgcn_sched_barrier(0);
+    for (;;) {
+        start<NT, DT>(m, l, o);
+        int stage = 0, k0 = t.k0;
+        for (; k0 + KEYS <= min(t.n_ctx, t.k1); k0 += KEYS, stage ^= 1) block(std::false_type(), k0, stage);
+        for (; k0 < t.k1; k0 += KEYS, stage ^= 1) block(std::true_type(), k0, stage);
+        __builtin_amdgcn_sched_barrier(0);
+        __builtin_amdgcn_s_waitcnt(0x0F70);                  // nothing lands in LDS after the end
+        __builtin_amdgcn_sched_barrier(0);
+        if (careful || t.k1 <= t.n_ctx) break;
+        if (!__syncthreads_or(live && any_nan<NT, DT>(o))) break;
+        careful = true;
+        load(t.k0, 0);
+        load(t.k0 + KEYS, 1);
+    }
     if (!live) return;
 #pragma unroll
     for (int n = 0; n < NT; ++n) {
@@ -447,7 +464,7 @@ __global__ void __launch_bounds__(64 * ROW_WAVES, 2) tree_rows16_kernel(TreeAttn
         l[n] += __shfl_xor(l[n], 32);
         const int r = 16 * n + dc, row = row0 + r;
         if (row >= R) continue;
-        const int64_t at = (int64_t)(t.node0 + row / G) * a.n_q_heads + kvh * G + row % G;
+        const int64_t at = row_at(a, t, kvh, row);
         if (t.index < a.n_parts) {
             const int64_t part = ((int64_t)t.index * a.n_kv_heads + kvh) * TR + wave * 16 * NT + r;
 #pragma unroll
@@ -476,10 +493,9 @@ __global__ void __launch_bounds__(64 * MASS_WAVES, 2) tree_mass16_kernel(TreeAtt
     __shared__ uint32_t row_span[MASS_ROWS], span_s[MAX_TREE_NODES];
     const int lane = threadIdx.x % 64, kg = lane / 16, dc = lane % 16;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
-    const int work = xcd_contiguous_index(blockIdx.x, gridDim.x);
-    const Work t = mass_item_of(a, w, work / a.n_kv_heads);
-    const int kvh = work % a.n_kv_heads;
-    const int G = a.n_q_heads / a.n_kv_heads, R = t.n_nodes * G, last = t.k1 - 1;
+    const Work t = mass_item_of(a, w, blockIdx.y);
+    const int kvh = blockIdx.x;
+    const int R = t.n_nodes * a.group, last = t.k1 - 1;
     const int stride2 = (int)a.slot_stride * 2;
     const uint16_t* kbase = (const uint16_t*)a.k + (int64_t)t.slot0 * a.slot_stride + kvh * a.head_stride;
     u32x4_t kr[2][KS];
@@ -504,14 +520,14 @@ __global__ void __launch_bounds__(64 * MASS_WAVES, 2) tree_mass16_kernel(TreeAtt
         if (r0) __syncthreads();
         for (int i = threadIdx.x; i < tiles * 16 * CHUNKS; i += 64 * MASS_WAVES) {
             const int r = i / CHUNKS, c = i % CHUNKS, row = min(r0 + r, R - 1);
-            uint4 x = *reinterpret_cast<const uint4*>((const uint16_t*)a.q + (int64_t)(t.node0 + row / G) * a.q_stride + (kvh * G + row % G) * HD + c * 8);
+            uint4 x = *reinterpret_cast<const uint4*>((const uint16_t*)a.q + query_at(a, t, kvh, row, HD) + c * 8);
             x.x ^= flip; x.y ^= flip; x.z ^= flip; x.w ^= flip;
             *reinterpret_cast<uint4*>(q_s + r * ROW + (c ^ k_swizzle<HD>(r)) * 16) = x;
         }
         for (int r = threadIdx.x; r < tiles * 16; r += 64 * MASS_WAVES) {
             const int row = min(r0 + r, R - 1);
-            lse_s[r] = r < rows ? a.lse[(int64_t)(t.node0 + row / G) * a.n_q_heads + kvh * G + row % G] * -LOG2E : -INFINITY;   // (rows behind the last: no weight)
-            row_span[r] = r < rows ? w(a.spans + t.node0 + row / G) : 0xffffu;
+            lse_s[r] = r < rows ? a.lse[row_at(a, t, kvh, row)] * -LOG2E : -INFINITY;   // (rows behind the last: no weight)
+            row_span[r] = r < rows ? w(a.spans + t.node0 + node_of(a, row)) : 0xffffu;
         }
         __syncthreads();
         if (r0) load_keys(first);
@@ -551,14 +567,14 @@ __global__ void __launch_bounds__(64 * MASS_WAVES, 2) tree_mass16_kernel(TreeAtt
 
 template <bool BF, int HD, class M>
 static void launch16(const TreeAttnArgs& a, const M& w, hipStream_t st) {
-    const dim3 grid(a.n_items * a.n_kv_heads);
+    const dim3 grid(a.n_kv_heads, a.n_items);
     if (a.tile_rows == 16) hipLaunchKernelGGL((tree_keys16_kernel<BF, HD, 1, M>), grid, dim3(64 * KEY_WAVES), 0, st, a, w);
     else if (a.tile_rows == 32) hipLaunchKernelGGL((tree_keys16_kernel<BF, HD, 2, M>), grid, dim3(64 * KEY_WAVES), 0, st, a, w);
     else if (a.tile_rows == 64) hipLaunchKernelGGL((tree_rows16_kernel<BF, HD, 1, M>), grid, dim3(64 * ROW_WAVES), 0, st, a, w);
     else hipLaunchKernelGGL((tree_rows16_kernel<BF, HD, 2, M>), grid, dim3(64 * ROW_WAVES), 0, st, a, w);
     if (a.n_joins)
         hipLaunchKernelGGL((tree_join_kernel<BF ? SSD_BF16 : SSD_F16, HD, M>), dim3(a.n_joins * a.tile_rows, a.n_kv_heads), dim3(256), 0, st, a, w, BIAS<BF>);
-    if (a.mass) hipLaunchKernelGGL((tree_mass16_kernel<BF, HD, M>), dim3(a.n_mass * a.n_kv_heads), dim3(64 * MASS_WAVES), 0, st, a, w);
+    if (a.mass) hipLaunchKernelGGL((tree_mass16_kernel<BF, HD, M>), dim3(a.n_kv_heads, a.n_mass), dim3(64 * MASS_WAVES), 0, st, a, w);
 }
 
 template <class M>

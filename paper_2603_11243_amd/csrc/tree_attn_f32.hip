@@ -29,10 +29,9 @@ __global__ void __launch_bounds__(64 * KEY_WAVES, 2) tree_attn32_kernel(TreeAttn
     __shared__ uint32_t span_s[MAX_TREE_NODES];
     const int lane = threadIdx.x % 64, kg = lane / 16, dc = lane % 16;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
-    const int work = xcd_contiguous_index(blockIdx.x, gridDim.x);
-    const Work t = item_of(a, w, work / a.n_kv_heads, TR);
-    const int kvh = work % a.n_kv_heads, hd = a.head_dim;
-    const int G = a.n_q_heads / a.n_kv_heads, R = t.n_nodes * G;
+    const Work t = item_of(a, w, blockIdx.y, TR);
+    const int kvh = blockIdx.x, hd = a.head_dim;
+    const int R = t.n_nodes * a.group;
     const int last = max(t.k0, t.k1 - 1);                    // (a range without keys: any row)
     const int n_spans = t.k1 > t.n_ctx ? t.n_nodes : 0;
     for (int i = threadIdx.x; i < n_spans; i += 64 * KEY_WAVES) span_s[i] = w(a.spans + t.node0 + i);
@@ -60,7 +59,7 @@ __global__ void __launch_bounds__(64 * KEY_WAVES, 2) tree_attn32_kernel(TreeAttn
 #pragma unroll
     for (int n = 0; n < NT; ++n) {
         const int row = min(t.row0 + 16 * n + dc, R - 1);
-        load_rows32<HD>(qf[n], (const float*)a.q + (int64_t)(t.node0 + row / G) * a.q_stride + (kvh * G + row % G) * hd, hd, kg);
+        load_rows32<HD>(qf[n], (const float*)a.q + query_at(a, t, kvh, row, hd), hd, kg);
 #pragma unroll
         for (int c = 0; c < DT; ++c) qf[n][c] *= sign;
     }
@@ -89,17 +88,13 @@ __global__ void __launch_bounds__(64 * KEY_WAVES, 2) tree_attn32_kernel(TreeAttn
         }
         const bool masked = k0 + TREE32_KEYS > min(t.n_ctx, t.k1);
         if (masked) {
-            uint32_t key[4];
-#pragma unroll
-            for (int r = 0; r < 4; ++r) {
-                const int at = k0 + 4 * kg + r;
-                key[r] = at < t.n_ctx ? 0xffff0000u : at < t.k1 ? span_s[at - t.n_ctx] : 0u;
-            }
+            uint32_t key[1][4];
+            key_spans<1>(key, t, k0, span_s);
 #pragma unroll
             for (int n = 0; n < NT; ++n) {
-                const uint32_t mine = span_s[min(t.row0 + 16 * n + dc, R - 1) / G];
+                const uint32_t mine = span_s[node_of(a, min(t.row0 + 16 * n + dc, R - 1))];
 #pragma unroll
-                for (int r = 0; r < 4; ++r) s[n][r] = sees(mine, key[r]) ? s[n][r] : -INFINITY;
+                for (int r = 0; r < 4; ++r) s[n][r] = sees(mine, key[0][r]) ? s[n][r] : -INFINITY;
             }
         }
         bool above = false;
@@ -186,10 +181,9 @@ __global__ void __launch_bounds__(64 * MASS_WAVES, 2) tree_mass32_kernel(TreeAtt
     __shared__ uint32_t row_span[MASS32_ROWS], span_s[MAX_TREE_NODES];
     const int lane = threadIdx.x % 64, kg = lane / 16, dc = lane % 16;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
-    const int work = xcd_contiguous_index(blockIdx.x, gridDim.x);
-    const Work t = mass_item_of(a, w, work / a.n_kv_heads);
-    const int kvh = work % a.n_kv_heads, hd = a.head_dim;
-    const int G = a.n_q_heads / a.n_kv_heads, R = t.n_nodes * G, last = t.k1 - 1;
+    const Work t = mass_item_of(a, w, blockIdx.y);
+    const int kvh = blockIdx.x, hd = a.head_dim;
+    const int R = t.n_nodes * a.group, last = t.k1 - 1;
     const float* kbase = (const float*)a.k + (int64_t)t.slot0 * a.slot_stride + kvh * a.head_stride;
     f32x4_t kr[DT];
     auto load_keys = [&](int k0) { load_rows32<HD>(kr, kbase + (int64_t)min(k0 + dc, last) * a.slot_stride, hd, kg); };
@@ -204,26 +198,21 @@ __global__ void __launch_bounds__(64 * MASS_WAVES, 2) tree_mass32_kernel(TreeAtt
         for (int i = threadIdx.x; i < tiles * 16 * CHUNKS; i += 64 * MASS_WAVES) {
             const int r = i / CHUNKS, c = i % CHUNKS, row = min(r0 + r, R - 1);
             f32x4_t x = {0.f, 0.f, 0.f, 0.f};
-            if (c * 4 < hd) x = *reinterpret_cast<const f32x4_t*>((const float*)a.q + (int64_t)(t.node0 + row / G) * a.q_stride + (kvh * G + row % G) * hd + c * 4);
+            if (c * 4 < hd) x = *reinterpret_cast<const f32x4_t*>((const float*)a.q + query_at(a, t, kvh, row, hd) + c * 4);
             *reinterpret_cast<f32x4_t*>(q_s + r * HD + (c ^ (r & 15)) * 4) = x * sign;
         }
         for (int r = threadIdx.x; r < tiles * 16; r += 64 * MASS_WAVES) {
             const int row = min(r0 + r, R - 1);
-            lse_s[r] = r < rows ? a.lse[(int64_t)(t.node0 + row / G) * a.n_q_heads + kvh * G + row % G] * -LOG2E : -INFINITY;   // (rows behind the last: no weight)
-            row_span[r] = r < rows ? w(a.spans + t.node0 + row / G) : 0xffffu;
+            lse_s[r] = r < rows ? a.lse[row_at(a, t, kvh, row)] * -LOG2E : -INFINITY;   // (rows behind the last: no weight)
+            row_span[r] = r < rows ? w(a.spans + t.node0 + node_of(a, row)) : 0xffffu;
         }
         __syncthreads();
         if (r0) load_keys(first);
         for (int k0 = first; k0 < t.k1; k0 += STEP) {
             f32x4_t acc[1] = {(f32x4_t){0.f, 0.f, 0.f, 0.f}};
             const bool masked = k0 + TREE32_KEYS > t.n_ctx;
-            uint32_t key[4];
-            if (masked)
-#pragma unroll
-                for (int r = 0; r < 4; ++r) {
-                    const int at = k0 + 4 * kg + r;
-                    key[r] = at < t.n_ctx ? 0xffff0000u : at < t.k1 ? span_s[at - t.n_ctx] : 0u;
-                }
+            uint32_t key[1][4];
+            if (masked) key_spans<1>(key, t, k0, span_s);
             for (int n = 0; n < tiles; ++n) {
                 const int r = 16 * n + dc;
                 f32x4_t s = {0.f, 0.f, 0.f, 0.f};
@@ -238,7 +227,7 @@ __global__ void __launch_bounds__(64 * MASS_WAVES, 2) tree_mass32_kernel(TreeAtt
 #pragma unroll
                 for (int e = 0; e < 4; ++e) {
                     const float p = __builtin_amdgcn_exp2f(fmaf(s[e], sc, base));
-                    acc[0][e] += masked && !sees(mine, key[e]) ? 0.f : p;
+                    acc[0][e] += masked && !sees(mine, key[0][e]) ? 0.f : p;
                 }
             }
             load_keys(k0 + STEP);
@@ -249,11 +238,11 @@ __global__ void __launch_bounds__(64 * MASS_WAVES, 2) tree_mass32_kernel(TreeAtt
 
 template <int HD, class M>
 static void launch32(const TreeAttnArgs& a, const M& w, hipStream_t st) {
-    const dim3 grid(a.n_items * a.n_kv_heads);
+    const dim3 grid(a.n_kv_heads, a.n_items);
     if (a.tile_rows == 16) hipLaunchKernelGGL((tree_attn32_kernel<HD, 1, M>), grid, dim3(64 * KEY_WAVES), 0, st, a, w);
     else hipLaunchKernelGGL((tree_attn32_kernel<HD, 2, M>), grid, dim3(64 * KEY_WAVES), 0, st, a, w);
     if (a.n_joins) hipLaunchKernelGGL((tree_join_kernel<SSD_F32, HD, M>), dim3(a.n_joins * a.tile_rows, a.n_kv_heads), dim3(256), 0, st, a, w, 0.f);
-    if (a.mass) hipLaunchKernelGGL((tree_mass32_kernel<HD, M>), dim3(a.n_mass * a.n_kv_heads), dim3(64 * MASS_WAVES), 0, st, a, w);
+    if (a.mass) hipLaunchKernelGGL((tree_mass32_kernel<HD, M>), dim3(a.n_kv_heads, a.n_mass), dim3(64 * MASS_WAVES), 0, st, a, w);
 }
 
 template <class M>

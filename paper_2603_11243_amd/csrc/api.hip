@@ -1772,7 +1772,7 @@ int kv_evict(ssd_ctx* ctx, const ssd_kv_view* from, const float* mass, int B, co
     e.n_layers = from->n_layers; e.n_kv_heads = from->n_kv_heads; e.row_chunks = from->head_dim / (int)unit;
     e.mass = mass; e.mass_slots = from->slots;
     e.mass_out = mass_out; e.mass_out_slots = to->slots;
-    e.utts = reinterpret_cast<const EvictUtt*>(ws + p.utts); e.B = B;
+    e.utts = reinterpret_cast<const EvictUtt*>(ws + p.utts); e.B = B; e.most_ctx = *std::max_element(ctx_len, ctx_len + B);
     e.n_first = n_first; e.n_recent = n_recent; e.n_kept = (int)kept;
     e.rows = rows_out ? rows_out : reinterpret_cast<int32_t*>(ws + p.rows);
     {

@@ -13,9 +13,14 @@ __device__ __forceinline__ uint32_t ordered(float v) {
     return u & 0x80000000u ? ~u : u | 0x80000000u;
 }
 
-constexpr int SEL_THREADS = 1024;
+// Selection: one workgroup of THREADS a (layer, head, utterance), whose weights stay in registers, V a thread, thread t those of rows t V .. t V + V - 1 of each
+// CHUNK = THREADS V rows (more than CHUNK rows: read again for every step).  The need-th largest is found digit by digit, 11, 11 and 10 bits from
+// the top: a histogram in LDS of the rows that agree with the digits found, of the bins the one in which the count from above reaches `need`.  Then the
+// kept rows in order: a thread's rows are consecutive, so that one scan over the threads places them.
+constexpr int BINS = 2048;
 
-// Sums of a value over the threads before this one and over all of them.
+// Sums of v over the threads before this one, and over all.
+template <int THREADS>
 __device__ __forceinline__ int2 scan(int v, int* waves) {
     const int lane = threadIdx.x % 64, wave = threadIdx.x / 64;
     int s = v;
@@ -24,53 +29,109 @@ __device__ __forceinline__ int2 scan(int v, int* waves) {
         const int o = __shfl_up(s, d);
         if (lane >= d) s += o;
     }
+    if constexpr (THREADS == 64) return make_int2(s - v, __shfl(s, 63));
     __syncthreads();
     if (lane == 63) waves[wave] = s;
     __syncthreads();
     int before = 0, all = 0;
-    for (int w = 0; w < SEL_THREADS / 64; ++w) {
+#pragma unroll
+    for (int w = 0; w < THREADS / 64; ++w) {
         if (w < wave) before += waves[w];
         all += waves[w];
     }
     return make_int2(before + s - v, all);
 }
 
-// One workgroup a (layer, head, utterance): the need-th largest weight bit by bit, then the kept rows in order.
-__global__ void __launch_bounds__(SEL_THREADS) evict_select_kernel(EvictArgs a) {
-    __shared__ int waves[SEL_THREADS / 64];
+template <int THREADS, int V, bool MORE>
+__global__ void __launch_bounds__(THREADS) evict_select_kernel(EvictArgs a) {
+    constexpr int CHUNK = THREADS * V, PER = BINS / THREADS;
+    __shared__ int hist[BINS];
+    __shared__ int waves[THREADS / 64];
+    __shared__ int found[2];                                 // digit, rows above it
     const EvictUtt u = a.utts[blockIdx.x];
     const int64_t lh = blockIdx.y;                           // layer * heads + head
     const float* w = a.mass + lh * a.mass_slots + u.slot0;
     int32_t* rows = a.rows + lh * a.n_kept + u.kept0;
     const int tid = threadIdx.x;
-    const bool all = u.keep >= u.n_ctx;
-    const int lo = all ? u.n_ctx : a.n_first, hi = all ? u.n_ctx : u.n_ctx - a.n_recent;
-    const int need = all ? 0 : u.keep - a.n_first - a.n_recent;
-    uint32_t t = 0;                                          // largest value that at least `need` weights reach
-    if (need > 0)
-        for (int bit = 31; bit >= 0; --bit) {
-            const uint32_t c = t | 1u << bit;
-            int n = 0;
-            for (int i = lo + tid; i < hi; i += SEL_THREADS) n += ordered(w[i]) >= c;
-            if (scan(n, waves).y >= need) t = c;
-        }
-    int n_above = 0;
-    if (need > 0) {
-        for (int i = lo + tid; i < hi; i += SEL_THREADS) n_above += ordered(w[i]) > t;
-        n_above = scan(n_above, waves).y;
+    if (u.keep >= u.n_ctx) {
+        for (int i = tid; i < u.n_ctx; i += THREADS) rows[i] = i;
+        return;
     }
-    int ties = need - n_above, out = 0;
-    for (int i0 = 0; i0 < u.n_ctx; i0 += SEL_THREADS) {
-        const int i = i0 + tid;
-        const bool between = i >= lo && i < hi;
-        const uint32_t o = between ? ordered(w[i]) : 0;
-        const int tie = need > 0 && between && o == t;
-        const int2 tr = scan(tie, waves);
-        const int keep = i < u.n_ctx && (!between || (need > 0 && (o > t || (tie && tr.x < ties))));
-        ties -= tr.y;
-        const int2 kr = scan(keep, waves);
-        if (keep) rows[out + kr.x] = i;
+    const int lo = a.n_first, hi = u.n_ctx - a.n_recent;     // rows between, of which `need` stay
+    int need = u.keep - a.n_first - a.n_recent;
+    uint32_t x[V];
+    auto load = [&](int c0) __attribute__((always_inline)) {
+#pragma unroll
+        for (int e = 0; e < V; ++e) {
+            const int i = c0 + tid * V + e;
+            x[e] = ordered(w[min(i, u.n_ctx - 1)]);
+        }
+    };
+    load(0);
+    uint32_t t = 0, mask = 0;                                // digits found, and which bits they are
+    if (need > 0) {
+#pragma unroll
+        for (int round = 0; round < 3; ++round) {
+            const int shift = round == 0 ? 21 : round == 1 ? 10 : 0, bits = round == 2 ? 10 : 11;
+            for (int i = tid; i < BINS; i += THREADS) hist[i] = 0;
+            __syncthreads();
+            for (int c0 = 0; c0 < u.n_ctx; c0 += CHUNK) {
+                if (MORE && (round || c0)) load(c0);
+#pragma unroll
+                for (int e = 0; e < V; ++e) {
+                    const int i = c0 + tid * V + e;
+                    if (i >= lo && i < hi && ((x[e] ^ t) & mask) == 0) atomicAdd(&hist[x[e] >> shift & ((1u << bits) - 1)], 1);
+                }
+                if (!MORE) break;
+            }
+            __syncthreads();
+            // bins from the top: thread t has bins BINS - 1 - t PER - e
+            int mine[PER], sum = 0;
+#pragma unroll
+            for (int e = 0; e < PER; ++e) sum += mine[e] = hist[BINS - 1 - tid * PER - e];
+            int above = scan<THREADS>(sum, waves).x;
+#pragma unroll
+            for (int e = 0; e < PER; ++e) {
+                if (above < need && above + mine[e] >= need) {
+                    found[0] = BINS - 1 - tid * PER - e;
+                    found[1] = above;
+                }
+                above += mine[e];
+            }
+            __syncthreads();
+            t |= (uint32_t)found[0] << shift;
+            mask |= ((1u << bits) - 1) << shift;
+            need -= found[1];
+            __syncthreads();
+        }
+    }
+    // rows of the weight t that stay: the first `need` of them
+    int ties_before = 0, out = 0;
+    for (int c0 = 0; c0 < u.n_ctx; c0 += CHUNK) {
+        if (MORE) load(c0);
+        int ties = 0, above = 0;                             // of this thread's rows; above: kept whatever the ties are
+        uint32_t tie[(V + 31) / 32] = {}, sure[(V + 31) / 32] = {};
+#pragma unroll
+        for (int e = 0; e < V; ++e) {
+            const int i = c0 + tid * V + e;
+            const bool between = i >= lo && i < hi;
+            if (between && mask && x[e] == t) { tie[e / 32] |= 1u << e % 32; ++ties; }
+            if (i < u.n_ctx && (!between || (mask && x[e] > t))) { sure[e / 32] |= 1u << e % 32; ++above; }
+        }
+        const int2 tr = scan<THREADS>(ties, waves);
+        int left = need - ties_before - tr.x;                // ties this thread may keep
+        left = min(max(left, 0), ties);
+        const int2 kr = scan<THREADS>(above + left, waves);
+        int at = out + kr.x;
+#pragma unroll
+        for (int e = 0; e < V; ++e) {
+            bool keep = sure[e / 32] >> e % 32 & 1;
+            if ((tie[e / 32] >> e % 32 & 1) && left > 0) { keep = true; --left; }
+            if (keep) rows[at++] = c0 + tid * V + e;
+        }
+        ties_before += tr.y;
         out += kr.y;
+        if (!MORE) break;
     }
 }
 
@@ -96,7 +157,11 @@ __global__ void __launch_bounds__(256) evict_copy_kernel(EvictArgs a) {
 }
 
 void launch_kv_evict(const EvictArgs& a, hipStream_t st) {
-    hipLaunchKernelGGL(evict_select_kernel, dim3(a.B, a.n_layers * a.n_kv_heads), dim3(SEL_THREADS), 0, st, a);
+    const dim3 grid(a.B, a.n_layers * a.n_kv_heads);
+    if (a.most_ctx <= 256 * 4) hipLaunchKernelGGL((evict_select_kernel<256, 4, false>), grid, dim3(256), 0, st, a);
+    else if (a.most_ctx <= 1024 * 8) hipLaunchKernelGGL((evict_select_kernel<1024, 8, false>), grid, dim3(1024), 0, st, a);
+    else if (a.most_ctx <= 1024 * 32) hipLaunchKernelGGL((evict_select_kernel<1024, 32, false>), grid, dim3(1024), 0, st, a);
+    else hipLaunchKernelGGL((evict_select_kernel<1024, 32, true>), grid, dim3(1024), 0, st, a);
     hipLaunchKernelGGL(evict_copy_kernel, dim3(a.n_kept, a.n_layers), dim3(256), 0, st, a);
 }
 

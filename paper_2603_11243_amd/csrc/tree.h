@@ -68,7 +68,7 @@ struct EvictArgs {
     int n_layers, n_kv_heads, row_chunks;    // 16-byte units of a row
     const float* mass; int64_t mass_slots;
     float* mass_out; int64_t mass_out_slots; // mass_out NULL: not wanted
-    const EvictUtt* utts; int B;
+    const EvictUtt* utts; int B, most_ctx;   // most_ctx: rows of the longest context
     int n_first, n_recent, n_kept;           // n_kept: rows that all utterances keep
     int32_t* rows;                           // [n_layers, n_kv_heads, n_kept]
 };

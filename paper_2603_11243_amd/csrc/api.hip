@@ -1561,12 +1561,15 @@ Extent extent_of(const ssd_kv_view& v, const void* p) {
 }
 bool overlap(const Extent& a, const Extent& b) { return a.a < b.z && b.a < a.z; }
 
-struct EvictPlan { size_t utts, rows, total; };
-EvictPlan plan_evict(int64_t layers_heads, int64_t kept, int64_t utts) {
+struct EvictPlan { size_t words, rows, counts, known, before, total; };
+EvictPlan plan_evict(int64_t layers_heads, int64_t kept, int64_t utts, int64_t pieces) {
     EvictPlan p;
     size_t o = 0;
-    p.utts = o; o = align_up(o + (size_t)utts * sizeof(EvictUtt));
+    p.words = o; o = align_up(o + (size_t)(6 * utts + pieces) * 4);
     p.rows = o; o = align_up(o + (size_t)(layers_heads * kept) * 4);
+    p.counts = o; o = align_up(o + (size_t)(layers_heads * pieces) * 2 * EVICT_BINS * sizeof(uint16_t));
+    p.known = o; o = align_up(o + (pieces ? (size_t)(layers_heads * utts) * 2 * EVICT_KNOWN_BYTES : 0));
+    p.before = o; o = align_up(o + (size_t)(layers_heads * pieces) * sizeof(int2));
     p.total = o;
     return p;
 }
@@ -1717,7 +1720,7 @@ int tree_path(ssd_ctx* ctx, const float* node_logp, int B, const int32_t* cu_nod
 
 size_t ssd_evict_workspace_bytes(const ssd_ctx* ctx, int n_layers, int n_kv_heads, int64_t max_kept_rows, int64_t max_utts) {
     if (!ctx || n_layers <= 0 || n_kv_heads <= 0 || max_kept_rows < 0 || max_utts < 0) return 0;
-    return plan_evict((int64_t)n_layers * n_kv_heads, max_kept_rows, max_utts).total + 256;
+    return plan_evict((int64_t)n_layers * n_kv_heads, max_kept_rows, max_utts, max_utts + EVICT_PIECES).total + 256;
 }
 
 int kv_evict(ssd_ctx* ctx, const ssd_kv_view* from, const float* mass, int B, const int32_t* kv_start, const int32_t* ctx_len, const int32_t* keep,
@@ -1756,15 +1759,41 @@ int kv_evict(ssd_ctx* ctx, const ssd_kv_view* from, const float* mass, int B, co
     if (kept > 0x7fffffff) return fail(ctx, SSD_ESHAPE, "kv_evict: more than 2^31 - 1 rows are kept; split the batch");
     if (!ranges_distinct(B, out_start, len)) return fail(ctx, SSD_EINVAL, "kv_evict: utterances share slots of the other cache");
     if (!kept) return SSD_OK;
-    const EvictPlan p = plan_evict(lh, rows_out ? 0 : kept, B);
-    if (!ctx->ws || ctx->ws_bytes < p.total) return fail(ctx, SSD_EWORKSPACE, "kv_evict: workspace of %zu bytes needed, %zu set", p.total, ctx->ws_bytes);
-    std::vector<uint32_t> meta((size_t)B * sizeof(EvictUtt) / 4);
-    memcpy(meta.data(), utts.data(), meta.size() * 4);
-    rc = place_meta(ctx, meta, ctx->ws);
-    if (rc != SSD_OK) return rc;
-    char* ws = static_cast<char*>(ctx->ws);
-    const int64_t unit = 16 / (int64_t)kv_elem(from->dtype);
     EvictArgs e;
+    static_assert(sizeof(EvictUtt) == 5 * 4, "words of an utterance");
+    const uint32_t* first_word = reinterpret_cast<const uint32_t*>(utts.data());
+    std::vector<uint32_t> words(first_word, first_word + (size_t)B * 5);
+    e.B = B; e.most_ctx = *std::max_element(ctx_len, ctx_len + B);
+    e.n_pieces = 0; e.piece_rows = EVICT_PIECE;
+    if (e.most_ctx > EVICT_PIECE) {
+        int64_t total = 0;
+        for (int b = 0; b < B; ++b) total += ctx_len[b];
+        // (in whole chunks of EVICT_PIECE, but no more rows than 16 bits count)
+        const int64_t share = (total + EVICT_PIECES - 1) / EVICT_PIECES;
+        const int64_t rows = (share + EVICT_PIECE - 1) / EVICT_PIECE * EVICT_PIECE;
+        if (rows > 65535) return fail(ctx, SSD_ESHAPE, "kv_evict: contexts of %lld rows in all; split the batch", (long long)total);
+        e.piece_rows = (int)rows;
+        e.pieces = (int)words.size() + B;
+        e.firsts = (int)words.size();
+        for (int b = 0; b < B; ++b) {
+            words.push_back(e.n_pieces);
+            e.n_pieces += (int)((ctx_len[b] + rows - 1) / rows);
+        }
+        for (int b = 0; b < B; ++b)
+            for (int64_t r = 0; r < ctx_len[b]; r += rows) words.push_back(b);
+    }
+    const EvictPlan p = plan_evict(lh, rows_out ? 0 : kept, B, e.n_pieces);
+    if (!ctx->ws || ctx->ws_bytes < p.total) return fail(ctx, SSD_EWORKSPACE, "kv_evict: workspace of %zu bytes needed, %zu set", p.total, ctx->ws_bytes);
+    char* ws = static_cast<char*>(ctx->ws);
+    const bool in_args = words.size() <= MetaWords::WORDS;
+    if (!in_args) {
+        rc = place_meta(ctx, words, ws + p.words);
+        if (rc != SSD_OK) return rc;
+    }
+    e.counts = reinterpret_cast<uint16_t*>(ws + p.counts);
+    e.known = reinterpret_cast<Known*>(ws + p.known);
+    e.before = reinterpret_cast<int2*>(ws + p.before);
+    const int64_t unit = 16 / (int64_t)kv_elem(from->dtype);
     e.k = from->k; e.v = from->v;
     e.slot_stride = from->slot_stride / unit; e.head_stride = from->head_stride / unit; e.layer_stride = from->n_layers > 1 ? from->layer_stride / unit : 0;
     e.k_out = to->k; e.v_out = to->v;
@@ -1772,12 +1801,11 @@ int kv_evict(ssd_ctx* ctx, const ssd_kv_view* from, const float* mass, int B, co
     e.n_layers = from->n_layers; e.n_kv_heads = from->n_kv_heads; e.row_chunks = from->head_dim / (int)unit;
     e.mass = mass; e.mass_slots = from->slots;
     e.mass_out = mass_out; e.mass_out_slots = to->slots;
-    e.utts = reinterpret_cast<const EvictUtt*>(ws + p.utts); e.B = B; e.most_ctx = *std::max_element(ctx_len, ctx_len + B);
     e.n_first = n_first; e.n_recent = n_recent; e.n_kept = (int)kept;
     e.rows = rows_out ? rows_out : reinterpret_cast<int32_t*>(ws + p.rows);
     {
         ProfScope ps(ctx, SSD_PROF_OTHER);
-        launch_kv_evict(e, ctx->stream);
+        launch_kv_evict(e, in_args ? words.data() : nullptr, (int)words.size(), reinterpret_cast<const uint32_t*>(ws + p.words), ctx->stream);
     }
     HIP_TRY(ctx, hipGetLastError());
     return SSD_OK;

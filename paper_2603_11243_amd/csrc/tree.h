@@ -61,6 +61,7 @@ void launch_tree_commit(void* k, void* v, int64_t slot_stride, int64_t layer_str
                         const int32_t* kv_start, const int32_t* ctx_len, const int32_t* cu, const int32_t* accept_len, const int32_t* path, int B,
                         hipStream_t st);
 
+struct Known;
 struct EvictUtt { int32_t slot0, n_ctx, keep, out0, kept0; };     // kept0: kept rows of the utterances before
 struct EvictArgs {
     const void* k; const void* v; int64_t slot_stride, head_stride, layer_stride;         // in 16-byte units
@@ -68,10 +69,18 @@ struct EvictArgs {
     int n_layers, n_kv_heads, row_chunks;    // 16-byte units of a row
     const float* mass; int64_t mass_slots;
     float* mass_out; int64_t mass_out_slots; // mass_out NULL: not wanted
-    const EvictUtt* utts; int B, most_ctx;   // most_ctx: rows of the longest context
+    int B, most_ctx;                         // most_ctx: rows of the longest context
     int n_first, n_recent, n_kept;           // n_kept: rows that all utterances keep
     int32_t* rows;                           // [n_layers, n_kv_heads, n_kept]
+    // contexts of more than EVICT_PIECE rows: pieces of piece_rows; from word `pieces` on the utterance of each, from `firsts` on each utterance's first
+    int n_pieces, piece_rows, pieces, firsts;
+    uint16_t* counts; Known* known; int2* before;      // [layers * heads][pieces][2][bins], [layers * heads][B][2], [layers * heads][pieces]
 };
-void launch_kv_evict(const EvictArgs& a, hipStream_t st);
+constexpr int EVICT_PIECE = 8192;            // rows of a workgroup (counts are 16 bits wide: at most 65535 rows a piece)
+constexpr int EVICT_PIECES = 64;             // longer contexts are cut into at most so many pieces, and one an utterance
+constexpr int EVICT_BINS = 2048;
+constexpr size_t EVICT_KNOWN_BYTES = 16;
+// words: the B EvictUtt, then those of the pieces, n in all, in host memory, to travel as arguments; or NULL, then they are in dev_words
+void launch_kv_evict(const EvictArgs& a, const uint32_t* words, int n, const uint32_t* dev_words, hipStream_t st);
 
 }  // namespace ssd

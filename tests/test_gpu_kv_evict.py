@@ -88,11 +88,22 @@ def test_equal_weights(n):
     _check(lambda r, *s: np.where(r.random(s) < 0.5, 0.0, -0.0), ctx_len=(n,), keep=(n // 2,), L=1)
 
 
-@pytest.mark.parametrize("n", [60, 5000])
+@pytest.mark.parametrize("n", [60, 5000, 20000])
 def test_weights_that_are_not_finite(n):
     values = np.array([np.nan, -np.nan, np.inf, -np.inf, 0.0, -1.5, 2.5, 1e-42, -1e-42, 3e38])
     for keep in (1, n // 4, n // 2, n - 5):
         _check(lambda r, *s: values[r.integers(0, len(values), size=s)], ctx_len=(n,), keep=(keep,), L=1, seed=keep)
+
+
+def test_long_and_short_contexts_in_one_call():
+    _check(_weights, ctx_len=(20000, 3, 8192, 8193, 0, 500, 40000), keep=(7000, 3, 1, 8000, 0, 100, 39990), first=1, recent=0, L=1, H=2)
+    _check(lambda r, *s: r.integers(0, 2, size=s) / 3, ctx_len=(30000, 100, 9000), keep=(16000, 100, 4500), first=5, recent=3, L=2, H=1)
+
+
+def test_contexts_of_more_chunks_than_pieces():
+    """600000 rows: two chunks a piece; values that fill one bin of every digit, and ordinary ones."""
+    _check(_weights, ctx_len=(600000,), keep=(150001,), first=3, recent=70000, L=1, H=1, hd=64)
+    _check(lambda r, *s: np.full(s, 0.125), ctx_len=(600001,), keep=(300000,), L=1, H=1, hd=64)
 
 
 def test_optional_outputs():

@@ -5,6 +5,7 @@ and for the stream handle.  Every computation happens inside libssd.so.
 """
 import ctypes as C
 import os
+import struct
 from typing import Optional, Sequence
 
 import numpy as np
@@ -164,6 +165,16 @@ def _host_i32(a: Sequence[int]) -> np.ndarray:
     return np.ascontiguousarray(np.asarray(a, dtype=np.int32))
 
 
+def _host_call_i32(a: Sequence[int]) -> np.ndarray:
+    """_host_i32 that leaves an array as it is which needs nothing: what small calls pass four of (0.6 us each)."""
+    return a if type(a) is np.ndarray and a.dtype == np.int32 and a.flags.c_contiguous else _host_i32(a)
+
+
+def _host_arg(a: np.ndarray):
+    """Argument for an array that the call reads before it returns: a copy of a few words (0.1 us), the address of many."""
+    return a.tobytes() if a.size <= 1024 else a.ctypes.data
+
+
 def _at(t: torch.Tensor, device) -> bool:
     return t.device == device or (device.index is None and t.device.type == device.type)
 
@@ -171,24 +182,34 @@ def _at(t: torch.Tensor, device) -> bool:
 def _on(device, dtype, **tensors):
     """Tensors that a call reads or writes as contiguous memory of its device: ValueError names the one that is not."""
     for name, t in tensors.items():
-        if t is not None and (not _at(t, device) or t.dtype != dtype or not t.is_contiguous()):
+        if t is not None and (t.dtype != dtype or not t.is_contiguous() or not _at(t, device)):
             raise ValueError(f"{name} must be a contiguous {dtype} tensor on {device}")
 
 
-def _kv_view(device, k: torch.Tensor, v: torch.Tensor) -> KvViewC:
-    """ssd_kv_view of k and v [slots, K/V heads, head_dim], or with a dimension of layers before; any strides but the last."""
-    if k.shape != v.shape or k.dim() not in (3, 4) or k.dtype != v.dtype or k.dtype not in _KV_CODE or not _at(k, device) or not _at(v, device):
-        raise ValueError(f"k and v must be alike: [layers,] slots, K/V heads, head_dim, float16, bfloat16 or float32, on {device}")
-    L, (n, H, hd) = (int(k.shape[0]) if k.dim() == 4 else 1), k.shape[-3:]
+_KV_VIEW = struct.Struct("=QQqqqqiiii")          # ssd_kv_view
 
-    def strides(t):                                          # of dimensions of one entry: as if the rows lay close together
-        ss, hs = int(t.stride(-3)), int(t.stride(-2)) if H > 1 else int(hd)
-        if n <= 1:
-            ss = max(int(hd), hs * (int(H) - 1) + int(hd))
-        return ss, hs, int(t.stride(0)) if L > 1 else 0
-    if strides(k) != strides(v) or k.stride(-1) != 1 and hd > 1 or v.stride(-1) != 1 and hd > 1:
-        raise ValueError("k and v must have the same strides, and consecutive elements in a row")
-    return KvViewC(k.data_ptr(), v.data_ptr(), int(n), *strides(k), L, int(H), int(hd), _KV_CODE[k.dtype])
+
+def _kv_view(device, k: torch.Tensor, v: torch.Tensor):
+    """(ssd_kv_view as bytes, slots, layers, K/V heads, head_dim) of k and v [slots, K/V heads, head_dim], or with a dimension of layers before; any
+    strides but the last."""
+    shape, st, sv, code = k.shape, k.stride(), v.stride(), _KV_CODE.get(k.dtype)
+    if shape != v.shape or len(shape) not in (3, 4) or k.dtype is not v.dtype or code is None or not _at(k, device) or k.device != v.device:
+        raise ValueError(f"k and v must be alike: [layers,] slots, K/V heads, head_dim, float16, bfloat16 or float32, on {device}")
+    n, H, hd = shape[-3:]
+    L = shape[0] if len(shape) == 4 else 1
+    if n > 1 and H > 1 and L == 1 and st == sv:
+        ss, hs, one = st[-3:]
+        ls = 0
+    else:
+        def strides(t):                                      # of dimensions of one entry: as if the rows lay close together
+            ss, hs = t[-3], t[-2] if H > 1 else hd
+            return ss if n > 1 else max(hd, hs * (H - 1) + hd), hs, t[0] if L > 1 else 0
+        (ss, hs, ls), one = strides(st), st[-1]
+        if strides(sv) != (ss, hs, ls) or hd > 1 and sv[-1] != one:
+            raise ValueError("k and v must have the same strides")
+    if one != 1 and hd > 1:
+        raise ValueError("the elements of a row of k and v must be consecutive")
+    return _KV_VIEW.pack(k.data_ptr(), v.data_ptr(), n, ss, hs, ls, L, H, hd, code), n, L, H, hd
 
 
 class Context:
@@ -479,36 +500,47 @@ class Context:
         """Attention of the nodes of trees (tree_attention): q [nodes, query heads, head_dim] (any stride between nodes) over k, v [slots, K/V heads,
         head_dim] (any strides but the last).  Returns out [nodes, query heads, head_dim]; mass [K/V heads, slots] collects the rows' weights, lse
         [nodes, query heads] takes the log-sum-exps (both fp32, optional).  scale: 1 / sqrt(head_dim) unless given."""
-        ks, cl, cn, pa = _host_i32(kv_start), _host_i32(ctx_len), _host_i32(cu_nodes), _host_i32(parent)
-        B, view = len(cn) - 1, _kv_view(self.device, k, v)
-        N, Hq, hd = (int(x) for x in q.shape)
-        if k.dim() != 3 or q.dtype != k.dtype or not _at(q, self.device) or hd != view.head_dim or q.stride(2) != 1 or (Hq > 1 and q.stride(1) != hd):
+        ks, cl, cn, pa = _host_call_i32(kv_start), _host_call_i32(ctx_len), _host_call_i32(cu_nodes), _host_call_i32(parent)
+        B, dev = len(cn) - 1, self.device
+        view, slots, _, H, hd = _kv_view(dev, k, v)
+        N, Hq, q_hd = q.shape
+        q_stride, head_stride, one = q.stride()
+        if len(k.shape) != 3 or q.dtype is not k.dtype or q.device != k.device or q_hd != hd or (one != 1 and hd > 1) or (Hq > 1 and head_stride != hd):
             raise ValueError("q must be [nodes, query heads, head_dim] in the type of k and v, the heads of a node consecutive, k and v of one layer")
-        if len(ks) != B or len(cl) != B or len(pa) != N or (B >= 0 and int(cn[-1]) != N):
+        if len(ks) != B or len(cl) != B or len(pa) != N or (B >= 0 and cn[-1] != N):
             raise ValueError("kv_start, ctx_len, cu_nodes, parent and q do not fit together")
         if out is None:
-            out = torch.empty((N, Hq, hd), dtype=q.dtype, device=self.device)
-        _on(self.device, q.dtype, out=out)
-        _on(self.device, torch.float32, mass=mass, lse=lse)
-        if out.numel() != N * Hq * hd or (lse is not None and lse.numel() != N * Hq) or (mass is not None and mass.numel() != view.n_kv_heads * view.slots):
-            raise ValueError("out, lse or mass has the wrong size")
-        self._check(self._lib.tree_attention(self._h, q.data_ptr(), int(q.stride(0)) if N > 1 else Hq * hd, Hq, C.byref(view), B, ks.tobytes(), cl.tobytes(),
-                                             cn.tobytes(), pa.tobytes(), hd ** -0.5 if scale is None else scale, _ptr(out), _ptr(lse), _ptr(mass)))
+            out = q.new_empty((N, Hq, hd))
+        else:
+            _on(dev, q.dtype, out=out)
+            if out.numel() != N * Hq * hd:
+                raise ValueError("out has the wrong size")
+        if mass is not None or lse is not None:
+            _on(dev, torch.float32, mass=mass, lse=lse)
+            if (lse is not None and lse.numel() != N * Hq) or (mass is not None and mass.numel() != H * slots):
+                raise ValueError("lse or mass has the wrong size")
+        self._check(self._lib.tree_attention(self._h, q.data_ptr(), q_stride if N > 1 else Hq * hd, Hq, view, B, _host_arg(ks), _host_arg(cl), _host_arg(cn),
+                                             _host_arg(pa), hd ** -0.5 if scale is None else scale, out.data_ptr(), None if lse is None else lse.data_ptr(),
+                                             None if mass is None else mass.data_ptr()))
         return out
 
     def tree_path(self, node_logp: torch.Tensor, cu_nodes, parent, tau: float, out: Optional[dict] = None) -> dict:
         """Accepted path of every tree (tree_path)."""
-        cn, pa = _host_i32(cu_nodes), _host_i32(parent)
-        B, N = len(cn) - 1, len(pa)
-        _on(self.device, torch.float32, node_logp=node_logp)
-        if node_logp.numel() != N or int(cn[-1]) != N:
+        cn, pa = _host_call_i32(cu_nodes), _host_call_i32(parent)
+        B, N, dev = len(cn) - 1, len(pa), self.device
+        if node_logp.dtype is not torch.float32 or not node_logp.is_contiguous() or not _at(node_logp, dev):
+            raise ValueError(f"node_logp must be a contiguous float32 tensor on {dev}")
+        if B < 0 or node_logp.numel() != N or cn[-1] != N:
             raise ValueError("cu_nodes, parent and node_logp do not fit together")
         if out is None:
-            out = {"accept_len": torch.empty(max(B, 0), dtype=torch.int32, device=self.device),
-                   "accept_node": torch.empty(max(B, 0), dtype=torch.int32, device=self.device),
-                   "path": torch.empty(N, dtype=torch.int32, device=self.device)}
-        self._check(self._lib.tree_path(self._h, _ptr(node_logp), B, cn.tobytes(), pa.tobytes(), tau, _ptr(out["accept_len"]),
-                                        _ptr(out["accept_node"]), _ptr(out["path"])))
+            i32 = torch.int32
+            out = {"accept_len": node_logp.new_empty(B, dtype=i32), "accept_node": node_logp.new_empty(B, dtype=i32), "path": node_logp.new_empty(N, dtype=i32)}
+        else:
+            _on(dev, torch.int32, **out)
+            if out["accept_len"].numel() < B or out["accept_node"].numel() < B or out["path"].numel() < N:
+                raise ValueError("accept_len, accept_node or path is too small")
+        self._check(self._lib.tree_path(self._h, node_logp.data_ptr(), B, _host_arg(cn), _host_arg(pa), tau, out["accept_len"].data_ptr(),
+                                        out["accept_node"].data_ptr(), out["path"].data_ptr()))
         return out
 
     def kv_evict(self, k: torch.Tensor, v: torch.Tensor, mass: torch.Tensor, kv_start, ctx_len, keep, n_first: int, n_recent: int,
@@ -516,19 +548,19 @@ class Context:
                  want_rows: bool = False) -> Optional[torch.Tensor]:
         """Copies the rows of largest weight to another cache (kv_evict): k, v [layers, slots, K/V heads, head_dim], mass [layers, K/V heads, slots].
         Returns the numbers of the kept rows [layers, K/V heads, kept rows] if they are wanted."""
-        ks, cl, kp, os_ = _host_i32(kv_start), _host_i32(ctx_len), _host_i32(keep), _host_i32(out_start)
-        view, to = _kv_view(self.device, k, v), _kv_view(self.device, k_out, v_out)
-        lh = view.n_layers * view.n_kv_heads
-        if not len(ks) == len(cl) == len(kp) == len(os_):
+        ks, cl, kp, to_at = _host_call_i32(kv_start), _host_call_i32(ctx_len), _host_call_i32(keep), _host_call_i32(out_start)
+        view, slots, L, H, _ = _kv_view(self.device, k, v)
+        to, to_slots, _, _, _ = _kv_view(self.device, k_out, v_out)
+        if not len(ks) == len(cl) == len(kp) == len(to_at):
             raise ValueError("kv_start, ctx_len, keep and out_start must be of one length")
         _on(self.device, torch.float32, mass=mass, mass_out=mass_out)
-        if mass.numel() != lh * view.slots or (mass_out is not None and mass_out.numel() != lh * to.slots):
+        if mass.numel() != L * H * slots or (mass_out is not None and mass_out.numel() != L * H * to_slots):
             raise ValueError("mass or mass_out has the wrong size")
         rows = None
         if want_rows:
-            rows = torch.empty((view.n_layers, view.n_kv_heads, int(np.minimum(kp, cl).clip(0).sum())), dtype=torch.int32, device=self.device)
-        self._check(self._lib.kv_evict(self._h, C.byref(view), _ptr(mass), len(ks), ks.tobytes(), cl.tobytes(), kp.tobytes(), n_first, n_recent,
-                                       C.byref(to), os_.tobytes(), _ptr(mass_out), _ptr(rows)))
+            rows = torch.empty((L, H, int(np.minimum(kp, cl).clip(0).sum())), dtype=torch.int32, device=self.device)
+        self._check(self._lib.kv_evict(self._h, view, mass.data_ptr(), len(ks), _host_arg(ks), _host_arg(cl), _host_arg(kp), n_first, n_recent, to,
+                                       _host_arg(to_at), _ptr(mass_out), _ptr(rows)))
         return rows
 
     def kv_tensors(self, buf: Optional[torch.Tensor] = None, slots: int = 0):

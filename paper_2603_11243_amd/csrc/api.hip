@@ -1539,17 +1539,15 @@ void run_tree_attention(ssd_ctx* c, TreeWork& w, const TreePlan& p, char* ws, bo
     launch_tree_attention(a, in_args ? w.words.data() : nullptr, (int)w.words.size(), reinterpret_cast<const uint32_t*>(ws + p.words), c->stream);
 }
 
-struct PathPlan { size_t parent, meta_bytes; };
-PathPlan plan_path(int64_t nodes, int64_t utts) {
-    PathPlan p;
-    p.parent = align_up((size_t)(utts + 1) * 4);
-    p.meta_bytes = p.parent + align_up((size_t)nodes * 2);
-    return p;
-}
-void path_meta(const PathPlan& p, int B, const int32_t* cu_nodes, const int32_t* parent, uint32_t* meta) {
-    memcpy(meta, cu_nodes, (size_t)(B + 1) * 4);
-    int16_t* up = reinterpret_cast<int16_t*>(reinterpret_cast<char*>(meta) + p.parent);
-    for (int i = 0; i < cu_nodes[B]; ++i) up[i] = (int16_t)parent[i];
+// Words of a tree_path call: prefix sums, then parents in 16 bits.
+int64_t path_parents(int64_t utts) { return utts + 1; }
+int64_t path_words(int64_t nodes, int64_t utts) { return path_parents(utts) + (nodes + 1) / 2; }
+size_t path_bytes(int64_t nodes, int64_t utts) { return align_up((size_t)path_words(nodes, utts) * 4); }
+void path_meta(int B, const int32_t* cu_nodes, const int32_t* parent, uint32_t* words) {
+    memcpy(words, cu_nodes, (size_t)(B + 1) * 4);
+    int16_t* up = reinterpret_cast<int16_t*>(words + path_parents(B));
+    const int n = cu_nodes[B];
+    for (int i = 0; i < n; ++i) up[i] = (int16_t)parent[i];
 }
 float ln_of(float tau) { return tau > 0.f ? (float)log((double)tau) : -INFINITY; }
 
@@ -1623,7 +1621,7 @@ AcceptTreePlan plan_accept_tree(const ssd_model_cfg& c, int64_t N, int64_t rows,
     p.row = o; o = align_up(o + (size_t)rows * 4);
     p.target = o; o = align_up(o + (size_t)rows * 4);
     p.row_of = o; o = align_up(o + (size_t)N * 4);
-    p.path = o; o += plan_path(N, utts).meta_bytes;
+    p.path = o; o += path_bytes(N, utts);
     o = align_up(o + (size_t)utts * 8);                      // kv_start, ctx_len
     p.meta_bytes = o;
     p.h = o; o = align_up(o + (size_t)(rows * c.d_model) * elem_size(c.dtype));
@@ -1651,7 +1649,7 @@ int ssd_kv_cache_view(ssd_ctx* ctx, void* dev_ptr, int64_t slots, ssd_kv_view* v
 
 size_t ssd_tree_workspace_bytes(const ssd_ctx* ctx, int n_q_heads, int n_kv_heads, int head_dim, int64_t max_nodes, int64_t max_utts) {
     if (!ctx || n_q_heads < 0 || n_kv_heads < 0 || head_dim < 0 || max_nodes < 0 || max_utts < 0) return 0;
-    size_t need = plan_path(max_nodes, max_utts).meta_bytes;
+    size_t need = path_bytes(max_nodes, max_utts);
     if (n_kv_heads > 0) need = std::max(need, max_tree_bytes(n_q_heads, n_kv_heads, head_dim, max_nodes, max_utts));
     return need + 256;
 }
@@ -1701,18 +1699,28 @@ int tree_path(ssd_ctx* ctx, const float* node_logp, int B, const int32_t* cu_nod
     if (rc != SSD_OK) return rc;
     if (!accept_len || !accept_node || (cu_nodes[B] && (!node_logp || !path))) return fail(ctx, SSD_EINVAL, "tree_path: NULL data pointer");
     if (tau != tau) return fail(ctx, SSD_EINVAL, "tree_path: tau is NaN");
-    const PathPlan p = plan_path(cu_nodes[B], B);
-    if (!ctx->ws || ctx->ws_bytes < p.meta_bytes)
-        return fail(ctx, SSD_EWORKSPACE, "tree_path: workspace of %zu bytes needed, %zu set", p.meta_bytes, ctx->ws_bytes);
-    std::vector<uint32_t> meta(p.meta_bytes / 4);
-    path_meta(p, B, cu_nodes, parent, meta.data());
-    rc = place_meta(ctx, meta, ctx->ws);
-    if (rc != SSD_OK) return rc;
-    const char* ws = static_cast<const char*>(ctx->ws);
-    {
-        ProfScope ps(ctx, SSD_PROF_OTHER);
-        launch_tree_path(node_logp, reinterpret_cast<const int32_t*>(ws), reinterpret_cast<const int16_t*>(ws + p.parent), B, most, ln_of(tau), false,
-                         accept_len, accept_node, path, ctx->stream);
+    const size_t n_words = (size_t)path_words(cu_nodes[B], B), need = path_bytes(cu_nodes[B], B);
+    if (!ctx->ws || ctx->ws_bytes < need) return fail(ctx, SSD_EWORKSPACE, "tree_path: workspace of %zu bytes needed, %zu set", need, ctx->ws_bytes);
+    const TreePathArgs a{node_logp, B, most, (int)path_parents(B), ln_of(tau), false, accept_len, accept_node, path};
+    ProfScope ps(ctx, SSD_PROF_OTHER);
+    uint32_t few[MetaWords::WORDS];
+    if (n_words <= MetaWords::WORDS) {
+        path_meta(B, cu_nodes, parent, few);
+        launch_tree_path(a, few, (int)n_words, nullptr, ctx->stream);
+    } else {
+        if (capturing(ctx->stream)) {
+            std::vector<uint32_t> words(n_words);
+            path_meta(B, cu_nodes, parent, words.data());
+            rc = place_meta(ctx, words, ctx->ws);
+            if (rc != SSD_OK) return rc;
+        } else {                                             // straight into the staging buffer: a large batch's copies are what it waits for
+            int slot; void* staged;
+            HIP_TRY(ctx, ctx->stager.acquire(n_words * 4, slot, staged));
+            path_meta(B, cu_nodes, parent, static_cast<uint32_t*>(staged));
+            HIP_TRY(ctx, hipMemcpyAsync(ctx->ws, staged, n_words * 4, hipMemcpyHostToDevice, ctx->stream));
+            HIP_TRY(ctx, ctx->stager.commit(slot, ctx->stream));
+        }
+        launch_tree_path(a, nullptr, 0, static_cast<const uint32_t*>(ctx->ws), ctx->stream);
     }
     HIP_TRY(ctx, hipGetLastError());
     return SSD_OK;
@@ -1952,13 +1960,12 @@ int accept_tree(ssd_ctx* ctx, const void* h_tree, const int32_t* node_ids, int B
     const AcceptTreePlan p = plan_accept_tree(m, N, R, B);
     if (!ctx->ws || ctx->ws_bytes < p.total)
         return fail(ctx, SSD_EWORKSPACE, "accept_tree: workspace of %zu bytes needed, %zu set", p.total, ctx->ws_bytes);
-    const PathPlan pp = plan_path(N, B);
     std::vector<uint32_t> meta(p.meta_bytes / 4);
     memcpy(meta.data() + p.row / 4, row.data(), (size_t)R * 4);
     memcpy(meta.data() + p.target / 4, target.data(), (size_t)R * 4);
     memcpy(meta.data() + p.row_of / 4, row_of.data(), (size_t)N * 4);
-    path_meta(pp, B, cu_nodes, parent, meta.data() + p.path / 4);
-    const size_t places = p.path + pp.meta_bytes;
+    path_meta(B, cu_nodes, parent, meta.data() + p.path / 4);
+    const size_t places = p.path + path_bytes(N, B);
     if (kv_start) {
         memcpy(meta.data() + places / 4, kv_start, (size_t)B * 4);
         memcpy(meta.data() + places / 4 + B, ctx_len, (size_t)B * 4);
@@ -1974,7 +1981,7 @@ int accept_tree(ssd_ctx* ctx, const void* h_tree, const int32_t* node_ids, int B
     float* tgt = reinterpret_cast<float*>(ws + p.tgt);
     int2* part_arg = reinterpret_cast<int2*>(ws + p.part_arg);
     const int32_t* d_cu = reinterpret_cast<const int32_t*>(ws + p.path);
-    const int16_t* d_parent = reinterpret_cast<const int16_t*>(ws + p.path + pp.parent);
+    const int16_t* d_parent = reinterpret_cast<const int16_t*>(d_cu + path_parents(B));
     const int32_t* d_places = reinterpret_cast<const int32_t*>(ws + places);
     hipStream_t st = ctx->stream;
     ProfScope ps_all(ctx, SSD_PROF_LMHEAD);
@@ -1989,7 +1996,8 @@ int accept_tree(ssd_ctx* ctx, const void* h_tree, const int32_t* node_ids, int B
         launch_lmhead_finalize(part_ms, tgt, part_arg, head_groups(m), (int)R, logp, greedy, head_flags(ctx), st);
         launch_tree_scatter(logp, greedy, reinterpret_cast<const int32_t*>(ws + p.row_of), d_parent, (int)N, node_logp, greedy_tok, st);
     }
-    launch_tree_path(node_logp, d_cu, d_parent, B, most, ln_of(tau_slm), true, accept_len, accept_node, path, st);
+    launch_tree_path(TreePathArgs{node_logp, B, most, (int)path_parents(B), ln_of(tau_slm), true, accept_len, accept_node, path}, nullptr, 0,
+                     reinterpret_cast<const uint32_t*>(d_cu), st);
     if (kv_start && N) {
         const ssd_kv_view v = model_view(m, ctx->bf16_ops, ctx->kv, ctx->kv_slots);
         const int64_t unit = 16 / (int64_t)kv_elem(v.dtype);

@@ -48,9 +48,16 @@ constexpr int TREE_WORKGROUPS = 512;         // long contexts are cut into about
 constexpr int TREE_SPLIT_KEYS = 512;         // a piece has at least as many keys
 constexpr int TREE_MASS_KEYS = 128;          // and one of the weights a multiple of these
 
-// nodes of an utterance: cu[b] .. cu[b + 1] - 1 (at most MAX_TREE_NODES); parent: index inside the utterance or -1
-void launch_tree_path(const float* logp, const int32_t* cu, const int16_t* parent, int B, int most_nodes, float ln_tau, bool roots_given, int32_t* accept_len,
-                      int32_t* accept_node, int32_t* path, hipStream_t st);
+// Words: the B + 1 prefix sums of the nodes (at most MAX_TREE_NODES an utterance); from `parents` on the nodes' parents inside their utterance or -1, 16
+// bits each.  words: host memory, n of them, to travel as arguments; or NULL, then they are in dev_words.
+struct TreePathArgs {
+    const float* logp;
+    int B, most_nodes, parents;
+    float ln_tau;
+    bool roots_given;                        // nodes without a parent pass
+    int32_t* accept_len; int32_t* accept_node; int32_t* path;
+};
+void launch_tree_path(const TreePathArgs& a, const uint32_t* words, int n, const uint32_t* dev_words, hipStream_t st);
 
 // node_logp[i] = logp[i], 0 where parent[i] < 0; greedy_tok[i] = greedy[row_of[i]]
 void launch_tree_scatter(const float* logp, const int32_t* greedy, const int32_t* row_of, const int16_t* parent, int n, float* node_logp,

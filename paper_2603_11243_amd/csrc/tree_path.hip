@@ -1,5 +1,7 @@
 // Accepted path of a tree of drafted tokens (Eq. 5 and the definition of j, Sec. 2.3, for more than one continuation): a node stands if
 // its own likelihood and those of all its ancestors pass; the deepest node that stands wins, the lowest index among equally deep ones.
+#include <string.h>
+
 #include "device_utils.h"
 #include "tree.h"
 
@@ -7,15 +9,14 @@ namespace ssd {
 
 // One workgroup a tree, one thread a node (NT of them).  Pointer jumping: after round r a node knows whether the 2^r nodes on the way up
 // from it pass, how many there are, and who comes next.
-template <int NT>
-__global__ void __launch_bounds__(NT) tree_path_kernel(const float* __restrict__ logp, const int32_t* __restrict__ cu, const int16_t* __restrict__ parent,
-                                                       float ln_tau, bool roots_given, int32_t* __restrict__ accept_len,
+template <int NT, class M>
+__global__ void __launch_bounds__(NT) tree_path_kernel(const float* __restrict__ logp, M w, int parents, float ln_tau, bool roots_given, int32_t* __restrict__ accept_len,
                                                        int32_t* __restrict__ accept_node, int32_t* __restrict__ path) {
     __shared__ int up_s[NT], way_s[NT], best_s;              // way: nodes on the way, negative if one of them fails
-    const int i = threadIdx.x, node0 = cu[blockIdx.x], n = cu[blockIdx.x + 1] - node0;
+    const int i = threadIdx.x, node0 = (int)w(blockIdx.x), n = (int)w(blockIdx.x + 1) - node0;
     int up = -1, way = -1;
     if (i < n) {
-        up = parent[node0 + i];
+        up = (int16_t)(w(parents + (node0 + i) / 2) >> 16 * ((node0 + i) % 2));
         way = (up < 0 && roots_given) || logp[node0 + i] > ln_tau ? 1 : -0x10000;
         path[node0 + i] = -1;
     }
@@ -95,13 +96,21 @@ void launch_tree_commit(void* k, void* v, int64_t slot_stride, int64_t layer_str
                        mass, slots, kv_start, ctx_len, cu, accept_len, path);
 }
 
-void launch_tree_path(const float* logp, const int32_t* cu, const int16_t* parent, int B, int most_nodes, float ln_tau, bool roots_given, int32_t* accept_len,
-                      int32_t* accept_node, int32_t* path, hipStream_t st) {
-#define SSD_PATH(NT_) hipLaunchKernelGGL(tree_path_kernel<NT_>, dim3(B), dim3(NT_), 0, st, logp, cu, parent, ln_tau, roots_given, accept_len, accept_node, path)
-    if (most_nodes <= 64) SSD_PATH(64);
-    else if (most_nodes <= 256) SSD_PATH(256);
+template <class M>
+static void launch(const TreePathArgs& a, const M& w, hipStream_t st) {
+#define SSD_PATH(NT_) hipLaunchKernelGGL((tree_path_kernel<NT_, M>), dim3(a.B), dim3(NT_), 0, st, a.logp, w, a.parents, a.ln_tau, a.roots_given, a.accept_len, a.accept_node, a.path)
+    if (a.most_nodes <= 64) SSD_PATH(64);
+    else if (a.most_nodes <= 256) SSD_PATH(256);
     else SSD_PATH(MAX_TREE_NODES);
 #undef SSD_PATH
+}
+
+void launch_tree_path(const TreePathArgs& a, const uint32_t* words, int n, const uint32_t* dev_words, hipStream_t st) {
+    if (!words) { launch(a, MetaArray{dev_words}, st); return; }
+    MetaWords w;
+    w.n = n;
+    memcpy(w.word, words, (size_t)n * 4);
+    launch(a, w, st);
 }
 
 }  // namespace ssd

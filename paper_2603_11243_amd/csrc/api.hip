@@ -1391,9 +1391,9 @@ int check_trees(ssd_ctx* c, const char* what, int B, const int32_t* cu_nodes, co
         const int n = cu_nodes[b + 1] - cu_nodes[b];
         most = std::max(most, n);
         if (n > MAX_TREE_NODES) return fail(c, SSD_ESHAPE, "%s: utterance %d has %d nodes, at most %d", what, b, n, MAX_TREE_NODES);
-        int bad = 0;
-        for (int i = 0; i < n; ++i) bad |= (p[i] < -1) | (p[i] >= i);
-        if (bad) return fail(c, SSD_EINVAL, "%s: a parent of utterance %d is not a node before its child, nor -1", what, b);
+        uint32_t signs = 0;                                  // of p + 1 and i - 1 - p: additions, which the compiler takes four at a time
+        for (uint32_t i = 0; i < (uint32_t)n; ++i) signs |= ((uint32_t)p[i] + 1u) | (i - 1u - (uint32_t)p[i]);
+        if (signs >> 31) return fail(c, SSD_EINVAL, "%s: a parent of utterance %d is not a node before its child, nor -1", what, b);
     }
     return SSD_OK;
 }

@@ -1461,7 +1461,7 @@ void tree_work(int B, const int32_t* kv_start, const int32_t* ctx_len, const int
     auto step_of = [](int64_t keys, int64_t pieces, int64_t unit) { return std::max<int64_t>(1, (keys + pieces * unit - 1) / (pieces * unit)) * unit; };
     const int64_t pieces = std::max(1, TREE_WORKGROUPS / n_kv_heads);
     const int64_t step = std::min<int64_t>(std::max<int64_t>(TREE_SPLIT_KEYS, step_of(total, pieces, 256)), 0x7fffff00);
-    const int64_t mass_step = std::min<int64_t>(step_of(per_row, pieces, TREE_MASS_KEYS), 0x7fffff00);
+    const int64_t mass_step = std::min<int64_t>(step_of(per_row, 2 * pieces, TREE_MASS_KEYS), 0x7fffff00);
     std::vector<uint32_t>& v = w.words;
     TreeAttnArgs& a = w.a;
     v.reserve((size_t)B * 12 + cu_nodes[B] + 512);
@@ -1524,7 +1524,7 @@ TreePlan plan_tree(const TreeWork& w, int64_t nodes, bool own_lse) {
 size_t max_tree_bytes(int n_q_heads, int n_kv_heads, int head_dim, int64_t max_nodes, int64_t max_utts) {
     const int64_t G = (n_q_heads + n_kv_heads - 1) / n_kv_heads, cut = 2 * std::max(1, TREE_WORKGROUPS / n_kv_heads), rows = max_nodes * G;
     const int64_t tile = rows <= 16 ? 16 : rows <= 32 ? (TREE_KEY_ROWS < 32 ? 64 : 32) : rows <= 64 ? 64 : 128;
-    return plan_tree(3 * max_utts + 1 + 5 * (rows + cut) + 3 * rows + max_utts + cut + max_nodes, max_nodes * n_q_heads, cut * n_kv_heads * tile, head_dim).total;
+    return plan_tree(4 * max_utts + 1 + 5 * (rows + cut) + 3 * rows + cut + max_nodes, max_nodes * n_q_heads, cut * n_kv_heads * tile, head_dim).total;
 }
 void run_tree_attention(ssd_ctx* c, TreeWork& w, const TreePlan& p, char* ws, bool in_args, const void* k, const void* v, int64_t slots, const void* q, int64_t q_stride,
                         float scale, void* out, float* lse, float* mass) {

@@ -498,19 +498,20 @@ __global__ void __launch_bounds__(64 * MASS_WAVES, 2) tree_mass16_kernel(TreeAtt
     const int R = t.n_nodes * a.group, last = t.k1 - 1;
     const int stride2 = (int)a.slot_stride * 2;
     const uint16_t* kbase = (const uint16_t*)a.k + (int64_t)t.slot0 * a.slot_stride + kvh * a.head_stride;
-    u32x4_t kr[2][KS];
-    auto load_keys = [&](int k0) {
+    // two blocks of keys: the next one loads while one is used
+    u32x4_t kr[2][2][KS];
+    auto load_keys = [&](int k0, u32x4_t (&x)[2][KS]) __attribute__((always_inline)) {
         const int r0 = min(k0, last), beyond = last - r0;
         const __amdgpu_buffer_rsrc_t rsrc = make_rsrc(kbase + (int64_t)r0 * a.slot_stride);
 #pragma unroll
         for (int c = 0; c < 2; ++c) {
             const int off = min(16 * c + dc, beyond) * stride2 + kg * 16;
 #pragma unroll
-            for (int s = 0; s < KS; ++s) kr[c][s] = __builtin_amdgcn_raw_buffer_load_b128(rsrc, off + 64 * s, 0, 0);
+            for (int s = 0; s < KS; ++s) x[c][s] = __builtin_amdgcn_raw_buffer_load_b128(rsrc, off + 64 * s, 0, 0);
         }
     };
     const int first = t.k0 + wave * MASS_KEYS;
-    load_keys(first);
+    load_keys(first, kr[0]);
     if (t.k1 > t.n_ctx)
         for (int i = threadIdx.x; i < t.n_nodes; i += 64 * MASS_WAVES) span_s[i] = w(a.spans + t.node0 + i);
     const float sc = fabsf(a.scale) * LOG2E;
@@ -530,14 +531,14 @@ __global__ void __launch_bounds__(64 * MASS_WAVES, 2) tree_mass16_kernel(TreeAtt
             row_span[r] = r < rows ? w(a.spans + t.node0 + node_of(a, row)) : 0xffffu;
         }
         __syncthreads();
-        if (r0) load_keys(first);
-        for (int k0 = first; k0 < t.k1; k0 += STEP) {
+        if (r0) load_keys(first, kr[0]);
+        auto block = [&](auto masked_c, int k0, const u32x4_t (&x)[2][KS]) __attribute__((always_inline)) {
+            constexpr bool MASKED = decltype(masked_c)::value;
             f32x4_t acc[2];
 #pragma unroll
             for (int c = 0; c < 2; ++c) acc[c] = (f32x4_t){0.f, 0.f, 0.f, 0.f};
-            const bool masked = k0 + MASS_KEYS > t.n_ctx;
             uint32_t key[2][4];
-            if (masked) key_spans<2>(key, t, k0, span_s);
+            if constexpr (MASKED) key_spans<2>(key, t, k0, span_s);
             for (int n = 0; n < tiles; ++n) {
                 const int r = 16 * n + dc;
                 f32x4_t s[2];
@@ -547,21 +548,32 @@ __global__ void __launch_bounds__(64 * MASS_WAVES, 2) tree_mass16_kernel(TreeAtt
                 for (int e = 0; e < KS; ++e) {
                     const f16x8_t q = as_f16x8(*reinterpret_cast<const uint4*>(q_s + r * ROW + ((kg + 4 * e) ^ k_swizzle<HD>(r)) * 16));
 #pragma unroll
-                    for (int c = 0; c < 2; ++c) s[c] = mfma_16x16x32<BF>(__builtin_bit_cast(f16x8_t, kr[c][e]), q, s[c]);
+                    for (int c = 0; c < 2; ++c) s[c] = mfma_16x16x32<BF>(__builtin_bit_cast(f16x8_t, x[c][e]), q, s[c]);
                 }
                 const float base = lse_s[r];
-                const uint32_t mine = row_span[r];
+                const uint32_t mine = MASKED ? row_span[r] : 0u;
 #pragma unroll
                 for (int c = 0; c < 2; ++c)
 #pragma unroll
                     for (int e = 0; e < 4; ++e) {
                         const float p = __builtin_amdgcn_exp2f(fmaf(s[c][e], sc, base));
-                        acc[c][e] += masked && !sees(mine, key[c][e]) ? 0.f : p;
+                        acc[c][e] += MASKED && !sees(mine, key[c][e]) ? 0.f : p;
                     }
             }
-            load_keys(k0 + STEP);
             add_mass(a, t, kvh, k0, r0 == 0, acc);
-        }
+        };
+        auto step = [&](auto masked_c, int k0) __attribute__((always_inline)) {          // two blocks
+            load_keys(k0 + STEP, kr[1]);
+            __builtin_amdgcn_sched_barrier(0);
+            block(masked_c, k0, kr[0]);
+            __builtin_amdgcn_sched_barrier(0);
+            load_keys(k0 + 2 * STEP, kr[0]);
+            __builtin_amdgcn_sched_barrier(0);
+            if (k0 + STEP < t.k1) block(masked_c, k0 + STEP, kr[1]);
+        };
+        int k0 = first;
+        for (; k0 + STEP + MASS_KEYS <= min(t.n_ctx, t.k1); k0 += 2 * STEP) step(std::false_type(), k0);
+        for (; k0 < t.k1; k0 += 2 * STEP) step(std::true_type(), k0);
     }
 }
 

@@ -1412,10 +1412,12 @@ int check_places(ssd_ctx* c, const char* what, int B, const int32_t* kv_start, c
     return SSD_OK;
 }
 
-// Host metadata of a call to its place in the workspace: as arguments of a launch where they are few, and in pieces of that size under
-// capture (the staging buffers of an upload would be read again by every replay); else one upload.
+// Host metadata of a call to its place in the workspace: as arguments of launches where a few hold it, and in pieces of that size under
+// capture (the staging buffers of an upload would be read again by every replay); else one upload.  Between two kernels an upload takes 17 us (6 of them
+// the copy of 24 KB, the rest the way to the copy engine and back), a launch with words 2.5: 90 trees of 6500 words 77 us by upload, 80 by seven launches.
+constexpr size_t META_LAUNCHES = 5;
 int place_meta(ssd_ctx* c, const std::vector<uint32_t>& meta, void* dev) {
-    if (meta.size() > MetaWords::WORDS && !capturing(c->stream)) return upload(c, meta.data(), dev, meta.size() * 4);
+    if (meta.size() > META_LAUNCHES * MetaWords::WORDS && !capturing(c->stream)) return upload(c, meta.data(), dev, meta.size() * 4);
     for (size_t at = 0; at < meta.size(); at += MetaWords::WORDS) {
         MetaWords w;
         w.n = (int)std::min<size_t>(MetaWords::WORDS, meta.size() - at);

@@ -132,8 +132,8 @@ int ssd_device_flags(ssd_ctx *ctx, int32_t *flags /*host*/);
  * discards earlier samples.  ssd_profile_read waits for the stream, writes per class the summed
  * device time in milliseconds and the number of bracketed launches since the last select/read
  * (arrays of SSD_PROF_N_CLASSES entries, host memory), and clears the samples.  A span covers one
- * kernel launch, except SSD_PROF_GATE (the one or two gate kernels of a call) and SSD_PROF_LMHEAD (LM head,
- * merge of partials and prefix scan). */
+ * kernel launch, except SSD_PROF_GATE (the one or two gate kernels of a call), SSD_PROF_LMHEAD (LM head,
+ * merge of partials and prefix scan; a whole accept_tree), SSD_PROF_ATTN for tree_attention (up to three) and SSD_PROF_OTHER for kv_evict. */
 enum ssd_prof_class {
     SSD_PROF_OFF = -2, SSD_PROF_ALL = -1,
     SSD_PROF_GATE = 0, SSD_PROF_GEMM_QKV = 1, SSD_PROF_ATTN = 2, SSD_PROF_GEMM_O = 3,
@@ -364,7 +364,7 @@ int accept_prefix(ssd_ctx *ctx, const void *h_verify, const int32_t *draft_ids /
  *
  * The rows of a cache, the library's own (ssd_kv_cache_view) or any other: row `slot` of K/V head h of layer l begins at element
  * l * layer_stride + slot * slot_stride + h * head_stride of k and of v, and its head_dim elements are consecutive.  Rows must not share
- * memory, every row begins at a multiple of 16 bytes, 64 slots are less than 2 GiB apart.  slots <= 2^31 - 1.
+ * memory, every row begins at a multiple of 16 bytes, 64 slots are less than 2 GiB apart.  slots <= 2^30.
  * dtype SSD_F16 or SSD_BF16: head_dim 64 or 128; SSD_F32: a multiple of 4 up to 128 (SSD_ESHAPE otherwise). */
 #define SSD_MAX_TREE_NODES 1024
 typedef struct {
@@ -385,7 +385,7 @@ size_t ssd_tree_workspace_bytes(const ssd_ctx *ctx, int n_q_heads, int n_kv_head
 /* Attention of all nodes (Eq. 4 for the nodes of a tree).  Per node i and query head h (its K/V head is h / (n_q_heads / n_kv_heads)), over
  * the rows j that the node sees:  s_j = scale q . k_j;  lse = log sum_j exp s_j;  out = sum_j exp(s_j - lse) v_j.
  *   q      dev, row cu_nodes[b] + i begins at element (cu_nodes[b] + i) * q_stride: n_q_heads * head_dim elements of the cache's type
- *          (q and q_stride multiples of 16 bytes)
+ *          (q and q_stride multiples of 16 bytes); must not overlap out
  *   kv     one layer (n_layers 1)
  *   out    dev [cu_nodes[B], n_q_heads * head_dim], the cache's type, 16-byte aligned
  *   lse    dev [cu_nodes[B], n_q_heads] fp32, or NULL
@@ -394,7 +394,9 @@ size_t ssd_tree_workspace_bytes(const ssd_ctx *ctx, int n_q_heads, int n_kv_head
  *          entry is touched.  The slots of different utterances must then be distinct.
  * Scores, sums and statistics are fp32; with 16-bit caches the weights that enter the second product are rounded to the cache's type.
  * A row that a node does not see has no influence on it, whatever it holds.  An utterance without nodes is skipped, ctx_len may be 0.
- * Calls under stream capture may be replayed.  Errors: SSD_EINVAL, SSD_ESHAPE, SSD_EUNSUPPORTED (dtype), SSD_EWORKSPACE. */
+ * Calls of this section may be captured: replays read the arrays of the captured call, not later ones, and use its workspace, so that two of them
+ * that share a workspace must not run at the same time.  Errors: SSD_EINVAL, SSD_ESHAPE (more than 65535 utterances, or tiles of 16, 64 or 128
+ * query rows of a K/V head, in all; more than 512 query heads a K/V head), SSD_EUNSUPPORTED (dtype), SSD_EWORKSPACE. */
 int tree_attention(ssd_ctx *ctx, const void *q /*dev*/, int64_t q_stride, int n_q_heads, const ssd_kv_view *kv /*host*/, int B,
                    const int32_t *kv_start /*host [B]*/, const int32_t *ctx_len /*host [B]*/, const int32_t *cu_nodes /*host [B+1]*/,
                    const int32_t *parent /*host [cu_nodes[B]]*/, float scale, void *out, float *lse, float *mass);
@@ -416,7 +418,7 @@ int tree_path(ssd_ctx *ctx, const float *node_logp /*dev [cu_nodes[B]]*/, int B,
  *   mass_out  dev [n_layers, n_kv_heads, to->slots] or NULL: the kept rows' entries, moved with them
  *   rows_out  dev int32 [n_layers, n_kv_heads, sum of kept rows] or NULL: numbers of the kept rows inside their utterance, utterances one
  *             behind the other
- * from and to must agree but for slots and strides and must not overlap in memory; the slots written for different utterances must be
+ * from and to must agree but for slots and strides, and the memory from the first to the last row of the one must not meet the other's; the slots written for different utterances must be
  * distinct.  Entries and rows behind an utterance's kept ones are left as they were.
  * Errors: SSD_EINVAL (keep[b] < n_first + n_recent where rows go, ...), SSD_ESHAPE (a context of more than 8192 rows in a call of more than 3.6
  * million), SSD_EUNSUPPORTED, SSD_EWORKSPACE. */

@@ -1343,8 +1343,8 @@ size_t kv_elem(int dtype) { return dtype == SSD_F32 ? 4 : 2; }
 int check_view(ssd_ctx* c, const char* what, const ssd_kv_view* v) {
     if (!v || !v->k || !v->v) return fail(c, SSD_EINVAL, "%s: NULL cache", what);
     if (v->dtype != SSD_F32 && v->dtype != SSD_BF16 && v->dtype != SSD_F16) return fail(c, SSD_EUNSUPPORTED, "%s: dtype %d", what, v->dtype);
-    if (v->slots <= 0 || v->slots > 0x7fffffff || v->n_layers <= 0 || v->n_kv_heads <= 0 || v->head_dim <= 0)
-        return fail(c, SSD_EINVAL, "%s: non-positive size of a cache, or more than 2^31 - 1 slots", what);
+    if (v->slots <= 0 || v->slots > 1 << 30 || v->n_layers <= 0 || v->n_kv_heads <= 0 || v->head_dim <= 0)
+        return fail(c, SSD_EINVAL, "%s: non-positive size of a cache, or more than 2^30 slots", what);
     if (v->n_kv_heads > 65535 || (int64_t)v->n_layers * v->n_kv_heads > 65535) return fail(c, SSD_ESHAPE, "%s: more than 65535 layers times K/V heads", what);
     const bool f32 = v->dtype == SSD_F32;
     if (f32 ? v->head_dim % 4 || v->head_dim > 128 : v->head_dim != 64 && v->head_dim != 128)
@@ -1354,7 +1354,7 @@ int check_view(ssd_ctx* c, const char* what, const ssd_kv_view* v) {
     if (((uintptr_t)v->k | (uintptr_t)v->v) & 15 || ss % unit || hs % unit || ls % unit)
         return fail(c, SSD_EINVAL, "%s: rows of a cache must begin at multiples of 16 bytes", what);
     // slots inside a head or heads inside a slot; then layers
-    const int64_t top = (int64_t)1 << 46;
+    const int64_t top = (int64_t)1 << 42;                    // (no product below leaves 64 bits)
     if (ss < hd || ss > top || hs > top || ls > top || (H > 1 && hs < hd)) return fail(c, SSD_EINVAL, "%s: strides of a cache", what);
     const bool heads_inside = H == 1 || hs * (H - 1) + hd <= ss;
     if (!heads_inside && hs / ss < v->slots - 1) return fail(c, SSD_EINVAL, "%s: rows of a cache share memory", what);
@@ -1412,19 +1412,38 @@ int check_places(ssd_ctx* c, const char* what, int B, const int32_t* kv_start, c
     return SSD_OK;
 }
 
-// Host metadata of a call to its place in the workspace: as arguments of launches where a few hold it, and in pieces of that size under
-// capture (the staging buffers of an upload would be read again by every replay); else one upload.  Between two kernels an upload takes 17 us (6 of them
-// the copy of 24 KB, the rest the way to the copy engine and back), a launch with words 2.5: 90 trees of 6500 words 77 us by upload, 80 by seven launches.
-constexpr size_t META_LAUNCHES = 5;
-int place_meta(ssd_ctx* c, const std::vector<uint32_t>& meta, void* dev) {
-    if (meta.size() > META_LAUNCHES * MetaWords::WORDS && !capturing(c->stream)) return upload(c, meta.data(), dev, meta.size() * 4);
-    for (size_t at = 0; at < meta.size(); at += MetaWords::WORDS) {
+// Host metadata of a call, n words that fill(words) writes, to its place in the workspace: as arguments of a launch where it holds them, and in pieces of that size
+// under capture (a staging buffer would be read again by every replay); else from a pinned staging buffer by a kernel that reads it over the
+// bus.  Between two kernels the copy engine takes 17 us for 24 KB (6 of them the copy, the rest the way there and back); see the kernel for its time.
+template <class F>
+int place_words(ssd_ctx* c, size_t n, void* dev, const F& fill) {
+    if (n <= MetaWords::WORDS) {
         MetaWords w;
-        w.n = (int)std::min<size_t>(MetaWords::WORDS, meta.size() - at);
-        memcpy(w.word, meta.data() + at, (size_t)w.n * 4);
+        w.n = (int)n;
+        fill(w.word);
+        launch_write_words(w, static_cast<uint32_t*>(dev), c->stream);
+        return SSD_OK;
+    }
+    if (!capturing(c->stream)) {
+        int slot; void* staged;
+        HIP_TRY(c, c->stager.acquire(n * 4, slot, staged));
+        fill(static_cast<uint32_t*>(staged));
+        launch_copy_words(static_cast<const uint32_t*>(staged), n, static_cast<uint32_t*>(dev), c->stream);
+        HIP_TRY(c, c->stager.commit(slot, c->stream));
+        return SSD_OK;
+    }
+    std::vector<uint32_t> words(n);
+    fill(words.data());
+    for (size_t at = 0; at < n; at += MetaWords::WORDS) {
+        MetaWords w;
+        w.n = (int)std::min<size_t>(MetaWords::WORDS, n - at);
+        memcpy(w.word, words.data() + at, (size_t)w.n * 4);
         launch_write_words(w, static_cast<uint32_t*>(dev) + at, c->stream);
     }
     return SSD_OK;
+}
+int place_meta(ssd_ctx* c, const std::vector<uint32_t>& meta, void* dev) {
+    return place_words(c, meta.size(), dev, [&](uint32_t* words) { memcpy(words, meta.data(), meta.size() * 4); });
 }
 
 // What a tree_attention call does: the arguments of its launches but for pointers, and the words they read.
@@ -1671,8 +1690,10 @@ int tree_attention(ssd_ctx* ctx, const void* q, int64_t q_stride, int n_q_heads,
     if (!std::isfinite(scale)) return fail(ctx, SSD_EINVAL, "tree_attention: scale is not finite");
     if (N == 0) return SSD_OK;
     if (!q || !out) return fail(ctx, SSD_EINVAL, "tree_attention: NULL data pointer");
-    if (q_stride < dq || q_stride > (int64_t)1 << 40 || q_stride * es % 16 || ((uintptr_t)q | (uintptr_t)out) & 15)
+    if (q_stride < dq || q_stride > (int64_t)1 << 32 || q_stride * es % 16 || ((uintptr_t)q | (uintptr_t)out) & 15)
         return fail(ctx, SSD_EINVAL, "tree_attention: rows of q and out must begin at multiples of 16 bytes, q_stride be at least n_q_heads * head_dim");
+    if (overlap(Extent{(uintptr_t)q, (uintptr_t)q + (uintptr_t)(((N - 1) * q_stride + dq) * es)}, Extent{(uintptr_t)out, (uintptr_t)out + (uintptr_t)(N * dq * es)}))
+        return fail(ctx, SSD_EINVAL, "tree_attention: q and out overlap in memory");
     TreeWork w;
     tree_work(B, kv_start, ctx_len, cu_nodes, parent, most, n_q_heads, *kv, mass != nullptr, w);
     if (w.a.n_items > 65535 || w.a.n_mass > 65535) return fail(ctx, SSD_ESHAPE, "tree_attention: more than 65535 tiles of query rows; split the batch");
@@ -1710,18 +1731,8 @@ int tree_path(ssd_ctx* ctx, const float* node_logp, int B, const int32_t* cu_nod
         path_meta(B, cu_nodes, parent, few);
         launch_tree_path(a, few, (int)n_words, nullptr, ctx->stream);
     } else {
-        if (capturing(ctx->stream)) {
-            std::vector<uint32_t> words(n_words);
-            path_meta(B, cu_nodes, parent, words.data());
-            rc = place_meta(ctx, words, ctx->ws);
-            if (rc != SSD_OK) return rc;
-        } else {                                             // straight into the staging buffer: a large batch's copies are what it waits for
-            int slot; void* staged;
-            HIP_TRY(ctx, ctx->stager.acquire(n_words * 4, slot, staged));
-            path_meta(B, cu_nodes, parent, static_cast<uint32_t*>(staged));
-            HIP_TRY(ctx, hipMemcpyAsync(ctx->ws, staged, n_words * 4, hipMemcpyHostToDevice, ctx->stream));
-            HIP_TRY(ctx, ctx->stager.commit(slot, ctx->stream));
-        }
+        rc = place_words(ctx, n_words, ctx->ws, [&](uint32_t* words) { path_meta(B, cu_nodes, parent, words); });
+        if (rc != SSD_OK) return rc;
         launch_tree_path(a, nullptr, 0, static_cast<const uint32_t*>(ctx->ws), ctx->stream);
     }
     HIP_TRY(ctx, hipGetLastError());
@@ -1749,6 +1760,7 @@ int kv_evict(ssd_ctx* ctx, const ssd_kv_view* from, const float* mass, int B, co
     const Extent a[2] = {extent_of(*from, from->k), extent_of(*from, from->v)}, z[2] = {extent_of(*to, to->k), extent_of(*to, to->v)};
     if (overlap(a[0], z[0]) || overlap(a[0], z[1]) || overlap(a[1], z[0]) || overlap(a[1], z[1]))
         return fail(ctx, SSD_EINVAL, "kv_evict: the caches overlap in memory");
+    if (to->k == to->v) return fail(ctx, SSD_EINVAL, "kv_evict: keys and values of the other cache share memory");
     const int64_t lh = (int64_t)from->n_layers * from->n_kv_heads;
     if (mass_out && overlap(Extent{(uintptr_t)mass, (uintptr_t)mass + (uintptr_t)(lh * from->slots * 4)},
                             Extent{(uintptr_t)mass_out, (uintptr_t)mass_out + (uintptr_t)(lh * to->slots * 4)}))

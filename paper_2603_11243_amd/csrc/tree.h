@@ -21,6 +21,8 @@ struct MetaArray {
     __device__ __forceinline__ uint32_t operator()(int i) const { return word[i]; }
 };
 void launch_write_words(const MetaWords& w, uint32_t* dst, hipStream_t st);
+// n words of pinned host memory to dst (16-byte aligned both)
+void launch_copy_words(const uint32_t* host, size_t n, uint32_t* dst, hipStream_t st);
 
 // Attention of nodes.  Query rows of one K/V head are numbered node * G + head of the group; keys are the rows of the utterance, n_ctx cached ones, then
 // the nodes.  The words: per item of work five, at a place known without another: first slot, n_ctx, first node, nodes | tile of tile_rows query rows << 11,

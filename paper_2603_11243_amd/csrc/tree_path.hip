@@ -55,6 +55,22 @@ void launch_write_words(const MetaWords& w, uint32_t* dst, hipStream_t st) {
     hipLaunchKernelGGL(write_words_kernel, dim3(1), dim3(256), 0, st, w, dst);
 }
 
+// All loads of a thread are requested before the first is used: one way over the bus.
+constexpr int COPY_UNITS = 4;                // of 16 bytes a thread
+__global__ void __launch_bounds__(256) copy_words_kernel(const uint4* __restrict__ host, int units, uint4* __restrict__ dst) {
+    const int at = (int)blockIdx.x * 256 * COPY_UNITS + threadIdx.x;
+    uint4 x[COPY_UNITS];
+#pragma unroll
+    for (int u = 0; u < COPY_UNITS; ++u) x[u] = host[min(at + u * 256, units - 1)];
+#pragma unroll
+    for (int u = 0; u < COPY_UNITS; ++u)
+        if (at + u * 256 < units) dst[at + u * 256] = x[u];
+}
+void launch_copy_words(const uint32_t* host, size_t n, uint32_t* dst, hipStream_t st) {
+    const int units = (int)((n + 3) / 4);                    // (both ends are allocated in larger units)
+    hipLaunchKernelGGL(copy_words_kernel, dim3((units + 256 * COPY_UNITS - 1) / (256 * COPY_UNITS)), dim3(256), 0, st, (const uint4*)host, units, (uint4*)dst);
+}
+
 __global__ void __launch_bounds__(256) tree_scatter_kernel(const float* __restrict__ logp, const int32_t* __restrict__ greedy, const int32_t* __restrict__ row_of,
                                                           const int16_t* __restrict__ parent, int n, float* __restrict__ node_logp,
                                                           int32_t* __restrict__ greedy_tok) {
@@ -68,26 +84,31 @@ void launch_tree_scatter(const float* logp, const int32_t* greedy, const int32_t
     hipLaunchKernelGGL(tree_scatter_kernel, dim3((n + 255) / 256), dim3(256), 0, st, logp, greedy, row_of, parent, n, node_logp, greedy_tok);
 }
 
-// One thread a 16-byte column of an utterance's rows in a layer.  Step d moves row path[d] >= d, so that in the order of d no row is
-// written that this thread still reads, and no other thread touches the column.
+// One thread a 16-byte column of an utterance's rows in a layer.  Step d moves row path[d] >= d to d, and path[d + 1] > path[d]: no row is written that a later step
+// reads, whatever the order of loads and stores, and no other thread touches the column.  Eight rows are requested at once.
+template <typename T>
+__device__ __forceinline__ void move_rows(T* col, int64_t stride, const int32_t* from, int n) {
+    for (int d0 = 0; d0 < n; d0 += 8) {
+        T x[8];
+#pragma unroll
+        for (int d = 0; d < 8; ++d) x[d] = col[from[min(d0 + d, n - 1)] * stride];
+#pragma unroll
+        for (int d = 0; d < 8; ++d)
+            if (d0 + d < n) col[(d0 + d) * stride] = x[d];
+    }
+}
+
 __global__ void __launch_bounds__(256) tree_commit_kernel(uint4* __restrict__ k, uint4* __restrict__ v, int64_t slot_stride, int64_t layer_stride, int n_kv_heads,
                                                          int cols, float* __restrict__ mass, int64_t slots, const int32_t* __restrict__ kv_start,
                                                          const int32_t* __restrict__ ctx_len, const int32_t* __restrict__ cu,
                                                          const int32_t* __restrict__ accept_len, const int32_t* __restrict__ path) {
     const int b = blockIdx.x, layer = blockIdx.y, n = accept_len[b];
     const int32_t* from = path + cu[b];
+    if (n <= 0 || from[n - 1] == n - 1) return;              // (a path of the first nodes is in its place)
     const int64_t slot0 = (int64_t)kv_start[b] + ctx_len[b], base = layer * layer_stride + slot0 * slot_stride;
-    for (int c = threadIdx.x; c < 2 * cols; c += 256) {
-        uint4* col = (c < cols ? k : v) + base + c % cols;
-        for (int d = 0; d < n; ++d)
-            if (from[d] != d) col[d * slot_stride] = col[from[d] * slot_stride];
-    }
+    for (int c = threadIdx.x; c < 2 * cols; c += 256) move_rows((c < cols ? k : v) + base + c % cols, slot_stride, from, n);
     if (mass)
-        for (int h = threadIdx.x; h < n_kv_heads; h += 256) {
-            float* col = mass + ((int64_t)layer * n_kv_heads + h) * slots + slot0;
-            for (int d = 0; d < n; ++d)
-                if (from[d] != d) col[d] = col[from[d]];
-        }
+        for (int h = threadIdx.x; h < n_kv_heads; h += 256) move_rows(mass + ((int64_t)layer * n_kv_heads + h) * slots + slot0, 1, from, n);
 }
 void launch_tree_commit(void* k, void* v, int64_t slot_stride, int64_t layer_stride, int n_layers, int n_kv_heads, int row_chunks, float* mass, int64_t slots,
                         const int32_t* kv_start, const int32_t* ctx_len, const int32_t* cu, const int32_t* accept_len, const int32_t* path, int B,

@@ -40,7 +40,10 @@ P = C.c_void_p(1 << 20)
 p = lambda a: None if a is None else a.ctypes.data
 
 
-def attention(lib, ctx, kv=None, q=P, q_stride=512, hq=4, B=2, start=i32([0, 50]), n=i32([20, 30]), cu=i32([0, 3, 5]), parent=i32([-1, 0, 0, -1, -1]), scale=0.1,
+Q = C.c_void_p(1 << 24)
+
+
+def attention(lib, ctx, kv=None, q=Q, q_stride=512, hq=4, B=2, start=i32([0, 50]), n=i32([20, 30]), cu=i32([0, 3, 5]), parent=i32([-1, 0, 0, -1, -1]), scale=0.1,
               out=P, lse=None, mass=None):
     return lib.tree_attention(ctx, q, q_stride, hq, C.byref(view() if kv is None else kv), B, p(start), p(n), p(cu), p(parent), C.c_float(scale), out, lse, mass)
 
@@ -65,6 +68,8 @@ def test_attention(lib, ctx):
     assert call(hq=3) == ESHAPE and call(hq=0) == ESHAPE
     assert call(q_stride=511) == EINVAL and call(q_stride=516) == EINVAL and call(q=C.c_void_p(8)) == EINVAL and call(out=C.c_void_p(8)) == EINVAL
     assert call(kv=view(L=2, ls=25600)) == EINVAL
+    near = lambda n: C.c_void_p((1 << 24) + n)
+    assert call(out=near(0)) == EINVAL and call(out=near(5120 - 16)) == EINVAL and call(out=near(5120)) == EWORKSPACE and call(out=near(-5120 + 16)) == EINVAL
     many = i32(np.arange(1025) - 1)
     assert call(B=1, cu=i32([0, 1025]), parent=many, kv=view(slots=5000), n=i32([20])) == ESHAPE
     assert call(B=1, cu=i32([0, 1024]), parent=many, kv=view(slots=5000), n=i32([20])) == EWORKSPACE
@@ -77,7 +82,7 @@ def test_views(lib, ctx):
     for good in ({}, {"hd": 64, "hs": 64}, {"dtype": BF16}, {"dtype": F32, "hd": 36, "hs": 36, "ss": 72}, {"ss": 128, "hs": 12800}, {"ss": 128, "hs": 20000},
                  {"H": 1, "ss": 128, "hs": 0}):
         assert call(**good) == EWORKSPACE, (good, lib.ssd_last_error(ctx))
-    for bad in ({"k": 0}, {"v": 0}, {"k": 8}, {"v": 24}, {"slots": 0}, {"slots": 1 << 31}, {"H": 0}, {"hd": 0}, {"L": 0}, {"ss": 264, "hs": 132}, {"ss": 260},
+    for bad in ({"k": 0}, {"v": 0}, {"k": 8}, {"v": 24}, {"slots": 0}, {"slots": (1 << 30) + 1}, {"slots": 1 << 31}, {"H": 0}, {"hd": 0}, {"L": 0}, {"ss": 264, "hs": 132}, {"ss": 260},
                 {"ss": 192}, {"hs": 64}, {"hs": -128}, {"ss": -256}, {"ss": 0}, {"ss": 128, "hs": 12792}, {"ss": 128, "hs": 256}):
         assert call(**bad) == EINVAL, bad
     assert call(dtype=3) == EUNSUPPORTED
@@ -108,7 +113,7 @@ def test_evict(lib, ctx):
     assert call(keep=i32([10, 20]), first=1 << 30, recent=1 << 30) == EINVAL
     assert call(keep=i32([40, 30]), first=99, recent=99, to=view(base=far, slots=70), out=i32([0, 40])) == EWORKSPACE      # nothing goes
     for to in (view(base=far, hd=64, hs=64, slots=30), view(base=far, dtype=BF16, slots=30), view(base=far, H=1, slots=30), view(base=far, L=2, ls=7680, slots=30),
-               view(slots=30), view(base=far, slots=30, v=(1 << 40) + 100 * 512 - 16), view(base=far, slots=30, k=(1 << 40) + (1 << 30) - 30 * 512 + 16)):
+               view(base=far, slots=30, v=far), view(slots=30), view(base=far, slots=30, v=(1 << 40) + 100 * 512 - 16), view(base=far, slots=30, k=(1 << 40) + (1 << 30) - 30 * 512 + 16)):
         assert call(to=to) == EINVAL
     assert call(mass=P, mass_out=C.c_void_p((1 << 20) + 796)) == EINVAL and call(mass=P, mass_out=C.c_void_p((1 << 20) + 800)) == EWORKSPACE
     assert call(keep=i32([0, 0]), first=0, recent=0) == 0                        # nothing stays: nothing to copy

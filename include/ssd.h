@@ -421,7 +421,7 @@ int tree_path(ssd_ctx *ctx, const float *node_logp /*dev [cu_nodes[B]]*/, int B,
  * from and to must agree but for slots and strides, and the memory from the first to the last row of the one must not meet the other's; the slots written for different utterances must be
  * distinct.  Entries and rows behind an utterance's kept ones are left as they were.
  * Errors: SSD_EINVAL (keep[b] < n_first + n_recent where rows go, ...), SSD_ESHAPE (a context of more than 8192 rows in a call of more than 3.6
- * million), SSD_EUNSUPPORTED, SSD_EWORKSPACE. */
+ * million, 2^24 kept rows, more than 65535 utterances), SSD_EUNSUPPORTED, SSD_EWORKSPACE. */
 size_t ssd_evict_workspace_bytes(const ssd_ctx *ctx, int n_layers, int n_kv_heads, int64_t max_kept_rows, int64_t max_utts);
 int kv_evict(ssd_ctx *ctx, const ssd_kv_view *from /*host*/, const float *mass, int B, const int32_t *kv_start /*host [B]*/,
              const int32_t *ctx_len /*host [B]*/, const int32_t *keep /*host [B]*/, int n_first, int n_recent, const ssd_kv_view *to /*host*/,

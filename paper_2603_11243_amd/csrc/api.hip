@@ -1465,9 +1465,10 @@ void tree_spans(int n, const int32_t* parent, uint32_t* span) {
         span[i] = (uint32_t)at | (uint32_t)(at + size[i]) << 16;
     }
 }
-// Query rows of an item of work: as many as the largest tree has, in one of the shapes of the kernels.  Up to TREE_KEY_ROWS rows the wavefronts of a workgroup
-// split the keys; fp32 has no other kernel.
-int tree_tile_rows(int dtype, int rows) { return rows <= 16 ? 16 : dtype == SSD_F32 || rows <= TREE_KEY_ROWS ? 32 : rows <= 64 ? 64 : 128; }
+// Query rows of an item of work: as many as the largest tree has, in one of the shapes of the kernels.  With 16 (fp32: 32) the wavefronts of a workgroup split the
+// keys; with 64 and 128 they split the rows and share the keys, which takes 32 rows over 300 keys in 13.6 us where a split of the keys takes 18.0.
+// 128 rows read the keys half as often: 90 utterances of 42 nodes, 24 heads on 8, over 1024 rows 113 us, with 64 rows 133 (64 nodes over 64 rows: 62.6 and 61.9).
+int tree_tile_rows(int dtype, int rows) { return rows <= 16 ? 16 : dtype == SSD_F32 ? 32 : rows <= 64 ? 64 : 128; }
 // Ranges of keys: one per item, unless that leaves most of the chip without work or an utterance is longer than its share; then pieces of such a share.
 void tree_work(int B, const int32_t* kv_start, const int32_t* ctx_len, const int32_t* cu_nodes, const int32_t* parent, int most, int n_q_heads, const ssd_kv_view& kv,
                bool mass, TreeWork& w) {
@@ -1544,7 +1545,7 @@ TreePlan plan_tree(const TreeWork& w, int64_t nodes, bool own_lse) {
 // cut only where its keys, times its tiles, are more than one of TREE_WORKGROUPS / n_kv_heads shares, so that there are at most twice as many pieces.
 size_t max_tree_bytes(int n_q_heads, int n_kv_heads, int head_dim, int64_t max_nodes, int64_t max_utts) {
     const int64_t G = (n_q_heads + n_kv_heads - 1) / n_kv_heads, cut = 2 * std::max(1, TREE_WORKGROUPS / n_kv_heads), rows = max_nodes * G;
-    const int64_t tile = rows <= 16 ? 16 : rows <= 32 ? (TREE_KEY_ROWS < 32 ? 64 : 32) : rows <= 64 ? 64 : 128;
+    const int64_t tile = rows <= 16 ? 16 : rows <= 64 ? 64 : 128;
     return plan_tree(4 * max_utts + 1 + 5 * (rows + cut) + 3 * rows + cut + max_nodes, max_nodes * n_q_heads, cut * n_kv_heads * tile, head_dim).total;
 }
 void run_tree_attention(ssd_ctx* c, TreeWork& w, const TreePlan& p, char* ws, bool in_args, const void* k, const void* v, int64_t slots, const void* q, int64_t q_stride,
@@ -1755,6 +1756,7 @@ int kv_evict(ssd_ctx* ctx, const ssd_kv_view* from, const float* mass, int B, co
         return fail(ctx, SSD_EINVAL, "kv_evict: the caches differ in layers, heads, head_dim or dtype");
     if (!mass || !keep || !out_start) return fail(ctx, SSD_EINVAL, "kv_evict: NULL argument");
     if (B <= 0 || n_first < 0 || n_recent < 0) return fail(ctx, SSD_EINVAL, "kv_evict: B must be positive, n_first and n_recent not negative");
+    if (B > 65535) return fail(ctx, SSD_ESHAPE, "kv_evict: more than 65535 utterances; split the batch");
     rc = check_places(ctx, "kv_evict", B, kv_start, ctx_len, nullptr, from->slots, false);
     if (rc != SSD_OK) return rc;
     const Extent a[2] = {extent_of(*from, from->k), extent_of(*from, from->v)}, z[2] = {extent_of(*to, to->k), extent_of(*to, to->v)};
@@ -1778,7 +1780,7 @@ int kv_evict(ssd_ctx* ctx, const ssd_kv_view* from, const float* mass, int B, co
         len[b] = k;
         kept += k;
     }
-    if (kept > 0x7fffffff) return fail(ctx, SSD_ESHAPE, "kv_evict: more than 2^31 - 1 rows are kept; split the batch");
+    if (kept >= 1 << 24) return fail(ctx, SSD_ESHAPE, "kv_evict: 2^24 rows or more are kept; split the batch");      // (a workgroup of 256 each, 2^32 in all)
     if (!ranges_distinct(B, out_start, len)) return fail(ctx, SSD_EINVAL, "kv_evict: utterances share slots of the other cache");
     if (!kept) return SSD_OK;
     EvictArgs e;

@@ -241,12 +241,12 @@ __device__ __forceinline__ void lds_barrier() {
     asm volatile("" ::: "memory");
 }
 
-// ---- few query rows: 16 NT of a K/V head a workgroup, whose wavefronts take the 32-key blocks of the range in turn, so that every cached row is read once,
+// ---- few query rows: 16 of a K/V head a workgroup, whose wavefronts take the 32-key blocks of the range in turn, so that every cached row is read once,
 // and merge their (maximum, sum, output) through LDS.  Key rows come straight from memory in operand registers; a wavefront's values are its own
 // and need no barrier.
-template <bool BF, int HD, int NT, class M>
+template <bool BF, int HD, class M>
 __global__ void __launch_bounds__(64 * KEY_WAVES, 2) tree_keys16_kernel(TreeAttnArgs a, M w) {
-    constexpr int KEYS = 32, ROW = HD * 2, BLOCK = KEYS * ROW, STEP = KEYS * KEY_WAVES;
+    constexpr int NT = 1, KEYS = 32, ROW = HD * 2, BLOCK = KEYS * ROW, STEP = KEYS * KEY_WAVES;
     constexpr int KS = HD / 32, DT = HD / 16, TR = 16 * NT;
     constexpr int ROW_CHUNKS = ROW / 16, V_ROWS = 64 / ROW_CHUNKS, V_LOADS = KEYS / V_ROWS, K_LOADS = 2 * KS;
     __shared__ __align__(1024) unsigned char v_s[KEY_WAVES][BLOCK];
@@ -580,8 +580,7 @@ __global__ void __launch_bounds__(64 * MASS_WAVES, 2) tree_mass16_kernel(TreeAtt
 template <bool BF, int HD, class M>
 static void launch16(const TreeAttnArgs& a, const M& w, hipStream_t st) {
     const dim3 grid(a.n_kv_heads, a.n_items);
-    if (a.tile_rows == 16) hipLaunchKernelGGL((tree_keys16_kernel<BF, HD, 1, M>), grid, dim3(64 * KEY_WAVES), 0, st, a, w);
-    else if (a.tile_rows == 32) hipLaunchKernelGGL((tree_keys16_kernel<BF, HD, 2, M>), grid, dim3(64 * KEY_WAVES), 0, st, a, w);
+    if (a.tile_rows == 16) hipLaunchKernelGGL((tree_keys16_kernel<BF, HD, M>), grid, dim3(64 * KEY_WAVES), 0, st, a, w);
     else if (a.tile_rows == 64) hipLaunchKernelGGL((tree_rows16_kernel<BF, HD, 1, M>), grid, dim3(64 * ROW_WAVES), 0, st, a, w);
     else hipLaunchKernelGGL((tree_rows16_kernel<BF, HD, 2, M>), grid, dim3(64 * ROW_WAVES), 0, st, a, w);
     if (a.n_joins)

@@ -117,6 +117,10 @@ def test_evict(lib, ctx):
         assert call(to=to) == EINVAL
     assert call(mass=P, mass_out=C.c_void_p((1 << 20) + 796)) == EINVAL and call(mass=P, mass_out=C.c_void_p((1 << 20) + 800)) == EWORKSPACE
     assert call(keep=i32([0, 0]), first=0, recent=0) == 0                        # nothing stays: nothing to copy
+    many = 65536
+    assert call(B=many, start=i32([0] * many), n=i32([0] * many), keep=i32([0] * many), out=i32([0] * many), first=0, recent=0) == ESHAPE
+    many, to = 2100, view(base=1 << 45, slots=1 << 25)                           # more than 2^24 rows of overlapping contexts
+    assert call(kv=view(slots=8192), B=many, start=i32([0] * many), n=i32([8192] * many), keep=i32([8192] * many), out=i32(np.arange(many) * 8192), to=to) == ESHAPE
     assert lib.ssd_evict_workspace_bytes(ctx, 0, 1, 1, 1) == 0 and lib.ssd_evict_workspace_bytes(ctx, 1, 1, 10, 1) > 40
 
 

@@ -257,8 +257,8 @@ class TwoPhaseDecoder:
                 acc = ctx.accept_prefix(hv, sel["draft_ids"], sel["cu_draft"], tau_slm, want_greedy=True)
                 first = ctx.gather_i32(acc["greedy_tok"], sel["cu_draft"][1:] - 1)
             if self.trees is not None:
-                f, ids = first.cpu().numpy(), g["draft_ctc"].cpu()
-                rest = [self.table.cpu()[ids[self.cu_frames[b] + A[b]:self.cu_frames[b] + draft_len[b]].long()].numpy() for b in utts]
+                f, ids, table = first.cpu().numpy(), g["draft_ctc"].cpu(), self.table.cpu()
+                rest = [table[ids[self.cu_frames[b] + A[b]:self.cu_frames[b] + draft_len[b]].long()].numpy() for b in utts]
                 for b, t in zip(utts, self.trees.run(ks, cl, f, rest, n_steps)):
                     res["tokens"][int(b)] = t
                 continue

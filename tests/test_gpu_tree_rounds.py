@@ -1,0 +1,122 @@
+"""Trees as they are used: the two-phase schedule with trees in place of the greedy fallback, a captured round of verification, acceptance and
+eviction, contexts side by side on streams of their own."""
+import numpy as np
+import pytest
+import torch
+
+from tests.test_gpu_verify_tree import _prefilled, _weights
+from trees import cu, flat, tree
+from workloads import WORKLOADS, make_ctc_batch, make_ctc_to_llm_map, make_verify_inputs
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.mark.parametrize("mode", ["resident", "offload"])
+def test_two_phases_with_trees(mode):
+    """An fp32 model whose choices are far from ties: the tokens are those of the greedy fallback; with contexts that are cut the first one is."""
+    from paper_2603_11243_amd.binding import Context
+    from paper_2603_11243_amd.pipeline import TwoPhaseDecoder
+    wl = WORKLOADS["cfg1_tiny_f32"]
+    cb, table, n_steps = make_ctc_batch(wl), make_ctc_to_llm_map(wl), 9
+    vi = make_verify_inputs(wl, cb.seconds, [np.zeros(0, np.int32)] * wl.B, device="cuda")
+    runs = {}
+    for name, trees in (("greedy", None), ("trees", dict(tau=0.5, depth=4)), ("short", dict(tau=0.5, depth=4, most_rows=40, n_first=2, n_recent=8))):
+        ctx = Context(wl.model, _weights(wl.model, 3))
+        dec = TwoPhaseDecoder(ctx, wl, cb.logits.cuda(), cb.cu_frames, torch.from_numpy(table).cuda(), vi.speech_emb, vi.cu_speech,
+                              torch.from_numpy(vi.prompt_ids).cuda(), vi.cu_prompt, budget=300, mode=mode, n_steps=n_steps, trees=trees)
+        runs[name] = dec.run(0.5)
+        again = dec.run(0.5)
+        assert all(np.array_equal(t, again["tokens"][b]) for b, t in runs[name]["tokens"].items())
+        torch.cuda.synchronize()
+        ctx.close()
+    want = runs["greedy"]
+    assert want["rejected"] > 0
+    for name in ("trees", "short"):
+        r = runs[name]
+        assert np.array_equal(r["accept_len"], want["accept_len"]) and set(r["tokens"]) == set(want["tokens"])
+        for b, t in r["tokens"].items():
+            assert len(t) == n_steps + 1 and t[0] == want["tokens"][b][0]
+            if name == "trees":
+                assert np.array_equal(t, want["tokens"][b])
+
+
+@pytest.mark.parametrize("name", ["tiny", "1b_half"])
+def test_a_captured_round(name):
+    """verify_tree, accept_tree and kv_evict in one graph: every replay, with eager calls of the same context between, gives what the eager calls give for the
+    tokens that are in place then."""
+    prompts, nodes, room = [40, 90, 7], [9, 20, 1], 24
+    side = torch.cuda.Stream()
+    with torch.cuda.stream(side):
+        ctx, m, w, start, r = _prefilled(name, prompts, room)
+    trees = [tree(r, n, "random") for n in nodes]
+    at, par, N, n = cu(trees), flat(trees), sum(nodes), np.array(prompts)
+    keep, to = np.minimum(n, 20), np.array([0, 25, 50])
+    k, v = ctx.kv_tensors()
+    ctx.reserve(evict_rows=80, evict_utts=3, evict_heads=(m.n_layers, m.n_kv_heads))
+    k_out, v_out = torch.zeros_like(k[:, :80]), torch.zeros_like(v[:, :80])
+    cache = ctx._kv.clone()
+    mass = torch.zeros((m.n_layers, m.n_kv_heads, k.shape[1]), device="cuda")
+    ids = torch.zeros(N, dtype=torch.int32, device="cuda")
+    choices = [torch.from_numpy(r.integers(0, m.vocab, size=N).astype(np.int32)).cuda() for _ in range(3)]
+
+    def round_():
+        h = ctx.verify_tree(ids, at, par, start, n, kv_mass=mass)
+        acc = ctx.accept_tree(h, ids, at, par, 0.0005, kv_start=start, ctx_len=n, kv_mass=mass)
+        rows = ctx.kv_evict(k, v, mass, start, n, keep, 2, 8, k_out, v_out, to, want_rows=True)
+        return dict(acc, h=h, rows=rows)
+
+    def place(choice):
+        ctx._kv.copy_(cache)
+        mass.zero_()
+        ids.copy_(choice)
+        k_out.zero_()
+        v_out.zero_()
+
+    def state(out):
+        return {key: x.clone() for key, x in dict(out, kv=ctx._kv, mass=mass, k_out=k_out, v_out=v_out).items()}
+    torch.cuda.synchronize()
+    with torch.cuda.stream(side):
+        want = []
+        for c in choices:
+            place(c)
+            want.append(state(round_()))
+        side.synchronize()
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph, stream=side):
+            out = round_()
+        for i in (0, 1, 2, 0):
+            place(choices[i])
+            side.synchronize()
+            graph.replay()
+            got = state(out)
+            side.synchronize()
+            for key in want[i]:
+                assert torch.equal(got[key], want[i][key]), (i, key)
+            place(choices[(i + 1) % 3])
+            round_()                                         # the workspace in other hands between replays
+    ctx.close()
+
+
+def test_contexts_side_by_side():
+    """Two contexts with workspaces of their own, calls interleaved on two streams: the results of each alone, and rows outside the ranges as they were."""
+    from test_gpu_tree_attention import Call, _batch
+    from paper_2603_11243_amd.binding import Context
+    calls = [Call("f16", (8, 2, 128), [3000, 40, 700], _batch(31, None, [20, 1, 9]), seed=31), Call("bf16", (6, 2, 64), [500, 2000], _batch(32, None, [300, 40]), seed=32)]
+    want = [(c.run().clone(), c.mass_out.clone()) for c in calls]
+    streams, contexts = [torch.cuda.Stream() for _ in calls], []
+    torch.cuda.synchronize()
+    for c, s in zip(calls, streams):
+        with torch.cuda.stream(s):
+            ctx = Context(device="cuda:0", stream=s)
+            ctx.reserve(tree_nodes=400, tree_utts=3, tree_heads=c.heads)
+        contexts.append(ctx)
+    got = [[], []]
+    for _ in range(4):
+        for i, (c, ctx, s) in enumerate(zip(calls, contexts, streams)):
+            with torch.cuda.stream(s):
+                mass = c.mass.clone()
+                got[i].append((ctx.tree_attention(c.q, c.k, c.v, c.kv_start, c.ctx_len, cu(c.trees), flat(c.trees), mass=mass), mass))
+    torch.cuda.synchronize()
+    for (out, mass), runs in zip(want, got):
+        for o, w in runs:
+            assert torch.equal(o, out) and torch.equal(w, mass)

@@ -30,6 +30,10 @@ __device__ __forceinline__ bool sees(uint32_t node, uint32_t key) {
 constexpr float LOG2E = 1.4426950408889634f, LN2 = 0.6931471805599453f;
 constexpr float F32_MOST = 3.4028234663852886e38f;
 
+// Scores are taken times a positive scale: the queries carry its sign, and are zero for a scale of zero, whose logits are (so that -infinity, a masked
+// score, stays what it is).
+__device__ __forceinline__ float scale_of(const TreeAttnArgs& a) { return a.scale == 0.f ? LOG2E : fabsf(a.scale) * LOG2E; }
+
 // Node of a query row (rows are fewer than 2^19, groups at most 512: the product is exact).
 __device__ __forceinline__ int node_of(const TreeAttnArgs& a, int row) { return a.group_magic ? (int)__umulhi((uint32_t)row, a.group_magic) : row; }
 
@@ -83,18 +87,28 @@ __device__ __forceinline__ Work mass_item_of(const TreeAttnArgs& a, const M& w, 
 constexpr int MASS_WAVES = 4;                // wavefronts of a workgroup of the weights
 constexpr int KEY_WAVES = 8;                 // wavefronts of a workgroup that split the keys
 
-// Spans of a lane's keys k0 + 16 c + 4 (lane / 16) + r: every node's place lies in that of a cached row, nobody's in that of a key behind the range.
+// Spans of the keys around the nodes in LDS: SPANS_BEFORE cached rows, the nodes, SPANS_BEHIND keys behind them, as far as a block with a node in it
+// reaches.  Every node's place lies in the span of a cached row, nobody's in that of a key behind the nodes (a node does not see a
+// later one; a range of keys that ends before the last node ends with a block, or where its rows see nothing more).
+constexpr int SPANS_BEFORE = 192, SPANS_BEHIND = 64, SPANS = SPANS_BEFORE + MAX_TREE_NODES + SPANS_BEHIND;
+// mine: the span of node threadIdx.x, requested before.
+template <int THREADS, class M>
+__device__ __forceinline__ void store_spans(uint32_t* span_s, const TreeAttnArgs& a, const M& w, const Work& t, uint32_t mine) {
+    const int i = threadIdx.x;
+    if (i < SPANS_BEFORE) span_s[i] = 0xffff0000u;
+    if (i < SPANS_BEHIND) span_s[SPANS_BEFORE + t.n_nodes + i] = 0u;
+    if (i < t.n_nodes) span_s[SPANS_BEFORE + i] = mine;
+    for (int j = i + THREADS; j < t.n_nodes; j += THREADS) span_s[SPANS_BEFORE + j] = w(a.spans + t.node0 + j);
+    static_assert(THREADS >= SPANS_BEFORE && SPANS_BEFORE >= SPANS_BEHIND, "one pass");
+}
+// Those of a lane's keys k0 + 16 c + 4 (lane / 16) + r.
 template <int C>
 __device__ __forceinline__ void key_spans(uint32_t (&key)[C][4], const Work& t, int k0, const uint32_t* span_s) {
-    const int kg = threadIdx.x % 64 / 16;
+    const uint32_t* from = span_s + SPANS_BEFORE + k0 + 4 * (threadIdx.x % 64 / 16) - t.n_ctx;
 #pragma unroll
     for (int c = 0; c < C; ++c)
 #pragma unroll
-        for (int r = 0; r < 4; ++r) {
-            const int at = k0 + 16 * c + 4 * kg + r - t.n_ctx;
-            const uint32_t span = span_s[min(max(at, 0), t.n_nodes - 1)];
-            key[c][r] = at < 0 ? 0xffff0000u : at < t.k1 - t.n_ctx ? span : 0u;
-        }
+        for (int r = 0; r < 4; ++r) key[c][r] = from[16 * c + r];
 }
 
 // The end of an attention workgroup: its wavefronts hold, for 16 NT rows, maxima m (raw scores), sums l (a lane's share) and outputs o[n][i] (row
@@ -189,7 +203,7 @@ __global__ void __launch_bounds__(256) tree_join_kernel(TreeAttnArgs a, M w, flo
     utterance_of(a, w, x & 0xffffu, t);
     const int R = t.n_nodes * G, tiles = (R + a.tile_rows - 1) / a.tile_rows, row = (int)(x >> 16) * a.tile_rows + r;
     if (row >= R) return;
-    const float sc = fabsf(a.scale) * LOG2E;
+    const float sc = scale_of(a);
     const int group = threadIdx.x / LANES, dim = threadIdx.x % LANES * 4;
     float m = -F32_MOST, l = 0.f;
     f32x4_t v = {0.f, 0.f, 0.f, 0.f};

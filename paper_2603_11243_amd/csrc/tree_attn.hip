@@ -46,7 +46,7 @@ template <bool BF> __device__ __forceinline__ uint32_t pack16(float lo, float hi
 }
 
 // Scores of 32 keys to weights in the operand type; maxima, sums and outputs follow.
-template <bool BF, int NT, int DT, bool MASKED>
+template <bool BF, int NT, int DT>
 __device__ __forceinline__ void weights_of(f32x4_t (&s)[NT][2], float (&m)[NT], float (&l)[NT], f32x4_t (&o)[NT][DT], float sc, f16x8_t (&pf)[NT]) {
     float mx[NT];
     bool above = false;
@@ -78,8 +78,7 @@ __device__ __forceinline__ void weights_of(f32x4_t (&s)[NT][2], float (&m)[NT], 
             f32x4_t& x = s[n][c];
 #pragma unroll
             for (int r = 0; r < 4; ++r) {
-                const float p = __builtin_amdgcn_exp2f(fmaf(x[r], sc, base));
-                x[r] = MASKED && x[r] == -INFINITY ? 0.f : p;
+                x[r] = __builtin_amdgcn_exp2f(fmaf(x[r], sc, base));
                 l[n] += x[r];
             }
             pw[2 * c] = pack16<BF>(x[0], x[1]);
@@ -218,7 +217,7 @@ __device__ __forceinline__ void add_values(const unsigned char* v, const f16x8_t
 template <int HD, int NT>
 __device__ __forceinline__ void load_queries(f16x8_t (&qf)[NT][HD / 32], const TreeAttnArgs& a, const Work& t, int kvh, int row0) {
     const int lane = threadIdx.x % 64;
-    const uint32_t flip = a.scale < 0.f ? 0x80008000u : 0u;
+    const uint32_t flip = a.scale < 0.f ? 0x80008000u : 0u, keep = a.scale == 0.f ? 0u : ~0u;
 #pragma unroll
     for (int n = 0; n < NT; ++n) {
         const int row = min(row0 + 16 * n + lane % 16, t.n_nodes * a.group - 1);
@@ -226,7 +225,7 @@ __device__ __forceinline__ void load_queries(f16x8_t (&qf)[NT][HD / 32], const T
 #pragma unroll
         for (int s = 0; s < HD / 32; ++s) {
             uint4 x = *reinterpret_cast<const uint4*>(q + 32 * s);
-            x.x ^= flip; x.y ^= flip; x.z ^= flip; x.w ^= flip;
+            x.x = (x.x ^ flip) & keep; x.y = (x.y ^ flip) & keep; x.z = (x.z ^ flip) & keep; x.w = (x.w ^ flip) & keep;
             qf[n][s] = as_f16x8(x);
         }
     }
@@ -251,7 +250,7 @@ __global__ void __launch_bounds__(64 * KEY_WAVES, 2) tree_keys16_kernel(TreeAttn
     constexpr int ROW_CHUNKS = ROW / 16, V_ROWS = 64 / ROW_CHUNKS, V_LOADS = KEYS / V_ROWS, K_LOADS = 2 * KS;
     __shared__ __align__(1024) unsigned char v_s[KEY_WAVES][BLOCK];
     __shared__ float2 ml_s[KEY_WAVES * TR];
-    __shared__ uint32_t span_s[MAX_TREE_NODES];
+    __shared__ uint32_t span_s[SPANS];
     const int lane = threadIdx.x % 64, kg = lane / 16, dc = lane % 16;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
     const Work t = item_of(a, w, blockIdx.y, TR);
@@ -293,15 +292,14 @@ __global__ void __launch_bounds__(64 * KEY_WAVES, 2) tree_keys16_kernel(TreeAttn
     f16x8_t qf[NT][KS];
     load_queries<HD, NT>(qf, a, t, kvh, t.row0);
     load_values(k_first);
-    const float sc = fabsf(a.scale) * LOG2E;
+    const float sc = scale_of(a);
     float m[NT], l[NT];
     f32x4_t o[NT][DT];
-    if ((int)threadIdx.x < n_spans) span_s[threadIdx.x] = span;
-    for (int i = threadIdx.x + 64 * KEY_WAVES; i < n_spans; i += 64 * KEY_WAVES) span_s[i] = w(a.spans + t.node0 + i);
+    if (n_spans) store_spans<64 * KEY_WAVES>(span_s, a, w, t, span);
     lds_barrier();
     uint32_t mine[NT];
 #pragma unroll
-    for (int n = 0; n < NT; ++n) mine[n] = span_s[node_of(a, min(t.row0 + 16 * n + dc, R - 1))];           // (not read without node keys)
+    for (int n = 0; n < NT; ++n) mine[n] = span_s[SPANS_BEFORE + node_of(a, min(t.row0 + 16 * n + dc, R - 1))];           // (not read without node keys)
     bool careful = false;
     auto block = [&](auto masked_c, int k0) __attribute__((always_inline)) {
         constexpr bool MASKED = decltype(masked_c)::value;
@@ -329,7 +327,7 @@ __global__ void __launch_bounds__(64 * KEY_WAVES, 2) tree_keys16_kernel(TreeAttn
             }
         }
         f16x8_t p[NT];
-        weights_of<BF, NT, DT, MASKED>(s, m, l, o, sc, p);
+        weights_of<BF, NT, DT>(s, m, l, o, sc, p);
         __builtin_amdgcn_sched_barrier(0);
         __builtin_amdgcn_s_waitcnt(0x0F70 | K_LOADS);        // the values of this block have landed (a wavefront reads its own only)
         __builtin_amdgcn_sched_barrier(0);
@@ -363,7 +361,7 @@ __global__ void __launch_bounds__(64 * ROW_WAVES, 2) tree_rows16_kernel(TreeAttn
     constexpr int KEYS = 64, ROW = HD * 2, BLOCK = KEYS * ROW, KS = HD / 32, DT = HD / 16, TR = 16 * NT * ROW_WAVES;
     constexpr int CHUNKS = ROW / 16, L_ROWS = 64 / CHUNKS, LOADS = KEYS / L_ROWS / ROW_WAVES;
     __shared__ __align__(1024) unsigned char kv_s[2][2][BLOCK];
-    __shared__ uint32_t span_s[MAX_TREE_NODES];
+    __shared__ uint32_t span_s[SPANS];
     const int lane = threadIdx.x % 64, kg = lane / 16, dc = lane % 16;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
     const Work t = item_of(a, w, blockIdx.y, TR);
@@ -392,13 +390,12 @@ __global__ void __launch_bounds__(64 * ROW_WAVES, 2) tree_rows16_kernel(TreeAttn
     load_queries<HD, NT>(qf, a, t, kvh, row0);
     load(t.k0, 0);
     load(t.k0 + KEYS, 1);
-    if ((int)threadIdx.x < n_spans) span_s[threadIdx.x] = span;
-    for (int i = threadIdx.x + 64 * ROW_WAVES; i < n_spans; i += 64 * ROW_WAVES) span_s[i] = w(a.spans + t.node0 + i);
+    if (n_spans) store_spans<64 * ROW_WAVES>(span_s, a, w, t, span);
     lds_barrier();
     uint32_t mine[NT];
 #pragma unroll
-    for (int n = 0; n < NT; ++n) mine[n] = span_s[node_of(a, min(row0 + 16 * n + dc, R - 1))];             // (not read without node keys)
-    const float sc = fabsf(a.scale) * LOG2E;
+    for (int n = 0; n < NT; ++n) mine[n] = span_s[SPANS_BEFORE + node_of(a, min(row0 + 16 * n + dc, R - 1))];             // (not read without node keys)
+    const float sc = scale_of(a);
     float m[NT], l[NT];
     f32x4_t o[NT][DT];
     bool careful = false;
@@ -428,7 +425,7 @@ __global__ void __launch_bounds__(64 * ROW_WAVES, 2) tree_rows16_kernel(TreeAttn
             }
         }
         f16x8_t p[NT];
-        weights_of<BF, NT, DT, MASKED>(s, m, l, o, sc, p);
+        weights_of<BF, NT, DT>(s, m, l, o, sc, p);
         add_values<BF, HD, NT, MASKED>(v, p, o, careful);
     };
     auto block = [&](auto masked_c, int k0, int stage) __attribute__((always_inline)) {
@@ -486,11 +483,11 @@ __global__ void __launch_bounds__(64 * ROW_WAVES, 2) tree_rows16_kernel(TreeAttn
 constexpr int MASS_ROWS = 128;
 
 template <bool BF, int HD, class M>
-__global__ void __launch_bounds__(64 * MASS_WAVES, 2) tree_mass16_kernel(TreeAttnArgs a, M w) {
+__global__ void __launch_bounds__(64 * MASS_WAVES, 4) tree_mass16_kernel(TreeAttnArgs a, M w) {
     constexpr int MASS_KEYS = 32, ROW = HD * 2, STEP = MASS_KEYS * MASS_WAVES, KS = HD / 32, CHUNKS = ROW / 16;
     __shared__ __align__(1024) unsigned char q_s[MASS_ROWS * ROW];
     __shared__ float lse_s[MASS_ROWS];
-    __shared__ uint32_t row_span[MASS_ROWS], span_s[MAX_TREE_NODES];
+    __shared__ uint32_t row_span[MASS_ROWS], span_s[SPANS];
     const int lane = threadIdx.x % 64, kg = lane / 16, dc = lane % 16;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
     const Work t = mass_item_of(a, w, blockIdx.y);
@@ -512,17 +509,16 @@ __global__ void __launch_bounds__(64 * MASS_WAVES, 2) tree_mass16_kernel(TreeAtt
     };
     const int first = t.k0 + wave * MASS_KEYS;
     load_keys(first, kr[0]);
-    if (t.k1 > t.n_ctx)
-        for (int i = threadIdx.x; i < t.n_nodes; i += 64 * MASS_WAVES) span_s[i] = w(a.spans + t.node0 + i);
-    const float sc = fabsf(a.scale) * LOG2E;
-    const uint32_t flip = a.scale < 0.f ? 0x80008000u : 0u;
+    if (t.k1 > t.n_ctx) store_spans<64 * MASS_WAVES>(span_s, a, w, t, (int)threadIdx.x < t.n_nodes ? w(a.spans + t.node0 + (int)threadIdx.x) : 0u);
+    const float sc = scale_of(a);
+    const uint32_t flip = a.scale < 0.f ? 0x80008000u : 0u, keep = a.scale == 0.f ? 0u : ~0u;
     for (int r0 = 0; r0 < R; r0 += MASS_ROWS) {
         const int rows = min(MASS_ROWS, R - r0), tiles = (rows + 15) / 16;
         if (r0) __syncthreads();
         for (int i = threadIdx.x; i < tiles * 16 * CHUNKS; i += 64 * MASS_WAVES) {
             const int r = i / CHUNKS, c = i % CHUNKS, row = min(r0 + r, R - 1);
             uint4 x = *reinterpret_cast<const uint4*>((const uint16_t*)a.q + query_at(a, t, kvh, row, HD) + c * 8);
-            x.x ^= flip; x.y ^= flip; x.z ^= flip; x.w ^= flip;
+            x.x = (x.x ^ flip) & keep; x.y = (x.y ^ flip) & keep; x.z = (x.z ^ flip) & keep; x.w = (x.w ^ flip) & keep;
             *reinterpret_cast<uint4*>(q_s + r * ROW + (c ^ k_swizzle<HD>(r)) * 16) = x;
         }
         for (int r = threadIdx.x; r < tiles * 16; r += 64 * MASS_WAVES) {
@@ -573,7 +569,10 @@ __global__ void __launch_bounds__(64 * MASS_WAVES, 2) tree_mass16_kernel(TreeAtt
         };
         int k0 = first;
         for (; k0 + STEP + MASS_KEYS <= min(t.n_ctx, t.k1); k0 += 2 * STEP) step(std::false_type(), k0);
-        for (; k0 < t.k1; k0 += 2 * STEP) step(std::true_type(), k0);
+        if (t.k1 <= t.n_ctx) {                               // a range that ends inside the context consists of whole blocks: one is left, or none
+            if (k0 < t.k1) block(std::false_type(), k0, kr[0]);
+        } else
+            for (; k0 < t.k1; k0 += 2 * STEP) step(std::true_type(), k0);
     }
 }
 

@@ -26,7 +26,7 @@ __global__ void __launch_bounds__(64 * KEY_WAVES, 2) tree_attn32_kernel(TreeAttn
     constexpr int ROW_CHUNKS = ROW / 16, V_ROWS = 64 / ROW_CHUNKS, V_LOADS = TREE32_KEYS / V_ROWS;
     __shared__ __align__(1024) unsigned char v_s[KEY_WAVES][BLOCK];
     __shared__ float2 ml_s[KEY_WAVES * TR];
-    __shared__ uint32_t span_s[MAX_TREE_NODES];
+    __shared__ uint32_t span_s[SPANS];
     const int lane = threadIdx.x % 64, kg = lane / 16, dc = lane % 16;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
     const Work t = item_of(a, w, blockIdx.y, TR);
@@ -34,7 +34,7 @@ __global__ void __launch_bounds__(64 * KEY_WAVES, 2) tree_attn32_kernel(TreeAttn
     const int R = t.n_nodes * a.group;
     const int last = max(t.k0, t.k1 - 1);                    // (a range without keys: any row)
     const int n_spans = t.k1 > t.n_ctx ? t.n_nodes : 0;
-    for (int i = threadIdx.x; i < n_spans; i += 64 * KEY_WAVES) span_s[i] = w(a.spans + t.node0 + i);
+    if (n_spans) store_spans<64 * KEY_WAVES>(span_s, a, w, t, (int)threadIdx.x < n_spans ? w(a.spans + t.node0 + (int)threadIdx.x) : 0u);
     const int64_t first = (int64_t)t.slot0 * a.slot_stride + kvh * a.head_stride;
     const float* kbase = (const float*)a.k + first;
     const float* vbase = (const float*)a.v + first;
@@ -55,7 +55,7 @@ __global__ void __launch_bounds__(64 * KEY_WAVES, 2) tree_attn32_kernel(TreeAttn
     int k0 = t.k0 + wave * TREE32_KEYS;
     load_keys(k0);
     f32x4_t qf[NT][DT];
-    const float sign = a.scale < 0.f ? -1.f : 1.f;
+    const float sign = a.scale < 0.f ? -1.f : a.scale == 0.f ? 0.f : 1.f;
 #pragma unroll
     for (int n = 0; n < NT; ++n) {
         const int row = min(t.row0 + 16 * n + dc, R - 1);
@@ -63,7 +63,7 @@ __global__ void __launch_bounds__(64 * KEY_WAVES, 2) tree_attn32_kernel(TreeAttn
 #pragma unroll
         for (int c = 0; c < DT; ++c) qf[n][c] *= sign;
     }
-    const float sc = fabsf(a.scale) * LOG2E;
+    const float sc = scale_of(a);
     float m[NT], l[NT];
     f32x4_t o[NT][DT];
 #pragma unroll
@@ -92,7 +92,7 @@ __global__ void __launch_bounds__(64 * KEY_WAVES, 2) tree_attn32_kernel(TreeAttn
             key_spans<1>(key, t, k0, span_s);
 #pragma unroll
             for (int n = 0; n < NT; ++n) {
-                const uint32_t mine = span_s[node_of(a, min(t.row0 + 16 * n + dc, R - 1))];
+                const uint32_t mine = span_s[SPANS_BEFORE + node_of(a, min(t.row0 + 16 * n + dc, R - 1))];
 #pragma unroll
                 for (int r = 0; r < 4; ++r) s[n][r] = sees(mine, key[0][r]) ? s[n][r] : -INFINITY;
             }
@@ -121,7 +121,7 @@ __global__ void __launch_bounds__(64 * KEY_WAVES, 2) tree_attn32_kernel(TreeAttn
             const float base = fminf(-m[n] * sc, F32_MOST);
 #pragma unroll
             for (int r = 0; r < 4; ++r) {
-                s[n][r] = s[n][r] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(fmaf(s[n][r], sc, base));
+                s[n][r] = __builtin_amdgcn_exp2f(fmaf(s[n][r], sc, base));
                 l[n] += s[n][r];
             }
         }
@@ -178,7 +178,7 @@ __global__ void __launch_bounds__(64 * MASS_WAVES, 2) tree_mass32_kernel(TreeAtt
     constexpr int STEP = TREE32_KEYS * MASS_WAVES, DT = HD / 16, CHUNKS = HD / 4;
     __shared__ __align__(1024) float q_s[MASS32_ROWS * HD];
     __shared__ float lse_s[MASS32_ROWS];
-    __shared__ uint32_t row_span[MASS32_ROWS], span_s[MAX_TREE_NODES];
+    __shared__ uint32_t row_span[MASS32_ROWS], span_s[SPANS];
     const int lane = threadIdx.x % 64, kg = lane / 16, dc = lane % 16;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
     const Work t = mass_item_of(a, w, blockIdx.y);
@@ -189,9 +189,8 @@ __global__ void __launch_bounds__(64 * MASS_WAVES, 2) tree_mass32_kernel(TreeAtt
     auto load_keys = [&](int k0) { load_rows32<HD>(kr, kbase + (int64_t)min(k0 + dc, last) * a.slot_stride, hd, kg); };
     const int first = t.k0 + wave * TREE32_KEYS;
     load_keys(first);
-    if (t.k1 > t.n_ctx)
-        for (int i = threadIdx.x; i < t.n_nodes; i += 64 * MASS_WAVES) span_s[i] = w(a.spans + t.node0 + i);
-    const float sc = fabsf(a.scale) * LOG2E, sign = a.scale < 0.f ? -1.f : 1.f;
+    if (t.k1 > t.n_ctx) store_spans<64 * MASS_WAVES>(span_s, a, w, t, (int)threadIdx.x < t.n_nodes ? w(a.spans + t.node0 + (int)threadIdx.x) : 0u);
+    const float sc = scale_of(a), sign = a.scale < 0.f ? -1.f : a.scale == 0.f ? 0.f : 1.f;
     for (int r0 = 0; r0 < R; r0 += MASS32_ROWS) {
         const int rows = min(MASS32_ROWS, R - r0), tiles = (rows + 15) / 16;
         if (r0) __syncthreads();

@@ -1413,8 +1413,7 @@ int check_places(ssd_ctx* c, const char* what, int B, const int32_t* kv_start, c
 }
 
 // Host metadata of a call, n words that fill(words) writes, to its place in the workspace: as arguments of a launch where it holds them, and in pieces of that size
-// under capture (a staging buffer would be read again by every replay); else from a pinned staging buffer by a kernel that reads it over the
-// bus.  Between two kernels the copy engine takes 17 us for 24 KB (6 of them the copy, the rest the way there and back); see the kernel for its time.
+// under capture (a staging buffer would be read again by every replay); else from a pinned staging buffer by a kernel that reads it over the bus.
 template <class F>
 int place_words(ssd_ctx* c, size_t n, void* dev, const F& fill) {
     if (n <= MetaWords::WORDS) {
@@ -1469,7 +1468,8 @@ void tree_spans(int n, const int32_t* parent, uint32_t* span) {
 // keys; with 64 and 128 they split the rows and share the keys, which takes 32 rows over 300 keys in 13.6 us where a split of the keys takes 18.0.
 // 128 rows read the keys half as often: 90 utterances of 42 nodes, 24 heads on 8, over 1024 rows 113 us, with 64 rows 133 (64 nodes over 64 rows: 62.6 and 61.9).
 int tree_tile_rows(int dtype, int rows) { return rows <= 16 ? 16 : dtype == SSD_F32 ? 32 : rows <= 64 ? 64 : 128; }
-// Ranges of keys: one per item, unless that leaves most of the chip without work or an utterance is longer than its share; then pieces of such a share.
+// Ranges of keys: one per item, unless that leaves most of the chip without work or an utterance is longer than its share; then pieces of such a share, at least
+// TREE_SPLIT_KEYS (a piece costs its partial results, 33 KB for 64 rows, written and read once: as much as 64 keys).
 void tree_work(int B, const int32_t* kv_start, const int32_t* ctx_len, const int32_t* cu_nodes, const int32_t* parent, int most, int n_q_heads, const ssd_kv_view& kv,
                bool mass, TreeWork& w) {
     const int n_kv_heads = kv.n_kv_heads, G = n_q_heads / n_kv_heads, rows = tree_tile_rows(kv.dtype, most * G);

@@ -85,7 +85,9 @@ __device__ __forceinline__ Work mass_item_of(const TreeAttnArgs& a, const M& w, 
 }
 
 constexpr int MASS_WAVES = 4;                // wavefronts of a workgroup of the weights
-constexpr int KEY_WAVES = 8;                 // wavefronts of a workgroup that split the keys
+// Wavefronts of a workgroup that split the keys.  Eight leave room for one workgroup a CU, four for two: 16 rows over 150 in 38 utterances, 16 heads on 8 of 128,
+// 14.8 and 9.6 us, one row over 106 6.0 and 5.3, over 20000 21.1 and 18.1; 16 over 200000 146 and 149.
+constexpr int KEY_WAVES = 4;
 
 // Spans of the keys around the nodes in LDS: SPANS_BEFORE cached rows, the nodes, SPANS_BEHIND keys behind them, as far as a block with a node in it
 // reaches.  Every node's place lies in the span of a cached row, nobody's in that of a key behind the nodes (a node does not see a
@@ -127,7 +129,7 @@ __device__ __forceinline__ void merge_wavefronts(const TreeAttnArgs& a, const Wo
         l[n] += __shfl_xor(l[n], 32);
         if (kg == 0) ml_s[wave * TR + 16 * n + dc] = make_float2(m[n], l[n]);
     }
-    static_assert(VPT == 2 || VPT == 4, "values of a thread");
+    static_assert(VPT == 2 || VPT == 4 || VPT == 8, "values of a thread");
     constexpr int CH = DPASS / 4;                            // chunks of a row
     const int orow = threadIdx.x / TPR, ocol = threadIdx.x % TPR * VPT;
     const int row = t.row0 + orow;
@@ -159,7 +161,7 @@ __device__ __forceinline__ void merge_wavefronts(const TreeAttnArgs& a, const Wo
 #pragma unroll
         for (int u = 0; u < WAVES; ++u)
 #pragma unroll
-            for (int e = 0; e < VPT; ++e) v[e] = fmaf(buf[(u * TR + orow) * DPASS + (ocol / 4 ^ (orow & (CH - 1))) * 4 + ocol % 4 + e], w[u], v[e]);
+            for (int e = 0; e < VPT; ++e) v[e] = fmaf(buf[(u * TR + orow) * DPASS + ((ocol + e) / 4 ^ (orow & (CH - 1))) * 4 + (ocol + e) % 4], w[u], v[e]);
         if (row >= R) continue;
         const int dim = pass * DPASS + ocol;
         if (t.index < a.n_parts) {
@@ -177,7 +179,8 @@ __device__ __forceinline__ void merge_wavefronts(const TreeAttnArgs& a, const Wo
                 uint32_t x[VPT / 2];
 #pragma unroll
                 for (int e = 0; e < VPT; e += 2) x[e / 2] = op_pack2<DT == SSD_BF16>(v[e] * inv, v[e + 1] * inv);
-                if constexpr (VPT == 4) *reinterpret_cast<uint2*>(dst) = make_uint2(x[0], x[1]);
+                if constexpr (VPT == 8) *reinterpret_cast<uint4*>(dst) = make_uint4(x[0], x[1], x[2], x[3]);
+                else if constexpr (VPT == 4) *reinterpret_cast<uint2*>(dst) = make_uint2(x[0], x[1]);
                 else *reinterpret_cast<uint32_t*>(dst) = x[0];
             }
         }
@@ -189,7 +192,7 @@ __device__ __forceinline__ void merge_wavefronts(const TreeAttnArgs& a, const Wo
 }
 
 // The pieces of a long context joined.  A workgroup has a query row: groups of HD / 4 lanes take its pieces in turn, each with a running maximum, and
-// are joined through LDS.
+// are joined through LDS: 48 rows of 8 heads in 64 pieces 5.7 us (one lane a dim over all pieces: 125, the pieces' latencies one after the other).
 template <int DT, int HD, class M>
 __global__ void __launch_bounds__(256) tree_join_kernel(TreeAttnArgs a, M w, float bias) {
     typedef Elem<DT> E;

@@ -8,7 +8,8 @@
 namespace ssd {
 
 // One workgroup a tree, one thread a node (NT of them).  Pointer jumping: after round r a node knows whether the 2^r nodes on the way up
-// from it pass, how many there are, and who comes next.
+// from it pass, how many there are, and who comes next: ten rounds of LDS for 1024 nodes, where a walk up a chain is 1024.  24 nodes 2.9 us, 256
+// trees of 64 to 1000 nodes 6.9: a launch; the calls take 9 and 37 us, of which the host checks, packs and hands over the parents.
 template <int NT, class M>
 __global__ void __launch_bounds__(NT) tree_path_kernel(const float* __restrict__ logp, M w, int parents, float ln_tau, bool roots_given, int32_t* __restrict__ accept_len,
                                                        int32_t* __restrict__ accept_node, int32_t* __restrict__ path) {
@@ -55,7 +56,8 @@ void launch_write_words(const MetaWords& w, uint32_t* dst, hipStream_t st) {
     hipLaunchKernelGGL(write_words_kernel, dim3(1), dim3(256), 0, st, w, dst);
 }
 
-// All loads of a thread are requested before the first is used: one way over the bus.
+// Metadata from pinned host memory.  All loads of a thread are requested before the first is used, one way over the bus: 26 KB 5.7 us, 275 KB 9.0; the copy
+// engine takes 17 us between two kernels for 24 KB.
 constexpr int COPY_UNITS = 4;                // of 16 bytes a thread
 __global__ void __launch_bounds__(256) copy_words_kernel(const uint4* __restrict__ host, int units, uint4* __restrict__ dst) {
     const int at = (int)blockIdx.x * 256 * COPY_UNITS + threadIdx.x;

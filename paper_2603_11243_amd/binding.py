@@ -566,6 +566,10 @@ class Context:
     def kv_tensors(self, buf: Optional[torch.Tensor] = None, slots: int = 0):
         """(k, v) [layers, slots, K/V heads, head_dim] of the attached K/V cache, or of a uint8 tensor laid out for `slots` slots (ssd_kv_cache_view)."""
         view = KvViewC()
+        if buf is not None:
+            _on(self.device, torch.uint8, buf=buf)
+            if buf.numel() < self.kv_cache_bytes(slots):
+                raise ValueError("buf is smaller than a K/V cache of so many slots")
         self._check(self._lib.ssd_kv_cache_view(self._h, _ptr(buf), slots, C.byref(view)))
         flat = (self._kv if buf is None else buf).view(self.act_dtype)
         shape = (view.n_layers, view.slots, view.n_kv_heads, view.head_dim)
@@ -577,6 +581,7 @@ class Context:
 
     def attach_kv_cache(self, buf: torch.Tensor, slots: int):
         """Attaches a uint8 tensor of kv_cache_bytes(slots) bytes as K/V cache."""
+        _on(self.device, torch.uint8, buf=buf)
         self._check(self._lib.ssd_set_kv_cache(self._h, _ptr(buf), buf.numel(), slots))
         self._kv = buf
 
@@ -593,6 +598,10 @@ class Context:
         self._check_kv_mass(kv_mass)
         if out is None:
             out = torch.empty((N, self.cfg.d_model), dtype=self.act_dtype, device=self.device)
+        else:
+            _on(self.device, self.act_dtype, out=out)
+            if out.numel() != N * self.cfg.d_model:
+                raise ValueError("out has the wrong size")
         self._check(self._lib.verify_tree(self._h, _ptr(node_ids), B, cn.tobytes(), pa.tobytes(), ks.tobytes(), cl.tobytes(),
                                           None if p0 is None else p0.tobytes(), _ptr(kv_mass), _ptr(out)))
         return out

@@ -5,6 +5,7 @@
 #include <string.h>
 
 #include <algorithm>
+#include <exception>
 
 #include "ssd_internal.h"
 #include "tree.h"
@@ -1468,9 +1469,10 @@ void tree_spans(int n, const int32_t* parent, uint32_t* span) {
 // keys; with 64 and 128 they split the rows and share the keys, which takes 32 rows over 300 keys in 13.6 us where a split of the keys takes 18.0.
 // 128 rows read the keys half as often: 90 utterances of 42 nodes, 24 heads on 8, over 1024 rows 113 us, with 64 rows 133 (64 nodes over 64 rows: 62.6 and 61.9).
 int tree_tile_rows(int dtype, int rows) { return rows <= 16 ? 16 : dtype == SSD_F32 ? 32 : rows <= 64 ? 64 : 128; }
+// false: more items of work than a grid has rows.
 // Ranges of keys: one per item, unless that leaves most of the chip without work or an utterance is longer than its share; then pieces of such a share, at least
 // TREE_SPLIT_KEYS (a piece costs its partial results, 33 KB for 64 rows, written and read once: as much as 64 keys).
-void tree_work(int B, const int32_t* kv_start, const int32_t* ctx_len, const int32_t* cu_nodes, const int32_t* parent, int most, int n_q_heads, const ssd_kv_view& kv,
+bool tree_work(int B, const int32_t* kv_start, const int32_t* ctx_len, const int32_t* cu_nodes, const int32_t* parent, int most, int n_q_heads, const ssd_kv_view& kv,
                bool mass, TreeWork& w) {
     const int n_kv_heads = kv.n_kv_heads, G = n_q_heads / n_kv_heads, rows = tree_tile_rows(kv.dtype, most * G);
     int64_t total = 0, per_row = 0;                          // keys of all items, of all utterances
@@ -1486,10 +1488,17 @@ void tree_work(int B, const int32_t* kv_start, const int32_t* ctx_len, const int
     const int64_t mass_step = std::min<int64_t>(step_of(per_row, 2 * pieces, TREE_MASS_KEYS), 0x7fffff00);
     std::vector<uint32_t>& v = w.words;
     TreeAttnArgs& a = w.a;
-    v.reserve((size_t)B * 12 + cu_nodes[B] + 512);
     a.n_items = a.n_parts = a.n_joins = a.n_mass = 0;
     auto tiles_of = [&](int b) { return ((cu_nodes[b + 1] - cu_nodes[b]) * G + rows - 1) / rows; };
     auto parts_of = [&](int b) { return ((int64_t)ctx_len[b] + cu_nodes[b + 1] - cu_nodes[b] + step - 1) / step; };
+    int64_t items = 0, mass_items = 0;
+    for (int b = 0; b < B; ++b) {
+        const int64_t n = cu_nodes[b + 1] - cu_nodes[b];
+        items += tiles_of(b) * parts_of(b);
+        mass_items += mass && n ? (ctx_len[b] + n + mass_step - 1) / mass_step : 0;
+    }
+    if (items > TREE_ITEMS || mass_items > TREE_ITEMS) return false;
+    v.reserve((size_t)B * 12 + cu_nodes[B] + 512);
     for (int cut = 1; cut >= 0; --cut)
         for (int b = 0; b < B; ++b) {
             const int tiles = tiles_of(b), parts = (int)parts_of(b);
@@ -1526,6 +1535,7 @@ void tree_work(int B, const int32_t* kv_start, const int32_t* ctx_len, const int
     a.slot_stride = kv.slot_stride; a.head_stride = n_kv_heads > 1 ? kv.head_stride : 0;
     a.group = G; a.group_magic = G > 1 ? (uint32_t)(((uint64_t)1 << 32) / G + 1) : 0;
     a.tile_rows = rows; a.step = (int)step; a.mass_step = (int)mass_step;
+    return true;
 }
 struct TreePlan { size_t words, lse, part_o, part_ml, total; };
 TreePlan plan_tree(int64_t n_words, int64_t lse_values, int64_t part_rows, int head_dim) {
@@ -1661,6 +1671,9 @@ AcceptTreePlan plan_accept_tree(const ssd_model_cfg& c, int64_t N, int64_t rows,
 
 extern "C" {
 
+// (host memory may not hold what a call builds: an error, as any other)
+#define SSD_NO_THROW(name) catch (const std::exception& e) { return fail(ctx, SSD_ESHAPE, name ": %s; split the batch", e.what()); }
+
 int ssd_kv_cache_view(ssd_ctx* ctx, void* dev_ptr, int64_t slots, ssd_kv_view* view) {
     if (!ctx || !view) return SSD_EINVAL;
     if (!ctx->has_model) return fail(ctx, SSD_EINVAL, "ssd_kv_cache_view: context was created without a model");
@@ -1677,7 +1690,7 @@ size_t ssd_tree_workspace_bytes(const ssd_ctx* ctx, int n_q_heads, int n_kv_head
 }
 
 int tree_attention(ssd_ctx* ctx, const void* q, int64_t q_stride, int n_q_heads, const ssd_kv_view* kv, int B, const int32_t* kv_start,
-                   const int32_t* ctx_len, const int32_t* cu_nodes, const int32_t* parent, float scale, void* out, float* lse, float* mass) {
+                   const int32_t* ctx_len, const int32_t* cu_nodes, const int32_t* parent, float scale, void* out, float* lse, float* mass) try {
     if (!ctx) return SSD_EINVAL;
     const OnDevice on(ctx);
     int most, rc = check_view(ctx, "tree_attention", kv);
@@ -1696,8 +1709,8 @@ int tree_attention(ssd_ctx* ctx, const void* q, int64_t q_stride, int n_q_heads,
     if (overlap(Extent{(uintptr_t)q, (uintptr_t)q + (uintptr_t)(((N - 1) * q_stride + dq) * es)}, Extent{(uintptr_t)out, (uintptr_t)out + (uintptr_t)(N * dq * es)}))
         return fail(ctx, SSD_EINVAL, "tree_attention: q and out overlap in memory");
     TreeWork w;
-    tree_work(B, kv_start, ctx_len, cu_nodes, parent, most, n_q_heads, *kv, mass != nullptr, w);
-    if (w.a.n_items > 65535 || w.a.n_mass > 65535) return fail(ctx, SSD_ESHAPE, "tree_attention: more than 65535 tiles of query rows; split the batch");
+    if (!tree_work(B, kv_start, ctx_len, cu_nodes, parent, most, n_q_heads, *kv, mass != nullptr, w))
+        return fail(ctx, SSD_ESHAPE, "tree_attention: more than 65535 tiles of query rows; split the batch");
     const TreePlan p = plan_tree(w, N, mass && !lse);
     if (!ctx->ws || ctx->ws_bytes < p.total)
         return fail(ctx, SSD_EWORKSPACE, "tree_attention: workspace of %zu bytes needed, %zu set", p.total, ctx->ws_bytes);
@@ -1713,10 +1726,10 @@ int tree_attention(ssd_ctx* ctx, const void* q, int64_t q_stride, int n_q_heads,
     }
     HIP_TRY(ctx, hipGetLastError());
     return SSD_OK;
-}
+} SSD_NO_THROW("tree_attention")
 
 int tree_path(ssd_ctx* ctx, const float* node_logp, int B, const int32_t* cu_nodes, const int32_t* parent, float tau, int32_t* accept_len,
-              int32_t* accept_node, int32_t* path) {
+              int32_t* accept_node, int32_t* path) try {
     if (!ctx) return SSD_EINVAL;
     const OnDevice on(ctx);
     int most, rc = check_trees(ctx, "tree_path", B, cu_nodes, parent, most);
@@ -1738,7 +1751,7 @@ int tree_path(ssd_ctx* ctx, const float* node_logp, int B, const int32_t* cu_nod
     }
     HIP_TRY(ctx, hipGetLastError());
     return SSD_OK;
-}
+} SSD_NO_THROW("tree_path")
 
 size_t ssd_evict_workspace_bytes(const ssd_ctx* ctx, int n_layers, int n_kv_heads, int64_t max_kept_rows, int64_t max_utts) {
     if (!ctx || n_layers <= 0 || n_kv_heads <= 0 || max_kept_rows < 0 || max_utts < 0) return 0;
@@ -1746,7 +1759,7 @@ size_t ssd_evict_workspace_bytes(const ssd_ctx* ctx, int n_layers, int n_kv_head
 }
 
 int kv_evict(ssd_ctx* ctx, const ssd_kv_view* from, const float* mass, int B, const int32_t* kv_start, const int32_t* ctx_len, const int32_t* keep,
-             int n_first, int n_recent, const ssd_kv_view* to, const int32_t* out_start, float* mass_out, int32_t* rows_out) {
+             int n_first, int n_recent, const ssd_kv_view* to, const int32_t* out_start, float* mass_out, int32_t* rows_out) try {
     if (!ctx) return SSD_EINVAL;
     const OnDevice on(ctx);
     int rc = check_view(ctx, "kv_evict", from);
@@ -1833,7 +1846,7 @@ int kv_evict(ssd_ctx* ctx, const ssd_kv_view* from, const float* mass, int B, co
     }
     HIP_TRY(ctx, hipGetLastError());
     return SSD_OK;
-}
+} SSD_NO_THROW("kv_evict")
 
 size_t ssd_verify_tree_workspace_bytes(const ssd_ctx* ctx, int64_t max_nodes, int64_t max_utts) {
     if (!ctx || !ctx->has_model || max_nodes < 0 || max_utts < 0) return 0;
@@ -1844,7 +1857,7 @@ size_t ssd_verify_tree_workspace_bytes(const ssd_ctx* ctx, int64_t max_nodes, in
 }
 
 int verify_tree(ssd_ctx* ctx, const int32_t* node_ids, int B, const int32_t* cu_nodes, const int32_t* parent, const int32_t* kv_start,
-                const int32_t* ctx_len, const int32_t* pos0, float* kv_mass, void* h_tree) {
+                const int32_t* ctx_len, const int32_t* pos0, float* kv_mass, void* h_tree) try {
     if (!ctx) return SSD_EINVAL;
     const OnDevice on(ctx);
     if (!ctx->has_model) return fail(ctx, SSD_EINVAL, "verify_tree: context was created without a model");
@@ -1865,8 +1878,8 @@ int verify_tree(ssd_ctx* ctx, const int32_t* node_ids, int B, const int32_t* cu_
                         (long long)N, (long long)widest);
     }
     TreeWork w;
-    tree_work(B, kv_start, ctx_len, cu_nodes, parent, most, m.n_q_heads, view, kv_mass != nullptr, w);
-    if (w.a.n_items > 65535 || w.a.n_mass > 65535) return fail(ctx, SSD_ESHAPE, "verify_tree: more than 65535 tiles of query rows; split the batch");
+    if (!tree_work(B, kv_start, ctx_len, cu_nodes, parent, most, m.n_q_heads, view, kv_mass != nullptr, w))
+        return fail(ctx, SSD_ESHAPE, "verify_tree: more than 65535 tiles of query rows; split the batch");
     const TreePlan t = plan_tree(w, N, kv_mass != nullptr);
     const VerifyTreePlan p = plan_verify_tree(m, N, t);
     if (!ctx->ws || ctx->ws_bytes < p.total)
@@ -1937,11 +1950,11 @@ int verify_tree(ssd_ctx* ctx, const int32_t* node_ids, int B, const int32_t* cu_
     { ProfScope ps(ctx, SSD_PROF_OTHER); launch_rmsnorm(m.dtype, x, ctx->norm_final, nullptr, Ni, d, m.rms_eps, h_tree, partials, pending, stride, ctx->dev_flags, ctx->bf16_ops, st); }
     HIP_TRY(ctx, hipGetLastError());
     return SSD_OK;
-}
+} SSD_NO_THROW("verify_tree")
 
 int accept_tree(ssd_ctx* ctx, const void* h_tree, const int32_t* node_ids, int B, const int32_t* cu_nodes, const int32_t* parent, float tau_slm,
                 const int32_t* kv_start, const int32_t* ctx_len, float* kv_mass, float* node_logp, int32_t* greedy_tok, int32_t* accept_len,
-                int32_t* accept_node, int32_t* path) {
+                int32_t* accept_node, int32_t* path) try {
     if (!ctx) return SSD_EINVAL;
     const OnDevice on(ctx);
     if (!ctx->has_model) return fail(ctx, SSD_EINVAL, "accept_tree: context was created without a model");
@@ -2022,6 +2035,6 @@ int accept_tree(ssd_ctx* ctx, const void* h_tree, const int32_t* node_ids, int B
     }
     HIP_TRY(ctx, hipGetLastError());
     return SSD_OK;
-}
+} SSD_NO_THROW("accept_tree")
 
 }  // extern "C"

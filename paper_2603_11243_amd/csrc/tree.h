@@ -45,6 +45,7 @@ struct TreeAttnArgs {
 };
 // words: host memory, n of them, to travel as arguments; or NULL, then they are in dev_words
 void launch_tree_attention(const TreeAttnArgs& a, const uint32_t* words, int n, const uint32_t* dev_words, hipStream_t st);
+constexpr int TREE_ITEMS = 65535;            // of a call: rows of a grid
 constexpr int TREE_WORKGROUPS = 512;         // long contexts are cut into about as many pieces in all, times K/V heads
 constexpr int TREE_SPLIT_KEYS = 512;         // a piece has at least as many keys
 constexpr int TREE_MASS_KEYS = 128;          // and one of the weights a multiple of these

@@ -84,8 +84,18 @@ class TreeFallback:
         token, at = [int(t) for t in first_tok], [0] * len(start)
         k, _ = ctx.kv_tensors()
         mass = None if self.most_rows is None else torch.zeros((k.shape[0], k.shape[2], k.shape[1]), device=dev)
-        before, cuts = (ctx._kv, int(k.shape[1])), 0
+        before = ctx._kv, int(k.shape[1])
         assert len(start) <= self.max_utts
+        try:
+            self._rounds(start, length, pos, done, token, at, drafts, n_steps, mass)
+        finally:
+            if ctx._kv is not before[0]:
+                ctx.attach_kv_cache(*before)
+        return [np.array(d + [t], dtype=np.int32) for d, t in zip(done, token)]
+
+    def _rounds(self, start, length, pos, done, token, at, drafts, n_steps, mass):
+        """Adds n_steps tokens to every list of done; the other arrays follow."""
+        ctx, dev, cuts = self.ctx, self.ctx.device, 0
         while True:
             live = [b for b in range(len(start)) if len(done[b]) < n_steps]
             if not live:
@@ -105,9 +115,6 @@ class TreeFallback:
                 length[b] += n[i]
                 pos[b] += n[i]
                 token[b], at[b] = greedy[cu[i] + nodes[-1]], trees[i][2][nodes[-1]]
-        if cuts:
-            ctx.attach_kv_cache(*before)
-        return [np.array(d + [t], dtype=np.int32) for d, t in zip(done, token)]
 
     def _evict(self, live, start, length, mass, turn):
         """Cuts the live utterances into a cache of the fallback's own and attaches it; returns the weights of the rows there."""

@@ -120,3 +120,49 @@ def test_contexts_side_by_side():
     for (out, mass), runs in zip(want, got):
         for o, w in runs:
             assert torch.equal(o, out) and torch.equal(w, mass)
+
+
+def test_outputs_and_caches_that_do_not_fit_are_refused():
+    ctx, m, w, start, r = _prefilled("tiny", [20, 20], 10)
+    ids = torch.zeros(4, dtype=torch.int32, device="cuda")
+    args = ids, [0, 2, 4], [-1, 0, -1, 0], start, [20, 20]
+    h = ctx.verify_tree(*args)
+    out = torch.empty_like(h)
+    assert ctx.verify_tree(*args, out=out) is out and torch.equal(out, h)
+    for bad in (torch.empty_like(h)[:3], torch.empty_like(h).half(), torch.empty_like(h).cpu(), torch.empty((m.d_model, 4), dtype=h.dtype, device="cuda").T):
+        with pytest.raises(ValueError):
+            ctx.verify_tree(*args, out=bad)
+    n = ctx.kv_cache_bytes(64)
+    for bad in (torch.empty(n, dtype=torch.uint8), torch.empty(n, dtype=torch.int8, device="cuda"), torch.empty(2 * n, dtype=torch.uint8, device="cuda")[::2]):
+        with pytest.raises(ValueError):
+            ctx.attach_kv_cache(bad, 64)
+        with pytest.raises(ValueError):
+            ctx.kv_tensors(bad, 64)
+    with pytest.raises(ValueError):
+        ctx.kv_tensors(torch.empty(n - 1, dtype=torch.uint8, device="cuda"), 64)
+    with pytest.raises(RuntimeError):
+        ctx.attach_kv_cache(torch.empty(n - 1, dtype=torch.uint8, device="cuda"), 64)
+    ctx.close()
+
+
+def test_the_attached_cache_comes_back_after_an_error():
+    """A fallback that fails in a later round, with its own cache attached: positions run out."""
+    from paper_2603_11243_amd.binding import SsdError
+    from paper_2603_11243_amd.pipeline import TreeFallback
+    n_steps, prompts = 60, [60, 50]
+    ctx, m, w, start, r = _prefilled("tiny", prompts, n_steps + 30)
+    kv = ctx._kv
+    fallback = TreeFallback(ctx, 2, tau=0.0, depth=5, most_rows=64, keep_rows=40, n_first=2, n_recent=8)
+    drafts = [r.integers(0, m.vocab, size=80).astype(np.int32) for _ in prompts]
+    inner, calls = ctx.verify_tree, []
+
+    def limited(*a, **k):
+        calls.append(1)
+        return inner(*a, **dict(k, pos0=[2000] * len(k["pos0"])) if len(calls) == 6 else k)
+    ctx.verify_tree = limited
+    with pytest.raises(SsdError):
+        fallback.run(start, prompts, [1, 2], drafts, n_steps)
+    assert len(calls) == 6 and ctx._kv is kv
+    ctx.verify_tree = inner
+    assert [len(t) for t in fallback.run(start, prompts, [1, 2], drafts, n_steps)] == [n_steps + 1] * 2
+    ctx.close()

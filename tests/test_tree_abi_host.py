@@ -141,3 +141,37 @@ def test_workspace_sizes_serve_smaller_calls(lib, ctx):
             assert lib.ssd_tree_workspace_bytes(ctx, 16, 8, 128, n, B) >= lib.ssd_tree_workspace_bytes(ctx, 16, 8, 128, n, 1) >= last
             assert lib.ssd_tree_workspace_bytes(ctx, 16, 8, 128, n, B) >= lib.ssd_tree_workspace_bytes(ctx, 0, 0, 0, n, B)
         last = lib.ssd_tree_workspace_bytes(ctx, 16, 8, 128, n, 1)
+
+
+def test_more_tiles_than_a_launch_has(lib, ctx):
+    """512 query heads on one: 4096 tiles of 128 rows an utterance of 1024 nodes."""
+    one = dict(kv=view(base=1 << 50, slots=1 << 20, H=1, ss=128, hs=0), hq=512, q_stride=1 << 16, q=C.c_void_p(1 << 45), out=C.c_void_p(1 << 46))
+    for B, want in ((15, EWORKSPACE), (16, ESHAPE), (800, ESHAPE)):
+        assert attention(lib, ctx, B=B, start=i32(np.arange(B) * 1024), n=i32([0] * B), cu=i32(np.arange(B + 1) * 1024), parent=i32(np.tile(np.arange(1024) - 1, B)),
+                         **one) == want
+
+
+def test_host_memory_that_does_not_suffice_is_an_error():
+    """In a process of its own, whose address space may not grow by what the call builds."""
+    import subprocess
+    import sys
+    code = """
+import ctypes as C, resource, sys
+import numpy as np
+sys.path[:0] = [%r, %r]
+from test_tree_abi_host import attention, i32, view
+from paper_2603_11243_amd import binding
+lib, h = binding.load_library(), C.c_void_p()
+assert lib.ssd_create(C.byref(h), None, None, None) == 0
+B = 8000
+args = dict(kv=view(base=1 << 50, slots=1 << 23, H=1, ss=128, hs=0), hq=1, q_stride=128, q=C.c_void_p(1 << 45), out=C.c_void_p(1 << 46), B=B, start=i32(np.arange(B) * 1024),
+            n=i32([0] * B), cu=i32(np.arange(B + 1) * 1024), parent=i32(np.tile(np.arange(1024) - 1, B)))
+assert attention(lib, h, **args) == -3
+now = int(open('/proc/self/statm').read().split()[0]) * resource.getpagesize()
+resource.setrlimit(resource.RLIMIT_AS, (now + (8 << 20), resource.getrlimit(resource.RLIMIT_AS)[1]))
+rc = attention(lib, h, **args)
+assert rc == -2 and b'tree_attention' in lib.ssd_last_error(h), rc
+print('refused')
+""" % (ROOT, os.path.join(ROOT, "tests"))
+    run = subprocess.run([sys.executable, "-c", code], capture_output=True, text=True, timeout=300, cwd=ROOT)
+    assert run.returncode == 0 and "refused" in run.stdout, run.stderr[-2000:]

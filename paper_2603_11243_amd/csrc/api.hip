@@ -1471,7 +1471,8 @@ void tree_spans(int n, const int32_t* parent, uint32_t* span) {
 int tree_tile_rows(int dtype, int rows) { return rows <= 16 ? 16 : dtype == SSD_F32 ? 32 : rows <= 64 ? 64 : 128; }
 // false: more items of work than a grid has rows.
 // Ranges of keys: one per item, unless that leaves most of the chip without work or an utterance is longer than its share; then pieces of such a share, at least
-// TREE_SPLIT_KEYS (a piece costs its partial results, 33 KB for 64 rows, written and read once: as much as 64 keys).
+// TREE_SPLIT_KEYS (a piece costs its partial results, 33 KB for 64 rows, written and read once: as much as 64 keys).  An utterance is cut into equal pieces, as many as
+// come nearest to the share: 57 utterances of 539 keys, 4 nodes, 8 fp32 heads, take 24.5 us whole and 50 in pieces of 512 and 27, 14 of them for joining.
 bool tree_work(int B, const int32_t* kv_start, const int32_t* ctx_len, const int32_t* cu_nodes, const int32_t* parent, int most, int n_q_heads, const ssd_kv_view& kv,
                bool mass, TreeWork& w) {
     const int n_kv_heads = kv.n_kv_heads, G = n_q_heads / n_kv_heads, rows = tree_tile_rows(kv.dtype, most * G);
@@ -1490,7 +1491,9 @@ bool tree_work(int B, const int32_t* kv_start, const int32_t* ctx_len, const int
     TreeAttnArgs& a = w.a;
     a.n_items = a.n_parts = a.n_joins = a.n_mass = 0;
     auto tiles_of = [&](int b) { return ((cu_nodes[b + 1] - cu_nodes[b]) * G + rows - 1) / rows; };
-    auto parts_of = [&](int b) { return ((int64_t)ctx_len[b] + cu_nodes[b + 1] - cu_nodes[b] + step - 1) / step; };
+    auto keys_of = [&](int b) { return (int64_t)ctx_len[b] + cu_nodes[b + 1] - cu_nodes[b]; };
+    auto piece_of = [&](int b) { return step_of(keys_of(b), std::max<int64_t>(1, (keys_of(b) + step / 2) / step), 128); };      // (whole blocks of every kernel)
+    auto parts_of = [&](int b) { return (keys_of(b) + piece_of(b) - 1) / piece_of(b); };
     int64_t items = 0, mass_items = 0;
     for (int b = 0; b < B; ++b) {
         const int64_t n = cu_nodes[b + 1] - cu_nodes[b];
@@ -1502,11 +1505,12 @@ bool tree_work(int B, const int32_t* kv_start, const int32_t* ctx_len, const int
     for (int cut = 1; cut >= 0; --cut)
         for (int b = 0; b < B; ++b) {
             const int tiles = tiles_of(b), parts = (int)parts_of(b);
+            const int64_t piece = piece_of(b);
             if (!tiles || (parts > 1) != (cut == 1)) continue;
             for (int p = 0; p < parts; ++p)                  // tiles of the same keys one behind the other: they meet in an L2
                 for (int t = 0; t < tiles; ++t)
                     for (uint32_t x : {(uint32_t)kv_start[b], (uint32_t)ctx_len[b], (uint32_t)cu_nodes[b], (uint32_t)(cu_nodes[b + 1] - cu_nodes[b]) | (uint32_t)t << 11,
-                                       (uint32_t)p})
+                                       (uint32_t)(p * piece), (uint32_t)((p + 1) * piece)})
                         v.push_back(x);
             a.n_items += parts * tiles;
             if (cut) a.n_parts = a.n_items;
@@ -1534,7 +1538,7 @@ bool tree_work(int B, const int32_t* kv_start, const int32_t* ctx_len, const int
     a.n_q_heads = n_q_heads; a.n_kv_heads = n_kv_heads; a.head_dim = kv.head_dim; a.dtype = kv.dtype;
     a.slot_stride = kv.slot_stride; a.head_stride = n_kv_heads > 1 ? kv.head_stride : 0;
     a.group = G; a.group_magic = G > 1 ? (uint32_t)(((uint64_t)1 << 32) / G + 1) : 0;
-    a.tile_rows = rows; a.step = (int)step; a.mass_step = (int)mass_step;
+    a.tile_rows = rows; a.mass_step = (int)mass_step;
     return true;
 }
 struct TreePlan { size_t words, lse, part_o, part_ml, total; };
@@ -1556,7 +1560,7 @@ TreePlan plan_tree(const TreeWork& w, int64_t nodes, bool own_lse) {
 size_t max_tree_bytes(int n_q_heads, int n_kv_heads, int head_dim, int64_t max_nodes, int64_t max_utts) {
     const int64_t G = (n_q_heads + n_kv_heads - 1) / n_kv_heads, cut = 2 * std::max(1, TREE_WORKGROUPS / n_kv_heads), rows = max_nodes * G;
     const int64_t tile = rows <= 16 ? 16 : rows <= 64 ? 64 : 128;
-    return plan_tree(4 * max_utts + 1 + 5 * (rows + cut) + 3 * rows + cut + max_nodes, max_nodes * n_q_heads, cut * n_kv_heads * tile, head_dim).total;
+    return plan_tree(4 * max_utts + 1 + 6 * (rows + cut) + 3 * rows + cut + max_nodes, max_nodes * n_q_heads, cut * n_kv_heads * tile, head_dim).total;
 }
 void run_tree_attention(ssd_ctx* c, TreeWork& w, const TreePlan& p, char* ws, bool in_args, const void* k, const void* v, int64_t slots, const void* q, int64_t q_stride,
                         float scale, void* out, float* lse, float* mass) {

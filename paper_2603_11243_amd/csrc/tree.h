@@ -25,8 +25,8 @@ void launch_write_words(const MetaWords& w, uint32_t* dst, hipStream_t st);
 void launch_copy_words(const uint32_t* host, size_t n, uint32_t* dst, hipStream_t st);
 
 // Attention of nodes.  Query rows of one K/V head are numbered node * G + head of the group; keys are the rows of the utterance, n_ctx cached ones, then
-// the nodes.  The words: per item of work five, at a place known without another: first slot, n_ctx, first node, nodes | tile of tile_rows query rows << 11,
-// piece of `step` keys (the first n_parts items leave partial results); from `utts` on per utterance first slot and n_ctx, from `cu` on the
+// the nodes.  The words: per item of work six, at a place known without another: first slot, n_ctx, first node, nodes | tile of tile_rows query rows << 11,
+// first key and the one behind the last (the first n_parts items, pieces of cut contexts, leave partial results); from `utts` on per utterance first slot and n_ctx, from `cu` on the
 // B + 1 prefix sums of the nodes; from `joins` on per tile of a cut utterance three: utterance | tile << 16, item of its first piece,
 // pieces; from `mass_items` on per item of the weights one: utterance | piece of mass_step keys << 16; from `spans` on per node its place in
 // depth-first order | end of its subtree << 16.
@@ -40,7 +40,7 @@ struct TreeAttnArgs {
     int n_q_heads, n_kv_heads, head_dim, dtype;
     int group; uint32_t group_magic;         // n_q_heads / n_kv_heads; 2^32 / group rounded up, 0 for 1
     float scale;
-    int tile_rows, step, mass_step, n_items, n_parts, n_joins, n_mass;
+    int tile_rows, mass_step, n_items, n_parts, n_joins, n_mass;
     int utts, cu, joins, mass_items, spans;
 };
 // words: host memory, n of them, to travel as arguments; or NULL, then they are in dev_words

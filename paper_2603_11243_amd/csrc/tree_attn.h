@@ -58,17 +58,16 @@ __device__ __forceinline__ void utterance_of(const TreeAttnArgs& a, const M& w, 
 template <class M>
 __device__ __forceinline__ Work item_of(const TreeAttnArgs& a, const M& w, int index, int tile_rows) {
     Work t;
-    const uint32_t x = w(5 * index + 3);
+    const uint32_t x = w(6 * index + 3);
     t.index = index;
-    t.slot0 = (int)w(5 * index);
-    t.n_ctx = (int)w(5 * index + 1);
-    t.node0 = (int)w(5 * index + 2);
+    t.slot0 = (int)w(6 * index);
+    t.n_ctx = (int)w(6 * index + 1);
+    t.node0 = (int)w(6 * index + 2);
     t.n_nodes = (int)(x & 0x7ffu);
     t.row0 = (int)(x >> 11) * tile_rows;
-    const int64_t k0 = (int64_t)w(5 * index + 4) * a.step;
     const int node = node_of(a, min(t.n_nodes * a.group, t.row0 + tile_rows) - 1);       // no row of the tile sees a later one
-    t.k0 = (int)k0;
-    t.k1 = (int)min((int64_t)t.n_ctx + node + 1, k0 + a.step);
+    t.k0 = (int)w(6 * index + 4);
+    t.k1 = min(t.n_ctx + node + 1, (int)w(6 * index + 5));
     return t;
 }
 template <class M>
@@ -86,7 +85,7 @@ __device__ __forceinline__ Work mass_item_of(const TreeAttnArgs& a, const M& w, 
 
 constexpr int MASS_WAVES = 4;                // wavefronts of a workgroup of the weights
 // Wavefronts of a workgroup that split the keys.  Eight leave room for one workgroup a CU, four for two: 16 rows over 150 in 38 utterances, 16 heads on 8 of 128,
-// 14.8 and 9.6 us, one row over 106 6.0 and 5.3, over 20000 21.1 and 18.1; 16 over 200000 146 and 149.
+// 14.8 and 9.6 us, one row over 106 6.0 and 5.3; 16 over 200000 146 and 149.
 constexpr int KEY_WAVES = 4;
 
 // Spans of the keys around the nodes in LDS: SPANS_BEFORE cached rows, the nodes, SPANS_BEHIND keys behind them, as far as a block with a node in it

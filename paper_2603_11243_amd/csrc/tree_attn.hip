@@ -243,7 +243,7 @@ __device__ __forceinline__ void lds_barrier() {
 // ---- few query rows: 16 of a K/V head a workgroup, whose wavefronts take the 32-key blocks of the range in turn, so that every cached row is read once,
 // and merge their (maximum, sum, output) through LDS.  Key rows come straight from memory in operand registers; a wavefront's values are its own
 // and need no barrier.  One token over 106 rows, 16 heads on 8: 5.3 us, the launch and three ways to memory and back one behind the other (words, keys and
-// queries, values); the kernel below, in which one wavefront has all 16 rows, takes 7.1, 18.5 us in place of 18.1 over 20000 rows, 155 in place of 149 over 200000, and for
+// queries, values); the kernel below, in which one wavefront has all 16 rows, takes 7.1, 155 in place of 149 over 200000 rows, and for
 // 38 utterances of 150 rows 9.0 in place of 9.6.
 template <bool BF, int HD, class M>
 __global__ void __launch_bounds__(64 * KEY_WAVES, 2) tree_keys16_kernel(TreeAttnArgs a, M w) {

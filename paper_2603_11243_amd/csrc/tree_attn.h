@@ -170,10 +170,11 @@ __device__ __forceinline__ void merge_wavefronts(const TreeAttnArgs& a, const Wo
         } else {
             const float inv = 1.f / lt;
             typename E::type* dst = (typename E::type*)a.out + (row_at(a, t, kvh, row)) * a.head_dim + dim;
-            if constexpr (DT == SSD_F32) {
+            if constexpr (DT == SSD_F32) {                   // (head_dim is a multiple of 4 and may end among a thread's 8 values)
+                static_assert(VPT % 4 == 0, "groups of four");
 #pragma unroll
-                for (int e = 0; e < VPT; ++e)
-                    if (dim < a.head_dim) dst[e] = v[e] * inv;
+                for (int e = 0; e < VPT; e += 4)
+                    if (dim + e < a.head_dim) *reinterpret_cast<f32x4_t*>(dst + e) = (f32x4_t){v[e] * inv, v[e + 1] * inv, v[e + 2] * inv, v[e + 3] * inv};
             } else {
                 uint32_t x[VPT / 2];
 #pragma unroll

@@ -102,10 +102,10 @@ __device__ __forceinline__ void store_spans(uint32_t* span_s, const TreeAttnArgs
     for (int j = i + THREADS; j < t.n_nodes; j += THREADS) span_s[SPANS_BEFORE + j] = w(a.spans + t.node0 + j);
     static_assert(THREADS >= SPANS_BEFORE && SPANS_BEFORE >= SPANS_BEHIND, "one pass");
 }
-// Those of a lane's keys k0 + 16 c + 4 (lane / 16) + r.
+// Those of a lane's keys k0 + 16 c + 4 (lane / 16) + r (blocks far before the nodes: of other cached rows, which are alike).
 template <int C>
 __device__ __forceinline__ void key_spans(uint32_t (&key)[C][4], const Work& t, int k0, const uint32_t* span_s) {
-    const uint32_t* from = span_s + SPANS_BEFORE + k0 + 4 * (threadIdx.x % 64 / 16) - t.n_ctx;
+    const uint32_t* from = span_s + max(SPANS_BEFORE + k0 - t.n_ctx, 0) + 4 * (threadIdx.x % 64 / 16);
 #pragma unroll
     for (int c = 0; c < C; ++c)
 #pragma unroll

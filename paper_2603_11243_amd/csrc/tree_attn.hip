@@ -14,11 +14,11 @@ namespace ssd {
 // transposing ds_read_b64_tr_b16): keys 4g .. 4g + 3 and 16 + 4g .. of 32 are the scores of lane group g and its operand of the second product alike.
 // The maximum that the exponents refer to may lag behind the true one by 2^LAG: it is raised (and the output rescaled) only by a score
 // beyond that, which spares nearly every block the exchange between lanes and the rescaling.  Probabilities enter the second product in
-// the type of the cache, their sum does not: half a step of the type each, as the output's own rounding.  IEEE half holds them times
-// 2^BIAS, so that those down to 2^-31 of the largest count (2^(BIAS + LAG) is in its range); bfloat16 has the range of fp32, and there they
-// stay below 1 so that values near its end do not overflow the sums.
-constexpr float LAG = 8.f;
-template <bool BF> constexpr float BIAS = BF ? -LAG : 6.f;
+// two pieces of the cache's type, rounded and what the rounding left, where the output has one; their sum is of the fp32 ones.  bfloat16: 16 bits of each;
+// it has the range of fp32, and they stay below 1.  IEEE half holds them times 2^BIAS (2^(BIAS + LAG) is in its range): 22 bits of those down to 2^-14 of the largest,
+// and of smaller ones the bits down to 2^-36 of it, below what fp32 sums keep.
+template <bool BF> constexpr float LAG = BF ? 8.f : 4.f;
+template <bool BF> constexpr float BIAS = BF ? -LAG<BF> : 11.f;
 
 // Pairs of 16-bit values w, as whole numbers (a magnitude plus TO_SIGN reaches the sign bit from the infinities on):
 template <bool BF> constexpr uint32_t TO_SIGN = BF ? 0x00800080u : 0x04000400u;
@@ -44,10 +44,21 @@ template <bool BF> __device__ __forceinline__ uint32_t pack16(float lo, float hi
     if constexpr (BF) return __builtin_bit_cast(uint32_t, __builtin_convertvector(v, bf16x2_t));
     else return __builtin_bit_cast(uint32_t, __builtin_convertvector(v, f16x2_t));
 }
+// What the rounding of two values to the pair w left of them, exact in fp32, as another pair.
+template <bool BF> __device__ __forceinline__ uint32_t rest16(float lo, float hi, uint32_t w) {
+    if constexpr (BF) return pack16<BF>(lo - __uint_as_float(w << 16), hi - __uint_as_float(w & 0xffff0000u));
+    else {
+        const f16x2_t h = __builtin_bit_cast(f16x2_t, w);
+        return pack16<BF>(lo - (float)h.x, hi - (float)h.y);
+    }
+}
 
-// Scores of 32 keys to weights in the operand type; maxima, sums and outputs follow.
+// Weights in the operand type: rounded ones and the rest of each.
+struct Weights { f16x8_t top, rest; };
+
+// Scores of 32 keys to weights; maxima, sums and outputs follow.
 template <bool BF, int NT, int DT>
-__device__ __forceinline__ void weights_of(f32x4_t (&s)[NT][2], float (&m)[NT], float (&l)[NT], f32x4_t (&o)[NT][DT], float sc, f16x8_t (&pf)[NT]) {
+__device__ __forceinline__ void weights_of(f32x4_t (&s)[NT][2], float (&m)[NT], float (&l)[NT], f32x4_t (&o)[NT][DT], float sc, Weights (&p)[NT]) {
     float mx[NT];
     bool above = false;
 #pragma unroll
@@ -55,7 +66,7 @@ __device__ __forceinline__ void weights_of(f32x4_t (&s)[NT][2], float (&m)[NT], 
         mx[n] = -INFINITY;
 #pragma unroll
         for (int c = 0; c < 2; ++c) mx[n] = fmaxf(mx[n], fmaxf(fmaxf(s[n][c][0], s[n][c][1]), fmaxf(s[n][c][2], s[n][c][3])));
-        above |= (mx[n] - m[n]) * sc > LAG;
+        above |= (mx[n] - m[n]) * sc > LAG<BF>;
     }
     if (__any(above)) {
 #pragma unroll
@@ -72,7 +83,7 @@ __device__ __forceinline__ void weights_of(f32x4_t (&s)[NT][2], float (&m)[NT], 
 #pragma unroll
     for (int n = 0; n < NT; ++n) {
         const float base = fminf(BIAS<BF> - m[n] * sc, F32_MOST);    // (finite: a score may be -infinity)
-        uint32_t pw[4];
+        uint32_t pw[4], rw[4];
 #pragma unroll
         for (int c = 0; c < 2; ++c) {
             f32x4_t& x = s[n][c];
@@ -81,10 +92,14 @@ __device__ __forceinline__ void weights_of(f32x4_t (&s)[NT][2], float (&m)[NT], 
                 x[r] = __builtin_amdgcn_exp2f(fmaf(x[r], sc, base));
                 l[n] += x[r];
             }
-            pw[2 * c] = pack16<BF>(x[0], x[1]);
-            pw[2 * c + 1] = pack16<BF>(x[2], x[3]);
+#pragma unroll
+            for (int e = 0; e < 2; ++e) {
+                pw[2 * c + e] = pack16<BF>(x[2 * e], x[2 * e + 1]);
+                rw[2 * c + e] = rest16<BF>(x[2 * e], x[2 * e + 1], pw[2 * c + e]);
+            }
         }
-        pf[n] = as_f16x8(make_uint4(pw[0], pw[1], pw[2], pw[3]));
+        p[n].top = as_f16x8(make_uint4(pw[0], pw[1], pw[2], pw[3]));
+        p[n].rest = as_f16x8(make_uint4(rw[0], rw[1], rw[2], rw[3]));
     }
 }
 
@@ -148,7 +163,7 @@ __device__ __forceinline__ bool any_nan(const f32x4_t (&o)[NT][DT]) {
 // O^T += V^T P^T over the 32 value rows at v, four 16-dim tiles at a time (read as in read_keys, for the same reason).  Transposing read: lane i of 16 passes row i / 4 and dims 4 (i % 4) .. + 3 of a
 // 16-dim tile, lane j receives dim j of four rows.
 template <bool BF, int HD, int NT, bool MASKED>
-__device__ __forceinline__ void add_values(const unsigned char* v, const f16x8_t (&pf)[NT], f32x4_t (&o)[NT][HD / 16], bool careful) {
+__device__ __forceinline__ void add_values(const unsigned char* v, const Weights (&p)[NT], f32x4_t (&o)[NT][HD / 16], bool careful) {
     constexpr int ROW = HD * 2;
     const int lane = threadIdx.x % 64, kg = lane / 16, dc = lane % 16;
     const int v_row = 4 * kg + dc / 4, v_low = (dc % 4) / 2;
@@ -171,9 +186,9 @@ __device__ __forceinline__ void add_values(const unsigned char* v, const f16x8_t
                          "s_waitcnt lgkmcnt(0)"
                          : "=&v"(vf[0][0]), "=&v"(vf[0][1]), "=&v"(vf[1][0]), "=&v"(vf[1][1]), "=&v"(vf[2][0]), "=&v"(vf[2][1]), "=&v"(vf[3][0]), "=&v"(vf[3][1])
                          : "v"(at[0]), "v"(at[1]), "v"(at[2]), "v"(at[3]) : "memory");
-        // A value that is not finite reaches the rows that do not see it as 0 times infinity, a NaN that stays.  A pass that ends with one is repeated with care:
-        // where a block holds such values the products run on the others, and two more count the infinities of either sign (a NaN as both) that rows
-        // with a probability meet.
+        // A value that is not finite reaches the rows that do not see it as 0 times infinity, and those that see it as the sum of its products with both pieces of
+        // a probability: a NaN that stays.  A pass that ends with one is repeated with care: where a block holds such values the products run on the
+        // others, and two more count the infinities of either sign (a NaN as both) that rows with a probability meet.
         uint32_t odd = 0;
         if (MASKED && careful) {
 #pragma unroll
@@ -182,12 +197,6 @@ __device__ __forceinline__ void add_values(const unsigned char* v, const f16x8_t
                 for (int e = 0; e < 2; ++e) odd |= beyond_of<BF>(vf[i][e].x) | beyond_of<BF>(vf[i][e].y);
         }
         if (MASKED && careful && __any(odd & SIGNS)) {
-            f16x8_t there[NT];
-#pragma unroll
-            for (int n = 0; n < NT; ++n) {
-                const uint4 x = __builtin_bit_cast(uint4, pf[n]);
-                there[n] = as_f16x8(make_uint4(one_where<BF>(not_zero(x.x)), one_where<BF>(not_zero(x.y)), one_where<BF>(not_zero(x.z)), one_where<BF>(not_zero(x.w))));
-            }
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
                 __builtin_amdgcn_sched_barrier(0);           // (one after the other: registers, not speed)
@@ -196,7 +205,10 @@ __device__ __forceinline__ void add_values(const unsigned char* v, const f16x8_t
                 const f16x8_t down = as_f16x8(make_uint4(infinite_of<BF>(x.x, ~0u), infinite_of<BF>(x.y, ~0u), infinite_of<BF>(y.x, ~0u), infinite_of<BF>(y.y, ~0u)));
 #pragma unroll
                 for (int n = 0; n < NT; ++n) {
-                    const f32x4_t zero = {0.f, 0.f, 0.f, 0.f}, u = mfma_16x16x32<BF>(up, there[n], zero), d = mfma_16x16x32<BF>(down, there[n], zero);
+                    const uint4 t = __builtin_bit_cast(uint4, p[n].top), e = __builtin_bit_cast(uint4, p[n].rest);
+                    const f16x8_t there = as_f16x8(make_uint4(one_where<BF>(not_zero(t.x) | not_zero(e.x)), one_where<BF>(not_zero(t.y) | not_zero(e.y)),
+                                                              one_where<BF>(not_zero(t.z) | not_zero(e.z)), one_where<BF>(not_zero(t.w) | not_zero(e.w))));
+                    const f32x4_t zero = {0.f, 0.f, 0.f, 0.f}, u = mfma_16x16x32<BF>(up, there, zero), d = mfma_16x16x32<BF>(down, there, zero);
 #pragma unroll
                     for (int r = 0; r < 4; ++r) o[n][g + i][r] += (u[r] > 0.f ? INFINITY : 0.f) - (d[r] > 0.f ? INFINITY : 0.f);
                 }
@@ -208,7 +220,10 @@ __device__ __forceinline__ void add_values(const unsigned char* v, const f16x8_t
         for (int i = 0; i < 4; ++i) {
             const f16x8_t x = __builtin_bit_cast(f16x8_t, __builtin_shufflevector(vf[i][0], vf[i][1], 0, 1, 2, 3));
 #pragma unroll
-            for (int n = 0; n < NT; ++n) o[n][g + i] = mfma_16x16x32<BF>(x, pf[n], o[n][g + i]);
+            for (int n = 0; n < NT; ++n) {
+                o[n][g + i] = mfma_16x16x32<BF>(x, p[n].top, o[n][g + i]);
+                o[n][g + i] = mfma_16x16x32<BF>(x, p[n].rest, o[n][g + i]);
+            }
         }
     }
 }
@@ -259,8 +274,7 @@ __global__ void __launch_bounds__(64 * KEY_WAVES, 2) tree_keys16_kernel(TreeAttn
     const int kvh = blockIdx.x;
     const int R = t.n_nodes * a.group;
     const int last = max(t.k0, t.k1 - 1);                    // (a range without keys: any row)
-    const int n_spans = t.k1 > t.n_ctx ? t.n_nodes : 0;
-    const uint32_t span = (int)threadIdx.x < n_spans ? w(a.spans + t.node0 + (int)threadIdx.x) : 0u;
+    const uint32_t span = (int)threadIdx.x < t.n_nodes ? w(a.spans + t.node0 + (int)threadIdx.x) : 0u;
     const int stride2 = (int)a.slot_stride * 2;
     const int64_t first = (int64_t)t.slot0 * a.slot_stride + kvh * a.head_stride;
     const uint16_t* kbase = (const uint16_t*)a.k + first;
@@ -297,11 +311,11 @@ __global__ void __launch_bounds__(64 * KEY_WAVES, 2) tree_keys16_kernel(TreeAttn
     const float sc = scale_of(a);
     float m[NT], l[NT];
     f32x4_t o[NT][DT];
-    if (n_spans) store_spans<64 * KEY_WAVES>(span_s, a, w, t, span);
+    store_spans<64 * KEY_WAVES>(span_s, a, w, t, span);
     lds_barrier();
     uint32_t mine[NT];
 #pragma unroll
-    for (int n = 0; n < NT; ++n) mine[n] = span_s[SPANS_BEFORE + node_of(a, min(t.row0 + 16 * n + dc, R - 1))];           // (not read without node keys)
+    for (int n = 0; n < NT; ++n) mine[n] = span_s[SPANS_BEFORE + node_of(a, min(t.row0 + 16 * n + dc, R - 1))];
     bool careful = false;
     auto block = [&](auto masked_c, int k0) __attribute__((always_inline)) {
         constexpr bool MASKED = decltype(masked_c)::value;
@@ -328,7 +342,7 @@ __global__ void __launch_bounds__(64 * KEY_WAVES, 2) tree_keys16_kernel(TreeAttn
                     for (int r = 0; r < 4; ++r) s[n][c][r] = sees(mine[n], key[c][r]) ? s[n][c][r] : -INFINITY;
             }
         }
-        f16x8_t p[NT];
+        Weights p[NT];
         weights_of<BF, NT, DT>(s, m, l, o, sc, p);
         __builtin_amdgcn_sched_barrier(0);
         __builtin_amdgcn_s_waitcnt(0x0F70 | K_LOADS);        // the values of this block have landed (a wavefront reads its own only)
@@ -341,12 +355,13 @@ __global__ void __launch_bounds__(64 * KEY_WAVES, 2) tree_keys16_kernel(TreeAttn
     for (;;) {
         start<NT, DT>(m, l, o);
         int k0 = k_first;
-        for (; k0 + KEYS <= min(t.n_ctx, t.k1); k0 += STEP) block(std::false_type(), k0);
+        if (!careful)
+            for (; k0 + KEYS <= min(t.n_ctx, t.k1); k0 += STEP) block(std::false_type(), k0);
         for (; k0 < t.k1; k0 += STEP) block(std::true_type(), k0);
         __builtin_amdgcn_sched_barrier(0);
         __builtin_amdgcn_s_waitcnt(0x0F70);                  // the values behind the last block: they land where the output goes
         __builtin_amdgcn_sched_barrier(0);
-        if (careful || t.k1 <= t.n_ctx || !any_nan<NT, DT>(o)) break;
+        if (careful || !any_nan<NT, DT>(o)) break;
         careful = true;
         load_keys(k_first);
         load_values(k_first);
@@ -374,8 +389,7 @@ __global__ void __launch_bounds__(64 * ROW_WAVES, 2) tree_rows16_kernel(TreeAttn
     const int kvh = blockIdx.x;
     const int R = t.n_nodes * a.group;
     const int last = max(t.k0, t.k1 - 1), row0 = t.row0 + wave * 16 * NT;
-    const int n_spans = t.k1 > t.n_ctx ? t.n_nodes : 0;
-    const uint32_t span = (int)threadIdx.x < n_spans ? w(a.spans + t.node0 + (int)threadIdx.x) : 0u;
+    const uint32_t span = (int)threadIdx.x < t.n_nodes ? w(a.spans + t.node0 + (int)threadIdx.x) : 0u;
     const int stride2 = (int)a.slot_stride * 2;
     const int64_t first = (int64_t)t.slot0 * a.slot_stride + kvh * a.head_stride;
     const uint16_t* kbase = (const uint16_t*)a.k + first;
@@ -396,11 +410,11 @@ __global__ void __launch_bounds__(64 * ROW_WAVES, 2) tree_rows16_kernel(TreeAttn
     load_queries<HD, NT>(qf, a, t, kvh, row0);
     load(t.k0, 0);
     load(t.k0 + KEYS, 1);
-    if (n_spans) store_spans<64 * ROW_WAVES>(span_s, a, w, t, span);
+    store_spans<64 * ROW_WAVES>(span_s, a, w, t, span);
     lds_barrier();
     uint32_t mine[NT];
 #pragma unroll
-    for (int n = 0; n < NT; ++n) mine[n] = span_s[SPANS_BEFORE + node_of(a, min(row0 + 16 * n + dc, R - 1))];             // (not read without node keys)
+    for (int n = 0; n < NT; ++n) mine[n] = span_s[SPANS_BEFORE + node_of(a, min(row0 + 16 * n + dc, R - 1))];
     const float sc = scale_of(a);
     float m[NT], l[NT];
     f32x4_t o[NT][DT];
@@ -430,7 +444,7 @@ __global__ void __launch_bounds__(64 * ROW_WAVES, 2) tree_rows16_kernel(TreeAttn
                     for (int r = 0; r < 4; ++r) s[n][c][r] = sees(mine[n], key[c][r]) ? s[n][c][r] : -INFINITY;
             }
         }
-        f16x8_t p[NT];
+        Weights p[NT];
         weights_of<BF, NT, DT>(s, m, l, o, sc, p);
         add_values<BF, HD, NT, MASKED>(v, p, o, careful);
     };
@@ -449,13 +463,13 @@ __global__ void __launch_bounds__(64 * ROW_WAVES, 2) tree_rows16_kernel(TreeAttn
     for (;;) {
         start<NT, DT>(m, l, o);
         int stage = 0, k0 = t.k0;
-        for (; k0 + KEYS <= min(t.n_ctx, t.k1); k0 += KEYS, stage ^= 1) block(std::false_type(), k0, stage);
+        if (!careful)
+            for (; k0 + KEYS <= min(t.n_ctx, t.k1); k0 += KEYS, stage ^= 1) block(std::false_type(), k0, stage);
         for (; k0 < t.k1; k0 += KEYS, stage ^= 1) block(std::true_type(), k0, stage);
         __builtin_amdgcn_sched_barrier(0);
         __builtin_amdgcn_s_waitcnt(0x0F70);                  // nothing lands in LDS after the end
         __builtin_amdgcn_sched_barrier(0);
-        if (careful || t.k1 <= t.n_ctx) break;
-        if (!__syncthreads_or(live && any_nan<NT, DT>(o))) break;
+        if (careful || !__syncthreads_or(live && any_nan<NT, DT>(o))) break;
         careful = true;
         load(t.k0, 0);
         load(t.k0 + KEYS, 1);

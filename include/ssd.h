@@ -393,8 +393,9 @@ size_t ssd_tree_workspace_bytes(const ssd_ctx *ctx, int n_q_heads, int n_kv_head
  *          head of exp(s_j - lse), is added to the entries of cached rows and stored to those of node rows (they are new); no other
  *          entry is touched.  The slots of different utterances must then be distinct.
  * Scores, sums and statistics are fp32; with 16-bit caches a weight enters the second product as two values of the cache's type: 16 bits of it with bfloat16,
- * 22 with IEEE half, there of weights below 2^-14 of the row's largest those down to 2^-36 of it (smaller ones count for nothing).  A seen infinite
- * value is the output of its column for a row to which it counts; infinities of both signs and NaN give NaN.
+ * 22 with IEEE half, there of weights below 2^-14 of the row's largest those down to 2^-36 of it.  Values may lie anywhere in their type's range (beside
+ * outputs that sums of them would take out of fp32's range, those below 2^-90 lose bits).  A seen infinite value is the output of its column unless its weight is
+ * below 2^-87 (IEEE half: 2^-36) of the row's largest: then it may count for nothing; infinities of both signs and NaN give NaN.
  * A row that a node does not see has no influence on it, whatever it holds.  An utterance without nodes is skipped, ctx_len may be 0.
  * Calls of this section may be captured: replays read the arrays of the captured call, not later ones, and use its workspace, so that two of them
  * that share a workspace must not run at the same time.  Errors: SSD_EINVAL, SSD_ESHAPE (more than 65535 utterances, or tiles of 16, 64 or 128

@@ -112,12 +112,43 @@ __device__ __forceinline__ void key_spans(uint32_t (&key)[C][4], const Work& t, 
         for (int r = 0; r < 4; ++r) key[c][r] = from[16 * c + r];
 }
 
+// Weights times values near the end of fp32's range (bfloat16 has the same) can leave it in the sum over many keys, though the division by the sum of
+// the weights would bring it back.  A pass with such an output is repeated, in the rows that have one, with weights 2^-DOWN of theirs: 2^30 keys of weight 2^-DOWN
+// sum up to 1/2.  Wavefronts and pieces are joined as means with shares of 1 in all, which stay inside.
+constexpr float DOWN = 31.f;
+__device__ __forceinline__ float lifted(float l, float down) { return down > 0.f ? l * 0x1p31f : l; }
+
+// Rows of a wavefront's output with an infinity or NaN; whether there are any.
+template <int NT, int DT>
+__device__ __forceinline__ bool not_finite(const f32x4_t (&o)[NT][DT], bool (&odd)[NT]) {
+    bool any = false;
+#pragma unroll
+    for (int n = 0; n < NT; ++n) {
+        float t = 0.f;
+#pragma unroll
+        for (int i = 0; i < DT; ++i)
+#pragma unroll
+            for (int r = 0; r < 4; ++r) t = fmaf(o[n][i][r], 0.f, t);
+        odd[n] = t != t;
+        any |= odd[n];
+    }
+    if (!__any(any)) return false;
+#pragma unroll
+    for (int n = 0; n < NT; ++n) {
+        int x = odd[n];
+        x |= __shfl_xor(x, 16);
+        x |= __shfl_xor(x, 32);
+        odd[n] = x != 0;
+    }
+    return true;
+}
+
 // The end of an attention workgroup: its wavefronts hold, for 16 NT rows, maxima m (raw scores), sums l (a lane's share) and outputs o[n][i] (row
-// 16 n + lane % 16, dims 16 i + 4 (lane / 16) ..) relative to 2^(m sc - bias).  DPASS dims of all rows at a time go through LDS (buf: 16 HD floats a wavefront,
-// the 16-byte chunks of a row permuted by its number); every thread adds VPT values of a row and stores them, or the sums of a piece.
+// 16 n + lane % 16, dims 16 i + 4 (lane / 16) ..) relative to 2^(m sc - bias + down).  DPASS dims of all rows at a time go through LDS (buf: 16 HD floats a wavefront,
+// the 16-byte chunks of a row permuted by its number) as means; every thread adds VPT values of a row, each by its wavefront's share of the weights, and stores them.
 template <int DT, int HD, int NT, int WAVES>
 __device__ __forceinline__ void merge_wavefronts(const TreeAttnArgs& a, const Work& t, int kvh, const float (&m)[NT], float (&l)[NT], const f32x4_t (&o)[NT][HD / 16],
-                                                 float sc, float bias, float* buf, float2* ml_s) {
+                                                 const float (&down)[NT], float sc, float bias, float* buf, float2* ml_s) {
     typedef Elem<DT> E;
     constexpr int TR = 16 * NT, DPASS = 16 * HD / TR, VPT = TR * DPASS / (64 * WAVES), TPR = 64 * WAVES / TR;      // values of a thread, threads of a row
     const int lane = threadIdx.x % 64, kg = lane / 16, dc = lane % 16, wave = threadIdx.x / 64;
@@ -126,7 +157,8 @@ __device__ __forceinline__ void merge_wavefronts(const TreeAttnArgs& a, const Wo
     for (int n = 0; n < NT; ++n) {
         l[n] += __shfl_xor(l[n], 16);
         l[n] += __shfl_xor(l[n], 32);
-        if (kg == 0) ml_s[wave * TR + 16 * n + dc] = make_float2(m[n], l[n]);
+        if (kg == 0) ml_s[wave * TR + 16 * n + dc] = make_float2(m[n], lifted(l[n], down[n]));
+        l[n] = l[n] == 0.f ? 0.f : 1.f / l[n];               // (nothing seen, nothing added)
     }
     static_assert(VPT == 2 || VPT == 4 || VPT == 8, "values of a thread");
     constexpr int CH = DPASS / 4;                            // chunks of a row
@@ -141,7 +173,7 @@ __device__ __forceinline__ void merge_wavefronts(const TreeAttnArgs& a, const Wo
 #pragma unroll
             for (int i = 0; i < DPASS / 16; ++i) {
                 const int r = 16 * n + dc, c = 4 * i + kg;
-                *reinterpret_cast<f32x4_t*>(buf + (wave * TR + r) * DPASS + (c ^ (r & (CH - 1))) * 4) = o[n][pass * (DPASS / 16) + i];
+                *reinterpret_cast<f32x4_t*>(buf + (wave * TR + r) * DPASS + (c ^ (r & (CH - 1))) * 4) = o[n][pass * (DPASS / 16) + i] * l[n];
             }
         __syncthreads();
         if (pass == 0) {
@@ -150,9 +182,12 @@ __device__ __forceinline__ void merge_wavefronts(const TreeAttnArgs& a, const Wo
 #pragma unroll
             for (int u = 0; u < WAVES; ++u) {
                 const float2 x = ml_s[u * TR + orow];
-                w[u] = x.y == 0.f ? 0.f : __builtin_amdgcn_exp2f((x.x - mt) * sc);
-                lt = fmaf(x.y, w[u], lt);
+                w[u] = x.y == 0.f ? 0.f : x.y * __builtin_amdgcn_exp2f((x.x - mt) * sc);
+                lt += w[u];
             }
+            const float inv = 1.f / lt;
+#pragma unroll
+            for (int u = 0; u < WAVES; ++u) w[u] *= inv;
         }
         float v[VPT];
 #pragma unroll
@@ -168,17 +203,16 @@ __device__ __forceinline__ void merge_wavefronts(const TreeAttnArgs& a, const Wo
 #pragma unroll
             for (int e = 0; e < VPT; ++e) dst[e] = v[e];
         } else {
-            const float inv = 1.f / lt;
             typename E::type* dst = (typename E::type*)a.out + (row_at(a, t, kvh, row)) * a.head_dim + dim;
             if constexpr (DT == SSD_F32) {                   // (head_dim is a multiple of 4 and may end among a thread's 8 values)
                 static_assert(VPT % 4 == 0, "groups of four");
 #pragma unroll
                 for (int e = 0; e < VPT; e += 4)
-                    if (dim + e < a.head_dim) *reinterpret_cast<f32x4_t*>(dst + e) = (f32x4_t){v[e] * inv, v[e + 1] * inv, v[e + 2] * inv, v[e + 3] * inv};
+                    if (dim + e < a.head_dim) *reinterpret_cast<f32x4_t*>(dst + e) = (f32x4_t){v[e], v[e + 1], v[e + 2], v[e + 3]};
             } else {
                 uint32_t x[VPT / 2];
 #pragma unroll
-                for (int e = 0; e < VPT; e += 2) x[e / 2] = op_pack2<DT == SSD_BF16>(v[e] * inv, v[e + 1] * inv);
+                for (int e = 0; e < VPT; e += 2) x[e / 2] = op_pack2<DT == SSD_BF16>(v[e], v[e + 1]);
                 if constexpr (VPT == 8) *reinterpret_cast<uint4*>(dst) = make_uint4(x[0], x[1], x[2], x[3]);
                 else if constexpr (VPT == 4) *reinterpret_cast<uint2*>(dst) = make_uint2(x[0], x[1]);
                 else *reinterpret_cast<uint32_t*>(dst) = x[0];
@@ -191,8 +225,8 @@ __device__ __forceinline__ void merge_wavefronts(const TreeAttnArgs& a, const Wo
     }
 }
 
-// The pieces of a long context joined.  A workgroup has a query row: groups of HD / 4 lanes take its pieces in turn, each with a running maximum, and
-// are joined through LDS: 48 rows of 8 heads in 64 pieces 5.7 us (one lane a dim over all pieces: 125, the pieces' latencies one after the other).
+// The pieces of a long context, a mean of values each, joined.  A workgroup has a query row: groups of HD / 4 lanes take its pieces in turn, each with a running
+// maximum and mean, and are joined through LDS: 48 rows of 8 heads in 64 pieces 5.7 us (one lane a dim over all pieces: 125, the pieces' latencies one after the other).
 template <int DT, int HD, class M>
 __global__ void __launch_bounds__(256) tree_join_kernel(TreeAttnArgs a, M w, float bias) {
     typedef Elem<DT> E;
@@ -224,10 +258,11 @@ __global__ void __launch_bounds__(256) tree_join_kernel(TreeAttnArgs a, M w, flo
 #pragma unroll
         for (int u = 0; u < U; ++u) {
             if (p0 + u * GROUPS >= n_parts || y[u].y == 0.f) continue;                     // (a piece whose keys no row of the tile sees)
-            const float top = fmaxf(m, y[u].x), old = __builtin_amdgcn_exp2f((m - top) * sc), now = __builtin_amdgcn_exp2f((y[u].x - top) * sc);
+            const float top = fmaxf(m, y[u].x), old = l * __builtin_amdgcn_exp2f((m - top) * sc), now = y[u].y * __builtin_amdgcn_exp2f((y[u].x - top) * sc);
             m = top;
-            l = l * old + y[u].y * now;
-            v = v * old + z[u] * now;
+            l = old + now;
+            const float inv = 1.f / l;
+            v = v * (old * inv) + z[u] * (now * inv);
         }
     }
     o_s[group][dim / 4] = v;
@@ -238,19 +273,21 @@ __global__ void __launch_bounds__(256) tree_join_kernel(TreeAttnArgs a, M w, flo
 #pragma unroll
     for (int g = 0; g < GROUPS; ++g) mt = fmaxf(mt, ml_s[g].x);
     f32x4_t s = {0.f, 0.f, 0.f, 0.f};
+    float f[GROUPS];
 #pragma unroll
     for (int g = 0; g < GROUPS; ++g) {
         const float2 y = ml_s[g];
-        const float f = y.y == 0.f ? 0.f : __builtin_amdgcn_exp2f((y.x - mt) * sc);
-        lt += y.y * f;
-        s += o_s[g][dim / 4] * f;
+        f[g] = y.y == 0.f ? 0.f : y.y * __builtin_amdgcn_exp2f((y.x - mt) * sc);
+        lt += f[g];
     }
+    const float inv = 1.f / lt;
+#pragma unroll
+    for (int g = 0; g < GROUPS; ++g) s += o_s[g][dim / 4] * (f[g] * inv);
     const int64_t at = row_at(a, t, kvh, row);
     typename E::type* dst = (typename E::type*)a.out + at * a.head_dim + dim;
-    const float inv = 1.f / lt;
     if (dim < a.head_dim)
 #pragma unroll
-        for (int e = 0; e < 4; ++e) dst[e] = E::put(s[e] * inv);
+        for (int e = 0; e < 4; ++e) dst[e] = E::put(s[e]);
     if (a.lse && dim == 0) a.lse[at] = (mt * sc - bias + __builtin_amdgcn_logf(lt)) * LN2;
 }
 

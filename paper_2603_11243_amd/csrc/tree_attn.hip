@@ -15,10 +15,13 @@ namespace ssd {
 // The maximum that the exponents refer to may lag behind the true one by 2^LAG: it is raised (and the output rescaled) only by a score
 // beyond that, which spares nearly every block the exchange between lanes and the rescaling.  Probabilities enter the second product in
 // two pieces of the cache's type, rounded and what the rounding left, where the output has one; their sum is of the fp32 ones.  bfloat16: 16 bits of each;
-// it has the range of fp32, and they stay below 1.  IEEE half holds them times 2^BIAS (2^(BIAS + LAG) is in its range): 22 bits of those down to 2^-14 of the largest,
+// it has the range of fp32, and they are at most 1.  IEEE half holds them times 2^BIAS (2^(BIAS + LAG) is in its range): 22 bits of those down to 2^-14 of the largest,
 // and of smaller ones the bits down to 2^-36 of it, below what fp32 sums keep.
 template <bool BF> constexpr float LAG = BF ? 8.f : 4.f;
 template <bool BF> constexpr float BIAS = BF ? -LAG<BF> : 11.f;
+
+// Passes at most: as it is; with care for values that are not finite; of bfloat16 with smaller weights in rows that are not finite still.
+template <bool BF> constexpr int TURNS = BF ? 3 : 2;
 
 // Pairs of 16-bit values w, as whole numbers (a magnitude plus TO_SIGN reaches the sign bit from the infinities on):
 template <bool BF> constexpr uint32_t TO_SIGN = BF ? 0x00800080u : 0x04000400u;
@@ -58,7 +61,7 @@ struct Weights { f16x8_t top, rest; };
 
 // Scores of 32 keys to weights; maxima, sums and outputs follow.
 template <bool BF, int NT, int DT>
-__device__ __forceinline__ void weights_of(f32x4_t (&s)[NT][2], float (&m)[NT], float (&l)[NT], f32x4_t (&o)[NT][DT], float sc, Weights (&p)[NT]) {
+__device__ __forceinline__ void weights_of(f32x4_t (&s)[NT][2], float (&m)[NT], float (&l)[NT], f32x4_t (&o)[NT][DT], float sc, const float (&down)[NT], Weights (&p)[NT]) {
     float mx[NT];
     bool above = false;
 #pragma unroll
@@ -82,7 +85,7 @@ __device__ __forceinline__ void weights_of(f32x4_t (&s)[NT][2], float (&m)[NT], 
     }
 #pragma unroll
     for (int n = 0; n < NT; ++n) {
-        const float base = fminf(BIAS<BF> - m[n] * sc, F32_MOST);    // (finite: a score may be -infinity)
+        const float base = fminf(BIAS<BF> - down[n] - m[n] * sc, F32_MOST);    // (finite: a score may be -infinity)
         uint32_t pw[4], rw[4];
 #pragma unroll
         for (int c = 0; c < 2; ++c) {
@@ -146,20 +149,6 @@ __device__ __forceinline__ void start(float (&m)[NT], float (&l)[NT], f32x4_t (&
     }
 }
 
-// Whether a wavefront's output holds a NaN.
-template <int NT, int DT>
-__device__ __forceinline__ bool any_nan(const f32x4_t (&o)[NT][DT]) {
-    bool bad = false;
-#pragma unroll
-    for (int n = 0; n < NT; ++n)
-#pragma unroll
-        for (int i = 0; i < DT; ++i) {
-            const float sum = (o[n][i][0] + o[n][i][1]) + (o[n][i][2] + o[n][i][3]);      // (of infinities of both signs: one more pass for nothing)
-            bad |= sum != sum;
-        }
-    return __any(bad);
-}
-
 // O^T += V^T P^T over the 32 value rows at v, four 16-dim tiles at a time (read as in read_keys, for the same reason).  Transposing read: lane i of 16 passes row i / 4 and dims 4 (i % 4) .. + 3 of a
 // 16-dim tile, lane j receives dim j of four rows.
 template <bool BF, int HD, int NT, bool MASKED>
@@ -187,7 +176,7 @@ __device__ __forceinline__ void add_values(const unsigned char* v, const Weights
                          : "=&v"(vf[0][0]), "=&v"(vf[0][1]), "=&v"(vf[1][0]), "=&v"(vf[1][1]), "=&v"(vf[2][0]), "=&v"(vf[2][1]), "=&v"(vf[3][0]), "=&v"(vf[3][1])
                          : "v"(at[0]), "v"(at[1]), "v"(at[2]), "v"(at[3]) : "memory");
         // A value that is not finite reaches the rows that do not see it as 0 times infinity, and those that see it as the sum of its products with both pieces of
-        // a probability: a NaN that stays.  A pass that ends with one is repeated with care: where a block holds such values the products run on the
+        // a probability: a NaN that stays.  A pass whose output is not finite is repeated with care: where a block holds such values the products run on the
         // others, and two more count the infinities of either sign (a NaN as both) that rows with a probability meet.
         uint32_t odd = 0;
         if (MASKED && careful) {
@@ -309,7 +298,7 @@ __global__ void __launch_bounds__(64 * KEY_WAVES, 2) tree_keys16_kernel(TreeAttn
     load_queries<HD, NT>(qf, a, t, kvh, t.row0);
     load_values(k_first);
     const float sc = scale_of(a);
-    float m[NT], l[NT];
+    float m[NT], l[NT], down[NT] = {};
     f32x4_t o[NT][DT];
     store_spans<64 * KEY_WAVES>(span_s, a, w, t, span);
     lds_barrier();
@@ -343,7 +332,7 @@ __global__ void __launch_bounds__(64 * KEY_WAVES, 2) tree_keys16_kernel(TreeAttn
             }
         }
         Weights p[NT];
-        weights_of<BF, NT, DT>(s, m, l, o, sc, p);
+        weights_of<BF, NT, DT>(s, m, l, o, sc, down, p);
         __builtin_amdgcn_sched_barrier(0);
         __builtin_amdgcn_s_waitcnt(0x0F70 | K_LOADS);        // the values of this block have landed (a wavefront reads its own only)
         __builtin_amdgcn_sched_barrier(0);
@@ -352,7 +341,7 @@ __global__ void __launch_bounds__(64 * KEY_WAVES, 2) tree_keys16_kernel(TreeAttn
         __builtin_amdgcn_sched_barrier(0);
         load_values(k0 + STEP);
     };
-    for (;;) {
+    for (int turn = 1;; ++turn) {
         start<NT, DT>(m, l, o);
         int k0 = k_first;
         if (!careful)
@@ -361,12 +350,16 @@ __global__ void __launch_bounds__(64 * KEY_WAVES, 2) tree_keys16_kernel(TreeAttn
         __builtin_amdgcn_sched_barrier(0);
         __builtin_amdgcn_s_waitcnt(0x0F70);                  // the values behind the last block: they land where the output goes
         __builtin_amdgcn_sched_barrier(0);
-        if (careful || !any_nan<NT, DT>(o)) break;
+        bool odd[NT];
+        if (turn == TURNS<BF> || !not_finite(o, odd)) break;
+        if (careful)
+#pragma unroll
+            for (int n = 0; n < NT; ++n) down[n] = odd[n] ? DOWN : 0.f;
         careful = true;
         load_keys(k_first);
         load_values(k_first);
     }
-    merge_wavefronts<BF ? SSD_BF16 : SSD_F16, HD, NT, KEY_WAVES>(a, t, kvh, m, l, o, sc, BIAS<BF>, reinterpret_cast<float*>(v_s), ml_s);
+    merge_wavefronts<BF ? SSD_BF16 : SSD_F16, HD, NT, KEY_WAVES>(a, t, kvh, m, l, o, down, sc, BIAS<BF>, reinterpret_cast<float*>(v_s), ml_s);
 }
 
 // ---- many query rows: a wavefront has 16 NT of a K/V head for itself, the ROW_WAVES of a workgroup share 64-key blocks of keys and values in LDS, two of them
@@ -416,7 +409,7 @@ __global__ void __launch_bounds__(64 * ROW_WAVES, 2) tree_rows16_kernel(TreeAttn
 #pragma unroll
     for (int n = 0; n < NT; ++n) mine[n] = span_s[SPANS_BEFORE + node_of(a, min(row0 + 16 * n + dc, R - 1))];
     const float sc = scale_of(a);
-    float m[NT], l[NT];
+    float m[NT], l[NT], down[NT] = {};
     f32x4_t o[NT][DT];
     bool careful = false;
     const bool live = row0 < R;
@@ -445,7 +438,7 @@ __global__ void __launch_bounds__(64 * ROW_WAVES, 2) tree_rows16_kernel(TreeAttn
             }
         }
         Weights p[NT];
-        weights_of<BF, NT, DT>(s, m, l, o, sc, p);
+        weights_of<BF, NT, DT>(s, m, l, o, sc, down, p);
         add_values<BF, HD, NT, MASKED>(v, p, o, careful);
     };
     auto block = [&](auto masked_c, int k0, int stage) __attribute__((always_inline)) {
@@ -460,7 +453,7 @@ __global__ void __launch_bounds__(64 * ROW_WAVES, 2) tree_rows16_kernel(TreeAttn
         lds_barrier();                                       // all wavefronts are done with the block
         load(k0 + 2 * KEYS, stage);
     };
-    for (;;) {
+    for (int turn = 1;; ++turn) {
         start<NT, DT>(m, l, o);
         int stage = 0, k0 = t.k0;
         if (!careful)
@@ -469,7 +462,11 @@ __global__ void __launch_bounds__(64 * ROW_WAVES, 2) tree_rows16_kernel(TreeAttn
         __builtin_amdgcn_sched_barrier(0);
         __builtin_amdgcn_s_waitcnt(0x0F70);                  // nothing lands in LDS after the end
         __builtin_amdgcn_sched_barrier(0);
-        if (careful || !__syncthreads_or(live && any_nan<NT, DT>(o))) break;
+        bool odd[NT];
+        if (turn == TURNS<BF> || !__syncthreads_or(live && not_finite(o, odd))) break;
+        if (careful && live)
+#pragma unroll
+            for (int n = 0; n < NT; ++n) down[n] = odd[n] ? DOWN : 0.f;
         careful = true;
         load(t.k0, 0);
         load(t.k0 + KEYS, 1);
@@ -482,13 +479,14 @@ __global__ void __launch_bounds__(64 * ROW_WAVES, 2) tree_rows16_kernel(TreeAttn
         const int r = 16 * n + dc, row = row0 + r;
         if (row >= R) continue;
         const int64_t at = row_at(a, t, kvh, row);
+        const float inv = 1.f / l[n];                        // (a piece whose keys this row does not see: not used)
+        l[n] = lifted(l[n], down[n]);
         if (t.index < a.n_parts) {
             const int64_t part = ((int64_t)t.index * a.n_kv_heads + kvh) * TR + wave * 16 * NT + r;
 #pragma unroll
-            for (int i = 0; i < DT; ++i) *reinterpret_cast<f32x4_t*>(a.part_o + part * HD + 16 * i + 4 * kg) = o[n][i];
+            for (int i = 0; i < DT; ++i) *reinterpret_cast<f32x4_t*>(a.part_o + part * HD + 16 * i + 4 * kg) = o[n][i] * inv;
             if (kg == 0) a.part_ml[part] = make_float2(m[n], l[n]);
         } else {
-            const float inv = 1.f / l[n];
 #pragma unroll
             for (int i = 0; i < DT; ++i)
                 *reinterpret_cast<uint2*>((uint16_t*)a.out + at * HD + 16 * i + 4 * kg) = make_uint2(op_pack2<BF>(o[n][i][0] * inv, o[n][i][1] * inv), op_pack2<BF>(o[n][i][2] * inv, o[n][i][3] * inv));

@@ -54,8 +54,8 @@ __global__ void __launch_bounds__(64 * KEY_WAVES, 2) tree_attn32_kernel(TreeAttn
             __builtin_amdgcn_raw_ptr_buffer_load_lds(rsrc, (lds_void_t*)(v_s[wave] + i * 1024), 16, off, 0, 0, 0);
         }
     };
-    int k0 = t.k0 + wave * TREE32_KEYS;
-    load_keys(k0);
+    const int k_first = t.k0 + wave * TREE32_KEYS;
+    load_keys(k_first);
     f32x4_t qf[NT][DT];
     const float sign = a.scale < 0.f ? -1.f : a.scale == 0.f ? 0.f : 1.f;
 #pragma unroll
@@ -66,111 +66,119 @@ __global__ void __launch_bounds__(64 * KEY_WAVES, 2) tree_attn32_kernel(TreeAttn
         for (int c = 0; c < DT; ++c) qf[n][c] *= sign;
     }
     const float sc = scale_of(a);
-    float m[NT], l[NT];
+    float m[NT], l[NT], down[NT] = {};
     f32x4_t o[NT][DT];
-#pragma unroll
-    for (int n = 0; n < NT; ++n) {
-        m[n] = -F32_MOST;
-        l[n] = 0.f;
-#pragma unroll
-        for (int i = 0; i < DT; ++i) o[n][i] = (f32x4_t){0.f, 0.f, 0.f, 0.f};
-    }
     __syncthreads();
-    load_values(k0);
+    load_values(k_first);
     const float* vr = reinterpret_cast<const float*>(v_s[wave]);
-    for (; k0 < t.k1; k0 += STEP) {
-        f32x4_t s[NT];
+    for (int turn = 1;; ++turn) {
 #pragma unroll
         for (int n = 0; n < NT; ++n) {
-            s[n] = (f32x4_t){0.f, 0.f, 0.f, 0.f};
+            m[n] = -F32_MOST;
+            l[n] = 0.f;
 #pragma unroll
-            for (int c = 0; c < DT; ++c)
-#pragma unroll
-                for (int e = 0; e < 4; ++e) s[n] = mfma_16x16x4(kr[c][e], qf[n][c][e], s[n]);
+            for (int i = 0; i < DT; ++i) o[n][i] = (f32x4_t){0.f, 0.f, 0.f, 0.f};
         }
-        const bool masked = k0 + TREE32_KEYS > min(t.n_ctx, t.k1);
-        if (masked) {
-            uint32_t key[1][4];
-            key_spans<1>(key, t, k0, span_s);
+        for (int k0 = k_first; k0 < t.k1; k0 += STEP) {
+            f32x4_t s[NT];
 #pragma unroll
             for (int n = 0; n < NT; ++n) {
-                const uint32_t mine = span_s[SPANS_BEFORE + node_of(a, min(t.row0 + 16 * n + dc, R - 1))];
+                s[n] = (f32x4_t){0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-                for (int r = 0; r < 4; ++r) s[n][r] = sees(mine, key[0][r]) ? s[n][r] : -INFINITY;
+                for (int c = 0; c < DT; ++c)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) s[n] = mfma_16x16x4(kr[c][e], qf[n][c][e], s[n]);
             }
-        }
-        bool above = false;
-        float mx[NT];
-#pragma unroll
-        for (int n = 0; n < NT; ++n) {
-            mx[n] = fmaxf(fmaxf(s[n][0], s[n][1]), fmaxf(s[n][2], s[n][3]));
-            above |= mx[n] > m[n];
-        }
-        if (__any(above)) {
-#pragma unroll
-            for (int n = 0; n < NT; ++n) {
-                float top = fmaxf(mx[n], __shfl_xor(mx[n], 16));
-                top = fmaxf(m[n], fmaxf(top, __shfl_xor(top, 32)));
-                const float alpha = __builtin_amdgcn_exp2f((m[n] - top) * sc);
-                m[n] = top;
-                l[n] *= alpha;
-#pragma unroll
-                for (int i = 0; i < DT; ++i) o[n][i] *= alpha;
-            }
-        }
-#pragma unroll
-        for (int n = 0; n < NT; ++n) {
-            const float base = fminf(-m[n] * sc, F32_MOST);
-#pragma unroll
-            for (int r = 0; r < 4; ++r) {
-                s[n][r] = __builtin_amdgcn_exp2f(fmaf(s[n][r], sc, base));
-                l[n] += s[n][r];
-            }
-        }
-        __builtin_amdgcn_sched_barrier(0);
-        __builtin_amdgcn_s_waitcnt(0x0F70);
-        __builtin_amdgcn_sched_barrier(0);
-        load_keys(k0 + STEP);
-        // A value that is not finite would reach the rows that do not see it as 0 times infinity: as in tree_attn.hip, the products run on the
-        // others, and two more count the infinities of either sign (a NaN as both) that rows with a probability meet.
-#pragma unroll
-        for (int i = 0; i < DT; ++i) {
-            float v[4];
-            bool odd = false;
-#pragma unroll
-            for (int r = 0; r < 4; ++r) {
-                v[r] = vr[(4 * kg + r) * HD + ((16 * i + dc) ^ (kg * 16))];
-                odd |= !(fabsf(v[r]) <= F32_MOST);
-            }
-            if (masked && __any(odd)) {
+            const bool masked = k0 + TREE32_KEYS > min(t.n_ctx, t.k1);
+            if (masked) {
+                uint32_t key[1][4];
+                key_spans<1>(key, t, k0, span_s);
 #pragma unroll
                 for (int n = 0; n < NT; ++n) {
-                    f32x4_t up = {0.f, 0.f, 0.f, 0.f}, down = up;
+                    const uint32_t mine = span_s[SPANS_BEFORE + node_of(a, min(t.row0 + 16 * n + dc, R - 1))];
 #pragma unroll
-                    for (int r = 0; r < 4; ++r) {
-                        const float there = s[n][r] > 0.f || s[n][r] != s[n][r] ? 1.f : 0.f;
-                        up = mfma_16x16x4(!(v[r] <= F32_MOST) ? 1.f : 0.f, there, up);
-                        down = mfma_16x16x4(!(v[r] >= -F32_MOST) ? 1.f : 0.f, there, down);
-                    }
-#pragma unroll
-                    for (int r = 0; r < 4; ++r) o[n][i][r] += (up[r] > 0.f ? INFINITY : 0.f) - (down[r] > 0.f ? INFINITY : 0.f);
+                    for (int r = 0; r < 4; ++r) s[n][r] = sees(mine, key[0][r]) ? s[n][r] : -INFINITY;
                 }
+            }
+            bool above = false;
+            float mx[NT];
 #pragma unroll
-                for (int r = 0; r < 4; ++r) v[r] = fabsf(v[r]) <= F32_MOST ? v[r] : 0.f;
+            for (int n = 0; n < NT; ++n) {
+                mx[n] = fmaxf(fmaxf(s[n][0], s[n][1]), fmaxf(s[n][2], s[n][3]));
+                above |= mx[n] > m[n];
+            }
+            if (__any(above)) {
+#pragma unroll
+                for (int n = 0; n < NT; ++n) {
+                    float top = fmaxf(mx[n], __shfl_xor(mx[n], 16));
+                    top = fmaxf(m[n], fmaxf(top, __shfl_xor(top, 32)));
+                    const float alpha = __builtin_amdgcn_exp2f((m[n] - top) * sc);
+                    m[n] = top;
+                    l[n] *= alpha;
+#pragma unroll
+                    for (int i = 0; i < DT; ++i) o[n][i] *= alpha;
+                }
             }
 #pragma unroll
-            for (int n = 0; n < NT; ++n)
+            for (int n = 0; n < NT; ++n) {
+                const float base = fminf(-down[n] - m[n] * sc, F32_MOST);
 #pragma unroll
-                for (int r = 0; r < 4; ++r) o[n][i] = mfma_16x16x4(v[r], s[n][r], o[n][i]);
+                for (int r = 0; r < 4; ++r) {
+                    s[n][r] = __builtin_amdgcn_exp2f(fmaf(s[n][r], sc, base));
+                    l[n] += s[n][r];
+                }
+            }
+            __builtin_amdgcn_sched_barrier(0);
+            __builtin_amdgcn_s_waitcnt(0x0F70);
+            __builtin_amdgcn_sched_barrier(0);
+            load_keys(k0 + STEP);
+            // A value that is not finite would reach the rows that do not see it as 0 times infinity: as in tree_attn.hip, the products run on the
+            // others, and two more count the infinities of either sign (a NaN as both) that rows with a probability meet.
+#pragma unroll
+            for (int i = 0; i < DT; ++i) {
+                float v[4];
+                bool odd = false;
+#pragma unroll
+                for (int r = 0; r < 4; ++r) {
+                    v[r] = vr[(4 * kg + r) * HD + ((16 * i + dc) ^ (kg * 16))];
+                    odd |= !(fabsf(v[r]) <= F32_MOST);
+                }
+                if ((masked || turn > 1) && __any(odd)) {
+#pragma unroll
+                    for (int n = 0; n < NT; ++n) {
+                        f32x4_t up = {0.f, 0.f, 0.f, 0.f}, below = up;
+#pragma unroll
+                        for (int r = 0; r < 4; ++r) {
+                            const float there = s[n][r] > 0.f || s[n][r] != s[n][r] ? 1.f : 0.f;
+                            up = mfma_16x16x4(!(v[r] <= F32_MOST) ? 1.f : 0.f, there, up);
+                            below = mfma_16x16x4(!(v[r] >= -F32_MOST) ? 1.f : 0.f, there, below);
+                        }
+#pragma unroll
+                        for (int r = 0; r < 4; ++r) o[n][i][r] += (up[r] > 0.f ? INFINITY : 0.f) - (below[r] > 0.f ? INFINITY : 0.f);
+                    }
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) v[r] = fabsf(v[r]) <= F32_MOST ? v[r] : 0.f;
+                }
+#pragma unroll
+                for (int n = 0; n < NT; ++n)
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) o[n][i] = mfma_16x16x4(v[r], s[n][r], o[n][i]);
+            }
+            __builtin_amdgcn_s_waitcnt(0xC07F);                  // the reads of this block are done
+            __builtin_amdgcn_sched_barrier(0);
+            load_values(k0 + STEP);
         }
-        __builtin_amdgcn_s_waitcnt(0xC07F);                  // the reads of this block are done
         __builtin_amdgcn_sched_barrier(0);
-        load_values(k0 + STEP);
+        __builtin_amdgcn_s_waitcnt(0x0F70);                      // the values behind the last block: they land where the output goes
+        __builtin_amdgcn_sched_barrier(0);
+        bool odd[NT];
+        if (turn == 2 || !not_finite(o, odd)) break;
+#pragma unroll
+        for (int n = 0; n < NT; ++n) down[n] = odd[n] ? DOWN : 0.f;
+        load_keys(k_first);
+        load_values(k_first);
     }
-    __builtin_amdgcn_sched_barrier(0);
-    __builtin_amdgcn_s_waitcnt(0x0F70);                      // the values behind the last block: they land where the output goes
-    __builtin_amdgcn_sched_barrier(0);
-    merge_wavefronts<SSD_F32, HD, NT, KEY_WAVES>(a, t, kvh, m, l, o, sc, 0.f, reinterpret_cast<float*>(v_s), ml_s);
+    merge_wavefronts<SSD_F32, HD, NT, KEY_WAVES>(a, t, kvh, m, l, o, down, sc, 0.f, reinterpret_cast<float*>(v_s), ml_s);
 }
 
 constexpr int MASS32_ROWS = 64;

@@ -97,3 +97,46 @@ def test_an_infinite_value_is_the_output_of_its_column(dtype, heads, ctx_len, no
     assert np.array_equal(got[odd], want[odd], equal_nan=True)
     # (columns that hold an infinity elsewhere: _exact took it into account where it is seen, the rest is as before)
     assert (abs(got[~odd] - want[~odd]) <= tol[~odd]).all()
+
+
+def _alike(dtype, heads, ctx_len, trees, seed):
+    """Every key counts the same."""
+    c = Call(dtype, heads, ctx_len, trees, seed=seed)
+    c.q.zero_()
+    return c
+
+
+ENDS = [("bf16", (16, 8, 128)), ("bf16", (4, 2, 64)), ("f32", (4, 2, 64)), ("f32", (2, 2, 100)), ("f16", (4, 2, 128))]
+
+
+@pytest.mark.parametrize("dtype, heads", ENDS)
+@pytest.mark.parametrize("ctx_len, nodes", [([300, 700], [1, 6]), ([515, 40], [40, 3]), ([900, 2], [3, 100]), ([20000, 30], [2, 5]), ([9000, 3000], [40, 70])])
+@pytest.mark.parametrize("signs", ["one", "both"])
+def test_means_of_values_near_the_end_of_the_range(dtype, heads, ctx_len, nodes, signs):
+    """Sums of many of them are beyond fp32's range, their means are not."""
+    c = _alike(dtype, heads, ctx_len, _batch(58, None, nodes, ("random", "chain")), 58)
+    size = torch.rand(c.v.shape, generator=torch.Generator().manual_seed(59)).cuda() * 0.05 + 0.9
+    if signs == "both":
+        size *= torch.sign(torch.randn(c.v.shape, generator=torch.Generator().manual_seed(60)).cuda())
+    c.v[:] = (size * torch.finfo(c.dtype).max).to(c.dtype)
+    _check(c, mass=False)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("at_the_end", [0.94, float("inf"), float("nan")])
+def test_small_values_beside_rows_near_the_end_of_the_range(dtype, at_the_end):
+    """Rows that see values near the end of the range, or infinities, beside rows that see small ones: the latter notice nothing."""
+    left, right = 600, 5
+    parent = [-1] + list(range(left - 1)) + [-1] + list(range(left, left + right - 1))
+    c = _alike(dtype, (2, 1, 128), [40], [parent], 61)
+    c.v[:] = (c.v.float() * 2.0 ** -110).to(c.dtype)
+    first = int(c.kv_start[0]) + 40
+    c.v[first:first + left] = 0
+    want = c.run(mass=False)[left:].clone()
+    out, tol = _exact(c, 1.0)
+    assert (abs(want.double().cpu().numpy() - out[left:]) <= tol[left:]).all()
+    c.v[first:first + left] = at_the_end * torch.finfo(c.dtype).max
+    got = c.run(mass=False)
+    assert torch.equal(got[left:], want)
+    if at_the_end < 1:
+        assert torch.isfinite(got).all() and (got[left - 1].float() > 0.8 * torch.finfo(c.dtype).max).all()

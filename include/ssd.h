@@ -363,8 +363,9 @@ int accept_prefix(ssd_ctx *ctx, const void *h_verify, const int32_t *draft_ids /
  * A node sees every cached row, its ancestors and itself.
  *
  * The rows of a cache, the library's own (ssd_kv_cache_view) or any other: row `slot` of K/V head h of layer l begins at element
- * l * layer_stride + slot * slot_stride + h * head_stride of k and of v, and its head_dim elements are consecutive.  Rows must not share
- * memory, every row begins at a multiple of 16 bytes, 64 slots are less than 2 GiB apart.  slots <= 2^30.
+ * l * layer_stride + slot * slot_stride + h * head_stride of k and of v, and its head_dim elements are consecutive.  Slots,
+ * heads and layers may lie inside each other in any order; rows must not share memory, every row begins at a multiple of 16 bytes, 64 slots are less than 2 GiB
+ * apart.  slots <= 2^30.
  * dtype SSD_F16 or SSD_BF16: head_dim 64 or 128; SSD_F32: a multiple of 4 up to 128 (SSD_ESHAPE otherwise). */
 #define SSD_MAX_TREE_NODES 1024
 typedef struct {

@@ -1354,15 +1354,18 @@ int check_view(ssd_ctx* c, const char* what, const ssd_kv_view* v) {
     const int64_t ss = v->slot_stride, hs = v->head_stride, ls = L > 1 ? v->layer_stride : 0;
     if (((uintptr_t)v->k | (uintptr_t)v->v) & 15 || ss % unit || hs % unit || ls % unit)
         return fail(c, SSD_EINVAL, "%s: rows of a cache must begin at multiples of 16 bytes", what);
-    // slots inside a head or heads inside a slot; then layers
     const int64_t top = (int64_t)1 << 42;                    // (no product below leaves 64 bits)
     if (ss < hd || ss > top || hs > top || ls > top || (H > 1 && hs < hd)) return fail(c, SSD_EINVAL, "%s: strides of a cache", what);
-    const bool heads_inside = H == 1 || hs * (H - 1) + hd <= ss;
-    if (!heads_inside && hs / ss < v->slots - 1) return fail(c, SSD_EINVAL, "%s: rows of a cache share memory", what);
-    if (!heads_inside && hs < (v->slots - 1) * ss + hd) return fail(c, SSD_EINVAL, "%s: rows of a cache share memory", what);
     if (ss * (int64_t)kv_elem(v->dtype) >= (int64_t)1 << 25) return fail(c, SSD_ESHAPE, "%s: 64 slots of a cache are 2 GiB apart or more", what);
-    const int64_t layer = (H - 1) * hs + (v->slots - 1) * ss + hd;
-    if (L > 1 && ls < layer) return fail(c, SSD_EINVAL, "%s: layers of a cache share memory", what);
+    // slots, heads and layers may lie inside each other in any order: from the smallest stride on, each holds what is inside it
+    struct Dim { int64_t stride, n; } dim[3] = {{ss, v->slots}, {hs, H}, {ls, L}};
+    std::sort(dim, dim + 3, [](const Dim& x, const Dim& y) { return x.stride < y.stride; });
+    int64_t inside = hd;
+    for (const Dim& d : dim) {
+        if (d.n == 1) continue;
+        if (d.stride < inside) return fail(c, SSD_EINVAL, "%s: rows of a cache share memory", what);
+        inside += d.stride * (d.n - 1);
+    }
     return SSD_OK;
 }
 

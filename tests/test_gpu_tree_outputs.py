@@ -3,6 +3,7 @@ import numpy as np
 import pytest
 import torch
 
+from paper_2603_11243_amd.binding import Context
 from tests import test_gpu_verify_tree as rounds
 from tests.test_gpu_tree_attention import Call, _batch
 from workloads.configs import ModelCfg
@@ -50,3 +51,28 @@ def test_rounds_of_fp32_models_of_any_head_dim(head_dim, monkeypatch):
     cfg = ModelCfg(n_layers=2, d_model=96, n_q_heads=4, n_kv_heads=2, head_dim=head_dim, d_ff=128, vocab=512, dtype="f32")
     monkeypatch.setitem(rounds.MODELS, "f32_any", (cfg, "f16"))
     rounds.test_rounds("f32_any", [40, 3, 100, 64], [9, 1, 20, 16])
+
+
+@pytest.mark.parametrize("dtype", [torch.float16, torch.float32])
+def test_eviction_between_caches_of_any_order(dtype):
+    """Slots outside with the layers inside them, heads outside, layers outside: the rows that caches of the usual order get, and nothing around them."""
+    L, H, hd, n, keep = 3, 2, 64, [70, 33], [20, 9]
+    g = torch.Generator().manual_seed(45)
+    k, v = (torch.randn(L, 110, H, hd, generator=g).to(dtype).cuda() for _ in range(2))
+    mass = torch.rand(L, H, 110, generator=g).cuda()
+    ctx = Context(device="cuda:0")
+    ctx.reserve(evict_rows=sum(keep), evict_utts=2, evict_heads=(L, H))
+    results = []
+    for order in ((0, 1, 2), (1, 0, 2), (2, 0, 1), (2, 1, 0)):
+        back = [order.index(i) for i in range(3)] + [3]
+        lay = lambda x: x.permute(*order, 3).contiguous().permute(back)
+        k_out, v_out = (lay(torch.full((L, 40, H, hd), 7.0, dtype=dtype, device="cuda")) for _ in range(2))
+        rows = ctx.kv_evict(lay(k), lay(v), mass, [0, 75], n, keep, 3, 5, k_out, v_out, [4, 28], want_rows=True)
+        torch.cuda.synchronize()
+        results.append((rows, k_out.clone(), v_out.clone()))
+    for r in results[1:]:
+        assert all(torch.equal(x, y) for x, y in zip(r, results[0]))
+    left = torch.ones(40, dtype=torch.bool)
+    left[4:24] = left[28:37] = False
+    assert (results[0][1][:, left.cuda()] == 7).all() and not (results[0][1][:, ~left.cuda()] == 7).all(-1).any()
+    ctx.close()

@@ -385,6 +385,7 @@ size_t ssd_tree_workspace_bytes(const ssd_ctx *ctx, int n_q_heads, int n_kv_head
 
 /* Attention of all nodes (Eq. 4 for the nodes of a tree).  Per node i and query head h (its K/V head is h / (n_q_heads / n_kv_heads)), over
  * the rows j that the node sees:  s_j = scale q . k_j;  lse = log sum_j exp s_j;  out = sum_j exp(s_j - lse) v_j.
+ *   scale  any for which scale * log2(e) is finite
  *   q      dev, row cu_nodes[b] + i begins at element (cu_nodes[b] + i) * q_stride: n_q_heads * head_dim elements of the cache's type
  *          (q and q_stride multiples of 16 bytes); must not overlap out
  *   kv     one layer (n_layers 1)
@@ -437,7 +438,7 @@ int kv_evict(ssd_ctx *ctx, const ssd_kv_view *from /*host*/, const float *mass, 
  * unless rows have been evicted.  kv_mass: dev [n_layers, n_kv_heads, slots] or NULL, updated as by tree_attention in every layer.
  * h_tree: dev [cu_nodes[B], d_model], the final-RMSNormed hidden row of every node in the type of verify_forward's h_verify.
  * ctx_len[b] may be 0; the slot ranges of different utterances must be distinct.
- * Workspace of both calls: ssd_verify_tree_workspace_bytes.  Errors as for verify_forward_kv. */
+ * Workspace of both calls: ssd_verify_tree_workspace_bytes.  Errors as for verify_forward_kv and tree_attention. */
 size_t ssd_verify_tree_workspace_bytes(const ssd_ctx *ctx, int64_t max_nodes, int64_t max_utts);
 int verify_tree(ssd_ctx *ctx, const int32_t *node_ids /*dev*/, int B, const int32_t *cu_nodes /*host*/, const int32_t *parent /*host*/,
                 const int32_t *kv_start /*host*/, const int32_t *ctx_len /*host*/, const int32_t *pos0 /*host or NULL*/, float *kv_mass, void *h_tree);

@@ -1708,7 +1708,7 @@ int tree_attention(ssd_ctx* ctx, const void* q, int64_t q_stride, int n_q_heads,
     if (kv->n_layers != 1) return fail(ctx, SSD_EINVAL, "tree_attention: a cache of one layer is needed (got %d)", kv->n_layers);
     if (n_q_heads <= 0 || n_q_heads % kv->n_kv_heads) return fail(ctx, SSD_ESHAPE, "tree_attention: n_q_heads must be a multiple of n_kv_heads");
     if (n_q_heads > 65535 || n_q_heads / kv->n_kv_heads > 512) return fail(ctx, SSD_ESHAPE, "tree_attention: more than 65535 query heads, or 512 per K/V head");
-    if (!std::isfinite(scale)) return fail(ctx, SSD_EINVAL, "tree_attention: scale is not finite");
+    if (!std::isfinite(scale * 1.4426950408889634f)) return fail(ctx, SSD_EINVAL, "tree_attention: scale is not finite, or not to base 2");
     if (N == 0) return SSD_OK;
     if (!q || !out) return fail(ctx, SSD_EINVAL, "tree_attention: NULL data pointer");
     if (q_stride < dq || q_stride > (int64_t)1 << 32 || q_stride * es % 16 || ((uintptr_t)q | (uintptr_t)out) & 15)

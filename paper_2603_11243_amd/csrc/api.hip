@@ -1875,6 +1875,7 @@ int verify_tree(ssd_ctx* ctx, const int32_t* node_ids, int B, const int32_t* cu_
     if (rc == SSD_OK) rc = check_trees(ctx, "verify_tree", B, cu_nodes, parent, most);
     if (rc == SSD_OK) rc = check_places(ctx, "verify_tree", B, kv_start, ctx_len, cu_nodes, ctx->kv_slots, true);
     if (rc != SSD_OK) return rc;
+    if (m.n_q_heads / m.n_kv_heads > 512) return fail(ctx, SSD_ESHAPE, "verify_tree: more than 512 query heads per K/V head");
     const int64_t N = cu_nodes[B];
     if (N == 0) return SSD_OK;
     if (!node_ids || !h_tree) return fail(ctx, SSD_EINVAL, "verify_tree: NULL data pointer");

@@ -176,6 +176,10 @@ class TwoPhaseDecoder:
         return plan_batches(lengths, self.budget, padded=False) if len(lengths) else []
 
     def run(self, tau_slm: float) -> dict:
+        with torch.cuda.stream(self.ctx.stream):             # what is copied to the host waits for the calls before it, whichever stream is current
+            return self._run(tau_slm)
+
+    def _run(self, tau_slm):
         ctx, wl, n_steps = self.ctx, self.wl, self.n_steps
         # ---- gate (Sec. 2.1) over everything
         g = ctx.ctc_gate(self.logits, self.cu_frames, wl.blank_id, wl.tau_ctc, out=self.gate_out)

@@ -34,7 +34,8 @@ class TreeFallback:
     it, once as if that token had replaced the draft's (substitution), once as if it had come before it (insertion) and once as if one more had been
     left out (deletion), common beginnings shared, goes through verify_tree; accept_tree keeps the longest branch whose tokens pass tau and moves its rows
     behind the context; the model's choice behind it begins the next round.  From tau 0.5 on a token that passes is the model's own choice, and the
-    result that of ar_fallback.
+    result that of ar_fallback up to the first near-tie: the two passes add in another order, and of two tokens whose likelihoods differ by no more
+    than that either may be chosen.
 
     most_rows: contexts longer than that are cut between rounds by kv_evict to keep_rows rows (three quarters of it unless given): the first n_first and last
     n_recent ones stay, of the others those of the largest attention weight here.  They go to two caches of the fallback's own in turn; the rows

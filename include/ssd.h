@@ -347,7 +347,7 @@ int ssd_plan_batches(const int32_t *lengths, int n, int64_t max_tokens, int padd
 /* Sec. 2.2-2.3 (Eq. 5, definition of j, Eq. 7).  draft_logp[r] = log softmax(lm_head . h_verify[r])
  * at token draft_ids[r]; the logits are never written to memory.  Token i passes iff
  * draft_logp > ln(tau_slm), evaluated in fp32 with ln(tau_slm) rounded from double (tau_slm <= 0
- * accepts everything).  accept_len[b] = j - 1 where j is the first failing token, or U if none;
+ * accepts every likelihood above -infinity).  accept_len[b] = j - 1 where j is the first failing token, or U if none;
  * all_accepted[b] = (accept_len[b] == U).  greedy_tok (optional, NULL to skip) receives the
  * lowest-index argmax over the vocabulary at every row: the token greedy decoding would emit there. */
 int accept_prefix(ssd_ctx *ctx, const void *h_verify, const int32_t *draft_ids /*dev*/,
@@ -407,7 +407,7 @@ int tree_attention(ssd_ctx *ctx, const void *q /*dev*/, int64_t q_stride, int n_
                    const int32_t *parent /*host [cu_nodes[B]]*/, float scale, void *out, float *lse, float *mass);
 
 /* Eq. 5 and the definition of j (Sec. 2.3) for the nodes of a tree: a node passes iff node_logp > ln(tau) (fp32, as in accept_prefix; tau <= 0
- * accepts everything), and stands iff it and all its ancestors pass.  accept_node[b] is the deepest node that stands, the lowest number
+ * accepts every likelihood above -infinity), and stands iff it and all its ancestors pass.  accept_node[b] is the deepest node that stands, the lowest number
  * among equally deep ones (callers list the better continuation first), -1 if none does; accept_len[b] the number of nodes on its path;
  * path[cu_nodes[b] + d], d < accept_len[b], that path from the top, -1 behind it.  A NaN likelihood does not pass.
  * Errors: SSD_EINVAL, SSD_ESHAPE, SSD_EWORKSPACE (size: ssd_tree_workspace_bytes). */

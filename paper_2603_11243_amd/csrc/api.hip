@@ -1469,11 +1469,12 @@ void tree_spans(int n, const int32_t* parent, uint32_t* span) {
     }
 }
 // Query rows of an item of work: as many as the largest tree has, in one of the shapes of the kernels.  With 16 (fp32: 32) the wavefronts of a workgroup split the
-// keys; with 64 and 128 they split the rows and share the keys, which takes 32 rows over 300 keys in 13.6 us where a split of the keys takes 18.0.
-// 128 rows read the keys half as often: 90 utterances of 42 nodes, 24 heads on 8, over 1024 rows 113 us, with 64 rows 133 (64 nodes over 64 rows: 62.6 and 61.9).
+// keys; with 64 and 128 they split the rows and share the keys, which takes 32 rows over 150 keys in 38 utterances 14.0 us where a split of the keys takes 16.5 (over 300
+// keys 19.2 and 20.6).  128 rows read the keys half as often: 90 utterances of 42 nodes, 24 heads on 8, over 1024 rows 132 us, with 64 rows 148; where tiles are left with few
+// rows and contexts are short it is the other way (64 nodes over 64 rows 61.7 and 62.6, 48 over 220 75.8 and 72.7).
 int tree_tile_rows(int dtype, int rows) { return rows <= 16 ? 16 : dtype == SSD_F32 ? 32 : rows <= 64 ? 64 : 128; }
 // false: more items of work than a grid has rows.
-// Ranges of keys: one per item, unless that leaves most of the chip without work or an utterance is longer than its share; then pieces of such a share, at least
+// Ranges of keys: one per item, unless that leaves most of the chip without work or an utterance is longer than its share; then pieces of about such a share, which is at least
 // TREE_SPLIT_KEYS (a piece costs its partial results, 33 KB for 64 rows, written and read once: as much as 64 keys).  An utterance is cut into equal pieces, as many as
 // come nearest to the share: 57 utterances of 539 keys, 4 nodes, 8 fp32 heads, take 24.5 us whole and 50 in pieces of 512 and 27, 14 of them for joining.
 bool tree_work(int B, const int32_t* kv_start, const int32_t* ctx_len, const int32_t* cu_nodes, const int32_t* parent, int most, int n_q_heads, const ssd_kv_view& kv,

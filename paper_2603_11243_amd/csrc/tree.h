@@ -47,7 +47,7 @@ struct TreeAttnArgs {
 void launch_tree_attention(const TreeAttnArgs& a, const uint32_t* words, int n, const uint32_t* dev_words, hipStream_t st);
 constexpr int TREE_ITEMS = 65535;            // of a call: rows of a grid
 constexpr int TREE_WORKGROUPS = 512;         // long contexts are cut into about as many pieces in all, times K/V heads
-constexpr int TREE_SPLIT_KEYS = 512;         // a piece has at least as many keys
+constexpr int TREE_SPLIT_KEYS = 512;         // a share has at least as many keys, a piece of a cut context from three quarters of that on (its last one fewer)
 constexpr int TREE_MASS_KEYS = 128;          // and one of the weights a multiple of these
 
 // Words: the B + 1 prefix sums of the nodes (at most MAX_TREE_NODES an utterance); from `parents` on the nodes' parents inside their utterance or -1, 16

@@ -85,7 +85,7 @@ __device__ __forceinline__ Work mass_item_of(const TreeAttnArgs& a, const M& w, 
 
 constexpr int MASS_WAVES = 4;                // wavefronts of a workgroup of the weights
 // Wavefronts of a workgroup that split the keys.  Eight leave room for one workgroup a CU, four for two: 16 rows over 150 in 38 utterances, 16 heads on 8 of 128,
-// 14.8 and 9.6 us, one row over 106 6.0 and 5.3; 16 over 200000 146 and 149.
+// 12.2 and 8.5 us, one row over 106 5.4 and 4.5; 16 over 200000 163 and 164.
 constexpr int KEY_WAVES = 4;
 
 // Spans of the keys around the nodes in LDS: SPANS_BEFORE cached rows, the nodes, SPANS_BEHIND keys behind them, as far as a block with a node in it
@@ -226,7 +226,7 @@ __device__ __forceinline__ void merge_wavefronts(const TreeAttnArgs& a, const Wo
 }
 
 // The pieces of a long context, a mean of values each, joined.  A workgroup has a query row: groups of HD / 4 lanes take its pieces in turn, each with a running
-// maximum and mean, and are joined through LDS: 48 rows of 8 heads in 64 pieces 5.7 us (one lane a dim over all pieces: 125, the pieces' latencies one after the other).
+// maximum and mean, and are joined through LDS: 48 rows of 8 heads in 64 pieces 5.9 us (one lane a dim over all pieces: 125, the pieces' latencies one after the other).
 template <int DT, int HD, class M>
 __global__ void __launch_bounds__(256) tree_join_kernel(TreeAttnArgs a, M w, float bias) {
     typedef Elem<DT> E;

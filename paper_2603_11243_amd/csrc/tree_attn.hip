@@ -16,7 +16,8 @@ namespace ssd {
 // beyond that, which spares nearly every block the exchange between lanes and the rescaling.  Probabilities enter the second product in
 // two pieces of the cache's type, rounded and what the rounding left, where the output has one; their sum is of the fp32 ones.  bfloat16: 16 bits of each;
 // it has the range of fp32, and they are at most 1.  IEEE half holds them times 2^BIAS (2^(BIAS + LAG) is in its range): 22 bits of those down to 2^-14 of the largest,
-// and of smaller ones the bits down to 2^-36 of it, below what fp32 sums keep.
+// and of smaller ones the bits down to 2^-36 of it, below what fp32 sums keep.  The second piece costs 3 to 5 % with up to 64 rows a K/V head, 8 % in 90 trees of 48 nodes
+// over 220 rows (24 heads on 8: 70 -> 76 us) and 19 % where 120 rows share long contexts (200001 rows 174 -> 206), whose blocks wait for the matrix cores.
 template <bool BF> constexpr float LAG = BF ? 8.f : 4.f;
 template <bool BF> constexpr float BIAS = BF ? -LAG<BF> : 11.f;
 
@@ -246,9 +247,9 @@ __device__ __forceinline__ void lds_barrier() {
 
 // ---- few query rows: 16 of a K/V head a workgroup, whose wavefronts take the 32-key blocks of the range in turn, so that every cached row is read once,
 // and merge their (maximum, sum, output) through LDS.  Key rows come straight from memory in operand registers; a wavefront's values are its own
-// and need no barrier.  One token over 106 rows, 16 heads on 8: 5.3 us, the launch and three ways to memory and back one behind the other (words, keys and
-// queries, values); the kernel below, in which one wavefront has all 16 rows, takes 7.1, 155 in place of 149 over 200000 rows, and for
-// 38 utterances of 150 rows 9.0 in place of 9.6.
+// and need no barrier.  One token over 106 rows, 16 heads on 8: 4.5 us in a graph, the launch and three ways to memory and back one behind the other (words, keys
+// and queries, values); the kernel below, in which one wavefront has all 16 rows, takes 6.0, over 200000 rows 161 in place of 164 and for 38 utterances of 150 rows
+// 7.9 in place of 8.5.
 template <bool BF, int HD, class M>
 __global__ void __launch_bounds__(64 * KEY_WAVES, 2) tree_keys16_kernel(TreeAttnArgs a, M w) {
     constexpr int NT = 1, KEYS = 32, ROW = HD * 2, BLOCK = KEYS * ROW, STEP = KEYS * KEY_WAVES;
@@ -364,10 +365,10 @@ __global__ void __launch_bounds__(64 * KEY_WAVES, 2) tree_keys16_kernel(TreeAttn
 
 // ---- many query rows: a wavefront has 16 NT of a K/V head for itself, the ROW_WAVES of a workgroup share 64-key blocks of keys and values in LDS, two of them
 // in turn: the next one loads while this one is used.  Two workgroups a CU (LDS, and the registers of NT 2; NT 3 and 4 spill).
-// 48 rows over 200001 and 32 to 66 over 20000 to 40000 cached ones, 8 K/V heads of 128: 156 and 90 us, 5.2 and 5.4 TB/s, what memory gives.  96 to 192 rows over 100 to 340,
-// 90 utterances: 58 us, 2.7 TB/s; the vector ALU is 30 % busy, the matrix cores 12, LDS 2, and the rest is the few blocks of a workgroup one after
-// the other, a barrier at each end.  Four workgroups a CU on 32-key blocks (NT 1) take 62 there and 104 in place of 90 over the long ones; all reads of a block's values
-// at once, or two waits for them, the same.
+// 48 rows over 200001 and 32 to 66 over 20000 to 40000 cached ones, 8 K/V heads of 128: 160 and 94 us, 5.1 and 5.2 TB/s, what memory gives.  96 to 192 rows over 100 to 340,
+// 90 utterances: 64 us, 2.5 TB/s; the vector ALU is 31 % busy, the matrix cores 17, LDS 2, and the rest is the few blocks of a workgroup one after
+// the other, a barrier at each end.  With weights as one value (58 and 90 us) four workgroups a CU on 32-key blocks (NT 1) took 62 there and 104 over the long ones; all reads
+// of a block's values at once, or two waits for them, the same.
 constexpr int ROW_WAVES = 4;
 
 template <bool BF, int HD, int NT, class M>

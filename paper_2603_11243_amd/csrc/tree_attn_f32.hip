@@ -1,8 +1,8 @@
 // The same for fp32 caches, head_dim a multiple of 4 up to 128, on v_mfma_f32_16x16x4_f32 (fp32 products and sums): the layout of tree_attn.hip with
 // 16-key blocks.  A lane's four dims 16 c + 4 g .. of a key row are its elements of four products, in the same order for the queries; a
 // lane's scores of keys 4 g .. 4 g + 3 are its elements of the second product, key r of every group in product r.  Products and sums are
-// fp32 throughout, and every larger score raises the maximum.  Only the shape that splits the keys, with 16 or 32 rows: the fp32 models are small.  20 rows
-// over 70, 4 heads of 64, 4 utterances: 7.7 us (eight wavefronts 8.4), the launch and the chain words, keys, values, merge.
+// fp32 throughout, and every larger score raises the maximum: weights are at most 1, and rows whose sums leave the range are taken again with smaller ones.  Only the shape that splits the keys, with 16 or 32 rows: the fp32 models are small.  20 rows
+// over 70, 4 heads of 64, 4 utterances: 8.1 us (eight wavefronts were 0.7 slower), the launch and the chain words, keys, values, merge.
 #include "tree_attn.h"
 
 namespace ssd {

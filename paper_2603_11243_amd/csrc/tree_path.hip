@@ -8,7 +8,8 @@
 namespace ssd {
 
 // One workgroup a tree, one thread a node (NT of them).  Pointer jumping: after round r a node knows whether the 2^r nodes on the way up
-// from it pass, how many there are, and who comes next: ten rounds of LDS for 1024 nodes, where a walk up a chain is 1024.  24 nodes 2.9 us, 256
+// from it pass, how many there are, and who comes next: ten rounds of LDS for 1024 nodes.  The accepted path is then written by one thread that walks it up, a read of
+// LDS and a store a node (some ten of them in the cases timed; a chain of 1024 that passes is 1024).  24 nodes 2.9 us, 256
 // trees of 64 to 1000 nodes 6.9: a launch; the calls take 9 and 37 us, of which the host checks, packs and hands over the parents.
 template <int NT, class M>
 __global__ void __launch_bounds__(NT) tree_path_kernel(const float* __restrict__ logp, M w, int parents, float ln_tau, bool roots_given, int32_t* __restrict__ accept_len,
@@ -87,7 +88,8 @@ void launch_tree_scatter(const float* logp, const int32_t* greedy, const int32_t
 }
 
 // One thread a 16-byte column of an utterance's rows in a layer.  Step d moves row path[d] >= d to d, and path[d + 1] > path[d]: no row is written that a later step
-// reads, whatever the order of loads and stores, and no other thread touches the column.  Eight rows are requested at once.
+// reads, whatever the order of loads and stores, and no other thread touches the column.  Rows go eight at a time through an array that the compiler keeps in private memory
+// (144 bytes a lane).
 template <typename T>
 __device__ __forceinline__ void move_rows(T* col, int64_t stride, const int32_t* from, int n) {
     for (int d0 = 0; d0 < n; d0 += 8) {

@@ -31,8 +31,8 @@ def _exact(call, scale):
             kk, vv, qq = k[s0:s0 + n + N, kv], v[s0:s0 + n + N, kv], q[at]
             vv = np.where(np.isfinite(vv), vv, 0)
             s = np.where(seen, qq @ kk.T * scale, -np.inf)
-            d = ((hd + 4) * 2.0 ** -24 * abs(scale) * (abs(qq) @ abs(kk).T) * seen).max(1)[:, None] + 2.0 ** -22
-            p = np.exp(s - s.max(1, keepdims=True))
+            d = ((hd + 4) * 2.0 ** -24 * abs(scale) * (abs(qq) @ abs(kk).T) * seen).max(1, initial=0)[:, None] + 2.0 ** -22
+            p = np.exp(s - s.max(1, keepdims=True, initial=-np.inf))
             l = p.sum(1, keepdims=True)
             p /= l
             out[at] = p @ vv

@@ -45,7 +45,8 @@ enum ssd_status {
     SSD_EUNSUPPORTED = -5   /* dtype / feature not built                                             */
 };
 
-enum ssd_dtype { SSD_F32 = 0, SSD_BF16 = 1, SSD_F16 = 2 };   /* SSD_F16: rows of an ssd_kv_view only */
+enum ssd_dtype { SSD_F32 = 0, SSD_BF16 = 1, SSD_F16 = 2,     /* SSD_F16: rows of an ssd_kv_view, pages and their queries only */
+                 SSD_E4M3 = 3, SSD_I8 = 4 };                 /* elements of pages only (ssd_kv_pages) */
 /* Matrix-core operand type of an SSD_BF16 model (the paper's stack runs in bfloat16, Sec. 3.2).
  *   SSD_OP_F16  (default) activations are rounded to IEEE half (11 significant bits) where they enter a
  *               contraction; the bf16 weights are converted once to half times a per-tensor power of two
@@ -122,8 +123,11 @@ const char *ssd_last_error(const ssd_ctx *ctx);
  *                           (|v| > 65504 for IEEE half, or NaN) at one of the points where the fp32 pipeline
  *                           rounds to it (RMSNorm output, rotated q / k and v, SiLU(gate)*up, K/V-cache rows, the projector's values) and
  *                           was stored saturated to +-65504, or a log-likelihood came out non-finite.  Results of
- *                           calls since the last read are then not the model's: re-run in fp32 or rescale. */
-enum ssd_device_flag { SSD_FLAG_TOKEN_CLAMPED = 1, SSD_FLAG_ACT_OVERFLOW = 2 };
+ *                           calls since the last read are then not the model's: re-run in fp32 or rescale.
+ *                           kv_write_pages: a row that is not finite; kv_read_pages: a value beyond IEEE half, or of such a row
+ *   SSD_FLAG_BAD_PAGE       calls on pages: a page number, length or slot in device memory was out of range; what it concerns was left out
+ * A context without a model has the flags of the calls on pages only (none if it was created while its stream was captured). */
+enum ssd_device_flag { SSD_FLAG_TOKEN_CLAMPED = 1, SSD_FLAG_ACT_OVERFLOW = 2, SSD_FLAG_BAD_PAGE = 4 };
 int ssd_device_flags(ssd_ctx *ctx, int32_t *flags /*host*/);
 
 /* Measurement aid (no counterpart in the paper): times kernel launches with HIP events recorded on
@@ -452,6 +456,69 @@ int accept_tree(ssd_ctx *ctx, const void *h_tree, const int32_t *node_ids /*dev*
                 const int32_t *parent /*host*/, float tau_slm, const int32_t *kv_start /*host or NULL*/, const int32_t *ctx_len /*host*/,
                 float *kv_mass, float *node_logp /*dev [cu_nodes[B]]*/, int32_t *greedy_tok /*dev [cu_nodes[B]]*/,
                 int32_t *accept_len /*dev [B]*/, int32_t *accept_node /*dev [B]*/, int32_t *path /*dev [cu_nodes[B]]*/);
+
+/* ---- K/V rows in pages, as they are or quantised to 8 bits: a cache that grows with its utterances.
+ *
+ * A page holds page_rows (16, 32, 64, 128 or 256) rows of every layer and K/V head.  k and v are [n_layers][pages][n_kv_heads][page_rows][head_dim] elements of
+ * dtype, the scales [n_layers][pages][n_kv_heads][page_rows] fp32, each one behind the other and 16-byte aligned.  An element is worth its value, with an
+ * 8-bit type its value times the scale of its row:
+ *   SSD_F16, SSD_BF16  head_dim 64 or 128; scales NULL
+ *   SSD_F32            head_dim a multiple of 4 up to 128; scales NULL
+ *   SSD_E4M3           head_dim 64 or 128; floats of 4 exponent and 3 fraction bits, up to 448, without infinities
+ *   SSD_I8             head_dim 64 or 128; whole numbers
+ * Layer l of pages of several layers is n_layers 1 with the pointers moved by l * pages * n_kv_heads * page_rows rows. */
+typedef struct {
+    void    *k, *v;               /* dev */
+    float   *k_scale, *v_scale;   /* dev, or NULL */
+    int64_t pages;                /* < 2^31 */
+    int32_t page_rows, n_layers, n_kv_heads, head_dim, dtype;   /* enum ssd_dtype */
+} ssd_kv_pages;
+
+/* Whose pages they are.  Row j of utterance b lies in page entries[b * stride + j / page_rows], at row j % page_rows of it.  The arrays are DEVICE arrays,
+ * unlike those of other calls: a captured step is replayed with the lengths and pages that they hold then.  Their values are checked on the device: rows of a page
+ * outside [0, pages) are left out (not written, not read, not seen), a ctx_len outside [0, max_ctx] counts as the nearer end (in kv_write_pages and kv_read_pages
+ * the rows outside are left out), and SSD_FLAG_BAD_PAGE is raised.  Entries behind an utterance's last row are not read.  Utterances may share pages that are only read. */
+typedef struct {
+    const int32_t *entries;       /* dev */
+    int64_t stride;               /* at least ceil(max_ctx / page_rows) */
+    const int32_t *ctx_len;       /* dev [B]: rows of an utterance, the newest among them */
+    int32_t B, max_ctx;           /* 0 <= max_ctx <= 2^30: what the launch is made for, of a captured call the longest that a replay may meet */
+} ssd_page_table;
+
+/* The last n_rows[b] of the ctx_len[b] rows of every utterance, in all layers: slots start[b] .. of `slots` to its pages, or back.
+ *   start   dev [B], or NULL: b * max_rows      n_rows  dev [B], or NULL: max_rows of each; one outside [0, max_rows] counts as the nearer end and raises SSD_FLAG_BAD_PAGE
+ * A row whose slot is not one of `slots`, or whose place is not one of its utterance, is left out (SSD_FLAG_BAD_PAGE).
+ * Rows of `slots` are SSD_F32, SSD_BF16 or SSD_F16; the pages of the same type, or of 8 bits.  `slots` and pages agree in layers, K/V heads and head_dim and share no
+ * memory, nor do the keys and the values of what is written; no row may be written twice in a call (which one is left is not determined).  Nothing else is written.
+ * kv_write_pages, rows to 8 bits, each row x of a head by its own largest magnitude a:
+ *   SSD_E4M3  scale = 2^k, the smallest k >= -126 with a <= 448 * 2^k;  code = x / scale, exact, rounded to nearest even (of k = 120 at most 240: 256 would be
+ *             worth 2^128)
+ *   SSD_I8    scale = a / 127 in fp32 (at most the largest of which 127 times is finite);  code = 127 x / a to the nearest whole number, halves to even, of the exact quotient
+ *   a row of zeros has scale 0; a row that is not finite has codes 0 and scale NaN, and raises SSD_FLAG_ACT_OVERFLOW
+ * kv_read_pages, back: code * scale in fp32, rounded to the type of `slots`; IEEE half: clamped to +-65504 with SSD_FLAG_ACT_OVERFLOW, which NaN raises too.
+ * No workspace.  Calls may be captured.  Errors: SSD_EINVAL, SSD_ESHAPE (sizes above; more than 65535 utterances), SSD_EUNSUPPORTED (types). */
+int kv_write_pages(ssd_ctx *ctx, const ssd_kv_view *slots /*host*/, const int32_t *start, const int32_t *n_rows, int max_rows,
+                   const ssd_kv_pages *pages /*host*/, const ssd_page_table *table /*host*/);
+int kv_read_pages(ssd_ctx *ctx, const ssd_kv_pages *pages /*host*/, const ssd_page_table *table /*host*/, const ssd_kv_view *slots /*host*/,
+                  const int32_t *start, const int32_t *n_rows, int max_rows);
+
+/* Bytes of workspace for paged_attention calls of at most B utterances with n_new tokens each and contexts of max_ctx rows.  A size serves all smaller calls. */
+size_t ssd_paged_workspace_bytes(const ssd_ctx *ctx, int n_q_heads, int n_kv_heads, int head_dim, int64_t B, int n_new, int64_t max_ctx);
+
+/* Attention of the newest n_new tokens of every utterance (their own rows written before).  Token t sees rows j < ctx_len[b] - (n_new - 1 - t); per query head h, whose
+ * K/V head is h / (n_q_heads / n_kv_heads):  s_j = scale q . k_j;  lse = log sum_j exp s_j;  out = sum_j exp(s_j - lse) v_j.  A token that sees nothing has out 0 and lse -infinity.
+ *   scale   any for which scale * log2(e) is finite
+ *   q       dev, row b * n_new + t begins at element (b * n_new + t) * q_stride: n_q_heads * head_dim elements of q_dtype (q and q_stride multiples of 16 bytes); must not overlap out
+ *   pages   one layer (n_layers 1): of q_dtype, or of an 8-bit type
+ *   out     dev [B * n_new, n_q_heads * head_dim] of q_dtype, 16-byte aligned
+ *   lse     dev [B * n_new, n_q_heads] fp32, or NULL
+ * Scores, sums and statistics are fp32; 8-bit codes are exact operands.  A weight enters the second product as two values of 16 bits (22 bits of it with SSD_F16 pages, 16 with
+ * others; three values, 24 bits, with 8-bit pages and SSD_F32 queries), with SSD_F32 pages as it is.  Outputs below 2^-90 lose bits.  A row that a token does not see, and what
+ * lies behind the last row of a page, has no influence on it, whatever it holds; a value that it sees and that is not finite makes its column infinite or NaN.
+ * Captured calls use the workspace of the time of capture: two that share one must not run at the same time.  Every call repeats to the bit.
+ * Errors: SSD_EINVAL, SSD_ESHAPE (B times tiles of 16 query rows of a K/V head more than 65535; more than 512 query heads a K/V head), SSD_EUNSUPPORTED, SSD_EWORKSPACE. */
+int paged_attention(ssd_ctx *ctx, const void *q /*dev*/, int q_dtype, int64_t q_stride, int n_q_heads, int n_new, const ssd_kv_pages *pages /*host*/,
+                    const ssd_page_table *table /*host*/, float scale, void *out, float *lse);
 
 #ifdef __cplusplus
 }

@@ -13,9 +13,10 @@ import torch
 
 _LIB_PATH = os.path.join(os.path.dirname(os.path.abspath(__file__)), "libssd.so")
 
-SSD_F32, SSD_BF16, SSD_F16 = 0, 1, 2
+SSD_F32, SSD_BF16, SSD_F16, SSD_E4M3, SSD_I8 = 0, 1, 2, 3, 4
 _DTYPE_CODE = {torch.float32: SSD_F32, torch.bfloat16: SSD_BF16}
 _KV_CODE = {torch.float32: SSD_F32, torch.bfloat16: SSD_BF16, torch.float16: SSD_F16}
+_PAGE_CODE = {**_KV_CODE, torch.float8_e4m3fn: SSD_E4M3, torch.int8: SSD_I8}
 _STATUS = {0: "SSD_OK", -1: "SSD_EINVAL", -2: "SSD_ESHAPE", -3: "SSD_EWORKSPACE", -4: "SSD_EHIP",
            -5: "SSD_EUNSUPPORTED"}
 
@@ -25,7 +26,8 @@ EXPORTS = ["ssd_create", "ssd_destroy", "ssd_workspace_bytes", "ssd_set_workspac
            "ssd_gate_grid", "ssd_accept_grid", "ssd_plan_batches", "ssd_set_ctc_head", "ctc_head_gate", "ssd_device_flags",
            "ctc_gate_noalloc", "ssd_inexact_weights", "ssd_select_unconfident", "ssd_gather_i32", "ssd_set_qformer", "qformer_pool",
            "ssd_kv_cache_view", "ssd_tree_workspace_bytes", "tree_attention", "tree_path", "ssd_evict_workspace_bytes", "kv_evict",
-           "ssd_verify_tree_workspace_bytes", "verify_tree", "accept_tree"]
+           "ssd_verify_tree_workspace_bytes", "verify_tree", "accept_tree", "kv_write_pages", "kv_read_pages", "ssd_paged_workspace_bytes",
+           "paged_attention"]
 
 PROF_OFF, PROF_ALL = -2, -1
 PROF_CLASSES = ["gate", "gemm_qkv", "attention", "gemm_o", "gemm_gate_up", "gemm_down", "lmhead_accept", "other",
@@ -137,6 +139,14 @@ def load_library() -> C.CDLL:
     lib.verify_tree.restype = i32
     lib.accept_tree.argtypes = [vp, vp, vp, i32, vp, vp, f32, vp, vp, vp, vp, vp, vp, vp, vp]
     lib.accept_tree.restype = i32
+    lib.kv_write_pages.argtypes = [vp, vp, vp, vp, i32, vp, vp]
+    lib.kv_write_pages.restype = i32
+    lib.kv_read_pages.argtypes = [vp, vp, vp, vp, vp, vp, i32]
+    lib.kv_read_pages.restype = i32
+    lib.ssd_paged_workspace_bytes.argtypes = [vp, i32, i32, i32, i64, i32, i64]
+    lib.ssd_paged_workspace_bytes.restype = C.c_size_t
+    lib.paged_attention.argtypes = [vp, vp, i32, i64, i32, i32, vp, vp, f32, vp, vp]
+    lib.paged_attention.restype = i32
     lib.ssd_inexact_weights.argtypes = [vp]
     lib.ssd_inexact_weights.restype = i64
     return lib
@@ -212,6 +222,50 @@ def _kv_view(device, k: torch.Tensor, v: torch.Tensor):
     return _KV_VIEW.pack(k.data_ptr(), v.data_ptr(), n, ss, hs, ls, L, H, hd, code), n, L, H, hd
 
 
+_KV_PAGES = struct.Struct("=QQQQqiiiiixxxx")     # ssd_kv_pages
+_PAGE_TABLE = struct.Struct("=QqQii")            # ssd_page_table
+
+
+class KvPages:
+    """K/V rows in pages (ssd_kv_pages): k and v [layers, pages, K/V heads, rows of a page, head_dim], float16, bfloat16 or float32, or float8_e4m3fn or int8 with
+    k_scale and v_scale [layers, pages, K/V heads, rows of a page] float32; contiguous, on one device; one layer may come without its dimension."""
+
+    def __init__(self, k: torch.Tensor, v: torch.Tensor, k_scale: Optional[torch.Tensor] = None, v_scale: Optional[torch.Tensor] = None):
+        code = _PAGE_CODE.get(k.dtype)
+        if k.shape != v.shape or k.dim() not in (4, 5) or k.dtype is not v.dtype or code is None or k.device != v.device or not k.is_contiguous() or not v.is_contiguous():
+            raise ValueError("k and v must be alike and contiguous: [layers,] pages, K/V heads, rows of a page, head_dim")
+        if (k_scale is not None) != (k.element_size() == 1) or (k_scale is None) != (v_scale is None):
+            raise ValueError("pages of 8-bit types have k_scale and v_scale, others none")
+        if k_scale is not None:
+            _on(k.device, torch.float32, k_scale=k_scale, v_scale=v_scale)
+            if k_scale.shape != k.shape[:-1] or v_scale.shape != k.shape[:-1]:
+                raise ValueError("k_scale and v_scale must be [layers,] pages, K/V heads, rows of a page")
+        self.k, self.v, self.k_scale, self.v_scale = k, v, k_scale, v_scale
+        self.device, self.dtype = k.device, k.dtype
+        self.n_pages, self.n_kv_heads, self.page_rows, self.head_dim = k.shape[-4:]
+        self.n_layers = k.shape[0] if k.dim() == 5 else 1
+        self._view = _KV_PAGES.pack(k.data_ptr(), v.data_ptr(), 0 if k_scale is None else k_scale.data_ptr(), 0 if v_scale is None else v_scale.data_ptr(), self.n_pages,
+                                    self.page_rows, self.n_layers, self.n_kv_heads, self.head_dim, code)
+        self._layers = {}
+
+    def layer(self, l: int) -> "KvPages":
+        """The pages of one layer, the same memory."""
+        if l not in self._layers:
+            if not 0 <= l < self.n_layers:
+                raise IndexError(f"layer {l} of {self.n_layers}")
+            parts = (self.k, self.v, self.k_scale, self.v_scale)
+            self._layers[l] = KvPages(*(t if t is None or self.k.dim() == 4 else t[l] for t in parts))
+        return self._layers[l]
+
+    @staticmethod
+    def empty(n_pages: int, page_rows: int, n_kv_heads: int, head_dim: int, dtype: torch.dtype, n_layers: int = 1, device="cuda:0") -> "KvPages":
+        """Pages allocated through torch, their contents not defined."""
+        shape = (n_layers, n_pages, n_kv_heads, page_rows, head_dim)
+        k, v = (torch.empty(shape, dtype=dtype, device=device) for _ in range(2))
+        scales = [torch.empty(shape[:-1], dtype=torch.float32, device=device) for _ in range(2)] if k.element_size() == 1 else []
+        return KvPages(k, v, *scales)
+
+
 class Context:
     """Owns one ssd_ctx.  `weights` is the dict layout of workloads.make_model_weights (device tensors)."""
 
@@ -277,10 +331,11 @@ class Context:
         return int(self._lib.ssd_workspace_bytes(self._h, max_frames, max_tokens, max_verify_rows, max_utts))
 
     def reserve(self, max_frames=0, max_tokens=0, max_verify_rows=0, max_utts=0, ar_utts=0, ar_steps=0, tree_nodes=0, tree_utts=0,
-                tree_heads=None, evict_rows=0, evict_utts=0, evict_heads=None):
+                tree_heads=None, evict_rows=0, evict_utts=0, evict_heads=None, paged_utts=0, paged_new=1, paged_ctx=0, paged_heads=None):
         """Allocates (through torch) and hands over a workspace big enough for the given maxima.  tree_nodes, tree_utts: tree_path, with
         tree_heads (query heads, K/V heads, head_dim) tree_attention, and for a context with a model verify_tree and accept_tree;
-        evict_rows (kept by all utterances), evict_utts and evict_heads (layers, K/V heads): kv_evict."""
+        evict_rows (kept by all utterances), evict_utts and evict_heads (layers, K/V heads): kv_evict.  paged_utts, paged_new (tokens of an utterance),
+        paged_ctx (longest context) and paged_heads (query heads, K/V heads, head_dim): paged_attention."""
         n = self.workspace_bytes(max_frames, max_tokens, max_verify_rows, max_utts)
         if ar_utts and ar_steps:
             n = max(n, int(self._lib.ssd_ar_workspace_bytes(self._h, ar_utts, ar_steps)))
@@ -289,6 +344,8 @@ class Context:
                     int(self._lib.ssd_verify_tree_workspace_bytes(self._h, tree_nodes, tree_utts)))
         if evict_utts:
             n = max(n, int(self._lib.ssd_evict_workspace_bytes(self._h, *evict_heads, evict_rows, evict_utts)))
+        if paged_utts:
+            n = max(n, int(self._lib.ssd_paged_workspace_bytes(self._h, *paged_heads, paged_utts, paged_new, paged_ctx)))
         if self._ws is None or self._ws.numel() < n:
             self._ws = torch.empty(n, dtype=torch.uint8, device=self.device)
             self._check(self._lib.ssd_set_workspace(self._h, _ptr(self._ws), n))
@@ -634,6 +691,90 @@ class Context:
                                           None if cl is None else cl.tobytes(), _ptr(kv_mass) if ks is not None else None, _ptr(out["node_logp"]),
                                           _ptr(out["greedy_tok"]), _ptr(out["accept_len"]), _ptr(out["accept_node"]), _ptr(out["path"])))
         return out
+
+    # ---- K/V rows in pages -----------------------------------------------------------------------
+
+    def _page_table(self, pages: KvPages, page_table: torch.Tensor, ctx_len: torch.Tensor, max_ctx: Optional[int]) -> bytes:
+        """ssd_page_table of page_table [B, entries] and ctx_len [B], both int32 on the device."""
+        if page_table.dim() != 2 or page_table.dtype is not torch.int32 or not _at(page_table, self.device) or (page_table.shape[1] > 1 and page_table.stride(1) != 1):
+            raise ValueError(f"page_table must be an int32 tensor [utterances, entries] on {self.device}, the entries of an utterance consecutive")
+        B, entries = page_table.shape
+        if ctx_len.dtype is not torch.int32 or ctx_len.dim() != 1 or ctx_len.shape[0] != B or not ctx_len.is_contiguous() or not _at(ctx_len, self.device):
+            raise ValueError(f"ctx_len must be a contiguous int32 tensor [{B}] on {self.device}")
+        if not _at(pages.k, self.device):
+            raise ValueError(f"the pages must be on {self.device}")
+        most = min(entries * pages.page_rows, 1 << 30)
+        if max_ctx is None:
+            max_ctx = most
+        elif max_ctx > most:
+            raise ValueError(f"a table of {entries} entries holds {most} rows an utterance, not {max_ctx}")
+        return _PAGE_TABLE.pack(page_table.data_ptr(), page_table.stride(0) if B > 1 else max(entries, 1), ctx_len.data_ptr(), B, max_ctx)
+
+    def _move_pages(self, write, pages, page_table, ctx_len, k, v, start, n_rows, max_rows, max_ctx):
+        table = self._page_table(pages, page_table, ctx_len, max_ctx)
+        view, slots, _, _, _ = _kv_view(self.device, k, v)
+        B = page_table.shape[0]
+        for name, t in (("start", start), ("n_rows", n_rows)):
+            if t is not None:
+                _on(self.device, torch.int32, **{name: t})
+                if t.numel() != B:
+                    raise ValueError(f"{name} must have an entry an utterance")
+        if max_rows is None:
+            if start is not None or n_rows is not None or B == 0 or slots % B:
+                raise ValueError("max_rows is needed where not every utterance has the same number of slots, one behind the other")
+            max_rows = slots // B
+        s, n = None if start is None else start.data_ptr(), None if n_rows is None else n_rows.data_ptr()
+        if write:
+            self._check(self._lib.kv_write_pages(self._h, view, s, n, max_rows, pages._view, table))
+        else:
+            self._check(self._lib.kv_read_pages(self._h, pages._view, table, view, s, n, max_rows))
+
+    def kv_write_pages(self, pages: KvPages, page_table: torch.Tensor, ctx_len: torch.Tensor, k: torch.Tensor, v: torch.Tensor, start: Optional[torch.Tensor] = None,
+                       n_rows: Optional[torch.Tensor] = None, max_rows: Optional[int] = None, max_ctx: Optional[int] = None):
+        """Rows of k, v [layers, slots, K/V heads, head_dim] (one layer also without its dimension; any strides but the last) to the pages of their utterances
+        (kv_write_pages), quantised where the pages are of 8 bits: the last n_rows[b] of the ctx_len[b] rows of utterance b are the slots from start[b] on.  Tensors of the
+        device (int32): page_table [utterances, entries], ctx_len, start, n_rows.  Without start and n_rows the slots belong to the utterances in equal parts."""
+        self._move_pages(True, pages, page_table, ctx_len, k, v, start, n_rows, max_rows, max_ctx)
+
+    def kv_read_pages(self, pages: KvPages, page_table: torch.Tensor, ctx_len: torch.Tensor, k: torch.Tensor, v: torch.Tensor, start: Optional[torch.Tensor] = None,
+                      n_rows: Optional[torch.Tensor] = None, max_rows: Optional[int] = None, max_ctx: Optional[int] = None):
+        """The way back (kv_read_pages): the same arguments; k and v are written."""
+        self._move_pages(False, pages, page_table, ctx_len, k, v, start, n_rows, max_rows, max_ctx)
+
+    def paged_attention(self, q: torch.Tensor, pages: KvPages, page_table: torch.Tensor, ctx_len: torch.Tensor, max_ctx: Optional[int] = None,
+                        scale: Optional[float] = None, out: Optional[torch.Tensor] = None, lse: Optional[torch.Tensor] = None) -> torch.Tensor:
+        """Attention of the newest tokens over the pages of their utterances (paged_attention): q [utterances, query heads, head_dim], or [utterances, tokens, query heads,
+        head_dim] (any stride between tokens).  ctx_len counts the new tokens; max_ctx: the longest context the launch is made for (what page_table holds unless
+        given).  Returns out in the shape of q; lse [.., query heads] takes the log-sum-exps (float32, optional).  scale: 1 / sqrt(head_dim) unless given."""
+        table = self._page_table(pages, page_table, ctx_len, max_ctx)
+        shape, st, code = q.shape, q.stride(), _KV_CODE.get(q.dtype)
+        if len(shape) not in (3, 4) or code is None or q.device != pages.device or shape[0] != ctx_len.shape[0]:
+            raise ValueError("q must be [utterances, [tokens,] query heads, head_dim], float16, bfloat16 or float32, on the device of the pages")
+        Hq, hd = shape[-2:]
+        n_new = shape[1] if len(shape) == 4 else 1
+        if hd != pages.head_dim or (hd > 1 and st[-1] != 1) or (Hq > 1 and st[-2] != hd) or (len(shape) == 4 and shape[0] > 1 and n_new > 1 and st[0] != n_new * st[1]):
+            raise ValueError("q must have the head_dim of the pages, the heads of a token consecutive, tokens at equal distances")
+        q_stride = st[1] if n_new > 1 else st[0] if shape[0] > 1 else Hq * hd
+        if out is None:
+            out = self._new(shape, q.dtype)
+        else:
+            _on(self.device, q.dtype, out=out)
+            if out.numel() != q.numel():
+                raise ValueError("out has the wrong size")
+        if lse is not None:
+            _on(self.device, torch.float32, lse=lse)
+            if lse.numel() * hd != q.numel():
+                raise ValueError("lse has the wrong size")
+        self._check(self._lib.paged_attention(self._h, q.data_ptr(), code, q_stride, Hq, n_new, pages._view, table, hd ** -0.5 if scale is None else scale, out.data_ptr(),
+                                              None if lse is None else lse.data_ptr()))
+        return out
+
+    def _new(self, shape, dtype) -> torch.Tensor:
+        """A tensor that the context's stream writes first: of that stream, so that memory in use on the current one is not given out again."""
+        if torch.cuda.current_stream(self.device) == self.stream:
+            return torch.empty(shape, dtype=dtype, device=self.device)
+        with torch.cuda.stream(self.stream):
+            return torch.empty(shape, dtype=dtype, device=self.device)
 
     def accept_prefix(self, h_verify: torch.Tensor, draft_ids: torch.Tensor, cu_draft, tau_slm: float,
                       want_greedy: bool = False, out: Optional[dict] = None) -> dict:

@@ -7,6 +7,7 @@
 #include <algorithm>
 #include <exception>
 
+#include "pages.h"
 #include "ssd_internal.h"
 #include "tree.h"
 
@@ -98,6 +99,7 @@ struct ssd_ctx {
     float* rope_tab = nullptr;               // [max_positions][head_dim/2] (cos, sin) pairs
     unsigned* gate_arrived = nullptr;        // rows done per utterance, all zero between calls (launch_gate_fused)
     int32_t* dev_flags = nullptr;            // sticky data-dependent conditions seen by kernels (ssd_device_flags)
+    int32_t* page_flags = nullptr;           // the same, or those of the calls on pages of a context without a model
     void* ws = nullptr;
     size_t ws_bytes = 0;
     uint16_t* head_w = nullptr;              // CTC output layer, padded with zero rows (bias -inf there)
@@ -317,9 +319,11 @@ void alloc_gate_counters(ssd_ctx* c) {
     hipStreamCaptureMode mode = hipStreamCaptureModeRelaxed;       // captures of other streams go on
     (void)hipThreadExchangeStreamCaptureMode(&mode);
     void* p = nullptr;
-    if (hipMalloc(&p, GATE_ARRIVED_BYTES) == hipSuccess && hipMemsetAsync(p, 0, GATE_ARRIVED_BYTES, c->stream) == hipSuccess) {
+    const size_t bytes = GATE_ARRIVED_BYTES + 256;                 // and the flags
+    if (hipMalloc(&p, bytes) == hipSuccess && hipMemsetAsync(p, 0, bytes, c->stream) == hipSuccess) {
         c->owned.push_back(p);
         c->gate_arrived = static_cast<unsigned*>(p);
+        if (!c->page_flags) c->page_flags = reinterpret_cast<int32_t*>(static_cast<char*>(p) + GATE_ARRIVED_BYTES);
     } else {
         if (p) (void)hipFree(p);
         (void)hipGetLastError();
@@ -456,6 +460,7 @@ int ssd_create(ssd_ctx** out, const ssd_model_cfg* cfg, const ssd_weights* w, vo
         return bail(e, "hipMemcpyAsync(rope)");
     if ((e = dev_alloc((void**)&c->dev_flags, 256)) != hipSuccess) return bail(e, "hipMalloc(flags)");
     if ((e = hipMemsetAsync(c->dev_flags, 0, 256, c->stream)) != hipSuccess) return bail(e, "hipMemsetAsync(flags)");
+    c->page_flags = c->dev_flags;
     unsigned long long n_inexact = 0;
     if ((e = hipMemcpyAsync(&n_inexact, d_inexact, 8, hipMemcpyDeviceToHost, c->stream)) != hipSuccess) return bail(e, "hipMemcpyAsync(inexact)");
     if ((e = hipStreamSynchronize(c->stream)) != hipSuccess) return bail(e, "weight packing");
@@ -497,10 +502,10 @@ size_t ssd_workspace_bytes(const ssd_ctx* ctx, int64_t max_frames, int64_t max_t
 int ssd_device_flags(ssd_ctx* ctx, int32_t* flags) {
     if (!ctx || !flags) return SSD_EINVAL;
     *flags = 0;
-    if (!ctx->dev_flags) return SSD_OK;
-    HIP_TRY(ctx, hipMemcpyAsync(flags, ctx->dev_flags, 4, hipMemcpyDeviceToHost, ctx->stream));
+    if (!ctx->page_flags) return SSD_OK;
+    HIP_TRY(ctx, hipMemcpyAsync(flags, ctx->page_flags, 4, hipMemcpyDeviceToHost, ctx->stream));
     HIP_TRY(ctx, hipStreamSynchronize(ctx->stream));
-    if (*flags) HIP_TRY(ctx, hipMemsetAsync(ctx->dev_flags, 0, 4, ctx->stream));
+    if (*flags) HIP_TRY(ctx, hipMemsetAsync(ctx->page_flags, 0, 4, ctx->stream));
     return SSD_OK;
 }
 
@@ -2045,5 +2050,147 @@ int accept_tree(ssd_ctx* ctx, const void* h_tree, const int32_t* node_ids, int B
     HIP_TRY(ctx, hipGetLastError());
     return SSD_OK;
 } SSD_NO_THROW("accept_tree")
+
+}  // extern "C"
+
+// ---- K/V rows in pages ------------------------------------------------------------------------------------------------------------
+
+namespace {
+
+size_t page_elem(int dtype) { return dtype == SSD_E4M3 || dtype == SSD_I8 ? 1 : kv_elem(dtype); }
+int64_t page_row_count(const ssd_kv_pages& p) { return (int64_t)p.n_layers * p.pages * p.n_kv_heads * p.page_rows; }
+
+int check_pages(ssd_ctx* c, const char* what, const ssd_kv_pages* p, const ssd_page_table* t) {
+    if (!p || !t || !p->k || !p->v) return fail(c, SSD_EINVAL, "%s: NULL pages or table", what);
+    if (p->dtype < SSD_F32 || p->dtype > SSD_I8) return fail(c, SSD_EUNSUPPORTED, "%s: dtype %d of pages", what, p->dtype);
+    const bool codes = page_elem(p->dtype) == 1;
+    if (codes != (p->k_scale != nullptr) || codes != (p->v_scale != nullptr)) return fail(c, SSD_EINVAL, "%s: pages of 8-bit types have scales, others none", what);
+    if (p->pages <= 0 || p->pages > INT32_MAX || p->n_layers <= 0 || p->n_kv_heads <= 0 || p->head_dim <= 0)
+        return fail(c, SSD_EINVAL, "%s: non-positive size of pages, or more than 2^31 - 1 of them", what);
+    if (p->page_rows != 16 && p->page_rows != 32 && p->page_rows != 64 && p->page_rows != 128 && p->page_rows != 256)
+        return fail(c, SSD_ESHAPE, "%s: pages of %d rows (16, 32, 64, 128 or 256)", what, p->page_rows);
+    if (p->dtype == SSD_F32 ? p->head_dim % 4 || p->head_dim > 128 : p->head_dim != 64 && p->head_dim != 128)
+        return fail(c, SSD_ESHAPE, "%s: head_dim %d (64 or 128, of fp32 pages a multiple of 4 up to 128)", what, p->head_dim);
+    if (p->n_kv_heads > 65535 || (int64_t)p->n_layers * p->n_kv_heads > 65535) return fail(c, SSD_ESHAPE, "%s: more than 65535 layers times K/V heads", what);
+    if (page_row_count(*p) > (int64_t)1 << 42) return fail(c, SSD_ESHAPE, "%s: more than 2^42 rows in pages", what);      // (no product below leaves 64 bits)
+    if (((uintptr_t)p->k | (uintptr_t)p->v | (uintptr_t)p->k_scale | (uintptr_t)p->v_scale) & 15)
+        return fail(c, SSD_EINVAL, "%s: pages and scales must begin at multiples of 16 bytes", what);
+    if (!t->ctx_len || (!t->entries && t->max_ctx > 0)) return fail(c, SSD_EINVAL, "%s: NULL entries or ctx_len", what);
+    if (t->B <= 0) return fail(c, SSD_EINVAL, "%s: B must be positive (got %d)", what, t->B);
+    if (t->B > 65535) return fail(c, SSD_ESHAPE, "%s: more than 65535 utterances; split the batch", what);
+    if (t->max_ctx < 0 || t->max_ctx > 1 << 30) return fail(c, SSD_EINVAL, "%s: max_ctx %d", what, t->max_ctx);
+    if (t->stride < (t->max_ctx + p->page_rows - 1) / p->page_rows || t->stride > (int64_t)1 << 42)
+        return fail(c, SSD_EINVAL, "%s: a table of %lld entries an utterance is too short for %d rows", what, (long long)t->stride, t->max_ctx);
+    return SSD_OK;
+}
+
+PagesArgs pages_args(const ssd_ctx* c, const ssd_kv_pages& p, const ssd_page_table& t) {
+    PagesArgs a;
+    a.k = p.k; a.v = p.v; a.k_scale = p.k_scale; a.v_scale = p.v_scale;
+    a.layer_rows = p.pages * p.n_kv_heads * p.page_rows;
+    a.n_pages = (int32_t)p.pages; a.n_kv_heads = p.n_kv_heads; a.head_dim = p.head_dim;
+    a.row_bits = 0;
+    while (1 << a.row_bits < p.page_rows) ++a.row_bits;
+    a.entries = t.entries; a.stride = t.stride; a.ctx_len = t.ctx_len;
+    a.B = t.B; a.max_ctx = t.max_ctx;
+    a.flags = c->page_flags;
+    return a;
+}
+
+int move_pages(ssd_ctx* ctx, const char* what, bool write, const ssd_kv_view* slots, const int32_t* start, const int32_t* n_rows, int max_rows, const ssd_kv_pages* pages,
+               const ssd_page_table* table) {
+    const OnDevice on(ctx);
+    int rc = check_view(ctx, what, slots);
+    if (rc == SSD_OK) rc = check_pages(ctx, what, pages, table);
+    if (rc != SSD_OK) return rc;
+    if (slots->n_layers != pages->n_layers || slots->n_kv_heads != pages->n_kv_heads || slots->head_dim != pages->head_dim)
+        return fail(ctx, SSD_EINVAL, "%s: slots and pages differ in layers, heads or head_dim", what);
+    if (page_elem(pages->dtype) != 1 && pages->dtype != slots->dtype)
+        return fail(ctx, SSD_EUNSUPPORTED, "%s: pages of dtype %d with slots of dtype %d", what, pages->dtype, slots->dtype);
+    if (max_rows < 0) return fail(ctx, SSD_EINVAL, "%s: max_rows is negative", what);
+    if (!start && !n_rows && (int64_t)table->B * max_rows > slots->slots)
+        return fail(ctx, SSD_EINVAL, "%s: %d utterances of %d rows do not fit %lld slots", what, table->B, max_rows, (long long)slots->slots);
+    const size_t rows = (size_t)page_row_count(*pages), bytes = rows * pages->head_dim * page_elem(pages->dtype);
+    auto block = [](const void* p, size_t n) { return Extent{(uintptr_t)p, (uintptr_t)p + n}; };
+    const Extent page_part[4] = {block(pages->k, bytes), block(pages->v, bytes), block(pages->k_scale, pages->k_scale ? rows * 4 : 0),
+                                 block(pages->v_scale, pages->v_scale ? rows * 4 : 0)};
+    const Extent slot_part[2] = {extent_of(*slots, slots->k), extent_of(*slots, slots->v)};
+    for (const Extent& p : page_part)
+        for (const Extent& s : slot_part)
+            if (overlap(p, s)) return fail(ctx, SSD_EINVAL, "%s: slots and pages overlap in memory", what);
+    if (write) {
+        for (int i = 0; i < 4; ++i)
+            for (int j = 0; j < i; ++j)
+                if (overlap(page_part[i], page_part[j])) return fail(ctx, SSD_EINVAL, "%s: keys, values and scales of the pages overlap in memory", what);
+    } else if (slots->k == slots->v) {
+        return fail(ctx, SSD_EINVAL, "%s: keys and values of the slots share memory", what);
+    }
+    if (!max_rows || !table->max_ctx) return SSD_OK;
+    MoveArgs a;
+    a.p = pages_args(ctx, *pages, *table);
+    a.k = slots->k; a.v = slots->v; a.slots = slots->slots;
+    a.slot_stride = slots->slot_stride; a.head_stride = slots->head_stride; a.layer_stride = slots->n_layers > 1 ? slots->layer_stride : 0;
+    a.start = start; a.n_rows = n_rows; a.max_rows = max_rows; a.n_layers = slots->n_layers;
+    {
+        ProfScope ps(ctx, SSD_PROF_OTHER);
+        if (write) launch_write_pages(a, slots->dtype, pages->dtype, ctx->stream);
+        else launch_read_pages(a, slots->dtype, pages->dtype, ctx->stream);
+    }
+    HIP_TRY(ctx, hipGetLastError());
+    return SSD_OK;
+}
+
+}  // namespace
+
+extern "C" {
+
+int kv_write_pages(ssd_ctx* ctx, const ssd_kv_view* slots, const int32_t* start, const int32_t* n_rows, int max_rows, const ssd_kv_pages* pages,
+                   const ssd_page_table* table) try {
+    return ctx ? move_pages(ctx, "kv_write_pages", true, slots, start, n_rows, max_rows, pages, table) : SSD_EINVAL;
+} SSD_NO_THROW("kv_write_pages")
+
+int kv_read_pages(ssd_ctx* ctx, const ssd_kv_pages* pages, const ssd_page_table* table, const ssd_kv_view* slots, const int32_t* start, const int32_t* n_rows,
+                  int max_rows) try {
+    return ctx ? move_pages(ctx, "kv_read_pages", false, slots, start, n_rows, max_rows, pages, table) : SSD_EINVAL;
+} SSD_NO_THROW("kv_read_pages")
+
+size_t ssd_paged_workspace_bytes(const ssd_ctx* ctx, int n_q_heads, int n_kv_heads, int head_dim, int64_t B, int n_new, int64_t max_ctx) {
+    if (!ctx || n_q_heads <= 0 || n_kv_heads <= 0 || head_dim <= 0 || B < 0 || n_new < 0 || max_ctx < 0) return 0;
+    return 256;
+}
+
+int paged_attention(ssd_ctx* ctx, const void* q, int q_dtype, int64_t q_stride, int n_q_heads, int n_new, const ssd_kv_pages* pages, const ssd_page_table* table,
+                    float scale, void* out, float* lse) try {
+    if (!ctx) return SSD_EINVAL;
+    const OnDevice on(ctx);
+    const int rc = check_pages(ctx, "paged_attention", pages, table);
+    if (rc != SSD_OK) return rc;
+    if (q_dtype != SSD_F32 && q_dtype != SSD_BF16 && q_dtype != SSD_F16) return fail(ctx, SSD_EUNSUPPORTED, "paged_attention: q_dtype %d", q_dtype);
+    if (page_elem(pages->dtype) != 1 && pages->dtype != q_dtype)
+        return fail(ctx, SSD_EUNSUPPORTED, "paged_attention: pages of dtype %d with queries of dtype %d", pages->dtype, q_dtype);
+    if (pages->n_layers != 1) return fail(ctx, SSD_EINVAL, "paged_attention: pages of one layer are needed (got %d)", pages->n_layers);
+    if (n_q_heads <= 0 || n_q_heads % pages->n_kv_heads) return fail(ctx, SSD_ESHAPE, "paged_attention: n_q_heads must be a multiple of n_kv_heads");
+    const int group = n_q_heads / pages->n_kv_heads;
+    if (n_q_heads > 65535 || group > 512) return fail(ctx, SSD_ESHAPE, "paged_attention: more than 65535 query heads, or 512 per K/V head");
+    if (n_new <= 0) return fail(ctx, SSD_EINVAL, "paged_attention: n_new must be positive (got %d)", n_new);
+    if (((int64_t)n_new * group + 15) / 16 * table->B > 65535) return fail(ctx, SSD_ESHAPE, "paged_attention: more than 65535 tiles of query rows; split the batch");
+    if (!std::isfinite(scale * 1.4426950408889634f)) return fail(ctx, SSD_EINVAL, "paged_attention: scale is not finite, or not to base 2");
+    if (!q || !out) return fail(ctx, SSD_EINVAL, "paged_attention: NULL data pointer");
+    const int64_t dq = (int64_t)n_q_heads * pages->head_dim, es = (int64_t)kv_elem(q_dtype), N = (int64_t)table->B * n_new;
+    if (q_stride < dq || q_stride > (int64_t)1 << 32 || q_stride * es % 16 || ((uintptr_t)q | (uintptr_t)out) & 15)
+        return fail(ctx, SSD_EINVAL, "paged_attention: rows of q and out must begin at multiples of 16 bytes, q_stride be at least n_q_heads * head_dim");
+    if (overlap(Extent{(uintptr_t)q, (uintptr_t)q + (uintptr_t)(((N - 1) * q_stride + dq) * es)}, Extent{(uintptr_t)out, (uintptr_t)out + (uintptr_t)(N * dq * es)}))
+        return fail(ctx, SSD_EINVAL, "paged_attention: q and out overlap in memory");
+    PagedAttnArgs a;
+    a.p = pages_args(ctx, *pages, *table);
+    a.q = q; a.q_stride = q_stride; a.out = out; a.lse = lse;
+    a.n_q_heads = n_q_heads; a.group = group; a.n_new = n_new; a.scale = scale;
+    {
+        ProfScope ps(ctx, SSD_PROF_ATTN);
+        launch_paged_attention(a, q_dtype, pages->dtype, ctx->stream);
+    }
+    HIP_TRY(ctx, hipGetLastError());
+    return SSD_OK;
+} SSD_NO_THROW("paged_attention")
 
 }  // extern "C"

@@ -1,0 +1,273 @@
+"""paged_attention against 64 bits: lengths, pages, head layouts, types, several tokens, rows that must not count, replays."""
+import numpy as np
+import pytest
+import torch
+
+from pages import TYPE, Pool, attention
+from paper_2603_11243_amd.binding import Context, KvPages, SsdError
+
+pytestmark = pytest.mark.gpu
+
+# (queries, pages)
+PAIRS = [("f16", "f16"), ("bf16", "bf16"), ("f32", "f32"), ("f16", "e4m3"), ("bf16", "e4m3"), ("f32", "e4m3"), ("f16", "i8"), ("bf16", "i8"), ("f32", "i8")]
+# (query heads, K/V heads, head_dim)
+HEADS = [(16, 8, 128), (24, 8, 128), (4, 4, 64), (14, 2, 64), (5, 1, 128), (40, 2, 64)]
+HEADS_32 = HEADS + [(3, 1, 4), (8, 2, 36), (2, 1, 100)]
+
+
+def _context(B, n_new, heads, most):
+    c = Context(device="cuda:0")
+    c.reserve(paged_utts=B, paged_new=n_new, paged_ctx=most, paged_heads=heads)
+    return c
+
+
+def _queries(dtype, B, n_new, heads, seed=0, gap=0, scale=1.5):
+    hq, _, hd = heads
+    q = torch.full((B, n_new, hq * hd + gap), float("nan"), dtype=TYPE[dtype])
+    q[..., :hq * hd] = (torch.randn(B, n_new, hq * hd, generator=torch.Generator().manual_seed(seed + 77)) * scale).to(TYPE[dtype])
+    return q.cuda()[..., :hq * hd].unflatten(2, (hq, hd))
+
+
+def _check(pair, heads, ctx_len, page_rows=16, n_new=1, seed=0, gap=0, scale=None, change=None, lost=lambda b, j: False, flags=0, most=None, ctx=None, pool=None, **more):
+    q = _queries(pair[0], len(ctx_len), n_new, heads, seed, gap)
+    pool = pool or Pool(pair[1], heads[1:], ctx_len, page_rows, seed, most=most)
+    c = ctx or _context(len(ctx_len), n_new, heads, pool.table.shape[1] * page_rows)
+    want, tol, want_lse, lse_tol = attention(q, pool, n_new, scale, lost)
+    if change:
+        change(q, pool)
+    lse = torch.full(q.shape[:3], 7.0, device="cuda")
+    c.device_flags()
+    out = c.paged_attention(q, pool.pages(), pool.table, pool.ctx_len, scale=scale, lse=lse, **more)
+    torch.cuda.synchronize()
+    got, got_lse = out.double().cpu().numpy(), lse.double().cpu().numpy()
+    off = np.abs(got - want) - tol
+    assert got.shape == want.shape and np.isfinite(got).all() and (off <= 0).all(), (np.argwhere(~(off <= 0))[:5], off.max(), tol.mean())
+    nothing = np.isinf(want_lse)
+    assert np.array_equal(nothing, np.isneginf(got_lse))
+    assert (np.abs(got_lse[~nothing] - want_lse[~nothing]) <= lse_tol[~nothing]).all()
+    assert c.device_flags() == flags
+    if ctx is None:
+        c.close()
+    return out
+
+
+@pytest.mark.parametrize("pair", PAIRS)
+@pytest.mark.parametrize("heads", HEADS)
+@pytest.mark.parametrize("page_rows, n_new", [(16, 1), (64, 1), (32, 3), (256, 5)])
+def test_ragged_batches(pair, heads, page_rows, n_new):
+    _check(pair, heads, [0, 1, 2, 15, 16, 17, 31, 33, 64, 65, 130, 200], page_rows, n_new)
+
+
+@pytest.mark.parametrize("heads", HEADS_32[len(HEADS):])
+@pytest.mark.parametrize("n_new", [1, 7])
+def test_head_dims_of_fp32(heads, n_new):
+    _check(("f32", "f32"), heads, [0, 1, 16, 40, 300, 77], 32, n_new)
+
+
+@pytest.mark.parametrize("pair", PAIRS)
+@pytest.mark.parametrize("n", [1, 127, 128, 129, 255, 256, 257, 511, 513, 1000, 2047, 2049, 4096, 4097, 9001])
+def test_lengths(pair, n):
+    _check(pair, (4, 2, 128), [n, max(1, n // 3)], 64)
+
+
+@pytest.mark.parametrize("pair", [("f16", "f16"), ("bf16", "e4m3"), ("f16", "i8"), ("f32", "f32")])
+@pytest.mark.parametrize("n_new", [2, 8, 9, 17, 40])
+@pytest.mark.parametrize("heads", [(4, 2, 64), (24, 8, 128), (3, 3, 128)])
+def test_several_tokens(pair, n_new, heads):
+    """More query rows than one tile holds; tokens that see nothing, in contexts shorter than the new tokens."""
+    _check(pair, heads, [0, 1, n_new - 1, n_new, n_new + 1, 64, 600], 16, n_new)
+
+
+@pytest.mark.parametrize("pair", [("f16", "f16"), ("bf16", "i8"), ("f32", "f32"), ("f32", "e4m3")])
+def test_many_query_heads(pair):
+    _check(pair, (512, 1, 64), [70, 3], 16)
+    _check(pair, (100, 4, 64), [40], 32, 3)
+
+
+@pytest.mark.parametrize("pair", PAIRS)
+@pytest.mark.parametrize("scale", [0.0, -0.3, 1.0, 1e-20])
+def test_scales(pair, scale):
+    _check(pair, (4, 2, 64), [50, 300], 16, 2, scale=scale)
+
+
+@pytest.mark.parametrize("pair", PAIRS)
+def test_strided_queries(pair):
+    _check(pair, (4, 2, 64), [50, 30, 9], 16, 2, gap=192)
+    q = _queries(pair[0], 3, 1, (4, 2, 64), gap=64)[:, 0]
+    pool, c = Pool(pair[1], (2, 64), [50, 30, 9], 16), _context(3, 1, (4, 2, 64), 64)
+    out = torch.empty(q.shape, dtype=q.dtype, device="cuda")
+    assert c.paged_attention(q, pool.pages(), pool.table, pool.ctx_len, out=out) is out
+    want, tol, _, _ = attention(q[:, None], pool, 1)
+    assert (np.abs(out.double().cpu().numpy() - want[:, 0]) <= tol[:, 0]).all()
+
+
+@pytest.mark.parametrize("pair", PAIRS)
+@pytest.mark.parametrize("bad", ["nan", "inf"])
+def test_rows_of_later_tokens_do_not_count(pair, bad):
+    """The last row is not finite: only the last token is touched."""
+    heads, n_new = (4, 2, 64), 4
+    q, pool = _queries(pair[0], 2, n_new, heads), Pool(pair[1], heads[1:], [50, 67], 16)
+    want, tol, _, _ = attention(q, pool, n_new)
+    for b in range(2):
+        j = int(pool.ctx_host[b]) - 1
+        at = (0, int(pool.table_host[b, j // 16]), slice(None), j % 16)
+        for name in ("k", "v"):
+            if pool.kind in ("e4m3", "i8"):
+                pool.parts[name + "_scale"][at] = float(bad)
+                if pool.kind == "e4m3" and bad == "nan":
+                    pool.parts[name].view(torch.uint8)[at] = 127
+            else:
+                pool.parts[name][at] = float(bad)
+    c = _context(2, n_new, heads, 80)
+    out = c.paged_attention(q, pool.pages(), pool.table, pool.ctx_len).double().cpu().numpy()
+    assert (np.abs(out - want) <= tol)[:, :-1].all()
+    assert not np.isfinite(out[:, -1]).any()
+
+
+@pytest.mark.parametrize("pair", [("f16", "f16"), ("bf16", "bf16"), ("f32", "f32")])
+def test_a_seen_value_that_is_not_finite_stays_in_its_column(pair):
+    for n in (40, 3000):
+        heads = (4, 2, 64)
+        q, pool = _queries(pair[0], 1, 2, heads), Pool(pair[1], heads[1:], [n], 16)
+        want, tol, _, _ = attention(q, pool, 2)
+        for j, d, x in ((n - 5, 7, "nan"), (3, 20, "inf"), (n - 20, 33, "-inf")):
+            pool.parts["v"][0, int(pool.table_host[0, j // 16]), 1, j % 16, d] = float(x)
+        out = _context(1, 2, heads, n + 16).paged_attention(q, pool.pages(), pool.table, pool.ctx_len).double().cpu().numpy()
+        touched = np.zeros(want.shape, dtype=bool)
+        touched[:, :, 2:, [7, 20, 33]] = True
+        assert not np.isfinite(out[touched]).any() and (np.abs(out - want) <= tol)[~touched].all()
+
+
+@pytest.mark.parametrize("pair", PAIRS)
+def test_pages_that_are_none(pair):
+    """Their rows are not seen, also if none is left."""
+    def change(q, pool):
+        pool.table[0, 2] = -1
+        pool.table[1, 0] = pool.n_pages
+        pool.table[2, :] = -2 ** 31
+    _check(pair, (4, 2, 64), [100, 20, 33, 50, 700], 16, 2, change=change, lost=lambda b, j: (b == 0 and 32 <= j < 48) or (b == 1 and j < 16) or b == 2, flags=4)
+
+
+@pytest.mark.parametrize("pair", [("f16", "f16"), ("bf16", "e4m3"), ("f32", "f32")])
+def test_lengths_out_of_range(pair):
+    heads = (4, 2, 64)
+    q, c = _queries(pair[0], 3, 1, heads), _context(3, 1, heads, 64)
+    pool = Pool(pair[1], heads[1:], [64, 64, 0], 16)
+    want, tol, _, _ = attention(q, pool, 1)
+    pool.ctx_len.copy_(torch.tensor([65, 2 ** 31 - 1, -3]))
+    c.device_flags()
+    out = c.paged_attention(q, pool.pages(), pool.table, pool.ctx_len).double().cpu().numpy()
+    assert (np.abs(out - want) <= tol).all() and c.device_flags() == 4
+    out = c.paged_attention(q, pool.pages(), pool.table[:, :0], torch.zeros_like(pool.ctx_len))
+    assert (out == 0).all() and c.device_flags() == 0
+
+
+def test_shared_pages():
+    """Two utterances whose first rows are the same pages, and one list three times."""
+    heads = (4, 2, 64)
+    pool = Pool("e4m3", heads[1:], [100, 100, 37, 100, 100], 32)
+    for b in (1, 3, 4):
+        for j in range(2):
+            pool.table_host[b, j] = pool.table_host[0, j]
+    pool.table_host[4] = pool.table_host[0]
+    pool.table.copy_(torch.from_numpy(pool.table_host))
+    _check(("f16", "e4m3"), heads, [100, 100, 37, 100, 100], 32, pool=pool)
+
+
+def test_no_precision_is_lost_between_equal_scores():
+    """Means of many values of one magnitude in fp32 pages and by three-value weights: errors of fp32, not of 16 bits."""
+    for pair in (("f32", "f32"), ("f32", "i8"), ("f32", "e4m3")):
+        heads, n = (2, 2, 64), 5000
+        pool = Pool(pair[1], heads[1:], [n], 64)
+        q = _queries("f32", 1, 1, heads, scale=0.1)
+        want, _, _, _ = attention(q, pool, 1)
+        out = _context(1, 1, heads, n + 64).paged_attention(q, pool.pages(), pool.table, pool.ctx_len).double().cpu().numpy()
+        assert np.linalg.norm(out - want) <= 2e-5 * np.linalg.norm(want)
+
+
+@pytest.mark.parametrize("pair", [("bf16", "bf16"), ("f32", "f32"), ("f32", "i8"), ("bf16", "e4m3")])
+def test_values_at_the_end_of_the_range(pair):
+    """Sums of values whose mean is in fp32's range, though they themselves are not."""
+    heads, n = (2, 2, 64), 700
+    pool, q = Pool(pair[1], heads[1:], [n], 16), _queries(pair[0], 1, 1, heads, scale=0.1)
+    if pair[1] in ("e4m3", "i8"):
+        s = pool.parts["v_scale"]
+        s.copy_(torch.where(s.isnan(), s, 2.0 ** 119 if pair[1] == "e4m3" else 2.0 ** 120))
+        pool.parts["v"].view(torch.uint8).fill_(0x7c if pair[1] == "e4m3" else 100)
+    else:
+        v = pool.parts["v"]
+        v.copy_(torch.where(v.isnan(), v, 3.2e38))
+    want, tol, _, _ = attention(q, pool, 1)
+    out = _context(1, 1, heads, n + 16).paged_attention(q, pool.pages(), pool.table, pool.ctx_len).double().cpu().numpy()
+    assert (np.abs(out / 2.0 ** 64 - want / 2.0 ** 64) <= tol / 2.0 ** 64).all()
+
+
+def test_pools_beyond_4_gib():
+    H, hd, R, n = 8, 128, 64, 1000
+    n_pages = (9 << 30) // (H * R * hd * 2)
+    big = torch.zeros(n_pages, H, R, hd, dtype=torch.bfloat16, device="cuda")
+    r = np.random.default_rng(0)
+    order = r.permutation(n_pages - 20)[:14].tolist() + [n_pages - 1, n_pages - 2]
+    table = torch.tensor([order], dtype=torch.int32, device="cuda")
+    small = Pool("bf16", (H, hd), [n], R, seed=3)
+    for j, page in enumerate(order):
+        big[page] = small.parts["k"][0, int(small.table_host[0, j])].nan_to_num()
+    q = _queries("bf16", 1, 1, (16, H, hd))
+    small.parts["v"] = small.parts["k"]
+    want, tol, _, _ = attention(q, small, 1)
+    out = _context(1, 1, (16, H, hd), 1024).paged_attention(q, KvPages(big, big), table, small.ctx_len).double().cpu().numpy()
+    assert (np.abs(out - want) <= tol).all()
+
+
+def test_repeats_to_the_bit_and_batches_do_not_mix():
+    """Twice the same; an utterance by itself, in the same launch shape, too."""
+    heads = (16, 8, 128)
+    pool = Pool("i8", heads[1:], [3000, 40, 777, 0, 2048], 64)
+    q, c = _queries("f16", 5, 2, heads), _context(5, 2, heads, 3072)
+    a = c.paged_attention(q, pool.pages(), pool.table, pool.ctx_len)
+    for _ in range(3):
+        assert torch.equal(a, c.paged_attention(q, pool.pages(), pool.table, pool.ctx_len))
+    swapped = c.paged_attention(q.flip(0).contiguous(), pool.pages(), pool.table.flip(0).contiguous(), pool.ctx_len.flip(0).contiguous())
+    assert torch.equal(a, swapped.flip(0))
+
+
+def test_other_streams():
+    """The context's stream does the work, whichever is current; results are in order there."""
+    heads = (4, 2, 64)
+    side = torch.cuda.Stream()
+    c = Context(device="cuda:0", stream=side)
+    c.reserve(paged_utts=2, paged_new=1, paged_ctx=2048, paged_heads=heads)
+    pool, q = Pool("e4m3", heads[1:], [2000, 900], 64), _queries("bf16", 2, 1, heads)
+    want, tol, _, _ = attention(q[:, :], pool, 1)
+    torch.cuda.synchronize()
+    out = c.paged_attention(q, pool.pages(), pool.table, pool.ctx_len)
+    side.synchronize()
+    assert (np.abs(out.double().cpu().numpy() - want) <= tol).all()
+    c.close()
+
+
+def test_refusals_of_the_binding():
+    heads = (4, 2, 64)
+    c, pool, q = _context(2, 1, heads, 64), Pool("i8", heads[1:], [60, 20], 16), _queries("f16", 2, 1, heads)
+    call = lambda q=q, pages=pool.pages(), table=pool.table, n=pool.ctx_len, **k: c.paged_attention(q, pages, table, n, **k)
+    call()
+    for bad in (dict(q=q[:1]), dict(q=q.double()), dict(q=torch.empty(2, 1, 64, 4, dtype=q.dtype, device="cuda").transpose(2, 3)), dict(q=q[..., :32]), dict(table=pool.table.long()), dict(table=pool.table.cpu()), dict(table=pool.table[0]),
+                dict(n=pool.ctx_len[:1]), dict(n=pool.ctx_len.long()), dict(n=pool.ctx_len.cpu()), dict(max_ctx=65), dict(out=torch.empty(3, device="cuda")),
+                dict(out=torch.empty(q.numel() + 64, dtype=q.dtype, device="cuda")), dict(lse=torch.empty(3, device="cuda")), dict(q=q.cpu())):
+        with pytest.raises(ValueError):
+            call(**bad)
+    for bad in (dict(q=q[:, :0]), dict(max_ctx=-1), dict(scale=float("inf")), dict(out=q)):
+        with pytest.raises(SsdError):
+            call(**bad)
+    with pytest.raises(SsdError):
+        call(q=q[..., :3, :])
+    moves = lambda **k: c.kv_write_pages(**{**dict(pages=pool.pages(), page_table=pool.table, ctx_len=pool.ctx_len, k=torch.zeros(1, 8, 2, 64, device="cuda"),
+                                                   v=torch.zeros(1, 8, 2, 64, device="cuda"), max_rows=4), **k})
+    moves()
+    moves(max_rows=None)
+    for bad in (dict(start=pool.ctx_len.long()), dict(start=pool.ctx_len[:1]), dict(n_rows=pool.ctx_len.cpu()), dict(max_rows=None, start=pool.ctx_len),
+                dict(k=torch.zeros(1, 7, 2, 64, device="cuda"), v=torch.zeros(1, 7, 2, 64, device="cuda"), max_rows=None), dict(max_ctx=65)):
+        with pytest.raises(ValueError):
+            moves(**bad)
+    with pytest.raises(SsdError):
+        moves(max_rows=5)

@@ -2097,6 +2097,10 @@ PagesArgs pages_args(const ssd_ctx* c, const ssd_kv_pages& p, const ssd_page_tab
     return a;
 }
 
+// Partial results of pieces: means of `rows` query rows, then maxima and sums.
+size_t paged_means(int64_t rows, int64_t pieces, int dims) { return align_up((size_t)(rows * pieces * dims) * 4); }
+size_t paged_bytes(int64_t rows, int64_t pieces, int dims) { return pieces > 1 ? paged_means(rows, pieces, dims) + align_up((size_t)(rows * pieces) * sizeof(float2)) : 0; }
+
 int move_pages(ssd_ctx* ctx, const char* what, bool write, const ssd_kv_view* slots, const int32_t* start, const int32_t* n_rows, int max_rows, const ssd_kv_pages* pages,
                const ssd_page_table* table) {
     const OnDevice on(ctx);
@@ -2156,7 +2160,8 @@ int kv_read_pages(ssd_ctx* ctx, const ssd_kv_pages* pages, const ssd_page_table*
 
 size_t ssd_paged_workspace_bytes(const ssd_ctx* ctx, int n_q_heads, int n_kv_heads, int head_dim, int64_t B, int n_new, int64_t max_ctx) {
     if (!ctx || n_q_heads <= 0 || n_kv_heads <= 0 || head_dim <= 0 || B < 0 || n_new < 0 || max_ctx < 0) return 0;
-    return 256;
+    const int64_t pieces = (max_ctx + PAGED_LEAST_PIECE - 1) / PAGED_LEAST_PIECE;       // at most: no piece is shorter
+    return paged_bytes(B * n_new * n_q_heads, pieces, paged_dims(head_dim)) + 256;
 }
 
 int paged_attention(ssd_ctx* ctx, const void* q, int q_dtype, int64_t q_stride, int n_q_heads, int n_new, const ssd_kv_pages* pages, const ssd_page_table* table,
@@ -2185,6 +2190,14 @@ int paged_attention(ssd_ctx* ctx, const void* q, int q_dtype, int64_t q_stride, 
     a.p = pages_args(ctx, *pages, *table);
     a.q = q; a.q_stride = q_stride; a.out = out; a.lse = lse;
     a.n_q_heads = n_q_heads; a.group = group; a.n_new = n_new; a.scale = scale;
+    a.tiles = (n_new * group + 15) / 16;
+    a.piece = paged_piece((int64_t)table->B * pages->n_kv_heads * a.tiles, table->max_ctx);
+    a.n_pieces = std::max(1, (table->max_ctx + a.piece - 1) / a.piece);
+    const int dims = paged_dims(pages->head_dim);
+    const size_t need = paged_bytes(N * n_q_heads, a.n_pieces, dims);
+    if (need && (!ctx->ws || ctx->ws_bytes < need)) return fail(ctx, SSD_EWORKSPACE, "paged_attention: workspace of %zu bytes needed, %zu set", need, ctx->ws_bytes);
+    a.part_o = static_cast<float*>(ctx->ws);
+    a.part_ml = reinterpret_cast<float2*>(static_cast<char*>(ctx->ws) + paged_means(N * n_q_heads, a.n_pieces, dims));
     {
         ProfScope ps(ctx, SSD_PROF_ATTN);
         launch_paged_attention(a, q_dtype, pages->dtype, ctx->stream);

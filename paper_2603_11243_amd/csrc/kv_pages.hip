@@ -8,8 +8,6 @@ namespace ssd {
 
 namespace {
 
-typedef float f32x2_t __attribute__((ext_vector_type(2)));
-
 // The row of a thread's group of lanes: where it lies on either side, or that it is left out.
 struct Place { int64_t slot, row; };
 __device__ __forceinline__ bool place_of(const MoveArgs& a, int b, int i, int head, int layer, int n, Place& at, bool& bad) {

@@ -42,7 +42,18 @@ struct PagedAttnArgs {
     void* out; float* lse;
     int32_t n_q_heads, group, n_new;         // group: query heads of a K/V head
     float scale;
+    int32_t tiles;                           // of 16 query rows, tokens times group
+    int32_t piece, n_pieces;                 // rows of a piece of a context, pieces of max_ctx rows
+    float* part_o; float2* part_ml;          // [token][query head][piece] mean of values (64 or 128 dims), (maximum to base 2, sum); not used by contexts of one piece
 };
+constexpr int PAGED_LEAST_PIECE = 256, PAGED_MOST_PIECE = 4096;      // (a wavefront has the pages of at most 4096 rows of its workgroup)
+inline int paged_dims(int head_dim) { return head_dim > 64 ? 128 : 64; }
+// Rows of a piece.
+inline int paged_piece(int64_t pairs, int64_t max_ctx) {
+    const int64_t share = pairs * max_ctx / 1024;
+    const int64_t rows = (share + 255) / 256 * 256;
+    return (int)(rows < PAGED_LEAST_PIECE ? PAGED_LEAST_PIECE : rows > 1024 ? 1024 : rows);
+}
 void launch_paged_attention(const PagedAttnArgs& a, int q_dtype, int pages_dtype, hipStream_t st);
 
 }  // namespace ssd

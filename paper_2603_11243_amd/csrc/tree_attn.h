@@ -1,4 +1,5 @@
-// What the kernels of tree_attn.hip (16-bit caches) and tree_attn_f32.hip share: element types, the mask, the merge of a workgroup's wavefronts.
+// What the kernels of tree_attn.hip (16-bit caches) and tree_attn_f32.hip share: element types, the mask, the merge of a workgroup's wavefronts; element
+// types and pairs of 16-bit values also with kv_pages.hip and paged_attn.hip.
 #pragma once
 #include "gemm_core.h"
 #include "tree.h"
@@ -25,6 +26,39 @@ template <> struct Elem<SSD_F16> {
 __device__ __forceinline__ bool sees(uint32_t node, uint32_t key) {
     const uint32_t at = node & 0xffffu;
     return at >= (key & 0xffffu) && at < (key >> 16);
+}
+
+// Pairs of 16-bit values w, as whole numbers (a magnitude plus TO_SIGN reaches the sign bit from the infinities on):
+template <bool BF> constexpr uint32_t TO_SIGN = BF ? 0x00800080u : 0x04000400u;
+template <bool BF> constexpr uint32_t ONE = BF ? 0x3f80u : 0x3c00u;
+constexpr uint32_t SIGNS = 0x80008000u;
+template <bool BF> __device__ __forceinline__ uint32_t beyond_of(uint32_t w) { return (w & ~SIGNS) + TO_SIGN<BF>; }   // sign bit: not finite
+__device__ __forceinline__ uint32_t not_zero(uint32_t w) { return (w & ~SIGNS) + ~SIGNS; }                               // sign bit: not zero
+template <bool BF> __device__ __forceinline__ uint32_t one_where(uint32_t w) { return ((w & SIGNS) >> 15) * ONE<BF>; }
+// infinities of a sign (negative: all bits) and NaN as 1, all else 0; what is finite, else 0
+template <bool BF> __device__ __forceinline__ uint32_t infinite_of(uint32_t w, uint32_t negative) {
+    const uint32_t t = beyond_of<BF>(w);
+    return one_where<BF>(t & (~(w ^ negative) | not_zero(t)));
+}
+template <bool BF> __device__ __forceinline__ uint32_t finite_of(uint32_t w) { return w & ~(((beyond_of<BF>(w) & SIGNS) >> 15) * 0xffffu); }
+
+// Two values to the operand type, round to nearest even, by the conversion instruction of a pair.
+typedef float f32x2_t __attribute__((ext_vector_type(2)));
+typedef _Float16 f16x2_t __attribute__((ext_vector_type(2)));
+typedef __bf16 bf16x2_t __attribute__((ext_vector_type(2)));
+typedef uint32_t u32x2_t __attribute__((ext_vector_type(2)));
+template <bool BF> __device__ __forceinline__ uint32_t pack16(float lo, float hi) {
+    const f32x2_t v = {lo, hi};
+    if constexpr (BF) return __builtin_bit_cast(uint32_t, __builtin_convertvector(v, bf16x2_t));
+    else return __builtin_bit_cast(uint32_t, __builtin_convertvector(v, f16x2_t));
+}
+// What the rounding of two values to the pair w left of them, exact in fp32, as another pair.
+template <bool BF> __device__ __forceinline__ uint32_t rest16(float lo, float hi, uint32_t w) {
+    if constexpr (BF) return pack16<BF>(lo - __uint_as_float(w << 16), hi - __uint_as_float(w & 0xffff0000u));
+    else {
+        const f16x2_t h = __builtin_bit_cast(f16x2_t, w);
+        return pack16<BF>(lo - (float)h.x, hi - (float)h.y);
+    }
 }
 
 constexpr float LOG2E = 1.4426950408889634f, LN2 = 0.6931471805599453f;

@@ -477,7 +477,7 @@ typedef struct {
 /* Whose pages they are.  Row j of utterance b lies in page entries[b * stride + j / page_rows], at row j % page_rows of it.  The arrays are DEVICE arrays,
  * unlike those of other calls: a captured step is replayed with the lengths and pages that they hold then.  Their values are checked on the device: rows of a page
  * outside [0, pages) are left out (not written, not read, not seen), a ctx_len outside [0, max_ctx] counts as the nearer end (in kv_write_pages and kv_read_pages
- * the rows outside are left out), and SSD_FLAG_BAD_PAGE is raised.  Entries behind an utterance's last row are not read.  Utterances may share pages that are only read. */
+ * the rows outside are left out), and SSD_FLAG_BAD_PAGE is raised.  Entries behind an utterance's last row may hold anything.  Utterances may share pages that are only read. */
 typedef struct {
     const int32_t *entries;       /* dev */
     int64_t stride;               /* at least ceil(max_ctx / page_rows) */

@@ -241,7 +241,7 @@ class KvPages:
             if k_scale.shape != k.shape[:-1] or v_scale.shape != k.shape[:-1]:
                 raise ValueError("k_scale and v_scale must be [layers,] pages, K/V heads, rows of a page")
         self.k, self.v, self.k_scale, self.v_scale = k, v, k_scale, v_scale
-        self.device, self.dtype = k.device, k.dtype
+        self.device, self.dtype, self._index = k.device, k.dtype, k.get_device()
         self.n_pages, self.n_kv_heads, self.page_rows, self.head_dim = k.shape[-4:]
         self.n_layers = k.shape[0] if k.dim() == 5 else 1
         self._view = _KV_PAGES.pack(k.data_ptr(), v.data_ptr(), 0 if k_scale is None else k_scale.data_ptr(), 0 if v_scale is None else v_scale.data_ptr(), self.n_pages,
@@ -278,6 +278,7 @@ class Context:
         self._ws = None
         self._h = C.c_void_p()
         torch.cuda.set_device(self.device)
+        self._index = torch.cuda.current_device()
         st = stream if stream is not None else torch.cuda.current_stream(self.device)
         self.stream = st
         cfg_p, w_p = None, None
@@ -694,40 +695,39 @@ class Context:
 
     # ---- K/V rows in pages -----------------------------------------------------------------------
 
-    def _page_table(self, pages: KvPages, page_table: torch.Tensor, ctx_len: torch.Tensor, max_ctx: Optional[int]) -> bytes:
-        """ssd_page_table of page_table [B, entries] and ctx_len [B], both int32 on the device."""
-        if page_table.dim() != 2 or page_table.dtype is not torch.int32 or not _at(page_table, self.device) or (page_table.shape[1] > 1 and page_table.stride(1) != 1):
-            raise ValueError(f"page_table must be an int32 tensor [utterances, entries] on {self.device}, the entries of an utterance consecutive")
-        B, entries = page_table.shape
-        if ctx_len.dtype is not torch.int32 or ctx_len.dim() != 1 or ctx_len.shape[0] != B or not ctx_len.is_contiguous() or not _at(ctx_len, self.device):
-            raise ValueError(f"ctx_len must be a contiguous int32 tensor [{B}] on {self.device}")
-        if not _at(pages.k, self.device):
-            raise ValueError(f"the pages must be on {self.device}")
+    def _page_table(self, pages: KvPages, page_table: torch.Tensor, ctx_len: torch.Tensor, max_ctx: Optional[int]):
+        """(ssd_page_table, utterances) of page_table [B, entries] and ctx_len [B], both int32 on the device.  (An attribute of a tensor is 0.1 us, its shape 0.25.)"""
+        i32, index = torch.int32, self._index
+        if page_table.dtype is not i32 or ctx_len.dtype is not i32 or page_table.get_device() != index or ctx_len.get_device() != index or pages._index != index:
+            raise ValueError(f"page_table and ctx_len must be int32 tensors on the device of the context, {self.device}, and the pages be there")
+        B = ctx_len.numel()
+        if page_table.dim() != 2 or ctx_len.dim() != 1 or not ctx_len.is_contiguous():
+            raise ValueError("page_table must be [utterances, entries], ctx_len [utterances] and contiguous")
+        rows, entries = page_table.shape
+        stride, one = page_table.stride()
+        if rows != B or (one != 1 and entries > 1):
+            raise ValueError("page_table and ctx_len must be of as many utterances, the entries of an utterance consecutive")
         most = min(entries * pages.page_rows, 1 << 30)
         if max_ctx is None:
             max_ctx = most
         elif max_ctx > most:
             raise ValueError(f"a table of {entries} entries holds {most} rows an utterance, not {max_ctx}")
-        return _PAGE_TABLE.pack(page_table.data_ptr(), page_table.stride(0) if B > 1 else max(entries, 1), ctx_len.data_ptr(), B, max_ctx)
+        return _PAGE_TABLE.pack(page_table.data_ptr(), stride if B > 1 else max(entries, 1), ctx_len.data_ptr(), B, max_ctx), B
 
     def _move_pages(self, write, pages, page_table, ctx_len, k, v, start, n_rows, max_rows, max_ctx):
-        table = self._page_table(pages, page_table, ctx_len, max_ctx)
+        table, B = self._page_table(pages, page_table, ctx_len, max_ctx)
         view, slots, _, _, _ = _kv_view(self.device, k, v)
-        B = page_table.shape[0]
-        for name, t in (("start", start), ("n_rows", n_rows)):
-            if t is not None:
-                _on(self.device, torch.int32, **{name: t})
-                if t.numel() != B:
-                    raise ValueError(f"{name} must have an entry an utterance")
+        for t in (start, n_rows):
+            if t is not None and (t.dtype is not torch.int32 or t.get_device() != self._index or t.numel() != B or not t.is_contiguous()):
+                raise ValueError(f"start and n_rows must be contiguous int32 tensors of an entry an utterance on {self.device}")
         if max_rows is None:
             if start is not None or n_rows is not None or B == 0 or slots % B:
                 raise ValueError("max_rows is needed where not every utterance has the same number of slots, one behind the other")
             max_rows = slots // B
         s, n = None if start is None else start.data_ptr(), None if n_rows is None else n_rows.data_ptr()
-        if write:
-            self._check(self._lib.kv_write_pages(self._h, view, s, n, max_rows, pages._view, table))
-        else:
-            self._check(self._lib.kv_read_pages(self._h, pages._view, table, view, s, n, max_rows))
+        rc = self._lib.kv_write_pages(self._h, view, s, n, max_rows, pages._view, table) if write else self._lib.kv_read_pages(self._h, pages._view, table, view, s, n, max_rows)
+        if rc:
+            self._check(rc)
 
     def kv_write_pages(self, pages: KvPages, page_table: torch.Tensor, ctx_len: torch.Tensor, k: torch.Tensor, v: torch.Tensor, start: Optional[torch.Tensor] = None,
                        n_rows: Optional[torch.Tensor] = None, max_rows: Optional[int] = None, max_ctx: Optional[int] = None):
@@ -746,35 +746,42 @@ class Context:
         """Attention of the newest tokens over the pages of their utterances (paged_attention): q [utterances, query heads, head_dim], or [utterances, tokens, query heads,
         head_dim] (any stride between tokens).  ctx_len counts the new tokens; max_ctx: the longest context the launch is made for (what page_table holds unless
         given).  Returns out in the shape of q; lse [.., query heads] takes the log-sum-exps (float32, optional).  scale: 1 / sqrt(head_dim) unless given."""
-        table = self._page_table(pages, page_table, ctx_len, max_ctx)
-        shape, st, code = q.shape, q.stride(), _KV_CODE.get(q.dtype)
-        if len(shape) not in (3, 4) or code is None or q.device != pages.device or shape[0] != ctx_len.shape[0]:
-            raise ValueError("q must be [utterances, [tokens,] query heads, head_dim], float16, bfloat16 or float32, on the device of the pages")
-        Hq, hd = shape[-2:]
-        n_new = shape[1] if len(shape) == 4 else 1
-        if hd != pages.head_dim or (hd > 1 and st[-1] != 1) or (Hq > 1 and st[-2] != hd) or (len(shape) == 4 and shape[0] > 1 and n_new > 1 and st[0] != n_new * st[1]):
-            raise ValueError("q must have the head_dim of the pages, the heads of a token consecutive, tokens at equal distances")
-        q_stride = st[1] if n_new > 1 else st[0] if shape[0] > 1 else Hq * hd
-        if out is None:
-            out = self._new(shape, q.dtype)
+        table, B = self._page_table(pages, page_table, ctx_len, max_ctx)
+        st, code, index = q.stride(), _KV_CODE.get(q.dtype), self._index
+        if len(st) == 4:
+            n, n_new, Hq, hd = q.shape
+            step, q_stride, head, one = st
+            if n_new == 1:
+                q_stride = step
+            elif n > 1 and n_new > 1 and step != n_new * q_stride:
+                raise ValueError("tokens of q must lie at equal distances")
+        elif len(st) == 3:
+            (n, Hq, hd), n_new = q.shape, 1
+            q_stride, head, one = st
         else:
-            _on(self.device, q.dtype, out=out)
-            if out.numel() != q.numel():
-                raise ValueError("out has the wrong size")
-        if lse is not None:
-            _on(self.device, torch.float32, lse=lse)
-            if lse.numel() * hd != q.numel():
-                raise ValueError("lse has the wrong size")
-        self._check(self._lib.paged_attention(self._h, q.data_ptr(), code, q_stride, Hq, n_new, pages._view, table, hd ** -0.5 if scale is None else scale, out.data_ptr(),
-                                              None if lse is None else lse.data_ptr()))
+            raise ValueError("q must be [utterances, [tokens,] query heads, head_dim]")
+        if n != B or hd != pages.head_dim or code is None or q.get_device() != index or (one != 1 and hd > 1) or (head != hd and Hq > 1):
+            raise ValueError("q must be float16, bfloat16 or float32 on the device of the pages, with their head_dim, a token of each utterance, the heads of a token consecutive")
+        if n * n_new <= 1:
+            q_stride = Hq * hd
+        if out is None:
+            out = self._like(q)
+        elif out.dtype is not q.dtype or out.get_device() != index or not out.is_contiguous() or out.numel() != q.numel():
+            raise ValueError("out must be contiguous, of the type, the size and the device of q")
+        if lse is not None and (lse.dtype is not torch.float32 or lse.get_device() != index or not lse.is_contiguous() or lse.numel() != n * n_new * Hq):
+            raise ValueError("lse must be a contiguous float32 tensor of an entry a token and query head on the device of q")
+        rc = self._lib.paged_attention(self._h, q.data_ptr(), code, q_stride, Hq, n_new, pages._view, table, hd ** -0.5 if scale is None else scale, out.data_ptr(),
+                                       None if lse is None else lse.data_ptr())
+        if rc:
+            self._check(rc)
         return out
 
-    def _new(self, shape, dtype) -> torch.Tensor:
-        """A tensor that the context's stream writes first: of that stream, so that memory in use on the current one is not given out again."""
-        if torch.cuda.current_stream(self.device) == self.stream:
-            return torch.empty(shape, dtype=dtype, device=self.device)
+    def _like(self, t) -> torch.Tensor:
+        """A contiguous tensor like t that the context's stream writes first: of that stream, so that memory in use on the current one is not given out again."""
+        if torch._C._cuda_getCurrentRawStream(self._index) == self.stream.cuda_stream:
+            return torch.empty_like(t, memory_format=torch.contiguous_format)
         with torch.cuda.stream(self.stream):
-            return torch.empty(shape, dtype=dtype, device=self.device)
+            return torch.empty_like(t, memory_format=torch.contiguous_format)
 
     def accept_prefix(self, h_verify: torch.Tensor, draft_ids: torch.Tensor, cu_draft, tau_slm: float,
                       want_greedy: bool = False, out: Optional[dict] = None) -> dict:

@@ -2097,9 +2097,33 @@ PagesArgs pages_args(const ssd_ctx* c, const ssd_kv_pages& p, const ssd_page_tab
     return a;
 }
 
-// Partial results of pieces: means of `rows` query rows, then maxima and sums.
-size_t paged_means(int64_t rows, int64_t pieces, int dims) { return align_up((size_t)(rows * pieces * dims) * 4); }
-size_t paged_bytes(int64_t rows, int64_t pieces, int dims) { return pieces > 1 ? paged_means(rows, pieces, dims) + align_up((size_t)(rows * pieces) * sizeof(float2)) : 0; }
+// How a paged_attention call cuts its contexts, and its workspace: means of pieces, maxima and sums, first pieces.
+// Bytes for means of `rows` rows of pieces, their maxima and sums, and B first pieces.
+size_t paged_ml(int64_t rows, int dims) { return align_up((size_t)(rows * dims) * 4); }
+size_t paged_first(int64_t rows, int dims) { return paged_ml(rows, dims) + align_up((size_t)rows * sizeof(float2)); }
+size_t paged_bytes(int64_t rows, int dims, int64_t B) { return paged_first(rows, dims) + align_up((size_t)B * sizeof(int2)); }
+struct PagedPlan { int shared, n_pieces; size_t ml, first, total; };
+PagedPlan plan_paged(int64_t B, int64_t n_kv_heads, int64_t rows, int head_dim, int64_t max_ctx) {
+    const int64_t tiles = (rows + paged_tile_rows(rows) - 1) / paged_tile_rows(rows), most = (max_ctx + PAGED_UNIT - 1) / PAGED_UNIT, pairs = n_kv_heads * tiles;
+    PagedPlan p = {0, 1, 0, 0, 0};
+    if (most > paged_whole(pairs * B)) {
+        if (B <= PAGED_UTTS && B * most < INT32_MAX) {
+            const int64_t at_once = std::max<int64_t>(1, PAGED_CUS * paged_per_cu(head_dim, paged_tile_rows(rows)) / pairs);
+            p.shared = (int)(at_once * ((PAGED_EACH * B + at_once - 1) / at_once));
+            const int64_t rounds = std::max<int64_t>(1, (B * most + (int64_t)p.shared * PAGED_MOST - 1) / ((int64_t)p.shared * PAGED_MOST));
+            p.n_pieces = (int)std::min<int64_t>(p.shared * rounds + B, B * most);
+        } else {
+            p.n_pieces = (int)((most + PAGED_MOST - 1) / PAGED_MOST);
+        }
+    }
+    if (p.n_pieces > 1) {
+        const int64_t all = (p.shared ? p.n_pieces : p.n_pieces * B) * n_kv_heads * rows;
+        p.ml = paged_ml(all, paged_dims(head_dim));
+        p.first = paged_first(all, paged_dims(head_dim));
+        p.total = paged_bytes(all, paged_dims(head_dim), B);
+    }
+    return p;
+}
 
 int move_pages(ssd_ctx* ctx, const char* what, bool write, const ssd_kv_view* slots, const int32_t* start, const int32_t* n_rows, int max_rows, const ssd_kv_pages* pages,
                const ssd_page_table* table) {
@@ -2160,8 +2184,9 @@ int kv_read_pages(ssd_ctx* ctx, const ssd_kv_pages* pages, const ssd_page_table*
 
 size_t ssd_paged_workspace_bytes(const ssd_ctx* ctx, int n_q_heads, int n_kv_heads, int head_dim, int64_t B, int n_new, int64_t max_ctx) {
     if (!ctx || n_q_heads <= 0 || n_kv_heads <= 0 || head_dim <= 0 || B < 0 || n_new < 0 || max_ctx < 0) return 0;
-    const int64_t pieces = (max_ctx + PAGED_LEAST_PIECE - 1) / PAGED_LEAST_PIECE;       // at most: no piece is shorter
-    return paged_bytes(B * n_new * n_q_heads, pieces, paged_dims(head_dim)) + 256;
+    const int64_t most = (max_ctx + PAGED_UNIT - 1) / PAGED_UNIT, rows = (int64_t)n_new * n_q_heads;
+    // (as many workgroups as run at once, four a CU at most, with 32 rows each, or more pieces: see plan_paged)
+    return paged_bytes(4 * PAGED_CUS * 32 + (B * most / PAGED_MOST + (PAGED_EACH + 1) * B + 2) * rows, paged_dims(head_dim), B) + 256;
 }
 
 int paged_attention(ssd_ctx* ctx, const void* q, int q_dtype, int64_t q_stride, int n_q_heads, int n_new, const ssd_kv_pages* pages, const ssd_page_table* table,
@@ -2190,14 +2215,16 @@ int paged_attention(ssd_ctx* ctx, const void* q, int q_dtype, int64_t q_stride, 
     a.p = pages_args(ctx, *pages, *table);
     a.q = q; a.q_stride = q_stride; a.out = out; a.lse = lse;
     a.n_q_heads = n_q_heads; a.group = group; a.n_new = n_new; a.scale = scale;
-    a.tiles = (n_new * group + 15) / 16;
-    a.piece = paged_piece((int64_t)table->B * pages->n_kv_heads * a.tiles, table->max_ctx);
-    a.n_pieces = std::max(1, (table->max_ctx + a.piece - 1) / a.piece);
-    const int dims = paged_dims(pages->head_dim);
-    const size_t need = paged_bytes(N * n_q_heads, a.n_pieces, dims);
-    if (need && (!ctx->ws || ctx->ws_bytes < need)) return fail(ctx, SSD_EWORKSPACE, "paged_attention: workspace of %zu bytes needed, %zu set", need, ctx->ws_bytes);
-    a.part_o = static_cast<float*>(ctx->ws);
-    a.part_ml = reinterpret_cast<float2*>(static_cast<char*>(ctx->ws) + paged_means(N * n_q_heads, a.n_pieces, dims));
+    a.tile_rows = paged_tile_rows((int64_t)n_new * group);
+    a.tiles = (n_new * group + a.tile_rows - 1) / a.tile_rows;
+    const PagedPlan plan = plan_paged(table->B, pages->n_kv_heads, (int64_t)n_new * group, pages->head_dim, table->max_ctx);
+    if (plan.total && (!ctx->ws || ctx->ws_bytes < plan.total))
+        return fail(ctx, SSD_EWORKSPACE, "paged_attention: workspace of %zu bytes needed, %zu set", plan.total, ctx->ws_bytes);
+    a.shared = plan.shared; a.n_pieces = plan.n_pieces;
+    char* ws = static_cast<char*>(ctx->ws);
+    a.part_o = reinterpret_cast<float*>(ws);
+    a.part_ml = reinterpret_cast<float2*>(ws + plan.ml);
+    a.first = reinterpret_cast<int2*>(ws + plan.first);
     {
         ProfScope ps(ctx, SSD_PROF_ATTN);
         launch_paged_attention(a, q_dtype, pages->dtype, ctx->stream);

@@ -24,19 +24,34 @@ template <int QT, int PT> struct Kind {
     static constexpr bool CODES = PT == SSD_E4M3 || PT == SSD_I8, F32 = PT == SSD_F32, BF = PT != SSD_F16;
     static constexpr int SIZE = CODES ? 1 : F32 ? 4 : 2;                     // bytes of an element
     static constexpr int KEYS = CODES ? 32 : F32 ? 16 : 32, TILES = KEYS / 16;     // 64 registers a lane of keys and values in flight
-    static constexpr int QN = !CODES || QT == SSD_BF16 ? 1 : QT == SSD_F16 ? 2 : 3;      // 16-bit values that a query is the exact sum of
+    static constexpr bool QBF = CODES ? QT != SSD_F16 : BF;                  // the first product's operands: the queries' type, which holds the codes exactly
+    static constexpr int QN = CODES && QT == SSD_F32 ? 3 : 1;                // 16-bit values that a query is the exact sum of
     static constexpr int PN = QT == SSD_F32 ? 3 : 2;                         // those of a weight
     // weights are taken times 2^BIAS: in half's upper range, or so that sums of 2^30 values at the end of fp32's range stay in it
     static constexpr float BIAS = PT == SSD_F16 ? 15.f : -32.f;
 };
 
-// Two codes to a pair of bfloat16, exactly: bytes 2 H and 2 H + 1 of w.
-template <int PT, bool HIGH>
+// Whole number in byte I of w as fp32.  (Written out because the compiler takes the bytes apart first.)
+template <int I>
+__device__ __forceinline__ float whole(uint32_t w) {
+    float v;
+    if constexpr (I == 0) asm("v_cvt_f32_i32_sdwa %0, sext(%1) dst_sel:DWORD dst_unused:UNUSED_PAD src0_sel:BYTE_0" : "=v"(v) : "v"(w));
+    else if constexpr (I == 1) asm("v_cvt_f32_i32_sdwa %0, sext(%1) dst_sel:DWORD dst_unused:UNUSED_PAD src0_sel:BYTE_1" : "=v"(v) : "v"(w));
+    else if constexpr (I == 2) asm("v_cvt_f32_i32_sdwa %0, sext(%1) dst_sel:DWORD dst_unused:UNUSED_PAD src0_sel:BYTE_2" : "=v"(v) : "v"(w));
+    else asm("v_cvt_f32_i32_sdwa %0, sext(%1) dst_sel:DWORD dst_unused:UNUSED_PAD src0_sel:BYTE_3" : "=v"(v) : "v"(w));
+    return v;
+}
+
+// Two codes to a pair of bfloat16 (BF) or half, exactly: bytes 2 HIGH and 2 HIGH + 1 of w.
+template <int PT, bool BF, bool HIGH>
 __device__ __forceinline__ uint32_t code_pair(uint32_t w) {
-    if constexpr (PT == SSD_E4M3) return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w, 1.f, HIGH));
-    else {
-        const float lo = (float)(int8_t)(w >> (HIGH ? 16 : 0)), hi = (float)(int8_t)(w >> (HIGH ? 24 : 8));
-        return __builtin_amdgcn_perm(__float_as_uint(hi), __float_as_uint(lo), 0x07060302u);
+    if constexpr (PT == SSD_E4M3) {
+        if constexpr (BF) return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w, 1.f, HIGH));
+        else return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(w, 1.f, HIGH));
+    } else {
+        const float lo = whole<2 * HIGH>(w), hi = whole<2 * HIGH + 1>(w);
+        if constexpr (BF) return __builtin_amdgcn_perm(__float_as_uint(hi), __float_as_uint(lo), 0x07060302u);
+        else return pack16<false>(lo, hi);
     }
 }
 
@@ -94,9 +109,126 @@ template <int HD> struct Queries<SSD_F32, SSD_F32, HD> {
 
 __device__ __forceinline__ f32x4_t mfma_f32(float a, float b, const f32x4_t& c) { return __builtin_amdgcn_mfma_f32_16x16x4f32(a, b, c, 0, 0, 0); }
 
-struct Piece { int b, kvh, tile, from, to, len; };
+// What a workgroup does: piece `part` of n of utterance b, rows from ..; index: the piece's number among all.
+struct Piece { int b, part, n, index, len, given, from, rows; };
 
-template <int QT, int PT, int HD>
+__device__ __forceinline__ int units(int rows) { return (rows + PAGED_UNIT - 1) / PAGED_UNIT; }
+__device__ __forceinline__ int clamped(const PagesArgs& p, int len) { return min(max(len, 0), p.max_ctx); }
+
+// Shared pieces for so many units in all; units of one.
+__device__ __forceinline__ int shared_pieces(const PagedAttnArgs& a, int total) {
+    const uint32_t whole = (uint32_t)a.shared * PAGED_MOST;
+    return a.shared * (int)max(1u, ((uint32_t)total + whole - 1) / whole);
+}
+__device__ __forceinline__ int shared_units(const PagedAttnArgs& a, int total, int pieces) {
+    return max(1, (int)(((uint32_t)total + pieces - 1) / (uint32_t)pieces));
+}
+
+__device__ __forceinline__ int lanes_sum(int v) {
+#pragma unroll
+    for (int d = 1; d < 64; d *= 2) v += __shfl_xor(v, d);
+    return v;
+}
+
+// The workgroup's piece; false: there is none.  Up to 64 utterances a wavefront finds it by itself, a lane an utterance.
+__device__ __forceinline__ bool find_piece(const PagedAttnArgs& a, Piece& t) {
+    const PagesArgs& p = a.p;
+    const int lane = threadIdx.x % 64, x = blockIdx.x;
+    int size;
+    if (a.shared == 0) {
+        t.b = blockIdx.z / a.tiles;
+        t.part = x;
+        t.given = p.ctx_len[t.b];
+        t.len = clamped(p, t.given);
+        size = PAGED_MOST;
+        t.n = max(1, (units(t.len) + size - 1) / size);
+        t.index = t.b * a.n_pieces + x;
+        if (a.n_pieces > 1 && x >= t.n) return false;
+    } else if (p.B <= 64) {
+        const int given = lane < p.B ? p.ctx_len[lane] : 0, len = clamped(p, given), u = units(len);
+        const int total = lanes_sum(u);
+        const int wanted = shared_pieces(a, total), want = max(wanted, p.B);
+        int share = shared_units(a, total, wanted), n, pieces;
+        // every utterance's last piece is a shorter one: so many more than wanted, and a second round of workgroups for them, until pieces are a little longer
+        for (int turn = 0;; ++turn) {
+            n = lane < p.B ? max(1, (int)((uint32_t)(u + share - 1) / (uint32_t)share)) : 0;
+            pieces = lanes_sum(n);
+            if (pieces <= want || share == PAGED_MOST || turn == 8) break;
+            share = min(PAGED_MOST, max(share + 1, (int)((float)share * (float)pieces / (float)want)));
+        }
+        int sum = n;
+#pragma unroll
+        for (int d = 1; d < 64; d *= 2) {
+            const int before = __shfl_up(sum, d);
+            sum += lane >= d ? before : 0;
+        }
+        const uint64_t behind = __ballot(sum > x);
+        if (!behind) return false;
+        t.b = __ffsll((unsigned long long)behind) - 1;
+        t.n = __builtin_amdgcn_readlane(n, t.b);
+        t.part = x - (__builtin_amdgcn_readlane(sum, t.b) - t.n);
+        t.given = __builtin_amdgcn_readlane(given, t.b);
+        t.len = __builtin_amdgcn_readlane(len, t.b);
+        t.index = x;
+    } else {
+        constexpr int THREADS = 64 * WAVES, PER = PAGED_UTTS / THREADS;
+        __shared__ int wave_s[WAVES], found_s[4];
+        const int tid = threadIdx.x, wave = tid / 64;
+        int given[PER], u = 0;
+#pragma unroll
+        for (int e = 0; e < PER; ++e) {
+            given[e] = tid * PER + e < p.B ? p.ctx_len[tid * PER + e] : 0;
+            u += units(clamped(p, given[e]));
+        }
+        u = lanes_sum(u);
+        if (lane == 0) wave_s[wave] = u;
+        __syncthreads();
+        int total = 0;
+#pragma unroll
+        for (int w = 0; w < WAVES; ++w) total += wave_s[w];
+        const int share = shared_units(a, total, shared_pieces(a, total));
+        int n[PER], mine = 0;
+#pragma unroll
+        for (int e = 0; e < PER; ++e) mine += n[e] = tid * PER + e < p.B ? max(1, (int)((uint32_t)(units(clamped(p, given[e])) + share - 1) / (uint32_t)share)) : 0;
+        int sum = mine;
+#pragma unroll
+        for (int d = 1; d < 64; d *= 2) {
+            const int before = __shfl_up(sum, d);
+            sum += lane >= d ? before : 0;
+        }
+        __syncthreads();
+        if (lane == 63) wave_s[wave] = sum;
+        if (tid == 0) found_s[0] = -1;
+        __syncthreads();
+#pragma unroll
+        for (int w = 0; w < WAVES; ++w) sum += w < wave ? wave_s[w] : 0;
+        int at = sum - mine;
+#pragma unroll
+        for (int e = 0; e < PER; ++e) {
+            if (x >= at && x < at + n[e]) {
+                found_s[0] = tid * PER + e;
+                found_s[1] = n[e];
+                found_s[2] = x - at;
+                found_s[3] = given[e];
+            }
+            at += n[e];
+        }
+        __syncthreads();
+        t.b = __builtin_amdgcn_readfirstlane(found_s[0]);
+        if (t.b < 0) return false;
+        t.n = __builtin_amdgcn_readfirstlane(found_s[1]);
+        t.part = __builtin_amdgcn_readfirstlane(found_s[2]);
+        t.given = __builtin_amdgcn_readfirstlane(found_s[3]);
+        t.len = clamped(p, t.given);
+        t.index = x;
+    }
+    if (a.shared) size = (int)((uint32_t)(units(t.len) + t.n - 1) / (uint32_t)t.n);     // equal pieces; (n - 1 of them are less than the context)
+    t.rows = size * PAGED_UNIT;
+    t.from = t.part * t.rows;
+    return true;
+}
+
+template <int QT, int PT, int HD, int NT>
 __global__ void __launch_bounds__(64 * WAVES, 2) paged_attn_kernel(PagedAttnArgs a) {
     typedef Kind<QT, PT> T;
     typedef Elem<QT> E;
@@ -107,28 +239,32 @@ __global__ void __launch_bounds__(64 * WAVES, 2) paged_attn_kernel(PagedAttnArgs
     const PagesArgs& p = a.p;
     const int lane = threadIdx.x % 64, g = lane / 16, dc = lane % 16, hd = T::F32 ? p.head_dim : HD;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
-    const int part = blockIdx.x, kvh = blockIdx.y, b = blockIdx.z / a.tiles, tile = blockIdx.z % a.tiles;
-    const int given = p.ctx_len[b], len = min(max(given, 0), p.max_ctx);
-    const int from = part * a.piece, to = min(len, from + a.piece);
-    if (part > 0 && from >= len) return;                     // (the first piece answers for an empty context)
-    const bool only = len <= a.piece;
-    bool bad = given != len;
+    const int kvh = blockIdx.y, tile = a.shared ? blockIdx.z : blockIdx.z % a.tiles;
+    Piece t;
+    if (!find_piece(a, t)) return;
+    const int b = t.b, len = t.len, from = t.from, to = min(len, from + t.rows);
+    const bool only = t.n == 1;
+    bool bad = t.given != len;
 
     // Pages of the wavefront's tiles: lane i has those of tile i % TILES of its block i / TILES.
     const int first = from + wave * KEYS, blocks = (to - first + STEP - 1) / STEP;
     int pages = -1;
     {
         const int key = first + lane / TILES * STEP + 16 * (lane % TILES);
-        if (key < to) {
-            pages = page_of(p, b, key);
-            bad |= pages < 0;
-        }
+        if (key < min(from + t.rows, p.max_ctx)) pages = page_of(p, b, key);      // (without waiting for the length)
+        bad |= key < to && pages < 0;
+        if (key >= to) pages = -1;
     }
-    const int rows = a.n_new * a.group, row = min(tile * 16 + dc, rows - 1), token = row / a.group;
-    const int limit = len - (a.n_new - 1 - token);           // the column's token sees the rows before it
-    const int least = len - (a.n_new - 1 - min(tile * 16, rows - 1) / a.group);     // what all columns see
-    Queries<QT, PT, HD> q;
-    q.load(a.q, ((int64_t)b * a.n_new + token) * a.q_stride + (int64_t)(kvh * a.group + row % a.group) * hd, hd, g);
+    const int rows = a.n_new * a.group, row0 = tile * 16 * NT;
+    const int least = len - (a.n_new - 1 - min(row0, rows - 1) / a.group);      // what all columns see
+    int limit[NT];                                           // the column's token sees the rows before it
+    Queries<QT, PT, HD> q[NT];
+#pragma unroll
+    for (int u = 0; u < NT; ++u) {
+        const int row = min(row0 + 16 * u + dc, rows - 1), token = row / a.group;
+        limit[u] = len - (a.n_new - 1 - token);
+        q[u].load(a.q, ((int64_t)b * a.n_new + token) * a.q_stride + (int64_t)(kvh * a.group + row % a.group) * hd, hd, g);
+    }
 
     u32x4_t kr[TILES][K_LOADS];
     constexpr int WORDS = T::F32 ? 4 : V_WORDS, V_PARTS = V_WORDS / WORDS;
@@ -174,83 +310,119 @@ __global__ void __launch_bounds__(64 * WAVES, 2) paged_attn_kernel(PagedAttnArgs
         load_values(0);
     }
     const float sc = a.scale * LOG2E;
-    float m = -F32_MOST, l = 0.f;
-    f32x4_t o[DT];
+    float m[NT], l[NT];
+    f32x4_t o[NT][DT];
+    uint32_t lost[NT];                                       // outputs 4 i + e of the lane that are NaN because of a row that only some columns see
 #pragma unroll
-    for (int i = 0; i < DT; ++i) o[i] = (f32x4_t){0.f, 0.f, 0.f, 0.f};
-
+    for (int u = 0; u < NT; ++u) {
+        m[u] = -F32_MOST;
+        l[u] = 0.f;
+        lost[u] = 0;
+#pragma unroll
+        for (int i = 0; i < DT; ++i) o[u][i] = (f32x4_t){0.f, 0.f, 0.f, 0.f};
+    }
     const bool whole = !__any(bad);
-    for (int block = 0; block < blocks; ++block) {
+    auto add_block = [&](auto last_c, int block) __attribute__((always_inline)) {
+        constexpr bool LAST = decltype(last_c)::value;
         const int k0 = first + block * STEP;
         const bool masked = !whole || k0 + KEYS > min(least, to);
-        float s[TILES][4];
+        float s[NT][TILES][4];
 #pragma unroll
         for (int c = 0; c < TILES; ++c) {
-            f32x4_t x = {0.f, 0.f, 0.f, 0.f};
+            f32x4_t x[NT];
+#pragma unroll
+            for (int u = 0; u < NT; ++u) x[u] = (f32x4_t){0.f, 0.f, 0.f, 0.f};
             if constexpr (T::F32) {
 #pragma unroll
                 for (int e = 0; e < K_LOADS; ++e) {
                     const f32x4_t k = __builtin_bit_cast(f32x4_t, kr[c][e]);
                     const bool there = 16 * e + 4 * g < hd;
 #pragma unroll
-                    for (int i = 0; i < 4; ++i) x = mfma_f32(there ? k[i] : 0.f, q.x[e][i], x);
-                }
-            } else if constexpr (T::CODES) {
+                    for (int i = 0; i < 4; ++i)
 #pragma unroll
-                for (int e = 0; e < HD / 32; ++e) {
-                    const uint32_t lo = kr[c][e / 2][e % 2 * 2], hi = kr[c][e / 2][e % 2 * 2 + 1];
-                    const f16x8_t k = as_f16x8(make_uint4(code_pair<PT, false>(lo), code_pair<PT, true>(lo), code_pair<PT, false>(hi), code_pair<PT, true>(hi)));
-#pragma unroll
-                    for (int n = 0; n < T::QN; ++n) x = mfma_16x16x32<true>(k, q.x[n][e], x);
+                        for (int u = 0; u < NT; ++u) x[u] = mfma_f32(there ? k[i] : 0.f, q[u].x[e][i], x[u]);
                 }
             } else {
 #pragma unroll
-                for (int e = 0; e < HD / 32; ++e) x = mfma_16x16x32<T::BF>(__builtin_bit_cast(f16x8_t, kr[c][e]), q.x[0][e], x);
+                for (int e = 0; e < HD / 32; ++e) {
+                    f16x8_t k;
+                    if constexpr (T::CODES) {
+                        const uint32_t lo = kr[c][e / 2][e % 2 * 2], hi = kr[c][e / 2][e % 2 * 2 + 1];
+                        k = as_f16x8(make_uint4(code_pair<PT, T::QBF, false>(lo), code_pair<PT, T::QBF, true>(lo), code_pair<PT, T::QBF, false>(hi),
+                                                code_pair<PT, T::QBF, true>(hi)));
+                    } else k = __builtin_bit_cast(f16x8_t, kr[c][e]);
+#pragma unroll
+                    for (int n = 0; n < T::QN; ++n)
+#pragma unroll
+                        for (int u = 0; u < NT; ++u) x[u] = mfma_16x16x32<T::QBF>(k, q[u].x[n][e], x[u]);
+                }
             }
 #pragma unroll
-            for (int r = 0; r < 4; ++r) s[c][r] = x[r] * (T::CODES ? ks[c][r] * sc : sc);
+            for (int r = 0; r < 4; ++r) {
+                const float scale = T::CODES ? ks[c][r] * sc : sc;
+#pragma unroll
+                for (int u = 0; u < NT; ++u) s[u][c][r] = x[u][r] * scale;
+            }
         }
-        // Keys of the lane that its column sees (bits 4 c + r), and that some column does.
-        uint32_t mine = ~0u, some = ~0u;
+        // Keys of the lane that its columns see (bits 4 c + r), and that some column does.
+        uint32_t mine[NT], some = ~0u;
+#pragma unroll
+        for (int u = 0; u < NT; ++u) mine[u] = ~0u;
         if (masked) {
-            mine = some = 0;
+            some = 0;
+#pragma unroll
+            for (int u = 0; u < NT; ++u) mine[u] = 0;
 #pragma unroll
             for (int c = 0; c < TILES; ++c) {
                 const bool here = __builtin_amdgcn_readlane(pages, block * TILES + c) >= 0;
 #pragma unroll
                 for (int r = 0; r < 4; ++r) {
                     const int j = k0 + 16 * c + 4 * g + r;
-                    mine |= (uint32_t)(here && j < limit) << (4 * c + r);
                     some |= (uint32_t)(here && j < len) << (4 * c + r);
-                    s[c][r] = mine >> (4 * c + r) & 1 ? s[c][r] : -INFINITY;
+#pragma unroll
+                    for (int u = 0; u < NT; ++u) {
+                        mine[u] |= (uint32_t)(here && j < limit[u]) << (4 * c + r);
+                        s[u][c][r] = mine[u] >> (4 * c + r) & 1 ? s[u][c][r] : -INFINITY;
+                    }
                 }
             }
         }
         __builtin_amdgcn_sched_barrier(0);
-        const int next = min(block + 1, blocks - 1);         // (behind the last block: it again)
-        load_keys(next);
+        if constexpr (!LAST) load_keys(block + 1);
         __builtin_amdgcn_sched_barrier(0);
-        float top = s[0][0];
+        float top[NT];
+        bool above = false;
 #pragma unroll
-        for (int i = 1; i < 4 * TILES; ++i) top = fmaxf(top, s[i / 4][i % 4]);
-        top = fmaxf(top, __shfl_xor(top, 16));
-        top = fmaxf(m, fmaxf(top, __shfl_xor(top, 32)));
-        if (__any(top > m)) {
-            const float alpha = __builtin_amdgcn_exp2f(m - top);
-            l *= alpha;
+        for (int u = 0; u < NT; ++u) {
+            float x = s[u][0][0];
 #pragma unroll
-            for (int i = 0; i < DT; ++i) o[i] *= alpha;
-            m = top;
+            for (int i = 1; i < 4 * TILES; ++i) x = fmaxf(x, s[u][i / 4][i % 4]);
+            x = fmaxf(x, __shfl_xor(x, 16));
+            top[u] = fmaxf(m[u], fmaxf(x, __shfl_xor(x, 32)));
+            above |= top[u] > m[u];
         }
-        const float base = T::BIAS - m;
+        if (__any(above)) {
 #pragma unroll
-        for (int c = 0; c < TILES; ++c)
+            for (int u = 0; u < NT; ++u) {
+                const float alpha = __builtin_amdgcn_exp2f(m[u] - top[u]);
+                l[u] *= alpha;
 #pragma unroll
-            for (int r = 0; r < 4; ++r) {
-                s[c][r] = __builtin_amdgcn_exp2f(s[c][r] + base);
-                l += s[c][r];
-                if (T::CODES) s[c][r] *= vs[c][r];
+                for (int i = 0; i < DT; ++i) o[u][i] *= alpha;
+                m[u] = top[u];
             }
+        }
+#pragma unroll
+        for (int u = 0; u < NT; ++u) {
+            const float base = T::BIAS - m[u];
+#pragma unroll
+            for (int c = 0; c < TILES; ++c)
+#pragma unroll
+                for (int r = 0; r < 4; ++r) {
+                    s[u][c][r] = __builtin_amdgcn_exp2f(s[u][c][r] + base);
+                    l[u] += s[u][c][r];
+                    if (T::CODES) s[u][c][r] *= vs[c][r];
+                }
+        }
         if (masked) {
             // Weights of rows that the column does not see are zeros, whatever their scales hold; rows that no column sees become zeros, whatever they hold.
             bool odd = false;
@@ -258,7 +430,9 @@ __global__ void __launch_bounds__(64 * WAVES, 2) paged_attn_kernel(PagedAttnArgs
             for (int c = 0; c < TILES; ++c)
 #pragma unroll
                 for (int r = 0; r < 4; ++r) {
-                    if (T::CODES) s[c][r] = mine >> (4 * c + r) & 1 ? s[c][r] : 0.f;
+                    if (T::CODES)
+#pragma unroll
+                        for (int u = 0; u < NT; ++u) s[u][c][r] = mine[u] >> (4 * c + r) & 1 ? s[u][c][r] : 0.f;
 #pragma unroll
                     for (int h = 0; h < V_PARTS; ++h) {
                         vr[c][r][h] = some >> (4 * c + r) & 1 ? vr[c][r][h] : (words_t)(0u);
@@ -272,14 +446,17 @@ __global__ void __launch_bounds__(64 * WAVES, 2) paged_attn_kernel(PagedAttnArgs
                 for (int c = 0; c < TILES; ++c)
 #pragma unroll
                     for (int r = 0; r < 4; ++r) {
-                        const float seen = mine >> (4 * c + r) & 1 ? 1.f : 0.f;
 #pragma unroll
                         for (int i = 0; i < DT; ++i) {
                             const uint32_t x = vr[c][r][T::F32 ? i / 4 : 0][T::F32 ? i % 4 : i * T::SIZE / 4];
                             const bool is = not_finite<PT>(x) >> (T::SIZE == 1 ? 8 * (i % 4) + 7 : T::SIZE == 2 ? 16 * (i % 2) + 15 : 31) & 1;
-                            const f32x4_t n = mfma_f32(is ? 1.f : 0.f, seen, (f32x4_t){0.f, 0.f, 0.f, 0.f});
 #pragma unroll
-                            for (int e = 0; e < 4; ++e) o[i][e] += n[e] > 0.f ? NAN : 0.f;
+                            for (int u = 0; u < NT; ++u) {
+                                const f32x4_t n = mfma_f32(is ? 1.f : 0.f, mine[u] >> (4 * c + r) & 1 ? 1.f : 0.f, (f32x4_t){0.f, 0.f, 0.f, 0.f});
+#pragma unroll
+                                for (int e = 0; e < 4; ++e) lost[u] |= (uint32_t)(n[e] > 0.f) << (4 * i + e);
+                                asm volatile("" : "+v"(lost[u]));        // (one after the other: registers, not speed)
+                            }
                         }
 #pragma unroll
                         for (int h = 0; h < V_PARTS; ++h)
@@ -292,116 +469,133 @@ __global__ void __launch_bounds__(64 * WAVES, 2) paged_attn_kernel(PagedAttnArgs
 #pragma unroll
             for (int r = 0; r < 4; ++r)
 #pragma unroll
-                for (int i = 0; i < DT; ++i) o[i] = mfma_f32(__uint_as_float(vr[0][r][i / 4][i % 4]), s[0][r], o[i]);
-        } else {
+                for (int i = 0; i < DT; ++i)
 #pragma unroll
-            for (int h = 0; h < TILES / 2; ++h) {            // 32 keys
-                f16x8_t w[T::PN];
+                    for (int u = 0; u < NT; ++u) o[u][i] = mfma_f32(__uint_as_float(vr[0][r][i / 4][i % 4]), s[u][0][r], o[u][i]);
+        } else {
+            static_assert(TILES == 2, "32 keys an operand");
+            f16x8_t w[NT][T::PN];
+#pragma unroll
+            for (int u = 0; u < NT; ++u)
 #pragma unroll
                 for (int n = 0; n < T::PN; ++n) {
                     uint32_t x[4];
 #pragma unroll
                     for (int e = 0; e < 4; ++e) {
-                        float& lo = s[2 * h + e / 2][e % 2 * 2];
-                        float& hi = s[2 * h + e / 2][e % 2 * 2 + 1];
+                        float& lo = s[u][e / 2][e % 2 * 2];
+                        float& hi = s[u][e / 2][e % 2 * 2 + 1];
                         x[e] = pack16<T::BF>(lo, hi);
                         const f16x2_t z = __builtin_bit_cast(f16x2_t, x[e]);
                         lo -= T::BF ? __uint_as_float(x[e] << 16) : (float)z.x;
                         hi -= T::BF ? __uint_as_float(x[e] & 0xffff0000u) : (float)z.y;
                     }
-                    w[n] = as_f16x8(make_uint4(x[0], x[1], x[2], x[3]));
+                    w[u][n] = as_f16x8(make_uint4(x[0], x[1], x[2], x[3]));
                 }
-                auto add = [&](int i, uint32_t x0, uint32_t x1, uint32_t x2, uint32_t x3) __attribute__((always_inline)) {
-                    const f16x8_t x = as_f16x8(make_uint4(x0, x1, x2, x3));
+            auto add = [&](int i, uint32_t x0, uint32_t x1, uint32_t x2, uint32_t x3) __attribute__((always_inline)) {
+                const f16x8_t x = as_f16x8(make_uint4(x0, x1, x2, x3));
 #pragma unroll
-                    for (int n = 0; n < T::PN; ++n) o[i] = mfma_16x16x32<T::BF>(x, w[n], o[i]);
-                };
-                const auto& v0 = vr[2 * h];
-                const auto& v1 = vr[2 * h + 1];
-                if constexpr (T::CODES) {
+                for (int n = 0; n < T::PN; ++n)
 #pragma unroll
-                    for (int i = 0; i < DT; i += 2) {        // bytes i, i + 1 of two rows side by side
-                        const uint32_t pick = i % 4 ? 0x07030602u : 0x05010400u;
-                        uint32_t t[4];
+                    for (int u = 0; u < NT; ++u) o[u][i] = mfma_16x16x32<T::BF>(x, w[u][n], o[u][i]);
+            };
+            const auto& v0 = vr[0];
+            const auto& v1 = vr[1];
+            if constexpr (T::CODES) {
 #pragma unroll
-                        for (int e = 0; e < 2; ++e) {
-                            t[e] = __builtin_amdgcn_perm(v0[2 * e + 1][0][i / 4], v0[2 * e][0][i / 4], pick);
-                            t[2 + e] = __builtin_amdgcn_perm(v1[2 * e + 1][0][i / 4], v1[2 * e][0][i / 4], pick);
-                        }
-                        add(i, code_pair<PT, false>(t[0]), code_pair<PT, false>(t[1]), code_pair<PT, false>(t[2]), code_pair<PT, false>(t[3]));
-                        add(i + 1, code_pair<PT, true>(t[0]), code_pair<PT, true>(t[1]), code_pair<PT, true>(t[2]), code_pair<PT, true>(t[3]));
+                for (int i = 0; i < DT; i += 2) {            // bytes i, i + 1 of two rows side by side
+                    const uint32_t pick = i % 4 ? 0x07030602u : 0x05010400u;
+                    uint32_t t[4];
+#pragma unroll
+                    for (int e = 0; e < 2; ++e) {
+                        t[e] = __builtin_amdgcn_perm(v0[2 * e + 1][0][i / 4], v0[2 * e][0][i / 4], pick);
+                        t[2 + e] = __builtin_amdgcn_perm(v1[2 * e + 1][0][i / 4], v1[2 * e][0][i / 4], pick);
                     }
-                } else {
+                    add(i, code_pair<PT, true, false>(t[0]), code_pair<PT, true, false>(t[1]), code_pair<PT, true, false>(t[2]), code_pair<PT, true, false>(t[3]));
+                    add(i + 1, code_pair<PT, true, true>(t[0]), code_pair<PT, true, true>(t[1]), code_pair<PT, true, true>(t[2]), code_pair<PT, true, true>(t[3]));
+                }
+            } else {
 #pragma unroll
-                    for (int i = 0; i < DT; ++i) {
-                        const uint32_t pick = i % 2 ? 0x07060302u : 0x05040100u;
-                        add(i, __builtin_amdgcn_perm(v0[1][0][i / 2], v0[0][0][i / 2], pick), __builtin_amdgcn_perm(v0[3][0][i / 2], v0[2][0][i / 2], pick),
-                            __builtin_amdgcn_perm(v1[1][0][i / 2], v1[0][0][i / 2], pick), __builtin_amdgcn_perm(v1[3][0][i / 2], v1[2][0][i / 2], pick));
-                    }
+                for (int i = 0; i < DT; ++i) {
+                    const uint32_t pick = i % 2 ? 0x07060302u : 0x05040100u;
+                    add(i, __builtin_amdgcn_perm(v0[1][0][i / 2], v0[0][0][i / 2], pick), __builtin_amdgcn_perm(v0[3][0][i / 2], v0[2][0][i / 2], pick),
+                        __builtin_amdgcn_perm(v1[1][0][i / 2], v1[0][0][i / 2], pick), __builtin_amdgcn_perm(v1[3][0][i / 2], v1[2][0][i / 2], pick));
                 }
             }
         }
         __builtin_amdgcn_sched_barrier(0);
-        load_values(next);
+        if constexpr (!LAST) load_values(block + 1);
         __builtin_amdgcn_sched_barrier(0);
-    }
+    };
+    for (int block = 0; block < blocks - 1; ++block) add_block(std::false_type(), block);
+    if (blocks > 0) add_block(std::true_type(), blocks - 1);
 
-    l += __shfl_xor(l, 16);
-    l += __shfl_xor(l, 32);
-    const float inv = l == 0.f ? 0.f : 1.f / l;
-    if (g == 0) ml_s[wave][dc] = make_float2(m, l);
 #pragma unroll
-    for (int i = 0; i < DT; i += 4)
+    for (int u = 0; u < NT; ++u) {
+        if (u) __syncthreads();
+        if (__any(lost[u] != 0)) {
 #pragma unroll
-        for (int r = 0; r < 4; ++r) {
-            const int dim = T::F32 ? 16 * i + 16 * g + 4 * r : DPL * (4 * g + r) + i;
-            *reinterpret_cast<f32x4_t*>(&o_s[wave][dc][dim]) = (f32x4_t){o[i][r] * inv, o[i + 1][r] * inv, o[i + 2][r] * inv, o[i + 3][r] * inv};
+            for (int i = 0; i < 4 * DT; ++i) o[u][i / 4][i % 4] = lost[u] >> i & 1 ? NAN : o[u][i / 4][i % 4];
         }
-    __syncthreads();
-    constexpr int PER = HD / 4;                              // threads of a row
-    for (int i = threadIdx.x; i < 16 * PER; i += 64 * WAVES) {
-        const int r = i / PER, dim = i % PER * 4, n = tile * 16 + r;
-        if (n >= rows || dim >= hd) continue;
-        float mt = -F32_MOST, lt = 0.f, w[WAVES];
+        l[u] += __shfl_xor(l[u], 16);
+        l[u] += __shfl_xor(l[u], 32);
+        const float inv = l[u] == 0.f ? 0.f : 1.f / l[u];
+        if (g == 0) ml_s[wave][dc] = make_float2(m[u], l[u]);
 #pragma unroll
-        for (int u = 0; u < WAVES; ++u) mt = fmaxf(mt, ml_s[u][r].x);
+        for (int i = 0; i < DT; i += 4)
 #pragma unroll
-        for (int u = 0; u < WAVES; ++u) {
-            const float2 x = ml_s[u][r];
-            w[u] = x.y == 0.f ? 0.f : x.y * __builtin_amdgcn_exp2f(x.x - mt);
-            lt += w[u];
-        }
-        const float share = lt == 0.f ? 0.f : 1.f / lt;
-        f32x4_t v = {0.f, 0.f, 0.f, 0.f};
+            for (int r = 0; r < 4; ++r) {
+                const int dim = T::F32 ? 16 * i + 16 * g + 4 * r : DPL * (4 * g + r) + i;
+                *reinterpret_cast<f32x4_t*>(&o_s[wave][dc][dim]) = (f32x4_t){o[u][i][r] * inv, o[u][i + 1][r] * inv, o[u][i + 2][r] * inv, o[u][i + 3][r] * inv};
+            }
+        __syncthreads();
+        constexpr int PER = HD / 4;                              // threads of a row
+        for (int i = threadIdx.x; i < 16 * PER; i += 64 * WAVES) {
+            const int r = i / PER, dim = i % PER * 4, n = row0 + 16 * u + r;
+            if (n >= rows || dim >= hd) continue;
+            float mt = -F32_MOST, lt = 0.f, share[WAVES];
 #pragma unroll
-        for (int u = 0; u < WAVES; ++u) v += *reinterpret_cast<const f32x4_t*>(&o_s[u][r][dim]) * (w[u] * share);
-        const int64_t at = ((int64_t)b * a.n_new + n / a.group) * a.n_q_heads + kvh * a.group + n % a.group;
-        if (only) {
-            typename E::type* out = (typename E::type*)a.out + at * hd + dim;
+            for (int w = 0; w < WAVES; ++w) mt = fmaxf(mt, ml_s[w][r].x);
 #pragma unroll
-            for (int e = 0; e < 4; ++e) out[e] = E::put(v[e]);
-            if (a.lse && dim == 0) a.lse[at] = lt == 0.f ? -INFINITY : (mt - T::BIAS + __builtin_amdgcn_logf(lt)) * LN2;
-        } else {
-            *reinterpret_cast<f32x4_t*>(a.part_o + (at * a.n_pieces + part) * HD + dim) = v;
-            if (dim == 0) a.part_ml[at * a.n_pieces + part] = make_float2(mt - T::BIAS, lt);
+            for (int w = 0; w < WAVES; ++w) {
+                const float2 x = ml_s[w][r];
+                share[w] = x.y == 0.f ? 0.f : x.y * __builtin_amdgcn_exp2f(x.x - mt);
+                lt += share[w];
+            }
+            const float one = lt == 0.f ? 0.f : 1.f / lt;
+            f32x4_t v = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+            for (int w = 0; w < WAVES; ++w) v += *reinterpret_cast<const f32x4_t*>(&o_s[w][r][dim]) * (share[w] * one);
+            const int64_t at = ((int64_t)b * a.n_new + n / a.group) * a.n_q_heads + kvh * a.group + n % a.group;
+            if (only) {
+                typename E::type* out = (typename E::type*)a.out + at * hd + dim;
+#pragma unroll
+                for (int e = 0; e < 4; ++e) out[e] = E::put(v[e]);
+                if (a.lse && dim == 0) a.lse[at] = lt == 0.f ? -INFINITY : (mt - T::BIAS + __builtin_amdgcn_logf(lt)) * LN2;
+            } else {
+                const int64_t to_at = ((int64_t)t.index * p.n_kv_heads + kvh) * rows + n;
+                *reinterpret_cast<f32x4_t*>(a.part_o + to_at * HD + dim) = v;
+                if (dim == 0) a.part_ml[to_at] = make_float2(mt - T::BIAS, lt);
+            }
         }
     }
+    if (a.n_pieces > 1 && t.part == 0 && kvh == 0 && tile == 0 && threadIdx.x == 0) a.first[b] = make_int2(t.index, t.n);
     if (bad) raise_flag(p.flags, SSD_FLAG_BAD_PAGE);
 }
 
 // The pieces of a context, a mean of values each, joined: a workgroup has a query row, groups of HD / 4 lanes take its pieces in turn and are joined through LDS.
-template <int QT, int HD>
-__global__ void __launch_bounds__(256) paged_join_kernel(PagedAttnArgs a) {
+template <int QT, int HD, int THREADS>
+__global__ void __launch_bounds__(THREADS) paged_join_kernel(PagedAttnArgs a) {
     typedef Elem<QT> E;
-    constexpr int LANES = HD / 4, GROUPS = 256 / LANES, U = 4;
+    constexpr int LANES = HD / 4, GROUPS = THREADS / LANES, U = 4;
     __shared__ f32x4_t o_s[GROUPS][LANES];
     __shared__ float2 ml_s[GROUPS];
     const int64_t at = blockIdx.x;
-    const int b = (int)(at / ((int64_t)a.n_new * a.n_q_heads)), len = min(max(a.p.ctx_len[b], 0), a.p.max_ctx), pieces = (len + a.piece - 1) / a.piece;
+    const int token = (int)(at / a.n_q_heads), head = (int)(at % a.n_q_heads), b = token / a.n_new;
+    const int first = a.first[b].x, pieces = a.first[b].y;
     if (pieces <= 1) return;
     const int group = threadIdx.x / LANES, dim = threadIdx.x % LANES * 4;
-    const float2* ml = a.part_ml + at * a.n_pieces;
-    const float* po = a.part_o + at * a.n_pieces * HD + dim;
+    const int64_t rows = a.n_new * a.group, step = rows * a.p.n_kv_heads;
+    const int64_t row0 = first * step + head / a.group * rows + token % a.n_new * a.group + head % a.group;
     float m = -F32_MOST, l = 0.f;
     f32x4_t v = {0.f, 0.f, 0.f, 0.f};
     for (int p0 = group; p0 < pieces; p0 += U * GROUPS) {
@@ -409,9 +603,9 @@ __global__ void __launch_bounds__(256) paged_join_kernel(PagedAttnArgs a) {
         f32x4_t z[U];
 #pragma unroll
         for (int u = 0; u < U; ++u) {
-            const int64_t i = min(p0 + u * GROUPS, pieces - 1);
-            y[u] = ml[i];
-            z[u] = *reinterpret_cast<const f32x4_t*>(po + i * HD);
+            const int64_t i = row0 + min(p0 + u * GROUPS, pieces - 1) * step;
+            y[u] = a.part_ml[i];
+            z[u] = *reinterpret_cast<const f32x4_t*>(a.part_o + i * HD + dim);
         }
 #pragma unroll
         for (int u = 0; u < U; ++u) {
@@ -448,8 +642,16 @@ __global__ void __launch_bounds__(256) paged_join_kernel(PagedAttnArgs a) {
 
 template <int QT, int PT, int HD>
 void launch_rows(const PagedAttnArgs& a, hipStream_t st) {
-    paged_attn_kernel<QT, PT, HD><<<dim3(a.n_pieces, a.p.n_kv_heads, a.p.B * a.tiles), 64 * WAVES, 0, st>>>(a);
-    if (a.n_pieces > 1) paged_join_kernel<QT, HD><<<(unsigned)((int64_t)a.p.B * a.n_new * a.n_q_heads), 256, 0, st>>>(a);
+    const dim3 grid(a.n_pieces, a.p.n_kv_heads, a.shared ? a.tiles : a.p.B * a.tiles);
+    constexpr int used = WAVES * 16 * ((HD + 4) * 4 + 8);
+    const int more = a.shared ? PAGED_CU_LDS / (paged_per_cu(a.p.head_dim, a.tile_rows) + 1) + 1024 - used : 0;
+    if (a.tile_rows == 16) paged_attn_kernel<QT, PT, HD, 1><<<grid, 64 * WAVES, more, st>>>(a);
+    else paged_attn_kernel<QT, PT, HD, 2><<<grid, 64 * WAVES, more, st>>>(a);
+    const unsigned n = (unsigned)((int64_t)a.p.B * a.n_new * a.n_q_heads);
+    const int each = a.shared ? a.n_pieces / a.p.B : a.n_pieces;             // pieces of an utterance, about
+    if (each > 64) paged_join_kernel<QT, HD, 1024><<<n, 1024, 0, st>>>(a);
+    else if (each > 8) paged_join_kernel<QT, HD, 256><<<n, 256, 0, st>>>(a);
+    else if (a.n_pieces > 1) paged_join_kernel<QT, HD, 64><<<n, 64, 0, st>>>(a);
 }
 template <int QT, int PT>
 void launch_dims(const PagedAttnArgs& a, hipStream_t st) {

@@ -42,18 +42,27 @@ struct PagedAttnArgs {
     void* out; float* lse;
     int32_t n_q_heads, group, n_new;         // group: query heads of a K/V head
     float scale;
-    int32_t tiles;                           // of 16 query rows, tokens times group
-    int32_t piece, n_pieces;                 // rows of a piece of a context, pieces of max_ctx rows
-    float* part_o; float2* part_ml;          // [token][query head][piece] mean of values (64 or 128 dims), (maximum to base 2, sum); not used by contexts of one piece
+    int32_t tile_rows, tiles;                // query rows of a K/V head, tokens times group, in tiles of 16 or 32
+    // Contexts are cut into pieces of whole PAGED_UNITs of rows: shared 0, each by itself every PAGED_MOST units, n_pieces of max_ctx rows; else all of a K/V head
+    // and tile into about `shared` equal ones (or the smallest multiple of it that has none longer than PAGED_MOST), at most n_pieces.
+    int32_t shared, n_pieces;
+    float* part_o; float2* part_ml;          // [piece (of an utterance with shared 0: utterance, piece)][query row of tile and K/V head]: mean of 64 or 128 values; (maximum to base 2, sum)
+    int2* first;                             // [utterance] first piece, pieces
 };
-constexpr int PAGED_LEAST_PIECE = 256, PAGED_MOST_PIECE = 4096;      // (a wavefront has the pages of at most 4096 rows of its workgroup)
+constexpr int PAGED_UNIT = 128, PAGED_MOST = 32;             // a round of four wavefronts of 32 rows; units of a piece, of which a wavefront has the page numbers in a register
+constexpr int PAGED_UTTS = 1024;                             // utterances of a batch that shares
 inline int paged_dims(int head_dim) { return head_dim > 64 ? 128 : 64; }
-// Rows of a piece.
-inline int paged_piece(int64_t pairs, int64_t max_ctx) {
-    const int64_t share = pairs * max_ctx / 1024;
-    const int64_t rows = (share + 255) / 256 * 256;
-    return (int)(rows < PAGED_LEAST_PIECE ? PAGED_LEAST_PIECE : rows > 1024 ? 1024 : rows);
-}
+inline int paged_tile_rows(int64_t rows) { return rows <= 16 ? 16 : 32; }
+// Workgroups of a CU whose registers fit; shared pieces are as many as run at once, and are held to so many a CU by the LDS they ask for.
+inline int paged_per_cu(int head_dim, int tile_rows) { return paged_dims(head_dim) == 128 ? 2 : tile_rows == 16 ? 4 : 3; }
+constexpr int PAGED_CUS = 256, PAGED_CU_LDS = 160 * 1024;
+// Pieces of a batch are at least so many times its utterances: their last pieces are shorter ones, which counts where there are few (40 utterances of 2000 to 4000 rows, half,
+// 8 heads: 108 us with 1, 97 with 2, 3 or 6; 90 of 1500 to 3000, e4m3: 98, 98, 101, 117).
+constexpr int PAGED_EACH = 2;
+// Units of the longest contexts that are not cut, by the workgroups there are without: the second launch and finding the piece cost 3 us.  In a graph, 8 heads, 64-row pages,
+// half, cut and not: 1 utterance of 600 rows 8.7 and 9.4 us, 1000 8.8 and 13.0; 16 of 300 to 600 13.9 and 10.9, 500 to 1000 15.8 and 14.9, 750 to 1500 18.9 and 19.0;
+// 40 of 1300 47.9 and 48.2 (e4m3 32.0 and 26.9), 2000 67.6 and 70.3 (43.2 and 38.7); 90 of 2000 136 and 125 (82 and 73); 200 of 375 to 1500 147 and 145 (106 and 82).
+inline int paged_whole(int64_t workgroups) { return workgroups >= 1024 ? PAGED_MOST : workgroups >= 256 ? 16 : workgroups >= 128 ? 8 : 5; }
 void launch_paged_attention(const PagedAttnArgs& a, int q_dtype, int pages_dtype, hipStream_t st);
 
 }  // namespace ssd

@@ -280,7 +280,7 @@ class Context:
         torch.cuda.set_device(self.device)
         self._index = torch.cuda.current_device()
         st = stream if stream is not None else torch.cuda.current_stream(self.device)
-        self.stream = st
+        self.stream, self._raw_stream = st, st.cuda_stream
         cfg_p, w_p = None, None
         if model_cfg is not None:
             m = model_cfg
@@ -778,7 +778,7 @@ class Context:
 
     def _like(self, t) -> torch.Tensor:
         """A contiguous tensor like t that the context's stream writes first: of that stream, so that memory in use on the current one is not given out again."""
-        if torch._C._cuda_getCurrentRawStream(self._index) == self.stream.cuda_stream:
+        if torch._C._cuda_getCurrentRawStream(self._index) == self._raw_stream:
             return torch.empty_like(t, memory_format=torch.contiguous_format)
         with torch.cuda.stream(self.stream):
             return torch.empty_like(t, memory_format=torch.contiguous_format)

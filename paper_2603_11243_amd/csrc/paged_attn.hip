@@ -109,6 +109,13 @@ template <int HD> struct Queries<SSD_F32, SSD_F32, HD> {
 
 __device__ __forceinline__ f32x4_t mfma_f32(float a, float b, const f32x4_t& c) { return __builtin_amdgcn_mfma_f32_16x16x4f32(a, b, c, 0, 0, 0); }
 
+// Four values of a result, one store.
+template <int QT>
+__device__ __forceinline__ void store4(typename Elem<QT>::type* out, const f32x4_t& v) {
+    if constexpr (QT == SSD_F32) *reinterpret_cast<f32x4_t*>(out) = v;
+    else *reinterpret_cast<uint2*>(out) = make_uint2(pack16<QT == SSD_BF16>(v[0], v[1]), pack16<QT == SSD_BF16>(v[2], v[3]));
+}
+
 // What a workgroup does: piece `part` of n of utterance b, rows from ..; index: the piece's number among all.
 struct Piece { int b, part, n, index, len, given, from, rows; };
 
@@ -567,9 +574,7 @@ __global__ void __launch_bounds__(64 * WAVES, 2) paged_attn_kernel(PagedAttnArgs
             for (int w = 0; w < WAVES; ++w) v += *reinterpret_cast<const f32x4_t*>(&o_s[w][r][dim]) * (share[w] * one);
             const int64_t at = ((int64_t)b * a.n_new + n / a.group) * a.n_q_heads + kvh * a.group + n % a.group;
             if (only) {
-                typename E::type* out = (typename E::type*)a.out + at * hd + dim;
-#pragma unroll
-                for (int e = 0; e < 4; ++e) out[e] = E::put(v[e]);
+                store4<QT>((typename E::type*)a.out + at * hd + dim, v);
                 if (a.lse && dim == 0) a.lse[at] = lt == 0.f ? -INFINITY : (mt - T::BIAS + __builtin_amdgcn_logf(lt)) * LN2;
             } else {
                 const int64_t to_at = ((int64_t)t.index * p.n_kv_heads + kvh) * rows + n;
@@ -634,9 +639,7 @@ __global__ void __launch_bounds__(THREADS) paged_join_kernel(PagedAttnArgs a) {
     f32x4_t s = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
     for (int i = 0; i < GROUPS; ++i) s += o_s[i][dim / 4] * (f[i] * inv);
-    typename E::type* out = (typename E::type*)a.out + at * a.p.head_dim + dim;
-#pragma unroll
-    for (int e = 0; e < 4; ++e) out[e] = E::put(s[e]);
+    store4<QT>((typename E::type*)a.out + at * a.p.head_dim + dim, s);
     if (a.lse && dim == 0) a.lse[at] = lt == 0.f ? -INFINITY : (mt + __builtin_amdgcn_logf(lt)) * LN2;
 }
 

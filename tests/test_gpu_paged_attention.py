@@ -231,6 +231,67 @@ def test_repeats_to_the_bit_and_batches_do_not_mix():
     assert torch.equal(a, swapped.flip(0))
 
 
+@pytest.mark.parametrize("pair", [("f16", "f16"), ("bf16", "e4m3"), ("f32", "f32")])
+@pytest.mark.parametrize("lens, most", [([3000, 5], 100000), ([700] * 9, 30000), ([0] * 63 + [2500], 2600), ([1], 1 << 20)])
+def test_tables_far_longer_than_the_contexts(pair, lens, most):
+    """What a captured step is made for: the pieces go by the lengths, not by what the table could hold."""
+    _check(pair, (4, 2, 64), lens, 64, 2, most=most)
+
+
+@pytest.mark.parametrize("B, long", [(65, 900), (70, 3000), (300, 2500), (1024, 4200), (1030, 4200), (1030, 9000)])
+def test_large_batches_with_one_long_context(B, long):
+    lens = [b % 7 for b in range(B)]
+    lens[B // 2] = long
+    lens[B - 1] = long - 300
+    _check(("f16", "e4m3"), (2, 1, 64), lens, 16)
+
+
+@pytest.mark.parametrize("hd", [64, 128])
+@pytest.mark.parametrize("B", [2, 7, 33])
+def test_ragged_long_contexts(hd, B):
+    """Every piece in its place: contexts from nothing to many pieces."""
+    r = np.random.default_rng(B)
+    lens = [int(n) for n in np.exp(r.uniform(0, np.log(6000), B))]
+    lens[0], lens[-1] = 0, 6000
+    _check(("bf16", "i8"), (6, 2, hd), lens, 128, 3)
+
+
+@pytest.mark.parametrize("kind", ["f16", "e4m3", "i8"])
+def test_a_captured_decoding_loop(kind):
+    """Append and attend, captured once and replayed while contexts grow over pages and are replaced: the eager results, with eager work of the program between replays."""
+    heads, B, R = (4, 2, 64), 3, 16
+    side = torch.cuda.Stream()
+    c, eager = Context(device="cuda:0", stream=side), Context(device="cuda:0", stream=side)
+    for x in (c, eager):
+        x.reserve(paged_utts=B, paged_new=1, paged_ctx=1600, paged_heads=heads)
+    pool = Pool(kind, heads[1:], [14, 700, 1590], R, most=1600)
+    with torch.cuda.stream(side):
+        free = [p for p in range(pool.n_pages) if p not in set(pool.table_host[pool.table_host >= 0].tolist())]
+        table, n = pool.table.clone().clamp_(min=-1), pool.ctx_len.clone()
+        table[0, 1], table[1, 44] = free                     # the pages that contexts of 14 and 700 rows grow into
+        q, k, v = (torch.randn(B, h, 64, device="cuda").half() for h in (4, 2, 2))
+        out, want = torch.empty_like(q), torch.empty_like(q)
+        pages, other = pool.pages(), KvPages(*(None if t is None else t.clone() for t in (pool.parts["k"], pool.parts["v"], pool.parts.get("k_scale"), pool.parts.get("v_scale"))))
+        graph = torch.cuda.CUDAGraph()
+        side.synchronize()
+        with torch.cuda.graph(graph, stream=side):
+            c.kv_write_pages(pages, table, n, k, v, max_ctx=1600)
+            c.paged_attention(q, pages.layer(0), table, n, max_ctx=1600, out=out)
+        for step in range(12):
+            for t in (q, k, v):
+                t.copy_(torch.randn(t.shape))
+            graph.replay()
+            eager.kv_write_pages(other, table, n, k, v, max_ctx=1600)
+            eager.paged_attention(q, other.layer(0), table, n, max_ctx=1600, out=want)
+            side.synchronize()
+            assert torch.equal(out, want) and torch.isfinite(out).all(), step
+            assert torch.equal(pages.k.view(torch.uint8), other.k.view(torch.uint8))
+            n.add_(torch.tensor([1, 1, 0 if step > 8 else 1], dtype=torch.int32, device="cuda"))
+    assert c.device_flags() == 0
+    for x in (c, eager):
+        x.close()
+
+
 def test_other_streams():
     """The context's stream does the work, whichever is current; results are in order there."""
     heads = (4, 2, 64)

@@ -116,6 +116,27 @@ def test_workspace_sizes(lib, ctx):  # noqa: F811
         last = size(16, 8, 128, 1, 1, n)
 
 
+def test_workspace_covers_every_call(lib, ctx):  # noqa: F811
+    """What a call without a workspace says it needs is at most what ssd_paged_workspace_bytes says, and what that says for more of anything."""
+    import random
+    import re
+    r = random.Random(1)
+    some = lambda top: max(1, int(top ** r.random()))
+    for _ in range(4000):
+        B, new, H, G, n, hd = some(65535), some(300), some(64), some(64), some(1 << 30), r.choice([64, 128])
+        if (new * G + 15) // 16 * B > 65535:
+            continue
+        rc = attention(lib, ctx, q=1 << 50, out=1 << 60, q_stride=G * H * hd, hq=G * H, n_new=new, p=pages(H=H, hd=hd, R=16), t=table(B=B, max_ctx=n, stride=1 << 27))
+        need = 0
+        if rc == EWORKSPACE:
+            need = int(re.search(rb"workspace of (\d+) bytes", lib.ssd_last_error(ctx)).group(1))
+            size = lambda *a: lib.ssd_paged_workspace_bytes(ctx, *a)
+            assert need <= size(G * H, H, hd, B, new, n) <= size(G * H, H, hd, B + some(100), new, n)
+            assert need <= size(G * H, H, 128, B, new + some(10), n + some(10000)) and need <= size(2 * G * H, H, hd, B, new, n)
+        else:
+            assert n <= 4096 or rc != 0
+
+
 def test_python_refusals():
     """What the binding sees before the library does."""
     import torch

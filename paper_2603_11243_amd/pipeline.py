@@ -9,11 +9,12 @@ in host memory between the two.  `TwoPhaseDecoder.run` is that schedule:
             per bin: ssd_select_unconfident -> verify_forward[_kv] -> accept_prefix
   between   mode "offload" (the paper's): the acoustic embeddings g of the rejected utterances are copied to pinned
             host memory and nothing else of phase 1 is kept; mode "resident": the K/V cache of phase 1 stays in HBM
-            (what 288 GB make possible: a 50K-token batch of the 1B-class decoder is 4.9 GB of keys and values)
+            (what 288 GB make possible: a 50K-token batch of the 1B-class decoder is 4.9 GB of keys and values); mode
+            "paged": the cache holds one bin, and behind each bin the rows of its rejected utterances go to pages, in 8 bits or as they are
   phase 2   fallback bins planned on context length + steps of the rejected utterances; per bin, "offload" reloads g,
             re-runs the prompt [g; prompt; accepted prefix + the rejected token] with verify_forward_kv (whose greedy
             token at the rejected position is the first fallback token) and then ar_fallback; "resident" calls
-            ar_fallback on the cached rows directly.
+            ar_fallback on the cached rows directly; "paged" reads them back from their pages first.
 
 Everything numeric happens inside the library; this module only decides what goes into which call.  Copies between
 device and pinned host memory are plain memcpys issued through torch on the context's stream.
@@ -26,7 +27,7 @@ from typing import List, Optional
 import numpy as np
 import torch
 
-from .binding import Context, plan_batches
+from .binding import Context, KvPages, plan_batches
 
 
 class TreeFallback:
@@ -136,9 +137,13 @@ class TreeFallback:
 class TwoPhaseDecoder:
     def __init__(self, ctx: Context, wl, logits: torch.Tensor, cu_frames, ctc_to_llm: torch.Tensor,
                  speech_all: torch.Tensor, cu_speech_all, prompt_all: torch.Tensor, cu_prompt_all,
-                 budget: int = 50000, mode: str = "resident", n_steps: int = 8, trees: Optional[dict] = None):
-        """trees: arguments of a TreeFallback (tau, depth, most_rows, ...) that continues the rejected utterances in place of ar_fallback."""
-        assert mode in ("offload", "resident")
+                 budget: int = 50000, mode: str = "resident", n_steps: int = 8, trees: Optional[dict] = None, pages_dtype: torch.dtype = torch.int8,
+                 page_rows: int = 64):
+        """trees: arguments of a TreeFallback (tau, depth, most_rows, ...) that continues the rejected utterances in place of ar_fallback.  pages_dtype, page_rows: of mode
+        "paged" (int8, float8_e4m3fn, or the type of the cache, which keeps the rows as they are)."""
+        assert mode in ("offload", "resident", "paged")
+        self.pages: Optional[KvPages] = None
+        self.pages_dtype, self.page_rows = pages_dtype, page_rows
         self.trees = None if trees is None else TreeFallback(ctx, len(cu_frames) - 1, **trees)
         self.room = n_steps + 2 + (0 if trees is None else self.trees.room)        # slots an utterance needs behind its rows
         self.ctx, self.wl, self.mode, self.budget, self.n_steps = ctx, wl, mode, int(budget), int(n_steps)
@@ -164,7 +169,7 @@ class TwoPhaseDecoder:
         self.logp_all = torch.empty(n_frames, dtype=torch.float32, device=dev)
         self.greedy_all = torch.empty(n_frames, dtype=torch.int32, device=dev)
         self.gate_out = None
-        # K/V slots: every verified utterance keeps its rows (resident), or one fallback bin at a time (offload)
+        # K/V slots: every verified utterance keeps its rows (resident), or one bin at a time (offload, paged)
         slots = (nS + nP + n_frames + self.B * self.room) if mode == "resident" else cap + self.B * self.room
         ctx.set_kv_cache(int(slots))
         self.kv_slots = int(slots)
@@ -175,6 +180,32 @@ class TwoPhaseDecoder:
 
     def _bins(self, lengths):
         return plan_batches(lengths, self.budget, padded=False) if len(lengths) else []
+
+    def _page_lists(self, utts, rows):
+        """Pages for so many rows of the utterances, one behind the other; [B, entries], -1 behind an utterance's last page."""
+        need = -(-np.asarray(rows) // self.page_rows)
+        if self.pages is None or self.pages.n_pages < need.sum():
+            m = self.ctx.cfg
+            self.pages = None                                # (the old ones go first)
+            self.pages = KvPages.empty(int(need.sum()), self.page_rows, m.n_kv_heads, m.head_dim, self.pages_dtype, m.n_layers, self.ctx.device)
+        lists = np.full((self.B, int(need.max())), -1, dtype=np.int32)
+        for b, n, at in zip(utts, need, np.cumsum(need) - need):
+            lists[b, :n] = np.arange(at, at + n)
+        return lists
+
+    def _to_pages(self, lists, utts, start, most, acc):
+        """The rows of a bin's rejected utterances, up to the end of their accepted prefixes, to their pages; lengths stay on the device."""
+        dev = self.ctx.device
+        k, v = self.ctx.kv_tensors()
+        length = torch.from_numpy((self.S + self.P)[utts].astype(np.int32)).to(dev) + acc["accept_len"]
+        moved = torch.where(acc["all_accepted"].bool(), 0, length).to(torch.int32)
+        self.ctx.kv_write_pages(self.pages, torch.from_numpy(lists[utts]).to(dev), length, k, v, start=torch.from_numpy(start).to(dev), n_rows=moved, max_rows=most, max_ctx=most)
+
+    def _from_pages(self, lists, utts, start, length):
+        k, v = self.ctx.kv_tensors()
+        n = torch.from_numpy(length).to(self.ctx.device)
+        self.ctx.kv_read_pages(self.pages, torch.from_numpy(lists[utts]).to(self.ctx.device), n, k, v, start=torch.from_numpy(start).to(self.ctx.device), n_rows=n,
+                               max_rows=int(length.max()), max_ctx=int(length.max()))
 
     def run(self, tau_slm: float) -> dict:
         with torch.cuda.stream(self.ctx.stream):             # what is copied to the host waits for the calls before it, whichever stream is current
@@ -196,6 +227,7 @@ class TwoPhaseDecoder:
         n_rows = (self.S + self.P + draft_len)[fail]
         bins = [fail[b] for b in self._bins(n_rows)]
         res["verify_bins"] = len(bins)
+        lists = self._page_lists(fail, n_rows) if self.mode == "paged" else None
         kv_next = 0
         kv_start = np.zeros(self.B, np.int32)
         pending = []
@@ -206,8 +238,10 @@ class TwoPhaseDecoder:
                                          self.cu_s, self.prompt_all, self.cu_p, out=self.sel_buf)
             Mv = int(sel["cu_draft"][-1])
             ks = None
-            if self.mode == "resident":
+            if self.mode != "offload":
                 cap = (self.S + self.P + draft_len)[utts] + self.room
+                if self.mode == "paged":
+                    kv_next = 0
                 ks = (kv_next + np.concatenate([[0], np.cumsum(cap)[:-1]])).astype(np.int32)
                 kv_start[utts] = ks
                 kv_next += int(cap.sum())
@@ -217,6 +251,8 @@ class TwoPhaseDecoder:
                                     out={"draft_logp": self.logp_all[off:off + Mv], "greedy_tok": self.greedy_all[off:off + Mv],
                                          "accept_len": torch.empty(len(utts), dtype=torch.int32, device=ctx.device),
                                          "all_accepted": torch.empty(len(utts), dtype=torch.uint8, device=ctx.device)})
+            if self.mode == "paged":
+                self._to_pages(lists, utts, ks, int((self.S + self.P + draft_len)[utts].max()), acc)
             goff[utts] = off + sel["cu_draft"][:-1]
             off += Mv
             pending.append((utts, acc))
@@ -242,10 +278,14 @@ class TwoPhaseDecoder:
         res["fallback_bins"] = len(fb_bins)
         outs = []
         for utts in fb_bins:
-            if self.mode == "resident":
+            if self.mode != "offload":
                 # the first fallback token is the model's own choice at the first rejected position
                 first = ctx.gather_i32(self.greedy_all, goff[utts] + A[utts])
                 ks, cl = kv_start[utts], ctx_len_all[utts]
+                if self.mode == "paged":
+                    cap = cl + self.room
+                    ks = np.concatenate([[0], np.cumsum(cap)[:-1]]).astype(np.int32)
+                    self._from_pages(lists, utts, ks, cl)
             else:
                 # reload g, then re-run [g; prompt; accepted prefix + the rejected token] with the K/V cache on
                 S_u = self.S[utts]

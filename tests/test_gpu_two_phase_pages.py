@@ -1,0 +1,40 @@
+"""The two-phase schedule with the rows of rejected utterances in pages between the phases."""
+import numpy as np
+import pytest
+import torch
+
+from tests.test_gpu_verify import _tau_for
+from workloads import WORKLOADS, make_ctc_batch, make_ctc_to_llm_map, make_model_weights, make_verify_inputs
+from workloads.configs import scaled_down
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.mark.parametrize("name, layers", [("cfg3_1b_ragged64", 2), ("cfg1_tiny_f32", 2)])
+def test_rows_in_pages_between_the_phases(name, layers):
+    """Pages of the cache's type: the tokens of the resident cache to the last one.  8 bits: the same decisions and first tokens (they are of the first phase), and a
+    full continuation of every rejected utterance."""
+    from paper_2603_11243_amd.binding import Context
+    from paper_2603_11243_amd.pipeline import TwoPhaseDecoder
+    wl = scaled_down(WORKLOADS[name], n_layers=layers, B=24 if layers and name.startswith("cfg3") else 4)
+    cb, table = make_ctc_batch(wl), make_ctc_to_llm_map(wl)
+    vi = make_verify_inputs(wl, cb.seconds, [np.zeros(0, np.int32)] * wl.B, device="cuda")
+    ctx = Context(wl.model, make_model_weights(wl.model, wl.seed, device="cuda"))
+    args = (ctx, wl, cb.logits.cuda(), cb.cu_frames, torch.from_numpy(table).cuda(), vi.speech_emb, vi.cu_speech, torch.from_numpy(vi.prompt_ids).cuda(), vi.cu_prompt)
+    budget = 1500 if name.startswith("cfg3") else 200
+    try:
+        ctx.device_flags()
+        resident = TwoPhaseDecoder(*args, budget=budget, n_steps=5).run(_tau_for(wl))
+        assert resident["rejected"] > 0 and resident["verify_bins"] > 1
+        for dtype in (ctx.act_dtype, torch.int8, torch.float8_e4m3fn):
+            dec = TwoPhaseDecoder(*args, budget=budget, mode="paged", n_steps=5, pages_dtype=dtype, page_rows=16)
+            for _ in range(2):                               # a second run on the same pages
+                run = dec.run(_tau_for(wl))
+                assert np.array_equal(run["accept_len"], resident["accept_len"]) and set(run["tokens"]) == set(resident["tokens"])
+                for b, t in run["tokens"].items():
+                    if dtype is ctx.act_dtype:
+                        assert np.array_equal(t, resident["tokens"][b]), b
+                    assert len(t) == 6 and t[0] == resident["tokens"][b][0] and (t >= 0).all() and (t < wl.model.vocab).all()
+        assert ctx.device_flags() == 0
+    finally:
+        ctx.close()

@@ -502,7 +502,8 @@ int kv_write_pages(ssd_ctx *ctx, const ssd_kv_view *slots /*host*/, const int32_
 int kv_read_pages(ssd_ctx *ctx, const ssd_kv_pages *pages /*host*/, const ssd_page_table *table /*host*/, const ssd_kv_view *slots /*host*/,
                   const int32_t *start, const int32_t *n_rows, int max_rows);
 
-/* Bytes of workspace for paged_attention calls of at most B utterances with n_new tokens each and contexts of max_ctx rows.  A size serves all smaller calls. */
+/* Bytes of workspace for paged_attention calls of at most B utterances with n_new tokens each and contexts of max_ctx rows.  A size serves all smaller calls.  0: no
+ * call is so large. */
 size_t ssd_paged_workspace_bytes(const ssd_ctx *ctx, int n_q_heads, int n_kv_heads, int head_dim, int64_t B, int n_new, int64_t max_ctx);
 
 /* Attention of the newest n_new tokens of every utterance (their own rows written before).  Token t sees rows j < ctx_len[b] - (n_new - 1 - t); per query head h, whose
@@ -516,7 +517,8 @@ size_t ssd_paged_workspace_bytes(const ssd_ctx *ctx, int n_q_heads, int n_kv_hea
  * others; three values, 24 bits, with 8-bit pages and SSD_F32 queries), with SSD_F32 pages as it is.  Outputs below 2^-90 lose bits.  A row that a token does not see, and what
  * lies behind the last row of a page, has no influence on it, whatever it holds; a value that it sees and that is not finite makes its column infinite or NaN.
  * Captured calls use the workspace of the time of capture: two that share one must not run at the same time.  Every call repeats to the bit.
- * Errors: SSD_EINVAL, SSD_ESHAPE (B times tiles of 16 query rows of a K/V head more than 65535; more than 512 query heads a K/V head), SSD_EUNSUPPORTED, SSD_EWORKSPACE. */
+ * Errors: SSD_EINVAL, SSD_ESHAPE (B times tiles of 16 query rows of a K/V head more than 65535; more than 512 query heads a K/V
+ * head, or 2^21 query heads of tokens), SSD_EUNSUPPORTED, SSD_EWORKSPACE. */
 int paged_attention(ssd_ctx *ctx, const void *q /*dev*/, int q_dtype, int64_t q_stride, int n_q_heads, int n_new, const ssd_kv_pages *pages /*host*/,
                     const ssd_page_table *table /*host*/, float scale, void *out, float *lse);
 

@@ -2107,7 +2107,7 @@ PagedPlan plan_paged(int64_t B, int64_t n_kv_heads, int64_t rows, int head_dim, 
     const int64_t tiles = (rows + paged_tile_rows(rows) - 1) / paged_tile_rows(rows), most = (max_ctx + PAGED_UNIT - 1) / PAGED_UNIT, pairs = n_kv_heads * tiles;
     PagedPlan p = {0, 1, 0, 0, 0};
     if (most > paged_whole(pairs * B)) {
-        if (B <= PAGED_UTTS && B * most < INT32_MAX) {
+        if (B <= PAGED_UTTS && B * most <= 1 << 28) {        // (a workgroup a piece: fewer than 2^24 along one dimension of a launch)
             const int64_t at_once = std::max<int64_t>(1, PAGED_CUS * paged_per_cu(head_dim, paged_tile_rows(rows)) / pairs);
             p.shared = (int)(at_once * ((PAGED_EACH * B + at_once - 1) / at_once));
             const int64_t rounds = std::max<int64_t>(1, (B * most + (int64_t)p.shared * PAGED_MOST - 1) / ((int64_t)p.shared * PAGED_MOST));
@@ -2184,6 +2184,7 @@ int kv_read_pages(ssd_ctx* ctx, const ssd_kv_pages* pages, const ssd_page_table*
 
 size_t ssd_paged_workspace_bytes(const ssd_ctx* ctx, int n_q_heads, int n_kv_heads, int head_dim, int64_t B, int n_new, int64_t max_ctx) {
     if (!ctx || n_q_heads <= 0 || n_kv_heads <= 0 || head_dim <= 0 || B < 0 || n_new < 0 || max_ctx < 0) return 0;
+    if (n_q_heads > 65535 || B > 65535 || max_ctx > 1 << 30 || B * n_new > PAGED_QUERIES || B * n_new * n_q_heads > PAGED_QUERIES) return 0;      // (no call is so large)
     const int64_t most = (max_ctx + PAGED_UNIT - 1) / PAGED_UNIT, rows = (int64_t)n_new * n_q_heads;
     // (as many workgroups as run at once, four a CU at most, with 32 rows each, or more pieces: see plan_paged)
     return paged_bytes(4 * PAGED_CUS * 32 + (B * most / PAGED_MOST + (PAGED_EACH + 1) * B + 2) * rows, paged_dims(head_dim), B) + 256;
@@ -2204,6 +2205,7 @@ int paged_attention(ssd_ctx* ctx, const void* q, int q_dtype, int64_t q_stride, 
     if (n_q_heads > 65535 || group > 512) return fail(ctx, SSD_ESHAPE, "paged_attention: more than 65535 query heads, or 512 per K/V head");
     if (n_new <= 0) return fail(ctx, SSD_EINVAL, "paged_attention: n_new must be positive (got %d)", n_new);
     if (((int64_t)n_new * group + 15) / 16 * table->B > 65535) return fail(ctx, SSD_ESHAPE, "paged_attention: more than 65535 tiles of query rows; split the batch");
+    if ((int64_t)table->B * n_new * n_q_heads > PAGED_QUERIES) return fail(ctx, SSD_ESHAPE, "paged_attention: more than 2^21 queries (tokens times heads); split the batch");
     if (!std::isfinite(scale * 1.4426950408889634f)) return fail(ctx, SSD_EINVAL, "paged_attention: scale is not finite, or not to base 2");
     if (!q || !out) return fail(ctx, SSD_EINVAL, "paged_attention: NULL data pointer");
     const int64_t dq = (int64_t)n_q_heads * pages->head_dim, es = (int64_t)kv_elem(q_dtype), N = (int64_t)table->B * n_new;

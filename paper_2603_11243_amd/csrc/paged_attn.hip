@@ -1,16 +1,21 @@
 // Attention of the newest tokens over the pages of their utterances:
 //   s_j = scale q . k_j,  lse = log sum_j exp s_j,  o = sum_j exp(s_j - lse) v_j   over the rows j that the token sees.
 //
-// One pass over the rows with a running maximum and sum.  A workgroup has up to 16 query rows of a K/V head (tokens times heads of the group), a column each of
-// the matrix instructions, and a piece of the context; its four wavefronts take blocks of KEYS rows in turn and are joined through LDS, the pieces of a context
+// One pass over the rows with a running maximum and sum.  A workgroup has 16 or 32 query rows of a K/V head (tokens times heads of the group), a column each of the
+// matrix instructions, and a piece of a context; its four wavefronts take blocks of KEYS rows in turn and are joined through LDS, the pieces of a context
 // by a second kernel.  S^T = K Q^T, then O^T += V^T P^T:
 //   first product   lane (dc = lane % 16, g = lane / 16) holds row dc of a tile of 16 keys, the dims that its loads of 16 bytes bring (queries in the same order)
 //   its result      column dc, keys 4 g + r
 //   second product  the same lane's keys: so the weights are operands where they are, and the values of rows 4 g + r, dims DPL dc .. are loaded into the lane that
-//                   needs them: a byte permutation inside its registers makes operands of them.  No LDS, no exchange, no barrier in the loop.
-// 16-bit pages and codes go through v_mfma_f32_16x16x32 (half pages: half; all else bfloat16, which holds the codes of both 8-bit types exactly), fp32 pages through
-// v_mfma_f32_16x16x4_f32.  The scale of a key row multiplies its score, that of a value row its weight.
-// What bounds it is memory: 16 rows are few for the matrix cores.
+//                   needs them: a byte permutation inside its registers makes operands of them.  No LDS and no barrier in the loop; lanes exchange the maximum alone.
+// 16-bit pages and codes go through v_mfma_f32_16x16x32 (half pages, and the first product of half queries with codes: half; all else bfloat16; both hold the codes of
+// the 8-bit types exactly), fp32 pages through v_mfma_f32_16x16x4_f32.  The scale of a key row multiplies its score, that of a value row its weight.
+//
+// Bound by memory: a block is 32 registers a lane of keys and values each, requested again as soon as they are used, with two workgroups a CU (head_dim 128) 16 KB a
+// wavefront on the way (codes 8 KB; twice as many keys a block changed nothing over long contexts and cost 90 short ones of int8 15.5 -> 20 us).  Eight K/V heads of 128, two query
+// heads each: 200001 rows of bfloat16 144 us, 5.7 TB/s; four of 40000 rows of half 118 us (5.6), e4m3 66 (5.2), int8 67 (5.0); eight of 60000, e4m3, 179 (5.7).  Three workgroups a CU
+// were slower (four recordings of e4m3 60 against 54 us: fewer, fuller rounds).  A context of 106 rows is 5.1 us in a graph: a launch, and length, page numbers, keys and
+// merge one behind the other; every further block of a wavefront 1.3 us.  32 columns where there are more than 16 rows: 27 rows over 16 contexts of int8 62 -> 50 us.
 #include "pages.h"
 #include "tree_attn.h"
 

@@ -50,6 +50,7 @@ struct PagedAttnArgs {
     int2* first;                             // [utterance] first piece, pieces
 };
 constexpr int PAGED_UNIT = 128, PAGED_MOST = 32;             // a round of four wavefronts of 32 rows; units of a piece, of which a wavefront has the page numbers in a register
+constexpr int64_t PAGED_QUERIES = 1 << 21;                   // of a call: workgroups of up to 1024 threads that join their pieces
 constexpr int PAGED_UTTS = 1024;                             // utterances of a batch that shares
 inline int paged_dims(int head_dim) { return head_dim > 64 ? 128 : 64; }
 inline int paged_tile_rows(int64_t rows) { return rows <= 16 ? 16 : 32; }

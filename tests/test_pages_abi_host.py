@@ -78,6 +78,9 @@ def test_attention(lib, ctx):  # noqa: F811
         assert call(**k) == EINVAL, k
     for k in ({"hq": 3}, {"hq": 0}, {"hq": -2}, {"hq": 1026, "q_stride": 1 << 18}, {"n_new": 16 * 65536 // 2 // 3 + 16}):
         assert call(**k) == ESHAPE, k
+    # 2^21 query heads of tokens: as many workgroups join the pieces
+    many = dict(p=pages(H=64, dtype=I8), hq=64, q_stride=8192, q=1 << 50, out=1 << 52, t=table(B=512, stride=1000, max_ctx=16000))
+    assert call(n_new=64, **many) == EWORKSPACE and call(n_new=65, **many) == ESHAPE
     for k in ({"dtype": 3}, {"dtype": 9}, {"dtype": BF16}, {"dtype": F32, "q_stride": 1024}, {"p": pages(dtype=F32)}, {"p": pages(dtype=BF16)}):
         assert call(**k) == EUNSUPPORTED, k
     for near in (0, 3 * 1024 - 16, -3 * 1024 + 16):
@@ -124,15 +127,16 @@ def test_workspace_covers_every_call(lib, ctx):  # noqa: F811
     some = lambda top: max(1, int(top ** r.random()))
     for _ in range(4000):
         B, new, H, G, n, hd = some(65535), some(300), some(64), some(64), some(1 << 30), r.choice([64, 128])
-        if (new * G + 15) // 16 * B > 65535:
+        if (new * G + 15) // 16 * B > 65535 or B * new * G * H > 1 << 21:
             continue
         rc = attention(lib, ctx, q=1 << 50, out=1 << 60, q_stride=G * H * hd, hq=G * H, n_new=new, p=pages(H=H, hd=hd, R=16), t=table(B=B, max_ctx=n, stride=1 << 27))
         need = 0
         if rc == EWORKSPACE:
             need = int(re.search(rb"workspace of (\d+) bytes", lib.ssd_last_error(ctx)).group(1))
             size = lambda *a: lib.ssd_paged_workspace_bytes(ctx, *a)
-            assert need <= size(G * H, H, hd, B, new, n) <= size(G * H, H, hd, B + some(100), new, n)
-            assert need <= size(G * H, H, 128, B, new + some(10), n + some(10000)) and need <= size(2 * G * H, H, hd, B, new, n)
+            assert need <= size(G * H, H, hd, B, new, n)
+            for more in (size(G * H, H, hd, B + some(100), new, n), size(G * H, H, 128, B, new + some(10), min(1 << 30, n + some(10000))), size(2 * G * H, H, hd, B, new, n)):
+                assert need <= more or more == 0                 # (0: no call is so large)
         else:
             assert n <= 4096 or rc != 0
 

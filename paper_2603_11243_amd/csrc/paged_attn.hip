@@ -60,6 +60,10 @@ __device__ __forceinline__ uint32_t code_pair(uint32_t w) {
     }
 }
 
+// Whole numbers in byte I of two words to a pair of bfloat16.
+template <int I>
+__device__ __forceinline__ uint32_t whole_pair(uint32_t lo, uint32_t hi) { return __builtin_amdgcn_perm(__float_as_uint(whole<I>(hi)), __float_as_uint(whole<I>(lo)), 0x07060302u); }
+
 // The sign bits of the elements of a word that are not finite; the word with zeros for them.
 template <int PT> __device__ __forceinline__ uint32_t not_finite(uint32_t w) {
     if constexpr (PT == SSD_I8) return 0u;
@@ -136,9 +140,16 @@ __device__ __forceinline__ int shared_units(const PagedAttnArgs& a, int total, i
     return max(1, (int)(((uint32_t)total + pieces - 1) / (uint32_t)pieces));
 }
 
-__device__ __forceinline__ int lanes_sum(int v) {
-#pragma unroll
-    for (int d = 1; d < 64; d *= 2) v += __shfl_xor(v, d);
+struct OpAdd { __device__ __forceinline__ int operator()(int x, int y) const { return x + y; } };
+__device__ __forceinline__ int lanes_sum(int v) { return group_allreduce_i<64>(v, OpAdd()); }
+// Sum of the lanes up to each: inside rows of 16, then over the rows before (their last lanes go to the rows behind).
+__device__ __forceinline__ int lanes_scan(int v) {
+    v += __builtin_amdgcn_update_dpp(0, v, 0x111, 0xf, 0xf, false);      // row_shr 1, 2, 4, 8
+    v += __builtin_amdgcn_update_dpp(0, v, 0x112, 0xf, 0xf, false);
+    v += __builtin_amdgcn_update_dpp(0, v, 0x114, 0xf, 0xf, false);
+    v += __builtin_amdgcn_update_dpp(0, v, 0x118, 0xf, 0xf, false);
+    v += __builtin_amdgcn_update_dpp(0, v, 0x142, 0xa, 0xf, false);      // row_bcast 15 to rows 1 and 3
+    v += __builtin_amdgcn_update_dpp(0, v, 0x143, 0xc, 0xf, false);      // row_bcast 31 to rows 2 and 3
     return v;
 }
 
@@ -168,12 +179,7 @@ __device__ __forceinline__ bool find_piece(const PagedAttnArgs& a, Piece& t) {
             if (pieces <= want || share == PAGED_MOST || turn == 8) break;
             share = min(PAGED_MOST, max(share + 1, (int)((float)share * (float)pieces / (float)want)));
         }
-        int sum = n;
-#pragma unroll
-        for (int d = 1; d < 64; d *= 2) {
-            const int before = __shfl_up(sum, d);
-            sum += lane >= d ? before : 0;
-        }
+        const int sum = lanes_scan(n);
         const uint64_t behind = __ballot(sum > x);
         if (!behind) return false;
         t.b = __ffsll((unsigned long long)behind) - 1;
@@ -202,12 +208,7 @@ __device__ __forceinline__ bool find_piece(const PagedAttnArgs& a, Piece& t) {
         int n[PER], mine = 0;
 #pragma unroll
         for (int e = 0; e < PER; ++e) mine += n[e] = tid * PER + e < p.B ? max(1, (int)((uint32_t)(units(clamped(p, given[e])) + share - 1) / (uint32_t)share)) : 0;
-        int sum = mine;
-#pragma unroll
-        for (int d = 1; d < 64; d *= 2) {
-            const int before = __shfl_up(sum, d);
-            sum += lane >= d ? before : 0;
-        }
+        int sum = lanes_scan(mine);
         __syncthreads();
         if (lane == 63) wave_s[wave] = sum;
         if (tid == 0) found_s[0] = -1;
@@ -512,7 +513,16 @@ __global__ void __launch_bounds__(64 * WAVES, 2) paged_attn_kernel(PagedAttnArgs
             };
             const auto& v0 = vr[0];
             const auto& v1 = vr[1];
-            if constexpr (T::CODES) {
+            if constexpr (PT == SSD_I8) {
+#pragma unroll
+                for (int i = 0; i < DT; i += 4) {            // byte i % 4 of two rows
+                    const auto rows = [&](int r) { return r < 4 ? v0[r][0][i / 4] : v1[r - 4][0][i / 4]; };
+                    add(i, whole_pair<0>(rows(0), rows(1)), whole_pair<0>(rows(2), rows(3)), whole_pair<0>(rows(4), rows(5)), whole_pair<0>(rows(6), rows(7)));
+                    add(i + 1, whole_pair<1>(rows(0), rows(1)), whole_pair<1>(rows(2), rows(3)), whole_pair<1>(rows(4), rows(5)), whole_pair<1>(rows(6), rows(7)));
+                    add(i + 2, whole_pair<2>(rows(0), rows(1)), whole_pair<2>(rows(2), rows(3)), whole_pair<2>(rows(4), rows(5)), whole_pair<2>(rows(6), rows(7)));
+                    add(i + 3, whole_pair<3>(rows(0), rows(1)), whole_pair<3>(rows(2), rows(3)), whole_pair<3>(rows(4), rows(5)), whole_pair<3>(rows(6), rows(7)));
+                }
+            } else if constexpr (PT == SSD_E4M3) {
 #pragma unroll
                 for (int i = 0; i < DT; i += 2) {            // bytes i, i + 1 of two rows side by side
                     const uint32_t pick = i % 4 ? 0x07030602u : 0x05010400u;

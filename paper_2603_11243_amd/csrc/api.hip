@@ -2103,12 +2103,12 @@ size_t paged_ml(int64_t rows, int dims) { return align_up((size_t)(rows * dims) 
 size_t paged_first(int64_t rows, int dims) { return paged_ml(rows, dims) + align_up((size_t)rows * sizeof(float2)); }
 size_t paged_bytes(int64_t rows, int dims, int64_t B) { return paged_first(rows, dims) + align_up((size_t)B * sizeof(int2)); }
 struct PagedPlan { int shared, n_pieces; size_t ml, first, total; };
-PagedPlan plan_paged(int64_t B, int64_t n_kv_heads, int64_t rows, int head_dim, int64_t max_ctx) {
-    const int64_t tiles = (rows + paged_tile_rows(rows) - 1) / paged_tile_rows(rows), most = (max_ctx + PAGED_UNIT - 1) / PAGED_UNIT, pairs = n_kv_heads * tiles;
+PagedPlan plan_paged(int64_t B, int64_t n_kv_heads, int64_t rows, int tile_rows, int head_dim, int64_t max_ctx) {
+    const int64_t tiles = (rows + tile_rows - 1) / tile_rows, most = (max_ctx + PAGED_UNIT - 1) / PAGED_UNIT, pairs = n_kv_heads * tiles;
     PagedPlan p = {0, 1, 0, 0, 0};
     if (most > paged_whole(pairs * B)) {
         if (B <= PAGED_UTTS && B * most <= 1 << 28) {        // (a workgroup a piece: fewer than 2^24 along one dimension of a launch)
-            const int64_t at_once = std::max<int64_t>(1, PAGED_CUS * paged_per_cu(head_dim, paged_tile_rows(rows)) / pairs);
+            const int64_t at_once = std::max<int64_t>(1, PAGED_CUS * paged_per_cu(head_dim, tile_rows) / pairs);
             p.shared = (int)(at_once * ((PAGED_EACH * B + at_once - 1) / at_once));
             const int64_t rounds = std::max<int64_t>(1, (B * most + (int64_t)p.shared * PAGED_MOST - 1) / ((int64_t)p.shared * PAGED_MOST));
             p.n_pieces = (int)std::min<int64_t>(p.shared * rounds + B, B * most);
@@ -2217,9 +2217,9 @@ int paged_attention(ssd_ctx* ctx, const void* q, int q_dtype, int64_t q_stride, 
     a.p = pages_args(ctx, *pages, *table);
     a.q = q; a.q_stride = q_stride; a.out = out; a.lse = lse;
     a.n_q_heads = n_q_heads; a.group = group; a.n_new = n_new; a.scale = scale;
-    a.tile_rows = paged_tile_rows((int64_t)n_new * group);
+    a.tile_rows = paged_tile_rows((int64_t)n_new * group, table->B, pages->n_kv_heads, table->max_ctx, pages->head_dim, q_dtype, pages->dtype);
     a.tiles = (n_new * group + a.tile_rows - 1) / a.tile_rows;
-    const PagedPlan plan = plan_paged(table->B, pages->n_kv_heads, (int64_t)n_new * group, pages->head_dim, table->max_ctx);
+    const PagedPlan plan = plan_paged(table->B, pages->n_kv_heads, (int64_t)n_new * group, a.tile_rows, pages->head_dim, table->max_ctx);
     if (plan.total && (!ctx->ws || ctx->ws_bytes < plan.total))
         return fail(ctx, SSD_EWORKSPACE, "paged_attention: workspace of %zu bytes needed, %zu set", plan.total, ctx->ws_bytes);
     a.shared = plan.shared; a.n_pieces = plan.n_pieces;

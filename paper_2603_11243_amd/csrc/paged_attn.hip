@@ -663,7 +663,8 @@ void launch_rows(const PagedAttnArgs& a, hipStream_t st) {
     const dim3 grid(a.n_pieces, a.p.n_kv_heads, a.shared ? a.tiles : a.p.B * a.tiles);
     constexpr int used = WAVES * 16 * ((HD + 4) * 4 + 8);
     const int more = a.shared ? PAGED_CU_LDS / (paged_per_cu(a.p.head_dim, a.tile_rows) + 1) + 1024 - used : 0;
-    if (a.tile_rows == 16) paged_attn_kernel<QT, PT, HD, 1><<<grid, 64 * WAVES, more, st>>>(a);
+    if constexpr (Kind<QT, PT>::CODES && QT == SSD_F32) paged_attn_kernel<QT, PT, HD, 1><<<grid, 64 * WAVES, more, st>>>(a);
+    else if (a.tile_rows == 16) paged_attn_kernel<QT, PT, HD, 1><<<grid, 64 * WAVES, more, st>>>(a);
     else paged_attn_kernel<QT, PT, HD, 2><<<grid, 64 * WAVES, more, st>>>(a);
     const unsigned n = (unsigned)((int64_t)a.p.B * a.n_new * a.n_q_heads);
     const int each = a.shared ? a.n_pieces / a.p.B : a.n_pieces;             // pieces of an utterance, about

@@ -53,7 +53,17 @@ constexpr int PAGED_UNIT = 128, PAGED_MOST = 32;             // a round of four 
 constexpr int64_t PAGED_QUERIES = 1 << 21;                   // of a call: workgroups of up to 1024 threads that join their pieces
 constexpr int PAGED_UTTS = 1024;                             // utterances of a batch that shares
 inline int paged_dims(int head_dim) { return head_dim > 64 ? 128 : 64; }
-inline int paged_tile_rows(int64_t rows) { return rows <= 16 ? 16 : 32; }
+// Query rows of a workgroup.  32 read keys and values half as often as 16, which halves what long contexts cost, but are longer on their way through a block and fewer workgroups: by the
+// units of rows that workgroups of 16 would take.  Half, 12 tokens of 16 heads on 8 of 128, 16 and 32: 4 contexts of 150 to 300 rows 7.8 and 9.8 us, 1250 to 2500 (1280 units) 17.3 and
+// 17.9, 10000 to 20000 72 and 61; 40 of 30 to 60 (640) 10.3 and 9.6, 300 to 600 25 and 22, 2000 to 4000 195 and 115.  Codes of 64 dims, 7 tokens of 16 heads on 4: 40 contexts of 750
+// to 1500 (3840) 16.0 and 17.8, 2000 to 4000 (10240) 25.9 and 23.7.  fp32 pages of 64 dims 20.5 and 22.5 (1600), 43 and 36 (3840), of 128 120 and 148 (7680), 375 and 281 (20480);
+// fp32 queries over codes have no registers for 32 (101 and 140).
+inline int paged_tile_rows(int64_t rows, int64_t B, int64_t n_kv_heads, int64_t max_ctx, int head_dim, int q_dtype, int pages_dtype) {
+    const bool codes = pages_dtype == SSD_E4M3 || pages_dtype == SSD_I8, wide = paged_dims(head_dim) == 128;
+    if (rows <= 16 || (codes && q_dtype == SSD_F32)) return 16;
+    const int64_t from = q_dtype == SSD_F32 ? (wide ? 15000 : 3000) : codes && !wide ? 8000 : 1000;
+    return B * n_kv_heads * ((rows + 15) / 16) * ((max_ctx + PAGED_UNIT - 1) / PAGED_UNIT) >= from ? 32 : 16;
+}
 // Workgroups of a CU whose registers fit; shared pieces are as many as run at once, and are held to so many a CU by the LDS they ask for.
 inline int paged_per_cu(int head_dim, int tile_rows) { return paged_dims(head_dim) == 128 ? 2 : tile_rows == 16 ? 4 : 3; }
 constexpr int PAGED_CUS = 256, PAGED_CU_LDS = 160 * 1024;

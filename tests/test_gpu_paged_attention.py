@@ -238,6 +238,35 @@ def test_tables_far_longer_than_the_contexts(pair, lens, most):
     _check(pair, (4, 2, 64), lens, 64, 2, most=most)
 
 
+@pytest.mark.parametrize("pair", PAIRS)
+@pytest.mark.parametrize("hd", [64, 128])
+def test_wide_tiles(pair, hd):
+    """What long contexts take where there are more than 16 query rows, over short ones too: the launch is made for 400000 rows."""
+    _check(pair, (8, 2, hd), [0, 5, 300, 2000, 8], 64, 9, most=400000)
+
+
+@pytest.mark.parametrize("pair", PAIRS)
+@pytest.mark.parametrize("bad", ["nan", "inf"])
+def test_rows_of_later_tokens_do_not_count_in_wide_tiles(pair, bad):
+    """The last row but two is not finite: tokens before it stay as they are, columns of either half of a tile."""
+    heads, n_new = (8, 2, 128), 9
+    q, pool = _queries(pair[0], 2, n_new, heads), Pool(pair[1], heads[1:], [50, 667], 16, most=400000)
+    want, tol, _, _ = attention(q, pool, n_new)
+    for b in range(2):
+        j = int(pool.ctx_host[b]) - 3
+        at = (0, int(pool.table_host[b, j // 16]), slice(None), j % 16)
+        for name in ("k", "v"):
+            if pool.kind in ("e4m3", "i8"):
+                pool.parts[name + "_scale"][at] = float(bad)
+                if pool.kind == "e4m3" and bad == "nan":
+                    pool.parts[name].view(torch.uint8)[at] = 127
+            else:
+                pool.parts[name][at] = float(bad)
+    out = _context(2, n_new, heads, 400000).paged_attention(q, pool.pages(), pool.table, pool.ctx_len).double().cpu().numpy()
+    assert (np.abs(out - want) <= tol)[:, :-3].all()
+    assert not np.isfinite(out[:, -3:]).any()
+
+
 @pytest.mark.parametrize("B, long", [(65, 900), (70, 3000), (300, 2500), (1024, 4200), (1030, 4200), (1030, 9000)])
 def test_large_batches_with_one_long_context(B, long):
     lens = [b % 7 for b in range(B)]

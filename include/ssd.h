@@ -496,7 +496,7 @@ typedef struct {
  *   SSD_I8    scale = a / 127 in fp32 (at most the largest of which 127 times is finite);  code = 127 x / a to the nearest whole number, halves to even, of the exact quotient
  *   a row of zeros has scale 0; a row that is not finite has codes 0 and scale NaN, and raises SSD_FLAG_ACT_OVERFLOW
  * kv_read_pages, back: code * scale in fp32, rounded to the type of `slots`; IEEE half: clamped to +-65504 with SSD_FLAG_ACT_OVERFLOW, which NaN raises too.
- * No workspace.  Calls may be captured.  Errors: SSD_EINVAL, SSD_ESHAPE (sizes above; more than 65535 utterances), SSD_EUNSUPPORTED (types). */
+ * max_rows or max_ctx 0: nothing is done.  No workspace.  Calls may be captured.  Errors: SSD_EINVAL, SSD_ESHAPE (sizes above; more than 65535 utterances), SSD_EUNSUPPORTED (types). */
 int kv_write_pages(ssd_ctx *ctx, const ssd_kv_view *slots /*host*/, const int32_t *start, const int32_t *n_rows, int max_rows,
                    const ssd_kv_pages *pages /*host*/, const ssd_page_table *table /*host*/);
 int kv_read_pages(ssd_ctx *ctx, const ssd_kv_pages *pages /*host*/, const ssd_page_table *table /*host*/, const ssd_kv_view *slots /*host*/,
@@ -514,7 +514,8 @@ size_t ssd_paged_workspace_bytes(const ssd_ctx *ctx, int n_q_heads, int n_kv_hea
  *   out     dev [B * n_new, n_q_heads * head_dim] of q_dtype, 16-byte aligned
  *   lse     dev [B * n_new, n_q_heads] fp32, or NULL
  * Scores, sums and statistics are fp32; 8-bit codes are exact operands.  A weight enters the second product as two values of 16 bits (22 bits of it with SSD_F16 pages, 16 with
- * others; three values, 24 bits, with 8-bit pages and SSD_F32 queries), with SSD_F32 pages as it is.  Outputs below 2^-90 lose bits.  A row that a token does not see, and what
+ * others; three values, 24 bits, with 8-bit pages and SSD_F32 queries), with SSD_F32 pages as it is.  Outputs below 2^-90 lose bits.  With 8-bit pages q . k is formed of codes
+ * before scales, and has to stay in fp32's range there: |q| up to 2^112 does.  A row that a token does not see, and what
  * lies behind the last row of a page, has no influence on it, whatever it holds; a value that it sees and that is not finite makes its column infinite or NaN.
  * Captured calls use the workspace of the time of capture: two that share one must not run at the same time.  Every call repeats to the bit.
  * Errors: SSD_EINVAL, SSD_ESHAPE (B times tiles of 16 query rows of a K/V head more than 65535; more than 512 query heads a K/V

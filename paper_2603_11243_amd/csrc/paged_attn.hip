@@ -15,7 +15,7 @@
 // wavefront on the way (codes 8 KB; twice as many keys a block changed nothing over long contexts and cost 90 short ones of int8 15.5 -> 20 us).  Eight K/V heads of 128, two query
 // heads each: 200001 rows of bfloat16 144 us, 5.7 TB/s; four of 40000 rows of half 118 us (5.6), e4m3 66 (5.2), int8 67 (5.0); eight of 60000, e4m3, 179 (5.7).  Three workgroups a CU
 // were slower (four recordings of e4m3 60 against 54 us: fewer, fuller rounds).  A context of 106 rows is 5.1 us in a graph: a launch, and length, page numbers, keys and
-// merge one behind the other; every further block of a wavefront 1.3 us.  32 columns where there are more than 16 rows: 27 rows over 16 contexts of int8 62 -> 50 us.
+// merge one behind the other; every further block of a wavefront 1.3 us.  32 columns where that pays (paged_tile_rows): 27 rows over 16 contexts of int8 62 -> 49 us.
 #include "pages.h"
 #include "tree_attn.h"
 
@@ -602,13 +602,14 @@ __global__ void __launch_bounds__(64 * WAVES, 2) paged_attn_kernel(PagedAttnArgs
     if (bad) raise_flag(p.flags, SSD_FLAG_BAD_PAGE);
 }
 
-// The pieces of a context, a mean of values each, joined: a workgroup has a query row, groups of HD / 4 lanes take its pieces in turn and are joined through LDS.
+// The pieces of a context, a mean of values each, joined: a workgroup has a query row, groups of HD / 4 lanes take its pieces in turn and are joined by lane moves, the
+// wavefronts through LDS.
 template <int QT, int HD, int THREADS>
 __global__ void __launch_bounds__(THREADS) paged_join_kernel(PagedAttnArgs a) {
     typedef Elem<QT> E;
-    constexpr int LANES = HD / 4, GROUPS = THREADS / LANES, U = 4;
-    __shared__ f32x4_t o_s[GROUPS][LANES];
-    __shared__ float2 ml_s[GROUPS];
+    constexpr int LANES = HD / 4, GROUPS = THREADS / LANES, U = 4, JOIN_WAVES = THREADS / 64;
+    __shared__ f32x4_t o_s[JOIN_WAVES][LANES];
+    __shared__ float2 ml_s[JOIN_WAVES];
     const int64_t at = blockIdx.x;
     const int token = (int)(at / a.n_q_heads), head = (int)(at % a.n_q_heads), b = token / a.n_new;
     const int first = a.first[b].x, pieces = a.first[b].y;
@@ -637,15 +638,26 @@ __global__ void __launch_bounds__(THREADS) paged_join_kernel(PagedAttnArgs a) {
             v = v * (old * inv) + z[u] * (now * inv);
         }
     }
-    o_s[group][dim / 4] = v;
-    if (dim == 0) ml_s[group] = make_float2(m, l);
+#pragma unroll
+    for (int off = LANES; off < 64; off *= 2) {
+        const float other_m = __shfl_xor(m, off), other_l = __shfl_xor(l, off);
+        const f32x4_t other_v = {__shfl_xor(v[0], off), __shfl_xor(v[1], off), __shfl_xor(v[2], off), __shfl_xor(v[3], off)};
+        const float top = fmaxf(m, other_m), old = l == 0.f ? 0.f : l * __builtin_amdgcn_exp2f(m - top);
+        const float now = other_l == 0.f ? 0.f : other_l * __builtin_amdgcn_exp2f(other_m - top), sum = old + now, inv = sum == 0.f ? 0.f : 1.f / sum;
+        m = top;
+        l = sum;
+        v = v * (old * inv) + other_v * (now * inv);
+    }
+    const int wave = threadIdx.x / 64;
+    if (threadIdx.x % 64 < LANES) o_s[wave][dim / 4] = v;
+    if (threadIdx.x % 64 == 0) ml_s[wave] = make_float2(m, l);
     __syncthreads();
     if (group || dim >= a.p.head_dim) return;
-    float mt = -F32_MOST, lt = 0.f, f[GROUPS];
+    float mt = -F32_MOST, lt = 0.f, f[JOIN_WAVES];
 #pragma unroll
-    for (int i = 0; i < GROUPS; ++i) mt = fmaxf(mt, ml_s[i].x);
+    for (int i = 0; i < JOIN_WAVES; ++i) mt = fmaxf(mt, ml_s[i].x);
 #pragma unroll
-    for (int i = 0; i < GROUPS; ++i) {
+    for (int i = 0; i < JOIN_WAVES; ++i) {
         const float2 y = ml_s[i];
         f[i] = y.y == 0.f ? 0.f : y.y * __builtin_amdgcn_exp2f(y.x - mt);
         lt += f[i];
@@ -653,7 +665,7 @@ __global__ void __launch_bounds__(THREADS) paged_join_kernel(PagedAttnArgs a) {
     const float inv = lt == 0.f ? 0.f : 1.f / lt;
     f32x4_t s = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-    for (int i = 0; i < GROUPS; ++i) s += o_s[i][dim / 4] * (f[i] * inv);
+    for (int i = 0; i < JOIN_WAVES; ++i) s += o_s[i][dim / 4] * (f[i] * inv);
     store4<QT>((typename E::type*)a.out + at * a.p.head_dim + dim, s);
     if (a.lse && dim == 0) a.lse[at] = lt == 0.f ? -INFINITY : (mt + __builtin_amdgcn_logf(lt)) * LN2;
 }
@@ -668,9 +680,12 @@ void launch_rows(const PagedAttnArgs& a, hipStream_t st) {
     else paged_attn_kernel<QT, PT, HD, 2><<<grid, 64 * WAVES, more, st>>>(a);
     const unsigned n = (unsigned)((int64_t)a.p.B * a.n_new * a.n_q_heads);
     const int each = a.shared ? a.n_pieces / a.p.B : a.n_pieces;             // pieces of an utterance, about
-    if (each > 64) paged_join_kernel<QT, HD, 1024><<<n, 1024, 0, st>>>(a);
+    // 128, 256, 512 and 1024 threads, whole calls in a graph: 2 pieces of 1288 rows 16.6, 17.0, 18.4, 21.4 us; 16 of 64 50.7, 50.0, 50.2, 50.6; 64 of 16 145.8, 144.1, 143.7,
+    // 144.2; 85 of 192 22.4, 20.7, 20.4, 20.1; 235 of 8 23.3, 17.0, 14.1, 13.0
+    if (each > 128) paged_join_kernel<QT, HD, 1024><<<n, 1024, 0, st>>>(a);
+    else if (each > 32) paged_join_kernel<QT, HD, 512><<<n, 512, 0, st>>>(a);
     else if (each > 8) paged_join_kernel<QT, HD, 256><<<n, 256, 0, st>>>(a);
-    else if (a.n_pieces > 1) paged_join_kernel<QT, HD, 64><<<n, 64, 0, st>>>(a);
+    else if (a.n_pieces > 1) paged_join_kernel<QT, HD, 128><<<n, 128, 0, st>>>(a);
 }
 template <int QT, int PT>
 void launch_dims(const PagedAttnArgs& a, hipStream_t st) {

@@ -223,7 +223,7 @@ def test_repeats_to_the_bit_and_batches_do_not_mix():
     """Twice the same; an utterance by itself, in the same launch shape, too."""
     heads = (16, 8, 128)
     pool = Pool("i8", heads[1:], [3000, 40, 777, 0, 2048], 64)
-    q, c = _queries("f16", 5, 2, heads), _context(5, 2, heads, 3072)
+    q, c = _queries("f16", 5, 2, heads), _context(5, 2, heads, 3200)
     a = c.paged_attention(q, pool.pages(), pool.table, pool.ctx_len)
     for _ in range(3):
         assert torch.equal(a, c.paged_attention(q, pool.pages(), pool.table, pool.ctx_len))
@@ -361,3 +361,10 @@ def test_refusals_of_the_binding():
             moves(**bad)
     with pytest.raises(SsdError):
         moves(max_rows=5)
+
+
+@pytest.mark.parametrize("pair", [("f16", "f16"), ("bf16", "i8"), ("f32", "e4m3"), ("f32", "f32")])
+@pytest.mark.parametrize("heads, lens", [((8, 1, 128), [30000]), ((16, 4, 64), [9000, 8000, 127]), ((8, 4, 128), [5000] * 7 + [1]), ((6, 6, 64), [4000] * 20)])
+def test_joining_few_and_many_pieces(pair, heads, lens):
+    """About 235, 70, 20 and 8 pieces a context, and one with a piece or two beside them; the first token sees one row less."""
+    _check(pair, heads, lens, 128, 2)

@@ -4,6 +4,7 @@ import pytest
 import torch
 
 from tests.test_gpu_verify import _tau_for
+from tests.test_gpu_verify_tree import _weights
 from workloads import WORKLOADS, make_ctc_batch, make_ctc_to_llm_map, make_model_weights, make_verify_inputs
 from workloads.configs import scaled_down
 
@@ -38,3 +39,31 @@ def test_rows_in_pages_between_the_phases(name, layers):
         assert ctx.device_flags() == 0
     finally:
         ctx.close()
+
+
+@pytest.mark.parametrize("trees", [None, dict(tau=0.5, depth=4)])
+def test_pages_with_trees_and_another_stream_current(trees):
+    """The rows come back to slots with the room that trees take; the calls are queued while another stream than the context's is the current one."""
+    from paper_2603_11243_amd.binding import Context
+    from paper_2603_11243_amd.pipeline import TwoPhaseDecoder
+    wl = WORKLOADS["cfg1_tiny_f32"]
+    cb, table = make_ctc_batch(wl), make_ctc_to_llm_map(wl)
+    vi = make_verify_inputs(wl, cb.seconds, [np.zeros(0, np.int32)] * wl.B, device="cuda")
+    runs, side = [], torch.cuda.Stream()
+    for mode, stream in (("resident", None), ("paged", side)):
+        ctx = Context(wl.model, _weights(wl.model, 3), stream=stream)
+        dec = TwoPhaseDecoder(ctx, wl, cb.logits.cuda(), cb.cu_frames, torch.from_numpy(table).cuda(), vi.speech_emb, vi.cu_speech,
+                              torch.from_numpy(vi.prompt_ids).cuda(), vi.cu_prompt, budget=300, mode=mode, n_steps=9, trees=trees, pages_dtype=torch.float32, page_rows=32)
+        torch.cuda.synchronize()
+        if stream is not None:
+            with torch.cuda.stream(side):
+                a = torch.randn(4096, 4096, device="cuda")
+                for _ in range(100):                         # some tens of milliseconds
+                    a = torch.matmul(a, a).clamp_(-1, 1)
+        runs.append(dec.run(0.5))
+        torch.cuda.synchronize()
+        assert ctx.device_flags() == 0
+        ctx.close()
+    want, got = runs
+    assert want["rejected"] > 0 and np.array_equal(got["accept_len"], want["accept_len"]) and set(got["tokens"]) == set(want["tokens"])
+    assert all(np.array_equal(t, want["tokens"][b]) for b, t in got["tokens"].items())

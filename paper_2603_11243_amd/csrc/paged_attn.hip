@@ -15,7 +15,7 @@
 // wavefront on the way (codes 8 KB; twice as many keys a block changed nothing over long contexts and cost 90 short ones of int8 15.5 -> 20 us).  Eight K/V heads of 128, two query
 // heads each: 200001 rows of bfloat16 144 us, 5.7 TB/s; four of 40000 rows of half 118 us (5.6), e4m3 66 (5.2), int8 67 (5.0); eight of 60000, e4m3, 179 (5.7).  Three workgroups a CU
 // were slower (four recordings of e4m3 60 against 54 us: fewer, fuller rounds).  A context of 106 rows is 5.1 us in a graph: a launch, and length, page numbers, keys and
-// merge one behind the other; every further block of a wavefront 1.3 us.  32 columns where that pays (paged_tile_rows): 27 rows over 16 contexts of int8 62 -> 49 us.
+// merge one behind the other; every further block of a wavefront 1.3 us.  32 columns where that pays (paged_tile_rows): 27 rows over 16 contexts of int8 62 -> 50 us.
 #include "pages.h"
 #include "tree_attn.h"
 
@@ -680,8 +680,8 @@ void launch_rows(const PagedAttnArgs& a, hipStream_t st) {
     else paged_attn_kernel<QT, PT, HD, 2><<<grid, 64 * WAVES, more, st>>>(a);
     const unsigned n = (unsigned)((int64_t)a.p.B * a.n_new * a.n_q_heads);
     const int each = a.shared ? a.n_pieces / a.p.B : a.n_pieces;             // pieces of an utterance, about
-    // 128, 256, 512 and 1024 threads, whole calls in a graph: 2 pieces of 1288 rows 16.6, 17.0, 18.4, 21.4 us; 16 of 64 50.7, 50.0, 50.2, 50.6; 64 of 16 145.8, 144.1, 143.7,
-    // 144.2; 85 of 192 22.4, 20.7, 20.4, 20.1; 235 of 8 23.3, 17.0, 14.1, 13.0
+    // 128, 256, 512 and 1024 threads, whole calls in a graph, by the pieces of a context and the query rows in all: 2 of 1288 16.6, 17.0, 18.4, 21.4 us;
+    // 16 of 64 50.7, 50.0, 50.2, 50.6; 64 of 16 145.8, 144.1, 143.7, 144.2; 85 of 192 22.4, 20.7, 20.4, 20.1; 235 of 8 23.3, 17.0, 14.1, 13.0
     if (each > 128) paged_join_kernel<QT, HD, 1024><<<n, 1024, 0, st>>>(a);
     else if (each > 32) paged_join_kernel<QT, HD, 512><<<n, 512, 0, st>>>(a);
     else if (each > 8) paged_join_kernel<QT, HD, 256><<<n, 256, 0, st>>>(a);

@@ -368,3 +368,15 @@ def test_refusals_of_the_binding():
 def test_joining_few_and_many_pieces(pair, heads, lens):
     """About 235, 70, 20 and 8 pieces a context, and one with a piece or two beside them; the first token sees one row less."""
     _check(pair, heads, lens, 128, 2)
+
+
+@pytest.mark.parametrize("pair", [("f32", "e4m3"), ("f32", "i8"), ("bf16", "i8"), ("bf16", "e4m3"), ("f32", "f32"), ("bf16", "bf16")])
+def test_large_queries(pair):
+    """Queries times a power of two and the scale divided by it: every product and sum is the same but for its exponent, and so every output is the same to the bit."""
+    heads = (8, 2, 128)
+    pool = Pool(pair[1], heads[1:], [700, 3, 64], 32)
+    q, c = _queries(pair[0], 3, 3, heads), _context(3, 3, heads, pool.table.shape[1] * 32)
+    want = c.paged_attention(q, pool.pages(), pool.table, pool.ctx_len, scale=0.0625)
+    got = c.paged_attention(q * 2.0 ** 100, pool.pages(), pool.table, pool.ctx_len, scale=0.0625 * 2.0 ** -100)
+    assert torch.equal(got, want) and c.device_flags() == 0
+    c.close()

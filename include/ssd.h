@@ -496,7 +496,7 @@ typedef struct {
  *   SSD_I8    scale = a / 127 in fp32 (at most the largest of which 127 times is finite);  code = 127 x / a to the nearest whole number, halves to even, of the exact quotient
  *   a row of zeros has scale 0; a row that is not finite has codes 0 and scale NaN, and raises SSD_FLAG_ACT_OVERFLOW
  * kv_read_pages, back: code * scale in fp32, rounded to the type of `slots`; IEEE half: clamped to +-65504 with SSD_FLAG_ACT_OVERFLOW, which NaN raises too.
- * max_rows or max_ctx 0: nothing is done.  No workspace.  Calls may be captured.  Errors: SSD_EINVAL, SSD_ESHAPE (sizes above; more than 65535 utterances), SSD_EUNSUPPORTED (types). */
+ * max_rows (0 to 2^30) or max_ctx 0: nothing is done.  No workspace.  Calls may be captured.  Errors: SSD_EINVAL, SSD_ESHAPE (sizes above; more than 65535 utterances), SSD_EUNSUPPORTED (types). */
 int kv_write_pages(ssd_ctx *ctx, const ssd_kv_view *slots /*host*/, const int32_t *start, const int32_t *n_rows, int max_rows,
                    const ssd_kv_pages *pages /*host*/, const ssd_page_table *table /*host*/);
 int kv_read_pages(ssd_ctx *ctx, const ssd_kv_pages *pages /*host*/, const ssd_page_table *table /*host*/, const ssd_kv_view *slots /*host*/,
@@ -509,10 +509,10 @@ size_t ssd_paged_workspace_bytes(const ssd_ctx *ctx, int n_q_heads, int n_kv_hea
 /* Attention of the newest n_new tokens of every utterance (their own rows written before).  Token t sees rows j < ctx_len[b] - (n_new - 1 - t); per query head h, whose
  * K/V head is h / (n_q_heads / n_kv_heads):  s_j = scale q . k_j;  lse = log sum_j exp s_j;  out = sum_j exp(s_j - lse) v_j.  A token that sees nothing has out 0 and lse -infinity.
  *   scale   any for which scale * log2(e) is finite
- *   q       dev, row b * n_new + t begins at element (b * n_new + t) * q_stride: n_q_heads * head_dim elements of q_dtype (q and q_stride multiples of 16 bytes); must not overlap out
+ *   q       dev, row b * n_new + t begins at element (b * n_new + t) * q_stride: n_q_heads * head_dim elements of q_dtype (q and q_stride multiples of 16 bytes)
  *   pages   one layer (n_layers 1): of q_dtype, or of an 8-bit type
  *   out     dev [B * n_new, n_q_heads * head_dim] of q_dtype, 16-byte aligned
- *   lse     dev [B * n_new, n_q_heads] fp32, or NULL
+ *   lse     dev [B * n_new, n_q_heads] fp32, or NULL; out and lse share no memory with each other, q or the pages
  * Scores, sums and statistics are fp32; 8-bit codes are exact operands.  A weight enters the second product as two values of 16 bits (22 bits of it with SSD_F16 pages, 16 with
  * others; three values, 24 bits, with 8-bit pages and SSD_F32 queries), with SSD_F32 pages as it is.  Outputs below 2^-90 lose bits.  With 8-bit pages q . k is formed of codes
  * before scales, and has to stay in fp32's range there: |q| up to 2^112 does.  A row that a token does not see, and what

@@ -2135,7 +2135,7 @@ int move_pages(ssd_ctx* ctx, const char* what, bool write, const ssd_kv_view* sl
         return fail(ctx, SSD_EINVAL, "%s: slots and pages differ in layers, heads or head_dim", what);
     if (page_elem(pages->dtype) != 1 && pages->dtype != slots->dtype)
         return fail(ctx, SSD_EUNSUPPORTED, "%s: pages of dtype %d with slots of dtype %d", what, pages->dtype, slots->dtype);
-    if (max_rows < 0) return fail(ctx, SSD_EINVAL, "%s: max_rows is negative", what);
+    if (max_rows < 0 || max_rows > 1 << 30) return fail(ctx, SSD_EINVAL, "%s: max_rows %d", what, max_rows);
     if (!start && !n_rows && (int64_t)table->B * max_rows > slots->slots)
         return fail(ctx, SSD_EINVAL, "%s: %d utterances of %d rows do not fit %lld slots", what, table->B, max_rows, (long long)slots->slots);
     const size_t rows = (size_t)page_row_count(*pages), bytes = rows * pages->head_dim * page_elem(pages->dtype);
@@ -2211,8 +2211,14 @@ int paged_attention(ssd_ctx* ctx, const void* q, int q_dtype, int64_t q_stride, 
     const int64_t dq = (int64_t)n_q_heads * pages->head_dim, es = (int64_t)kv_elem(q_dtype), N = (int64_t)table->B * n_new;
     if (q_stride < dq || q_stride > (int64_t)1 << 32 || q_stride * es % 16 || ((uintptr_t)q | (uintptr_t)out) & 15)
         return fail(ctx, SSD_EINVAL, "paged_attention: rows of q and out must begin at multiples of 16 bytes, q_stride be at least n_q_heads * head_dim");
-    if (overlap(Extent{(uintptr_t)q, (uintptr_t)q + (uintptr_t)(((N - 1) * q_stride + dq) * es)}, Extent{(uintptr_t)out, (uintptr_t)out + (uintptr_t)(N * dq * es)}))
-        return fail(ctx, SSD_EINVAL, "paged_attention: q and out overlap in memory");
+    auto block = [](const void* p, size_t n) { return Extent{(uintptr_t)p, (uintptr_t)p + (p ? n : 0)}; };
+    const size_t rows = (size_t)page_row_count(*pages), bytes = rows * pages->head_dim * page_elem(pages->dtype);
+    const Extent in[5] = {block(q, (size_t)(((N - 1) * q_stride + dq) * es)), block(pages->k, bytes), block(pages->v, bytes), block(pages->k_scale, rows * 4), block(pages->v_scale, rows * 4)};
+    const Extent result[2] = {block(out, (size_t)(N * dq * es)), block(lse, (size_t)(N * n_q_heads) * 4)};
+    for (const Extent& r : result)
+        for (const Extent& i : in)
+            if (overlap(r, i)) return fail(ctx, SSD_EINVAL, "paged_attention: out or lse overlap q or the pages in memory");
+    if (overlap(result[0], result[1])) return fail(ctx, SSD_EINVAL, "paged_attention: out and lse overlap in memory");
     PagedAttnArgs a;
     a.p = pages_args(ctx, *pages, *table);
     a.q = q; a.q_stride = q_stride; a.out = out; a.lse = lse;

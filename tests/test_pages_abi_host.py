@@ -104,6 +104,9 @@ def test_moves(lib, ctx):  # noqa: F811
     for p in (pages(dtype=I8, v=K), pages(dtype=I8, v=K + n - 16), pages(dtype=I8, ks=K + 16), pages(dtype=I8, vs=KS + 64)):
         assert write(p) == EINVAL
     assert lib.kv_read_pages(ctx, ref(pages(dtype=I8)), ref(table()), ref(view(v=1 << 40)), None, None, 20) == EINVAL
+    for most in ((1 << 30) + 1, (1 << 31) - 1):
+        assert lib.kv_write_pages(ctx, ref(view()), LEN, LEN, most, ref(pages(dtype=I8)), ref(table())) == EINVAL
+        assert lib.kv_read_pages(ctx, ref(pages(dtype=I8)), ref(table()), ref(view()), LEN, LEN, most) == EINVAL
     # nothing to do is not an error
     assert call(most=0) == 0 and call(t=table(max_ctx=0, entries=0)) == 0
 
@@ -157,3 +160,14 @@ def test_python_refusals():
             KvPages(*bad)
     with pytest.raises(IndexError):
         codes.layer(1)
+
+
+def test_results_share_no_memory(lib, ctx):  # noqa: F811
+    rows = 1000 * 2 * 16
+    places = {"k": (K, rows * 128), "v": (V, rows * 128), "ks": (KS, rows * 4), "vs": (VS, rows * 4), "q": (Q, 3 * 512 * 2)}
+    for name, (at, size) in places.items():
+        for near in (at, at + size - 16, at - 16):
+            for k in ({"out": near}, {"lse": near}):
+                assert attention(lib, ctx, p=pages(dtype=I8), **k) == EINVAL and b"overlap" in lib.ssd_last_error(ctx), (name, k)
+    for lse in (OUT, OUT + 3 * 512 * 2 - 16, OUT - 16):
+        assert attention(lib, ctx, p=pages(dtype=I8), lse=lse) == EINVAL and b"overlap" in lib.ssd_last_error(ctx)

@@ -32,8 +32,9 @@ template <int QT, int PT> struct Kind {
     static constexpr bool QBF = CODES ? QT != SSD_F16 : BF;                  // the first product's operands: the queries' type, which holds the codes exactly
     static constexpr int QN = CODES && QT == SSD_F32 ? 3 : 1;                // 16-bit values that a query is the exact sum of
     static constexpr int PN = QT == SSD_F32 ? 3 : 2;                         // those of a weight
-    // weights are taken times 2^BIAS: in half's upper range, or so that sums of 2^30 values at the end of fp32's range stay in it
-    static constexpr float BIAS = PT == SSD_F16 ? 15.f : -32.f;
+    // Weights are taken times a power of two: in half's upper range, or so that sums of 2^30 values at the end of fp32's range stay in it.  A factor, not a term of the
+    // exponent: there it would take five bits of the difference to the maximum.
+    static constexpr float UNIT = PT == SSD_F16 ? 0x1p15f : 0x1p-32f;
 };
 
 // Whole number in byte I of w as fp32.  (Written out because the compiler takes the bytes apart first.)
@@ -426,14 +427,13 @@ __global__ void __launch_bounds__(64 * WAVES, 2) paged_attn_kernel(PagedAttnArgs
         }
 #pragma unroll
         for (int u = 0; u < NT; ++u) {
-            const float base = T::BIAS - m[u];
 #pragma unroll
             for (int c = 0; c < TILES; ++c)
 #pragma unroll
                 for (int r = 0; r < 4; ++r) {
-                    s[u][c][r] = __builtin_amdgcn_exp2f(s[u][c][r] + base);
+                    s[u][c][r] = __builtin_amdgcn_exp2f(s[u][c][r] - m[u]);
                     l[u] += s[u][c][r];
-                    if (T::CODES) s[u][c][r] *= vs[c][r];
+                    s[u][c][r] *= T::CODES ? vs[c][r] * T::UNIT : T::UNIT;
                 }
         }
         if (masked) {
@@ -560,7 +560,7 @@ __global__ void __launch_bounds__(64 * WAVES, 2) paged_attn_kernel(PagedAttnArgs
         }
         l[u] += __shfl_xor(l[u], 16);
         l[u] += __shfl_xor(l[u], 32);
-        const float inv = l[u] == 0.f ? 0.f : 1.f / l[u];
+        const float inv = l[u] == 0.f ? 0.f : 1.f / (T::UNIT * l[u]);
         if (g == 0) ml_s[wave][dc] = make_float2(m[u], l[u]);
 #pragma unroll
         for (int i = 0; i < DT; i += 4)
@@ -590,11 +590,11 @@ __global__ void __launch_bounds__(64 * WAVES, 2) paged_attn_kernel(PagedAttnArgs
             const int64_t at = ((int64_t)b * a.n_new + n / a.group) * a.n_q_heads + kvh * a.group + n % a.group;
             if (only) {
                 store4<QT>((typename E::type*)a.out + at * hd + dim, v);
-                if (a.lse && dim == 0) a.lse[at] = lt == 0.f ? -INFINITY : (mt - T::BIAS + __builtin_amdgcn_logf(lt)) * LN2;
+                if (a.lse && dim == 0) a.lse[at] = lt == 0.f ? -INFINITY : (mt + __builtin_amdgcn_logf(lt)) * LN2;
             } else {
                 const int64_t to_at = ((int64_t)t.index * p.n_kv_heads + kvh) * rows + n;
                 *reinterpret_cast<f32x4_t*>(a.part_o + to_at * HD + dim) = v;
-                if (dim == 0) a.part_ml[to_at] = make_float2(mt - T::BIAS, lt);
+                if (dim == 0) a.part_ml[to_at] = make_float2(mt, lt);
             }
         }
     }

@@ -124,7 +124,8 @@ const char *ssd_last_error(const ssd_ctx *ctx);
  *                           rounds to it (RMSNorm output, rotated q / k and v, SiLU(gate)*up, K/V-cache rows, the projector's values) and
  *                           was stored saturated to +-65504, or a log-likelihood came out non-finite.  Results of
  *                           calls since the last read are then not the model's: re-run in fp32 or rescale.
- *                           kv_write_pages: a row that is not finite; kv_read_pages: a value beyond IEEE half, or of such a row
+ *                           kv_write_pages: a row that is not finite; kv_read_pages: a value beyond IEEE half, or of such a row;
+ *                           paged_attention: an output of IEEE half over 8-bit pages that is beyond it, or not finite
  *   SSD_FLAG_BAD_PAGE       calls on pages: a page number, length or slot in device memory was out of range; what it concerns was left out
  * A context without a model has the flags of the calls on pages only (none if it was created while its stream was captured). */
 enum ssd_device_flag { SSD_FLAG_TOKEN_CLAMPED = 1, SSD_FLAG_ACT_OVERFLOW = 2, SSD_FLAG_BAD_PAGE = 4 };
@@ -517,6 +518,7 @@ size_t ssd_paged_workspace_bytes(const ssd_ctx *ctx, int n_q_heads, int n_kv_hea
  * others; three values, 24 bits, with 8-bit pages and SSD_F32 queries), with SSD_F32 pages as it is.  Outputs below 2^-90 lose bits.  With 8-bit pages q . k is formed of codes
  * before scales, and has to stay in fp32's range there: |q| up to 2^112 does.  A row that a token does not see, and what
  * lies behind the last row of a page, has no influence on it, whatever it holds; a value that it sees and that is not finite makes its column infinite or NaN.
+ * SSD_F16 queries over 8-bit pages: a finite output that rounds beyond half is stored as +-65504 and raises SSD_FLAG_ACT_OVERFLOW, which one that is not finite raises too.
  * Captured calls use the workspace of the time of capture: two that share one must not run at the same time.  Every call repeats to the bit.
  * Errors: SSD_EINVAL, SSD_ESHAPE (B times tiles of 16 query rows of a K/V head more than 65535; more than 512 query heads a K/V
  * head, or 2^21 query heads of tokens), SSD_EUNSUPPORTED, SSD_EWORKSPACE. */

@@ -2223,6 +2223,7 @@ int paged_attention(ssd_ctx* ctx, const void* q, int q_dtype, int64_t q_stride, 
     a.p = pages_args(ctx, *pages, *table);
     a.q = q; a.q_stride = q_stride; a.out = out; a.lse = lse;
     a.n_q_heads = n_q_heads; a.group = group; a.n_new = n_new; a.scale = scale;
+    a.codes = page_elem(pages->dtype) == 1;
     a.tile_rows = paged_tile_rows((int64_t)n_new * group, table->B, pages->n_kv_heads, table->max_ctx, pages->head_dim, q_dtype, pages->dtype);
     a.tiles = (n_new * group + a.tile_rows - 1) / a.tile_rows;
     const PagedPlan plan = plan_paged(table->B, pages->n_kv_heads, (int64_t)n_new * group, a.tile_rows, pages->head_dim, table->max_ctx);

@@ -24,6 +24,7 @@ namespace ssd {
 namespace {
 
 constexpr int WAVES = KEY_WAVES;
+constexpr float F16_END = 65520.f;                           // what rounds to half's largest value or less is smaller
 
 template <int QT, int PT> struct Kind {
     static constexpr bool CODES = PT == SSD_E4M3 || PT == SSD_I8, F32 = PT == SSD_F32, BF = PT != SSD_F16;
@@ -119,11 +120,23 @@ template <int HD> struct Queries<SSD_F32, SSD_F32, HD> {
 
 __device__ __forceinline__ f32x4_t mfma_f32(float a, float b, const f32x4_t& c) { return __builtin_amdgcn_mfma_f32_16x16x4f32(a, b, c, 0, 0, 0); }
 
-// Four values of a result, one store.
+// Four values of a result, one store.  Means of 8-bit pages may lie beyond half's range, those of half pages do not.
 template <int QT>
-__device__ __forceinline__ void store4(typename Elem<QT>::type* out, const f32x4_t& v) {
+__device__ __forceinline__ void store4(typename Elem<QT>::type* out, f32x4_t v, bool codes, int32_t* flags) {
     if constexpr (QT == SSD_F32) *reinterpret_cast<f32x4_t*>(out) = v;
-    else *reinterpret_cast<uint2*>(out) = make_uint2(pack16<QT == SSD_BF16>(v[0], v[1]), pack16<QT == SSD_BF16>(v[2], v[3]));
+    else {
+        if (QT == SSD_F16 && codes) {
+            bool over = false;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) over |= !(fabsf(v[e]) < F16_END);
+            if (over) {
+                raise_flag(flags, SSD_FLAG_ACT_OVERFLOW);
+#pragma unroll
+                for (int e = 0; e < 4; ++e) v[e] = fabsf(v[e]) <= F32_MOST ? fminf(fmaxf(v[e], -F16_MAX), F16_MAX) : v[e];
+            }
+        }
+        *reinterpret_cast<uint2*>(out) = make_uint2(pack16<QT == SSD_BF16>(v[0], v[1]), pack16<QT == SSD_BF16>(v[2], v[3]));
+    }
 }
 
 // What a workgroup does: piece `part` of n of utterance b, rows from ..; index: the piece's number among all.
@@ -589,7 +602,7 @@ __global__ void __launch_bounds__(64 * WAVES, 2) paged_attn_kernel(PagedAttnArgs
             for (int w = 0; w < WAVES; ++w) v += *reinterpret_cast<const f32x4_t*>(&o_s[w][r][dim]) * (share[w] * one);
             const int64_t at = ((int64_t)b * a.n_new + n / a.group) * a.n_q_heads + kvh * a.group + n % a.group;
             if (only) {
-                store4<QT>((typename E::type*)a.out + at * hd + dim, v);
+                store4<QT>((typename E::type*)a.out + at * hd + dim, v, T::CODES, p.flags);
                 if (a.lse && dim == 0) a.lse[at] = lt == 0.f ? -INFINITY : (mt + __builtin_amdgcn_logf(lt)) * LN2;
             } else {
                 const int64_t to_at = ((int64_t)t.index * p.n_kv_heads + kvh) * rows + n;
@@ -666,7 +679,7 @@ __global__ void __launch_bounds__(THREADS) paged_join_kernel(PagedAttnArgs a) {
     f32x4_t s = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
     for (int i = 0; i < JOIN_WAVES; ++i) s += o_s[i][dim / 4] * (f[i] * inv);
-    store4<QT>((typename E::type*)a.out + at * a.p.head_dim + dim, s);
+    store4<QT>((typename E::type*)a.out + at * a.p.head_dim + dim, s, a.codes, a.p.flags);
     if (a.lse && dim == 0) a.lse[at] = lt == 0.f ? -INFINITY : (mt + __builtin_amdgcn_logf(lt)) * LN2;
 }
 

@@ -42,6 +42,7 @@ struct PagedAttnArgs {
     void* out; float* lse;
     int32_t n_q_heads, group, n_new;         // group: query heads of a K/V head
     float scale;
+    bool codes;                              // pages of an 8-bit type
     int32_t tile_rows, tiles;                // query rows of a K/V head, tokens times group, in tiles of 16 or 32
     // Contexts are cut into pieces of whole PAGED_UNITs of rows: shared 0, each by itself every PAGED_MOST units, n_pieces of max_ctx rows; else all of a K/V head
     // and tile into about `shared` equal ones (or the smallest multiple of it that has none longer than PAGED_MOST), at most n_pieces.

@@ -96,3 +96,51 @@ def test_log_sum_exp_of_a_row_or_two(pair, n):
             s, d = _dot(q, pool, b, h, 3)
             want = np.log(np.exp(s).sum())
             assert abs(got[b, 0, h] - want) <= d + 2.0 ** -22 * abs(want) + (n - 1) * 2.0 ** -22, (b, h)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("kind", ["e4m3", "i8"])
+@pytest.mark.parametrize("n, n_new", [(40, 1), (40, 9), (5000, 2)])
+def test_half_outputs_beyond_half(kind, n, n_new):
+    """Means of values beyond half are stored as its largest ones, and the flag says so; where only the values are beyond it nothing is clamped or raised.  A wavefront adds at most 64 times 32 products, each off by
+    2^-24, of weights off by 2^-17: 1.3e-4 of a value, less than what lies between 65504 or 65508 and where half's rounding goes elsewhere."""
+    heads = (4, 2, 64)
+    pool, q = Pool(kind, heads[1:], [n], 16), _queries("f16", 1, n_new, heads)
+    c = _context(1, n_new, heads, n + 16)
+    v, scale = pool.parts["v"].view(torch.uint8), pool.parts["v_scale"]
+    one = torch.tensor([1.0]).to(pool.parts["v"].dtype).view(torch.uint8).item()
+    run = lambda: c.paged_attention(q, pool.pages(), pool.table, pool.ctx_len)
+
+    def fill(x):
+        v.fill_(one)
+        scale.copy_(torch.where(scale.isnan(), scale, x))
+
+    fill(65504.0)
+    c.device_flags()
+    assert (run() == 65504).all() and c.device_flags() == 0
+    fill(-65508.0)
+    assert (run() == -65504).all() and c.device_flags() == 0
+    fill(70000.0)
+    assert (run() == 65504).all() and c.device_flags() == 2
+    fill(-1e30)
+    assert (run() == -65504).all() and c.device_flags() == 2
+    fill(float("inf"))
+    assert not torch.isfinite(run()).any() and c.device_flags() == 2
+    fill(1e5)                                                # every other row of the other sign, the queries too small to tell them apart
+    _in_pairs(pool)
+    q.mul_(1e-4)
+    out = run()
+    assert torch.isfinite(out).all() and (out.abs() < 65504).all() and c.device_flags() == 0
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("n", [40, 5000])
+def test_infinities_of_half_pages_stay(n):
+    heads = (4, 2, 64)
+    pool, q = Pool("f16", heads[1:], [n], 16), _queries("f16", 1, 1, heads)
+    pool.parts["v"].fill_(65504.0)
+    c = _context(1, 1, heads, n + 16)
+    c.device_flags()
+    assert (c.paged_attention(q, pool.pages(), pool.table, pool.ctx_len) == 65504).all()
+    pool.parts["v"].fill_(float("inf"))
+    assert not torch.isfinite(c.paged_attention(q, pool.pages(), pool.table, pool.ctx_len)).any() and c.device_flags() == 0

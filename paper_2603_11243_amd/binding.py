@@ -274,7 +274,7 @@ class Context:
         self._lib = lib()
         self.device = torch.device(device)
         self.cfg = model_cfg
-        self._keep = []               # tensors whose storage the library reads in place
+        self._keep = []               # tensors whose storage the library reads in place, and workspaces of the time before
         self._ws = None
         self._h = C.c_void_p()
         torch.cuda.set_device(self.device)
@@ -336,7 +336,8 @@ class Context:
         """Allocates (through torch) and hands over a workspace big enough for the given maxima.  tree_nodes, tree_utts: tree_path, with
         tree_heads (query heads, K/V heads, head_dim) tree_attention, and for a context with a model verify_tree and accept_tree;
         evict_rows (kept by all utterances), evict_utts and evict_heads (layers, K/V heads): kv_evict.  paged_utts, paged_new (tokens of an utterance),
-        paged_ctx (longest context) and paged_heads (query heads, K/V heads, head_dim): paged_attention."""
+        paged_ctx (longest context) and paged_heads (query heads, K/V heads, head_dim): paged_attention.  A workspace that is too small is replaced by one
+        at least a quarter larger and kept as long as this object: calls that were captured, or still run on the context's stream, use it."""
         n = self.workspace_bytes(max_frames, max_tokens, max_verify_rows, max_utts)
         if ar_utts and ar_steps:
             n = max(n, int(self._lib.ssd_ar_workspace_bytes(self._h, ar_utts, ar_steps)))
@@ -348,10 +349,14 @@ class Context:
         if paged_utts:
             n = max(n, int(self._lib.ssd_paged_workspace_bytes(self._h, *paged_heads, paged_utts, paged_new, paged_ctx)))
         if self._ws is None or self._ws.numel() < n:
-            self._ws = torch.empty(n, dtype=torch.uint8, device=self.device)
-            self._check(self._lib.ssd_set_workspace(self._h, _ptr(self._ws), n))
+            if self._ws is not None:
+                n = max(n, self._ws.numel() * 5 // 4)        # (all that are kept: five times the last at most)
+            self.set_workspace(torch.empty(n, dtype=torch.uint8, device=self.device))
 
     def set_workspace(self, buf: Optional[torch.Tensor]):
+        """buf is used from here on; the one before is kept as `reserve` says."""
+        if self._ws is not None and self._ws is not buf:
+            self._keep.append(self._ws)
         self._ws = buf
         self._check(self._lib.ssd_set_workspace(self._h, _ptr(buf), 0 if buf is None else buf.numel()))
 

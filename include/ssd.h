@@ -127,7 +127,8 @@ const char *ssd_last_error(const ssd_ctx *ctx);
  *                           kv_write_pages: a row that is not finite; kv_read_pages: a value beyond IEEE half, or of such a row;
  *                           paged_attention: an output of IEEE half over 8-bit pages that is beyond it, or not finite
  *   SSD_FLAG_BAD_PAGE       calls on pages: a page number, length or slot in device memory was out of range; what it concerns was left out
- * A context without a model has the flags of the calls on pages only (none if it was created while its stream was captured). */
+ * While the stream is captured the call is refused (SSD_EHIP) and the capture goes on.  A context without a model has the flags of the calls on pages only: before the
+ * first of them the call returns 0 at once, also under capture (none if it was created while its stream was captured). */
 enum ssd_device_flag { SSD_FLAG_TOKEN_CLAMPED = 1, SSD_FLAG_ACT_OVERFLOW = 2, SSD_FLAG_BAD_PAGE = 4 };
 int ssd_device_flags(ssd_ctx *ctx, int32_t *flags /*host*/);
 

@@ -366,7 +366,8 @@ class Context:
 
     def device_flags(self) -> int:
         """Sticky flags raised by kernels since the last call (waits for the stream); 1 = a token id was clamped,
-        2 = an activation left the half range and was stored saturated (or a log-likelihood was not finite)."""
+        2 = an activation left the half range and was stored saturated (or a log-likelihood was not finite), 4 = a page number,
+        length or slot was out of range and left out.  Refused while the stream is captured."""
         f = C.c_int32(0)
         self._check(self._lib.ssd_device_flags(self._h, C.byref(f)))
         return int(f.value)

@@ -100,6 +100,7 @@ struct ssd_ctx {
     unsigned* gate_arrived = nullptr;        // rows done per utterance, all zero between calls (launch_gate_fused)
     int32_t* dev_flags = nullptr;            // sticky data-dependent conditions seen by kernels (ssd_device_flags)
     int32_t* page_flags = nullptr;           // the same, or those of the calls on pages of a context without a model
+    bool flags_used = false;                 // a call was made that may raise one of page_flags
     void* ws = nullptr;
     size_t ws_bytes = 0;
     uint16_t* head_w = nullptr;              // CTC output layer, padded with zero rows (bias -inf there)
@@ -502,7 +503,8 @@ size_t ssd_workspace_bytes(const ssd_ctx* ctx, int64_t max_frames, int64_t max_t
 int ssd_device_flags(ssd_ctx* ctx, int32_t* flags) {
     if (!ctx || !flags) return SSD_EINVAL;
     *flags = 0;
-    if (!ctx->page_flags) return SSD_OK;
+    if (!ctx->page_flags || (!ctx->has_model && !ctx->flags_used)) return SSD_OK;
+    if (capturing(ctx->stream)) return fail(ctx, SSD_EHIP, "ssd_device_flags: the stream is being captured");
     HIP_TRY(ctx, hipMemcpyAsync(flags, ctx->page_flags, 4, hipMemcpyDeviceToHost, ctx->stream));
     HIP_TRY(ctx, hipStreamSynchronize(ctx->stream));
     if (*flags) HIP_TRY(ctx, hipMemsetAsync(ctx->page_flags, 0, 4, ctx->stream));
@@ -2159,6 +2161,7 @@ int move_pages(ssd_ctx* ctx, const char* what, bool write, const ssd_kv_view* sl
     a.k = slots->k; a.v = slots->v; a.slots = slots->slots;
     a.slot_stride = slots->slot_stride; a.head_stride = slots->head_stride; a.layer_stride = slots->n_layers > 1 ? slots->layer_stride : 0;
     a.start = start; a.n_rows = n_rows; a.max_rows = max_rows; a.n_layers = slots->n_layers;
+    ctx->flags_used = true;
     {
         ProfScope ps(ctx, SSD_PROF_OTHER);
         if (write) launch_write_pages(a, slots->dtype, pages->dtype, ctx->stream);
@@ -2234,6 +2237,7 @@ int paged_attention(ssd_ctx* ctx, const void* q, int q_dtype, int64_t q_stride, 
     a.part_o = reinterpret_cast<float*>(ws);
     a.part_ml = reinterpret_cast<float2*>(ws + plan.ml);
     a.first = reinterpret_cast<int2*>(ws + plan.first);
+    ctx->flags_used = true;
     {
         ProfScope ps(ctx, SSD_PROF_ATTN);
         launch_paged_attention(a, q_dtype, pages->dtype, ctx->stream);

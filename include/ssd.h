@@ -128,7 +128,7 @@ const char *ssd_last_error(const ssd_ctx *ctx);
  *                           paged_attention: an output of IEEE half over 8-bit pages that is beyond it, or not finite
  *   SSD_FLAG_BAD_PAGE       calls on pages: a page number, length or slot in device memory was out of range; what it concerns was left out
  * While the stream is captured the call is refused (SSD_EHIP) and the capture goes on.  A context without a model has the flags of the calls on pages only: before the
- * first of them the call returns 0 at once, also under capture (none if it was created while its stream was captured). */
+ * first of them the call returns 0 at once, also under capture. */
 enum ssd_device_flag { SSD_FLAG_TOKEN_CLAMPED = 1, SSD_FLAG_ACT_OVERFLOW = 2, SSD_FLAG_BAD_PAGE = 4 };
 int ssd_device_flags(ssd_ctx *ctx, int32_t *flags /*host*/);
 
@@ -498,7 +498,8 @@ typedef struct {
  *   SSD_I8    scale = a / 127 in fp32 (at most the largest of which 127 times is finite);  code = 127 x / a to the nearest whole number, halves to even, of the exact quotient
  *   a row of zeros has scale 0; a row that is not finite has codes 0 and scale NaN, and raises SSD_FLAG_ACT_OVERFLOW
  * kv_read_pages, back: code * scale in fp32, rounded to the type of `slots`; IEEE half: clamped to +-65504 with SSD_FLAG_ACT_OVERFLOW, which NaN raises too.
- * max_rows (0 to 2^30) or max_ctx 0: nothing is done.  No workspace.  Calls may be captured.  Errors: SSD_EINVAL, SSD_ESHAPE (sizes above; more than 65535 utterances), SSD_EUNSUPPORTED (types). */
+ * max_rows (0 to 2^30) or max_ctx 0: nothing is done.  No workspace.  Calls may be captured.  Errors of these and of paged_attention: SSD_EHIP if ssd_create
+ * found no device memory for the flags; SSD_EINVAL, SSD_ESHAPE (sizes above; more than 65535 utterances), SSD_EUNSUPPORTED (types). */
 int kv_write_pages(ssd_ctx *ctx, const ssd_kv_view *slots /*host*/, const int32_t *start, const int32_t *n_rows, int max_rows,
                    const ssd_kv_pages *pages /*host*/, const ssd_page_table *table /*host*/);
 int kv_read_pages(ssd_ctx *ctx, const ssd_kv_pages *pages /*host*/, const ssd_page_table *table /*host*/, const ssd_kv_view *slots /*host*/,

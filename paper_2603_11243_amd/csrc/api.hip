@@ -320,15 +320,31 @@ void alloc_gate_counters(ssd_ctx* c) {
     hipStreamCaptureMode mode = hipStreamCaptureModeRelaxed;       // captures of other streams go on
     (void)hipThreadExchangeStreamCaptureMode(&mode);
     void* p = nullptr;
-    const size_t bytes = GATE_ARRIVED_BYTES + 256;                 // and the flags
-    if (hipMalloc(&p, bytes) == hipSuccess && hipMemsetAsync(p, 0, bytes, c->stream) == hipSuccess) {
+    if (hipMalloc(&p, GATE_ARRIVED_BYTES) == hipSuccess && hipMemsetAsync(p, 0, GATE_ARRIVED_BYTES, c->stream) == hipSuccess) {
         c->owned.push_back(p);
         c->gate_arrived = static_cast<unsigned*>(p);
-        if (!c->page_flags) c->page_flags = reinterpret_cast<int32_t*>(static_cast<char*>(p) + GATE_ARRIVED_BYTES);
     } else {
         if (p) (void)hipFree(p);
         (void)hipGetLastError();
     }
+    (void)hipThreadExchangeStreamCaptureMode(&mode);
+}
+// Flags of a context without a model, which may never need them: the calls on pages refuse to run without.  Cleared on a stream of their own, since the context's
+// may be under capture.
+void alloc_page_flags(ssd_ctx* c) {
+    hipStreamCaptureMode mode = hipStreamCaptureModeRelaxed;
+    (void)hipThreadExchangeStreamCaptureMode(&mode);
+    void* p = nullptr;
+    hipStream_t own = nullptr;
+    if (hipMalloc(&p, 256) == hipSuccess && hipStreamCreateWithFlags(&own, hipStreamNonBlocking) == hipSuccess && hipMemsetAsync(p, 0, 256, own) == hipSuccess &&
+        hipStreamSynchronize(own) == hipSuccess) {
+        c->owned.push_back(p);
+        c->page_flags = static_cast<int32_t*>(p);
+    } else {
+        if (p) (void)hipFree(p);
+        (void)hipGetLastError();
+    }
+    if (own) (void)hipStreamDestroy(own);
     (void)hipThreadExchangeStreamCaptureMode(&mode);
 }
 
@@ -347,6 +363,7 @@ int ssd_create(ssd_ctx** out, const ssd_model_cfg* cfg, const ssd_weights* w, vo
     if (hipGetDevice(&c->device) != hipSuccess) { c->device = -1; (void)hipGetLastError(); }
     if (!cfg) {
         alloc_gate_counters(c);
+        alloc_page_flags(c);
         *out = c;
         return SSD_OK;
     }
@@ -503,7 +520,7 @@ size_t ssd_workspace_bytes(const ssd_ctx* ctx, int64_t max_frames, int64_t max_t
 int ssd_device_flags(ssd_ctx* ctx, int32_t* flags) {
     if (!ctx || !flags) return SSD_EINVAL;
     *flags = 0;
-    if (!ctx->page_flags || (!ctx->has_model && !ctx->flags_used)) return SSD_OK;
+    if (!ctx->has_model && !ctx->flags_used) return SSD_OK;
     if (capturing(ctx->stream)) return fail(ctx, SSD_EHIP, "ssd_device_flags: the stream is being captured");
     HIP_TRY(ctx, hipMemcpyAsync(flags, ctx->page_flags, 4, hipMemcpyDeviceToHost, ctx->stream));
     HIP_TRY(ctx, hipStreamSynchronize(ctx->stream));
@@ -2086,6 +2103,13 @@ int check_pages(ssd_ctx* c, const char* what, const ssd_kv_pages* p, const ssd_p
     return SSD_OK;
 }
 
+// Rows that are left out without a word would be wrong results.
+int use_flags(ssd_ctx* c, const char* what) {
+    if (!c->page_flags) return fail(c, SSD_EHIP, "%s: there was no device memory for the flags when the context was created", what);
+    c->flags_used = true;
+    return SSD_OK;
+}
+
 PagesArgs pages_args(const ssd_ctx* c, const ssd_kv_pages& p, const ssd_page_table& t) {
     PagesArgs a;
     a.k = p.k; a.v = p.v; a.k_scale = p.k_scale; a.v_scale = p.v_scale;
@@ -2156,12 +2180,12 @@ int move_pages(ssd_ctx* ctx, const char* what, bool write, const ssd_kv_view* sl
         return fail(ctx, SSD_EINVAL, "%s: keys and values of the slots share memory", what);
     }
     if (!max_rows || !table->max_ctx) return SSD_OK;
+    if ((rc = use_flags(ctx, what)) != SSD_OK) return rc;
     MoveArgs a;
     a.p = pages_args(ctx, *pages, *table);
     a.k = slots->k; a.v = slots->v; a.slots = slots->slots;
     a.slot_stride = slots->slot_stride; a.head_stride = slots->head_stride; a.layer_stride = slots->n_layers > 1 ? slots->layer_stride : 0;
     a.start = start; a.n_rows = n_rows; a.max_rows = max_rows; a.n_layers = slots->n_layers;
-    ctx->flags_used = true;
     {
         ProfScope ps(ctx, SSD_PROF_OTHER);
         if (write) launch_write_pages(a, slots->dtype, pages->dtype, ctx->stream);
@@ -2232,12 +2256,12 @@ int paged_attention(ssd_ctx* ctx, const void* q, int q_dtype, int64_t q_stride, 
     const PagedPlan plan = plan_paged(table->B, pages->n_kv_heads, (int64_t)n_new * group, a.tile_rows, pages->head_dim, table->max_ctx);
     if (plan.total && (!ctx->ws || ctx->ws_bytes < plan.total))
         return fail(ctx, SSD_EWORKSPACE, "paged_attention: workspace of %zu bytes needed, %zu set", plan.total, ctx->ws_bytes);
+    if (const int no = use_flags(ctx, "paged_attention")) return no;
     a.shared = plan.shared; a.n_pieces = plan.n_pieces;
     char* ws = static_cast<char*>(ctx->ws);
     a.part_o = reinterpret_cast<float*>(ws);
     a.part_ml = reinterpret_cast<float2*>(ws + plan.ml);
     a.first = reinterpret_cast<int2*>(ws + plan.first);
-    ctx->flags_used = true;
     {
         ProfScope ps(ctx, SSD_PROF_ATTN);
         launch_paged_attention(a, q_dtype, pages->dtype, ctx->stream);

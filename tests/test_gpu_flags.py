@@ -55,3 +55,25 @@ def test_flags_are_refused_while_the_stream_is_captured(model):
             side.synchronize()
             assert (x == 2 * i + 2).all() and c.device_flags() == 4 and c.device_flags() == 0
     c.close()
+
+
+@pytest.mark.parametrize("call", ["write", "read", "attention"])
+def test_a_context_made_under_capture_has_flags(call):
+    side = torch.cuda.Stream()
+    with torch.cuda.stream(side):
+        pool, args = _move()
+        q, out = (torch.randn(1, 4, 64, device="cuda").half() for _ in range(2))
+        graph = torch.cuda.CUDAGraph()
+        side.synchronize()
+        with torch.cuda.graph(graph, stream=side):
+            c = Context(device="cuda:0", stream=side)
+            if call == "attention":
+                c.paged_attention(q, *args[:3], out=out)
+            else:
+                (c.kv_write_pages if call == "write" else c.kv_read_pages)(*args)
+        table = pool.table.clone()
+        for bad in (0, 4, 0, 4):
+            pool.table.copy_(table if not bad else torch.full_like(table, -1))
+            graph.replay()
+            assert c.device_flags() == bad
+        c.close()

@@ -171,3 +171,14 @@ def test_results_share_no_memory(lib, ctx):  # noqa: F811
                 assert attention(lib, ctx, p=pages(dtype=I8), **k) == EINVAL and b"overlap" in lib.ssd_last_error(ctx), (name, k)
     for lse in (OUT, OUT + 3 * 512 * 2 - 16, OUT - 16):
         assert attention(lib, ctx, p=pages(dtype=I8), lse=lse) == EINVAL and b"overlap" in lib.ssd_last_error(ctx)
+
+
+def test_no_call_without_flags(lib, ctx):  # noqa: F811
+    """Without a GPU a context has none: nothing is launched, and the call says why."""
+    import torch
+    if torch.cuda.is_available():
+        pytest.skip("this context has flags")
+    assert attention(lib, ctx) == -4 and b"flags" in lib.ssd_last_error(ctx)
+    assert both(lib, ctx) == -4 and b"flags" in lib.ssd_last_error(ctx)
+    flags = C.c_int32(7)
+    assert lib.ssd_device_flags(ctx, C.byref(flags)) == 0 and flags.value == 0

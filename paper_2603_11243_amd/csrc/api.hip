@@ -2128,16 +2128,16 @@ PagesArgs pages_args(const ssd_ctx* c, const ssd_kv_pages& p, const ssd_page_tab
 size_t paged_ml(int64_t rows, int dims) { return align_up((size_t)(rows * dims) * 4); }
 size_t paged_first(int64_t rows, int dims) { return paged_ml(rows, dims) + align_up((size_t)rows * sizeof(float2)); }
 size_t paged_bytes(int64_t rows, int dims, int64_t B) { return paged_first(rows, dims) + align_up((size_t)B * sizeof(int2)); }
+bool paged_shares(int64_t B, int64_t most) { return B <= PAGED_UTTS && B * most <= 1 << 28; }      // (the device counts units in 32 bits)
 struct PagedPlan { int shared, n_pieces; size_t ml, first, total; };
 PagedPlan plan_paged(int64_t B, int64_t n_kv_heads, int64_t rows, int tile_rows, int head_dim, int64_t max_ctx) {
     const int64_t tiles = (rows + tile_rows - 1) / tile_rows, most = (max_ctx + PAGED_UNIT - 1) / PAGED_UNIT, pairs = n_kv_heads * tiles;
     PagedPlan p = {0, 1, 0, 0, 0};
     if (most > paged_whole(pairs * B)) {
-        if (B <= PAGED_UTTS && B * most <= 1 << 28) {        // (a workgroup a piece: fewer than 2^24 along one dimension of a launch)
+        if (paged_shares(B, most)) {
             const int64_t at_once = std::max<int64_t>(1, PAGED_CUS * paged_per_cu(head_dim, tile_rows) / pairs);
             p.shared = (int)(at_once * ((PAGED_EACH * B + at_once - 1) / at_once));
-            const int64_t rounds = std::max<int64_t>(1, (B * most + (int64_t)p.shared * PAGED_MOST - 1) / ((int64_t)p.shared * PAGED_MOST));
-            p.n_pieces = (int)std::min<int64_t>(p.shared * rounds + B, B * most);
+            p.n_pieces = (int)std::min<int64_t>(p.shared + B, B * most);
         } else {
             p.n_pieces = (int)((most + PAGED_MOST - 1) / PAGED_MOST);
         }
@@ -2213,8 +2213,9 @@ size_t ssd_paged_workspace_bytes(const ssd_ctx* ctx, int n_q_heads, int n_kv_hea
     if (!ctx || n_q_heads <= 0 || n_kv_heads <= 0 || head_dim <= 0 || B < 0 || n_new < 0 || max_ctx < 0) return 0;
     if (n_q_heads > 65535 || B > 65535 || max_ctx > 1 << 30 || B * n_new > PAGED_QUERIES || B * n_new * n_q_heads > PAGED_QUERIES) return 0;      // (no call is so large)
     const int64_t most = (max_ctx + PAGED_UNIT - 1) / PAGED_UNIT, rows = (int64_t)n_new * n_q_heads;
-    // (as many workgroups as run at once, four a CU at most, with 32 rows each, or more pieces: see plan_paged)
-    return paged_bytes(4 * PAGED_CUS * 32 + (B * most / PAGED_MOST + (PAGED_EACH + 1) * B + 2) * rows, paged_dims(head_dim), B) + 256;
+    // as many workgroups as run at once, four a CU at most, with 32 rows each, and pieces by the utterances; of contexts cut each by itself also by their length (plan_paged)
+    const int64_t by_length = paged_shares(B, most) ? 0 : B * most / PAGED_MOST;
+    return paged_bytes(4 * PAGED_CUS * 32 + (by_length + (PAGED_EACH + 1) * B + 2) * rows, paged_dims(head_dim), B) + 256;
 }
 
 int paged_attention(ssd_ctx* ctx, const void* q, int q_dtype, int64_t q_stride, int n_q_heads, int n_new, const ssd_kv_pages* pages, const ssd_page_table* table,

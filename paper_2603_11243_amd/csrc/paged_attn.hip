@@ -145,14 +145,8 @@ struct Piece { int b, part, n, index, len, given, from, rows; };
 __device__ __forceinline__ int units(int rows) { return (rows + PAGED_UNIT - 1) / PAGED_UNIT; }
 __device__ __forceinline__ int clamped(const PagesArgs& p, int len) { return min(max(len, 0), p.max_ctx); }
 
-// Shared pieces for so many units in all; units of one.
-__device__ __forceinline__ int shared_pieces(const PagedAttnArgs& a, int total) {
-    const uint32_t whole = (uint32_t)a.shared * PAGED_MOST;
-    return a.shared * (int)max(1u, ((uint32_t)total + whole - 1) / whole);
-}
-__device__ __forceinline__ int shared_units(const PagedAttnArgs& a, int total, int pieces) {
-    return max(1, (int)(((uint32_t)total + pieces - 1) / (uint32_t)pieces));
-}
+// Units of a shared piece for so many in all.
+__device__ __forceinline__ int shared_units(const PagedAttnArgs& a, int total) { return max(1, (int)(((uint32_t)total + a.shared - 1) / (uint32_t)a.shared)); }
 
 struct OpAdd { __device__ __forceinline__ int operator()(int x, int y) const { return x + y; } };
 __device__ __forceinline__ int lanes_sum(int v) { return group_allreduce_i<64>(v, OpAdd()); }
@@ -183,15 +177,14 @@ __device__ __forceinline__ bool find_piece(const PagedAttnArgs& a, Piece& t) {
         if (a.n_pieces > 1 && x >= t.n) return false;
     } else if (p.B <= 64) {
         const int given = lane < p.B ? p.ctx_len[lane] : 0, len = clamped(p, given), u = units(len);
-        const int total = lanes_sum(u);
-        const int wanted = shared_pieces(a, total), want = max(wanted, p.B);
-        int share = shared_units(a, total, wanted), n, pieces;
+        const int want = max(a.shared, p.B);
+        int share = shared_units(a, lanes_sum(u)), n, pieces;
         // every utterance's last piece is a shorter one: so many more than wanted, and a second round of workgroups for them, until pieces are a little longer
         for (int turn = 0;; ++turn) {
             n = lane < p.B ? max(1, (int)((uint32_t)(u + share - 1) / (uint32_t)share)) : 0;
             pieces = lanes_sum(n);
-            if (pieces <= want || share == PAGED_MOST || turn == 8) break;
-            share = min(PAGED_MOST, max(share + 1, (int)((float)share * (float)pieces / (float)want)));
+            if (pieces <= want || turn == 8) break;
+            share = max(share + 1, (int)((float)share * (float)pieces / (float)want));
         }
         const int sum = lanes_scan(n);
         const uint64_t behind = __ballot(sum > x);
@@ -218,7 +211,7 @@ __device__ __forceinline__ bool find_piece(const PagedAttnArgs& a, Piece& t) {
         int total = 0;
 #pragma unroll
         for (int w = 0; w < WAVES; ++w) total += wave_s[w];
-        const int share = shared_units(a, total, shared_pieces(a, total));
+        const int share = shared_units(a, total);
         int n[PER], mine = 0;
 #pragma unroll
         for (int e = 0; e < PER; ++e) mine += n[e] = tid * PER + e < p.B ? max(1, (int)((uint32_t)(units(clamped(p, given[e])) + share - 1) / (uint32_t)share)) : 0;
@@ -260,7 +253,7 @@ __global__ void __launch_bounds__(64 * WAVES, 2) paged_attn_kernel(PagedAttnArgs
     typedef Kind<QT, PT> T;
     typedef Elem<QT> E;
     constexpr int KEYS = T::KEYS, TILES = T::TILES, DPL = HD / 16, DT = HD / 16, STEP = KEYS * WAVES, PITCH = HD + 4;
-    constexpr int K_LOADS = HD * T::SIZE / 64, V_WORDS = DPL * T::SIZE / 4;
+    constexpr int K_LOADS = HD * T::SIZE / 64, V_WORDS = DPL * T::SIZE / 4, KNOWN = 64 / TILES;
     __shared__ float o_s[WAVES][16][PITCH];
     __shared__ float2 ml_s[WAVES][16];
     const PagesArgs& p = a.p;
@@ -273,15 +266,16 @@ __global__ void __launch_bounds__(64 * WAVES, 2) paged_attn_kernel(PagedAttnArgs
     const bool only = t.n == 1;
     bool bad = t.given != len;
 
-    // Pages of the wavefront's tiles: lane i has those of tile i % TILES of its block i / TILES.
+    // Pages of the wavefront's tiles, of KNOWN blocks at a time: lane i has those of tile i % TILES of the block i / TILES behind the first of them.
     const int first = from + wave * KEYS, blocks = (to - first + STEP - 1) / STEP;
     int pages = -1;
-    {
-        const int key = first + lane / TILES * STEP + 16 * (lane % TILES);
-        if (key < min(from + t.rows, p.max_ctx)) pages = page_of(p, b, key);      // (without waiting for the length)
+    auto find_pages = [&](int block, int lane) {
+        const int key = first + (block + lane / TILES) * STEP + 16 * (lane % TILES);
+        pages = key < min(from + t.rows, p.max_ctx) ? page_of(p, b, key) : -1;      // (the first ones without waiting for the length)
         bad |= key < to && pages < 0;
         if (key >= to) pages = -1;
-    }
+    };
+    find_pages(0, lane);
     const int rows = a.n_new * a.group, row0 = tile * 16 * NT;
     const int least = len - (a.n_new - 1 - min(row0, rows - 1) / a.group);      // what all columns see
     int limit[NT];                                           // the column's token sees the rows before it
@@ -299,7 +293,7 @@ __global__ void __launch_bounds__(64 * WAVES, 2) paged_attn_kernel(PagedAttnArgs
     words_t vr[TILES][4][V_PARTS];
     f32x4_t ks[T::CODES ? TILES : 1], vs[T::CODES ? TILES : 1];
     auto row_of = [&](int block, int c) {                    // first row of a tile; of pages that are none, any
-        const int page = __builtin_amdgcn_readlane(pages, block * TILES + c);
+        const int page = __builtin_amdgcn_readlane(pages, block % KNOWN * TILES + c);
         return row_in_pages(p, max(page, 0), kvh, first + block * STEP + 16 * c);
     };
     auto load_keys = [&](int block) {
@@ -348,7 +342,7 @@ __global__ void __launch_bounds__(64 * WAVES, 2) paged_attn_kernel(PagedAttnArgs
 #pragma unroll
         for (int i = 0; i < DT; ++i) o[u][i] = (f32x4_t){0.f, 0.f, 0.f, 0.f};
     }
-    const bool whole = !__any(bad);
+    bool whole = !__any(bad);
     auto add_block = [&](auto last_c, int block) __attribute__((always_inline)) {
         constexpr bool LAST = decltype(last_c)::value;
         const int k0 = first + block * STEP;
@@ -401,7 +395,7 @@ __global__ void __launch_bounds__(64 * WAVES, 2) paged_attn_kernel(PagedAttnArgs
             for (int u = 0; u < NT; ++u) mine[u] = 0;
 #pragma unroll
             for (int c = 0; c < TILES; ++c) {
-                const bool here = __builtin_amdgcn_readlane(pages, block * TILES + c) >= 0;
+                const bool here = __builtin_amdgcn_readlane(pages, block % KNOWN * TILES + c) >= 0;
 #pragma unroll
                 for (int r = 0; r < 4; ++r) {
                     const int j = k0 + 16 * c + 4 * g + r;
@@ -415,7 +409,15 @@ __global__ void __launch_bounds__(64 * WAVES, 2) paged_attn_kernel(PagedAttnArgs
             }
         }
         __builtin_amdgcn_sched_barrier(0);
-        if constexpr (!LAST) load_keys(block + 1);
+        if constexpr (!LAST) {
+            if ((block + 1) % KNOWN == 0) {
+                uint32_t all = ~0u;
+                asm volatile("" : "+s"(all));                // (the lane's number is counted again: kept, with what follows from it, it takes registers of every block)
+                find_pages(block + 1, __builtin_amdgcn_mbcnt_hi(all, __builtin_amdgcn_mbcnt_lo(all, 0)));
+                whole = !__any(bad);
+            }
+            load_keys(block + 1);
+        }
         __builtin_amdgcn_sched_barrier(0);
         float top[NT];
         bool above = false;

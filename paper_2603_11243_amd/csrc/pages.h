@@ -45,12 +45,12 @@ struct PagedAttnArgs {
     bool codes;                              // pages of an 8-bit type
     int32_t tile_rows, tiles;                // query rows of a K/V head, tokens times group, in tiles of 16 or 32
     // Contexts are cut into pieces of whole PAGED_UNITs of rows: shared 0, each by itself every PAGED_MOST units, n_pieces of max_ctx rows; else all of a K/V head
-    // and tile into about `shared` equal ones (or the smallest multiple of it that has none longer than PAGED_MOST), at most n_pieces.
+    // and tile into about `shared` equal ones, at most n_pieces.
     int32_t shared, n_pieces;
     float* part_o; float2* part_ml;          // [piece (of an utterance with shared 0: utterance, piece)][query row of tile and K/V head]: mean of 64 or 128 values; (maximum to base 2, sum)
     int2* first;                             // [utterance] first piece, pieces
 };
-constexpr int PAGED_UNIT = 128, PAGED_MOST = 32;             // a round of four wavefronts of 32 rows; units of a piece, of which a wavefront has the page numbers in a register
+constexpr int PAGED_UNIT = 128, PAGED_MOST = 32;             // a round of four wavefronts of 32 rows; units of an unshared piece: a wavefront has the page numbers of so many in a register
 constexpr int64_t PAGED_QUERIES = 1 << 21;                   // of a call: workgroups of up to 1024 threads that join their pieces
 constexpr int PAGED_UTTS = 1024;                             // utterances of a batch that shares
 inline int paged_dims(int head_dim) { return head_dim > 64 ? 128 : 64; }

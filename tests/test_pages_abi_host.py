@@ -182,3 +182,16 @@ def test_no_call_without_flags(lib, ctx):  # noqa: F811
     assert both(lib, ctx) == -4 and b"flags" in lib.ssd_last_error(ctx)
     flags = C.c_int32(7)
     assert lib.ssd_device_flags(ctx, C.byref(flags)) == 0 and flags.value == 0
+
+
+@pytest.mark.parametrize("B, H, G, new", [(64, 8, 2, 1), (1, 8, 3, 9), (1024, 2, 1, 1), (20, 1, 64, 4)])
+def test_shared_pieces_do_not_grow_with_the_table(lib, ctx, B, H, G, new):  # noqa: F811
+    """What a call needs, and so what it launches, is by its utterances and heads: the same for tables of 2^16 rows an utterance and of 2^24."""
+    import re
+    need = []
+    for bits in (16, 20, 24):
+        rc = attention(lib, ctx, q=1 << 50, out=1 << 52, hq=H * G, q_stride=H * G * 128, n_new=new, p=pages(H=H, R=64), t=table(B=B, max_ctx=1 << bits, stride=1 << bits))
+        assert rc == EWORKSPACE
+        need.append(int(re.search(rb"workspace of (\d+) bytes", lib.ssd_last_error(ctx)).group(1)))
+        assert need[-1] <= lib.ssd_paged_workspace_bytes(ctx, H * G, H, 128, B, new, 1 << bits) < (64 << 20) + 8 * 1024 * B * new * H * G
+    assert need[0] == need[1] == need[2]

@@ -11,6 +11,7 @@ in host memory between the two.  `TwoPhaseDecoder.run` is that schedule:
             host memory and nothing else of phase 1 is kept; mode "resident": the K/V cache of phase 1 stays in HBM
             (what 288 GB make possible: a 50K-token batch of the 1B-class decoder is 4.9 GB of keys and values); mode
             "paged": the cache holds one bin, and behind each bin the rows of its rejected utterances go to pages, in 8 bits or as they are
+            (which utterances those are is known on the device only: there are pages for the rows of all that are verified)
   phase 2   fallback bins planned on context length + steps of the rejected utterances; per bin, "offload" reloads g,
             re-runs the prompt [g; prompt; accepted prefix + the rejected token] with verify_forward_kv (whose greedy
             token at the rejected position is the first fallback token) and then ar_fallback; "resident" calls
@@ -193,19 +194,26 @@ class TwoPhaseDecoder:
             lists[b, :n] = np.arange(at, at + n)
         return lists
 
-    def _to_pages(self, lists, utts, start, most, acc):
-        """The rows of a bin's rejected utterances, up to the end of their accepted prefixes, to their pages; lengths stay on the device."""
-        dev = self.ctx.device
-        k, v = self.ctx.kv_tensors()
-        length = torch.from_numpy((self.S + self.P)[utts].astype(np.int32)).to(dev) + acc["accept_len"]
-        moved = torch.where(acc["all_accepted"].bool(), 0, length).to(torch.int32)
-        self.ctx.kv_write_pages(self.pages, torch.from_numpy(lists[utts]).to(dev), length, k, v, start=torch.from_numpy(start).to(dev), n_rows=moved, max_rows=most, max_ctx=most)
+    def _starts(self, bins, rows):
+        """First slots of the utterances of each bin, `room` behind the rows of each."""
+        return [np.concatenate([[0], np.cumsum(rows[utts] + self.room)[:-1]]).astype(np.int32) for utts in bins]
 
-    def _from_pages(self, lists, utts, start, length):
-        k, v = self.ctx.kv_tensors()
-        n = torch.from_numpy(length).to(self.ctx.device)
-        self.ctx.kv_read_pages(self.pages, torch.from_numpy(lists[utts]).to(self.ctx.device), n, k, v, start=torch.from_numpy(start).to(self.ctx.device), n_rows=n,
-                               max_rows=int(length.max()), max_ctx=int(length.max()))
+    def _on_device(self, lists, bins, starts, rows):
+        """(page lists, first slots, rows) of every bin.  One upload of each for all bins, while the stream has no work: a copy waits for what is queued before it."""
+        utts, ends = np.concatenate(bins), np.cumsum([len(b) for b in bins])[:-1].tolist()
+        parts = (torch.from_numpy(x).to(self.ctx.device).tensor_split(ends) for x in (lists[utts], np.concatenate(starts), rows[utts].astype(np.int32)))
+        return list(zip(*parts))
+
+    def _to_pages(self, place, most, acc):
+        """The rows of a bin's rejected utterances, up to the end of their accepted prefixes, to their pages; lengths stay on the device."""
+        (lists, start, before), (k, v) = place, self.ctx.kv_tensors()
+        length = before + acc["accept_len"]
+        moved = torch.where(acc["all_accepted"].bool(), 0, length).to(torch.int32)
+        self.ctx.kv_write_pages(self.pages, lists, length, k, v, start=start, n_rows=moved, max_rows=most, max_ctx=most)
+
+    def _from_pages(self, place, most):
+        (lists, start, length), (k, v) = place, self.ctx.kv_tensors()
+        self.ctx.kv_read_pages(self.pages, lists, length, k, v, start=start, n_rows=length, max_rows=most, max_ctx=most)
 
     def run(self, tau_slm: float) -> dict:
         with torch.cuda.stream(self.ctx.stream):             # what is copied to the host waits for the calls before it, whichever stream is current
@@ -227,21 +235,23 @@ class TwoPhaseDecoder:
         n_rows = (self.S + self.P + draft_len)[fail]
         bins = [fail[b] for b in self._bins(n_rows)]
         res["verify_bins"] = len(bins)
-        lists = self._page_lists(fail, n_rows) if self.mode == "paged" else None
+        if self.mode == "paged":
+            lists, starts = self._page_lists(fail, n_rows), self._starts(bins, self.S + self.P + draft_len)
+            places = self._on_device(lists, bins, starts, self.S + self.P)
         kv_next = 0
         kv_start = np.zeros(self.B, np.int32)
         pending = []
         off = 0                                                # draft positions handed out so far
         goff = np.zeros(self.B, np.int64)                      # where an utterance's draft starts in logp_all / greedy_all
-        for utts in bins:
+        for i, utts in enumerate(bins):
             sel = ctx.select_unconfident(utts, self.cu_frames, draft_len, g["draft_ctc"], self.table, self.speech_all,
                                          self.cu_s, self.prompt_all, self.cu_p, out=self.sel_buf)
             Mv = int(sel["cu_draft"][-1])
             ks = None
-            if self.mode != "offload":
+            if self.mode == "paged":
+                ks = starts[i]
+            elif self.mode == "resident":
                 cap = (self.S + self.P + draft_len)[utts] + self.room
-                if self.mode == "paged":
-                    kv_next = 0
                 ks = (kv_next + np.concatenate([[0], np.cumsum(cap)[:-1]])).astype(np.int32)
                 kv_start[utts] = ks
                 kv_next += int(cap.sum())
@@ -252,7 +262,7 @@ class TwoPhaseDecoder:
                                          "accept_len": torch.empty(len(utts), dtype=torch.int32, device=ctx.device),
                                          "all_accepted": torch.empty(len(utts), dtype=torch.uint8, device=ctx.device)})
             if self.mode == "paged":
-                self._to_pages(lists, utts, ks, int((self.S + self.P + draft_len)[utts].max()), acc)
+                self._to_pages(places[i], int((self.S + self.P + draft_len)[utts].max()), acc)
             goff[utts] = off + sel["cu_draft"][:-1]
             off += Mv
             pending.append((utts, acc))
@@ -277,15 +287,17 @@ class TwoPhaseDecoder:
         fb_bins = [rej[b] for b in self._bins((ctx_len_all[rej] + n_steps + 2).astype(np.int32))]
         res["fallback_bins"] = len(fb_bins)
         outs = []
-        for utts in fb_bins:
+        if self.mode == "paged":
+            starts = self._starts(fb_bins, ctx_len_all)
+            places = self._on_device(lists, fb_bins, starts, ctx_len_all)
+        for i, utts in enumerate(fb_bins):
             if self.mode != "offload":
                 # the first fallback token is the model's own choice at the first rejected position
                 first = ctx.gather_i32(self.greedy_all, goff[utts] + A[utts])
                 ks, cl = kv_start[utts], ctx_len_all[utts]
                 if self.mode == "paged":
-                    cap = cl + self.room
-                    ks = np.concatenate([[0], np.cumsum(cap)[:-1]]).astype(np.int32)
-                    self._from_pages(lists, utts, ks, cl)
+                    ks = starts[i]
+                    self._from_pages(places[i], int(cl.max()))
             else:
                 # reload g, then re-run [g; prompt; accepted prefix + the rejected token] with the K/V cache on
                 S_u = self.S[utts]

@@ -67,3 +67,33 @@ def test_pages_with_trees_and_another_stream_current(trees):
     want, got = runs
     assert want["rejected"] > 0 and np.array_equal(got["accept_len"], want["accept_len"]) and set(got["tokens"]) == set(want["tokens"])
     assert all(np.array_equal(t, want["tokens"][b]) for b, t in got["tokens"].items())
+
+
+def test_no_wait_inside_a_phase(monkeypatch):
+    """Nothing between the bins of a phase waits for the stream: torch refuses copies that would while rows go to pages or come back."""
+    from paper_2603_11243_amd.binding import Context
+    from paper_2603_11243_amd.pipeline import TwoPhaseDecoder
+    wl = scaled_down(WORKLOADS["cfg3_1b_ragged64"], n_layers=2, B=24)
+    cb, table = make_ctc_batch(wl), make_ctc_to_llm_map(wl)
+    vi = make_verify_inputs(wl, cb.seconds, [np.zeros(0, np.int32)] * wl.B, device="cuda")
+    ctx = Context(wl.model, make_model_weights(wl.model, wl.seed, device="cuda"))
+    dec = TwoPhaseDecoder(ctx, wl, cb.logits.cuda(), cb.cu_frames, torch.from_numpy(table).cuda(), vi.speech_emb, vi.cu_speech, torch.from_numpy(vi.prompt_ids).cuda(), vi.cu_prompt,
+                          budget=1500, mode="paged", n_steps=5, page_rows=16)
+    calls = []
+
+    def watched(name):
+        call = getattr(dec, name)
+
+        def quiet(*args):
+            torch.cuda.set_sync_debug_mode("error")
+            try:
+                call(*args)
+            finally:
+                torch.cuda.set_sync_debug_mode("default")
+            calls.append(name)
+        monkeypatch.setattr(dec, name, quiet)
+    watched("_to_pages")
+    watched("_from_pages")
+    run = dec.run(_tau_for(wl))
+    assert calls.count("_to_pages") == run["verify_bins"] > 1 and calls.count("_from_pages") == run["fallback_bins"] > 0
+    ctx.close()

@@ -329,15 +329,19 @@ void alloc_gate_counters(ssd_ctx* c) {
     }
     (void)hipThreadExchangeStreamCaptureMode(&mode);
 }
-// Flags of a context without a model, which may never need them: the calls on pages refuse to run without.  Cleared on a stream of their own, since the context's
-// may be under capture.
+// Flags of a context without a model, which may never need them: the calls on pages refuse to run without.  While the context's stream is captured they are cleared on
+// one of their own (which takes 50 us).
 void alloc_page_flags(ssd_ctx* c) {
     hipStreamCaptureMode mode = hipStreamCaptureModeRelaxed;
     (void)hipThreadExchangeStreamCaptureMode(&mode);
     void* p = nullptr;
     hipStream_t own = nullptr;
-    if (hipMalloc(&p, 256) == hipSuccess && hipStreamCreateWithFlags(&own, hipStreamNonBlocking) == hipSuccess && hipMemsetAsync(p, 0, 256, own) == hipSuccess &&
-        hipStreamSynchronize(own) == hipSuccess) {
+    bool ok = hipMalloc(&p, 256) == hipSuccess;
+    if (!capturing(c->stream)) ok = ok && hipMemsetAsync(p, 0, 256, c->stream) == hipSuccess;
+    else
+        ok = ok && hipStreamCreateWithFlags(&own, hipStreamNonBlocking) == hipSuccess && hipMemsetAsync(p, 0, 256, own) == hipSuccess &&
+             hipStreamSynchronize(own) == hipSuccess;
+    if (ok) {
         c->owned.push_back(p);
         c->page_flags = static_cast<int32_t*>(p);
     } else {

@@ -517,9 +517,9 @@ size_t ssd_paged_workspace_bytes(const ssd_ctx *ctx, int n_q_heads, int n_kv_hea
  *   out     dev [B * n_new, n_q_heads * head_dim] of q_dtype, 16-byte aligned
  *   lse     dev [B * n_new, n_q_heads] fp32, or NULL; out and lse share no memory with each other, q or the pages
  * Scores, sums and statistics are fp32; 8-bit codes are exact operands.  A weight enters the second product as two values of 16 bits (22 bits of it with SSD_F16 pages, 16 with
- * others; three values, 24 bits, with 8-bit pages and SSD_F32 queries), with SSD_F32 pages as it is.  Outputs below 2^-90 lose bits.  With 8-bit pages q . k is formed of codes
- * before scales, and has to stay in fp32's range there: |q| up to 2^112 does.  A row that a token does not see, and what
- * lies behind the last row of a page, has no influence on it, whatever it holds; a value that it sees and that is not finite makes its column infinite or NaN.
+ * others; three values, 24 bits, with 8-bit pages and SSD_F32 queries), with SSD_F32 pages as it is.  Outputs below 2^-90 lose bits, with 8-bit pages those of rows whose
+ * largest magnitude is below 2^-66.  With 8-bit pages q . k is formed of codes before scales, and has to stay in fp32's range there: |q| up to 2^112 does.
+ * A row that a token does not see, and what lies behind the last row of a page, has no influence on it, whatever it holds; a value that it sees and that is not finite makes its column infinite or NaN.
  * SSD_F16 queries over 8-bit pages: a finite output that rounds beyond half is stored as +-65504 and raises SSD_FLAG_ACT_OVERFLOW, which one that is not finite raises too.
  * Captured calls use the workspace of the time of capture: two that share one must not run at the same time.  Every call repeats to the bit.
  * Errors: SSD_EINVAL, SSD_ESHAPE (B times tiles of 16 query rows of a K/V head more than 65535; more than 512 query heads a K/V

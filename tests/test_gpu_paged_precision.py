@@ -144,3 +144,24 @@ def test_infinities_of_half_pages_stay(n):
     assert (c.paged_attention(q, pool.pages(), pool.table, pool.ctx_len) == 65504).all()
     pool.parts["v"].fill_(float("inf"))
     assert not torch.isfinite(c.paged_attention(q, pool.pages(), pool.table, pool.ctx_len)).any() and c.device_flags() == 0
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("pair", [p for p in PAIRS if p[0] != "f16"])
+def test_small_values(pair):
+    """Values times a power of two: outputs times the same, down to where bits are lost (8-bit rows below 2^-66, others below 2^-90).  A part of a weight is held to
+    2^-134 at worst (half of bfloat16's smallest step) where the largest is 2^-32 times the row's scale, 2^-75 or more: n 2^-27 of the largest value."""
+    heads, n = (4, 2, 64), 300
+    pool, q = Pool(pair[1], heads[1:], [n, 50], 16), _queries(pair[0], 2, 1, heads)
+    c = _context(2, 1, heads, 320)
+    run = lambda: c.paged_attention(q, pool.pages(), pool.table, pool.ctx_len).double()
+    want, eight = run(), "v_scale" in pool.parts
+    top = [max(pool.rows(pool.value("v"), b)[0].max(), -pool.rows(pool.value("v"), b)[0].min()) for b in range(2)]
+    least = min(abs(pool.rows(pool.value("v"), b)[0]).max(-1).min() for b in range(2))
+    down = int(np.log2(least) + 66) if eight else 80
+    t = pool.parts["v_scale" if eight else "v"]
+    t.copy_((t.double() * 2.0 ** -down).to(t.dtype))
+    got = run() * 2.0 ** down
+    u = torch.finfo(q.dtype).eps
+    for b in range(2):
+        assert ((got[b] - want[b]).abs() <= n * 2.0 ** -27 * top[b] + u * want[b].abs()).all(), (pair, down)

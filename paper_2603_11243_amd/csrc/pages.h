@@ -57,12 +57,14 @@ inline int paged_dims(int head_dim) { return head_dim > 64 ? 128 : 64; }
 // Query rows of a workgroup.  32 read keys and values half as often as 16, which halves what long contexts cost, but are longer on their way through a block and fewer workgroups: by the
 // units of rows that workgroups of 16 would take.  Half, 12 tokens of 16 heads on 8 of 128, 16 and 32: 4 contexts of 150 to 300 rows 7.8 and 9.8 us, 1250 to 2500 (1280 units) 17.3 and
 // 17.9, 10000 to 20000 72 and 61; 40 of 30 to 60 (640) 10.3 and 9.6, 300 to 600 25 and 22, 2000 to 4000 195 and 115.  Codes of 64 dims, 7 tokens of 16 heads on 4: 40 contexts of 750
-// to 1500 (3840) 16.0 and 17.8, 2000 to 4000 (10240) 25.9 and 23.7.  fp32 pages of 64 dims 20.5 and 22.5 (1600), 43 and 36 (3840), of 128 120 and 148 (7680), 375 and 281 (20480);
+// to 1500 (3840) 16.0 and 17.8, 2000 to 4000 (10240) 25.9 and 23.7.  Of 128 dims, 12 tokens of 16 heads on 8, int8 and e4m3: 4 of 1250 to 2500 (1216) 14.5 and 16.1, 13.9 and 16.2; 8 of 500 to
+// 1000 (1024) 14.0 and 15.6, 12.5 and 15.2; 10 of 1000 to 2000 (2400) 20.7 and 19.1, 19.2 and 18.4; 40 of 2000 to 4000 (19840) 103 and 74, 99 and 71.  The units are those that the launch
+// is made for: one made for long contexts takes 32 over short ones too (40 of 30 to 60 rows 8.2 and 9.4, 9.4 and 9.2).  fp32 pages of 64 dims 20.5 and 22.5 (1600), 43 and 36 (3840), of 128 120 and 148 (7680), 375 and 281 (20480);
 // fp32 queries over codes have no registers for 32 (101 and 140).
 inline int paged_tile_rows(int64_t rows, int64_t B, int64_t n_kv_heads, int64_t max_ctx, int head_dim, int q_dtype, int pages_dtype) {
     const bool codes = pages_dtype == SSD_E4M3 || pages_dtype == SSD_I8, wide = paged_dims(head_dim) == 128;
     if (rows <= 16 || (codes && q_dtype == SSD_F32)) return 16;
-    const int64_t from = q_dtype == SSD_F32 ? (wide ? 15000 : 3000) : codes && !wide ? 8000 : 1000;
+    const int64_t from = q_dtype == SSD_F32 ? (wide ? 15000 : 3000) : codes && !wide ? 8000 : 2000;
     return B * n_kv_heads * ((rows + 15) / 16) * ((max_ctx + PAGED_UNIT - 1) / PAGED_UNIT) >= from ? 32 : 16;
 }
 // Workgroups of a CU whose registers fit; shared pieces are as many as run at once, and are held to so many a CU by the LDS they ask for.

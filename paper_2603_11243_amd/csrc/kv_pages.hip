@@ -1,9 +1,9 @@
 // Rows of a slot cache to pages and back, as they are or by 8-bit codes with a scale per row and head (definitions in ssd.h).  A workgroup takes consecutive rows of
 // an utterance (or of short ones side by side), HEADS heads of each: a thread finds its row's places once, requests the heads' values together and has 8 elements of each.
 // Four heads, or one where that makes few workgroups (64 rows of 8 heads of 128, half to e4m3: 3.9 and 3.3 us; 24 layers of 6 utterances of 200 to 400 rows, half to int8, with two
-// heads 80 us, four 58, eight 56; 2 layers of 65537 rows, bfloat16 to e4m3, 168, 149, 153; back from e4m3, 24 layers, 69, 57, 57).
-// Every row is read and written once, 16 bytes a load, past the caches (with ordinary loads and stores 63 and 155 us, and 24 layers of half as they are 80 for 69): what bounds it is
-// memory, at 4.7 TB/s for int8 and 5.4 for long runs of rows.
+// heads 81 us, four 59, eight 57; 2 layers of 65537 rows, bfloat16 to e4m3, 172, 157, 158; back from e4m3, 24 layers, 70, 58, 58).
+// Every row is read and written once, 16 bytes a load, past the caches (with ordinary loads and stores 24 layers to int8 take 64 us for 59, as they are 78 for 70, fp32 146 for 129; long runs
+// of rows 158 for 157): what bounds it is memory, at 4.7 TB/s for int8 and 5.2 for long runs of rows.
 #include <algorithm>
 
 #include "pages.h"

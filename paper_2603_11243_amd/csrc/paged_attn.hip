@@ -15,7 +15,8 @@
 // wavefront on the way (codes 8 KB; twice as many keys a block changed nothing over long contexts and cost 90 short ones of int8 15.5 -> 20 us).  Eight K/V heads of 128, two query
 // heads each: 200001 rows of bfloat16 144 us, 5.7 TB/s; four of 40000 rows of half 118 us (5.6), e4m3 66 (5.2), int8 67 (5.0); eight of 60000, e4m3, 179 (5.7).  Three workgroups a CU
 // were slower (four recordings of e4m3 60 against 54 us: fewer, fuller rounds).  A context of 106 rows is 5.1 us in a graph: a launch, and length, page numbers, keys and
-// merge one behind the other; every further block of a wavefront 1.3 us.  32 columns where that pays (paged_tile_rows): 27 rows over 16 contexts of int8 62 -> 50 us.
+// merge one behind the other; every further block of a wavefront 1.3 us.  32 columns where that pays (paged_tile_rows): 27 rows over 16 contexts of int8 62 -> 50 us;
+// with fp32 pages of 128 dims they spill 73 registers a lane and value loads wait for one another (12 tokens over 40 contexts of 2000 to 4000 rows 336 us, 201 by bytes), with 16-bit ones four.
 #include "pages.h"
 #include "tree_attn.h"
 
@@ -32,7 +33,7 @@ template <int QT, int PT> struct Kind {
     static constexpr int KEYS = CODES ? 32 : F32 ? 16 : 32, TILES = KEYS / 16;     // 64 registers a lane of keys and values in flight
     static constexpr bool QBF = CODES ? QT != SSD_F16 : BF;                  // the first product's operands: the queries' type, which holds the codes exactly
     static constexpr int QN = CODES && QT == SSD_F32 ? 3 : 1;                // 16-bit values that a query is the exact sum of
-    static constexpr int PN = QT == SSD_F32 ? 3 : 2;                         // those of a weight
+    static constexpr int PN = QT == SSD_F32 ? 3 : 2;                         // those of a weight: of outputs of 16 bits two, which hold it 2^9 (half: 2^6) times as exactly; a third cost 49.3 -> 52.5 us (16 contexts of int8)
     // Weights are taken times a power of two: in half's upper range, or so that sums of 2^30 values at the end of fp32's range stay in it.  A factor, not a term of the
     // exponent: there it would take five bits of the difference to the maximum.
     static constexpr float UNIT = PT == SSD_F16 ? 0x1p15f : 0x1p-32f;

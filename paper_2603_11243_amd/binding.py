@@ -274,8 +274,8 @@ class Context:
         self._lib = lib()
         self.device = torch.device(device)
         self.cfg = model_cfg
-        self._keep = []               # tensors whose storage the library reads in place, and workspaces of the time before
-        self._ws = None
+        self._keep = []               # tensors whose storage the library reads in place
+        self._ws, self._reserved = None, []           # the workspace; all that reserve allocated
         self._h = C.c_void_p()
         torch.cuda.set_device(self.device)
         self._index = torch.cuda.current_device()
@@ -349,14 +349,13 @@ class Context:
         if paged_utts:
             n = max(n, int(self._lib.ssd_paged_workspace_bytes(self._h, *paged_heads, paged_utts, paged_new, paged_ctx)))
         if self._ws is None or self._ws.numel() < n:
-            if self._ws is not None:
-                n = max(n, self._ws.numel() * 5 // 4)        # (all that are kept: five times the last at most)
-            self.set_workspace(torch.empty(n, dtype=torch.uint8, device=self.device))
+            last = self._reserved[-1].numel() if self._reserved else 0
+            if last < n:                                     # (all of them together: five times the last at most)
+                self._reserved.append(torch.empty(max(n, last * 5 // 4), dtype=torch.uint8, device=self.device))
+            self.set_workspace(self._reserved[-1])
 
     def set_workspace(self, buf: Optional[torch.Tensor]):
-        """buf is used from here on; the one before is kept as `reserve` says."""
-        if self._ws is not None and self._ws is not buf:
-            self._keep.append(self._ws)
+        """buf is used from here on, and held until the next; calls that were captured with it need it longer, which is the caller's to see to."""
         self._ws = buf
         self._check(self._lib.ssd_set_workspace(self._h, _ptr(buf), 0 if buf is None else buf.numel()))
 

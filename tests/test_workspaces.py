@@ -1,4 +1,4 @@
-"""A workspace that reserve or set_workspace replaces stays allocated while the context lives: captured calls use it at every replay."""
+"""Workspaces that reserve allocated stay while the context lives, since captured calls use them at every replay; a caller's own are the caller's."""
 import gc
 import weakref
 
@@ -28,7 +28,7 @@ class _Lib:
 def _context(monkeypatch):
     monkeypatch.setattr(binding, "_ptr", lambda t: None if t is None else t.data_ptr())
     c = binding.Context.__new__(binding.Context)
-    c._lib, c._h, c.device, c._keep, c._ws = _Lib(), 1, torch.device("cpu"), [], None
+    c._lib, c._h, c.device, c._ws, c._reserved = _Lib(), 1, torch.device("cpu"), None, []
     return c
 
 
@@ -39,12 +39,16 @@ def test_replaced_workspaces_live_as_long_as_the_context(monkeypatch):
         c.reserve()
         alive.append(weakref.ref(c._ws))
     assert c._lib.set == [1000, 3000, 3750]                  # one a quarter larger at least
-    own = torch.empty(10, dtype=torch.uint8)
-    c.set_workspace(own)
-    c.set_workspace(own)
-    c.set_workspace(None)
+    own = [torch.empty(10, dtype=torch.uint8) for _ in range(2)]
+    gone = [weakref.ref(t) for t in own]
+    for t in own + own + [None]:
+        c.set_workspace(t)
+    del own, t
     gc.collect()
-    assert all(w() is not None for w in alive) and len(c._keep) == 4
+    assert all(w() is not None for w in alive) and all(w() is None for w in gone)
+    c._lib.bytes = 100
+    c.reserve()
+    assert c._lib.set[-1] == 3750 and c._ws is alive[-1]()      # (the last one is large enough)
     del c
     gc.collect()
     assert all(w() is None for w in alive)
